@@ -29,7 +29,7 @@
  *     nothing is enqueued for it, but make that first call outside a stream capture.
  *   - Calls that use one context or one workspace are issued in stream order on one stream: the workspace
  *     (partial results, the counters of a merge) is shared by them.
- *   - All instances share one length t_cur per call.
+ *   - All instances share one length t_cur per call; the ap_cache_* calls take a length per instance.
  *   - Inputs must be finite; NaN scores give an unspecified (but in-range, duplicate-free) selection.
  */
 #ifndef ATTNPRED_H
@@ -266,6 +266,59 @@ int ap_offload_step(ap_ctx* ctx, float* hist, int64_t n_pushed, const void* q, c
                     float* out, int32_t* idx, int32_t* cnt, float* pred, float* pstate, int32_t pred_mode,
                     void* pool_K, void* pool_V, int32_t* block_table, int32_t* state, float* row, void* ws,
                     void* compute_stream, void* copy_stream);
+
+/* Caches whose instances have lengths of their own, for the layers and the baselines that do not go by a predicted selection: rows are
+ * appended, one new token or a chunk of them attends to the whole cache or to a window and the first rows, and caches beyond a budget
+ * lose the rows that gathered the least attention weight.  They use the context's n_inst, g, head_dim, block, t_cap, kv_dtype and block
+ * table; nothing of its history, predictor or selection, and no state is kept between calls.
+ *   K,V   as in ap_sparse_decode: device [n_inst][t_cap][d], or pools with ap_set_block_table.  The calls that write rows
+ *         (append, evict) need pages of an instance's own: a page that the table names twice is not to be written, and rows whose table
+ *         entry lies outside the pool are not written
+ *   len   device int32 [n_inst]: rows of each cache, the new tokens' included.  0 is an empty cache; values outside [0, t_cap] count
+ *         as the nearest one (ap_cache_append leaves out rows that would lie outside)
+ *   acc   device float [n_inst][t_cap]: the attention weight that each row gathered so far, over the heads of the group and all
+ *         queries.  Zero-filled by the caller before the first call
+ *   window, n_first  a token at position p sees the rows j <= p, with window > 0 only those with j > p - window or j < n_first; window
+ *         = 0 shows all.  Positions are places in the cache: rows that an eviction moved have their new ones
+ *   ws    device scratch of ap_cache_workspace_bytes; its contents carry nothing between calls, and calls that share one are issued in
+ *         stream order on one stream
+ * The lengths are read on the device only: a captured call follows lengths that change between replays. */
+
+/* Bytes of `ws` for ap_cache_decode and ap_cache_prefill of up to q_cap tokens an instance (q_cap = 0: decode only); weights: whether
+ * calls with acc are among them.  0 for arguments that no call would accept. */
+size_t ap_cache_workspace_bytes(const ap_ctx* ctx, int32_t q_cap, int32_t weights);
+
+/* Writes the new tokens' rows: row r of k_new[i] (r < n_new[i]) becomes row len[i] - n_new[i] + r of cache i.
+ *   k_new,v_new  device [n_inst][q_cap][d] kv dtype; rows from n_new[i] on are not read
+ *   n_new        device int32 [n_inst], clamped into [0, q_cap]; NULL: q_cap for all */
+int ap_cache_append(ap_ctx* ctx, const void* k_new, const void* v_new, const int32_t* n_new, int32_t q_cap, const int32_t* len,
+                    void* K, void* V, void* stream);
+
+/* Attention of the newest token of every cache (position len[i] - 1, whose row has been appended).
+ *   q    device [n_inst][g][d] kv dtype
+ *   out  device float [n_inst][g][d]; zero for an empty cache
+ *   acc  NULL, or the weights are added: acc[i][j] += sum over the g heads of the probability of row j, for the rows seen */
+int ap_cache_decode(ap_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* len, int32_t window, int32_t n_first,
+                    float* out, float* acc, void* ws, void* stream);
+
+/* Attention of the newest n_q[i] tokens of every cache, whose rows have been appended: query r lies at position len[i] - n_q[i] + r.
+ *   q    device [n_inst][q_cap][g][d] kv dtype
+ *   n_q  device int32 [n_inst], clamped into [0, q_cap]; NULL: q_cap for all
+ *   out  device [n_inst][q_cap][g][d] kv dtype (bf16 probabilities multiply bf16 rows, so more digits would not be real); rows from
+ *        n_q[i] on are left as they are.  A query before position 0 (n_q > len) sees nothing and has a zero output
+ *   acc  as in ap_cache_decode, summed over the queries too */
+int ap_cache_prefill(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
+                     int32_t window, int32_t n_first, void* out, float* acc, void* ws, void* stream);
+
+/* Brings every cache down to `budget` rows: its first n_first and last n_last stay, and of those between them the budget - n_first -
+ * n_last with the largest acc, equal ones by the lower index (-0 == +0).  The rows that stay keep their order and become rows
+ * 0 .. budget - 1 of K and V (in place) and of acc_out; rows behind them in K and V are left as they are, acc_out is 0 from there up
+ * to the old length.  Caches of at most `budget` rows stay as they are (acc_out receives their acc).
+ *   acc_out  device float [n_inst][t_cap], may be acc;  len_out  device int32 [n_inst], may be len
+ *   kept     device int32 [n_inst][budget]: the old index of every row that stayed, ascending; entries from len_out[i] on are left alone
+ * n_first + n_last <= budget <= t_cap.  NaN in acc: an unspecified choice, in range and without repeats. */
+int ap_cache_evict(ap_ctx* ctx, void* K, void* V, const float* acc, const int32_t* len, int32_t budget, int32_t n_first, int32_t n_last,
+                   float* acc_out, int32_t* len_out, int32_t* kept, void* stream);
 
 /* Measurement aids (no part of Algorithm 1): a streaming read of `bytes` bytes (multiple of 16) of
  * device memory with 16-byte non-temporal loads per lane, and a plain copy.  They give the read bandwidth the

@@ -23,7 +23,8 @@ AP_OK, AP_ERR_ARG, AP_ERR_ALIGN, AP_ERR_RANGE, AP_ERR_HIP, AP_ERR_UNSUPPORTED, A
 EXPORTS = [
     "ap_create", "ap_destroy", "ap_workspace_bytes", "ap_hist_slots", "ap_nb_cap", "ap_set_weights", "ap_score_offset", "ap_set_block_table",
     "ap_predict", "ap_predict_incremental", "ap_select_topk", "ap_refresh_selection", "ap_sparse_decode", "ap_sparse_decode_noalloc", "ap_calibrate", "ap_update_history", "ap_step",
-    "ap_prefetch_state_bytes", "ap_prefetch_blocks", "ap_append_kv", "ap_offload_begin", "ap_offload_step", "ap_stream_read", "ap_stream_copy", "ap_strerror",
+    "ap_prefetch_state_bytes", "ap_prefetch_blocks", "ap_append_kv", "ap_offload_begin", "ap_offload_step",
+    "ap_cache_workspace_bytes", "ap_cache_append", "ap_cache_decode", "ap_cache_prefill", "ap_cache_evict", "ap_stream_read", "ap_stream_copy", "ap_strerror",
 ]
 
 
@@ -81,13 +82,19 @@ def load_library() -> C.CDLL:
     lib.ap_offload_begin.argtypes = [vp, vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.ap_offload_step.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp,
                                     vp, vp, vp, vp]
+    lib.ap_cache_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.ap_cache_workspace_bytes.restype = sz
+    lib.ap_cache_append.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.ap_cache_decode.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.ap_cache_prefill.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.ap_cache_evict.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
     lib.ap_stream_read.argtypes = [vp, sz, vp, i32, vp]
     lib.ap_stream_copy.argtypes = [vp, sz, vp, i32, vp]
     lib.ap_strerror.argtypes = [C.c_int]
     lib.ap_strerror.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("ap_workspace_bytes", "ap_prefetch_state_bytes", "ap_hist_slots", "ap_nb_cap", "ap_strerror",
-                        "ap_score_offset"):
+                        "ap_score_offset", "ap_cache_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -102,6 +109,10 @@ def _ptr(t: torch.Tensor) -> int:
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("expected a contiguous device tensor")
     return t.data_ptr()
+
+
+def _optr(t):
+    return None if t is None else _ptr(t)
 
 
 def _rptr(t: torch.Tensor) -> int:
@@ -137,6 +148,7 @@ class Context:
         _check(lib.ap_create(C.byref(self.cfg), C.byref(h)))
         self._h = h
         self._lib = lib
+        self._n_phys = 0          # pages of the pool that the block table points into; 0: the contiguous layout
 
     def close(self):
         if getattr(self, "_h", None):
@@ -171,6 +183,7 @@ class Context:
     def set_block_table(self, table, n_phys_blocks: int = 0) -> None:
         """table: device int32 [n_inst][nb_cap] (kept alive by the caller), or None for the contiguous layout."""
         _check(self._lib.ap_set_block_table(self._h, None if table is None else _ptr(table), n_phys_blocks))
+        self._n_phys = 0 if table is None else n_phys_blocks
 
     def predict(self, hist, n_pushed, nb_cur, pred, ws) -> None:
         _check(self._lib.ap_predict(self._h, _ptr(hist), n_pushed, nb_cur, _ptr(pred), _ptr(ws), _stream()))
@@ -219,6 +232,82 @@ class Context:
     def append_kv(self, k_new, v_new, t_pos, table, state, pool_K, pool_V) -> None:
         _check(self._lib.ap_append_kv(self._h, _ptr(k_new), _ptr(v_new), t_pos, _ptr(table), _ptr(state), _ptr(pool_K),
                                       _ptr(pool_V), _stream()))
+
+    # -- caches whose instances have lengths of their own ---------------------------------------
+    def cache_workspace_bytes(self, q_cap: int = 0, weights: bool = False) -> int:
+        """Bytes of `ws` for cache_decode and cache_prefill of up to q_cap tokens; weights: with acc."""
+        return int(self._lib.ap_cache_workspace_bytes(self._h, q_cap, int(bool(weights))))
+
+    def _kv_type(self):
+        return torch.bfloat16 if self.cfg.kv_dtype == AP_BF16 else torch.float32
+
+    def _cache_args(self, K, V, length, **more):
+        """Checks types, shapes and devices of what a cache_* call is given; returns the device whose current stream it uses.
+        more: name -> (tensor or None, dtype, shape), a shape of None taken as it is."""
+        c = self.cfg
+        if K.shape != V.shape or K.shape[-1:] != (c.head_dim,) or K.dtype != self._kv_type() or V.dtype != K.dtype:
+            raise ValueError("K and V: two tensors [..., head_dim] of one shape, in the context's dtype")
+        rows = K.numel() // c.head_dim
+        if rows < (self._n_phys * c.block if self._n_phys else c.n_inst * c.t_cap):
+            raise ValueError("K and V: fewer rows than the context's caches, or than the pages of its pool")
+        more["len"] = (length, torch.int32, (c.n_inst,))
+        for name, (t, dtype, shape) in more.items():
+            if t is None:
+                continue
+            if t.dtype != dtype or tuple(t.shape) != shape:
+                raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+            if t.device != K.device:
+                raise ValueError(f"{name} lies on {t.device}, K on {K.device}")
+        if V.device != K.device:
+            raise ValueError("K and V lie on different devices")
+        return K.device
+
+    @staticmethod
+    def _cache_ws(ws, need, device):
+        if ws.device != device or ws.numel() * ws.element_size() < need:
+            raise ValueError(f"ws: expected {need} bytes on {device}")
+
+    def cache_append(self, k_new, v_new, n_new, length, K, V) -> None:
+        """k_new, v_new: [n_inst][q_cap][d]; n_new: int32 [n_inst] or None (q_cap each)."""
+        c, q_cap = self.cfg, k_new.shape[1] if k_new.dim() == 3 else 0
+        new = (c.n_inst, q_cap, c.head_dim)
+        dev = self._cache_args(K, V, length, k_new=(k_new, self._kv_type(), new), v_new=(v_new, self._kv_type(), new),
+                               n_new=(n_new, torch.int32, (c.n_inst,)))
+        with torch.cuda.device(dev):
+            _check(self._lib.ap_cache_append(self._h, _ptr(k_new), _ptr(v_new), _optr(n_new), q_cap, _ptr(length), _ptr(K), _ptr(V),
+                                             _stream()))
+
+    def cache_decode(self, q, K, V, length, window, n_first, out, acc, ws) -> None:
+        """q: [n_inst][g][d]; out: float [n_inst][g][d]; acc: float [n_inst][t_cap] or None."""
+        c = self.cfg
+        shape = (c.n_inst, c.g, c.head_dim)
+        dev = self._cache_args(K, V, length, q=(q, self._kv_type(), shape), out=(out, torch.float32, shape),
+                               acc=(acc, torch.float32, (c.n_inst, c.t_cap)))
+        self._cache_ws(ws, self.cache_workspace_bytes(0, acc is not None), dev)
+        with torch.cuda.device(dev):
+            _check(self._lib.ap_cache_decode(self._h, _ptr(q), _ptr(K), _ptr(V), _ptr(length), window, n_first, _ptr(out), _optr(acc),
+                                             _ptr(ws), _stream()))
+
+    def cache_prefill(self, q, n_q, K, V, length, window, n_first, out, acc, ws) -> None:
+        """q: [n_inst][q_cap][g][d]; n_q: int32 [n_inst] or None (q_cap each); out: as q; acc: float [n_inst][t_cap] or None."""
+        c, q_cap = self.cfg, q.shape[1] if q.dim() == 4 else 0
+        shape = (c.n_inst, q_cap, c.g, c.head_dim)
+        dev = self._cache_args(K, V, length, q=(q, self._kv_type(), shape), out=(out, self._kv_type(), shape),
+                               n_q=(n_q, torch.int32, (c.n_inst,)), acc=(acc, torch.float32, (c.n_inst, c.t_cap)))
+        self._cache_ws(ws, self.cache_workspace_bytes(q_cap, acc is not None), dev)
+        with torch.cuda.device(dev):
+            _check(self._lib.ap_cache_prefill(self._h, _ptr(q), _optr(n_q), q_cap, _ptr(K), _ptr(V), _ptr(length), window, n_first,
+                                              _ptr(out), _optr(acc), _ptr(ws), _stream()))
+
+    def cache_evict(self, K, V, acc, length, budget, n_first, n_last, acc_out, len_out, kept) -> None:
+        """acc_out may be acc, len_out may be length; kept: int32 [n_inst][budget]."""
+        c = self.cfg
+        rows = (c.n_inst, c.t_cap)
+        dev = self._cache_args(K, V, length, acc=(acc, torch.float32, rows), acc_out=(acc_out, torch.float32, rows),
+                               len_out=(len_out, torch.int32, (c.n_inst,)), kept=(kept, torch.int32, (c.n_inst, budget)))
+        with torch.cuda.device(dev):
+            _check(self._lib.ap_cache_evict(self._h, _ptr(K), _ptr(V), _ptr(acc), _ptr(length), budget, n_first, n_last, _ptr(acc_out),
+                                            _ptr(len_out), _ptr(kept), _stream()))
 
     def update_history(self, hist, n_pushed, row) -> None:
         _check(self._lib.ap_update_history(self._h, _ptr(hist), n_pushed, _ptr(row), _stream()))

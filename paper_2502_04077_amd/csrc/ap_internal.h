@@ -182,3 +182,14 @@ size_t sparse_ws_floats(const Shape& s);
 hipError_t static_scratch(float** ptr, size_t* bytes);
 
 }  // namespace ap
+
+struct ap_ctx {
+  ap::Shape s;
+  float* dweights;      // device copy of the re-packed predictor weights, owned
+  bool have_weights;
+  double score_offset;  // P0: what the predictor answers to an all-zero history (pred is relative to it)
+  // ap_offload_*: "selection for the next token is written" / "its blocks are staged"; created on first use, owned
+  hipEvent_t ev_selected, ev_staged;
+  bool have_events;
+  ap::Occupancy occ;         // what the device holds at once; s.occ points here
+};

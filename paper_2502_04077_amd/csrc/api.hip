@@ -6,17 +6,6 @@
 
 #include "ap_internal.h"
 
-struct ap_ctx {
-  ap::Shape s;
-  float* dweights;      // device copy of the re-packed predictor weights, owned
-  bool have_weights;
-  double score_offset;  // P0: what the predictor answers to an all-zero history (pred is relative to it)
-  // ap_offload_*: "selection for the next token is written" / "its blocks are staged"; created on first use, owned
-  hipEvent_t ev_selected, ev_staged;
-  bool have_events;
-  ap::Occupancy occ;         // what the device holds at once; s.occ points here
-};
-
 namespace ap {
 
 static size_t align4(size_t x) { return (x + 3) & ~(size_t)3; }

@@ -1,0 +1,366 @@
+// Attention of one new token per instance over a cache of the instance's own length, the whole of it or a window and the first rows.
+//
+//   s_hj = q_h . K_j / sqrt(d),  m_h = max_j s_hj,  P_hj = exp(s_hj - m_h) / sum_j exp(s_hj - m_h),  out_h = sum_j P_hj V_j,
+//   acc_j += sum_h P_hj,  over the rows j that the token at position L - 1 sees.
+//
+// Memory-bound: 2 d sizeof(T) bytes a row and 4 g d operations on them.  Lengths differ, so the rows are not dealt by instance: the rows
+// seen by all instances, in groups of 16 and in the instances' order, are cut into equal shares, one a workgroup, and every
+// workgroup finds out from the lengths where its share begins.  A workgroup that goes over a whole instance writes its output; the
+// pieces of the others are joined by a second launch.
+#include "cache_body.h"
+
+namespace ap {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4, kGroup = 16;
+constexpr int kLeastGroups = 8;      // least share of a workgroup: two passes a wave
+
+// The rows that an instance's new token sees: [0, f) and [lo, L), f <= lo; in groups of 16 rows: gs groups from 0 on, the others from gb.
+struct Seen {
+  int L, lo, f, gs, gb, n;
+  __device__ __forceinline__ int group(int u) const { return u < gs ? u : gb + (u - gs); }
+  __device__ __forceinline__ bool row(int j) const { return j < L && (j >= lo || j < f); }
+};
+__device__ __forceinline__ Seen seen_of(int len, int t_cap, int window, int n_first) {
+  Seen s;
+  s.L = clamped(len, 0, t_cap);
+  s.lo = window > 0 && s.L > window ? s.L - window : 0;
+  s.f = n_first < s.lo ? n_first : s.lo;
+  s.gs = (s.f + kGroup - 1) / kGroup;
+  s.gb = s.lo / kGroup > s.gs ? s.lo / kGroup : s.gs;
+  s.n = s.L == 0 ? 0 : s.gs + (s.L - 1) / kGroup - s.gb + 1;
+  return s;
+}
+
+__device__ __forceinline__ unsigned long long share_of(unsigned long long groups) {
+  const unsigned long long per = (groups + kCacheDecodeWgs - 1) / kCacheDecodeWgs;
+  return per > kLeastGroups ? per : kLeastGroups;
+}
+
+template <typename T, int D, int G> struct Form {
+  static constexpr int E = 16 / (int)sizeof(T);            // elements of a 16-byte piece
+  static constexpr int PIECES = D / E;                     // pieces of a row = lanes that read a V row
+  static constexpr int KL = PIECES / 4;                    // loads of a K group: lane (m, kg) has piece 4 l + kg of row m
+  static constexpr int RPL = kWave / PIECES;               // V rows a load
+  static constexpr int VL = kGroup / RPL;                  // loads of a V group
+};
+
+// One group's K and V pieces of a lane.
+template <typename T, int D, int G> struct Rows {
+  u32x4 k[Form<T, D, G>::KL], v[Form<T, D, G>::VL];
+};
+
+template <typename T, int D, int G>
+__device__ __forceinline__ void load_group(const DecodeArgs& a, int inst, const Seen& s, int grp, int lane, Rows<T, D, G>& x) {
+  using F = Form<T, D, G>;
+  const int t0 = grp * kGroup;
+  // Rows that are not seen are not read: their lanes read a row of the group that is.
+  const int other = t0 < s.f ? t0 : (t0 > s.lo ? t0 : s.lo);
+  const u32x4* K = static_cast<const u32x4*>(a.K);
+  const u32x4* V = static_cast<const u32x4*>(a.V);
+  {
+    const int j = t0 + (lane & 15);
+    const size_t at = row_at(a.r, inst, s.row(j) ? j : other) * F::PIECES + (lane >> 4);
+#pragma unroll
+    for (int l = 0; l < F::KL; ++l) x.k[l] = K[at + 4 * l];
+  }
+#pragma unroll
+  for (int l = 0; l < F::VL; ++l) {
+    const int j = t0 + l * F::RPL + lane / F::PIECES;
+    x.v[l] = V[row_at(a.r, inst, s.row(j) ? j : other) * F::PIECES + lane % F::PIECES];
+  }
+}
+
+template <typename T, int D, int G, bool ACC>
+__global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
+  using F = Form<T, D, G>;
+  __shared__ __attribute__((aligned(16))) float s_out[kWaves][G][D];
+  __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
+  __shared__ float s_ml[kWaves][G][2];
+  __shared__ unsigned long long s_wave[kWaves];
+  __shared__ int s_inst, s_from;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int head = lane & 15, kg = lane >> 4;
+
+  // Where this workgroup's share begins: every thread sums the groups of consecutive instances.
+  const int chunk = (a.r.n_inst + kThreads - 1) / kThreads;
+  const int i_begin = tid * chunk < a.r.n_inst ? tid * chunk : a.r.n_inst;
+  const int i_end = i_begin + chunk < a.r.n_inst ? i_begin + chunk : a.r.n_inst;
+  unsigned long long mine = 0;
+  for (int i = i_begin; i < i_end; ++i) mine += (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+  unsigned long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long y = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) s_wave[wave] = upto;
+  if (tid == 0) s_inst = -1;
+  __syncthreads();
+  unsigned long long groups = 0, ahead = upto - mine;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) ahead += s_wave[w];
+    groups += s_wave[w];
+  }
+  const unsigned long long per = share_of(groups), begin = (unsigned long long)blockIdx.x * per;
+  const unsigned long long end = begin + per < groups ? begin + per : groups;
+  if (blockIdx.x == 0) {
+    unsigned long long at = ahead;
+    for (int i = i_begin; i < i_end; ++i) {
+      a.before[i] = at;
+      at += (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+    }
+    if (tid == kThreads - 1) a.before[a.r.n_inst] = groups;
+  }
+  if (begin >= end) return;
+  if (ahead <= begin && begin < ahead + mine) {
+    unsigned long long at = ahead;
+    for (int i = i_begin; i < i_end; ++i) {
+      const unsigned n = (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+      if (begin < at + n) {
+        s_inst = i;
+        s_from = (int)(begin - at);
+        break;
+      }
+      at += n;
+    }
+  }
+  __syncthreads();
+  int inst = s_inst, from = s_from;
+  unsigned long long left = end - begin;
+
+  const float scale = kLog2E / sqrtf((float)D);
+  for (; left > 0; ++inst, from = 0) {
+    const Seen s = seen_of(a.r.len[inst], a.r.t_cap, a.window, a.n_first);
+    if (s.n <= from) continue;                             // an empty instance
+    const int to = (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
+    left -= (unsigned)(to - from);
+
+    // B operand of the products q . K: lane (head, kg) has piece 4 l + kg of the head's query; heads beyond g are zero.
+    u32x4 qf[F::KL];
+#pragma unroll
+    for (int l = 0; l < F::KL; ++l) {
+      const u32x4 zero = {0u, 0u, 0u, 0u};
+      qf[l] = head < G ? static_cast<const u32x4*>(a.q)[((size_t)inst * G + head) * F::PIECES + 4 * l + kg] : zero;
+    }
+    float m = -INFINITY, sum = 0.f;                        // of head `head`; the sum over this lane's rows
+    float o[G][F::E];
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+#pragma unroll
+      for (int e = 0; e < F::E; ++e) o[h][e] = 0.f;
+
+    Rows<T, D, G> next;
+    int u = from + wave;
+    if (u < to) load_group<T, D, G>(a, inst, s, s.group(u), lane, next);
+    for (; u < to; u += kWaves) {
+      const Rows<T, D, G> x = next;
+      const int t0 = s.group(u) * kGroup;
+      if (u + kWaves < to) load_group<T, D, G>(a, inst, s, s.group(u + kWaves), lane, next);
+      float4v c = {0.f, 0.f, 0.f, 0.f};                    // rows t0 + 4 kg + r of head `head`
+#pragma unroll
+      for (int l = 0; l < F::KL; ++l) {
+        if constexpr (sizeof(T) == 2) {
+          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[l]), __builtin_bit_cast(bf16x8, qf[l]), c, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[l][e]), __uint_as_float(qf[l][e]), c, 0, 0, 0);
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (!s.row(t0 + 4 * kg + r)) c[r] = -INFINITY;
+        top = fmaxf(top, c[r]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      // The reference is a whole number in units of log2: changing it multiplies by a power of two and rounds nothing, and the exponent
+      // is one fused multiply-add.
+      const float ref = fmaxf(m, ceilf(top * scale));
+      if (__any(ref != m)) {
+        const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
+        sum *= shrink;
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+          const float f = __shfl(shrink, h, 64);
+#pragma unroll
+          for (int e = 0; e < F::E; ++e) o[h][e] *= f;
+        }
+        m = ref;
+      }
+      if (ACC && head < G && t0 + 4 * kg < a.r.t_cap) {    // (t_cap is a multiple of 8: four rows are within it or not)
+        float4v z;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[r] = c[r];
+        *reinterpret_cast<float4v*>(a.logits + ((size_t)inst * G + head) * a.r.t_cap + t0 + 4 * kg) = z;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = exp2_fast(__builtin_fmaf(c[r], scale, -m));
+        sum += p;
+        if (head < G) s_p[wave][4 * kg + r][head] = p;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int l = 0; l < F::VL; ++l) {
+        float v[F::E];
+        unpack16(make_uint4(x.v[l].x, x.v[l].y, x.v[l].z, x.v[l].w), v, T{});
+        const float* p = s_p[wave][l * F::RPL + lane / F::PIECES];
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int e = 0; e < F::E; ++e) o[h][e] = __builtin_fmaf(p[h], v[e], o[h][e]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+
+    // The wave's lanes, then the workgroup's waves.
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+#pragma unroll
+    for (int x = F::PIECES; x < 64; x <<= 1)
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int e = 0; e < F::E; ++e) o[h][e] += __shfl_xor(o[h][e], x, 64);
+    if (lane < F::PIECES) {
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int e = 0; e < F::E; ++e) s_out[wave][h][lane * F::E + e] = o[h][e];
+    }
+    if (lane < G) {
+      s_ml[wave][lane][0] = m;
+      s_ml[wave][lane][1] = sum;
+    }
+    __syncthreads();
+    const bool whole = from == 0 && to == s.n;
+    const size_t slot = 2 * (size_t)blockIdx.x + (from == 0 ? 1 : 0);   // the piece an instance begins with is its workgroup's last
+    for (int x = tid; x < G * D; x += kThreads) {
+      const int h = x / D, e = x % D;
+      float top = s_ml[0][h][0];
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_ml[w][h][0]);
+      float all = 0.f, val = 0.f;
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2_fast(s_ml[w][h][0] - top);
+        all += f * s_ml[w][h][1];
+        val += f * s_out[w][h][e];
+      }
+      if (whole) a.out[((size_t)inst * G + h) * D + e] = val / all;
+      else a.part_acc[(slot * G + h) * D + e] = val;
+      if (e == 0) {
+        float* ml = whole ? a.whole + ((size_t)inst * G + h) * 2 : a.part_ml + (slot * G + h) * 2;
+        ml[0] = top;
+        ml[1] = all;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the pieces of instances that several workgroups went over, and adds the weights.  Workgroup (0, instance) has the output,
+// workgroup (1 + x, instance) the weights of 1024 rows.
+template <int G>
+__global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int D) {
+  __shared__ float s_f[kCacheDecodeWgs + 1][G];            // factors of the pieces
+  __shared__ float s_m[G], s_inv[G];
+  const int i = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Seen s = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first);
+  const float scale = kLog2E / sqrtf((float)D);
+  if (s.n == 0) {
+    if (blockIdx.x == 0)
+      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
+    return;
+  }
+  const int j0 = ((int)blockIdx.x - 1) * 4 * kThreads;
+  if (blockIdx.x > 0 && (j0 >= s.L || (j0 >= s.f && j0 + 4 * kThreads <= s.lo))) return;
+  const unsigned long long at = a.before[i], per = share_of(a.before[a.r.n_inst]);
+  const int w0 = (int)(at / per), parts = (int)((at + (unsigned)s.n - 1) / per) - w0 + 1;
+  if (blockIdx.x == 0 && parts == 1) return;
+  auto slot = [&](int p) { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };
+  if (parts == 1) {
+    if (tid < G) {
+      s_m[tid] = a.whole[((size_t)i * G + tid) * 2];
+      s_inv[tid] = 1.f / a.whole[((size_t)i * G + tid) * 2 + 1];
+    }
+  } else {
+    for (int h = wave; h < G; h += kWaves) {
+      float top = -INFINITY;
+      for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[(slot(p) * G + h) * 2]);
+      top = wave_max(top);
+      float all = 0.f;
+      for (int p = lane; p < parts; p += 64) {
+        const float f = exp2_fast(a.part_ml[(slot(p) * G + h) * 2] - top);
+        s_f[p][h] = f;
+        all += f * a.part_ml[(slot(p) * G + h) * 2 + 1];
+      }
+      all = wave_sum(all);
+      if (lane == 0) {
+        s_m[h] = top;
+        s_inv[h] = 1.f / all;
+      }
+    }
+  }
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    for (int x = tid; x < G * D; x += kThreads) {
+      const int h = x / D;
+      float val = 0.f;
+      for (int p = 0; p < parts; ++p) val += s_f[p][h] * a.part_acc[slot(p) * G * D + x];
+      a.out[(size_t)i * G * D + x] = val * s_inv[h];
+    }
+    return;
+  }
+  const int j = j0 + 4 * tid;
+  if (j >= a.r.t_cap) return;
+  float add[4] = {0.f, 0.f, 0.f, 0.f};
+  if (j >= s.L || (j >= s.f && j + 4 <= s.lo)) return;
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    const float4v z = *reinterpret_cast<const float4v*>(a.logits + ((size_t)i * G + h) * a.r.t_cap + j);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) add[r] += exp2_fast(__builtin_fmaf(z[r], scale, -s_m[h])) * s_inv[h];
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (s.row(j + r)) a.acc[(size_t)i * a.r.t_cap + j + r] += add[r];
+}
+
+template <typename T, int D, int G> hipError_t run(const DecodeArgs& a, hipStream_t st) {
+  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true><<<kCacheDecodeWgs, kThreads, 0, st>>>(a);
+  else cache_decode_kernel<T, D, G, false><<<kCacheDecodeWgs, kThreads, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const unsigned columns = a.acc != nullptr ? (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads)) : 0;
+  cache_join_kernel<G><<<dim3(1 + columns, a.r.n_inst), kThreads, 0, st>>>(a, D);
+  return hipGetLastError();
+}
+template <typename T, int D> hipError_t run_g(int g, const DecodeArgs& a, hipStream_t st) {
+  return g == 1 ? run<T, D, 1>(a, st) : g == 2 ? run<T, D, 2>(a, st) : g == 4 ? run<T, D, 4>(a, st) : run<T, D, 8>(a, st);
+}
+
+}  // namespace
+
+CacheWs cache_decode_ws(const Shape& s, bool weights) {
+  CacheWs w;
+  size_t o = 0;
+  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
+  w.before = take(((size_t)s.n_inst + 1) * 8);
+  w.whole = take((size_t)s.n_inst * s.g * 2 * 4);
+  w.part_ml = take((size_t)2 * kCacheDecodeWgs * s.g * 2 * 4);
+  w.part_acc = take((size_t)2 * kCacheDecodeWgs * s.g * s.d * 4);
+  w.logits = take(weights ? (size_t)s.n_inst * s.g * s.t_cap * 4 : 0);
+  w.total = o;
+  return w;
+}
+
+hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& a, hipStream_t st) {
+  if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s.g, a, st) : run_g<bf16_t, 64>(s.g, a, st);
+  return s.d == 128 ? run_g<float, 128>(s.g, a, st) : run_g<float, 64>(s.g, a, st);
+}
+
+}  // namespace ap

@@ -1,0 +1,53 @@
+// Caches whose instances have lengths of their own: what the calls on them (cache_api.hip) hand to the kernels.
+#pragma once
+
+#include "ap_internal.h"
+
+namespace ap {
+
+// Rows of the caches: instance i's row j lies at row i * t_cap + j of K and V, or, with a table, at row j % b of the page that the
+// table names for block j / b.
+struct CacheRows {
+  const int32_t* table;    // [n_inst][nb_cap], or null
+  const int32_t* len;      // [n_inst]
+  int n_inst, t_cap, nb_cap, n_phys, lb;   // lb = log2(b)
+};
+
+struct DecodeArgs {
+  CacheRows r;
+  const void *q, *K, *V;
+  int window, n_first;
+  float *out, *acc;
+  unsigned long long* before;   // workspace: [n_inst + 1] groups of 16 rows in the instances before
+  float* whole;                 // workspace: [n_inst][g][2] maximum and sum of the instances that one workgroup goes over
+  float *part_ml, *part_acc;    // workspace: [2 * kCacheDecodeWgs][g][2] and [..][g][d] of the others' pieces
+  float* logits;                // workspace: [n_inst][g][t_cap], with acc only
+};
+
+struct PrefillArgs {
+  CacheRows r;
+  const void *q, *K, *V;
+  const int32_t* n_q;           // [n_inst], or null: q_cap each
+  int q_cap, window, n_first;
+  void* out;
+  float* acc;
+  float* stat;                  // workspace: [n_inst][q_cap * g][2] maximum and 1 / sum of every row, with acc only
+  float* sums;                  // workspace: [chunks][n_inst][t_cap] columns' sums over a chunk of the queries, with acc only
+  int chunks;
+};
+
+constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call
+
+struct CacheWs { size_t before, whole, part_ml, part_acc, logits, total; };     // decode, in bytes
+CacheWs cache_decode_ws(const Shape& s, bool weights);
+struct CacheQWs { size_t stat, sums, total; int chunks; };                       // prefill, in bytes
+CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights);
+
+hipError_t launch_cache_append(const Shape& s, const CacheRows& r, const void* k_new, const void* v_new, const int32_t* n_new, int q_cap,
+                               void* K, void* V, hipStream_t st);
+hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& a, hipStream_t st);
+hipError_t launch_cache_evict(const Shape& s, const CacheRows& r, void* K, void* V, const float* acc, int budget, int n_first, int n_last,
+                              float* acc_out, int32_t* len_out, int32_t* kept, hipStream_t st);
+
+}  // namespace ap

@@ -1,0 +1,395 @@
+// Attention of a chunk of new tokens per instance over its cache, which holds their rows already.  Query r of n lies at position
+// p = L - n + r and sees the rows j <= p, with a window only those with j > p - window or j < n_first:
+//
+//   s_rhj = q_rh . K_j / sqrt(d),  P_rhj = exp(s_rhj - m_rh) / sum_j exp(s_rhj - m_rh),  out_rh = sum_j P_rhj V_j,
+//   acc_j += sum_r sum_h P_rhj.
+//
+// The g heads of a group read the same K and V, so a workgroup's tile is 128 rows of q seen as [n * g][d], 32 a wave.  K and V go through
+// LDS, 64 rows (fp32: 32) at a time, in two buffers that are filled from memory without registers.  Both products are made transposed,
+// K q^T and V^T P^T: a lane then has scores, statistics and outputs of one query row, and the scores' registers are the second product's
+// operand as they are, since the order of its contraction index is free.
+#include "cache_body.h"
+
+namespace ap {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kTileRows = 128;               // rows of q per workgroup
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+template <typename T, int D> struct Form {
+  static constexpr int E = 16 / (int)sizeof(T);            // elements of a 16-byte piece
+  static constexpr int PIECES = D / E;                     // pieces of a row
+  static constexpr int TT = sizeof(T) == 2 ? 64 : 32;      // cache rows of a tile
+  static constexpr int TB = TT / 32;                       // blocks of 32 of them
+  static constexpr int KS = PIECES / 2;                    // pieces a lane contributes to a product over d
+  static constexpr int DB = D / 32;                        // blocks of 32 output dims
+  static constexpr int LOADS = TT * PIECES / kThreads;     // pieces a thread fetches of a tile of K, or V
+  static constexpr int TILE = TT * PIECES;                 // pieces of a tile
+  // Piece p of row r lies at place p ^ swizzle(r) of the row, so that the lanes of one LDS cycle use different banks: K is read a row
+  // per lane, V (16 bits) in blocks of four rows by two pieces.
+  __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
+  __device__ static __forceinline__ int v_place(int r, int p) { return sizeof(T) == 2 ? p ^ ((2 * r) & (PIECES - 1)) : p; }
+};
+
+typedef const __attribute__((address_space(1))) void* gptr;
+typedef __attribute__((address_space(3))) void* lptr;
+
+// What the queries of a tile see of an instance.
+struct Span {
+  int L, n, base;        // length, queries, position of query 0 (may be negative)
+  int p0, p1;            // positions of the tile's first and last query
+  int lo0, f;            // rows [0, f) and [lo0, p1] are seen by one of them at least, f <= lo0
+  int tiles, ts, tb;     // tiles of TT rows: ts from 0 on, the others from tb
+  __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
+};
+template <int TT, int G>
+__device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, int q_cap, int window, int n_first, int inst, int row0, int rows) {
+  Span s;
+  s.L = clamped(r.len[inst], 0, r.t_cap);
+  s.n = n_q == nullptr ? q_cap : clamped(n_q[inst], 0, q_cap);
+  s.base = s.L - s.n;
+  const int last = row0 + rows < s.n * G ? row0 + rows : s.n * G;        // rows of q up to here
+  s.p0 = s.base + row0 / G;
+  s.p1 = s.base + (last - 1) / G;
+  if (last <= row0) s.p1 = -1;
+  s.lo0 = window > 0 && s.p0 >= window ? s.p0 - window + 1 : 0;
+  s.f = n_first < s.lo0 ? n_first : s.lo0;
+  if (s.p1 < 0) { s.tiles = s.ts = s.tb = 0; return s; }
+  s.ts = (s.f + TT - 1) / TT;
+  s.tb = s.lo0 / TT > s.ts ? s.lo0 / TT : s.ts;
+  s.tiles = s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
+  return s;
+}
+
+// Sends a tile of rows [t0, t0 + TT) of X to LDS: the lane chooses the piece, so that it lies where the swizzle says.  Rows that no query
+// of the tile sees are not read; a row that the last query sees stands in for them.
+template <typename T, int D, bool IS_V>
+__device__ __forceinline__ void fetch_tile(const PrefillArgs& a, const void* X, int inst, const Span& s, int t0, u32x4* dst) {
+  using F = Form<T, D>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int l = 0; l < F::LOADS; ++l) {
+    const int first = (l * kWaves + wave) * 64, x = first + lane, r = x / F::PIECES, place = x % F::PIECES;
+    const int p = IS_V ? F::v_place(r, place) : F::k_place(r, place);
+    int j = t0 + r;
+    if (j > s.p1 || (j >= s.f && j < s.lo0)) j = s.p1;
+    const u32x4* src = static_cast<const u32x4*>(X) + row_at(a.r, inst, j) * F::PIECES + p;
+    __builtin_amdgcn_global_load_lds((gptr)src, (lptr)(dst + first), 16, 0, 0);
+  }
+}
+
+// (32 rows of X in LDS) . (32 rows held as operands)^T, fp32: one block of scores.
+template <typename T, int D>
+__device__ __forceinline__ float16v product(const u32x4* X, int row0, const u32x4 (&b)[Form<T, D>::KS]) {
+  using F = Form<T, D>;
+  const int lane = threadIdx.x & 63, m = lane & 31, hb = lane >> 5;
+  float16v c;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) c[i] = 0.f;
+#pragma unroll
+  for (int k = 0; k < F::KS; ++k) {
+    const u32x4 x = X[(row0 + m) * F::PIECES + F::k_place(row0 + m, 2 * k + hb)];
+    if constexpr (sizeof(T) == 2) {
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, b[k]), c, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(b[k][e]), c, 0, 0, 0);
+    }
+  }
+  return c;
+}
+
+__device__ __forceinline__ void wait_tiles() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): this wave's pieces of the tile are in LDS
+  __syncthreads();
+}
+
+// Which of 16 registers' rows: register i of a block holds row 8 (i / 4) + 4 hb + i % 4.
+__device__ __forceinline__ int reg_row(int i, int hb) { return 8 * (i >> 2) + 4 * hb + (i & 3); }
+
+template <typename T, int D, int G, bool STAT>
+__global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
+  using F = Form<T, D>;
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2 buffers][K, V][TILE]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, hb = lane >> 5;
+  const int inst = blockIdx.y, row0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileRows;    // the longest ones first
+  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kTileRows);
+  const int rows = s.n * G;                                // of q
+  if (row0 >= rows) return;
+
+  const int row = row0 + wave * 32 + n;                    // this lane's row of q; beyond the last it is computed and not stored
+  const size_t q_row = (size_t)inst * a.q_cap * G + (row < rows ? row : rows - 1);
+  u32x4 qf[F::KS];
+#pragma unroll
+  for (int k = 0; k < F::KS; ++k) qf[k] = static_cast<const u32x4*>(a.q)[q_row * F::PIECES + 2 * k + hb];
+  const int p = s.base + (row < rows ? row : rows - 1) / G;               // its position
+  const int lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
+
+  float16v o[F::DB];
+#pragma unroll
+  for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+  float m = -INFINITY, sum = 0.f;                          // the sum over this lane's half of the cache rows
+  const float scale = kLog2E / sqrtf((float)D);
+
+  if (s.tiles > 0) {
+    const int t0 = s.tile(0) * F::TT;
+    fetch_tile<T, D, false>(a, a.K, inst, s, t0, s_tiles);
+    fetch_tile<T, D, true>(a, a.V, inst, s, t0, s_tiles + F::TILE);
+  }
+  for (int u = 0; u < s.tiles; ++u) {
+    wait_tiles();                                          // ... and everybody is done with the other buffer
+    const int t0 = s.tile(u) * F::TT;
+    const u32x4* Kt = s_tiles + (u & 1) * 2 * F::TILE;
+    const u32x4* Vt = Kt + F::TILE;
+    if (u + 1 < s.tiles) {
+      u32x4* other = s_tiles + (~u & 1) * 2 * F::TILE;
+      const int t1 = s.tile(u + 1) * F::TT;
+      fetch_tile<T, D, false>(a, a.K, inst, s, t1, other);
+      fetch_tile<T, D, true>(a, a.V, inst, s, t1, other + F::TILE);
+    }
+    float16v c[F::TB];
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
+    // Every row of the tile is seen by every query of it, or the scores of those that are not become -inf.
+    const bool all = t0 + F::TT - 1 <= s.p0 && (a.window <= 0 || t0 > s.p1 - a.window || t0 + F::TT <= a.n_first);
+    if (!all) {
+#pragma unroll
+      for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = t0 + 32 * b + reg_row(i, hb);
+          if (j > p || (j < lo && j >= a.n_first)) c[b][i] = -INFINITY;
+        }
+    }
+    float top = c[0][0];
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, c[b][i]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    // The reference is a whole number in units of log2 (a change of it rounds nothing), 0 as long as nothing is seen.
+    const float ref = fmaxf(m, ceilf(top * scale));
+    if (__any(ref != m)) {
+      const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
+      sum *= shrink;
+#pragma unroll
+      for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
+      m = ref;
+    }
+    const float use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        c[b][i] = exp2_fast(__builtin_fmaf(c[b][i], scale, -use));
+        sum += c[b][i];
+      }
+    if constexpr (sizeof(T) == 2) {
+      // Probabilities are rounded to bf16 for the matrix unit, which adds an error of the size of the output's own rounding; their sum
+      // is taken before.
+#pragma unroll
+      for (int k = 0; k < F::TT / 16; ++k) {
+        bf16x8 pb;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pb[e] = (__bf16)c[k / 2][8 * (k % 2) + e];
+        // V^T of 16 cache rows: the transposing read gives lane (m, hb) column m of four rows; a lane of 16 points to the 8 bytes at
+        // row lane / 4, columns 4 (lane % 4).
+        const int i = lane & 15, r = 16 * k + 4 * hb + (i >> 2);
+#pragma unroll
+        for (int b = 0; b < F::DB; ++b) {
+          const int col = 32 * b + 16 * ((lane >> 4) & 1) + 4 * (i & 3), piece = col / 8;
+          bf16x8 va;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int rr = r + 8 * half;
+            const char* at = reinterpret_cast<const char*>(Vt + rr * F::PIECES + F::v_place(rr, piece)) + (col % 8) * 2;
+            const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+            const bf16x4 y = __builtin_bit_cast(bf16x4, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) va[4 * half + e] = y[e];
+          }
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb, o[b], 0, 0, 0);
+        }
+      }
+    } else {
+      const float* Vf = reinterpret_cast<const float*>(Vt);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int b = 0; b < F::DB; ++b)
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(Vf[reg_row(i, hb) * D + 32 * b + n], c[0][i], o[b], 0, 0, 0);
+      }
+    }
+  }
+
+  sum += __shfl_xor(sum, 32, 64);
+  if (row >= rows) return;
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;           // a query that sees nothing has a zero output
+  if (STAT && hb == 0) {
+    float* st = a.stat + ((size_t)inst * a.q_cap * G + row) * 2;
+    st[0] = m == -INFINITY ? 0.f : m;
+    st[1] = inv;
+  }
+  T* out = static_cast<T*>(a.out) + ((size_t)inst * a.q_cap * G + row) * D;
+#pragma unroll
+  for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d = 32 * b + reg_row(i, hb);
+      if constexpr (sizeof(T) == 2) {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[b][i + e] * inv);
+        *reinterpret_cast<bf16x4*>(out + d) = y;
+      } else {
+        float4v y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = o[b][i + e] * inv;
+        *reinterpret_cast<float4v*>(out + d) = y;
+      }
+    }
+}
+
+// Sums of the columns of P over a chunk of the query rows.  A workgroup has 128 cache rows, 32 a wave, held as operands; the queries go
+// through LDS, 64 rows (fp32: 32) at a time.  The product is q K^T this way round: a lane has scores of one cache row, and its sum
+// is taken in registers.
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) {
+  using F = Form<T, D>;
+  constexpr int QT = F::TT;
+  __shared__ __attribute__((aligned(16))) u32x4 s_q[2][F::TILE];
+  __shared__ __attribute__((aligned(16))) float s_stat[2][QT][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, hb = lane >> 5;
+  const int inst = blockIdx.y, chunk = blockIdx.z, t0 = (int)blockIdx.x * kTileRows;
+  const int L = clamped(a.r.len[inst], 0, a.r.t_cap), nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
+  if (t0 >= L) return;
+  const int base = L - nq, rows = nq * G;
+  // Rows of q in this chunk, whole tiles of them, that see one of the cache rows at least.
+  const int all_tiles = (a.q_cap * G + QT - 1) / QT, each = (all_tiles + a.chunks - 1) / a.chunks;
+  int begin = chunk * each * QT, end = begin + each * QT < rows ? begin + each * QT : rows;
+  const int first_q = t0 - base > 0 ? t0 - base : 0;                          // the first query that lies at t0 or behind it
+  if (begin < first_q * G) begin = first_q * G / QT * QT;
+  if (a.window > 0 && t0 >= a.n_first) {                                      // and the last that still sees t0 + 127
+    const long long last_q = (long long)t0 + kTileRows - 1 + a.window - 1 - base;
+    if ((last_q + 1) * G < end) end = (int)((last_q + 1) * G);
+  }
+  const int j = t0 + 32 * wave + n;                        // this lane's cache row
+  const bool mine = j < L;
+  const size_t k_row = row_at(a.r, inst, mine ? j : L - 1);
+  u32x4 kf[F::KS];
+#pragma unroll
+  for (int k = 0; k < F::KS; ++k) kf[k] = static_cast<const u32x4*>(a.K)[k_row * F::PIECES + 2 * k + hb];
+  const float scale = kLog2E / sqrtf((float)D);
+  float total = 0.f;
+
+  auto fetch = [&](int r0, int buf) {
+    const int w = tid >> 6;
+#pragma unroll
+    for (int l = 0; l < F::LOADS; ++l) {
+      const int first = (l * kWaves + w) * 64, x = first + lane, r = x / F::PIECES, p = F::k_place(r, x % F::PIECES);
+      const int row = r0 + r < rows ? r0 + r : rows - 1;
+      const u32x4* src = static_cast<const u32x4*>(a.q) + ((size_t)inst * a.q_cap * G + row) * F::PIECES + p;
+      __builtin_amdgcn_global_load_lds((gptr)src, (lptr)(&s_q[buf][first]), 16, 0, 0);
+    }
+    for (int x = tid; x < 2 * QT; x += kThreads) {
+      const int row = r0 + x / 2;
+      s_stat[buf][x / 2][x % 2] = row < rows ? a.stat[((size_t)inst * a.q_cap * G + row) * 2 + x % 2] : 0.f;
+    }
+  };
+  if (begin < end) fetch(begin, 0);
+  int buf = 0;
+  for (int r0 = begin; r0 < end; r0 += QT, buf ^= 1) {
+    wait_tiles();
+    if (r0 + QT < end) fetch(r0 + QT, buf ^ 1);
+    const int p0 = base + r0 / G;
+    const int r_last = r0 + QT < rows ? r0 + QT - 1 : rows - 1, p1 = base + r_last / G;
+    const bool all = t0 + kTileRows - 1 <= p0 && t0 + kTileRows <= L && r0 + QT <= rows &&
+                     (a.window <= 0 || t0 > p1 - a.window || t0 + kTileRows <= a.n_first);
+    float part = 0.f;
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b) {
+      const float16v c = product<T, D>(s_q[buf], 32 * b, kf);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = 32 * b + reg_row(i, hb);
+        float w = exp2_fast(__builtin_fmaf(c[i], scale, -s_stat[buf][r][0])) * s_stat[buf][r][1];
+        if (!all) {
+          const int p = base + (r0 + r) / G;
+          const bool seen = r0 + r < rows && j <= p && (a.window <= 0 || j > p - a.window || j < a.n_first);
+          w = seen ? w : 0.f;
+        }
+        part += w;
+      }
+    }
+    total += part;
+  }
+  total += __shfl_xor(total, 32, 64);
+  if (hb == 0 && mine) {
+    if (a.chunks == 1) a.acc[(size_t)inst * a.r.t_cap + j] += total;
+    else a.sums[((size_t)chunk * a.r.n_inst + inst) * a.r.t_cap + j] = total;
+  }
+}
+
+// The chunks' sums, one after the other, so that the result does not depend on which was ready first.
+__global__ __launch_bounds__(kThreads) void cache_weights_add_kernel(PrefillArgs a) {
+  const int i = blockIdx.y, j = blockIdx.x * kThreads + threadIdx.x;
+  const int L = clamped(a.r.len[i], 0, a.r.t_cap);
+  if (j >= L) return;
+  float x = 0.f;
+  for (int c = 0; c < a.chunks; ++c) x += a.sums[((size_t)c * a.r.n_inst + i) * a.r.t_cap + j];
+  a.acc[(size_t)i * a.r.t_cap + j] += x;
+}
+
+template <typename T, int D, int G> hipError_t run(const PrefillArgs& a, hipStream_t st) {
+  const size_t lds = (size_t)4 * Form<T, D>::TILE * 16;
+  const unsigned tiles = (unsigned)(((long long)a.q_cap * G + kTileRows - 1) / kTileRows);
+  const dim3 grid(tiles, a.r.n_inst);
+  if (a.acc == nullptr) {
+    cache_prefill_kernel<T, D, G, false><<<grid, kThreads, lds, st>>>(a);
+    return hipGetLastError();
+  }
+  cache_prefill_kernel<T, D, G, true><<<grid, kThreads, lds, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  cache_weights_kernel<T, D, G><<<dim3((a.r.t_cap + kTileRows - 1) / kTileRows, a.r.n_inst, a.chunks), kThreads, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.chunks == 1) return e;
+  cache_weights_add_kernel<<<dim3((a.r.t_cap + kThreads - 1) / kThreads, a.r.n_inst), kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <typename T, int D> hipError_t run_g(int g, const PrefillArgs& a, hipStream_t st) {
+  return g == 1 ? run<T, D, 1>(a, st) : g == 2 ? run<T, D, 2>(a, st) : g == 4 ? run<T, D, 4>(a, st) : run<T, D, 8>(a, st);
+}
+
+}  // namespace
+
+CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
+  CacheQWs w;
+  size_t o = 0;
+  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
+  // Query rows are cut into chunks where cache tiles alone would leave CUs without work, not below 512 rows each.
+  const long long tiles = (long long)s.n_inst * ((s.t_cap + kTileRows - 1) / kTileRows), q_rows = (long long)q_cap * s.g;
+  long long chunks = (2048 + tiles - 1) / tiles;
+  if (chunks > (q_rows + 511) / 512) chunks = (q_rows + 511) / 512;
+  if (chunks > 16) chunks = 16;
+  w.chunks = chunks < 1 ? 1 : (int)chunks;
+  w.stat = take(weights ? (size_t)s.n_inst * q_rows * 2 * 4 : 0);
+  w.sums = take(weights && w.chunks > 1 ? (size_t)w.chunks * s.n_inst * s.t_cap * 4 : 0);
+  w.total = o;
+  return w;
+}
+
+hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& a, hipStream_t st) {
+  if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s.g, a, st) : run_g<bf16_t, 64>(s.g, a, st);
+  return s.d == 128 ? run_g<float, 128>(s.g, a, st) : run_g<float, 64>(s.g, a, st);
+}
+
+}  // namespace ap

@@ -159,3 +159,69 @@ class DenseRun:
             self.ctx.select_topk(self.row, nb, self.idx, self.cnt, self.ws)
             self.nb_listed = nb
         self.ctx.sparse_decode(q, K, V, t, self.idx, self.cnt, self.out, self.row, self.ws)
+
+
+class CacheRun:
+    """Layers whose caches have lengths of their own: prompts of different lengths go in by chunks, every token attends to its whole
+    cache (or to a window and the first rows), and every `evict_every` steps caches beyond the budget lose the rows that gathered the
+    least attention weight - the eviction that the predicted selection of DecodeRun is an alternative to.  The first n_sink and the last
+    n_local blocks of the workload's budget stay, as there; no history and no predictor.
+
+    Every instance starts empty.  The lengths live on the device, so the host only knows how long a cache can be at most."""
+
+    def __init__(self, w, device="cuda:0", q_cap=1, window=0, evict_every=64, table=None, n_pages=0):
+        """q_cap: most tokens of a chunk.  table: int32 [n_inst][nb_cap] into a pool of n_pages pages, every page an instance's own;
+        None for the contiguous layout."""
+        self.w, self.q_cap, self.window, self.evict_every = w, q_cap, window, evict_every
+        self.dev = torch.device(device)
+        self.ctx = Context(n_inst=w.n_inst, g=w.g, head_dim=w.head_dim, block=w.block, hist_len=w.hist_len, t_cap=w.t_cap,
+                           k_blocks=w.k_blocks, n_sink=w.n_sink, n_local=w.n_local, c1=w.c1, c2=w.c2, kv_dtype=w.kv_dtype)
+        self.table = table
+        if table is not None:
+            self.ctx.set_block_table(table, n_pages)
+        self.n_first, self.n_last = w.n_sink * w.block, w.n_local * w.block
+        shape = (w.n_inst, w.t_cap, w.head_dim) if table is None else (n_pages, w.block, w.head_dim)
+        self.K = torch.zeros(shape, dtype=w.torch_dtype(), device=self.dev)
+        self.V = torch.zeros_like(self.K)
+        self.len = torch.zeros((w.n_inst,), dtype=torch.int32, device=self.dev)
+        self.acc = torch.zeros((w.n_inst, w.t_cap), dtype=torch.float32, device=self.dev)
+        self.kept = torch.zeros((w.n_inst, w.budget_tokens), dtype=torch.int32, device=self.dev)
+        self.out = torch.zeros((w.n_inst, w.g, w.head_dim), dtype=torch.float32, device=self.dev)
+        self.chunk_out = torch.zeros((w.n_inst, q_cap, w.g, w.head_dim), dtype=w.torch_dtype(), device=self.dev)
+        size = max(16, self.ctx.cache_workspace_bytes(q_cap, True))
+        self.ws = torch.zeros((size,), dtype=torch.uint8, device=self.dev)
+        self.steps_done = 0
+        self.longest = 0          # no cache is longer than this
+
+    def _grow(self, n, by):
+        if self.longest + by > self.w.t_cap:
+            raise ValueError(f"caches of up to {self.longest} rows have no room for {by} more (t_cap = {self.w.t_cap})")
+        self.longest += by
+        self.len += n
+
+    def prefill(self, q, k, v, n_new=None):
+        """The next chunk of every prompt, q [n_inst][m][g][d] and k, v [n_inst][m][d] with m <= q_cap; n_new: int32 [n_inst], how many
+        of the m tokens count.  Returns the outputs [n_inst][m][g][d]."""
+        m = q.shape[1]
+        if m > self.q_cap:
+            raise ValueError(f"a chunk has at most q_cap = {self.q_cap} tokens")
+        self._grow(m if n_new is None else n_new.clamp(0, m), m)
+        self.ctx.cache_append(k, v, n_new, self.len, self.K, self.V)
+        out = self.chunk_out.view(-1)[:q.numel()].view(q.shape)
+        self.ctx.cache_prefill(q, n_new, self.K, self.V, self.len, self.window, self.n_first, out, self.acc, self.ws)
+        return out
+
+    def step(self, q, k, v):
+        """One decode step: q [n_inst][g][d], k and v [n_inst][d].  Returns the outputs, float [n_inst][g][d]."""
+        self._grow(1, 1)
+        self.ctx.cache_append(k.unsqueeze(1), v.unsqueeze(1), None, self.len, self.K, self.V)
+        self.ctx.cache_decode(q, self.K, self.V, self.len, self.window, self.n_first, self.out, self.acc, self.ws)
+        self.steps_done += 1
+        if self.steps_done % self.evict_every == 0:
+            self.evict()
+        return self.out
+
+    def evict(self):
+        self.ctx.cache_evict(self.K, self.V, self.acc, self.len, self.w.budget_tokens, self.n_first, self.n_last, self.acc, self.len,
+                             self.kept)
+        self.longest = min(self.longest, self.w.budget_tokens)
