@@ -32,54 +32,67 @@ __device__ __forceinline__ Seen seen_of(int len, int t_cap, int window, int n_fi
   return s;
 }
 
-__device__ __forceinline__ unsigned long long share_of(unsigned long long groups) {
-  const unsigned long long per = (groups + kCacheDecodeWgs - 1) / kCacheDecodeWgs;
+__device__ __forceinline__ unsigned long long share_of(unsigned long long groups, int wgs) {
+  const unsigned long long per = (groups + wgs - 1) / wgs;
   return per > kLeastGroups ? per : kLeastGroups;
 }
 
 template <typename T, int D, int G> struct Form {
   static constexpr int E = 16 / (int)sizeof(T);            // elements of a 16-byte piece
-  static constexpr int PIECES = D / E;                     // pieces of a row = lanes that read a V row
-  static constexpr int KL = PIECES / 4;                    // loads of a K group: lane (m, kg) has piece 4 l + kg of row m
-  static constexpr int RPL = kWave / PIECES;               // V rows a load
-  static constexpr int VL = kGroup / RPL;                  // loads of a V group
+  static constexpr int PIECES = D / E;                     // pieces of a row = lanes that have a V row
+  static constexpr int N = PIECES / 4;                     // pieces of a group's K (or V) per lane
+  static constexpr int RPL = kWave / PIECES;               // V rows that a wave reads at a time
+  static constexpr int TILE = kGroup * PIECES;             // pieces of a group's K (or V)
+  static constexpr int BUFFERS = kWaves * 2 * 2 * TILE * 16;           // bytes of LDS: every wave has two groups of K and V
+  static constexpr int PER_CU = PIECES == 8 ? 4 : (PIECES == 16 ? 2 : 1);   // workgroups a CU, as LDS has room for
+  static constexpr int WGS = 256 * PER_CU;                 // the workgroups that 256 CUs hold at once
+  static_assert(WGS <= kCacheDecodeWgs && PER_CU * (BUFFERS + 4096) <= 160 * 1024, "workspace, LDS");
+  // Piece p of row r of a K group lies at place p ^ (r % PIECES): the operand layout reads a row per lane.
+  __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
 };
 
-// One group's K and V pieces of a lane.
-template <typename T, int D, int G> struct Rows {
-  u32x4 k[Form<T, D, G>::KL], v[Form<T, D, G>::VL];
-};
-
-template <typename T, int D, int G>
-__device__ __forceinline__ void load_group(const DecodeArgs& a, int inst, const Seen& s, int grp, int lane, Rows<T, D, G>& x) {
-  using F = Form<T, D, G>;
-  const int t0 = grp * kGroup;
-  // Rows that are not seen are not read: their lanes read a row of the group that is.
-  const int other = t0 < s.f ? t0 : (t0 > s.lo ? t0 : s.lo);
-  const u32x4* K = static_cast<const u32x4*>(a.K);
-  const u32x4* V = static_cast<const u32x4*>(a.V);
-  {
-    const int j = t0 + (lane & 15);
-    const size_t at = row_at(a.r, inst, s.row(j) ? j : other) * F::PIECES + (lane >> 4);
+// Where a group of 16 rows lies: its first and its second eight, in rows of K and V; and whether all 16 are seen.  Wave-uniform.
+struct Place { size_t a, b; int t0; bool all; };
+__device__ __forceinline__ Place place_of(const CacheRows& r, int inst, const Seen& s, int u) {
+  Place p;
+  p.t0 = __builtin_amdgcn_readfirstlane(s.group(u) * kGroup);
+  p.a = rows_at(r, inst, p.t0);
+  p.b = r.lb == 3 && r.table != nullptr ? rows_at(r, inst, p.t0 + 8) : p.a + 8;
+  p.all = p.t0 + kGroup <= s.L && (p.t0 >= s.lo || p.t0 + kGroup <= s.f);
+  return p;
+}
+// Sends the rows of a group of K (or V) to LDS.
+template <typename F, bool IS_V> __device__ __forceinline__ void send(const void* X, const Place& p, const Seen& s, int lane, unsigned lds) {
+  constexpr unsigned row = F::PIECES * 16;
+  if (p.all && p.b == p.a + 8) {
+    const char* base = static_cast<const char*>(X) + p.a * row;
 #pragma unroll
-    for (int l = 0; l < F::KL; ++l) x.k[l] = K[at + 4 * l];
-  }
-#pragma unroll
-  for (int l = 0; l < F::VL; ++l) {
-    const int j = t0 + l * F::RPL + lane / F::PIECES;
-    x.v[l] = V[row_at(a.r, inst, s.row(j) ? j : other) * F::PIECES + lane % F::PIECES];
+    for (int l = 0; l < F::N; ++l) {
+      const int x = l * kWave + lane, r = x / F::PIECES, place = x % F::PIECES;
+      to_lds(base, r * row + (IS_V ? place : F::k_place(r, place)) * 16, lds + l * 1024);
+    }
+  } else {
+    // Rows that are not seen are not read: another row of the group, which is, stands in for them.
+    const int other = (p.t0 < s.f ? p.t0 : (p.t0 > s.lo ? p.t0 : s.lo)) - p.t0;
+#pragma unroll 1
+    for (int l = 0; l < F::N; ++l) {
+      const int x = l * kWave + lane, r = x / F::PIECES, place = x % F::PIECES;
+      const int y = s.row(p.t0 + r) ? r : other;
+      const size_t at = y < 8 ? p.a + y : p.b + (y - 8);
+      to_lds_from(static_cast<const char*>(X) + at * row + (IS_V ? place : F::k_place(r, place)) * 16, lds + l * 1024);
+    }
   }
 }
 
 template <typename T, int D, int G, bool ACC>
-__global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(DecodeArgs a) {
   using F = Form<T, D, G>;
-  __shared__ __attribute__((aligned(16))) float s_out[kWaves][G][D];
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_rows[];          // [wave][buffer][K, V][TILE]; at the end outputs, [wave][G][D]
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
   __shared__ unsigned long long s_wave[kWaves];
   __shared__ int s_inst, s_from;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = lane & 15, kg = lane >> 4;
 
   // Where this workgroup's share begins: every thread sums the groups of consecutive instances.
@@ -102,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
     if (w < wave) ahead += s_wave[w];
     groups += s_wave[w];
   }
-  const unsigned long long per = share_of(groups), begin = (unsigned long long)blockIdx.x * per;
+  const unsigned long long per = share_of(groups, F::WGS), begin = (unsigned long long)blockIdx.x * per;
   const unsigned long long end = begin + per < groups ? begin + per : groups;
   if (blockIdx.x == 0) {
     unsigned long long at = ahead;
@@ -126,20 +139,37 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
     }
   }
   __syncthreads();
-  int inst = s_inst, from = s_from;
+  int inst = __builtin_amdgcn_readfirstlane(s_inst), from = __builtin_amdgcn_readfirstlane(s_from);
   unsigned long long left = end - begin;
 
   const float scale = kLog2E / sqrtf((float)D);
+  const u32x4* mine_rows = s_rows + wave * 4 * F::TILE;
+  const unsigned ring = lds_address(mine_rows);
+  float* s_out = reinterpret_cast<float*>(s_rows);
   for (; left > 0; ++inst, from = 0) {
     const Seen s = seen_of(a.r.len[inst], a.r.t_cap, a.window, a.n_first);
     if (s.n <= from) continue;                             // an empty instance
     const int to = (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
     left -= (unsigned)(to - from);
 
+    // This wave's groups are from + wave, from + wave + 4, ...; two of them are on their way to LDS while one is worked off.
+    const int mine_n = to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
+    const int u0 = from + wave;
+    Place next[2];                                         // of the groups behind the ones that were sent for
+    if (mine_n > 0) {
+      const Place p = place_of(a.r, inst, s, u0), p1 = place_of(a.r, inst, s, mine_n > 1 ? u0 + kWaves : u0);
+      send<F, false>(a.K, p, s, lane, ring);
+      send<F, true>(a.V, p, s, lane, ring + F::TILE * 16);
+      if (mine_n > 1) {
+        send<F, false>(a.K, p1, s, lane, ring + 2 * F::TILE * 16);
+        send<F, true>(a.V, p1, s, lane, ring + 3 * F::TILE * 16);
+      }
+      next[0] = p; next[1] = p1;
+    }
     // B operand of the products q . K: lane (head, kg) has piece 4 l + kg of the head's query; heads beyond g are zero.
-    u32x4 qf[F::KL];
+    u32x4 qf[F::N];
 #pragma unroll
-    for (int l = 0; l < F::KL; ++l) {
+    for (int l = 0; l < F::N; ++l) {
       const u32x4 zero = {0u, 0u, 0u, 0u};
       qf[l] = head < G ? static_cast<const u32x4*>(a.q)[((size_t)inst * G + head) * F::PIECES + 4 * l + kg] : zero;
     }
@@ -150,32 +180,40 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
 #pragma unroll
       for (int e = 0; e < F::E; ++e) o[h][e] = 0.f;
 
-    Rows<T, D, G> next;
-    int u = from + wave;
-    if (u < to) load_group<T, D, G>(a, inst, s, s.group(u), lane, next);
-    for (; u < to; u += kWaves) {
-      const Rows<T, D, G> x = next;
-      const int t0 = s.group(u) * kGroup;
-      if (u + kWaves < to) load_group<T, D, G>(a, inst, s, s.group(u + kWaves), lane, next);
+    for (int it = 0; it < mine_n; ++it) {
+      const Place here = next[0];
+      next[0] = next[1];
+      next[1] = place_of(a.r, inst, s, u0 + kWaves * (it + 2 < mine_n ? it + 2 : it));
+      const bool more = it + 2 < mine_n;
+      const int t0 = here.t0;
+      const unsigned slot = ring + (it & 1) * 2 * F::TILE * 16;
+      const u32x4* Kt = mine_rows + (it & 1) * 2 * F::TILE;
+      const u32x4* Vt = Kt + F::TILE;
+      if (it + 1 < mine_n) landed<3 * F::N>(); else landed<F::N>();
       float4v c = {0.f, 0.f, 0.f, 0.f};                    // rows t0 + 4 kg + r of head `head`
 #pragma unroll
-      for (int l = 0; l < F::KL; ++l) {
+      for (int l = 0; l < F::N; ++l) {
+        const u32x4 k = Kt[head * F::PIECES + F::k_place(head, 4 * l + kg)];
         if constexpr (sizeof(T) == 2) {
-          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[l]), __builtin_bit_cast(bf16x8, qf[l]), c, 0, 0, 0);
+          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), c, 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[l][e]), __uint_as_float(qf[l][e]), c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), c, 0, 0, 0);
         }
       }
-      float top = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (!s.row(t0 + 4 * kg + r)) c[r] = -INFINITY;
-        top = fmaxf(top, c[r]);
+      if (more) {
+        lds_read();
+        send<F, false>(a.K, next[1], s, lane, slot);
       }
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      if (!here.all) {
+        const int j = t0 + 4 * kg;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (!s.row(j + r)) c[r] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
+      top = max32(max16(top));
       // The reference is a whole number in units of log2: changing it multiplies by a power of two and rounds nothing, and the exponent
       // is one fused multiply-add.
       const float ref = fmaxf(m, ceilf(top * scale));
@@ -204,10 +242,14 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      if (more) landed<3 * F::N>();
+      else if (it + 1 < mine_n) landed<2 * F::N>();
+      else landed<0>();
 #pragma unroll
-      for (int l = 0; l < F::VL; ++l) {
+      for (int l = 0; l < F::N; ++l) {
         float v[F::E];
-        unpack16(make_uint4(x.v[l].x, x.v[l].y, x.v[l].z, x.v[l].w), v, T{});
+        const u32x4 x = Vt[l * kWave + lane];              // piece lane % PIECES of row l * RPL + lane / PIECES
+        unpack16(make_uint4(x.x, x.y, x.z, x.w), v, T{});
         const float* p = s_p[wave][l * F::RPL + lane / F::PIECES];
 #pragma unroll
         for (int h = 0; h < G; ++h)
@@ -216,22 +258,28 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      if (more) {
+        lds_read();
+        send<F, true>(a.V, next[1], s, lane, slot + F::TILE * 16);
+      }
     }
 
     // The wave's lanes, then the workgroup's waves.
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
+    sum = sum32(sum16(sum));
 #pragma unroll
-    for (int x = F::PIECES; x < 64; x <<= 1)
+    for (int h = 0; h < G; ++h) {
 #pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int e = 0; e < F::E; ++e) o[h][e] += __shfl_xor(o[h][e], x, 64);
+      for (int e = 0; e < F::E; ++e) {
+        if (F::PIECES <= 8) o[h][e] += dpp_move<0x128>(o[h][e]);          // row_ror:8
+        if (F::PIECES <= 16) o[h][e] = sum16(o[h][e]);
+        o[h][e] = sum32(o[h][e]);
+      }
+    }
     if (lane < F::PIECES) {
 #pragma unroll
       for (int h = 0; h < G; ++h)
 #pragma unroll
-        for (int e = 0; e < F::E; ++e) s_out[wave][h][lane * F::E + e] = o[h][e];
+        for (int e = 0; e < F::E; ++e) s_out[(wave * 4 * F::TILE * 4) + h * D + lane * F::E + e] = o[h][e];
     }
     if (lane < G) {
       s_ml[wave][lane][0] = m;
@@ -248,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
       for (int w = 0; w < kWaves; ++w) {
         const float f = exp2_fast(s_ml[w][h][0] - top);
         all += f * s_ml[w][h][1];
-        val += f * s_out[w][h][e];
+        val += f * s_out[w * 4 * F::TILE * 4 + x];
       }
       if (whole) a.out[((size_t)inst * G + h) * D + e] = val / all;
       else a.part_acc[(slot * G + h) * D + e] = val;
@@ -265,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void cache_decode_kernel(DecodeArgs a) {
 // Joins the pieces of instances that several workgroups went over, and adds the weights.  Workgroup (0, instance) has the output,
 // workgroup (1 + x, instance) the weights of 1024 rows.
 template <int G>
-__global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int D) {
+__global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int D, int wgs) {
   __shared__ float s_f[kCacheDecodeWgs + 1][G];            // factors of the pieces
   __shared__ float s_m[G], s_inv[G];
   const int i = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -278,7 +326,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
   }
   const int j0 = ((int)blockIdx.x - 1) * 4 * kThreads;
   if (blockIdx.x > 0 && (j0 >= s.L || (j0 >= s.f && j0 + 4 * kThreads <= s.lo))) return;
-  const unsigned long long at = a.before[i], per = share_of(a.before[a.r.n_inst]);
+  const unsigned long long at = a.before[i], per = share_of(a.before[a.r.n_inst], wgs);
   const int w0 = (int)(at / per), parts = (int)((at + (unsigned)s.n - 1) / per) - w0 + 1;
   if (blockIdx.x == 0 && parts == 1) return;
   auto slot = [&](int p) { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };
@@ -331,12 +379,13 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
 }
 
 template <typename T, int D, int G> hipError_t run(const DecodeArgs& a, hipStream_t st) {
-  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true><<<kCacheDecodeWgs, kThreads, 0, st>>>(a);
-  else cache_decode_kernel<T, D, G, false><<<kCacheDecodeWgs, kThreads, 0, st>>>(a);
+  using F = Form<T, D, G>;
+  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
+  else cache_decode_kernel<T, D, G, false><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned columns = a.acc != nullptr ? (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads)) : 0;
-  cache_join_kernel<G><<<dim3(1 + columns, a.r.n_inst), kThreads, 0, st>>>(a, D);
+  cache_join_kernel<G><<<dim3(1 + columns, a.r.n_inst), kThreads, 0, st>>>(a, D, F::WGS);
   return hipGetLastError();
 }
 template <typename T, int D> hipError_t run_g(int g, const DecodeArgs& a, hipStream_t st) {

@@ -28,14 +28,12 @@ template <typename T, int D> struct Form {
   static constexpr int DB = D / 32;                        // blocks of 32 output dims
   static constexpr int LOADS = TT * PIECES / kThreads;     // pieces a thread fetches of a tile of K, or V
   static constexpr int TILE = TT * PIECES;                 // pieces of a tile
+  static constexpr int RPL = 64 / PIECES;                  // rows that a wave fetches with a load
   // Piece p of row r lies at place p ^ swizzle(r) of the row, so that the lanes of one LDS cycle use different banks: K is read a row
   // per lane, V (16 bits) in blocks of four rows by two pieces.
   __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
   __device__ static __forceinline__ int v_place(int r, int p) { return sizeof(T) == 2 ? p ^ ((2 * r) & (PIECES - 1)) : p; }
 };
-
-typedef const __attribute__((address_space(1))) void* gptr;
-typedef __attribute__((address_space(3))) void* lptr;
 
 // What the queries of a tile see of an instance.
 struct Span {
@@ -64,20 +62,48 @@ __device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, 
   return s;
 }
 
-// Sends a tile of rows [t0, t0 + TT) of X to LDS: the lane chooses the piece, so that it lies where the swizzle says.  Rows that no query
-// of the tile sees are not read; a row that the last query sees stands in for them.
-template <typename T, int D, bool IS_V>
-__device__ __forceinline__ void fetch_tile(const PrefillArgs& a, const void* X, int inst, const Span& s, int t0, u32x4* dst) {
+// Where the rows lie that this wave fetches of a tile: LOADS runs of RPL rows, each of them in one page.  Rows that no query of the tile sees
+// are not read: row `alt`, which is seen, stands in for them.  Wave-uniform.
+template <typename T, int D> struct Places {
+  size_t at[Form<T, D>::LOADS];                            // row j of the run lies at at + j
+  int alt[Form<T, D>::LOADS];                              // -1: all of the run is seen
+};
+template <typename T, int D>
+__device__ __forceinline__ Places<T, D> places_of(const PrefillArgs& a, int inst, const Span& s, int t0, int wave) {
   using F = Form<T, D>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Places<T, D> x;
 #pragma unroll
   for (int l = 0; l < F::LOADS; ++l) {
-    const int first = (l * kWaves + wave) * 64, x = first + lane, r = x / F::PIECES, place = x % F::PIECES;
-    const int p = IS_V ? F::v_place(r, place) : F::k_place(r, place);
-    int j = t0 + r;
-    if (j > s.p1 || (j >= s.f && j < s.lo0)) j = s.p1;
-    const u32x4* src = static_cast<const u32x4*>(X) + row_at(a.r, inst, j) * F::PIECES + p;
-    __builtin_amdgcn_global_load_lds((gptr)src, (lptr)(dst + first), 16, 0, 0);
+    const int g0 = t0 + (l * kWaves + wave) * F::RPL;
+    const bool all = g0 + F::RPL - 1 <= s.p1 && (g0 >= s.lo0 || g0 + F::RPL <= s.f);
+    int alt = g0;                                          // a row of the run that is seen, or one of another run
+    if (g0 >= s.f) alt = g0 > s.lo0 ? g0 : s.lo0;
+    const bool none = alt > s.p1 || alt >= g0 + F::RPL;
+    if (none) alt = s.p1;
+    const int eight = (none ? s.p1 : g0) & ~7;
+    x.at[l] = rows_at(a.r, inst, eight) - eight;
+    x.alt[l] = all ? -1 : alt;
+  }
+  return x;
+}
+// Sends a tile of rows [t0, t0 + TT) of X to LDS: the lane chooses the piece, so that it lies where the swizzle says.
+template <typename T, int D, bool IS_V>
+__device__ __forceinline__ void send_tile(const void* X, const Places<T, D>& at, const Span& s, int t0, int wave, unsigned lds) {
+  using F = Form<T, D>;
+  constexpr unsigned bytes = F::PIECES * 16;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int l = 0; l < F::LOADS; ++l) {
+    const int run = (l * kWaves + wave) * F::RPL, in = lane / F::PIECES, place = lane % F::PIECES;
+    const int p = IS_V ? F::v_place(run + in, place) : F::k_place(run + in, place);
+    const unsigned to = lds + (l * kWaves + wave) * 1024;
+    if (at.alt[l] < 0) {
+      to_lds(static_cast<const char*>(X) + (at.at[l] + t0 + run) * bytes, in * bytes + p * 16, to);
+    } else {
+      int j = t0 + run + in;
+      if (j > s.p1 || (j >= s.f && j < s.lo0)) j = at.alt[l];
+      to_lds_from(static_cast<const char*>(X) + (at.at[l] + j) * bytes + p * 16, to);
+    }
   }
 }
 
@@ -103,9 +129,11 @@ __device__ __forceinline__ float16v product(const u32x4* X, int row0, const u32x
   return c;
 }
 
+// Everybody's pieces of the tile are in LDS, and everybody is done with the buffer that is filled next.
 __device__ __forceinline__ void wait_tiles() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): this wave's pieces of the tile are in LDS
-  __syncthreads();
+  landed<0>();
+  lds_read();
+  __builtin_amdgcn_s_barrier();
 }
 
 // Which of 16 registers' rows: register i of a block holds row 8 (i / 4) + 4 hb + i % 4.
@@ -115,7 +143,7 @@ template <typename T, int D, int G, bool STAT>
 __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
   using F = Form<T, D>;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2 buffers][K, V][TILE]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, hb = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const int inst = blockIdx.y, row0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileRows;    // the longest ones first
   const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kTileRows);
   const int rows = s.n * G;                                // of q
@@ -137,21 +165,26 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   float m = -INFINITY, sum = 0.f;                          // the sum over this lane's half of the cache rows
   const float scale = kLog2E / sqrtf((float)D);
 
+  const unsigned buffers = lds_address(s_tiles);
+  Places<T, D> next;
   if (s.tiles > 0) {
     const int t0 = s.tile(0) * F::TT;
-    fetch_tile<T, D, false>(a, a.K, inst, s, t0, s_tiles);
-    fetch_tile<T, D, true>(a, a.V, inst, s, t0, s_tiles + F::TILE);
+    next = places_of<T, D>(a, inst, s, t0, wave);
+    send_tile<T, D, false>(a.K, next, s, t0, wave, buffers);
+    send_tile<T, D, true>(a.V, next, s, t0, wave, buffers + F::TILE * 16);
+    next = places_of<T, D>(a, inst, s, s.tile(s.tiles > 1 ? 1 : 0) * F::TT, wave);
   }
   for (int u = 0; u < s.tiles; ++u) {
-    wait_tiles();                                          // ... and everybody is done with the other buffer
+    wait_tiles();
     const int t0 = s.tile(u) * F::TT;
     const u32x4* Kt = s_tiles + (u & 1) * 2 * F::TILE;
     const u32x4* Vt = Kt + F::TILE;
     if (u + 1 < s.tiles) {
-      u32x4* other = s_tiles + (~u & 1) * 2 * F::TILE;
+      const unsigned other = buffers + (~u & 1) * 2 * F::TILE * 16;
       const int t1 = s.tile(u + 1) * F::TT;
-      fetch_tile<T, D, false>(a, a.K, inst, s, t1, other);
-      fetch_tile<T, D, true>(a, a.V, inst, s, t1, other + F::TILE);
+      send_tile<T, D, false>(a.K, next, s, t1, wave, other);
+      send_tile<T, D, true>(a.V, next, s, t1, wave, other + F::TILE * 16);
+      next = places_of<T, D>(a, inst, s, s.tile(u + 2 < s.tiles ? u + 2 : u) * F::TT, wave);   // a tile ahead: the table's latency
     }
     float16v c[F::TB];
 #pragma unroll
@@ -172,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     for (int b = 0; b < F::TB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, c[b][i]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    top = max32(top);
     // The reference is a whole number in units of log2 (a change of it rounds nothing), 0 as long as nothing is seen.
     const float ref = fmaxf(m, ceilf(top * scale));
     if (__any(ref != m)) {
@@ -230,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     }
   }
 
-  sum += __shfl_xor(sum, 32, 64);
+  sum = sum32(sum);
   if (row >= rows) return;
   const float inv = sum > 0.f ? 1.f / sum : 0.f;           // a query that sees nothing has a zero output
   if (STAT && hb == 0) {
@@ -267,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
   constexpr int QT = F::TT;
   __shared__ __attribute__((aligned(16))) u32x4 s_q[2][F::TILE];
   __shared__ __attribute__((aligned(16))) float s_stat[2][QT][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, hb = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
   const int inst = blockIdx.y, chunk = blockIdx.z, t0 = (int)blockIdx.x * kTileRows;
   const int L = clamped(a.r.len[inst], 0, a.r.t_cap), nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
   if (t0 >= L) return;
@@ -291,13 +324,12 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
   float total = 0.f;
 
   auto fetch = [&](int r0, int buf) {
-    const int w = tid >> 6;
 #pragma unroll
     for (int l = 0; l < F::LOADS; ++l) {
-      const int first = (l * kWaves + w) * 64, x = first + lane, r = x / F::PIECES, p = F::k_place(r, x % F::PIECES);
+      const int r = (l * kWaves + wave) * F::RPL + lane / F::PIECES, p = F::k_place(r, lane % F::PIECES);
       const int row = r0 + r < rows ? r0 + r : rows - 1;
-      const u32x4* src = static_cast<const u32x4*>(a.q) + ((size_t)inst * a.q_cap * G + row) * F::PIECES + p;
-      __builtin_amdgcn_global_load_lds((gptr)src, (lptr)(&s_q[buf][first]), 16, 0, 0);
+      to_lds_from(static_cast<const u32x4*>(a.q) + ((size_t)inst * a.q_cap * G + row) * F::PIECES + p,
+                  lds_address(s_q[buf]) + (l * kWaves + wave) * 1024);
     }
     for (int x = tid; x < 2 * QT; x += kThreads) {
       const int row = r0 + x / 2;
@@ -331,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
     }
     total += part;
   }
-  total += __shfl_xor(total, 32, 64);
+  total = sum32(total);
   if (hb == 0 && mine) {
     if (a.chunks == 1) a.acc[(size_t)inst * a.r.t_cap + j] += total;
     else a.sums[((size_t)chunk * a.r.n_inst + inst) * a.r.t_cap + j] = total;
