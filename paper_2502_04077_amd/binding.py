@@ -111,10 +111,6 @@ def _ptr(t: torch.Tensor) -> int:
     return t.data_ptr()
 
 
-def _optr(t):
-    return None if t is None else _ptr(t)
-
-
 def _rptr(t: torch.Tensor) -> int:
     """A tensor a kernel may read: device memory, or pinned (device-mapped) host memory."""
     if not (t.is_cuda or t.is_pinned()) or not t.is_contiguous():
@@ -124,6 +120,10 @@ def _rptr(t: torch.Tensor) -> int:
 
 def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
+
+
+# The current stream of a device as a hipStream_t, without the object around it (which costs as much as a launch).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def stream_read(src: torch.Tensor, sink: torch.Tensor, n_workgroups: int) -> None:
@@ -148,7 +148,11 @@ class Context:
         _check(lib.ap_create(C.byref(self.cfg), C.byref(h)))
         self._h = h
         self._lib = lib
-        self._n_phys = 0          # pages of the pool that the block table points into; 0: the contiguous layout
+        # what the cache_* calls check their tensors against on every call
+        self._n, self._g, self._d, self._t_cap = n_inst, g, head_dim, t_cap
+        self._dtype = torch.bfloat16 if self.cfg.kv_dtype == AP_BF16 else torch.float32
+        self._kv_numel = n_inst * t_cap * head_dim
+        self._decode_ws = [self.cache_workspace_bytes(0, weights) for weights in (False, True)]
 
     def close(self):
         if getattr(self, "_h", None):
@@ -183,7 +187,7 @@ class Context:
     def set_block_table(self, table, n_phys_blocks: int = 0) -> None:
         """table: device int32 [n_inst][nb_cap] (kept alive by the caller), or None for the contiguous layout."""
         _check(self._lib.ap_set_block_table(self._h, None if table is None else _ptr(table), n_phys_blocks))
-        self._n_phys = 0 if table is None else n_phys_blocks
+        self._kv_numel = (self._n * self._t_cap if table is None else n_phys_blocks * self.cfg.block) * self._d
 
     def predict(self, hist, n_pushed, nb_cur, pred, ws) -> None:
         _check(self._lib.ap_predict(self._h, _ptr(hist), n_pushed, nb_cur, _ptr(pred), _ptr(ws), _stream()))
@@ -238,76 +242,80 @@ class Context:
         """Bytes of `ws` for cache_decode and cache_prefill of up to q_cap tokens; weights: with acc."""
         return int(self._lib.ap_cache_workspace_bytes(self._h, q_cap, int(bool(weights))))
 
-    def _kv_type(self):
-        return torch.bfloat16 if self.cfg.kv_dtype == AP_BF16 else torch.float32
-
-    def _cache_args(self, K, V, length, **more):
-        """Checks types, shapes and devices of what a cache_* call is given; returns the device whose current stream it uses.
-        more: name -> (tensor or None, dtype, shape), a shape of None taken as it is."""
-        c = self.cfg
-        if K.shape != V.shape or K.shape[-1:] != (c.head_dim,) or K.dtype != self._kv_type() or V.dtype != K.dtype:
+    def _cache_kv(self, K, V) -> int:
+        """Checks K and V; the index of the device they lie on."""
+        dev = K.get_device()
+        if K.shape != V.shape or K.shape[-1:] != (self._d,) or K.dtype is not self._dtype or V.dtype is not self._dtype:
             raise ValueError("K and V: two tensors [..., head_dim] of one shape, in the context's dtype")
-        rows = K.numel() // c.head_dim
-        if rows < (self._n_phys * c.block if self._n_phys else c.n_inst * c.t_cap):
+        if dev < 0 or V.get_device() != dev or not (K.is_contiguous() and V.is_contiguous()):
+            raise ValueError("K and V: expected contiguous tensors on one device")
+        if K.numel() < self._kv_numel:
             raise ValueError("K and V: fewer rows than the context's caches, or than the pages of its pool")
-        more["len"] = (length, torch.int32, (c.n_inst,))
-        for name, (t, dtype, shape) in more.items():
-            if t is None:
-                continue
-            if t.dtype != dtype or tuple(t.shape) != shape:
-                raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-            if t.device != K.device:
-                raise ValueError(f"{name} lies on {t.device}, K on {K.device}")
-        if V.device != K.device:
-            raise ValueError("K and V lie on different devices")
-        return K.device
+        return dev
 
     @staticmethod
-    def _cache_ws(ws, need, device):
-        if ws.device != device or ws.numel() * ws.element_size() < need:
-            raise ValueError(f"ws: expected {need} bytes on {device}")
+    def _cache_arg(name, t, dtype, shape, dev) -> int:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {dtype} {list(shape)} on device {dev}, got {t.dtype} {list(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    @staticmethod
+    def _cache_ws(ws, need, dev) -> int:
+        if ws.get_device() != dev or not ws.is_contiguous() or ws.numel() * ws.element_size() < need:
+            raise ValueError(f"ws: expected {need} bytes on device {dev}, contiguous")
+        return ws.data_ptr()
+
+    @staticmethod
+    def _cache_call(dev, call, *args) -> None:
+        """The call on the current stream of device `dev`, whichever device is current."""
+        if dev == torch.cuda.current_device():
+            rc = call(*args, _raw_stream(dev))
+        else:
+            with torch.cuda.device(dev):
+                rc = call(*args, _raw_stream(dev))
+        _check(rc)
 
     def cache_append(self, k_new, v_new, n_new, length, K, V) -> None:
         """k_new, v_new: [n_inst][q_cap][d]; n_new: int32 [n_inst] or None (q_cap each)."""
-        c, q_cap = self.cfg, k_new.shape[1] if k_new.dim() == 3 else 0
-        new = (c.n_inst, q_cap, c.head_dim)
-        dev = self._cache_args(K, V, length, k_new=(k_new, self._kv_type(), new), v_new=(v_new, self._kv_type(), new),
-                               n_new=(n_new, torch.int32, (c.n_inst,)))
-        with torch.cuda.device(dev):
-            _check(self._lib.ap_cache_append(self._h, _ptr(k_new), _ptr(v_new), _optr(n_new), q_cap, _ptr(length), _ptr(K), _ptr(V),
-                                             _stream()))
+        dev, arg = self._cache_kv(K, V), self._cache_arg
+        q_cap = k_new.shape[1] if k_new.dim() == 3 else 0
+        new = (self._n, q_cap, self._d)
+        self._cache_call(dev, self._lib.ap_cache_append, self._h, arg("k_new", k_new, self._dtype, new, dev),
+                         arg("v_new", v_new, self._dtype, new, dev),
+                         None if n_new is None else arg("n_new", n_new, torch.int32, (self._n,), dev), q_cap,
+                         arg("length", length, torch.int32, (self._n,), dev), K.data_ptr(), V.data_ptr())
 
     def cache_decode(self, q, K, V, length, window, n_first, out, acc, ws) -> None:
         """q: [n_inst][g][d]; out: float [n_inst][g][d]; acc: float [n_inst][t_cap] or None."""
-        c = self.cfg
-        shape = (c.n_inst, c.g, c.head_dim)
-        dev = self._cache_args(K, V, length, q=(q, self._kv_type(), shape), out=(out, torch.float32, shape),
-                               acc=(acc, torch.float32, (c.n_inst, c.t_cap)))
-        self._cache_ws(ws, self.cache_workspace_bytes(0, acc is not None), dev)
-        with torch.cuda.device(dev):
-            _check(self._lib.ap_cache_decode(self._h, _ptr(q), _ptr(K), _ptr(V), _ptr(length), window, n_first, _ptr(out), _optr(acc),
-                                             _ptr(ws), _stream()))
+        dev, arg = self._cache_kv(K, V), self._cache_arg
+        shape = (self._n, self._g, self._d)
+        self._cache_call(dev, self._lib.ap_cache_decode, self._h, arg("q", q, self._dtype, shape, dev), K.data_ptr(), V.data_ptr(),
+                         arg("length", length, torch.int32, (self._n,), dev), window, n_first,
+                         arg("out", out, torch.float32, shape, dev),
+                         None if acc is None else arg("acc", acc, torch.float32, (self._n, self._t_cap), dev),
+                         self._cache_ws(ws, self._decode_ws[acc is not None], dev))
 
     def cache_prefill(self, q, n_q, K, V, length, window, n_first, out, acc, ws) -> None:
         """q: [n_inst][q_cap][g][d]; n_q: int32 [n_inst] or None (q_cap each); out: as q; acc: float [n_inst][t_cap] or None."""
-        c, q_cap = self.cfg, q.shape[1] if q.dim() == 4 else 0
-        shape = (c.n_inst, q_cap, c.g, c.head_dim)
-        dev = self._cache_args(K, V, length, q=(q, self._kv_type(), shape), out=(out, self._kv_type(), shape),
-                               n_q=(n_q, torch.int32, (c.n_inst,)), acc=(acc, torch.float32, (c.n_inst, c.t_cap)))
-        self._cache_ws(ws, self.cache_workspace_bytes(q_cap, acc is not None), dev)
-        with torch.cuda.device(dev):
-            _check(self._lib.ap_cache_prefill(self._h, _ptr(q), _optr(n_q), q_cap, _ptr(K), _ptr(V), _ptr(length), window, n_first,
-                                              _ptr(out), _optr(acc), _ptr(ws), _stream()))
+        dev, arg = self._cache_kv(K, V), self._cache_arg
+        q_cap = q.shape[1] if q.dim() == 4 else 0
+        shape = (self._n, q_cap, self._g, self._d)
+        self._cache_call(dev, self._lib.ap_cache_prefill, self._h, arg("q", q, self._dtype, shape, dev),
+                         None if n_q is None else arg("n_q", n_q, torch.int32, (self._n,), dev), q_cap, K.data_ptr(), V.data_ptr(),
+                         arg("length", length, torch.int32, (self._n,), dev), window, n_first,
+                         arg("out", out, self._dtype, shape, dev),
+                         None if acc is None else arg("acc", acc, torch.float32, (self._n, self._t_cap), dev),
+                         self._cache_ws(ws, self.cache_workspace_bytes(q_cap, acc is not None), dev))
 
     def cache_evict(self, K, V, acc, length, budget, n_first, n_last, acc_out, len_out, kept) -> None:
         """acc_out may be acc, len_out may be length; kept: int32 [n_inst][budget]."""
-        c = self.cfg
-        rows = (c.n_inst, c.t_cap)
-        dev = self._cache_args(K, V, length, acc=(acc, torch.float32, rows), acc_out=(acc_out, torch.float32, rows),
-                               len_out=(len_out, torch.int32, (c.n_inst,)), kept=(kept, torch.int32, (c.n_inst, budget)))
-        with torch.cuda.device(dev):
-            _check(self._lib.ap_cache_evict(self._h, _ptr(K), _ptr(V), _ptr(acc), _ptr(length), budget, n_first, n_last, _ptr(acc_out),
-                                            _ptr(len_out), _ptr(kept), _stream()))
+        dev, arg = self._cache_kv(K, V), self._cache_arg
+        rows = (self._n, self._t_cap)
+        self._cache_call(dev, self._lib.ap_cache_evict, self._h, K.data_ptr(), V.data_ptr(), arg("acc", acc, torch.float32, rows, dev),
+                         arg("length", length, torch.int32, (self._n,), dev), budget, n_first, n_last,
+                         arg("acc_out", acc_out, torch.float32, rows, dev),
+                         arg("len_out", len_out, torch.int32, (self._n,), dev),
+                         arg("kept", kept, torch.int32, (self._n, budget), dev))
 
     def update_history(self, hist, n_pushed, row) -> None:
         _check(self._lib.ap_update_history(self._h, _ptr(hist), n_pushed, _ptr(row), _stream()))

@@ -69,7 +69,7 @@ template <typename F, bool IS_V> __device__ __forceinline__ void send(const void
 #pragma unroll
     for (int l = 0; l < F::N; ++l) {
       const int x = l * kWave + lane, r = x / F::PIECES, place = x % F::PIECES;
-      to_lds(base, r * row + (IS_V ? place : F::k_place(r, place)) * 16, lds + l * 1024);
+      to_lds<true>(base, r * row + (IS_V ? place : F::k_place(r, place)) * 16, lds + l * 1024);
     }
   } else {
     // Rows that are not seen are not read: another row of the group, which is, stands in for them.

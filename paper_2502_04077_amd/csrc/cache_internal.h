@@ -32,15 +32,15 @@ struct PrefillArgs {
   void* out;
   float* acc;
   float* stat;                  // workspace: [n_inst][q_cap * g][2] maximum and 1 / sum of every row, with acc only
-  float* sums;                  // workspace: [chunks][n_inst][t_cap] columns' sums over a chunk of the queries, with acc only
-  int chunks;
+  float* sums;                  // workspace: [chunks][n_inst][tiles][128] columns' sums over a chunk of the queries, with acc only
+  int chunks;                   // set by the launcher
 };
 
 constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call
 
 struct CacheWs { size_t before, whole, part_ml, part_acc, logits, total; };     // decode, in bytes
 CacheWs cache_decode_ws(const Shape& s, bool weights);
-struct CacheQWs { size_t stat, sums, total; int chunks; };                       // prefill, in bytes
+struct CacheQWs { size_t stat, sums, total; };                                   // prefill, in bytes
 CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights);
 
 hipError_t launch_cache_append(const Shape& s, const CacheRows& r, const void* k_new, const void* v_new, const int32_t* n_new, int q_cap,

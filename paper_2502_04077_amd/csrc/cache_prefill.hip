@@ -14,7 +14,8 @@ namespace ap {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kTileRows = 128;               // rows of q per workgroup
+constexpr int kTileRows = 128;               // rows of q per workgroup; of the cache, for the columns' sums
+constexpr int kColumnWgs = 2048;             // workgroups of the columns' sums that fill the chip
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -98,7 +99,7 @@ __device__ __forceinline__ void send_tile(const void* X, const Places<T, D>& at,
     const int p = IS_V ? F::v_place(run + in, place) : F::k_place(run + in, place);
     const unsigned to = lds + (l * kWaves + wave) * 1024;
     if (at.alt[l] < 0) {
-      to_lds(static_cast<const char*>(X) + (at.at[l] + t0 + run) * bytes, in * bytes + p * 16, to);
+      to_lds<false>(static_cast<const char*>(X) + (at.at[l] + t0 + run) * bytes, in * bytes + p * 16, to);
     } else {
       int j = t0 + run + in;
       if (j > s.p1 || (j >= s.f && j < s.lo0)) j = at.alt[l];
@@ -291,22 +292,38 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     }
 }
 
+// Tiles of kTileRows cache rows that an instance's queries see: rows [0, f) and [lo, L), f <= lo.
+struct Columns {
+  int L, nq, base, tiles, ts, tb;
+  __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
+};
+__device__ __forceinline__ Columns columns_of(const PrefillArgs& a, int inst) {
+  Columns c;
+  c.L = clamped(a.r.len[inst], 0, a.r.t_cap);
+  c.nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
+  c.base = c.L - c.nq;
+  const int lo = a.window > 0 && c.base >= a.window ? c.base - a.window + 1 : 0, f = a.n_first < lo ? a.n_first : lo;
+  c.ts = (f + kTileRows - 1) / kTileRows;
+  c.tb = lo / kTileRows > c.ts ? lo / kTileRows : c.ts;
+  c.tiles = c.L == 0 || c.nq == 0 ? 0 : c.ts + ((c.L - 1) / kTileRows >= c.tb ? (c.L - 1) / kTileRows - c.tb + 1 : 0);
+  return c;
+}
+
 // Sums of the columns of P over a chunk of the query rows.  A workgroup has 128 cache rows, 32 a wave, held as operands; the queries go
-// through LDS, 64 rows (fp32: 32) at a time.  The product is q K^T this way round: a lane has scores of one cache row, and its sum
-// is taken in registers.
+// through LDS, 64 rows (fp32: 32) at a time.  A lane has scores of one query row, whose statistics are two registers, and of 16 cache
+// rows, whose sums stay in registers to the end.
 template <typename T, int D, int G>
 __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) {
   using F = Form<T, D>;
   constexpr int QT = F::TT;
   __shared__ __attribute__((aligned(16))) u32x4 s_q[2][F::TILE];
-  __shared__ __attribute__((aligned(16))) float s_stat[2][QT][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
-  const int inst = blockIdx.y, chunk = blockIdx.z, t0 = (int)blockIdx.x * kTileRows;
-  const int L = clamped(a.r.len[inst], 0, a.r.t_cap), nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
-  if (t0 >= L) return;
-  const int base = L - nq, rows = nq * G;
+  const int inst = blockIdx.y, chunk = blockIdx.z;
+  const Columns col = columns_of(a, inst);
+  if ((int)blockIdx.x >= col.tiles) return;
+  const int t0 = col.tile(blockIdx.x) * kTileRows, L = col.L, base = col.base, rows = col.nq * G;
   // Rows of q in this chunk, whole tiles of them, that see one of the cache rows at least.
-  const int all_tiles = (a.q_cap * G + QT - 1) / QT, each = (all_tiles + a.chunks - 1) / a.chunks;
+  const int all_tiles = (rows + QT - 1) / QT, each = (all_tiles + a.chunks - 1) / a.chunks;
   int begin = chunk * each * QT, end = begin + each * QT < rows ? begin + each * QT : rows;
   const int first_q = t0 - base > 0 ? t0 - base : 0;                          // the first query that lies at t0 or behind it
   if (begin < first_q * G) begin = first_q * G / QT * QT;
@@ -314,73 +331,134 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
     const long long last_q = (long long)t0 + kTileRows - 1 + a.window - 1 - base;
     if ((last_q + 1) * G < end) end = (int)((last_q + 1) * G);
   }
-  const int j = t0 + 32 * wave + n;                        // this lane's cache row
-  const bool mine = j < L;
-  const size_t k_row = row_at(a.r, inst, mine ? j : L - 1);
+  const int j0 = t0 + 32 * wave;                           // this wave's cache rows
   u32x4 kf[F::KS];
+  {
+    const int j = j0 + n < L ? j0 + n : L - 1;
+    const u32x4* k = static_cast<const u32x4*>(a.K) + row_at(a.r, inst, j) * F::PIECES + hb;
 #pragma unroll
-  for (int k = 0; k < F::KS; ++k) kf[k] = static_cast<const u32x4*>(a.K)[k_row * F::PIECES + 2 * k + hb];
+    for (int x = 0; x < F::KS; ++x) kf[x] = k[2 * x];
+  }
   const float scale = kLog2E / sqrtf((float)D);
-  float total = 0.f;
-
+  float total[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) total[i] = 0.f;
+  const size_t q0 = (size_t)inst * a.q_cap * G;
+  const unsigned lds = lds_address(s_q);
   auto fetch = [&](int r0, int buf) {
 #pragma unroll
     for (int l = 0; l < F::LOADS; ++l) {
       const int r = (l * kWaves + wave) * F::RPL + lane / F::PIECES, p = F::k_place(r, lane % F::PIECES);
       const int row = r0 + r < rows ? r0 + r : rows - 1;
-      to_lds_from(static_cast<const u32x4*>(a.q) + ((size_t)inst * a.q_cap * G + row) * F::PIECES + p,
-                  lds_address(s_q[buf]) + (l * kWaves + wave) * 1024);
-    }
-    for (int x = tid; x < 2 * QT; x += kThreads) {
-      const int row = r0 + x / 2;
-      s_stat[buf][x / 2][x % 2] = row < rows ? a.stat[((size_t)inst * a.q_cap * G + row) * 2 + x % 2] : 0.f;
+      to_lds_from(static_cast<const u32x4*>(a.q) + (q0 + row) * F::PIECES + p, lds + (buf * F::TILE + (l * kWaves + wave) * 64) * 16);
     }
   };
-  if (begin < end) fetch(begin, 0);
+  struct Stat { float m, inv; };
+  auto stat_of = [&](int row) {
+    return *reinterpret_cast<const Stat*>(a.stat + (q0 + (row < rows ? row : rows - 1)) * 2);
+  };
+  Stat next[F::TB];
+  if (begin < end) {
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b) next[b] = stat_of(begin + 32 * b + n);
+    fetch(begin, 0);
+  }
   int buf = 0;
   for (int r0 = begin; r0 < end; r0 += QT, buf ^= 1) {
-    wait_tiles();
-    if (r0 + QT < end) fetch(r0 + QT, buf ^ 1);
-    const int p0 = base + r0 / G;
-    const int r_last = r0 + QT < rows ? r0 + QT - 1 : rows - 1, p1 = base + r_last / G;
-    const bool all = t0 + kTileRows - 1 <= p0 && t0 + kTileRows <= L && r0 + QT <= rows &&
-                     (a.window <= 0 || t0 > p1 - a.window || t0 + kTileRows <= a.n_first);
-    float part = 0.f;
+    Stat st[F::TB];
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) {
-      const float16v c = product<T, D>(s_q[buf], 32 * b, kf);
+      st[b] = next[b];
+      if (r0 + 32 * b + n >= rows) st[b].inv = 0.f;        // no row of q: counts nothing
+    }
+    wait_tiles();
+    if (r0 + QT < end) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = 32 * b + reg_row(i, hb);
-        float w = exp2_fast(__builtin_fmaf(c[i], scale, -s_stat[buf][r][0])) * s_stat[buf][r][1];
-        if (!all) {
-          const int p = base + (r0 + r) / G;
-          const bool seen = r0 + r < rows && j <= p && (a.window <= 0 || j > p - a.window || j < a.n_first);
-          w = seen ? w : 0.f;
+      for (int b = 0; b < F::TB; ++b) next[b] = stat_of(r0 + QT + 32 * b + n);
+      fetch(r0 + QT, buf ^ 1);
+    }
+    const int r_last = r0 + QT < rows ? r0 + QT - 1 : rows - 1;
+    const bool all = j0 + 31 <= base + r0 / G && (a.window <= 0 || j0 > base + r_last / G - a.window || j0 + 32 <= a.n_first);
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b) {
+      float16v c;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < F::KS; ++k) {
+        const u32x4 x = s_q[buf][(32 * b + n) * F::PIECES + F::k_place(32 * b + n, 2 * k + hb)];
+        if constexpr (sizeof(T) == 2) {
+          c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[k]), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k][e]), __uint_as_float(x[e]), c, 0, 0, 0);
         }
-        part += w;
+      }
+      if (all) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          total[i] = __builtin_fmaf(exp2_fast(__builtin_fmaf(c[i], scale, -st[b].m)), st[b].inv, total[i]);
+      } else {
+        const int p = base + (r0 + 32 * b + n) / G;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + reg_row(i, hb);
+          const bool seen = j <= p && (a.window <= 0 || j > p - a.window || j < a.n_first);
+          const float w = exp2_fast(__builtin_fmaf(c[i], scale, -st[b].m)) * st[b].inv;
+          total[i] += seen && st[b].inv > 0.f ? w : 0.f;
+        }
       }
     }
-    total += part;
   }
-  total = sum32(total);
-  if (hb == 0 && mine) {
-    if (a.chunks == 1) a.acc[(size_t)inst * a.r.t_cap + j] += total;
-    else a.sums[((size_t)chunk * a.r.n_inst + inst) * a.r.t_cap + j] = total;
+  // The lanes of a half have the same cache rows.
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    total[i] = lane_group_sum<16>(total[i]);
+    total[i] = sum16(total[i]);
+  }
+  if (n == 0) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int j = j0 + reg_row(i, hb);
+      if (j >= L) continue;
+      if (a.chunks == 1) a.acc[(size_t)inst * a.r.t_cap + j] += total[i];
+      else a.sums[(((size_t)chunk * a.r.n_inst + inst) * gridDim.x + blockIdx.x) * kTileRows + j - t0] = total[i];
+    }
   }
 }
 
 // The chunks' sums, one after the other, so that the result does not depend on which was ready first.
-__global__ __launch_bounds__(kThreads) void cache_weights_add_kernel(PrefillArgs a) {
-  const int i = blockIdx.y, j = blockIdx.x * kThreads + threadIdx.x;
-  const int L = clamped(a.r.len[i], 0, a.r.t_cap);
-  if (j >= L) return;
+__global__ __launch_bounds__(kTileRows) void cache_weights_add_kernel(PrefillArgs a) {
+  const int inst = blockIdx.y;
+  const Columns col = columns_of(a, inst);
+  if ((int)blockIdx.x >= col.tiles) return;
+  const int j = col.tile(blockIdx.x) * kTileRows + threadIdx.x;
+  if (j >= col.L) return;
   float x = 0.f;
-  for (int c = 0; c < a.chunks; ++c) x += a.sums[((size_t)c * a.r.n_inst + i) * a.r.t_cap + j];
-  a.acc[(size_t)i * a.r.t_cap + j] += x;
+#pragma unroll 8
+  for (int c = 0; c < a.chunks; ++c)
+    x += a.sums[(((size_t)c * a.r.n_inst + inst) * gridDim.x + blockIdx.x) * kTileRows + threadIdx.x];
+  a.acc[(size_t)inst * a.r.t_cap + j] += x;
 }
 
-template <typename T, int D, int G> hipError_t run(const PrefillArgs& a, hipStream_t st) {
+// Most tiles of cache rows that an instance's queries can see.
+static long long most_columns(const Shape& s, int q_cap, int window, int n_first) {
+  const long long all = ((long long)s.t_cap + kTileRows - 1) / kTileRows;
+  if (window <= 0) return all;
+  const long long some = ((long long)n_first + kTileRows - 1) / kTileRows + ((long long)window + q_cap) / kTileRows + 2;
+  return some < all ? some : all;
+}
+// Workgroups of the columns' sums: chunks of the query rows, of at least 512 rows, where the tiles alone are few for the chip.
+static int column_chunks(const Shape& s, int q_cap, long long columns) {
+  const long long q_rows = (long long)q_cap * s.g;
+  long long chunks = (kColumnWgs + s.n_inst * columns - 1) / (s.n_inst * columns);
+  if (chunks > (q_rows + 511) / 512) chunks = (q_rows + 511) / 512;
+  if (chunks > 16) chunks = 16;
+  return (int)chunks;
+}
+
+template <typename T, int D, int G> hipError_t run(const Shape& s, const PrefillArgs& a, hipStream_t st) {
   const size_t lds = (size_t)4 * Form<T, D>::TILE * 16;
   const unsigned tiles = (unsigned)(((long long)a.q_cap * G + kTileRows - 1) / kTileRows);
   const dim3 grid(tiles, a.r.n_inst);
@@ -391,14 +469,15 @@ template <typename T, int D, int G> hipError_t run(const PrefillArgs& a, hipStre
   cache_prefill_kernel<T, D, G, true><<<grid, kThreads, lds, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  cache_weights_kernel<T, D, G><<<dim3((a.r.t_cap + kTileRows - 1) / kTileRows, a.r.n_inst, a.chunks), kThreads, 0, st>>>(a);
+  const dim3 columns((unsigned)most_columns(s, a.q_cap, a.window, a.n_first), a.r.n_inst, a.chunks);
+  cache_weights_kernel<T, D, G><<<columns, kThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.chunks == 1) return e;
-  cache_weights_add_kernel<<<dim3((a.r.t_cap + kThreads - 1) / kThreads, a.r.n_inst), kThreads, 0, st>>>(a);
+  cache_weights_add_kernel<<<dim3(columns.x, columns.y), kTileRows, 0, st>>>(a);
   return hipGetLastError();
 }
-template <typename T, int D> hipError_t run_g(int g, const PrefillArgs& a, hipStream_t st) {
-  return g == 1 ? run<T, D, 1>(a, st) : g == 2 ? run<T, D, 2>(a, st) : g == 4 ? run<T, D, 4>(a, st) : run<T, D, 8>(a, st);
+template <typename T, int D> hipError_t run_g(const Shape& s, const PrefillArgs& a, hipStream_t st) {
+  return s.g == 1 ? run<T, D, 1>(s, a, st) : s.g == 2 ? run<T, D, 2>(s, a, st) : s.g == 4 ? run<T, D, 4>(s, a, st) : run<T, D, 8>(s, a, st);
 }
 
 }  // namespace
@@ -407,21 +486,18 @@ CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
   CacheQWs w;
   size_t o = 0;
   auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
-  // Query rows are cut into chunks where cache tiles alone would leave CUs without work, not below 512 rows each.
-  const long long tiles = (long long)s.n_inst * ((s.t_cap + kTileRows - 1) / kTileRows), q_rows = (long long)q_cap * s.g;
-  long long chunks = (2048 + tiles - 1) / tiles;
-  if (chunks > (q_rows + 511) / 512) chunks = (q_rows + 511) / 512;
-  if (chunks > 16) chunks = 16;
-  w.chunks = chunks < 1 ? 1 : (int)chunks;
-  w.stat = take(weights ? (size_t)s.n_inst * q_rows * 2 * 4 : 0);
-  w.sums = take(weights && w.chunks > 1 ? (size_t)w.chunks * s.n_inst * s.t_cap * 4 : 0);
+  w.stat = take(weights ? (size_t)s.n_inst * q_cap * s.g * 2 * 4 : 0);
+  // (chunks x instances x tiles, whatever the window: more than one chunk only below kColumnWgs workgroups)
+  w.sums = take(weights ? (size_t)(2 * kColumnWgs) * kTileRows * 4 : 0);
   w.total = o;
   return w;
 }
 
-hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& a, hipStream_t st) {
-  if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s.g, a, st) : run_g<bf16_t, 64>(s.g, a, st);
-  return s.d == 128 ? run_g<float, 128>(s.g, a, st) : run_g<float, 64>(s.g, a, st);
+hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) {
+  PrefillArgs a = args;
+  a.chunks = a.acc == nullptr ? 1 : column_chunks(s, a.q_cap, most_columns(s, a.q_cap, a.window, a.n_first));
+  if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s, a, st) : run_g<bf16_t, 64>(s, a, st);
+  return s.d == 128 ? run_g<float, 128>(s, a, st) : run_g<float, 64>(s, a, st);
 }
 
 }  // namespace ap

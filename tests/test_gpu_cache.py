@@ -184,6 +184,8 @@ EVICT = [
     (128, 16, "f32", True, 512, 300, 300, 0, [512, 301, 4]),
     (128, 64, "bf16", True, 5120, 1, 0, 1, [5120, 2, 1, 0]),
     (64, 8, "bf16", True, 3000, 2900, 1, 1, [3000, 2901, 2950]),
+    (64, 16, "bf16", False, 65536 + 128, 5000, 33, 70, [65536 + 128, 65536 + 103, 65535, 5001, 10000]),
+    (64, 64, "bf16", True, 140032, 1024, 64, 64, [140000, 131072, 70000]),
 ]
 
 
