@@ -33,7 +33,7 @@ struct PrefillArgs {
   float* acc;
   float* stat;                  // workspace: [n_inst][q_cap * g][2] maximum and 1 / sum of every row, with acc only
   float* sums;                  // workspace: [chunks][n_inst][tiles][128] columns' sums over a chunk of the queries, with acc only
-  int chunks;                   // set by the launcher
+  int chunks, tiles;            // set by the launcher: chunks of the queries; tiles of rows of q an instance
 };
 
 constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call

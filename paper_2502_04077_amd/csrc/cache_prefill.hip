@@ -30,10 +30,14 @@ template <typename T, int D> struct Form {
   static constexpr int LOADS = TT * PIECES / kThreads;     // pieces a thread fetches of a tile of K, or V
   static constexpr int TILE = TT * PIECES;                 // pieces of a tile
   static constexpr int RPL = 64 / PIECES;                  // rows that a wave fetches with a load
+  static constexpr int RW = TT / kWaves;                   // rows of a tile that a wave fetches
+  static_assert(RPL * LOADS == RW, "a wave's rows");
   // Piece p of row r lies at place p ^ swizzle(r) of the row, so that the lanes of one LDS cycle use different banks: K is read a row
-  // per lane, V (16 bits) in blocks of four rows by two pieces.
+  // per lane, V (16 bits) in blocks of four rows by four pieces, half a wave at a time.
   __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
-  __device__ static __forceinline__ int v_place(int r, int p) { return sizeof(T) == 2 ? p ^ ((2 * r) & (PIECES - 1)) : p; }
+  __device__ static __forceinline__ int v_place(int r, int p) {
+    return sizeof(T) == 2 ? p ^ (PIECES == 16 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) : p;
+  }
 };
 
 // What the queries of a tile see of an instance.
@@ -63,47 +67,64 @@ __device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, 
   return s;
 }
 
-// Where the rows lie that this wave fetches of a tile: LOADS runs of RPL rows, each of them in one page.  Rows that no query of the tile sees
-// are not read: row `alt`, which is seen, stands in for them.  Wave-uniform.
-template <typename T, int D> struct Places {
-  size_t at[Form<T, D>::LOADS];                            // row j of the run lies at at + j
-  int alt[Form<T, D>::LOADS];                              // -1: all of the run is seen
+// A wave fetches RW consecutive rows of a tile, which lie in one page, or in two of eight rows.  Rows that no query of the tile sees are not
+// read: row `alt`, which is seen, stands in for them, and may be any row of the cache.  Wave-uniform.
+struct Run {
+  const char *k, *v;                                       // row 0 of the run, as if all of it lay together
+  long long second;                                        // and what to add for its second eight rows, in bytes
+  bool all;
+  int j0, alt;
 };
-template <typename T, int D>
-__device__ __forceinline__ Places<T, D> places_of(const PrefillArgs& a, int inst, const Span& s, int t0, int wave) {
-  using F = Form<T, D>;
-  Places<T, D> x;
-#pragma unroll
-  for (int l = 0; l < F::LOADS; ++l) {
-    const int g0 = t0 + (l * kWaves + wave) * F::RPL;
-    const bool all = g0 + F::RPL - 1 <= s.p1 && (g0 >= s.lo0 || g0 + F::RPL <= s.f);
-    int alt = g0;                                          // a row of the run that is seen, or one of another run
-    if (g0 >= s.f) alt = g0 > s.lo0 ? g0 : s.lo0;
-    const bool none = alt > s.p1 || alt >= g0 + F::RPL;
-    if (none) alt = s.p1;
-    const int eight = (none ? s.p1 : g0) & ~7;
-    x.at[l] = rows_at(a.r, inst, eight) - eight;
-    x.alt[l] = all ? -1 : alt;
+// The instance's part of the table, looked up through the scalar cache.
+struct Pages {
+  const __attribute__((address_space(4))) int32_t* table;  // of this instance, or null
+  size_t row0;                                             // contiguous: the instance's first row
+  int lb, nb_cap, n_phys;
+  __device__ __forceinline__ size_t at(int j) const {      // of row j, a multiple of 8
+    if (table == nullptr) return row0 + j;
+    const int block = j >> lb;
+    const int page = clamped(table[block < nb_cap ? block : nb_cap - 1], 0, n_phys - 1);
+    return ((size_t)page << lb) + (j & ((1 << lb) - 1));
   }
+};
+__device__ __forceinline__ Pages pages_of(const CacheRows& r, int inst) {
+  Pages p;
+  p.table = r.table == nullptr ? nullptr : (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(r.table + (size_t)inst * r.nb_cap);
+  p.row0 = (size_t)inst * r.t_cap;
+  p.lb = r.lb; p.nb_cap = r.nb_cap; p.n_phys = r.n_phys;
+  return p;
+}
+template <typename F> __device__ __forceinline__ Run run_of(const PrefillArgs& a, const Pages& pages, const Span& s, int t0, int wave) {
+  constexpr size_t bytes = F::PIECES * 16;
+  Run x;
+  x.j0 = t0 + wave * F::RW;
+  x.all = x.j0 + F::RW - 1 <= s.p1 && (x.j0 >= s.lo0 || x.j0 + F::RW <= s.f);
+  int alt = x.j0;                                          // a row of the run that is seen, or one of another run
+  if (x.j0 >= s.f) alt = x.j0 > s.lo0 ? x.j0 : s.lo0;
+  if (alt > s.p1) alt = s.p1;
+  x.alt = alt;
+  const size_t at = pages.at(x.j0);
+  x.k = static_cast<const char*>(a.K) + at * bytes;
+  x.v = static_cast<const char*>(a.V) + at * bytes;
+  x.second = F::RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(x.j0 + 8) - at) - 8) * (long long)bytes : 0;
   return x;
 }
-// Sends a tile of rows [t0, t0 + TT) of X to LDS: the lane chooses the piece, so that it lies where the swizzle says.
-template <typename T, int D, bool IS_V>
-__device__ __forceinline__ void send_tile(const void* X, const Places<T, D>& at, const Span& s, int t0, int wave, unsigned lds) {
-  using F = Form<T, D>;
+// Sends a tile of K (or V) to LDS: the lane chooses the piece, so that it lies where the swizzle says.
+template <typename F, bool IS_V>
+__device__ __forceinline__ void send_tile(const PrefillArgs& a, int inst, const Run& run, const Span& s, int wave, unsigned lds) {
   constexpr unsigned bytes = F::PIECES * 16;
   const int lane = threadIdx.x & 63;
+  const unsigned to = lds + wave * F::LOADS * 1024;
 #pragma unroll
   for (int l = 0; l < F::LOADS; ++l) {
-    const int run = (l * kWaves + wave) * F::RPL, in = lane / F::PIECES, place = lane % F::PIECES;
-    const int p = IS_V ? F::v_place(run + in, place) : F::k_place(run + in, place);
-    const unsigned to = lds + (l * kWaves + wave) * 1024;
-    if (at.alt[l] < 0) {
-      to_lds<false>(static_cast<const char*>(X) + (at.at[l] + t0 + run) * bytes, in * bytes + p * 16, to);
+    const int r = l * F::RPL + lane / F::PIECES, place = lane % F::PIECES;           // of the run; it begins at a multiple of RW rows
+    const int p = IS_V ? F::v_place(r, place) : F::k_place(wave * F::RW + r, place);
+    if (run.all) {
+      to_lds<false>((IS_V ? run.v : run.k) + (l >= F::LOADS / 2 ? run.second : 0), r * bytes + p * 16, to + l * 1024);
     } else {
-      int j = t0 + run + in;
-      if (j > s.p1 || (j >= s.f && j < s.lo0)) j = at.alt[l];
-      to_lds_from(static_cast<const char*>(X) + (at.at[l] + j) * bytes + p * 16, to);
+      int j = run.j0 + r;
+      if (j > s.p1 || (j >= s.f && j < s.lo0)) j = run.alt;
+      to_lds_from(static_cast<const char*>(IS_V ? a.V : a.K) + row_at(a.r, inst, j) * bytes + p * 16, to + l * 1024);
     }
   }
 }
@@ -140,12 +161,26 @@ __device__ __forceinline__ void wait_tiles() {
 // Which of 16 registers' rows: register i of a block holds row 8 (i / 4) + 4 hb + i % 4.
 __device__ __forceinline__ int reg_row(int i, int hb) { return 8 * (i >> 2) + 4 * hb + (i & 3); }
 
+// Workgroup b of tiles * n_inst: which instance and which tile.  Consecutive workgroups go to the 8 XCDs in turn, so instances are dealt
+// eight at a time, one an XCD, whose L2 then serves one instance's K and V; the fewer than eight that are left share the XCDs.
+struct Work { int inst, tile; };
+__device__ __forceinline__ Work work_of(unsigned b, int tiles, int n_inst) {
+  const unsigned whole = (unsigned)n_inst / 8 * 8, rest = (unsigned)n_inst - whole;
+  if (b < whole * (unsigned)tiles) {
+    const unsigned eight = b / (8u * tiles), x = b % (8u * tiles);
+    return {(int)(eight * 8 + x % 8), (int)(x / 8)};
+  }
+  const unsigned x = b - whole * (unsigned)tiles;
+  return {(int)(whole + x % rest), (int)(x / rest)};
+}
+
 template <typename T, int D, int G, bool STAT>
 __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
   using F = Form<T, D>;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2 buffers][K, V][TILE]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
-  const int inst = blockIdx.y, row0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileRows;    // the longest ones first
+  const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
+  const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kTileRows;            // the longest ones first
   const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kTileRows);
   const int rows = s.n * G;                                // of q
   if (row0 >= rows) return;
@@ -167,13 +202,13 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   const float scale = kLog2E / sqrtf((float)D);
 
   const unsigned buffers = lds_address(s_tiles);
-  Places<T, D> next;
+  const Pages pages = pages_of(a.r, inst);
+  Run next;
   if (s.tiles > 0) {
-    const int t0 = s.tile(0) * F::TT;
-    next = places_of<T, D>(a, inst, s, t0, wave);
-    send_tile<T, D, false>(a.K, next, s, t0, wave, buffers);
-    send_tile<T, D, true>(a.V, next, s, t0, wave, buffers + F::TILE * 16);
-    next = places_of<T, D>(a, inst, s, s.tile(s.tiles > 1 ? 1 : 0) * F::TT, wave);
+    next = run_of<F>(a, pages, s, s.tile(0) * F::TT, wave);
+    send_tile<F, false>(a, inst, next, s, wave, buffers);
+    send_tile<F, true>(a, inst, next, s, wave, buffers + F::TILE * 16);
+    next = run_of<F>(a, pages, s, s.tile(s.tiles > 1 ? 1 : 0) * F::TT, wave);
   }
   for (int u = 0; u < s.tiles; ++u) {
     wait_tiles();
@@ -182,10 +217,9 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     const u32x4* Vt = Kt + F::TILE;
     if (u + 1 < s.tiles) {
       const unsigned other = buffers + (~u & 1) * 2 * F::TILE * 16;
-      const int t1 = s.tile(u + 1) * F::TT;
-      send_tile<T, D, false>(a.K, next, s, t1, wave, other);
-      send_tile<T, D, true>(a.V, next, s, t1, wave, other + F::TILE * 16);
-      next = places_of<T, D>(a, inst, s, s.tile(u + 2 < s.tiles ? u + 2 : u) * F::TT, wave);   // a tile ahead: the table's latency
+      send_tile<F, false>(a, inst, next, s, wave, other);
+      send_tile<F, true>(a, inst, next, s, wave, other + F::TILE * 16);
+      next = run_of<F>(a, pages, s, s.tile(u + 2 < s.tiles ? u + 2 : u) * F::TT, wave);     // a tile ahead: the table's latency
     }
     float16v c[F::TB];
 #pragma unroll
@@ -348,9 +382,9 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
   auto fetch = [&](int r0, int buf) {
 #pragma unroll
     for (int l = 0; l < F::LOADS; ++l) {
-      const int r = (l * kWaves + wave) * F::RPL + lane / F::PIECES, p = F::k_place(r, lane % F::PIECES);
+      const int r = wave * F::RW + l * F::RPL + lane / F::PIECES, p = F::k_place(r, lane % F::PIECES);
       const int row = r0 + r < rows ? r0 + r : rows - 1;
-      to_lds_from(static_cast<const u32x4*>(a.q) + (q0 + row) * F::PIECES + p, lds + (buf * F::TILE + (l * kWaves + wave) * 64) * 16);
+      to_lds_from(static_cast<const u32x4*>(a.q) + (q0 + row) * F::PIECES + p, lds + (buf * F::TILE + (wave * F::LOADS + l) * 64) * 16);
     }
   };
   struct Stat { float m, inv; };
@@ -460,8 +494,7 @@ static int column_chunks(const Shape& s, int q_cap, long long columns) {
 
 template <typename T, int D, int G> hipError_t run(const Shape& s, const PrefillArgs& a, hipStream_t st) {
   const size_t lds = (size_t)4 * Form<T, D>::TILE * 16;
-  const unsigned tiles = (unsigned)(((long long)a.q_cap * G + kTileRows - 1) / kTileRows);
-  const dim3 grid(tiles, a.r.n_inst);
+  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst);
   if (a.acc == nullptr) {
     cache_prefill_kernel<T, D, G, false><<<grid, kThreads, lds, st>>>(a);
     return hipGetLastError();
@@ -495,6 +528,8 @@ CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
 
 hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) {
   PrefillArgs a = args;
+  a.tiles = (int)(((long long)a.q_cap * s.g + kTileRows - 1) / kTileRows);
+  if ((long long)a.tiles * s.n_inst > 0x7fffffffll) return hipErrorInvalidValue;
   a.chunks = a.acc == nullptr ? 1 : column_chunks(s, a.q_cap, most_columns(s, a.q_cap, a.window, a.n_first));
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s, a, st) : run_g<bf16_t, 64>(s, a, st);
   return s.d == 128 ? run_g<float, 128>(s, a, st) : run_g<float, 64>(s, a, st);
