@@ -43,7 +43,9 @@ template <typename T, int D, int G> struct Form {
   static constexpr int N = PIECES / 4;                     // pieces of a group's K (or V) per lane
   static constexpr int RPL = kWave / PIECES;               // V rows that a wave reads at a time
   static constexpr int TILE = kGroup * PIECES;             // pieces of a group's K (or V)
-  static constexpr int BUFFERS = kWaves * 2 * 2 * TILE * 16;           // bytes of LDS: every wave has two groups of K and V
+  static constexpr int QUERIES = (G * PIECES + kWave - 1) / kWave;     // loads of a wave for the queries
+  static constexpr int WAVE = 4 * TILE + QUERIES * kWave;              // pieces of LDS of a wave: two groups of K and V, and the queries
+  static constexpr int BUFFERS = kWaves * WAVE * 16;
   static constexpr int PER_CU = PIECES == 8 ? 4 : (PIECES == 16 ? 2 : 1);   // workgroups a CU, as LDS has room for
   static constexpr int WGS = 256 * PER_CU;                 // the workgroups that 256 CUs hold at once
   static_assert(WGS <= kCacheDecodeWgs && PER_CU * (BUFFERS + 4096) <= 160 * 1024, "workspace, LDS");
@@ -87,7 +89,7 @@ template <typename F, bool IS_V> __device__ __forceinline__ void send(const void
 template <typename T, int D, int G, bool ACC>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(DecodeArgs a) {
   using F = Form<T, D, G>;
-  extern __shared__ __attribute__((aligned(16))) u32x4 s_rows[];          // [wave][buffer][K, V][TILE]; at the end outputs, [wave][G][D]
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_rows[];          // [wave]: [buffer][K, V][TILE], queries; at the end outputs, [G][D]
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
   __shared__ unsigned long long s_wave[kWaves];
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   unsigned long long left = end - begin;
 
   const float scale = kLog2E / sqrtf((float)D);
-  const u32x4* mine_rows = s_rows + wave * 4 * F::TILE;
+  const u32x4* mine_rows = s_rows + wave * F::WAVE;
   const unsigned ring = lds_address(mine_rows);
   float* s_out = reinterpret_cast<float*>(s_rows);
   for (; left > 0; ++inst, from = 0) {
@@ -157,6 +159,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     const int u0 = from + wave;
     Place next[2];                                         // of the groups behind the ones that were sent for
     if (mine_n > 0) {
+#pragma unroll
+      for (int x = 0; x < F::QUERIES; ++x) {
+        const int piece = x * kWave + lane;
+        to_lds<false>(static_cast<const u32x4*>(a.q) + (size_t)inst * G * F::PIECES, (piece < G * F::PIECES ? piece : 0) * 16,
+                      ring + (4 * F::TILE + x * kWave) * 16);
+      }
       const Place p = place_of(a.r, inst, s, u0), p1 = place_of(a.r, inst, s, mine_n > 1 ? u0 + kWaves : u0);
       send<F, false>(a.K, p, s, lane, ring);
       send<F, true>(a.V, p, s, lane, ring + F::TILE * 16);
@@ -166,12 +174,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       }
       next[0] = p; next[1] = p1;
     }
-    // B operand of the products q . K: lane (head, kg) has piece 4 l + kg of the head's query; heads beyond g are zero.
+    // B operand of the products q . K: lane (head, kg) has piece 4 l + kg of the head's query; heads beyond g count for nothing.  The queries
+    // were sent for first.
     u32x4 qf[F::N];
+    if (mine_n > 1) landed<4 * F::N>(); else landed<2 * F::N>();
 #pragma unroll
     for (int l = 0; l < F::N; ++l) {
-      const u32x4 zero = {0u, 0u, 0u, 0u};
-      qf[l] = head < G ? static_cast<const u32x4*>(a.q)[((size_t)inst * G + head) * F::PIECES + 4 * l + kg] : zero;
+      const u32x4 x = mine_rows[4 * F::TILE + (head % G) * F::PIECES + 4 * l + kg];
+      qf[l] = x;
     }
     float m = -INFINITY, sum = 0.f;                        // of head `head`; the sum over this lane's rows
     float o[G][F::E];
@@ -279,7 +289,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
 #pragma unroll
       for (int h = 0; h < G; ++h)
 #pragma unroll
-        for (int e = 0; e < F::E; ++e) s_out[(wave * 4 * F::TILE * 4) + h * D + lane * F::E + e] = o[h][e];
+        for (int e = 0; e < F::E; ++e) s_out[wave * F::WAVE * 4 + h * D + lane * F::E + e] = o[h][e];
     }
     if (lane < G) {
       s_ml[wave][lane][0] = m;
@@ -296,7 +306,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       for (int w = 0; w < kWaves; ++w) {
         const float f = exp2_fast(s_ml[w][h][0] - top);
         all += f * s_ml[w][h][1];
-        val += f * s_out[w * 4 * F::TILE * 4 + x];
+        val += f * s_out[w * F::WAVE * 4 + x];
       }
       if (whole) a.out[((size_t)inst * G + h) * D + e] = val / all;
       else a.part_acc[(slot * G + h) * D + e] = val;

@@ -115,16 +115,21 @@ __device__ __forceinline__ void send_tile(const PrefillArgs& a, int inst, const 
   constexpr unsigned bytes = F::PIECES * 16;
   const int lane = threadIdx.x & 63;
   const unsigned to = lds + wave * F::LOADS * 1024;
+  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };                   // of the run, which begins at a multiple of RW rows
+  auto piece = [&](int l) {
+    const int place = lane % F::PIECES;
+    return IS_V ? F::v_place(row(l), place) : F::k_place(wave * F::RW + row(l), place);
+  };
+  if (run.all) {
 #pragma unroll
-  for (int l = 0; l < F::LOADS; ++l) {
-    const int r = l * F::RPL + lane / F::PIECES, place = lane % F::PIECES;           // of the run; it begins at a multiple of RW rows
-    const int p = IS_V ? F::v_place(r, place) : F::k_place(wave * F::RW + r, place);
-    if (run.all) {
-      to_lds<false>((IS_V ? run.v : run.k) + (l >= F::LOADS / 2 ? run.second : 0), r * bytes + p * 16, to + l * 1024);
-    } else {
-      int j = run.j0 + r;
+    for (int l = 0; l < F::LOADS; ++l)
+      to_lds<false>((IS_V ? run.v : run.k) + (l >= F::LOADS / 2 ? run.second : 0), row(l) * bytes + piece(l) * 16, to + l * 1024);
+  } else {
+#pragma unroll 1
+    for (int l = 0; l < F::LOADS; ++l) {
+      int j = run.j0 + row(l);
       if (j > s.p1 || (j >= s.f && j < s.lo0)) j = run.alt;
-      to_lds_from(static_cast<const char*>(IS_V ? a.V : a.K) + row_at(a.r, inst, j) * bytes + p * 16, to + l * 1024);
+      to_lds_from(static_cast<const char*>(IS_V ? a.V : a.K) + row_at(a.r, inst, j) * bytes + piece(l) * 16, to + l * 1024);
     }
   }
 }
@@ -210,6 +215,9 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     send_tile<F, true>(a, inst, next, s, wave, buffers + F::TILE * 16);
     next = run_of<F>(a, pages, s, s.tile(s.tiles > 1 ? 1 : 0) * F::TT, wave);
   }
+  // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
+#pragma unroll
+  for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
   for (int u = 0; u < s.tiles; ++u) {
     wait_tiles();
     const int t0 = s.tile(u) * F::TT;
@@ -232,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = t0 + 32 * b + reg_row(i, hb);
-          if (j > p || (j < lo && j >= a.n_first)) c[b][i] = -INFINITY;
+          c[b][i] = (j > p) | ((j < lo) & (j >= a.n_first)) ? -INFINITY : c[b][i];
         }
     }
     float top = c[0][0];
@@ -397,6 +405,8 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
     for (int b = 0; b < F::TB; ++b) next[b] = stat_of(begin + 32 * b + n);
     fetch(begin, 0);
   }
+#pragma unroll
+  for (int x = 0; x < F::KS; ++x) asm volatile("" : "+v"(kf[x]));
   int buf = 0;
   for (int r0 = begin; r0 < end; r0 += QT, buf ^= 1) {
     Stat st[F::TB];
@@ -434,13 +444,13 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
         for (int i = 0; i < 16; ++i)
           total[i] = __builtin_fmaf(exp2_fast(__builtin_fmaf(c[i], scale, -st[b].m)), st[b].inv, total[i]);
       } else {
-        const int p = base + (r0 + 32 * b + n) / G;
+        const int p = base + (r0 + 32 * b + n) / G, lo_q = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = j0 + reg_row(i, hb);
-          const bool seen = j <= p && (a.window <= 0 || j > p - a.window || j < a.n_first);
+          const bool seen = (j <= p) & ((j >= lo_q) | (j < a.n_first));
           const float w = exp2_fast(__builtin_fmaf(c[i], scale, -st[b].m)) * st[b].inv;
-          total[i] += seen && st[b].inv > 0.f ? w : 0.f;
+          total[i] += seen & (st[b].inv > 0.f) ? w : 0.f;
         }
       }
     }
