@@ -31,9 +31,9 @@ struct PrefillArgs {
   int q_cap, window, n_first;
   void* out;
   float* acc;
-  float* stat;                  // workspace: [n_inst][q_cap * g][2] maximum and 1 / sum of every row, with acc only
+  float* stat;                  // workspace: [n_inst][stat_rows][2] maximum and 1 / sum of every row of q, with acc only
   float* sums;                  // workspace: [chunks][n_inst][tiles][128] columns' sums over a chunk of the queries, with acc only
-  int chunks, tiles;            // set by the launcher: chunks of the queries; tiles of rows of q an instance
+  int chunks, tiles, stat_rows; // set by the launcher: chunks of the queries; tiles of rows of q, and rows in whole tiles, an instance
 };
 
 constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call

@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTileRows = 128;               // rows of q per workgroup; of the cache, for the columns' sums
-constexpr int kColumnWgs = 2048;             // workgroups of the columns' sums that fill the chip
+constexpr int kColumnWgs = 4096;             // workgroups of the columns' sums that fill the chip
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   if (row >= rows) return;
   const float inv = sum > 0.f ? 1.f / sum : 0.f;           // a query that sees nothing has a zero output
   if (STAT && hb == 0) {
-    float* st = a.stat + ((size_t)inst * a.q_cap * G + row) * 2;
+    float* st = a.stat + ((size_t)inst * a.stat_rows + row) * 2;
     st[0] = m == -INFINITY ? 0.f : m;
     st[1] = inv;
   }
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 
 // Tiles of kTileRows cache rows that an instance's queries see: rows [0, f) and [lo, L), f <= lo.
 struct Columns {
-  int L, nq, base, tiles, ts, tb;
+  int L, nq, base, lo, f, tiles, ts, tb;
   __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
 };
 __device__ __forceinline__ Columns columns_of(const PrefillArgs& a, int inst) {
@@ -344,9 +344,10 @@ __device__ __forceinline__ Columns columns_of(const PrefillArgs& a, int inst) {
   c.L = clamped(a.r.len[inst], 0, a.r.t_cap);
   c.nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
   c.base = c.L - c.nq;
-  const int lo = a.window > 0 && c.base >= a.window ? c.base - a.window + 1 : 0, f = a.n_first < lo ? a.n_first : lo;
-  c.ts = (f + kTileRows - 1) / kTileRows;
-  c.tb = lo / kTileRows > c.ts ? lo / kTileRows : c.ts;
+  c.lo = a.window > 0 && c.base >= a.window ? c.base - a.window + 1 : 0;
+  c.f = a.n_first < c.lo ? a.n_first : c.lo;
+  c.ts = (c.f + kTileRows - 1) / kTileRows;
+  c.tb = c.lo / kTileRows > c.ts ? c.lo / kTileRows : c.ts;
   c.tiles = c.L == 0 || c.nq == 0 ? 0 : c.ts + ((c.L - 1) / kTileRows >= c.tb ? (c.L - 1) / kTileRows - c.tb + 1 : 0);
   return c;
 }
@@ -357,8 +358,8 @@ __device__ __forceinline__ Columns columns_of(const PrefillArgs& a, int inst) {
 template <typename T, int D, int G>
 __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) {
   using F = Form<T, D>;
-  constexpr int QT = F::TT;
-  __shared__ __attribute__((aligned(16))) u32x4 s_q[2][F::TILE];
+  constexpr int QT = F::TT, RING = 3, BUFFER = F::TILE + QT / 2;          // of a buffer, in pieces: the queries and their statistics
+  __shared__ __attribute__((aligned(16))) u32x4 s_q[RING * BUFFER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
   const int inst = blockIdx.y, chunk = blockIdx.z;
   const Columns col = columns_of(a, inst);
@@ -374,6 +375,29 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
     if ((last_q + 1) * G < end) end = (int)((last_q + 1) * G);
   }
   const int j0 = t0 + 32 * wave;                           // this wave's cache rows
+  const bool none = j0 >= L || (j0 >= col.f && j0 + 32 <= col.lo);          // that no query sees
+  const float scale = kLog2E / sqrtf((float)D);
+  float total[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) total[i] = 0.f;
+  const u32x4* q = static_cast<const u32x4*>(a.q) + (size_t)inst * a.q_cap * G * F::PIECES;
+  const float* stat = a.stat + (size_t)inst * a.stat_rows * 2;
+  const unsigned lds = lds_address(s_q);
+  const int tiles = begin < end ? (end - begin + QT - 1) / QT : 0;
+  auto send = [&](int u) {
+    const int r0 = begin + u * QT;
+    const unsigned to = lds + (u % RING) * BUFFER * 16;
+    // (behind the last row of q there is room for the statistics of a whole tile; what lies there is not used)
+    if (wave == 0 && lane < QT / 2) to_lds_from(stat + (r0 + 2 * lane) * 2, to + F::TILE * 16);
+#pragma unroll
+    for (int l = 0; l < F::LOADS; ++l) {
+      const int r = wave * F::RW + l * F::RPL + lane / F::PIECES, p = F::k_place(r, lane % F::PIECES);
+      const int row = r0 + r < rows ? r0 + r : rows - 1;
+      to_lds_from(q + (size_t)row * F::PIECES + p, to + (wave * F::LOADS + l) * 1024);
+    }
+  };
+  if (tiles > 0) send(0);
+  if (tiles > 1) send(1);
   u32x4 kf[F::KS];
   {
     const int j = j0 + n < L ? j0 + n : L - 1;
@@ -381,48 +405,19 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
 #pragma unroll
     for (int x = 0; x < F::KS; ++x) kf[x] = k[2 * x];
   }
-  const float scale = kLog2E / sqrtf((float)D);
-  float total[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) total[i] = 0.f;
-  const size_t q0 = (size_t)inst * a.q_cap * G;
-  const unsigned lds = lds_address(s_q);
-  auto fetch = [&](int r0, int buf) {
-#pragma unroll
-    for (int l = 0; l < F::LOADS; ++l) {
-      const int r = wave * F::RW + l * F::RPL + lane / F::PIECES, p = F::k_place(r, lane % F::PIECES);
-      const int row = r0 + r < rows ? r0 + r : rows - 1;
-      to_lds_from(static_cast<const u32x4*>(a.q) + (q0 + row) * F::PIECES + p, lds + (buf * F::TILE + (wave * F::LOADS + l) * 64) * 16);
-    }
-  };
-  struct Stat { float m, inv; };
-  auto stat_of = [&](int row) {
-    return *reinterpret_cast<const Stat*>(a.stat + (q0 + (row < rows ? row : rows - 1)) * 2);
-  };
-  Stat next[F::TB];
-  if (begin < end) {
-#pragma unroll
-    for (int b = 0; b < F::TB; ++b) next[b] = stat_of(begin + 32 * b + n);
-    fetch(begin, 0);
-  }
-#pragma unroll
-  for (int x = 0; x < F::KS; ++x) asm volatile("" : "+v"(kf[x]));
-  int buf = 0;
-  for (int r0 = begin; r0 < end; r0 += QT, buf ^= 1) {
-    Stat st[F::TB];
-#pragma unroll
-    for (int b = 0; b < F::TB; ++b) {
-      st[b] = next[b];
-      if (r0 + 32 * b + n >= rows) st[b].inv = 0.f;        // no row of q: counts nothing
-    }
-    wait_tiles();
-    if (r0 + QT < end) {
-#pragma unroll
-      for (int b = 0; b < F::TB; ++b) next[b] = stat_of(r0 + QT + 32 * b + n);
-      fetch(r0 + QT, buf ^ 1);
-    }
+  for (int x = 0; x < F::KS; ++x) asm volatile("" : "+v"(kf[x]));           // (they are there: the loop waits for none of them)
+  for (int u = 0; u < tiles; ++u) {
+    const int r0 = begin + u * QT;
+    if (u + 1 < tiles) landed<F::LOADS>(); else landed<0>();                // this tile's; the next one's are under way
+    lds_read();
+    __builtin_amdgcn_s_barrier();                                           // ... of all waves; and everybody is done with the tile before
+    if (u + 2 < tiles) send(u + 2);
+    if (none) continue;
+    const u32x4* Q = s_q + (u % RING) * BUFFER;
     const int r_last = r0 + QT < rows ? r0 + QT - 1 : rows - 1;
-    const bool all = j0 + 31 <= base + r0 / G && (a.window <= 0 || j0 > base + r_last / G - a.window || j0 + 32 <= a.n_first);
+    const bool all = r0 + QT <= rows && j0 + 31 <= base + r0 / G &&
+                     (a.window <= 0 || j0 > base + r_last / G - a.window || j0 + 32 <= a.n_first);
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) {
       float16v c;
@@ -430,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
       for (int i = 0; i < 16; ++i) c[i] = 0.f;
 #pragma unroll
       for (int k = 0; k < F::KS; ++k) {
-        const u32x4 x = s_q[buf][(32 * b + n) * F::PIECES + F::k_place(32 * b + n, 2 * k + hb)];
+        const u32x4 x = Q[(32 * b + n) * F::PIECES + F::k_place(32 * b + n, 2 * k + hb)];
         if constexpr (sizeof(T) == 2) {
           c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[k]), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
         } else {
@@ -439,18 +434,20 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
             c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[k][e]), __uint_as_float(x[e]), c, 0, 0, 0);
         }
       }
+      struct Stat { float m, inv; };
+      Stat st = reinterpret_cast<const Stat*>(Q + F::TILE)[32 * b + n];
       if (all) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          total[i] = __builtin_fmaf(exp2_fast(__builtin_fmaf(c[i], scale, -st[b].m)), st[b].inv, total[i]);
+        for (int i = 0; i < 16; ++i) total[i] = __builtin_fmaf(exp2_fast(__builtin_fmaf(c[i], scale, -st.m)), st.inv, total[i]);
       } else {
-        const int p = base + (r0 + 32 * b + n) / G, lo_q = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
+        const int row = r0 + 32 * b + n, p = base + row / G, lo_q = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
+        if (row >= rows) st.m = st.inv = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = j0 + reg_row(i, hb);
-          const bool seen = (j <= p) & ((j >= lo_q) | (j < a.n_first));
-          const float w = exp2_fast(__builtin_fmaf(c[i], scale, -st[b].m)) * st[b].inv;
-          total[i] += seen & (st[b].inv > 0.f) ? w : 0.f;
+          const bool seen = (j <= p) & ((j >= lo_q) | (j < a.n_first)) & (st.inv > 0.f);
+          const float w = exp2_fast(__builtin_fmaf(c[i], scale, -st.m)) * st.inv;
+          total[i] += seen ? w : 0.f;
         }
       }
     }
@@ -486,6 +483,8 @@ __global__ __launch_bounds__(kTileRows) void cache_weights_add_kernel(PrefillArg
   a.acc[(size_t)inst * a.r.t_cap + j] += x;
 }
 
+// Rows of q of an instance, in whole tiles.
+static int stat_rows(const Shape& s, int q_cap) { return (q_cap * s.g + 63) / 64 * 64; }
 // Most tiles of cache rows that an instance's queries can see.
 static long long most_columns(const Shape& s, int q_cap, int window, int n_first) {
   const long long all = ((long long)s.t_cap + kTileRows - 1) / kTileRows;
@@ -529,7 +528,7 @@ CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
   CacheQWs w;
   size_t o = 0;
   auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
-  w.stat = take(weights ? (size_t)s.n_inst * q_cap * s.g * 2 * 4 : 0);
+  w.stat = take(weights ? (size_t)s.n_inst * stat_rows(s, q_cap) * 2 * 4 : 0);
   // (chunks x instances x tiles, whatever the window: more than one chunk only below kColumnWgs workgroups)
   w.sums = take(weights ? (size_t)(2 * kColumnWgs) * kTileRows * 4 : 0);
   w.total = o;
@@ -538,6 +537,7 @@ CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
 
 hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) {
   PrefillArgs a = args;
+  a.stat_rows = stat_rows(s, a.q_cap);
   a.tiles = (int)(((long long)a.q_cap * s.g + kTileRows - 1) / kTileRows);
   if ((long long)a.tiles * s.n_inst > 0x7fffffffll) return hipErrorInvalidValue;
   a.chunks = a.acc == nullptr ? 1 : column_chunks(s, a.q_cap, most_columns(s, a.q_cap, a.window, a.n_first));
