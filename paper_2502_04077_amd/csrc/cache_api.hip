@@ -61,6 +61,8 @@ int ap_cache_decode(ap_ctx* ctx, const void* q, const void* K, const void* V, co
   a.whole = reinterpret_cast<float*>(base + w.whole);
   a.part_ml = reinterpret_cast<float*>(base + w.part_ml);
   a.part_acc = reinterpret_cast<float*>(base + w.part_acc);
+  a.tickets = reinterpret_cast<unsigned long long*>(base + w.tickets);
+  a.nonce = 0;            // (the launcher draws it)
   a.logits = reinterpret_cast<float*>(base + w.logits);
   return ap::launch_cache_decode(s, a, static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
 }

@@ -6,7 +6,8 @@
 // Memory-bound: 2 d sizeof(T) bytes a row and 4 g d operations on them.  Lengths differ, so the rows are not dealt by instance: the rows
 // seen by all instances, in groups of 16 and in the instances' order, are cut into equal shares, one a workgroup, and every
 // workgroup finds out from the lengths where its share begins.  A workgroup that goes over a whole instance writes its output; the
-// pieces of the others are joined by a second launch.
+// pieces of the others are joined by the last workgroup of the instance to be done.  With weights, which need the joined maximum and
+// sum, a second launch joins and adds them.
 #include "cache_body.h"
 
 namespace ap {
@@ -46,8 +47,9 @@ template <typename T, int D, int G> struct Form {
   static constexpr int QUERIES = (G * PIECES + kWave - 1) / kWave;     // loads of a wave for the queries
   static constexpr int WAVE = 4 * TILE + QUERIES * kWave;              // pieces of LDS of a wave: two groups of K and V, and the queries
   static constexpr int BUFFERS = kWaves * WAVE * 16;
-  static constexpr int PER_CU = PIECES == 8 ? 4 : (PIECES == 16 ? 2 : 1);   // workgroups a CU, as LDS has room for
+  static constexpr int PER_CU = PIECES == 8 ? (G == 8 ? 3 : 4) : (PIECES == 16 ? 2 : 1);   // workgroups a CU, as LDS (G = 8: registers) has room for
   static constexpr int WGS = 256 * PER_CU;                 // the workgroups that 256 CUs hold at once
+  static_assert((WGS + 1) * G * 4 <= BUFFERS && WGS < (1 << kTicketBits), "factors of the pieces, counts");
   static_assert(WGS <= kCacheDecodeWgs && PER_CU * (BUFFERS + 4096) <= 160 * 1024, "workspace, LDS");
   // Piece p of row r of a K group lies at place p ^ (r % PIECES): the operand layout reads a row per lane.
   __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
@@ -86,6 +88,58 @@ template <typename F, bool IS_V> __device__ __forceinline__ void send(const void
   }
 }
 
+// Joins `parts` pieces, from that of workgroup w0 on, by one workgroup: maximum and 1 / sum of every head to s_m and s_inv, and, unless
+// inst < 0, the output.  SHARED: the pieces were written by workgroups of the same launch.  s_f: [parts][G].
+template <int G, bool SHARED>
+__device__ __forceinline__ void join_pieces(const DecodeArgs& a, int D, int inst, int w0, int parts, float* s_f, float* s_m, float* s_inv) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto read = [](const float* p) { return SHARED ? ld_shared_out(p) : *p; };
+  auto slot = [&](int p) { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };      // the first is the last piece of its workgroup
+  // What depends on nothing is asked for first: this thread's first output of the first pieces.
+  constexpr int kAhead = 8;
+  float first[kAhead];
+#pragma unroll
+  for (int p = 0; p < kAhead; ++p) first[p] = p < parts && inst >= 0 && tid < G * D ? read(a.part_acc + slot(p) * G * D + tid) : 0.f;
+  for (int h = wave; h < G; h += kWaves) {
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, read(a.part_ml + (slot(p) * G + h) * 2));
+    top = wave_max(top);
+    float all = 0.f;
+    for (int p = lane; p < parts; p += 64) {
+      const float f = exp2_fast(read(a.part_ml + (slot(p) * G + h) * 2) - top);
+      s_f[p * G + h] = f;
+      all += f * read(a.part_ml + (slot(p) * G + h) * 2 + 1);
+    }
+    all = wave_sum(all);
+    if (lane == 0) {
+      s_m[h] = top;
+      s_inv[h] = 1.f / all;
+    }
+  }
+  __syncthreads();
+  if (inst < 0) return;
+  for (int x = tid; x < G * D; x += kThreads) {
+    const int h = x / D;
+    float val = 0.f;
+    int p = 0;
+    if (x == tid) {
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q)
+        if (q < parts) val += s_f[q * G + h] * first[q];
+      p = kAhead;
+    }
+    for (; p < parts; p += kAhead) {
+      float v[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) v[q] = p + q < parts ? read(a.part_acc + slot(p + q) * G * D + x) : 0.f;
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q)
+        if (p + q < parts) val += s_f[(p + q) * G + h] * v[q];
+    }
+    a.out[(size_t)inst * G * D + x] = val * s_inv[h];
+  }
+}
+
 template <typename T, int D, int G, bool ACC>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(DecodeArgs a) {
   using F = Form<T, D, G>;
@@ -93,7 +147,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
   __shared__ unsigned long long s_wave[kWaves];
-  __shared__ int s_inst, s_from;
+  __shared__ int s_inst, s_from, s_last;
+  __shared__ float s_m[G], s_inv[G];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = lane & 15, kg = lane >> 4;
 
@@ -119,7 +174,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   }
   const unsigned long long per = share_of(groups, F::WGS), begin = (unsigned long long)blockIdx.x * per;
   const unsigned long long end = begin + per < groups ? begin + per : groups;
-  if (blockIdx.x == 0) {
+  // Empty instances have no share; their outputs are zero.
+  for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS)
+    if (a.r.len[i] <= 0)
+      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
+  if (ACC && blockIdx.x == 0) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
       a.before[i] = at;
@@ -142,8 +201,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   }
   __syncthreads();
   int inst = __builtin_amdgcn_readfirstlane(s_inst), from = __builtin_amdgcn_readfirstlane(s_from);
-  unsigned long long left = end - begin;
-
+  unsigned long long left = end - begin, done = begin;      // groups to do, and the number of the next one
   const float scale = kLog2E / sqrtf((float)D);
   const u32x4* mine_rows = s_rows + wave * F::WAVE;
   const unsigned ring = lds_address(mine_rows);
@@ -153,6 +211,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     if (s.n <= from) continue;                             // an empty instance
     const int to = (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
     left -= (unsigned)(to - from);
+    const bool whole = from == 0 && to == s.n;
+    // The other pieces: of the workgroups from w0 on.  The last of them to be done joins them; with weights a second launch does.
+    int w0 = blockIdx.x, parts = 1;
+    if (!ACC && !whole) {
+      if (from > 0) w0 = (int)((done - (unsigned)from) / per);
+      parts = (int)((done + (unsigned)(s.n - from) - 1) / per) - w0 + 1;
+    }
+    done += (unsigned)(to - from);
+    unsigned long long* ticket = a.tickets + (size_t)w0 * kTicketStride;      // (an instance that begins in a workgroup and does not end there: one at most)
+    unsigned long long seen = 0;
+    if (!ACC && !whole && tid == 0) seen = begin_tickets(ticket, a.nonce);
 
     // This wave's groups are from + wave, from + wave + 4, ...; two of them are on their way to LDS while one is worked off.
     const int mine_n = to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
@@ -296,7 +365,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       s_ml[wave][lane][1] = sum;
     }
     __syncthreads();
-    const bool whole = from == 0 && to == s.n;
     const size_t slot = 2 * (size_t)blockIdx.x + (from == 0 ? 1 : 0);   // the piece an instance begins with is its workgroup's last
     for (int x = tid; x < G * D; x += kThreads) {
       const int h = x / D, e = x % D;
@@ -309,74 +377,44 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         val += f * s_out[w * F::WAVE * 4 + x];
       }
       if (whole) a.out[((size_t)inst * G + h) * D + e] = val / all;
-      else a.part_acc[(slot * G + h) * D + e] = val;
-      if (e == 0) {
+      else st_shared_out<!ACC>(a.part_acc + (slot * G + h) * D + e, val);
+      if (e == 0 && (ACC || !whole)) {
         float* ml = whole ? a.whole + ((size_t)inst * G + h) * 2 : a.part_ml + (slot * G + h) * 2;
-        ml[0] = top;
-        ml[1] = all;
+        st_shared_out<!ACC>(ml, top);
+        st_shared_out<!ACC>(ml + 1, all);
       }
     }
+    if (!ACC && !whole && last_to_finish<true>(ticket, a.nonce, seen, parts, &s_last))
+      join_pieces<G, true>(a, D, inst, w0, parts, s_out, s_m, s_inv);
     __syncthreads();
   }
 }
 
-// Joins the pieces of instances that several workgroups went over, and adds the weights.  Workgroup (0, instance) has the output,
+// Adds the weights, and joins the pieces of instances that several workgroups went over.  Workgroup (0, instance) has the output,
 // workgroup (1 + x, instance) the weights of 1024 rows.
 template <int G>
 __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int D, int wgs) {
-  __shared__ float s_f[kCacheDecodeWgs + 1][G];            // factors of the pieces
+  __shared__ float s_f[(kCacheDecodeWgs + 1) * G];
   __shared__ float s_m[G], s_inv[G];
-  const int i = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int i = blockIdx.y, tid = threadIdx.x;
   const Seen s = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first);
   const float scale = kLog2E / sqrtf((float)D);
-  if (s.n == 0) {
-    if (blockIdx.x == 0)
-      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
-    return;
-  }
+  if (s.n == 0) return;
   const int j0 = ((int)blockIdx.x - 1) * 4 * kThreads;
   if (blockIdx.x > 0 && (j0 >= s.L || (j0 >= s.f && j0 + 4 * kThreads <= s.lo))) return;
   const unsigned long long at = a.before[i], per = share_of(a.before[a.r.n_inst], wgs);
   const int w0 = (int)(at / per), parts = (int)((at + (unsigned)s.n - 1) / per) - w0 + 1;
-  if (blockIdx.x == 0 && parts == 1) return;
-  auto slot = [&](int p) { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };
-  if (parts == 1) {
-    if (tid < G) {
-      s_m[tid] = a.whole[((size_t)i * G + tid) * 2];
-      s_inv[tid] = 1.f / a.whole[((size_t)i * G + tid) * 2 + 1];
-    }
-  } else {
-    for (int h = wave; h < G; h += kWaves) {
-      float top = -INFINITY;
-      for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[(slot(p) * G + h) * 2]);
-      top = wave_max(top);
-      float all = 0.f;
-      for (int p = lane; p < parts; p += 64) {
-        const float f = exp2_fast(a.part_ml[(slot(p) * G + h) * 2] - top);
-        s_f[p][h] = f;
-        all += f * a.part_ml[(slot(p) * G + h) * 2 + 1];
-      }
-      all = wave_sum(all);
-      if (lane == 0) {
-        s_m[h] = top;
-        s_inv[h] = 1.f / all;
-      }
-    }
+  if (parts > 1) {
+    join_pieces<G, false>(a, D, blockIdx.x == 0 ? i : -1, w0, parts, s_f, s_m, s_inv);
+  } else if (tid < G) {
+    s_m[tid] = a.whole[((size_t)i * G + tid) * 2];
+    s_inv[tid] = 1.f / a.whole[((size_t)i * G + tid) * 2 + 1];
   }
+  if (blockIdx.x == 0) return;
   __syncthreads();
-  if (blockIdx.x == 0) {
-    for (int x = tid; x < G * D; x += kThreads) {
-      const int h = x / D;
-      float val = 0.f;
-      for (int p = 0; p < parts; ++p) val += s_f[p][h] * a.part_acc[slot(p) * G * D + x];
-      a.out[(size_t)i * G * D + x] = val * s_inv[h];
-    }
-    return;
-  }
   const int j = j0 + 4 * tid;
-  if (j >= a.r.t_cap) return;
+  if (j >= s.L || (j >= s.f && j + 4 <= s.lo)) return;     // (so j < t_cap, and j + 3 too: it is a multiple of 8)
   float add[4] = {0.f, 0.f, 0.f, 0.f};
-  if (j >= s.L || (j >= s.f && j + 4 <= s.lo)) return;
 #pragma unroll
   for (int h = 0; h < G; ++h) {
     const float4v z = *reinterpret_cast<const float4v*>(a.logits + ((size_t)i * G + h) * a.r.t_cap + j);
@@ -393,8 +431,8 @@ template <typename T, int D, int G> hipError_t run(const DecodeArgs& a, hipStrea
   if (a.acc != nullptr) cache_decode_kernel<T, D, G, true><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
   else cache_decode_kernel<T, D, G, false><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const unsigned columns = a.acc != nullptr ? (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads)) : 0;
+  if (e != hipSuccess || a.acc == nullptr) return e;
+  const unsigned columns = (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads));
   cache_join_kernel<G><<<dim3(1 + columns, a.r.n_inst), kThreads, 0, st>>>(a, D, F::WGS);
   return hipGetLastError();
 }
@@ -412,12 +450,15 @@ CacheWs cache_decode_ws(const Shape& s, bool weights) {
   w.whole = take((size_t)s.n_inst * s.g * 2 * 4);
   w.part_ml = take((size_t)2 * kCacheDecodeWgs * s.g * 2 * 4);
   w.part_acc = take((size_t)2 * kCacheDecodeWgs * s.g * s.d * 4);
+  w.tickets = take((size_t)kCacheDecodeWgs * kTicketStride * 8);
   w.logits = take(weights ? (size_t)s.n_inst * s.g * s.t_cap * 4 : 0);
   w.total = o;
   return w;
 }
 
-hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& a, hipStream_t st) {
+hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& args, hipStream_t st) {
+  DecodeArgs a = args;
+  a.nonce = new_nonce(kTicketBits);
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s.g, a, st) : run_g<bf16_t, 64>(s.g, a, st);
   return s.d == 128 ? run_g<float, 128>(s.g, a, st) : run_g<float, 64>(s.g, a, st);
 }

@@ -21,6 +21,8 @@ struct DecodeArgs {
   unsigned long long* before;   // workspace: [n_inst + 1] groups of 16 rows in the instances before
   float* whole;                 // workspace: [n_inst][g][2] maximum and sum of the instances that one workgroup goes over
   float *part_ml, *part_acc;    // workspace: [2 * kCacheDecodeWgs][g][2] and [..][g][d] of the others' pieces
+  unsigned long long* tickets;  // workspace: [kCacheDecodeWgs][kTicketStride], without acc: pieces done of the instance that begins in a workgroup
+  unsigned long long nonce;     // a number of this launch's own (new_nonce)
   float* logits;                // workspace: [n_inst][g][t_cap], with acc only
 };
 
@@ -38,7 +40,7 @@ struct PrefillArgs {
 
 constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call
 
-struct CacheWs { size_t before, whole, part_ml, part_acc, logits, total; };     // decode, in bytes
+struct CacheWs { size_t before, whole, part_ml, part_acc, tickets, logits, total; };     // decode, in bytes
 CacheWs cache_decode_ws(const Shape& s, bool weights);
 struct CacheQWs { size_t stat, sums, total; };                                   // prefill, in bytes
 CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights);
