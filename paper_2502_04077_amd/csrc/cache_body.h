@@ -63,6 +63,11 @@ __device__ __forceinline__ void to_lds_from(const void* p, unsigned lds) {
   lds = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
+// The same past the XCD's L2: what workgroups of this launch wrote with st_shared_out.
+__device__ __forceinline__ void shared_to_lds(const void* p, unsigned lds) {
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off sc1" ::"s"(lds), "v"(p) : "memory", "m0");
+}
 template <int N> __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // Reads of LDS are over: what they read may be overwritten.
 __device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }

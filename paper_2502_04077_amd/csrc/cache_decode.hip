@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kGroup = 16;
 constexpr int kLeastGroups = 8;      // least share of a workgroup: two passes a wave
+constexpr int kLongShare = 64;       // share from which on a CU has several workgroups
 
 // The rows that an instance's new token sees: [0, f) and [lo, L), f <= lo; in groups of 16 rows: gs groups from 0 on, the others from gb.
 struct Seen {
@@ -33,9 +34,12 @@ __device__ __forceinline__ Seen seen_of(int len, int t_cap, int window, int n_fi
   return s;
 }
 
+// Groups of a workgroup.  Up to kLongShare one workgroup a CU: what several gain in loads under way is less than what their pieces cost to
+// join (8 instances of 8000 rows, g = 4, d = 128: 512 workgroups 22 us, 250 19; of 32000 rows 36 and 33; 16 of 32000 rows, from
+// where on it does not matter, 53 and 51; 8 of 2041 rows by shares of 4, 8, 16: 13.5, 12.4, 13.4).
 __device__ __forceinline__ unsigned long long share_of(unsigned long long groups, int wgs) {
-  const unsigned long long per = (groups + wgs - 1) / wgs;
-  return per > kLeastGroups ? per : kLeastGroups;
+  const unsigned long long one = (groups + 255) / 256, all = (groups + wgs - 1) / wgs;
+  return one <= kLeastGroups ? kLeastGroups : (one <= kLongShare ? one : (all > kLongShare ? all : kLongShare));
 }
 
 template <typename T, int D, int G> struct Form {
@@ -49,7 +53,7 @@ template <typename T, int D, int G> struct Form {
   static constexpr int BUFFERS = kWaves * WAVE * 16;
   static constexpr int PER_CU = PIECES == 8 ? (G == 8 ? 3 : 4) : (PIECES == 16 ? 2 : 1);   // workgroups a CU, as LDS (G = 8: registers) has room for
   static constexpr int WGS = 256 * PER_CU;                 // the workgroups that 256 CUs hold at once
-  static_assert((WGS + 1) * G * 4 <= BUFFERS && WGS < (1 << kTicketBits), "factors of the pieces, counts");
+  static_assert((WGS + 4) * G * 4 + G * D * 4 <= BUFFERS && WGS < (1 << kTicketBits), "factors of the pieces, counts");
   static_assert(WGS <= kCacheDecodeWgs && PER_CU * (BUFFERS + 4096) <= 160 * 1024, "workspace, LDS");
   // Piece p of row r of a K group lies at place p ^ (r % PIECES): the operand layout reads a row per lane.
   __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
@@ -88,26 +92,85 @@ template <typename F, bool IS_V> __device__ __forceinline__ void send(const void
   }
 }
 
+// Called by every thread of a workgroup that has left its piece: true in the last of `parts` to get here.  The word, of a workspace that may
+// hold anything, counts below the launch's number in its upper bits (as in take_ticket, but nobody sees to the number beforehand: many
+// workgroups that do so at a time keep the first rows waiting): who finds another number there has counted for nothing and
+// puts the number and a first count in the place of what it left, unless somebody was faster.  The last leaves zero.
+__device__ __forceinline__ bool last_of(unsigned long long* word, unsigned long long nonce, int parts, int* s_last) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wave's share of the piece has reached memory
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    constexpr unsigned long long low = (1ull << kTicketBits) - 1;
+    unsigned long long at = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (((at ^ nonce) >> kTicketBits) != 0) {
+      ++at;
+      for (;;) {
+        if (__hip_atomic_compare_exchange_strong(word, &at, nonce | 1, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) {
+          at = nonce;
+          break;
+        }
+        if (((at ^ nonce) >> kTicketBits) == 0) {
+          at = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          break;
+        }
+      }
+    }
+    const bool last = (int)(at & low) == parts - 1;
+    if (last) end_tickets(word);
+    *s_last = last;
+  }
+  __syncthreads();
+  return *s_last != 0;
+}
+
 // Joins `parts` pieces, from that of workgroup w0 on, by one workgroup: maximum and 1 / sum of every head to s_m and s_inv, and, unless
-// inst < 0, the output.  SHARED: the pieces were written by workgroups of the same launch.  s_f: [parts][G].
-template <int G, bool SHARED>
-__device__ __forceinline__ void join_pieces(const DecodeArgs& a, int D, int inst, int w0, int parts, float* s_f, float* s_m, float* s_inv) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// inst < 0, the output.  SHARED: the pieces were written by workgroups of the same launch.  s: `bytes` of LDS, the factors of the pieces in
+// front, and behind them pieces, of which as many as there is room for are on their way at a time: one workgroup's loads are what this
+// costs (64 pieces of g = 4, d = 128, 16 in registers at a time: 12 us).
+template <int G, int D, bool SHARED>
+__device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w0, int parts, float* s, int bytes, float* s_m, float* s_inv) {
+  constexpr int PP = G * D / 4, R = (G * D + kThreads - 1) / kThreads;              // 16-byte pieces of a part, outputs of a thread
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   auto read = [](const float* p) { return SHARED ? ld_shared_out(p) : *p; };
   auto slot = [&](int p) { return 2 * (size_t)(w0 + p) + (p == 0 ? 1 : 0); };      // the first is the last piece of its workgroup
-  // What depends on nothing is asked for first: this thread's first output of the first pieces.
-  constexpr int kAhead = 8;
-  float first[kAhead];
+  const int front = (parts * G + 3) / 4 * 4;               // floats
+  float* s_parts = s + front;
+  const int room = (bytes / 4 - front) / (G * D);          // parts
+  const unsigned lds = lds_address(s_parts);
+  auto send = [&](int p0) {
+    const int n = parts - p0 < room ? parts - p0 : room;
+    for (int x0 = wave * 64; x0 < n * PP; x0 += kThreads) {
+      const int x = x0 + lane;
+      if (x < n * PP) {
+        const float* src = a.part_acc + slot(p0 + x / PP) * (G * D) + x % PP * 4;
+        if constexpr (SHARED) shared_to_lds(src, lds + x0 * 16);
+        else to_lds_from(src, lds + x0 * 16);
+      }
+    }
+  };
+  if (inst >= 0) send(0);
+  constexpr int HEADS = (G + kWaves - 1) / kWaves;         // of a wave
+  float m0[HEADS], l0[HEADS];                              // of the lane's first piece
 #pragma unroll
-  for (int p = 0; p < kAhead; ++p) first[p] = p < parts && inst >= 0 && tid < G * D ? read(a.part_acc + slot(p) * G * D + tid) : 0.f;
-  for (int h = wave; h < G; h += kWaves) {
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, read(a.part_ml + (slot(p) * G + h) * 2));
+  for (int x = 0; x < HEADS; ++x) {
+    const int h = wave + x * kWaves;
+    const bool have = h < G && lane < parts;
+    m0[x] = have ? read(a.part_ml + (slot(lane) * G + h) * 2) : -INFINITY;
+    l0[x] = have ? read(a.part_ml + (slot(lane) * G + h) * 2 + 1) : 0.f;
+  }
+#pragma unroll
+  for (int x = 0; x < HEADS; ++x) {
+    const int h = wave + x * kWaves;
+    if (h >= G) break;
+    float top = m0[x];
+    for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, read(a.part_ml + (slot(p) * G + h) * 2));
     top = wave_max(top);
-    float all = 0.f;
-    for (int p = lane; p < parts; p += 64) {
+    const float f0 = exp2_fast(m0[x] - top);
+    if (lane < parts) s[lane * G + h] = f0;
+    float all = f0 * l0[x];
+    for (int p = lane + 64; p < parts; p += 64) {
       const float f = exp2_fast(read(a.part_ml + (slot(p) * G + h) * 2) - top);
-      s_f[p * G + h] = f;
+      s[p * G + h] = f;
       all += f * read(a.part_ml + (slot(p) * G + h) * 2 + 1);
     }
     all = wave_sum(all);
@@ -116,27 +179,33 @@ __device__ __forceinline__ void join_pieces(const DecodeArgs& a, int D, int inst
       s_inv[h] = 1.f / all;
     }
   }
-  __syncthreads();
-  if (inst < 0) return;
-  for (int x = tid; x < G * D; x += kThreads) {
-    const int h = x / D;
-    float val = 0.f;
-    int p = 0;
-    if (x == tid) {
+  if (inst < 0) {
+    __syncthreads();
+    return;
+  }
+  float val[R];
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q)
-        if (q < parts) val += s_f[q * G + h] * first[q];
-      p = kAhead;
+  for (int r = 0; r < R; ++r) val[r] = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += room) {
+    if (p0 > 0) {
+      __syncthreads();
+      send(p0);
     }
-    for (; p < parts; p += kAhead) {
-      float v[kAhead];
+    landed<0>();
+    __syncthreads();
+    const int n = parts - p0 < room ? parts - p0 : room;
+#pragma unroll 4
+    for (int p = 0; p < n; ++p)
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q) v[q] = p + q < parts ? read(a.part_acc + slot(p + q) * G * D + x) : 0.f;
+      for (int r = 0; r < R; ++r) {
+        const int x = r * kThreads + tid;
+        if (x < G * D) val[r] += s[(p0 + p) * G + x / D] * s_parts[p * G * D + x];
+      }
+  }
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q)
-        if (p + q < parts) val += s_f[(p + q) * G + h] * v[q];
-    }
-    a.out[(size_t)inst * G * D + x] = val * s_inv[h];
+  for (int r = 0; r < R; ++r) {
+    const int x = r * kThreads + tid;
+    if (x < G * D) a.out[(size_t)inst * G * D + x] = val[r] * s_inv[x / D];
   }
 }
 
@@ -220,8 +289,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     }
     done += (unsigned)(to - from);
     unsigned long long* ticket = a.tickets + (size_t)w0 * kTicketStride;      // (an instance that begins in a workgroup and does not end there: one at most)
-    unsigned long long seen = 0;
-    if (!ACC && !whole && tid == 0) seen = begin_tickets(ticket, a.nonce);
 
     // This wave's groups are from + wave, from + wave + 4, ...; two of them are on their way to LDS while one is worked off.
     const int mine_n = to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
@@ -384,17 +451,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         st_shared_out<!ACC>(ml + 1, all);
       }
     }
-    if (!ACC && !whole && last_to_finish<true>(ticket, a.nonce, seen, parts, &s_last))
-      join_pieces<G, true>(a, D, inst, w0, parts, s_out, s_m, s_inv);
+    if (!ACC && !whole && last_of(ticket, a.nonce, parts, &s_last))
+      join_pieces<G, D, true>(a, inst, w0, parts, s_out, F::BUFFERS, s_m, s_inv);
     __syncthreads();
   }
 }
 
 // Adds the weights, and joins the pieces of instances that several workgroups went over.  Workgroup (0, instance) has the output,
 // workgroup (1 + x, instance) the weights of 1024 rows.
-template <int G>
-__global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int D, int wgs) {
-  __shared__ float s_f[(kCacheDecodeWgs + 1) * G];
+constexpr int join_bytes(int g, int d) { return (kCacheDecodeWgs + 4) * g * 4 + 8 * g * d * 4; }
+template <int G, int D>
+__global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int wgs) {
+  extern __shared__ __attribute__((aligned(16))) float s_join[];          // join_bytes
   __shared__ float s_m[G], s_inv[G];
   const int i = blockIdx.y, tid = threadIdx.x;
   const Seen s = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first);
@@ -405,7 +473,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
   const unsigned long long at = a.before[i], per = share_of(a.before[a.r.n_inst], wgs);
   const int w0 = (int)(at / per), parts = (int)((at + (unsigned)s.n - 1) / per) - w0 + 1;
   if (parts > 1) {
-    join_pieces<G, false>(a, D, blockIdx.x == 0 ? i : -1, w0, parts, s_f, s_m, s_inv);
+    join_pieces<G, D, false>(a, blockIdx.x == 0 ? i : -1, w0, parts, s_join, join_bytes(G, D), s_m, s_inv);
   } else if (tid < G) {
     s_m[tid] = a.whole[((size_t)i * G + tid) * 2];
     s_inv[tid] = 1.f / a.whole[((size_t)i * G + tid) * 2 + 1];
@@ -433,7 +501,7 @@ template <typename T, int D, int G> hipError_t run(const DecodeArgs& a, hipStrea
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.acc == nullptr) return e;
   const unsigned columns = (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads));
-  cache_join_kernel<G><<<dim3(1 + columns, a.r.n_inst), kThreads, 0, st>>>(a, D, F::WGS);
+  cache_join_kernel<G, D><<<dim3(1 + columns, a.r.n_inst), kThreads, join_bytes(G, D), st>>>(a, F::WGS);
   return hipGetLastError();
 }
 template <typename T, int D> hipError_t run_g(int g, const DecodeArgs& a, hipStream_t st) {
