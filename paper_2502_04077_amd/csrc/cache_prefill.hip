@@ -156,13 +156,6 @@ __device__ __forceinline__ float16v product(const u32x4* X, int row0, const u32x
   return c;
 }
 
-// Everybody's pieces of the tile are in LDS, and everybody is done with the buffer that is filled next.
-__device__ __forceinline__ void wait_tiles() {
-  landed<0>();
-  lds_read();
-  __builtin_amdgcn_s_barrier();
-}
-
 // Which of 16 registers' rows: register i of a block holds row 8 (i / 4) + 4 hb + i % 4.
 __device__ __forceinline__ int reg_row(int i, int hb) { return 8 * (i >> 2) + 4 * hb + (i & 3); }
 
@@ -179,10 +172,11 @@ __device__ __forceinline__ Work work_of(unsigned b, int tiles, int n_inst) {
   return {(int)(whole + x % rest), (int)(x / rest)};
 }
 
-template <typename T, int D, int G, bool STAT>
+// NB: buffers, NB - 1 of which are on their way.
+template <typename T, int D, int G, bool STAT, int NB>
 __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
   using F = Form<T, D>;
-  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2 buffers][K, V][TILE]
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [NB][K, V][TILE]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
   const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kTileRows;            // the longest ones first
@@ -209,26 +203,32 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   const unsigned buffers = lds_address(s_tiles);
   const Pages pages = pages_of(a.r, inst);
   Run next;
+  auto send = [&](int u) {                                 // tile u, whose rows are those of `next`
+    const unsigned to = buffers + (u % NB) * 2 * F::TILE * 16;
+    send_tile<F, false>(a, inst, next, s, wave, to);
+    send_tile<F, true>(a, inst, next, s, wave, to + F::TILE * 16);
+    next = run_of<F>(a, pages, s, s.tile(u + 1 < s.tiles ? u + 1 : u) * F::TT, wave);       // a tile ahead: the table's latency
+  };
   if (s.tiles > 0) {
     next = run_of<F>(a, pages, s, s.tile(0) * F::TT, wave);
-    send_tile<F, false>(a, inst, next, s, wave, buffers);
-    send_tile<F, true>(a, inst, next, s, wave, buffers + F::TILE * 16);
-    next = run_of<F>(a, pages, s, s.tile(s.tiles > 1 ? 1 : 0) * F::TT, wave);
+#pragma unroll
+    for (int u = 0; u < NB - 1; ++u)
+      if (u < s.tiles) send(u);
   }
   // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
 #pragma unroll
   for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
   for (int u = 0; u < s.tiles; ++u) {
-    wait_tiles();
+    // This tile has landed, those behind it (two at most) are under way; everybody is done with the buffer that is filled next.
+    if (NB > 3 && u + 2 < s.tiles) landed<4 * F::LOADS>();
+    else if (NB > 2 && u + 1 < s.tiles) landed<2 * F::LOADS>();
+    else landed<0>();
+    lds_read();
+    __builtin_amdgcn_s_barrier();
     const int t0 = s.tile(u) * F::TT;
-    const u32x4* Kt = s_tiles + (u & 1) * 2 * F::TILE;
+    const u32x4* Kt = s_tiles + (u % NB) * 2 * F::TILE;
     const u32x4* Vt = Kt + F::TILE;
-    if (u + 1 < s.tiles) {
-      const unsigned other = buffers + (~u & 1) * 2 * F::TILE * 16;
-      send_tile<F, false>(a, inst, next, s, wave, other);
-      send_tile<F, true>(a, inst, next, s, wave, other + F::TILE * 16);
-      next = run_of<F>(a, pages, s, s.tile(u + 2 < s.tiles ? u + 2 : u) * F::TT, wave);     // a tile ahead: the table's latency
-    }
+    if (u + NB - 1 < s.tiles) send(u + NB - 1);
     float16v c[F::TB];
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
@@ -501,14 +501,18 @@ static int column_chunks(const Shape& s, int q_cap, long long columns) {
   return (int)chunks;
 }
 
-template <typename T, int D, int G> hipError_t run(const Shape& s, const PrefillArgs& a, hipStream_t st) {
-  const size_t lds = (size_t)4 * Form<T, D>::TILE * 16;
+template <typename T, int D, int G, int NB> void run_attention(const PrefillArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst);
-  if (a.acc == nullptr) {
-    cache_prefill_kernel<T, D, G, false><<<grid, kThreads, lds, st>>>(a);
-    return hipGetLastError();
-  }
-  cache_prefill_kernel<T, D, G, true><<<grid, kThreads, lds, st>>>(a);
+  const size_t lds = (size_t)NB * 2 * Form<T, D>::TILE * 16;
+  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false, NB><<<grid, kThreads, lds, st>>>(a);
+  else cache_prefill_kernel<T, D, G, true, NB><<<grid, kThreads, lds, st>>>(a);
+}
+template <typename T, int D, int G> hipError_t run(const Shape& s, const PrefillArgs& a, hipStream_t st) {
+  // Where a CU has one workgroup at most, a tile's work does not cover the next one's way: more of them are under way, in LDS that nobody
+  // else needs.
+  if ((long long)a.tiles * a.r.n_inst <= 256) run_attention<T, D, G, 4>(a, st);
+  else run_attention<T, D, G, 2>(a, st);
+  if (a.acc == nullptr) return hipGetLastError();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 columns((unsigned)most_columns(s, a.q_cap, a.window, a.n_first), a.r.n_inst, a.chunks);

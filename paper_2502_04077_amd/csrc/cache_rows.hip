@@ -7,7 +7,7 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kMoveThreads = 256;
-constexpr int kMoveLoads = 8;        // 16-byte pieces that a thread holds at a time
+constexpr int kMoveLoads = 16;       // 16-byte pieces that a thread holds at a time
 
 // K[i][L - n + r] = k_new[i][r], V the same: a copy of 16-byte pieces, a thread each, whose bound is the memory's rate.
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheRows c, const u32x4* __restrict__ k_new,
