@@ -82,7 +82,8 @@ int ap_cache_prefill(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_c
   a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.window = window; a.n_first = n_first; a.out = out; a.acc = acc;
   a.stat = reinterpret_cast<float*>(base + w.stat);
   a.sums = reinterpret_cast<float*>(base + w.sums);
-  a.chunks = 1;
+  a.part_ml = reinterpret_cast<float*>(base + w.part_ml);
+  a.part_o = reinterpret_cast<float*>(base + w.part_o);
   return ap::launch_cache_prefill(s, a, static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
 }
 

@@ -35,6 +35,8 @@ struct PrefillArgs {
   float* acc;
   float* stat;                  // workspace: [n_inst][stat_rows][2] maximum and 1 / sum of every row of q, with acc only
   float* sums;                  // workspace: [chunks][n_inst][tiles][128] columns' sums over a chunk of the queries, with acc only
+  float *part_ml, *part_o;      // workspace: [splits][n_inst][q_cap * g][2] and [..][d], where the cache is in splits
+  int splits;                   // set by the launcher, as the next ones
   int chunks, tiles, stat_rows; // set by the launcher: chunks of the queries; tiles of rows of q, and rows in whole tiles, an instance
 };
 
@@ -42,7 +44,7 @@ constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a 
 
 struct CacheWs { size_t before, whole, part_ml, part_acc, tickets, logits, total; };     // decode, in bytes
 CacheWs cache_decode_ws(const Shape& s, bool weights);
-struct CacheQWs { size_t stat, sums, total; };                                   // prefill, in bytes
+struct CacheQWs { size_t stat, sums, part_ml, part_o, total; };                                   // prefill, in bytes
 CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights);
 
 hipError_t launch_cache_append(const Shape& s, const CacheRows& r, const void* k_new, const void* v_new, const int32_t* n_new, int q_cap,

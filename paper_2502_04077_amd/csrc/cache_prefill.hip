@@ -15,6 +15,9 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTileRows = 128;               // rows of q per workgroup; of the cache, for the columns' sums
+constexpr int kSplitWgs = 512;               // workgroups that splits of the cache may come to
+constexpr int kMostSplits = 64;
+constexpr int kLeastTiles = 2;               // tiles of a split
 constexpr int kColumnWgs = 4096;             // workgroups of the columns' sums that fill the chip
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -202,33 +205,37 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 
   const unsigned buffers = lds_address(s_tiles);
   const Pages pages = pages_of(a.r, inst);
+  // Tiles of the cache in splits: this workgroup's.
+  const int each = (s.tiles + a.splits - 1) / a.splits > kLeastTiles ? (s.tiles + a.splits - 1) / a.splits : kLeastTiles;
+  const int u_begin = a.splits == 1 ? 0 : (int)blockIdx.y * each;
+  const int u_end = a.splits == 1 || s.tiles < u_begin + each ? s.tiles : u_begin + each;
   Run next;
   auto send = [&](int u) {                                 // tile u, whose rows are those of `next`
     const unsigned to = buffers + (u % NB) * 2 * F::TILE * 16;
     send_tile<F, false>(a, inst, next, s, wave, to);
     send_tile<F, true>(a, inst, next, s, wave, to + F::TILE * 16);
-    next = run_of<F>(a, pages, s, s.tile(u + 1 < s.tiles ? u + 1 : u) * F::TT, wave);       // a tile ahead: the table's latency
+    next = run_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);         // a tile ahead: the table's latency
   };
-  if (s.tiles > 0) {
-    next = run_of<F>(a, pages, s, s.tile(0) * F::TT, wave);
+  if (u_begin < u_end) {
+    next = run_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
 #pragma unroll
     for (int u = 0; u < NB - 1; ++u)
-      if (u < s.tiles) send(u);
+      if (u_begin + u < u_end) send(u_begin + u);
   }
   // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
 #pragma unroll
   for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
-  for (int u = 0; u < s.tiles; ++u) {
+  for (int u = u_begin; u < u_end; ++u) {
     // This tile has landed, those behind it (two at most) are under way; everybody is done with the buffer that is filled next.
-    if (NB > 3 && u + 2 < s.tiles) landed<4 * F::LOADS>();
-    else if (NB > 2 && u + 1 < s.tiles) landed<2 * F::LOADS>();
+    if (NB > 3 && u + 2 < u_end) landed<4 * F::LOADS>();
+    else if (NB > 2 && u + 1 < u_end) landed<2 * F::LOADS>();
     else landed<0>();
     lds_read();
     __builtin_amdgcn_s_barrier();
     const int t0 = s.tile(u) * F::TT;
     const u32x4* Kt = s_tiles + (u % NB) * 2 * F::TILE;
     const u32x4* Vt = Kt + F::TILE;
-    if (u + NB - 1 < s.tiles) send(u + NB - 1);
+    if (u + NB - 1 < u_end) send(u + NB - 1);
     float16v c[F::TB];
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
@@ -261,13 +268,15 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
       m = ref;
     }
     const float use = m == -INFINITY ? 0.f : m;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};                  // (sums of a tile first: long caches lose fewer digits so)
 #pragma unroll
     for (int b = 0; b < F::TB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         c[b][i] = exp2_fast(__builtin_fmaf(c[b][i], scale, -use));
-        sum += c[b][i];
+        part[i & 3] += c[b][i];
       }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
     if constexpr (sizeof(T) == 2) {
       // Probabilities are rounded to bf16 for the matrix unit, which adds an error of the size of the output's own rounding; their sum
       // is taken before.
@@ -298,16 +307,40 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     } else {
       const float* Vf = reinterpret_cast<const float*>(Vt);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int b = 0; b < F::DB; ++b) {
+        float16v x;                                        // of this tile alone, as the sums
 #pragma unroll
-        for (int b = 0; b < F::DB; ++b)
-          o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(Vf[reg_row(i, hb) * D + 32 * b + n], c[0][i], o[b], 0, 0, 0);
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          x = __builtin_amdgcn_mfma_f32_32x32x2f32(Vf[reg_row(i, hb) * D + 32 * b + n], c[0][i], x, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] += x[i];
       }
     }
   }
 
   sum = sum32(sum);
   if (row >= rows) return;
+  if (a.splits > 1) {                                      // (whatever its share: the join goes by the maximum)
+    const size_t at = ((size_t)blockIdx.y * a.r.n_inst + inst) * a.q_cap * G + row;
+    if (hb == 0) {
+      a.part_ml[at * 2] = m;
+      a.part_ml[at * 2 + 1] = sum;
+    }
+    if (u_begin < u_end) {
+#pragma unroll
+      for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          float4v y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = o[b][i + e];
+          *reinterpret_cast<float4v*>(a.part_o + at * D + 32 * b + reg_row(i, hb)) = y;
+        }
+    }
+    return;
+  }
   const float inv = sum > 0.f ? 1.f / sum : 0.f;           // a query that sees nothing has a zero output
   if (STAT && hb == 0) {
     float* st = a.stat + ((size_t)inst * a.stat_rows + row) * 2;
@@ -332,6 +365,50 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
         *reinterpret_cast<float4v*>(out + d) = y;
       }
     }
+}
+
+// Joins the splits of the cache: a wave per row of q.
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kThreads) void cache_prefill_join_kernel(PrefillArgs a) {
+  constexpr int E = D / 64;                                // outputs of a lane
+  const int inst = blockIdx.y, lane = threadIdx.x & 63, row = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
+  if (row >= nq * G) return;
+  const size_t at = (size_t)inst * a.q_cap * G + row, step = (size_t)a.r.n_inst * a.q_cap * G;
+  // A lane has the statistics of a split (there are at most 64).
+  const float m = lane < a.splits ? a.part_ml[(lane * step + at) * 2] : -INFINITY, l = lane < a.splits ? a.part_ml[(lane * step + at) * 2 + 1] : 0.f;
+  const float top = wave_max(m), use = top == -INFINITY ? 0.f : top;
+  const float f = exp2_fast(m - use), sum = wave_sum(f * l), inv = sum > 0.f ? 1.f / sum : 0.f;
+  float o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  constexpr int kAhead = 8;                                // loads under way
+  for (int x0 = 0; x0 < a.splits; x0 += kAhead) {
+    float v[kAhead][E];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int y = x0 + x < a.splits ? x0 + x : a.splits - 1;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[x][e] = a.part_o[(y * step + at) * D + lane * E + e];
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const float w = x0 + x < a.splits ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x0 + x)) : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += w > 0.f ? w * v[x][e] : 0.f;                // (a split without tiles has left no sums)
+    }
+  }
+  T* out = static_cast<T*>(a.out) + at * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if constexpr (sizeof(T) == 2) out[e].bits = __builtin_bit_cast(uint16_t, (__bf16)(o[e] * inv));
+    else out[e] = o[e] * inv;
+  }
+  if (a.acc != nullptr && lane == 0) {
+    float* st = a.stat + ((size_t)inst * a.stat_rows + row) * 2;
+    st[0] = use;
+    st[1] = inv;
+  }
 }
 
 // Tiles of kTileRows cache rows that an instance's queries see: rows [0, f) and [lo, L), f <= lo.
@@ -492,6 +569,16 @@ static long long most_columns(const Shape& s, int q_cap, int window, int n_first
   const long long some = ((long long)n_first + kTileRows - 1) / kTileRows + ((long long)window + q_cap) / kTileRows + 2;
   return some < all ? some : all;
 }
+// Splits of the cache where the rows of q alone leave CUs without work: up to 512 workgroups, of at least kLeastTiles tiles.
+static int cache_splits(const Shape& s, int q_cap, int window, int n_first) {
+  const long long wgs = (((long long)q_cap * s.g + kTileRows - 1) / kTileRows) * s.n_inst;
+  const long long rows = window > 0 && (long long)window + q_cap + n_first < s.t_cap ? (long long)window + q_cap + n_first : s.t_cap;
+  const int tt = s.kv_dtype == AP_BF16 ? 64 : 32;
+  long long splits = kSplitWgs / wgs, most = (rows + tt * kLeastTiles - 1) / (tt * kLeastTiles);
+  if (splits > most) splits = most;
+  if (splits > kMostSplits) splits = kMostSplits;
+  return splits < 1 ? 1 : (int)splits;
+}
 // Workgroups of the columns' sums: chunks of the query rows, of at least 512 rows, where the tiles alone are few for the chip.
 static int column_chunks(const Shape& s, int q_cap, long long columns) {
   const long long q_rows = (long long)q_cap * s.g;
@@ -502,7 +589,7 @@ static int column_chunks(const Shape& s, int q_cap, long long columns) {
 }
 
 template <typename T, int D, int G, int NB> void run_attention(const PrefillArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst);
+  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
   const size_t lds = (size_t)NB * 2 * Form<T, D>::TILE * 16;
   if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false, NB><<<grid, kThreads, lds, st>>>(a);
   else cache_prefill_kernel<T, D, G, true, NB><<<grid, kThreads, lds, st>>>(a);
@@ -510,8 +597,13 @@ template <typename T, int D, int G, int NB> void run_attention(const PrefillArgs
 template <typename T, int D, int G> hipError_t run(const Shape& s, const PrefillArgs& a, hipStream_t st) {
   // Where a CU has one workgroup at most, a tile's work does not cover the next one's way: more of them are under way, in LDS that nobody
   // else needs.
-  if ((long long)a.tiles * a.r.n_inst <= 256) run_attention<T, D, G, 4>(a, st);
+  if ((long long)a.tiles * a.r.n_inst * a.splits <= 256) run_attention<T, D, G, 4>(a, st);
   else run_attention<T, D, G, 2>(a, st);
+  if (a.splits > 1) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    cache_prefill_join_kernel<T, D, G><<<dim3((a.q_cap * G + kWaves - 1) / kWaves, a.r.n_inst), kThreads, 0, st>>>(a);
+  }
   if (a.acc == nullptr) return hipGetLastError();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -535,6 +627,12 @@ CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
   w.stat = take(weights ? (size_t)s.n_inst * stat_rows(s, q_cap) * 2 * 4 : 0);
   // (chunks x instances x tiles, whatever the window: more than one chunk only below kColumnWgs workgroups)
   w.sums = take(weights ? (size_t)(2 * kColumnWgs) * kTileRows * 4 : 0);
+  // Rows of q in splits, for any q_cap up to this one: a workgroup's 128 each, and not more than all rows in the most splits.
+  long long part = (long long)kSplitWgs * kTileRows;
+  if (part > (long long)kMostSplits * s.n_inst * q_cap * s.g) part = (long long)kMostSplits * s.n_inst * q_cap * s.g;
+  if (s.n_inst > kSplitWgs / 2) part = 0;
+  w.part_ml = take((size_t)part * 2 * 4);
+  w.part_o = take((size_t)part * s.d * 4);
   w.total = o;
   return w;
 }
@@ -544,6 +642,7 @@ hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStre
   a.stat_rows = stat_rows(s, a.q_cap);
   a.tiles = (int)(((long long)a.q_cap * s.g + kTileRows - 1) / kTileRows);
   if ((long long)a.tiles * s.n_inst > 0x7fffffffll) return hipErrorInvalidValue;
+  a.splits = cache_splits(s, a.q_cap, a.window, a.n_first);
   a.chunks = a.acc == nullptr ? 1 : column_chunks(s, a.q_cap, most_columns(s, a.q_cap, a.window, a.n_first));
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s, a, st) : run_g<bf16_t, 64>(s, a, st);
   return s.d == 128 ? run_g<float, 128>(s, a, st) : run_g<float, 64>(s, a, st);

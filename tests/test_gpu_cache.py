@@ -111,6 +111,12 @@ PREFILL = [
     (8, 128, 8, "f32", False, 136, 33, 0, 0, [136, 33, 20], [33, 33, 33]),
     (1, 64, 32, "f32", True, 256, 140, 20, 33, [256, 140], [140, 129]),
     (2, 128, 16, "f32", True, 96, 96, 3, 1, [96, 5], [96, 5]),
+    # few queries behind long caches, which are cut into splits
+    (2, 128, 16, "bf16", True, 8192, 3, 0, 0, [8190, 5000, 2, 0], [3, 2, 2, 1]),
+    (4, 128, 32, "bf16", False, 2048, 101, 0, 0, [2040, 517, 64], [101, 77, 3]),
+    (8, 64, 8, "bf16", True, 5000, 9, 1300, 200, [4999, 1309, 1200], [9, 9, 8]),
+    (2, 64, 32, "f32", True, 4096, 4, 1500, 70, [4096, 3001, 4], [4, 4, 3]),
+    (1, 128, 16, "f32", False, 2048, 5, 0, 0, [2047, 1], [5, 1]),
 ]
 
 
