@@ -7,7 +7,7 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kMoveThreads = 256;
-constexpr int kMoveLoads = 16;       // 16-byte pieces that a thread holds at a time
+constexpr int kMoveLoads = 8;        // 16-byte pieces that a thread holds at a time
 
 // K[i][L - n + r] = k_new[i][r], V the same: a copy of 16-byte pieces, a thread each, whose bound is the memory's rate.
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheRows c, const u32x4* __restrict__ k_new,
@@ -277,22 +277,39 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(CacheRows c, u
   const int piece = (blockIdx.x % columns) * W + threadIdx.x % W, r = threadIdx.x / W;
   const int n = len_out[i];
   kept += (size_t)i * budget;
-  for (int j0 = 0; j0 < n; j0 += RPL * kMoveLoads) {
-    u32x4 x[kMoveLoads];
-    bool moves[kMoveLoads];
+  // A round's rows: where they come from, and what they hold.  The next round's are looked up before this one's have arrived, and asked for
+  // before this one's are written: what is still to come lies behind what is written.
+  auto look = [&](int j0, int (&src)[kMoveLoads]) {
 #pragma unroll
     for (int l = 0; l < kMoveLoads; ++l) {
       const int j = j0 + l * RPL + r;
-      const int src = j < n ? kept[j] : j;
-      moves[l] = src != j;
-      if (moves[l]) x[l] = X[row_at(c, i, src) * pieces + piece];
+      src[l] = j < n ? kept[j] : j;
     }
+  };
+  auto load = [&](int j0, const int (&src)[kMoveLoads], u32x4 (&x)[kMoveLoads]) {
+#pragma unroll
+    for (int l = 0; l < kMoveLoads; ++l)
+      if (src[l] != j0 + l * RPL + r) x[l] = X[row_at(c, i, src[l]) * pieces + piece];
+  };
+  int src[kMoveLoads], next[kMoveLoads];
+  u32x4 x[kMoveLoads], y[kMoveLoads];
+  look(0, src);
+  load(0, src, x);
+  for (int j0 = 0; j0 < n; j0 += RPL * kMoveLoads) {
+    const int j1 = j0 + RPL * kMoveLoads;
+    if (j1 < n) look(j1, next);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    __syncthreads();                                       // this round's rows have arrived, everywhere
+    if (j1 < n) load(j1, next, y);
 #pragma unroll
     for (int l = 0; l < kMoveLoads; ++l) {
       size_t to;
-      if (moves[l] && row_to_write(c, i, j0 + l * RPL + r, &to)) X[to * pieces + piece] = x[l];
+      if (src[l] != j0 + l * RPL + r && row_to_write(c, i, j0 + l * RPL + r, &to)) X[to * pieces + piece] = x[l];
+    }
+#pragma unroll
+    for (int l = 0; l < kMoveLoads; ++l) {
+      src[l] = next[l];
+      x[l] = y[l];
     }
   }
 }
@@ -323,12 +340,12 @@ hipError_t launch_cache_evict(const Shape& s, const CacheRows& r, void* K, void*
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int pieces = pieces_of(s);
-  if (s.n_inst * 2 * pieces / 8 < 512)
-    evict_move_kernel<4><<<dim3(2 * pieces / 4, s.n_inst), kMoveThreads, 0, st>>>(r, static_cast<u32x4*>(K), static_cast<u32x4*>(V), pieces,
-                                                                                budget, len_out, kept);
-  else
-    evict_move_kernel<8><<<dim3(2 * pieces / 8, s.n_inst), kMoveThreads, 0, st>>>(r, static_cast<u32x4*>(K), static_cast<u32x4*>(V), pieces,
-                                                                                budget, len_out, kept);
+  // Whole rows a workgroup read best, but every workgroup has only so much under way: columns as wide as leave two workgroups a CU.
+  auto move = [&](auto kernel, int w) {
+    kernel<<<dim3(2 * pieces / w, s.n_inst), kMoveThreads, 0, st>>>(r, static_cast<u32x4*>(K), static_cast<u32x4*>(V), pieces, budget, len_out, kept);
+  };
+  if (s.n_inst * (2 * pieces / 8) >= 512) move(evict_move_kernel<8>, 8);
+  else move(evict_move_kernel<4>, 4);
   return hipGetLastError();
 }
 
