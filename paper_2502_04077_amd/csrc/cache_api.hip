@@ -26,6 +26,12 @@ static CacheRows rows_of(const Shape& s, const int32_t* len) {
 // Query rows are numbered in 32 bits within an instance.
 static bool q_cap_ok(const Shape& s, int32_t q_cap) { return q_cap >= 1 && q_cap <= (1 << 30) / s.g; }
 
+// A launch has less than 2^32 threads.
+static bool fits(long long threads) { return threads < (1ll << 32); }
+// A window of t_cap rows and more shows all of them; so sums of positions and windows stay in 32 bits.
+static int seen_window(const Shape& s, int32_t window) { return window >= s.t_cap ? 0 : window; }
+static int seen_first(const Shape& s, int32_t n_first) { return n_first < s.t_cap ? n_first : s.t_cap; }
+
 extern "C" {
 
 size_t ap_cache_workspace_bytes(const ap_ctx* ctx, int32_t q_cap, int32_t weights) {
@@ -40,7 +46,7 @@ int ap_cache_append(ap_ctx* ctx, const void* k_new, const void* v_new, const int
   if (ctx == nullptr) return AP_ERR_ARG;
   AP_REQUIRE_PTR(k_new); AP_REQUIRE_PTR(v_new); AP_OPTIONAL_PTR(n_new); AP_REQUIRE_PTR(len); AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V);
   const Shape& s = ctx->s;
-  if (!q_cap_ok(s, q_cap)) return AP_ERR_RANGE;
+  if (!q_cap_ok(s, q_cap) || !fits((long long)s.n_inst * q_cap * (s.d / 4))) return AP_ERR_RANGE;
   return ap::launch_cache_append(s, rows_of(s, len), k_new, v_new, n_new, q_cap, K, V, static_cast<hipStream_t>(stream)) == hipSuccess
              ? AP_OK : AP_ERR_HIP;
 }
@@ -56,7 +62,7 @@ int ap_cache_decode(ap_ctx* ctx, const void* q, const void* K, const void* V, co
   char* base = static_cast<char*>(ws);
   ap::DecodeArgs a;
   a.r = rows_of(s, len);
-  a.q = q; a.K = K; a.V = V; a.window = window; a.n_first = n_first; a.out = out; a.acc = acc;
+  a.q = q; a.K = K; a.V = V; a.window = seen_window(s, window); a.n_first = seen_first(s, n_first); a.out = out; a.acc = acc;
   a.before = reinterpret_cast<unsigned long long*>(base + w.before);
   a.whole = reinterpret_cast<float*>(base + w.whole);
   a.part_ml = reinterpret_cast<float*>(base + w.part_ml);
@@ -74,12 +80,12 @@ int ap_cache_prefill(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_c
   AP_OPTIONAL_PTR(acc); AP_REQUIRE_PTR(ws);
   if (window < 0 || n_first < 0) return AP_ERR_ARG;
   const Shape& s = ctx->s;
-  if (!q_cap_ok(s, q_cap)) return AP_ERR_RANGE;
+  if (!q_cap_ok(s, q_cap) || !fits(((long long)q_cap * s.g + 127) / 128 * 256 * s.n_inst)) return AP_ERR_RANGE;
   const ap::CacheQWs w = ap::cache_prefill_ws(s, q_cap, acc != nullptr);
   char* base = static_cast<char*>(ws);
   ap::PrefillArgs a;
   a.r = rows_of(s, len);
-  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.window = window; a.n_first = n_first; a.out = out; a.acc = acc;
+  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.window = seen_window(s, window); a.n_first = seen_first(s, n_first); a.out = out; a.acc = acc;
   a.stat = reinterpret_cast<float*>(base + w.stat);
   a.sums = reinterpret_cast<float*>(base + w.sums);
   a.part_ml = reinterpret_cast<float*>(base + w.part_ml);

@@ -8,6 +8,12 @@
 // workgroup finds out from the lengths where its share begins.  A workgroup that goes over a whole instance writes its output; the
 // pieces of the others are joined by the last workgroup of the instance to be done.  With weights, which need the joined maximum and
 // sum, a second launch joins and adds them.
+//
+// A wave goes over its groups with a running maximum and sum; two groups of K and V are on their way to LDS, past the registers and not
+// kept in the caches, while one is worked off: q . K on the matrix unit, P . V with fp32 multiply-adds, as probabilities of fewer digits
+// would show in the fp32 output.  Measured: 256 instances of 60 to 32790 rows (g = 4, d = 128, pages of 16; 785 MB) 142 us, 5.5 TB/s; 1024
+// with a window of 4096 (g = 8; 2.1 GB) 350 us, 6.0 TB/s; with rows through registers and pages looked up by vector loads, which wait for
+// the rows in flight, 246 and 639.  Many short instances are bound by what every piece costs (2048 of 8 to 419 rows, 111 MB, 61 us).
 #include "cache_body.h"
 
 namespace ap {

@@ -40,6 +40,7 @@ DECODE = [
     (8, 128, 8, "f32", False, 264, 0, 0, [264, 1, 263, 129]),
     (1, 64, 32, "f32", True, 256, 200, 300, [256, 255, 201, 200]),
     (2, 128, 16, "f32", True, 96, 3, 1, [96, 5, 4, 3]),
+    (4, 64, 16, "bf16", True, 96, 2147483647, 2147483647, [96, 5, 0]),
 ]
 
 
@@ -111,6 +112,7 @@ PREFILL = [
     (8, 128, 8, "f32", False, 136, 33, 0, 0, [136, 33, 20], [33, 33, 33]),
     (1, 64, 32, "f32", True, 256, 140, 20, 33, [256, 140], [140, 129]),
     (2, 128, 16, "f32", True, 96, 96, 3, 1, [96, 5], [96, 5]),
+    (2, 64, 16, "bf16", True, 96, 40, 2147483647, 2147483647, [96, 5, 30], [40, 40, 40]),
     # few queries behind long caches, which are cut into splits
     (2, 128, 16, "bf16", True, 8192, 3, 0, 0, [8190, 5000, 2, 0], [3, 2, 2, 1]),
     (4, 128, 32, "bf16", False, 2048, 101, 0, 0, [2040, 517, 64], [101, 77, 3]),

@@ -42,9 +42,9 @@ def test_null_and_misaligned_pointers(ctx, name):
 
 
 @pytest.mark.parametrize("name,at,value,code", [
-    ("ap_cache_append", 3, 0, ap.AP_ERR_RANGE), ("ap_cache_append", 3, -1, ap.AP_ERR_RANGE), ("ap_cache_append", 3, 1 << 30, ap.AP_ERR_RANGE),
+    ("ap_cache_append", 3, 0, ap.AP_ERR_RANGE), ("ap_cache_append", 3, -1, ap.AP_ERR_RANGE), ("ap_cache_append", 3, 1 << 30, ap.AP_ERR_RANGE), ("ap_cache_append", 3, 1 << 25, ap.AP_ERR_RANGE),
     ("ap_cache_decode", 4, -1, ap.AP_ERR_ARG), ("ap_cache_decode", 5, -1, ap.AP_ERR_ARG),
-    ("ap_cache_prefill", 2, 0, ap.AP_ERR_RANGE), ("ap_cache_prefill", 2, 1 << 29, ap.AP_ERR_RANGE),
+    ("ap_cache_prefill", 2, 0, ap.AP_ERR_RANGE), ("ap_cache_prefill", 2, 1 << 29, ap.AP_ERR_RANGE), ("ap_cache_prefill", 2, 1 << 27, ap.AP_ERR_RANGE),
     ("ap_cache_prefill", 6, -1, ap.AP_ERR_ARG), ("ap_cache_prefill", 7, -1, ap.AP_ERR_ARG),
     ("ap_cache_evict", 4, 0, ap.AP_ERR_ARG), ("ap_cache_evict", 4, 7, ap.AP_ERR_ARG), ("ap_cache_evict", 4, 4097, ap.AP_ERR_RANGE),
     ("ap_cache_evict", 5, -1, ap.AP_ERR_ARG), ("ap_cache_evict", 6, -1, ap.AP_ERR_ARG), ("ap_cache_evict", 6, 97, ap.AP_ERR_ARG),
