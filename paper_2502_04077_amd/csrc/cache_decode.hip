@@ -13,7 +13,8 @@
 // kept in the caches, while one is worked off: q . K on the matrix unit, P . V with fp32 multiply-adds, as probabilities of fewer digits
 // would show in the fp32 output.  Measured: 256 instances of 60 to 32790 rows (g = 4, d = 128, pages of 16; 785 MB) 142 us, 5.5 TB/s; 1024
 // with a window of 4096 (g = 8; 2.1 GB) 350 us, 6.0 TB/s; with rows through registers and pages looked up by vector loads, which wait for
-// the rows in flight, 246 and 639.  Many short instances are bound by what every piece costs (2048 of 8 to 419 rows, 111 MB, 61 us).
+// the rows in flight, 246 and 639.  Where more instances than workgroups are all short, every wave takes whole ones: 2048 of 8 to 419 rows
+// (g = 1, 111 MB) 38 us, by shares of a workgroup 61; of 16 to 56 (g = 2, d = 64) 18 and 40.
 #include "cache_body.h"
 
 namespace ap {
@@ -21,6 +22,8 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kGroup = 16;
 constexpr int kLeastGroups = 8;      // least share of a workgroup: two passes a wave
+constexpr int kShort = 64;           // groups of an instance that a wave goes over alone
+constexpr unsigned long long kAlone = ~0ull;   // in the place of the number of groups: every instance was whole
 constexpr int kLongShare = 64;       // share from which on a CU has several workgroups
 
 // The rows that an instance's new token sees: [0, f) and [lo, L), f <= lo; in groups of 16 rows: gs groups from 0 on, the others from gb.
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
   __shared__ unsigned long long s_wave[kWaves];
-  __shared__ int s_inst, s_from, s_last;
+  __shared__ int s_first[kWaves], s_longest[kWaves], s_end, s_from, s_last;
   __shared__ float s_m[G], s_inv[G];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = lane & 15, kg = lane >> 4;
@@ -232,22 +235,37 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const int i_begin = tid * chunk < a.r.n_inst ? tid * chunk : a.r.n_inst;
   const int i_end = i_begin + chunk < a.r.n_inst ? i_begin + chunk : a.r.n_inst;
   unsigned long long mine = 0;
-  for (int i = i_begin; i < i_end; ++i) mine += (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+  int longest = 0;
+  for (int i = i_begin; i < i_end; ++i) {
+    const int n = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+    mine += (unsigned)n;
+    longest = n > longest ? n : longest;
+  }
   unsigned long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const unsigned long long y = __shfl_up(upto, o, 64);
     if (lane >= o) upto += y;
   }
-  if (lane == 63) s_wave[wave] = upto;
-  if (tid == 0) s_inst = -1;
+  longest = (int)wave_max((float)(longest < kShort + 1 ? longest : kShort + 1));
+  if (lane == 63) {
+    s_wave[wave] = upto;
+    s_longest[wave] = longest;
+  }
+  if (tid < kWaves) s_first[tid] = a.r.n_inst;
+  if (tid == 0) s_end = 0;
   __syncthreads();
   unsigned long long groups = 0, ahead = upto - mine;
   for (int w = 0; w < kWaves; ++w) {
     if (w < wave) ahead += s_wave[w];
     groups += s_wave[w];
+    longest = s_longest[w] > longest ? s_longest[w] : longest;
   }
-  const unsigned long long per = share_of(groups, F::WGS), begin = (unsigned long long)blockIdx.x * per;
+  // More instances than workgroups, all of them short: every wave takes whole instances, those that begin in its share, with no pieces and
+  // nobody to wait for.
+  const bool alone = __builtin_amdgcn_readfirstlane(a.r.n_inst > F::WGS && longest <= kShort);
+  const unsigned long long per = alone ? kWaves * ((groups + kWaves * F::WGS - 1) / (kWaves * F::WGS)) : share_of(groups, F::WGS);
+  const unsigned long long begin = (unsigned long long)blockIdx.x * per;
   const unsigned long long end = begin + per < groups ? begin + per : groups;
   // Empty instances have no share; their outputs are zero.
   for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS)
@@ -259,15 +277,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       a.before[i] = at;
       at += (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
     }
-    if (tid == kThreads - 1) a.before[a.r.n_inst] = groups;
+    if (tid == kThreads - 1) a.before[a.r.n_inst] = alone ? kAlone : groups;
   }
   if (begin >= end) return;
-  if (ahead <= begin && begin < ahead + mine) {
+  const unsigned long long share = per / kWaves;           // alone: of a wave
+  if (alone ? ahead < end && begin < ahead + mine : ahead <= begin && begin < ahead + mine) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
       const unsigned n = (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
-      if (begin < at + n) {
-        s_inst = i;
+      if (alone) {
+        if (n > 0 && at >= begin && at < end) {
+          atomicMin(&s_first[(int)((at - begin) / share)], i);
+          atomicMax(&s_end, i + 1);
+        }
+      } else if (begin < at + n) {
+        s_first[0] = i;
         s_from = (int)(begin - at);
         break;
       }
@@ -275,17 +299,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     }
   }
   __syncthreads();
-  int inst = __builtin_amdgcn_readfirstlane(s_inst), from = __builtin_amdgcn_readfirstlane(s_from);
+  int inst = __builtin_amdgcn_readfirstlane(s_first[alone ? wave : 0]), from = alone ? 0 : __builtin_amdgcn_readfirstlane(s_from);
   unsigned long long left = end - begin, done = begin;      // groups to do, and the number of the next one
+  int mine_to = 0;                                          // alone: the first instance behind this wave's
+  if (alone) {
+    mine_to = s_end;
+    for (int w = kWaves - 1; w > wave; --w) mine_to = s_first[w] < mine_to ? s_first[w] : mine_to;
+  }
+  const int step = alone ? 1 : kWaves;
+
   const float scale = kLog2E / sqrtf((float)D);
   const u32x4* mine_rows = s_rows + wave * F::WAVE;
   const unsigned ring = lds_address(mine_rows);
   float* s_out = reinterpret_cast<float*>(s_rows);
-  for (; left > 0; ++inst, from = 0) {
+  for (; alone ? left > 0 && inst < mine_to : left > 0; ++inst, from = 0) {
     const Seen s = seen_of(a.r.len[inst], a.r.t_cap, a.window, a.n_first);
     if (s.n <= from) continue;                             // an empty instance
-    const int to = (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
-    left -= (unsigned)(to - from);
+    const int to = alone ? s.n : (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
+    if (!alone) left -= (unsigned)(to - from);
     const bool whole = from == 0 && to == s.n;
     // The other pieces: of the workgroups from w0 on.  The last of them to be done joins them; with weights a second launch does.
     int w0 = blockIdx.x, parts = 1;
@@ -297,8 +328,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     unsigned long long* ticket = a.tickets + (size_t)w0 * kTicketStride;      // (an instance that begins in a workgroup and does not end there: one at most)
 
     // This wave's groups are from + wave, from + wave + 4, ...; two of them are on their way to LDS while one is worked off.
-    const int mine_n = to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0;
-    const int u0 = from + wave;
+    const int mine_n = alone ? s.n : (to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0);
+    const int u0 = alone ? 0 : from + wave;
     Place next[2];                                         // of the groups behind the ones that were sent for
     if (mine_n > 0) {
 #pragma unroll
@@ -307,7 +338,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         to_lds<false>(static_cast<const u32x4*>(a.q) + (size_t)inst * G * F::PIECES, (piece < G * F::PIECES ? piece : 0) * 16,
                       ring + (4 * F::TILE + x * kWave) * 16);
       }
-      const Place p = place_of(a.r, inst, s, u0), p1 = place_of(a.r, inst, s, mine_n > 1 ? u0 + kWaves : u0);
+      const Place p = place_of(a.r, inst, s, u0), p1 = place_of(a.r, inst, s, mine_n > 1 ? u0 + step : u0);
       send<F, false>(a.K, p, s, lane, ring);
       send<F, true>(a.V, p, s, lane, ring + F::TILE * 16);
       if (mine_n > 1) {
@@ -335,7 +366,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     for (int it = 0; it < mine_n; ++it) {
       const Place here = next[0];
       next[0] = next[1];
-      next[1] = place_of(a.r, inst, s, u0 + kWaves * (it + 2 < mine_n ? it + 2 : it));
+      next[1] = place_of(a.r, inst, s, u0 + step * (it + 2 < mine_n ? it + 2 : it));
       const bool more = it + 2 < mine_n;
       const int t0 = here.t0;
       const unsigned slot = ring + (it & 1) * 2 * F::TILE * 16;
@@ -427,6 +458,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         o[h][e] = sum32(o[h][e]);
       }
     }
+    if (alone) {
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        const float all = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), h));
+        if (lane < F::PIECES) {
+          float* to_out = a.out + ((size_t)inst * G + h) * D + lane * F::E;
+#pragma unroll
+          for (int e = 0; e < F::E; ++e) to_out[e] = o[h][e] / all;
+        }
+      }
+      if (ACC && lane < G) {
+        a.whole[((size_t)inst * G + lane) * 2] = m;
+        a.whole[((size_t)inst * G + lane) * 2 + 1] = sum;
+      }
+      continue;
+    }
     if (lane < F::PIECES) {
 #pragma unroll
       for (int h = 0; h < G; ++h)
@@ -476,8 +523,8 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
   if (s.n == 0) return;
   const int j0 = ((int)blockIdx.x - 1) * 4 * kThreads;
   if (blockIdx.x > 0 && (j0 >= s.L || (j0 >= s.f && j0 + 4 * kThreads <= s.lo))) return;
-  const unsigned long long at = a.before[i], per = share_of(a.before[a.r.n_inst], wgs);
-  const int w0 = (int)(at / per), parts = (int)((at + (unsigned)s.n - 1) / per) - w0 + 1;
+  const unsigned long long at = a.before[i], groups = a.before[a.r.n_inst], per = share_of(groups, wgs);
+  const int w0 = (int)(at / per), parts = groups == kAlone ? 1 : (int)((at + (unsigned)s.n - 1) / per) - w0 + 1;
   if (parts > 1) {
     join_pieces<G, D, false>(a, blockIdx.x == 0 ? i : -1, w0, parts, s_join, join_bytes(G, D), s_m, s_inv);
   } else if (tid < G) {

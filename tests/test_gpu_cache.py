@@ -77,6 +77,10 @@ def test_decode(case, weights):
     (1500, 32, lambda i: 0 if i != 777 else 31),          # one that is not empty
     (40, 4096, lambda i: 4096 if i == 39 else i % 5),     # nearly all of the rows in the last one
     (3, 16384, lambda i: 16383 - i),                      # pieces of one instance in many workgroups
+    (2500, 64, lambda i: (i * 37) % 65),                  # more instances than workgroups, short: a wave each
+    (1300, 1040, lambda i: 1024 if i % 97 == 0 else i % 3),   # the longest that a wave takes, and many empty ones
+    (1300, 1040, lambda i: 1025 if i == 700 else 16),     # one row longer
+    (6000, 32, lambda i: 32 if i > 5000 else 0),          # all in the last ones
 ])
 def test_decode_shares(n, t_cap, lens):
     """Rows dealt to workgroups regardless of where instances begin: every kind of piece, weights and outputs."""
@@ -89,10 +93,12 @@ def test_decode_shares(n, t_cap, lens):
     ctx = c.context(g, ap)
     out, acc = torch.full((n, g, d), 7.0, device="cuda:0"), torch.zeros((n, t_cap), device="cuda:0")
     ctx.cache_decode(q.to("cuda:0"), c.gK, c.gV, torch.tensor(lens, dtype=torch.int32, device="cuda:0"), 0, 0, out, acc, _ws(ctx, 0, True))
-    out, acc = out.cpu().double(), acc.cpu().double()
+    alone = torch.full_like(out, 7.0)
+    ctx.cache_decode(q.to("cuda:0"), c.gK, c.gV, torch.tensor(lens, dtype=torch.int32, device="cuda:0"), 0, 0, alone, None, _ws(ctx, 0, False))
+    out, acc, alone = out.cpu().double(), acc.cpu().double(), alone.cpu().double()
     for i, L in enumerate(lens):
         ref, w, out_off, w_off = attend(q[i], c.K[i, :L], c.V[i, :L], L - 1, 0, 0)
-        assert ((out[i] - ref).abs() <= out_off).all(), (i, L)
+        assert ((out[i] - ref).abs() <= out_off).all() and ((alone[i] - ref).abs() <= out_off).all(), (i, L)
         assert ((acc[i, :L] - w).abs() <= w_off + HALF[torch.float32] * w).all(), (i, L)
         assert not acc[i, L:].any()
 
