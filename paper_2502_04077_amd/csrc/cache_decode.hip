@@ -236,6 +236,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const int i_end = i_begin + chunk < a.r.n_inst ? i_begin + chunk : a.r.n_inst;
   unsigned long long mine = 0;
   int longest = 0;
+#pragma unroll 4
   for (int i = i_begin; i < i_end; ++i) {
     const int n = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
     mine += (unsigned)n;
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     const unsigned long long y = __shfl_up(upto, o, 64);
     if (lane >= o) upto += y;
   }
-  longest = (int)wave_max((float)(longest < kShort + 1 ? longest : kShort + 1));
+  if (a.r.n_inst > F::WGS) longest = (int)wave_max((float)(longest < kShort + 1 ? longest : kShort + 1));
   if (lane == 63) {
     s_wave[wave] = upto;
     s_longest[wave] = longest;

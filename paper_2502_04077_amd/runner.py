@@ -201,7 +201,8 @@ class CacheRun:
 
     def prefill(self, q, k, v, n_new=None):
         """The next chunk of every prompt, q [n_inst][m][g][d] and k, v [n_inst][m][d] with m <= q_cap; n_new: int32 [n_inst], how many
-        of the m tokens count.  Returns the outputs [n_inst][m][g][d]."""
+        of the m tokens count.  Returns the outputs [n_inst][m][g][d], a buffer that the next chunk uses again; its rows from n_new[i]
+        on hold nothing of this chunk."""
         m = q.shape[1]
         if m > self.q_cap:
             raise ValueError(f"a chunk has at most q_cap = {self.q_cap} tokens")
@@ -212,7 +213,8 @@ class CacheRun:
         return out
 
     def step(self, q, k, v):
-        """One decode step: q [n_inst][g][d], k and v [n_inst][d].  Returns the outputs, float [n_inst][g][d]."""
+        """One decode step: q [n_inst][g][d], k and v [n_inst][d].  Returns the outputs, float [n_inst][g][d], a buffer that the
+        next step uses again."""
         self._grow(1, 1)
         self.ctx.cache_append(k.unsqueeze(1), v.unsqueeze(1), None, self.len, self.K, self.V)
         self.ctx.cache_decode(q, self.K, self.V, self.len, self.window, self.n_first, self.out, self.acc, self.ws)

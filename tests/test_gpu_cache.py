@@ -344,3 +344,43 @@ def test_run_under_a_budget(paged):
     full = run.K.view(n, cap, 128) if not paged else run.K[table.long().view(-1)].view(n, cap, 128)
     for i in range(n):
         assert torch.equal(full[i, :len(K[i])].cpu(), K[i])
+
+
+def test_far_rows():
+    """Caches of 12 million rows: offsets pass 32 bits, in rows' bytes and in the pool's; only a window and a few rows are seen or kept."""
+    import paper_2502_04077_amd as ap
+    n, t_cap, d, b, window, n_first, lens = 2, 12_000_000, 128, 64, 50, 5, [12_000_000, 11_999_989]
+    dev = torch.device("cuda:0")
+    ctx = ap.Context(n_inst=n, g=1, head_dim=d, block=b, hist_len=1, t_cap=t_cap, k_blocks=1, n_sink=0, n_local=0, c1=4, c2=4, kv_dtype="bf16")
+    K, V = (torch.empty((n, t_cap, d), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    gen = torch.Generator().manual_seed(3)
+    rows = lambda *s: torch.randn(s, generator=gen).to(torch.bfloat16)  # noqa: E731
+    L = torch.tensor(lens, dtype=torch.int32, device=dev)
+    head_k, head_v, tail_k, tail_v = rows(n, n_first, d), rows(n, n_first, d), rows(n, 60, d), rows(n, 60, d)
+    K[:, :n_first], V[:, :n_first] = head_k.to(dev), head_v.to(dev)
+    ctx.cache_append(tail_k.to(dev), tail_v.to(dev), None, L, K, V)
+    for i in range(n):
+        assert torch.equal(K[i, lens[i] - 60:lens[i]].cpu(), tail_k[i]) and torch.equal(V[i, lens[i] - 60:lens[i]].cpu(), tail_v[i])
+    q, out, acc = rows(n, 3, 1, d), torch.zeros((n, 1, d), device=dev), torch.zeros((n, t_cap), device=dev)
+    chunk = torch.zeros((n, 3, 1, d), dtype=torch.bfloat16, device=dev)
+    ctx.cache_prefill(q.to(dev), None, K, V, L, window, n_first, chunk, None, _ws(ctx, 3, False))
+    ctx.cache_decode(q[:, 2].contiguous().to(dev), K, V, L, window, n_first, out, acc, _ws(ctx, 0, True))
+    for i in range(n):
+        for r in range(3):
+            k, v = (torch.cat([h[i], t[i, 10 - 2 + r:58 + r]]) for h, t in ((head_k, tail_k), (head_v, tail_v)))
+            ref, w, off, w_off = attend(q[i, r], k, v, len(k) - 1, 0, 0)
+            assert (chunk[i, r].cpu().double() - ref).abs().max() <= 2.5 * HALF[torch.bfloat16] * v.double().abs().max() + off.max(), (i, r)
+        assert ((out[i].cpu().double() - ref).abs() <= off).all(), i
+        got = torch.cat([acc[i, :n_first], acc[i, lens[i] - 50:lens[i]]]).cpu().double()
+        assert ((got - w).abs() <= w_off + HALF[torch.float32] * w).all() and abs(acc[i].double().sum().item() - 1) < 1e-5, i
+    far = [7, 4_000_000, 8_388_608, 9_000_001, 11_000_000]
+    acc.zero_()
+    acc[:, far] = 3.0
+    for i in range(n):
+        K[i, far] = V[i, far] = rows(len(far), d).to(dev)
+    kept = torch.zeros((n, 20), dtype=torch.int32, device=dev)
+    want = [torch.cat([K[i, :n_first], K[i, far], K[i, lens[i] - 10:lens[i]]]).clone() for i in range(n)]
+    ctx.cache_evict(K, V, acc, L, 20, n_first, 10, acc, L, kept)
+    for i in range(n):
+        assert kept[i].tolist() == list(range(n_first)) + far + list(range(lens[i] - 10, lens[i]))
+        assert torch.equal(K[i, :20], want[i]) and acc[i].count_nonzero().item() == len(far)
