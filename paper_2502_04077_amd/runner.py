@@ -196,8 +196,20 @@ class CacheRun:
     def _grow(self, n, by):
         if self.longest + by > self.w.t_cap:
             raise ValueError(f"caches of up to {self.longest} rows have no room for {by} more (t_cap = {self.w.t_cap})")
-        self.longest += by
         self.len += n
+        self.longest += by
+
+    def _grown(self, n, by, calls):
+        """The calls on caches that are n rows longer.  If one of them is refused, the lengths are what they were: rows behind them
+        hold nothing."""
+        longest = self.longest
+        self._grow(n, by)
+        try:
+            calls()
+        except Exception:
+            self.len -= n
+            self.longest = longest
+            raise
 
     def prefill(self, q, k, v, n_new=None):
         """The next chunk of every prompt, q [n_inst][m][g][d] and k, v [n_inst][m][d] with m <= q_cap; n_new: int32 [n_inst], how many
@@ -206,18 +218,21 @@ class CacheRun:
         m = q.shape[1]
         if m > self.q_cap:
             raise ValueError(f"a chunk has at most q_cap = {self.q_cap} tokens")
-        self._grow(m if n_new is None else n_new.clamp(0, m), m)
-        self.ctx.cache_append(k, v, n_new, self.len, self.K, self.V)
         out = self.chunk_out.view(-1)[:q.numel()].view(q.shape)
-        self.ctx.cache_prefill(q, n_new, self.K, self.V, self.len, self.window, self.n_first, out, self.acc, self.ws)
+
+        def calls():
+            self.ctx.cache_append(k, v, n_new, self.len, self.K, self.V)
+            self.ctx.cache_prefill(q, n_new, self.K, self.V, self.len, self.window, self.n_first, out, self.acc, self.ws)
+        self._grown(m if n_new is None else n_new.clamp(0, m), m, calls)
         return out
 
     def step(self, q, k, v):
         """One decode step: q [n_inst][g][d], k and v [n_inst][d].  Returns the outputs, float [n_inst][g][d], a buffer that the
         next step uses again."""
-        self._grow(1, 1)
-        self.ctx.cache_append(k.unsqueeze(1), v.unsqueeze(1), None, self.len, self.K, self.V)
-        self.ctx.cache_decode(q, self.K, self.V, self.len, self.window, self.n_first, self.out, self.acc, self.ws)
+        def calls():
+            self.ctx.cache_append(k.unsqueeze(1), v.unsqueeze(1), None, self.len, self.K, self.V)
+            self.ctx.cache_decode(q, self.K, self.V, self.len, self.window, self.n_first, self.out, self.acc, self.ws)
+        self._grown(1, 1, calls)
         self.steps_done += 1
         if self.steps_done % self.evict_every == 0:
             self.evict()
