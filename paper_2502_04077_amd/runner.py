@@ -218,6 +218,8 @@ class CacheRun:
         m = q.shape[1]
         if m > self.q_cap:
             raise ValueError(f"a chunk has at most q_cap = {self.q_cap} tokens")
+        if k.shape[:2] != q.shape[:2] or v.shape[:2] != q.shape[:2]:
+            raise ValueError(f"{list(q.shape[:2])} queries and rows k, v of {list(k.shape[:2])}, {list(v.shape[:2])}")
         out = self.chunk_out.view(-1)[:q.numel()].view(q.shape)
 
         def calls():

@@ -24,6 +24,12 @@ def _state(run):
     return run.len.tolist(), run.longest, run.steps_done
 
 
+class _Nothing:
+    """Calls that do nothing."""
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 I32 = torch.int32
 REFUSED = {   # name -> call that the library or torch refuses
     "step on the host": lambda run: run.step(*_rows()),
@@ -34,6 +40,8 @@ REFUSED = {   # name -> call that the library or torch refuses
     "too few counts": lambda run: run.prefill(*_rows(7), torch.ones(5, dtype=I32)),
     "one count": lambda run: run.prefill(*_rows(7), torch.ones(1, dtype=I32)),
     "queries of more heads": lambda run: run.prefill(torch.zeros(6, 80, 5, 128, dtype=torch.bfloat16), *_rows(80)[1:], torch.ones(6, dtype=I32)),
+    "fewer rows than queries": lambda run: run.prefill(_rows(7)[0], *_rows(5)[1:]),
+    "more rows than queries": lambda run: run.prefill(_rows(5)[0], *_rows(7)[1:], torch.full((6,), 5, dtype=I32)),
     "a longer chunk than q_cap": lambda run: run.prefill(*_rows(81)),
 }
 
@@ -44,6 +52,8 @@ def test_a_refused_call_leaves_the_lengths(name):
     run.len += torch.tensor([3, 0, 17, 90, 90, 1], dtype=I32)
     run.longest = 90
     before, kept = _state(run), run.len
+    if "fewer" in name or "more rows" in name:
+        run.ctx = _Nothing()                               # (what the run has to see by itself)
     with pytest.raises((ValueError, RuntimeError)):
         REFUSED[name](run)
     assert _state(run) == before and run.len is kept
