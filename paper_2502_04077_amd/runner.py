@@ -167,7 +167,8 @@ class CacheRun:
     least attention weight - the eviction that the predicted selection of DecodeRun is an alternative to.  The first n_sink and the last
     n_local blocks of the workload's budget stay, as there; no history and no predictor.
 
-    Every instance starts empty.  The lengths live on the device, so the host only knows how long a cache can be at most."""
+    Every instance starts empty.  The lengths live on the device, so the host only knows how long a cache can be at most; it asks for them
+    where that is too long for what is to come."""
 
     def __init__(self, w, device="cuda:0", q_cap=1, window=0, evict_every=64, table=None, n_pages=0):
         """q_cap: most tokens of a chunk.  table: int32 [n_inst][nb_cap] into a pool of n_pages pages, every page an instance's own;
@@ -202,6 +203,10 @@ class CacheRun:
     def _grown(self, n, by, calls):
         """The calls on caches that are n rows longer.  If one of them is refused, the lengths are what they were: rows behind them
         hold nothing."""
+        if self.longest + by > self.w.t_cap:
+            # The bound counts every token of a chunk, the caches may be shorter: only now are the device's lengths asked, and waited for.
+            self.longest, after = torch.stack([self.len.max(), (self.len + n).max()]).tolist()
+            by = after - self.longest
         longest = self.longest
         self._grow(n, by)
         try:

@@ -78,3 +78,36 @@ def test_a_call_that_fails_behind_others_leaves_the_lengths(call):
         else:
             run.step(*_rows())
     assert done[-1] == call and _state(run) == before
+
+
+def test_ragged_chunks_go_in_while_there_is_room():
+    """Chunks of 80 of which few tokens count: no cache is anywhere near its 208 rows, whatever the chunks' sum."""
+    run = _run()
+    run.ctx = _Nothing()
+    new = torch.tensor([16, 0, 3, 1, 16, 9], dtype=I32)
+    for i in range(13):
+        run.prefill(*_rows(80), new)
+        assert run.len.tolist() == ((i + 1) * new).tolist() and run.longest >= 16 * (i + 1)
+    assert run.len.max() == 208 == run.longest
+    before = _state(run)
+    with pytest.raises(ValueError):
+        run.prefill(*_rows(80), new)                       # two caches are full
+    with pytest.raises(ValueError):
+        run.step(*_rows())
+    assert _state(run) == before
+    run.prefill(*_rows(80), torch.tensor([0, 80, 80, 80, -5, 91], dtype=I32))
+    assert run.len.tolist() == [208, 80, 39 + 80, 13 + 80, 208, 117 + 80] and run.longest == 208
+
+
+def test_steps_go_on_behind_a_ragged_chunk():
+    run = _run()
+    run.ctx = _Nothing()
+    run.evict_every = 10 ** 9
+    for new in (1, 2):
+        run.prefill(*_rows(80), torch.full((6,), new, dtype=I32))
+    for _ in range(205):
+        run.step(*_rows())
+    assert run.len.tolist() == [208] * 6 and run.longest == 208
+    with pytest.raises(ValueError):
+        run.step(*_rows())
+    assert run.len.tolist() == [208] * 6
