@@ -28,6 +28,10 @@ static bool q_cap_ok(const Shape& s, int32_t q_cap) { return q_cap >= 1 && q_cap
 
 // A launch has less than 2^32 threads.
 static bool fits(long long threads) { return threads < (1ll << 32); }
+// Chunks that a prefill takes: 256 threads for 128 rows of q.
+static bool chunk_ok(const Shape& s, int32_t q_cap) {
+  return q_cap_ok(s, q_cap) && fits(((long long)q_cap * s.g + 127) / 128 * 256 * s.n_inst);
+}
 // A window of t_cap rows and more shows all of them; so sums of positions and windows stay in 32 bits.
 static int seen_window(const Shape& s, int32_t window) { return window >= s.t_cap ? 0 : window; }
 static int seen_first(const Shape& s, int32_t n_first) { return n_first < s.t_cap ? n_first : s.t_cap; }
@@ -35,7 +39,7 @@ static int seen_first(const Shape& s, int32_t n_first) { return n_first < s.t_ca
 extern "C" {
 
 size_t ap_cache_workspace_bytes(const ap_ctx* ctx, int32_t q_cap, int32_t weights) {
-  if (ctx == nullptr || q_cap < 0 || (q_cap > 0 && !q_cap_ok(ctx->s, q_cap))) return 0;
+  if (ctx == nullptr || q_cap < 0 || (q_cap > 0 && !chunk_ok(ctx->s, q_cap))) return 0;
   const size_t decode = ap::cache_decode_ws(ctx->s, weights != 0).total;
   const size_t prefill = q_cap > 0 ? ap::cache_prefill_ws(ctx->s, q_cap, weights != 0).total : 0;
   return decode > prefill ? decode : prefill;
@@ -80,7 +84,7 @@ int ap_cache_prefill(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_c
   AP_OPTIONAL_PTR(acc); AP_REQUIRE_PTR(ws);
   if (window < 0 || n_first < 0) return AP_ERR_ARG;
   const Shape& s = ctx->s;
-  if (!q_cap_ok(s, q_cap) || !fits(((long long)q_cap * s.g + 127) / 128 * 256 * s.n_inst)) return AP_ERR_RANGE;
+  if (!chunk_ok(s, q_cap)) return AP_ERR_RANGE;
   const ap::CacheQWs w = ap::cache_prefill_ws(s, q_cap, acc != nullptr);
   char* base = static_cast<char*>(ws);
   ap::PrefillArgs a;
