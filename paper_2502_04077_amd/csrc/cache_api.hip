@@ -1,6 +1,40 @@
 // C entry points of the calls on caches whose instances have lengths of their own: argument checks, workspace, launches.
 #include "cache_internal.h"
 
+namespace ap {
+
+CacheWs cache_decode_ws(const Shape& s, bool weights) {
+  CacheWs w;
+  size_t o = 0;
+  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
+  w.before = take(((size_t)s.n_inst + 1) * 8);
+  w.whole = take((size_t)s.n_inst * s.g * 2 * 4);
+  w.part_ml = take((size_t)2 * kCacheDecodeWgs * s.g * 2 * 4);
+  w.part_acc = take((size_t)2 * kCacheDecodeWgs * s.g * s.d * 4);
+  w.tickets = take((size_t)kCacheDecodeWgs * kTicketStride * 8);
+  w.logits = take(weights ? (size_t)s.n_inst * s.g * s.t_cap * 4 : 0);
+  w.total = o;
+  return w;
+}
+CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
+  CacheQWs w;
+  size_t o = 0;
+  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
+  w.stat = take(weights ? (size_t)s.n_inst * cache_stat_rows(s, q_cap) * 2 * 4 : 0);
+  // (chunks x instances x tiles, whatever the window: more than one chunk only below kColumnWgs workgroups)
+  w.sums = take(weights ? (size_t)(2 * kColumnWgs) * kPrefillRows * 4 : 0);
+  // Rows of q in splits, for any q_cap up to this one: a workgroup's 128 each, and not more than all rows in the most splits.
+  long long part = (long long)kSplitWgs * kPrefillRows;
+  if (part > (long long)kMostSplits * s.n_inst * q_cap * s.g) part = (long long)kMostSplits * s.n_inst * q_cap * s.g;
+  if (s.n_inst > kSplitWgs / 2) part = 0;
+  w.part_ml = take((size_t)part * 2 * 4);
+  w.part_o = take((size_t)part * s.d * 4);
+  w.total = o;
+  return w;
+}
+
+}  // namespace ap
+
 using ap::CacheRows;
 using ap::Shape;
 

@@ -564,20 +564,6 @@ template <typename T, int D> hipError_t run_g(int g, const DecodeArgs& a, hipStr
 
 }  // namespace
 
-CacheWs cache_decode_ws(const Shape& s, bool weights) {
-  CacheWs w;
-  size_t o = 0;
-  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
-  w.before = take(((size_t)s.n_inst + 1) * 8);
-  w.whole = take((size_t)s.n_inst * s.g * 2 * 4);
-  w.part_ml = take((size_t)2 * kCacheDecodeWgs * s.g * 2 * 4);
-  w.part_acc = take((size_t)2 * kCacheDecodeWgs * s.g * s.d * 4);
-  w.tickets = take((size_t)kCacheDecodeWgs * kTicketStride * 8);
-  w.logits = take(weights ? (size_t)s.n_inst * s.g * s.t_cap * 4 : 0);
-  w.total = o;
-  return w;
-}
-
 hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& args, hipStream_t st) {
   DecodeArgs a = args;
   a.nonce = new_nonce(kTicketBits);

@@ -41,6 +41,12 @@ struct PrefillArgs {
 };
 
 constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call
+constexpr int kPrefillRows = 128;        // rows of q per workgroup of a prefill; of the cache, for the columns' sums
+constexpr int kSplitWgs = 512;           // workgroups that splits of the cache may come to
+constexpr int kMostSplits = 64;
+constexpr int kColumnWgs = 4096;         // workgroups of the columns' sums that fill the chip
+// Rows of q of an instance, in whole tiles.
+inline int cache_stat_rows(const Shape& s, int q_cap) { return (q_cap * s.g + 63) / 64 * 64; }
 
 struct CacheWs { size_t before, whole, part_ml, part_acc, tickets, logits, total; };     // decode, in bytes
 CacheWs cache_decode_ws(const Shape& s, bool weights);

@@ -20,11 +20,7 @@ namespace ap {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kTileRows = 128;               // rows of q per workgroup; of the cache, for the columns' sums
-constexpr int kSplitWgs = 512;               // workgroups that splits of the cache may come to
-constexpr int kMostSplits = 64;
 constexpr int kLeastTiles = 2;               // tiles of a split
-constexpr int kColumnWgs = 4096;             // workgroups of the columns' sums that fill the chip
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -188,8 +184,8 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [NB][K, V][TILE]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
-  const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kTileRows;            // the longest ones first
-  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kTileRows);
+  const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kPrefillRows;            // the longest ones first
+  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kPrefillRows);
   const int rows = s.n * G;                                // of q
   if (row0 >= rows) return;
 
@@ -417,7 +413,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_join_kernel(PrefillArg
   }
 }
 
-// Tiles of kTileRows cache rows that an instance's queries see: rows [0, f) and [lo, L), f <= lo.
+// Tiles of kPrefillRows cache rows that an instance's queries see: rows [0, f) and [lo, L), f <= lo.
 struct Columns {
   int L, nq, base, lo, f, tiles, ts, tb;
   __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
@@ -429,9 +425,9 @@ __device__ __forceinline__ Columns columns_of(const PrefillArgs& a, int inst) {
   c.base = c.L - c.nq;
   c.lo = a.window > 0 && c.base >= a.window ? c.base - a.window + 1 : 0;
   c.f = a.n_first < c.lo ? a.n_first : c.lo;
-  c.ts = (c.f + kTileRows - 1) / kTileRows;
-  c.tb = c.lo / kTileRows > c.ts ? c.lo / kTileRows : c.ts;
-  c.tiles = c.L == 0 || c.nq == 0 ? 0 : c.ts + ((c.L - 1) / kTileRows >= c.tb ? (c.L - 1) / kTileRows - c.tb + 1 : 0);
+  c.ts = (c.f + kPrefillRows - 1) / kPrefillRows;
+  c.tb = c.lo / kPrefillRows > c.ts ? c.lo / kPrefillRows : c.ts;
+  c.tiles = c.L == 0 || c.nq == 0 ? 0 : c.ts + ((c.L - 1) / kPrefillRows >= c.tb ? (c.L - 1) / kPrefillRows - c.tb + 1 : 0);
   return c;
 }
 
@@ -447,14 +443,14 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
   const int inst = blockIdx.y, chunk = blockIdx.z;
   const Columns col = columns_of(a, inst);
   if ((int)blockIdx.x >= col.tiles) return;
-  const int t0 = col.tile(blockIdx.x) * kTileRows, L = col.L, base = col.base, rows = col.nq * G;
+  const int t0 = col.tile(blockIdx.x) * kPrefillRows, L = col.L, base = col.base, rows = col.nq * G;
   // Rows of q in this chunk, whole tiles of them, that see one of the cache rows at least.
   const int all_tiles = (rows + QT - 1) / QT, each = (all_tiles + a.chunks - 1) / a.chunks;
   int begin = chunk * each * QT, end = begin + each * QT < rows ? begin + each * QT : rows;
   const int first_q = t0 - base > 0 ? t0 - base : 0;                          // the first query that lies at t0 or behind it
   if (begin < first_q * G) begin = first_q * G / QT * QT;
   if (a.window > 0 && t0 >= a.n_first) {                                      // and the last that still sees t0 + 127
-    const long long last_q = (long long)t0 + kTileRows - 1 + a.window - 1 - base;
+    const long long last_q = (long long)t0 + kPrefillRows - 1 + a.window - 1 - base;
     if ((last_q + 1) * G < end) end = (int)((last_q + 1) * G);
   }
   const int j0 = t0 + 32 * wave;                           // this wave's cache rows
@@ -547,37 +543,35 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
       const int j = j0 + reg_row(i, hb);
       if (j >= L) continue;
       if (a.chunks == 1) a.acc[(size_t)inst * a.r.t_cap + j] += total[i];
-      else a.sums[(((size_t)chunk * a.r.n_inst + inst) * gridDim.x + blockIdx.x) * kTileRows + j - t0] = total[i];
+      else a.sums[(((size_t)chunk * a.r.n_inst + inst) * gridDim.x + blockIdx.x) * kPrefillRows + j - t0] = total[i];
     }
   }
 }
 
 // The chunks' sums, one after the other, so that the result does not depend on which was ready first.
-__global__ __launch_bounds__(kTileRows) void cache_weights_add_kernel(PrefillArgs a) {
+__global__ __launch_bounds__(kPrefillRows) void cache_weights_add_kernel(PrefillArgs a) {
   const int inst = blockIdx.y;
   const Columns col = columns_of(a, inst);
   if ((int)blockIdx.x >= col.tiles) return;
-  const int j = col.tile(blockIdx.x) * kTileRows + threadIdx.x;
+  const int j = col.tile(blockIdx.x) * kPrefillRows + threadIdx.x;
   if (j >= col.L) return;
   float x = 0.f;
 #pragma unroll 8
   for (int c = 0; c < a.chunks; ++c)
-    x += a.sums[(((size_t)c * a.r.n_inst + inst) * gridDim.x + blockIdx.x) * kTileRows + threadIdx.x];
+    x += a.sums[(((size_t)c * a.r.n_inst + inst) * gridDim.x + blockIdx.x) * kPrefillRows + threadIdx.x];
   a.acc[(size_t)inst * a.r.t_cap + j] += x;
 }
 
-// Rows of q of an instance, in whole tiles.
-static int stat_rows(const Shape& s, int q_cap) { return (q_cap * s.g + 63) / 64 * 64; }
 // Most tiles of cache rows that an instance's queries can see.
 static long long most_columns(const Shape& s, int q_cap, int window, int n_first) {
-  const long long all = ((long long)s.t_cap + kTileRows - 1) / kTileRows;
+  const long long all = ((long long)s.t_cap + kPrefillRows - 1) / kPrefillRows;
   if (window <= 0) return all;
-  const long long some = ((long long)n_first + kTileRows - 1) / kTileRows + ((long long)window + q_cap) / kTileRows + 2;
+  const long long some = ((long long)n_first + kPrefillRows - 1) / kPrefillRows + ((long long)window + q_cap) / kPrefillRows + 2;
   return some < all ? some : all;
 }
 // Splits of the cache where the rows of q alone leave CUs without work: up to 512 workgroups, of at least kLeastTiles tiles.
 static int cache_splits(const Shape& s, int q_cap, int window, int n_first) {
-  const long long wgs = (((long long)q_cap * s.g + kTileRows - 1) / kTileRows) * s.n_inst;
+  const long long wgs = (((long long)q_cap * s.g + kPrefillRows - 1) / kPrefillRows) * s.n_inst;
   const long long rows = window > 0 && (long long)window + q_cap + n_first < s.t_cap ? (long long)window + q_cap + n_first : s.t_cap;
   const int tt = s.kv_dtype == AP_BF16 ? 64 : 32;
   long long splits = kSplitWgs / wgs, most = (rows + tt * kLeastTiles - 1) / (tt * kLeastTiles);
@@ -617,7 +611,7 @@ template <typename T, int D, int G> hipError_t run(const Shape& s, const Prefill
   cache_weights_kernel<T, D, G><<<columns, kThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.chunks == 1) return e;
-  cache_weights_add_kernel<<<dim3(columns.x, columns.y), kTileRows, 0, st>>>(a);
+  cache_weights_add_kernel<<<dim3(columns.x, columns.y), kPrefillRows, 0, st>>>(a);
   return hipGetLastError();
 }
 template <typename T, int D> hipError_t run_g(const Shape& s, const PrefillArgs& a, hipStream_t st) {
@@ -626,27 +620,10 @@ template <typename T, int D> hipError_t run_g(const Shape& s, const PrefillArgs&
 
 }  // namespace
 
-CacheQWs cache_prefill_ws(const Shape& s, int q_cap, bool weights) {
-  CacheQWs w;
-  size_t o = 0;
-  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
-  w.stat = take(weights ? (size_t)s.n_inst * stat_rows(s, q_cap) * 2 * 4 : 0);
-  // (chunks x instances x tiles, whatever the window: more than one chunk only below kColumnWgs workgroups)
-  w.sums = take(weights ? (size_t)(2 * kColumnWgs) * kTileRows * 4 : 0);
-  // Rows of q in splits, for any q_cap up to this one: a workgroup's 128 each, and not more than all rows in the most splits.
-  long long part = (long long)kSplitWgs * kTileRows;
-  if (part > (long long)kMostSplits * s.n_inst * q_cap * s.g) part = (long long)kMostSplits * s.n_inst * q_cap * s.g;
-  if (s.n_inst > kSplitWgs / 2) part = 0;
-  w.part_ml = take((size_t)part * 2 * 4);
-  w.part_o = take((size_t)part * s.d * 4);
-  w.total = o;
-  return w;
-}
-
 hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) {
   PrefillArgs a = args;
-  a.stat_rows = stat_rows(s, a.q_cap);
-  a.tiles = (int)(((long long)a.q_cap * s.g + kTileRows - 1) / kTileRows);
+  a.stat_rows = cache_stat_rows(s, a.q_cap);
+  a.tiles = (int)(((long long)a.q_cap * s.g + kPrefillRows - 1) / kPrefillRows);
   a.splits = cache_splits(s, a.q_cap, a.window, a.n_first);
   a.chunks = a.acc == nullptr ? 1 : column_chunks(s, a.q_cap, most_columns(s, a.q_cap, a.window, a.n_first));
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s, a, st) : run_g<bf16_t, 64>(s, a, st);
