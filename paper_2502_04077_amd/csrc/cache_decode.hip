@@ -51,6 +51,11 @@ __device__ __forceinline__ unsigned long long share_of(unsigned long long groups
   return one <= kLeastGroups ? kLeastGroups : (one <= kLongShare ? one : (all > kLongShare ? all : kLongShare));
 }
 
+// Scores below what 32 bits hold are -inf and weigh nothing.  Where a head has no others yet its maximum is -inf, which exponents do not refer to,
+// and its sum 0, by which nothing is divided: the output is zero.
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float over(float x, float sum) { return sum == 0.f ? 0.f : x / sum; }
+
 template <typename T, int D, int G> struct Form {
   static constexpr int E = 16 / (int)sizeof(T);            // elements of a 16-byte piece
   static constexpr int PIECES = D / E;                     // pieces of a row = lanes that have a V row
@@ -174,18 +179,19 @@ __device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w
     float top = m0[x];
     for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, read(a.part_ml + (slot(p) * G + h) * 2));
     top = wave_max(top);
-    const float f0 = exp2_fast(m0[x] - top);
+    const float use = reference(top);
+    const float f0 = exp2_fast(m0[x] - use);
     if (lane < parts) s[lane * G + h] = f0;
     float all = f0 * l0[x];
     for (int p = lane + 64; p < parts; p += 64) {
-      const float f = exp2_fast(read(a.part_ml + (slot(p) * G + h) * 2) - top);
+      const float f = exp2_fast(read(a.part_ml + (slot(p) * G + h) * 2) - use);
       s[p * G + h] = f;
       all += f * read(a.part_ml + (slot(p) * G + h) * 2 + 1);
     }
     all = wave_sum(all);
     if (lane == 0) {
-      s_m[h] = top;
-      s_inv[h] = 1.f / all;
+      s_m[h] = use;
+      s_inv[h] = over(1.f, all);
     }
   }
   if (inst < 0) {
@@ -412,6 +418,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         }
         m = ref;
       }
+      const float use = reference(m);
       if (ACC && head < G && t0 + 4 * kg < a.r.t_cap) {    // (t_cap is a multiple of 8: four rows are within it or not)
         float4v z;
 #pragma unroll
@@ -420,7 +427,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = exp2_fast(__builtin_fmaf(c[r], scale, -m));
+        const float p = exp2_fast(__builtin_fmaf(c[r], scale, -use));
         sum += p;
         if (head < G) s_p[wave][4 * kg + r][head] = p;
       }
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         if (lane < F::PIECES) {
           float* to_out = a.out + ((size_t)inst * G + h) * D + lane * F::E;
 #pragma unroll
-          for (int e = 0; e < F::E; ++e) to_out[e] = o[h][e] / all;
+          for (int e = 0; e < F::E; ++e) to_out[e] = over(o[h][e], all);
         }
       }
       if (ACC && lane < G) {
@@ -491,13 +498,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       const int h = x / D, e = x % D;
       float top = s_ml[0][h][0];
       for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_ml[w][h][0]);
+      const float use = reference(top);
       float all = 0.f, val = 0.f;
       for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2_fast(s_ml[w][h][0] - top);
+        const float f = exp2_fast(s_ml[w][h][0] - use);
         all += f * s_ml[w][h][1];
         val += f * s_out[w * F::WAVE * 4 + x];
       }
-      if (whole) a.out[((size_t)inst * G + h) * D + e] = val / all;
+      if (whole) a.out[((size_t)inst * G + h) * D + e] = over(val, all);
       else st_shared_out<!ACC>(a.part_acc + (slot * G + h) * D + e, val);
       if (e == 0 && (ACC || !whole)) {
         float* ml = whole ? a.whole + ((size_t)inst * G + h) * 2 : a.part_ml + (slot * G + h) * 2;
@@ -529,8 +537,8 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
   if (parts > 1) {
     join_pieces<G, D, false>(a, blockIdx.x == 0 ? i : -1, w0, parts, s_join, join_bytes(G, D), s_m, s_inv);
   } else if (tid < G) {
-    s_m[tid] = a.whole[((size_t)i * G + tid) * 2];
-    s_inv[tid] = 1.f / a.whole[((size_t)i * G + tid) * 2 + 1];
+    s_m[tid] = reference(a.whole[((size_t)i * G + tid) * 2]);
+    s_inv[tid] = over(1.f, a.whole[((size_t)i * G + tid) * 2 + 1]);
   }
   if (blockIdx.x == 0) return;
   __syncthreads();
