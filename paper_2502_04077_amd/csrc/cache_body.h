@@ -72,6 +72,21 @@ template <int N> __device__ __forceinline__ void landed() { asm volatile("s_wait
 // Reads of LDS are over: what they read may be overwritten.
 __device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// Exponents, in units of log2, are c * scale - m with one rounding, for m the largest product's whole number above.  From 2^24 on the
+// product's own rounding, which m has, is some whole numbers itself (from 2^31 on more than an exponent of 32 bits): there, it is rounded as m
+// was before m is subtracted, and the largest score has the exponent 0.  (-inf, of a head that has seen nothing, counts as far.)
+__device__ __forceinline__ bool is_far(float m) { return !(fabsf(m) < 16777216.f); }
+__device__ __forceinline__ float exp2_of(float c, float scale, float m) {           // exp2(c * scale - m) for any m but -inf
+#pragma clang fp contract(off)
+  const float x = c * scale;
+  return exp2_fast(is_far(m) ? x - m : __builtin_fmaf(c, scale, -m));
+}
+__device__ __forceinline__ float brought_near(float c, float scale, float m) {      // the score whose exponent relative to 0 is c's relative to m
+#pragma clang fp contract(off)
+  const float x = c * scale;
+  return (x - m) / scale;
+}
+
 // Bytes of a 16-byte piece are moved whatever their type.
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 

@@ -427,7 +427,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = exp2_fast(__builtin_fmaf(c[r], scale, -use));
+        const float p = exp2_of(c[r], scale, use);
         sum += p;
         if (head < G) s_p[wave][4 * kg + r][head] = p;
       }
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
   for (int h = 0; h < G; ++h) {
     const float4v z = *reinterpret_cast<const float4v*>(a.logits + ((size_t)i * G + h) * a.r.t_cap + j);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) add[r] += exp2_fast(__builtin_fmaf(z[r], scale, -s_m[h])) * s_inv[h];
+    for (int r = 0; r < 4; ++r) add[r] += exp2_of(z[r], scale, s_m[h]) * s_inv[h];
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r)

@@ -258,9 +258,11 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, c[b][i]);
     top = max32(top);
-    // The reference is a whole number in units of log2 (a change of it rounds nothing), 0 as long as nothing is seen.
+    // The reference is a whole number in units of log2 (a change of it rounds nothing).  Exponents refer to 0 as long as nothing is seen, and where
+    // it is far, as the scores are brought near then.
     const float ref = fmaxf(m, ceilf(top * scale));
-    if (__any(ref != m)) {
+    const bool far = is_far(ref);
+    if (__any((ref != m) | far)) {
       const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
       sum *= shrink;
 #pragma unroll
@@ -268,8 +270,14 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
       m = ref;
+      if (__any(far && m != -INFINITY)) {
+#pragma unroll
+        for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) c[b][i] = far && m != -INFINITY ? brought_near(c[b][i], scale, m) : c[b][i];
+      }
     }
-    const float use = m == -INFINITY ? 0.f : m;
+    const float use = far ? 0.f : ref;
     float part[4] = {0.f, 0.f, 0.f, 0.f};                  // (sums of a tile first: long caches lose fewer digits so)
 #pragma unroll
     for (int b = 0; b < F::TB; ++b)
@@ -515,6 +523,11 @@ __global__ __launch_bounds__(kThreads) void cache_weights_kernel(PrefillArgs a) 
       }
       struct Stat { float m, inv; };
       Stat st = reinterpret_cast<const Stat*>(Q + F::TILE)[32 * b + n];
+      if (__any(is_far(st.m))) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = is_far(st.m) ? brought_near(c[i], scale, st.m) : c[i];
+        st.m = is_far(st.m) ? 0.f : st.m;
+      }
       if (all) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) total[i] = __builtin_fmaf(exp2_fast(__builtin_fmaf(c[i], scale, -st.m)), st.inv, total[i]);

@@ -1,5 +1,5 @@
 """Scores of any size that 32 bits hold: attention over caches where one component of q and K makes them, as powers of two that every
-product and sum holds exactly, and below what 32 bits hold.  Neighbouring scores lie so far apart that the definition gives equal
+product and sum holds exactly, up to 2^102, and below what 32 bits hold.  Neighbouring scores lie so far apart that the definition gives equal
 weight to the rows with the largest one and none to the others, whatever the rounding of the scale."""
 import pytest
 import torch
@@ -18,7 +18,7 @@ SHAPES = [
     (4, 128, "bf16", True, 1040, 300, 0, 0, [1040] * 30 + [300, 301]),      # chunks in many workgroups
 ]
 BELOW = "below"      # scores that 32 bits hold as -inf, in all rows but some of the last
-SIZES = [(k, sign) for k in (20, 26) for sign in (1, -1)] + [(BELOW, 1)]
+SIZES = [(k, sign) for k in (20, 26, 31, 40, 100) for sign in (1, -1)] + [(BELOW, 1)]
 
 
 def _inputs(shape, size, n_q):
