@@ -151,7 +151,7 @@ class Context:
         # what the cache_* calls check their tensors against on every call
         self._n, self._g, self._d, self._t_cap = n_inst, g, head_dim, t_cap
         self._dtype = torch.bfloat16 if self.cfg.kv_dtype == AP_BF16 else torch.float32
-        self._kv_numel = n_inst * t_cap * head_dim
+        self._kv_numel, self._kv_unit = n_inst * t_cap * head_dim, t_cap * head_dim      # of K; of a cache, or a page
         self._decode_ws = [self.cache_workspace_bytes(0, weights) for weights in (False, True)]
 
     def close(self):
@@ -187,7 +187,8 @@ class Context:
     def set_block_table(self, table, n_phys_blocks: int = 0) -> None:
         """table: device int32 [n_inst][nb_cap] (kept alive by the caller), or None for the contiguous layout."""
         _check(self._lib.ap_set_block_table(self._h, None if table is None else _ptr(table), n_phys_blocks))
-        self._kv_numel = (self._n * self._t_cap if table is None else n_phys_blocks * self.cfg.block) * self._d
+        count, rows = (self._n, self._t_cap) if table is None else (n_phys_blocks, self.cfg.block)
+        self._kv_numel, self._kv_unit = count * rows * self._d, rows * self._d
 
     def predict(self, hist, n_pushed, nb_cur, pred, ws) -> None:
         _check(self._lib.ap_predict(self._h, _ptr(hist), n_pushed, nb_cur, _ptr(pred), _ptr(ws), _stream()))
@@ -247,11 +248,23 @@ class Context:
         dev = K.get_device()
         if K.shape != V.shape or K.shape[-1:] != (self._d,) or K.dtype is not self._dtype or V.dtype is not self._dtype:
             raise ValueError("K and V: two tensors [..., head_dim] of one shape, in the context's dtype")
+        if K.numel() != self._kv_numel:
+            self._cache_more(K)
         if dev < 0 or V.get_device() != dev or not (K.is_contiguous() and V.is_contiguous()):
             raise ValueError("K and V: expected contiguous tensors on one device")
+        return dev
+
+    def _cache_more(self, K) -> None:
+        """Checks caches (pools) of another size than the context's: larger ones are taken by rows, or by whole caches (pages)."""
         if K.numel() < self._kv_numel:
             raise ValueError("K and V: fewer rows than the context's caches, or than the pages of its pool")
-        return dev
+        one = 1
+        for x in reversed(K.shape):
+            one *= x
+            if one >= self._kv_unit:
+                break
+        if one != self._kv_unit and K.dim() > 2:
+            raise ValueError(f"K and V: caches (pages) of {self._kv_unit // self._d} rows do not come out of {list(K.shape)}")
 
     @staticmethod
     def _cache_arg(name, t, dtype, shape, dev) -> int:
