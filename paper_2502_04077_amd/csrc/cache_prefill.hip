@@ -177,11 +177,10 @@ __device__ __forceinline__ Work work_of(unsigned b, int tiles, int n_inst) {
   return {(int)(whole + x % rest), (int)(x / rest)};
 }
 
-// NB: buffers, NB - 1 of which are on their way.
-template <typename T, int D, int G, bool STAT, int NB>
+template <typename T, int D, int G, bool STAT>
 __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
   using F = Form<T, D>;
-  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [NB][K, V][TILE]
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
   const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kPrefillRows;            // the longest ones first
@@ -213,31 +212,27 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   const int u_end = a.splits == 1 || s.tiles < u_begin + each ? s.tiles : u_begin + each;
   Run next;
   auto send = [&](int u) {                                 // tile u, whose rows are those of `next`
-    const unsigned to = buffers + (u % NB) * 2 * F::TILE * 16;
+    const unsigned to = buffers + (u % 2) * 2 * F::TILE * 16;
     send_tile<F, false>(a, inst, next, s, wave, to);
     send_tile<F, true>(a, inst, next, s, wave, to + F::TILE * 16);
     next = run_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);         // a tile ahead: the table's latency
   };
   if (u_begin < u_end) {
     next = run_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
-#pragma unroll
-    for (int u = 0; u < NB - 1; ++u)
-      if (u_begin + u < u_end) send(u_begin + u);
+    send(u_begin);
   }
   // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
 #pragma unroll
   for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
   for (int u = u_begin; u < u_end; ++u) {
-    // This tile has landed, those behind it (two at most) are under way; everybody is done with the buffer that is filled next.
-    if (NB > 3 && u + 2 < u_end) landed<4 * F::LOADS>();
-    else if (NB > 2 && u + 1 < u_end) landed<2 * F::LOADS>();
-    else landed<0>();
+    // This tile has landed; everybody is done with the buffer that is filled next.
+    landed<0>();
     lds_read();
     __builtin_amdgcn_s_barrier();
     const int t0 = s.tile(u) * F::TT;
-    const u32x4* Kt = s_tiles + (u % NB) * 2 * F::TILE;
+    const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
     const u32x4* Vt = Kt + F::TILE;
-    if (u + NB - 1 < u_end) send(u + NB - 1);
+    if (u + 1 < u_end) send(u + 1);
     float16v c[F::TB];
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
@@ -601,17 +596,13 @@ static int column_chunks(const Shape& s, int q_cap, long long columns) {
   return (int)chunks;
 }
 
-template <typename T, int D, int G, int NB> void run_attention(const PrefillArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
-  const size_t lds = (size_t)NB * 2 * Form<T, D>::TILE * 16;
-  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false, NB><<<grid, kThreads, lds, st>>>(a);
-  else cache_prefill_kernel<T, D, G, true, NB><<<grid, kThreads, lds, st>>>(a);
-}
 template <typename T, int D, int G> hipError_t run(const Shape& s, const PrefillArgs& a, hipStream_t st) {
-  // Where a CU has one workgroup at most, a tile's work does not cover the next one's way: more of them are under way, in LDS that nobody
-  // else needs.
-  if ((long long)a.tiles * a.r.n_inst * a.splits <= 256) run_attention<T, D, G, 4>(a, st);
-  else run_attention<T, D, G, 2>(a, st);
+  // (More buffers where a CU has one workgroup at most are no faster: with four, a chunk of 100 behind 400 rows, 8 instances, g = 4, d = 128,
+  // 15.2 us and 15.3; 4 tokens behind 32 thousand rows, one instance 21.7 and 21.3, four 24.3 and 23.0.)
+  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
+  const size_t lds = (size_t)2 * 2 * Form<T, D>::TILE * 16;
+  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false><<<grid, kThreads, lds, st>>>(a);
+  else cache_prefill_kernel<T, D, G, true><<<grid, kThreads, lds, st>>>(a);
   if (a.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
