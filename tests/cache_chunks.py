@@ -18,13 +18,13 @@ def attend_chunk(q, K, V, base, window, n_first):
         seen &= (j > p - window) | (j < n_first)
     rows = seen.any(0)
     seen, K, V = seen[:, rows], K[rows], V[rows]
-    count = seen.sum(1)
-    x = (q.reshape(m * g, d) @ K.T).view(m, g, -1) / math.sqrt(d)
+    count, nr = seen.sum(1), K.shape[0]
+    x = (q.reshape(m * g, d) @ K.T).view(m, g, nr) / math.sqrt(d)
     P = torch.softmax(x.masked_fill(~seen[:, None, :], -math.inf), dim=2).nan_to_num(0.0)
-    size = (q.reshape(m * g, d).abs() @ K.abs().T).view(m, g, -1).masked_fill(~seen[:, None, :], 0.0)
+    size = (q.reshape(m * g, d).abs() @ K.abs().T).view(m, g, nr).masked_fill(~seen[:, None, :], 0.0)
     size = size.flatten(1).amax(1) / math.sqrt(d) if size.numel() else torch.zeros(m, dtype=torch.float64)
     rel = 2 * (d + 4) * HALF[torch.float32] * size + (2 * count + 8) * HALF[torch.float32]
     w, w_off = torch.zeros(L, dtype=torch.float64), torch.zeros(L, dtype=torch.float64)
     w[rows], w_off[rows] = P.sum((0, 1)), (P.sum(1) * rel[:, None]).sum(0)
-    by_size = (P.view(m * g, -1) @ V.abs()).view(m, g, d)
-    return (P.view(m * g, -1) @ V).view(m, g, d), w, rel[:, None, None] * by_size, w_off, by_size
+    by_size = (P.view(m * g, nr) @ V.abs()).view(m, g, d)
+    return (P.view(m * g, nr) @ V).view(m, g, d), w, rel[:, None, None] * by_size, w_off, by_size

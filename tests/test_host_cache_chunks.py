@@ -7,7 +7,7 @@ from cache_reference import attend
 
 
 @pytest.mark.parametrize("window,n_first", [(0, 0), (5, 0), (5, 3), (1, 40), (200, 2)])
-@pytest.mark.parametrize("L,m", [(30, 30), (30, 7), (5, 9), (1, 1), (0, 2), (17, 16)])
+@pytest.mark.parametrize("L,m", [(30, 30), (30, 7), (5, 9), (1, 1), (0, 2), (17, 16), (17, 0), (0, 0)])
 def test_by_chunks_and_by_queries(L, m, window, n_first):
     gen = torch.Generator().manual_seed(L * 100 + m)
     q, K, V = (torch.randn(s, generator=gen) for s in ((m, 4, 64), (L, 64), (L, 64)))
