@@ -306,8 +306,9 @@ int ap_cache_decode(ap_ctx* ctx, const void* q, const void* K, const void* V, co
 /* Attention of the newest n_q[i] tokens of every cache, whose rows have been appended: query r lies at position len[i] - n_q[i] + r.
  *   q    device [n_inst][q_cap][g][d] kv dtype
  *   n_q  device int32 [n_inst], clamped into [0, q_cap]; NULL: q_cap for all
- *   out  device [n_inst][q_cap][g][d] kv dtype (bf16 probabilities multiply bf16 rows, so more digits would not be real); rows from
- *        n_q[i] on are left as they are.  A query before position 0 (n_q > len) sees nothing and has a zero output
+ *   out  device [n_inst][q_cap][g][d] kv dtype; rows from n_q[i] on are left as they are.  With bf16, the probabilities that multiply the
+ *        rows of V are rounded to bf16 too, which adds an error of the size of the output's own rounding (sums, maxima and weights are
+ *        not: 32 bits; ap_cache_decode keeps them throughout).  A query before position 0 (n_q > len) sees nothing and has a zero output
  *   acc  as in ap_cache_decode, summed over the queries too */
 int ap_cache_prefill(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
                      int32_t window, int32_t n_first, void* out, float* acc, void* ws, void* stream);

@@ -11,8 +11,9 @@
 //
 // A wave goes over its groups with a running maximum and sum; two groups of K and V are on their way to LDS, past the registers and not
 // kept in the caches, while one is worked off: q . K on the matrix unit, P . V with fp32 multiply-adds, as probabilities of fewer digits
-// would show in the fp32 output.  Measured: 256 instances of 60 to 32790 rows (g = 4, d = 128, pages of 16; 785 MB) 142 us, 5.5 TB/s; 1024
-// with a window of 4096 (g = 8; 2.1 GB) 350 us, 6.0 TB/s; with rows through registers and pages looked up by vector loads, which wait for
+// would show in the fp32 output.  Measured: 256 instances of 60 to 32790 rows (g = 4, d = 128, pages of 16; 785 MB) 149-157 us, 5.1 TB/s; 1024
+// with a window of 4096 (g = 8; 2.1 GB) 353 us, 5.9 TB/s; 64 of 2000 to 16000 rows in fp32 (g = 4; 465 MB, a workgroup a CU) 82 us, 5.7 TB/s,
+// d = 64 49 us, 4.8; with rows through registers and pages looked up by vector loads, which wait for
 // the rows in flight, 246 and 639.  Where more instances than workgroups are all short, every wave takes whole ones: 2048 of 8 to 419 rows
 // (g = 1, 111 MB) 38 us, by shares of a workgroup 61; of 16 to 56 (g = 2, d = 64) 18 and 40.
 #include "cache_body.h"

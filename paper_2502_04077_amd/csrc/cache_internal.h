@@ -42,9 +42,15 @@ struct PrefillArgs {
 
 constexpr int kCacheDecodeWgs = 1024;    // workgroups that share the rows of a decode call
 constexpr int kPrefillRows = 128;        // rows of q per workgroup of a prefill; of the cache, for the columns' sums
-constexpr int kSplitWgs = 512;           // workgroups that splits of the cache may come to
+// Workgroups that splits of the cache may come to, two a CU.  (g = 4, d = 128, 8 instances but where said; up to 256, 512, 1024 of them: 512 tokens
+// behind 15 thousand rows 182, 158, 169 us, 128 behind 16 thousand 57, 55, 69, 1000 behind 3000 92, 92, 96, 300 of 1000 22.4, 25.5, 30.3; 16 behind
+// 8000, 64 instances, 62, 61, 71.)
+constexpr int kSplitWgs = 512;
+// The join has a split a lane.  (4 tokens behind 32 thousand rows, one instance, by 32 and 64 splits 29.5 and 21.7 us, 83 and 153 in fp32.)
 constexpr int kMostSplits = 64;
-constexpr int kColumnWgs = 4096;         // workgroups of the columns' sums that fill the chip
+// Workgroups of the columns' sums that fill the chip.  (Up to 2048, 4096, 8192: chunks of 1365 and 2048 tokens with a window of 2048, whole calls,
+// 289, 277, 285 us; a prompt of 8000 930, 925, 917.)
+constexpr int kColumnWgs = 4096;
 // Rows of q of an instance, in whole tiles.
 inline int cache_stat_rows(const Shape& s, int q_cap) { return (q_cap * s.g + 63) / 64 * 64; }
 

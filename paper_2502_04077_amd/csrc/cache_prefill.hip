@@ -10,17 +10,20 @@
 // operand as they are, since the order of its contraction index is free.  V^T comes out of LDS by the transposing read.
 //
 // A prompt of 8190 tokens (8 instances, g = 4, d = 128) takes 556 us, 990 TFLOP/s of useful products, where a large library product
-// reaches 1223.  What bounds it is the vector unit, which has 32 exponentials and some 170 other instructions a lane for the 32 matrix
-// instructions of a wave's tile, with two waves a SIMD to cover each other, and the clock, which falls to 1.8 GHz under it.  Tried and
-// no faster: the next tile's scores beside this one's exponentials, three waves a SIMD with tiles of 32 rows, 256 rows a workgroup, a
-// higher priority for the matrix phases.
+// reaches 1210.  What bounds it is the vector unit beside the matrix unit: a wave's tile has 32 exponentials and some 170 other instructions a
+// lane for its 32 matrix instructions, some 1180 cycles and 1024, and a SIMD's two waves hardly cover each other - the cycles of both units
+// add up to nearly all of the time -, and the clock, which falls to 1.8 GHz under it.  Tried and no faster: the next tile's scores beside
+// this one's exponentials, three waves a SIMD with tiles of 32 rows, 256 rows a workgroup, a higher priority for the matrix phases.
+// In fp32 (4000 tokens, 8 instances) 1125 us, 117 TFLOP/s, where a large library product reaches 154.
 #include "cache_body.h"
 
 namespace ap {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kLeastTiles = 2;               // tiles of a split
+// Tiles of a split.  (g = 4, d = 128: a chunk of 101 behind 416 rows, 8 instances, by splits of 1, 2, 4 tiles 15.6, 15.6, 16.9 us; 4 tokens
+// behind 2000 rows 12.1, 11.8, 13.5; 300 of 1000 rows 25.5, 25.5, 23.0.)
+constexpr int kLeastTiles = 2;
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -283,8 +286,10 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
       }
     sum += (part[0] + part[1]) + (part[2] + part[3]);
     if constexpr (sizeof(T) == 2) {
-      // Probabilities are rounded to bf16 for the matrix unit, which adds an error of the size of the output's own rounding; their sum
-      // is taken before.
+      // Probabilities are rounded to bf16 for the matrix unit; their sum is taken before.  That adds an error of the size of the output's own
+      // rounding: relative to the definition, outputs of scores spread by 2 are off by 0.0024 (root mean square), 0.0017 if the rounding of the output
+      // were all.  Two bf16 parts of each probability reach the latter, with half as many matrix instructions again and a third of the vector
+      // unit's: a prompt 556 -> 742 us, a window with weights 272 -> 318, a chunk of 101 behind a prefix 15.6 -> 16.4.
 #pragma unroll
       for (int k = 0; k < F::TT / 16; ++k) {
         bf16x8 pb;
@@ -587,7 +592,9 @@ static int cache_splits(const Shape& s, int q_cap, int window, int n_first) {
   if (splits > kMostSplits) splits = kMostSplits;
   return splits < 1 ? 1 : (int)splits;
 }
-// Workgroups of the columns' sums: chunks of the query rows, of at least 512 rows, where the tiles alone are few for the chip.
+// Workgroups of the columns' sums: chunks of the query rows, of at least 512 rows, where the tiles alone are few for the chip.  (Whole calls
+// with weights, g = 4, d = 128.  Chunks of at least 256, 512, 1024 rows: 101 tokens behind 416 rows, 8 instances, 29.0, 31.9, 31.9 us, 1000
+// behind 7000 255, 253, 252.  At most 8, 16, 32 chunks: a prompt of 4000 in one instance 92, 79, 83.)
 static int column_chunks(const Shape& s, int q_cap, long long columns) {
   const long long q_rows = (long long)q_cap * s.g;
   long long chunks = (kColumnWgs + s.n_inst * columns - 1) / (s.n_inst * columns);

@@ -10,7 +10,8 @@ constexpr int kMoveThreads = 256;
 constexpr int kMoveLoads = 8;        // 16-byte pieces that a thread holds at a time
 
 // K[i][L - n + r] = k_new[i][r], V the same: a copy of 16-byte pieces, a thread each, whose bound is the memory's rate (chunks of 128
-// instances, 220 MB read and written: 37 us alone, 47 among other calls, which a large copy at 5.2 TB/s would take 42 for).
+// instances, 220 MB read and written: 47 us among other calls, which a large copy at 5.2 TB/s would take 42 for; over and over on the same rows,
+// which the last-level cache then has, 37).
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheRows c, const u32x4* __restrict__ k_new,
                                                                       const u32x4* __restrict__ v_new, const int32_t* __restrict__ n_new,
                                                                       int q_cap, int pieces, u32x4* __restrict__ K, u32x4* __restrict__ V) {
@@ -40,7 +41,7 @@ __device__ __forceinline__ float of_order(unsigned k) { return __uint_as_float((
 // give every row that stays its new place.  A thread has up to 64 rows in registers, four in a row next to its neighbours' four, so that
 // caches of up to 65536 rows (256 threads: 16384) are read once, longer ones in rounds of as many, three times as a rule.
 // Weights move along: a row's new place is never behind its old one, and a round's weights are all read before any is written, so acc_out
-// may be acc.  Bound by the chain of its steps on one CU: 64 caches of 2 to 33 thousand rows 28 us, 256 of 1088 rows 11.5.
+// may be acc.  Bound by the chain of its steps on one CU: 64 caches of 2 to 33 thousand rows 28 us, 256 of 1088 rows 13.5.
 constexpr int kQuads = 16;                                 // quads of rows that a thread has in a round
 constexpr int kFew = 2048;                                 // keys that a wave has in registers
 
