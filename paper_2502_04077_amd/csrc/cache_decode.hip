@@ -381,17 +381,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
       const u32x4* Kt = mine_rows + (it & 1) * 2 * F::TILE;
       const u32x4* Vt = Kt + F::TILE;
       if (it + 1 < mine_n) landed<3 * F::N>(); else landed<F::N>();
-      float4v c = {0.f, 0.f, 0.f, 0.f};                    // rows t0 + 4 kg + r of head `head`
+      // Rows t0 + 4 kg + r of head `head`.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
+      constexpr int SUMS = sizeof(T) == 2 ? 1 : 4;
+      float4v sums[SUMS];
+#pragma unroll
+      for (int x = 0; x < SUMS; ++x) sums[x] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int l = 0; l < F::N; ++l) {
         const u32x4 k = Kt[head * F::PIECES + F::k_place(head, 4 * l + kg)];
         if constexpr (sizeof(T) == 2) {
-          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), c, 0, 0, 0);
+          sums[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), sums[0], 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), c, 0, 0, 0);
+            sums[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), sums[e], 0, 0, 0);
         }
+      }
+      float4v c = sums[0];
+      if constexpr (SUMS == 4) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[r] = (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]);
       }
       if (more) {
         lds_read();
