@@ -32,8 +32,7 @@ def _hide(c, lens, first_p, window, n_first):
     c.upload()
 
 
-# Chunks of more than 256 workgroups of 128 rows of q (n instances of t_cap rows, chunks of q_cap, in `splits` splits of the cache): two
-# buffers of tiles, whatever is behind them.
+# Chunks of more workgroups of 128 rows of q than there are CUs: n instances of t_cap rows, chunks of q_cap.
 def _chunks(g, n=48, tiles=6):
     return dict(n=n, q_cap=(tiles * 128 - 60) // g, t_cap=(tiles * 128 // g + 64) // 64 * 64 + 128)
 
