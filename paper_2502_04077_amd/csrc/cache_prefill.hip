@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
     }
     return;
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;           // a query that sees nothing has a zero output
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;           // a query that sees nothing has a zero output
   if (STAT && hb == 0) {
     float* st = a.stat + ((size_t)inst * a.stat_rows + row) * 2;
     st[0] = m == -INFINITY ? 0.f : m;
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_join_kernel(PrefillArg
   // A lane has the statistics of a split (there are at most 64).
   const float m = lane < a.splits ? a.part_ml[(lane * step + at) * 2] : -INFINITY, l = lane < a.splits ? a.part_ml[(lane * step + at) * 2 + 1] : 0.f;
   const float top = wave_max(m), use = top == -INFINITY ? 0.f : top;
-  const float f = exp2_fast(m - use), sum = wave_sum(f * l), inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float f = exp2_fast(m - use), sum = wave_sum(f * l), inv = sum == 0.f ? 0.f : 1.f / sum;
   float o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;

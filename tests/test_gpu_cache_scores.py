@@ -105,3 +105,33 @@ def test_prefill(shape, size):
         if q_cap < 20 or i == 0:
             assert ((acc[i, :L] - total).abs() <= (2 * L + q_cap * g + 16) * HALF[torch.float32] * total).all(), (i, L)
             assert not acc[i, L:].any()
+
+
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_scores_above_32_bits_make_nan_of_their_head(shape):
+    """The first head's scores pass 32 bits at the newest row: NaN there, in whatever form, and the other heads as without it."""
+    import paper_2502_04077_amd as ap
+    g, d, dt, paged, t_cap, q_cap, window, n_first, lens = SHAPES[shape]
+    c, _ = _inputs(shape, (20, 1), 1)
+    q = torch.randn((c.n, q_cap, g, d), generator=torch.Generator().manual_seed(shape)).to(DT[dt])
+    for i, L in enumerate(lens):
+        if L:
+            c.K[i, L - 1] = 0.0
+            c.K[i, L - 1, 0] = 2.0 ** 20
+    c.upload()
+    big = q.clone()
+    big[:, -1, 0] = 0.0
+    big[:, -1, 0, 0] = 2.0 ** 120
+    ctx, L32, got = c.context(g, ap), torch.tensor(lens, dtype=torch.int32, device="cuda:0"), []
+    for x in (q, big):
+        out, one = torch.full(q.shape, 7.0, dtype=DT[dt], device="cuda:0"), torch.full((c.n, g, d), 7.0, device="cuda:0")
+        ctx.cache_prefill(x.to("cuda:0"), None, c.gK, c.gV, L32, window, n_first, out, None, _ws(ctx, q_cap))
+        ctx.cache_decode(x[:, -1].contiguous().to("cuda:0"), c.gK, c.gV, L32, window, n_first, one, None, _ws(ctx, 0))
+        got.append((out.cpu(), one.cpu()))
+    (out, one), (big_out, big_one) = got
+    assert torch.equal(out[:, :-1], big_out[:, :-1]) and torch.equal(out[:, -1, 1:], big_out[:, -1, 1:]) and torch.equal(one[:, 1:], big_one[:, 1:])
+    for i, L in enumerate(lens):
+        if L:
+            assert big_out[i, -1, 0].isnan().all() and big_one[i, 0].isnan().all(), (i, L)
+        else:
+            assert not big_out[i].any() and not big_one[i].any()
