@@ -323,6 +323,74 @@ int ap_cache_prefill(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_c
 int ap_cache_evict(ap_ctx* ctx, void* K, void* V, const float* acc, const int32_t* len, int32_t budget, int32_t n_first, int32_t n_last,
                    float* acc_out, int32_t* len_out, int32_t* kept, void* stream);
 
+/* Pages that instances share.  The calls above take a block table as it is; these give its pages out.  A page of a pool of n_pages pages holds
+ * b rows of K and of V.  An entry of the table outside [0, n_pages), as -1, names no page.
+ *   K,V    pools, device [n_pages][b][d] kv dtype
+ *   table  device int32 [n_inst][nb_cap], the caller's; ap_set_block_table(ctx, table, n_pages) has the other calls read it.  Written by these
+ *          calls alone, or counted again (ap_pages_count)
+ *   state  device int32, ap_pages_state_bytes: word p < n_pages is how often the table names page p, and p is free where that is 0; the
+ *          words behind are the library's.  Written by ap_pages_count first.  Where it does not belong to the table what these calls do is
+ *          unspecified, but they stay inside the pool
+ *   info   device int32 [2]: free pages after the call; and of resize and fork how many pages were lacking.  With one lacking nothing at all
+ *          is changed
+ *   ws     device scratch of ap_pages_workspace_bytes; its contents carry nothing between calls, and calls that share one are issued in
+ *          stream order on one stream
+ * Pages are given out the lowest free one first, to the needs in the order of instances and of their blocks; a page that a call itself gives
+ * up is free from the next call on.  All of it goes by device memory only: a captured call follows lengths and tables that change between
+ * replays.  1 <= n_pages <= 2^30; the size queries are 0 for arguments that no call would accept. */
+size_t ap_pages_state_bytes(const ap_ctx* ctx, int32_t n_pages);
+size_t ap_pages_workspace_bytes(const ap_ctx* ctx, int32_t n_pages);
+
+/* Makes `state` what belongs to the table: in the beginning (of a table of -1 entries, or of any other), or after the caller has changed it. */
+int ap_pages_count(ap_ctx* ctx, const int32_t* table, int32_t n_pages, int32_t* state, void* stream);
+
+/* Brings the tables in line with lengths: blocks behind an instance's rows give their pages up, blocks of its rows that have no page get one, and
+ * those of the rows that are about to be written, [len - n_new, len), that share theirs get one of their own, with the rows in front of
+ * len - n_new copied.  To be called before the rows are appended; after rows were taken back, or evicted; with len 0, for instances that end.
+ *   len    device int32 [n_inst]: as in ap_cache_append, the new rows included; clamped into [0, t_cap]
+ *   n_new  device int32 [n_inst], clamped into [0, q_cap]; NULL: q_cap for all.  q_cap >= 0 (0: no rows are going to be written)
+ * Rows of a fresh page that are not copied are left as they are. */
+int ap_pages_resize(ap_ctx* ctx, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state, const int32_t* len, const int32_t* n_new,
+                    int32_t q_cap, int32_t* info, void* ws, void* stream);
+
+/* Every instance j goes on from instance parent[j], with its rows: one that becomes several samples, beams that are chosen and left (parent[j] == j:
+ * it stays as it is, pages for rows to come included; outside [0, n_inst): it ends).  Full pages are shared.  A last page that is not full is
+ * copied, the rows in use alone, but for one: of a parent that does not go on itself, the lowest instance that goes on from it takes it over.
+ *   parent   device int32 [n_inst]
+ *   len_out  device int32 [n_inst], may be len: the lengths from now on (len where pages were lacking) */
+int ap_pages_fork(ap_ctx* ctx, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state, const int32_t* parent, const int32_t* len,
+                  int32_t* len_out, int32_t* info, void* ws, void* stream);
+
+/* Moves pages so that the N in use are pages 0 .. N - 1: the x-th of those behind goes to the x-th free one in front.  Tables and state follow.
+ *   info  free pages, and how many were moved */
+int ap_pages_compact(ap_ctx* ctx, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state, int32_t* info, void* ws, void* stream);
+
+/* Copies pages of a pool to another one (or to other pages of the same): page dst[x] becomes what page src[x] is, x < n.  Entries outside their
+ * pool are left out.  No page may be written twice, or be written and read, by one call; what it holds then is unspecified.
+ *   K_src,V_src,K_dst,V_dst  [n_src] and [n_dst] pages: device memory, or pinned (mapped) host memory, as where a sequence has to wait
+ *                            outside the device.  Pageable host memory is refused with AP_ERR_ARG
+ *   src,dst                  device int32 [n], or NULL: 0, 1, 2, ... */
+int ap_pages_copy(ap_ctx* ctx, const void* K_src, const void* V_src, int32_t n_src, const int32_t* src, void* K_dst, void* V_dst, int32_t n_dst,
+                  const int32_t* dst, int32_t n, void* stream);
+
+/* Attention of instances whose first rows are the same (samples of one prompt, beams, sequences behind one system prompt): the rows in common
+ * are read once for all of a group, the others as in ap_cache_decode and ap_cache_prefill, whose other arguments and results these share (but for
+ * the weights: rows in common are no instance's own).  The rows in common are the same pages (ap_pages_fork) or hold the same values in every
+ * member's cache; which member's are read is not said.
+ *   group   device int32 [n_inst]: instances with the same number form a group; a negative one stands alone
+ *   shared  device int32 [n_inst]: first rows that the instance has in common with its group; the group's are the fewest of its members'.
+ *           A call counts no more of them than the group's lowest instance has rows
+ *   plan    device, ap_cache_share_bytes: what ap_cache_share makes of both.  It stays valid as long as they do, however the lengths grow
+ *   ws      device scratch of ap_cache_shared_workspace_bytes (q_cap = 0: decode only), else as `ws` above */
+size_t ap_cache_share_bytes(const ap_ctx* ctx);
+int ap_cache_share(ap_ctx* ctx, const int32_t* group, const int32_t* shared, void* plan, void* stream);
+size_t ap_cache_shared_workspace_bytes(const ap_ctx* ctx, int32_t q_cap);
+int ap_cache_decode_shared(ap_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* len, const void* plan, int32_t window,
+                           int32_t n_first, float* out, void* ws, void* stream);
+/* Chunks of few tokens (g q_cap <= 64) go through the groups; larger ones read every instance's own rows, which costs no more. */
+int ap_cache_prefill_shared(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
+                            const void* plan, int32_t window, int32_t n_first, void* out, void* ws, void* stream);
+
 /* Measurement aids (no part of Algorithm 1): a streaming read of `bytes` bytes (multiple of 16) of
  * device memory with 16-byte non-temporal loads per lane, and a plain copy.  They give the read bandwidth the
  * machine actually reaches, quoted beside the published peak, and a kernel of known traffic against

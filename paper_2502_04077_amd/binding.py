@@ -24,7 +24,9 @@ EXPORTS = [
     "ap_create", "ap_destroy", "ap_workspace_bytes", "ap_hist_slots", "ap_nb_cap", "ap_set_weights", "ap_score_offset", "ap_set_block_table",
     "ap_predict", "ap_predict_incremental", "ap_select_topk", "ap_refresh_selection", "ap_sparse_decode", "ap_sparse_decode_noalloc", "ap_calibrate", "ap_update_history", "ap_step",
     "ap_prefetch_state_bytes", "ap_prefetch_blocks", "ap_append_kv", "ap_offload_begin", "ap_offload_step",
-    "ap_cache_workspace_bytes", "ap_cache_append", "ap_cache_decode", "ap_cache_prefill", "ap_cache_evict", "ap_stream_read", "ap_stream_copy", "ap_strerror",
+    "ap_cache_workspace_bytes", "ap_cache_append", "ap_cache_decode", "ap_cache_prefill", "ap_cache_evict",
+    "ap_pages_state_bytes", "ap_pages_workspace_bytes", "ap_pages_count", "ap_pages_resize", "ap_pages_fork", "ap_pages_compact", "ap_pages_copy",
+    "ap_cache_share_bytes", "ap_cache_share", "ap_cache_shared_workspace_bytes", "ap_cache_decode_shared", "ap_cache_prefill_shared", "ap_stream_read", "ap_stream_copy", "ap_strerror",
 ]
 
 
@@ -88,13 +90,30 @@ def load_library() -> C.CDLL:
     lib.ap_cache_decode.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.ap_cache_prefill.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.ap_cache_evict.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.ap_pages_state_bytes.argtypes = [vp, i32]
+    lib.ap_pages_state_bytes.restype = sz
+    lib.ap_pages_workspace_bytes.argtypes = [vp, i32]
+    lib.ap_pages_workspace_bytes.restype = sz
+    lib.ap_pages_count.argtypes = [vp, vp, i32, vp, vp]
+    lib.ap_pages_resize.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp]
+    lib.ap_pages_fork.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.ap_pages_compact.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.ap_pages_copy.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, vp, i32, vp]
+    lib.ap_cache_share_bytes.argtypes = [vp]
+    lib.ap_cache_share_bytes.restype = sz
+    lib.ap_cache_share.argtypes = [vp, vp, vp, vp, vp]
+    lib.ap_cache_shared_workspace_bytes.argtypes = [vp, i32]
+    lib.ap_cache_shared_workspace_bytes.restype = sz
+    lib.ap_cache_decode_shared.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.ap_cache_prefill_shared.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp]
     lib.ap_stream_read.argtypes = [vp, sz, vp, i32, vp]
     lib.ap_stream_copy.argtypes = [vp, sz, vp, i32, vp]
     lib.ap_strerror.argtypes = [C.c_int]
     lib.ap_strerror.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("ap_workspace_bytes", "ap_prefetch_state_bytes", "ap_hist_slots", "ap_nb_cap", "ap_strerror",
-                        "ap_score_offset", "ap_cache_workspace_bytes"):
+                        "ap_score_offset", "ap_cache_workspace_bytes", "ap_pages_state_bytes", "ap_pages_workspace_bytes", "ap_cache_share_bytes",
+                        "ap_cache_shared_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -153,6 +172,8 @@ class Context:
         self._dtype = torch.bfloat16 if self.cfg.kv_dtype == AP_BF16 else torch.float32
         self._kv_numel, self._kv_unit = n_inst * t_cap * head_dim, t_cap * head_dim      # of K; of a cache, or a page
         self._decode_ws = [self.cache_workspace_bytes(0, weights) for weights in (False, True)]
+        self._shared_ws = (self.cache_share_bytes(), self.cache_shared_workspace_bytes(0))
+        self._pages = (0, 0, 0)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -273,10 +294,14 @@ class Context:
         return t.data_ptr()
 
     @staticmethod
+    def _buffer(name, t, need, dev) -> int:
+        if t.get_device() != dev or not t.is_contiguous() or t.numel() * t.element_size() < need:
+            raise ValueError(f"{name}: expected {need} bytes on device {dev}, contiguous")
+        return t.data_ptr()
+
+    @staticmethod
     def _cache_ws(ws, need, dev) -> int:
-        if ws.get_device() != dev or not ws.is_contiguous() or ws.numel() * ws.element_size() < need:
-            raise ValueError(f"ws: expected {need} bytes on device {dev}, contiguous")
-        return ws.data_ptr()
+        return Context._buffer("ws", ws, need, dev)
 
     @staticmethod
     def _cache_call(dev, call, *args) -> None:
@@ -329,6 +354,116 @@ class Context:
                          arg("acc_out", acc_out, torch.float32, rows, dev),
                          arg("len_out", len_out, torch.int32, (self._n,), dev),
                          arg("kept", kept, torch.int32, (self._n, budget), dev))
+
+    # -- pages that instances share --------------------------------------------------------------
+    def pages_state_bytes(self, n_pages: int) -> int:
+        return int(self._lib.ap_pages_state_bytes(self._h, n_pages))
+
+    def pages_workspace_bytes(self, n_pages: int) -> int:
+        return int(self._lib.ap_pages_workspace_bytes(self._h, n_pages))
+
+    def _pool(self, K, V):
+        """Checks the pools K and V [n_pages][b][d]; the device they lie on, and their pages."""
+        dev = K.get_device()
+        if K.dim() != 3 or K.shape[1:] != (self.cfg.block, self._d) or K.shape != V.shape or K.dtype is not self._dtype or V.dtype is not self._dtype:
+            raise ValueError(f"K and V: two pools [n_pages][{self.cfg.block}][{self._d}] of one shape, in the context's dtype")
+        if dev < 0 or V.get_device() != dev or not (K.is_contiguous() and V.is_contiguous()):
+            raise ValueError("K and V: expected contiguous tensors on one device")
+        return dev, K.shape[0]
+
+    def _pages_state(self, table, state, n_pages, dev):
+        nb, key = self._t_cap // self.cfg.block, n_pages
+        if self._pages[0] != key:                             # (the sizes of a pool, asked once)
+            self._pages = (key, self.pages_state_bytes(n_pages) // 4, self.pages_workspace_bytes(n_pages))
+        return self._cache_arg("table", table, torch.int32, (self._n, nb), dev), self._cache_arg("state", state, torch.int32, (self._pages[1],), dev)
+
+    def pages_count(self, table, n_pages, state) -> None:
+        """table: int32 [n_inst][nb_cap]; state: int32 of pages_state_bytes(n_pages)."""
+        dev = table.get_device()
+        if dev < 0:
+            raise ValueError("table: expected a device tensor")
+        table, state = self._pages_state(table, state, n_pages, dev)
+        self._cache_call(dev, self._lib.ap_pages_count, self._h, table, n_pages, state)
+
+    def pages_resize(self, K, V, table, state, length, n_new, q_cap, info, ws) -> None:
+        """K, V: [n_pages][b][d]; length: int32 [n_inst], the new rows included; n_new: int32 [n_inst] or None (q_cap each); info: int32 [2]."""
+        (dev, n_pages), arg = self._pool(K, V), self._cache_arg
+        table, state = self._pages_state(table, state, n_pages, dev)
+        self._cache_call(dev, self._lib.ap_pages_resize, self._h, K.data_ptr(), V.data_ptr(), table, n_pages, state,
+                         arg("length", length, torch.int32, (self._n,), dev),
+                         None if n_new is None else arg("n_new", n_new, torch.int32, (self._n,), dev), q_cap,
+                         arg("info", info, torch.int32, (2,), dev), self._cache_ws(ws, self._pages[2], dev))
+
+    def pages_fork(self, K, V, table, state, parent, length, len_out, info, ws) -> None:
+        """parent: int32 [n_inst]; len_out: int32 [n_inst], may be length."""
+        (dev, n_pages), arg = self._pool(K, V), self._cache_arg
+        table, state = self._pages_state(table, state, n_pages, dev)
+        self._cache_call(dev, self._lib.ap_pages_fork, self._h, K.data_ptr(), V.data_ptr(), table, n_pages, state,
+                         arg("parent", parent, torch.int32, (self._n,), dev), arg("length", length, torch.int32, (self._n,), dev),
+                         arg("len_out", len_out, torch.int32, (self._n,), dev), arg("info", info, torch.int32, (2,), dev),
+                         self._cache_ws(ws, self._pages[2], dev))
+
+    def pages_compact(self, K, V, table, state, info, ws) -> None:
+        (dev, n_pages), arg = self._pool(K, V), self._cache_arg
+        table, state = self._pages_state(table, state, n_pages, dev)
+        self._cache_call(dev, self._lib.ap_pages_compact, self._h, K.data_ptr(), V.data_ptr(), table, n_pages, state,
+                         arg("info", info, torch.int32, (2,), dev), self._cache_ws(ws, self._pages[2], dev))
+
+    def pages_copy(self, K_src, V_src, src, K_dst, V_dst, dst, n=None) -> None:
+        """Pools [..][b][d], on the device or in pinned host memory; src, dst: int32 [n] or None (0, 1, 2, ...; with both None, n says how many)."""
+        dev = max(t.get_device() for t in (K_src, K_dst, *(x for x in (src, dst) if x is not None)))
+        for a, b in ((K_src, V_src), (K_dst, V_dst)):
+            if a.dim() != 3 or a.shape[1:] != (self.cfg.block, self._d) or a.shape != b.shape or a.dtype is not self._dtype or b.dtype is not self._dtype:
+                raise ValueError(f"K and V: pools [..][{self.cfg.block}][{self._d}] in the context's dtype")
+            for t in (a, b):
+                if not t.is_contiguous() or not (t.get_device() == dev if t.is_cuda else t.is_pinned()):
+                    raise ValueError("pools: expected contiguous tensors on one device, or in pinned host memory")
+        if dev < 0:
+            raise ValueError("pools: one of them at least lies on a device")
+        counts = {x.numel() for x in (src, dst) if x is not None} | ({n} if n is not None else set())
+        if len(counts) != 1:
+            raise ValueError("src and dst: as many entries each; n where both are None")
+        n, = counts
+        if n < 0 or any(x is None and n > t.shape[0] for x, t in ((src, K_src), (dst, K_dst))):
+            raise ValueError(f"{n} pages are more than a pool has")
+        list_of = lambda name, x: None if x is None else self._cache_arg(name, x, torch.int32, (n,), dev)  # noqa: E731
+        self._cache_call(dev, self._lib.ap_pages_copy, self._h, K_src.data_ptr(), V_src.data_ptr(), K_src.shape[0], list_of("src", src),
+                         K_dst.data_ptr(), V_dst.data_ptr(), K_dst.shape[0], list_of("dst", dst), n)
+
+    # -- attention of instances whose first rows are the same ------------------------------------
+    def cache_share_bytes(self) -> int:
+        """Bytes of `plan`."""
+        return int(self._lib.ap_cache_share_bytes(self._h))
+
+    def cache_share(self, group, shared, plan) -> None:
+        """group, shared: int32 [n_inst]; plan: a device buffer of cache_share_bytes()."""
+        dev, arg = group.get_device(), self._cache_arg
+        if dev < 0:
+            raise ValueError("group: expected a device tensor")
+        self._cache_call(dev, self._lib.ap_cache_share, self._h, arg("group", group, torch.int32, (self._n,), dev),
+                         arg("shared", shared, torch.int32, (self._n,), dev), self._buffer("plan", plan, self._shared_ws[0], dev))
+
+    def cache_shared_workspace_bytes(self, q_cap: int = 0) -> int:
+        """Bytes of `ws` for cache_decode_shared and cache_prefill_shared of up to q_cap tokens."""
+        return int(self._lib.ap_cache_shared_workspace_bytes(self._h, q_cap))
+
+    def cache_decode_shared(self, q, K, V, length, plan, window, n_first, out, ws) -> None:
+        """As cache_decode; plan: of cache_share."""
+        dev, arg = self._cache_kv(K, V), self._cache_arg
+        shape = (self._n, self._g, self._d)
+        self._cache_call(dev, self._lib.ap_cache_decode_shared, self._h, arg("q", q, self._dtype, shape, dev), K.data_ptr(), V.data_ptr(),
+                         arg("length", length, torch.int32, (self._n,), dev), self._buffer("plan", plan, self._shared_ws[0], dev), window, n_first,
+                         arg("out", out, torch.float32, shape, dev), self._cache_ws(ws, self._shared_ws[1], dev))
+
+    def cache_prefill_shared(self, q, n_q, K, V, length, plan, window, n_first, out, ws) -> None:
+        """As cache_prefill; plan: of cache_share."""
+        dev, arg = self._cache_kv(K, V), self._cache_arg
+        q_cap = q.shape[1] if q.dim() == 4 else 0
+        shape = (self._n, q_cap, self._g, self._d)
+        self._cache_call(dev, self._lib.ap_cache_prefill_shared, self._h, arg("q", q, self._dtype, shape, dev),
+                         None if n_q is None else arg("n_q", n_q, torch.int32, (self._n,), dev), q_cap, K.data_ptr(), V.data_ptr(),
+                         arg("length", length, torch.int32, (self._n,), dev), self._buffer("plan", plan, self._shared_ws[0], dev), window, n_first,
+                         arg("out", out, self._dtype, shape, dev), self._cache_ws(ws, self.cache_shared_workspace_bytes(q_cap), dev))
 
     def update_history(self, hist, n_pushed, row) -> None:
         _check(self._lib.ap_update_history(self._h, _ptr(hist), n_pushed, _ptr(row), _stream()))

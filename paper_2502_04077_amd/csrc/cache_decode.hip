@@ -16,7 +16,7 @@
 // d = 64 49 us, 4.8; with rows through registers and pages looked up by vector loads, which wait for
 // the rows in flight, 246 and 639.  Where more instances than workgroups are all short, every wave takes whole ones: 2048 of 8 to 419 rows
 // (g = 1, 111 MB) 38 us, by shares of a workgroup 61; of 16 to 56 (g = 2, d = 64) 18 and 40.
-#include "cache_body.h"
+#include "share_body.h"
 
 namespace ap {
 namespace {
@@ -41,6 +41,29 @@ __device__ __forceinline__ Seen seen_of(int len, int t_cap, int window, int n_fi
   s.gs = (s.f + kGroup - 1) / kGroup;
   s.gb = s.lo / kGroup > s.gs ? s.lo / kGroup : s.gs;
   s.n = s.L == 0 ? 0 : s.gs + (s.L - 1) / kGroup - s.gb + 1;
+  return s;
+}
+
+// The same without the rows [0, s0), which were read as the beginning of a group: [s0, f) and [lo, L), s0 <= f <= lo or f = 0.
+struct SeenBehind {
+  int L, lo, f, s0, ga, gs, gb, n;
+  __device__ __forceinline__ int group(int u) const { return u < gs ? ga + u : gb + (u - gs); }
+  __device__ __forceinline__ bool row(int j) const { return j < L && j >= s0 && (j >= lo || j < f); }
+};
+__device__ __forceinline__ SeenBehind seen_behind(int len, int s0, int t_cap, int window, int n_first) {
+  SeenBehind s;
+  s.L = clamped(len, 0, t_cap);
+  s.s0 = s0;
+  s.lo = window > 0 && s.L > window ? s.L - window : 0;
+  s.f = n_first < s.lo ? n_first : s.lo;
+  if (s.lo < s0) s.lo = s0;
+  if (s.f <= s0) s.f = 0;
+  s.ga = s0 / kGroup;
+  const int end = (s.f + kGroup - 1) / kGroup;             // behind the first rows' groups
+  s.gs = s.f > 0 ? end - s.ga : 0;
+  s.gb = s.lo / kGroup;
+  if (s.gs > 0 && s.gb < end) s.gb = end;
+  s.n = s.lo < s.L ? s.gs + (s.L - 1) / kGroup - s.gb + 1 : 0;
   return s;
 }
 
@@ -76,16 +99,25 @@ template <typename T, int D, int G> struct Form {
 
 // Where a group of 16 rows lies: its first and its second eight, in rows of K and V; and whether all 16 are seen.  Wave-uniform.
 struct Place { size_t a, b; int t0; bool all; };
-__device__ __forceinline__ Place place_of(const CacheRows& r, int inst, const Seen& s, int u) {
+__device__ __forceinline__ bool all_seen(const Seen& s, int t0) { return t0 + kGroup <= s.L && (t0 >= s.lo || t0 + kGroup <= s.f); }
+__device__ __forceinline__ bool all_seen(const SeenBehind& s, int t0) { return t0 + kGroup <= s.L && (t0 >= s.lo || (t0 >= s.s0 && t0 + kGroup <= s.f)); }
+// A row of the group that is seen.
+__device__ __forceinline__ int one_seen(const Seen& s, int t0) { return t0 < s.f ? t0 : (t0 > s.lo ? t0 : s.lo); }
+__device__ __forceinline__ int one_seen(const SeenBehind& s, int t0) {
+  const int from = t0 < s.f ? s.s0 : s.lo;
+  return t0 > from ? t0 : from;
+}
+template <typename SEEN> __device__ __forceinline__ Place place_of(const CacheRows& r, int inst, const SEEN& s, int u) {
   Place p;
   p.t0 = __builtin_amdgcn_readfirstlane(s.group(u) * kGroup);
   p.a = rows_at(r, inst, p.t0);
   p.b = r.lb == 3 && r.table != nullptr ? rows_at(r, inst, p.t0 + 8) : p.a + 8;
-  p.all = p.t0 + kGroup <= s.L && (p.t0 >= s.lo || p.t0 + kGroup <= s.f);
+  p.all = all_seen(s, p.t0);
   return p;
 }
 // Sends the rows of a group of K (or V) to LDS.
-template <typename F, bool IS_V> __device__ __forceinline__ void send(const void* X, const Place& p, const Seen& s, int lane, unsigned lds) {
+template <typename F, bool IS_V, typename SEEN>
+__device__ __forceinline__ void send(const void* X, const Place& p, const SEEN& s, int lane, unsigned lds) {
   constexpr unsigned row = F::PIECES * 16;
   if (p.all && p.b == p.a + 8) {
     const char* base = static_cast<const char*>(X) + p.a * row;
@@ -96,7 +128,7 @@ template <typename F, bool IS_V> __device__ __forceinline__ void send(const void
     }
   } else {
     // Rows that are not seen are not read: another row of the group, which is, stands in for them.
-    const int other = (p.t0 < s.f ? p.t0 : (p.t0 > s.lo ? p.t0 : s.lo)) - p.t0;
+    const int other = one_seen(s, p.t0) - p.t0;
 #pragma unroll 1
     for (int l = 0; l < F::N; ++l) {
       const int x = l * kWave + lane, r = x / F::PIECES, place = x % F::PIECES;
@@ -138,12 +170,32 @@ __device__ __forceinline__ bool last_of(unsigned long long* word, unsigned long 
   return *s_last != 0;
 }
 
+// An output (of maximum `top` and sum `all`, which `val` has not been divided by), joined with the pieces of the beginning.
+template <int D> __device__ __forceinline__ float joined(const Beginnings& b, const Ahead& at, int h, int e, float top, float all, float val) {
+  float m = top;
+  const size_t first = (size_t)at.row + h;
+#pragma unroll 4
+  for (int p = 0; p < at.parts; ++p) m = fmaxf(m, b.ml[(first + (size_t)kPrefillRows * p) * 2]);
+  const float use = reference(m), f0 = exp2_fast(top - use);
+  all *= f0;
+  val *= f0;
+#pragma unroll 4
+  for (int p = 0; p < at.parts; ++p) {
+    const size_t x = first + (size_t)kPrefillRows * p;
+    const float f = exp2_fast(b.ml[x * 2] - use);
+    all += f * b.ml[x * 2 + 1];
+    val += f * b.o[x * D + e];
+  }
+  return over(val, all);
+}
+
 // Joins `parts` pieces, from that of workgroup w0 on, by one workgroup: maximum and 1 / sum of every head to s_m and s_inv, and, unless
 // inst < 0, the output.  SHARED: the pieces were written by workgroups of the same launch.  s: `bytes` of LDS, the factors of the pieces in
 // front, and behind them pieces, of which as many as there is room for are on their way at a time: one workgroup's loads are what this
 // costs (64 pieces of g = 4, d = 128, 16 in registers at a time: 12 us).
-template <int G, int D, bool SHARED>
-__device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w0, int parts, float* s, int bytes, float* s_m, float* s_inv) {
+template <int G, int D, bool SHARED, typename ARGS>
+__device__ __forceinline__ void join_pieces(const ARGS& a, int inst, int w0, int parts, float* s, int bytes, float* s_m, float* s_inv) {
+  constexpr bool BEHIND = std::is_same<ARGS, SharedDecodeArgs>::value;
   constexpr int PP = G * D / 4, R = (G * D + kThreads - 1) / kThreads;              // 16-byte pieces of a part, outputs of a thread
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   auto read = [](const float* p) { return SHARED ? ld_shared_out(p) : *p; };
@@ -191,8 +243,8 @@ __device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w
     }
     all = wave_sum(all);
     if (lane == 0) {
-      s_m[h] = use;
-      s_inv[h] = over(1.f, all);
+      s_m[h] = BEHIND ? top : use;
+      s_inv[h] = BEHIND ? all : over(1.f, all);
     }
   }
   if (inst < 0) {
@@ -221,13 +273,24 @@ __device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int x = r * kThreads + tid;
-    if (x < G * D) a.out[(size_t)inst * G * D + x] = val[r] * s_inv[x / D];
+    if constexpr (BEHIND) {
+      const Ahead at = ahead_of(a.b, inst, 0);
+      if (x < G * D) a.out[(size_t)inst * G * D + x] = joined<D>(a.b, at, x / D, x % D, s_m[x / D], s_inv[x / D], val[r]);
+    } else {
+      if (x < G * D) a.out[(size_t)inst * G * D + x] = val[r] * s_inv[x / D];
+    }
   }
 }
 
-template <typename T, int D, int G, bool ACC>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(DecodeArgs a) {
+// ARGS: SharedDecodeArgs where beginnings were read for groups of instances: their rows are not seen here, and their pieces are joined to the outputs.
+template <typename T, int D, int G, bool ACC, typename ARGS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(ARGS a) {
+  constexpr bool BEHIND = std::is_same<ARGS, SharedDecodeArgs>::value;
   using F = Form<T, D, G>;
+  auto see = [&](int i) {
+    if constexpr (BEHIND) return seen_behind(a.r.len[i], a.b.start[i], a.r.t_cap, a.window, a.n_first);
+    else return seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first);
+  };
   extern __shared__ __attribute__((aligned(16))) u32x4 s_rows[];          // [wave]: [buffer][K, V][TILE], queries; at the end outputs, [G][D]
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
@@ -245,7 +308,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   int longest = 0;
 #pragma unroll 4
   for (int i = i_begin; i < i_end; ++i) {
-    const int n = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+    const int n = see(i).n;
     mine += (unsigned)n;
     longest = n > longest ? n : longest;
   }
@@ -276,14 +339,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const unsigned long long begin = (unsigned long long)blockIdx.x * per;
   const unsigned long long end = begin + per < groups ? begin + per : groups;
   // Empty instances have no share; their outputs are zero.
-  for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS)
-    if (a.r.len[i] <= 0)
+  for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS) {
+    if constexpr (BEHIND) {                                // (what their beginning gives)
+      if (see(i).n > 0) continue;
+      const Ahead at = ahead_of(a.b, i, 0);
+      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = joined<D>(a.b, at, x / D, x % D, -INFINITY, 0.f, 0.f);
+    } else if (a.r.len[i] <= 0) {
       for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
+    }
+  }
   if (ACC && blockIdx.x == 0) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
       a.before[i] = at;
-      at += (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+      at += (unsigned)see(i).n;
     }
     if (tid == kThreads - 1) a.before[a.r.n_inst] = alone ? kAlone : groups;
   }
@@ -292,7 +361,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   if (alone ? ahead < end && begin < ahead + mine : ahead <= begin && begin < ahead + mine) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
-      const unsigned n = (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
+      const unsigned n = (unsigned)see(i).n;
       if (alone) {
         if (n > 0 && at >= begin && at < end) {
           atomicMin(&s_first[(int)((at - begin) / share)], i);
@@ -321,7 +390,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const unsigned ring = lds_address(mine_rows);
   float* s_out = reinterpret_cast<float*>(s_rows);
   for (; alone ? left > 0 && inst < mine_to : left > 0; ++inst, from = 0) {
-    const Seen s = seen_of(a.r.len[inst], a.r.t_cap, a.window, a.n_first);
+    const auto s = see(inst);
     if (s.n <= from) continue;                             // an empty instance
     const int to = alone ? s.n : (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
     if (!alone) left -= (unsigned)(to - from);
@@ -476,14 +545,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         o[h][e] = sum32(o[h][e]);
       }
     }
+    Ahead ahead_here = {0, 0};
+    if constexpr (BEHIND) ahead_here = ahead_of(a.b, inst, 0);
     if (alone) {
 #pragma unroll
       for (int h = 0; h < G; ++h) {
         const float all = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), h));
+        const float top = BEHIND ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), h)) : 0.f;
         if (lane < F::PIECES) {
           float* to_out = a.out + ((size_t)inst * G + h) * D + lane * F::E;
 #pragma unroll
-          for (int e = 0; e < F::E; ++e) to_out[e] = over(o[h][e], all);
+          for (int e = 0; e < F::E; ++e) {
+            if constexpr (BEHIND) to_out[e] = joined<D>(a.b, ahead_here, h, lane * F::E + e, top, all, o[h][e]);
+            else to_out[e] = over(o[h][e], all);
+          }
         }
       }
       if (ACC && lane < G) {
@@ -515,7 +590,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         all += f * s_ml[w][h][1];
         val += f * s_out[w * F::WAVE * 4 + x];
       }
-      if (whole) a.out[((size_t)inst * G + h) * D + e] = over(val, all);
+      if (whole && BEHIND) {
+        if constexpr (BEHIND) a.out[((size_t)inst * G + h) * D + e] = joined<D>(a.b, ahead_here, h, e, top, all, val);
+      } else if (whole) a.out[((size_t)inst * G + h) * D + e] = over(val, all);
       else st_shared_out<!ACC>(a.part_acc + (slot * G + h) * D + e, val);
       if (e == 0 && (ACC || !whole)) {
         float* ml = whole ? a.whole + ((size_t)inst * G + h) * 2 : a.part_ml + (slot * G + h) * 2;
@@ -568,25 +645,32 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
 
 template <typename T, int D, int G> hipError_t run(const DecodeArgs& a, hipStream_t st) {
   using F = Form<T, D, G>;
-  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
-  else cache_decode_kernel<T, D, G, false><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
+  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true, DecodeArgs><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
+  else cache_decode_kernel<T, D, G, false, DecodeArgs><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.acc == nullptr) return e;
   const unsigned columns = (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads));
   cache_join_kernel<G, D><<<dim3(1 + columns, a.r.n_inst), kThreads, join_bytes(G, D), st>>>(a, F::WGS);
   return hipGetLastError();
 }
-template <typename T, int D> hipError_t run_g(int g, const DecodeArgs& a, hipStream_t st) {
+template <typename T, int D, int G> hipError_t run(const SharedDecodeArgs& a, hipStream_t st) {
+  using F = Form<T, D, G>;
+  cache_decode_kernel<T, D, G, false, SharedDecodeArgs><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
+  return hipGetLastError();
+}
+template <typename T, int D, typename ARGS> hipError_t run_g(int g, const ARGS& a, hipStream_t st) {
   return g == 1 ? run<T, D, 1>(a, st) : g == 2 ? run<T, D, 2>(a, st) : g == 4 ? run<T, D, 4>(a, st) : run<T, D, 8>(a, st);
 }
 
 }  // namespace
 
-hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& args, hipStream_t st) {
-  DecodeArgs a = args;
+template <typename ARGS> static hipError_t launch(const Shape& s, const ARGS& args, hipStream_t st) {
+  ARGS a = args;
   a.nonce = new_nonce(kTicketBits);
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s.g, a, st) : run_g<bf16_t, 64>(s.g, a, st);
   return s.d == 128 ? run_g<float, 128>(s.g, a, st) : run_g<float, 64>(s.g, a, st);
 }
+hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& args, hipStream_t st) { return launch(s, args, st); }
+hipError_t launch_cache_decode_shared(const Shape& s, const SharedDecodeArgs& args, hipStream_t st) { return launch(s, args, st); }
 
 }  // namespace ap

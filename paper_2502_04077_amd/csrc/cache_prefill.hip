@@ -15,39 +15,15 @@
 // add up to nearly all of the time -, and the clock, which falls to 1.8 GHz under it.  Tried and no faster: the next tile's scores beside
 // this one's exponentials, three waves a SIMD with tiles of 32 rows, 256 rows a workgroup, a higher priority for the matrix phases.
 // In fp32 (4000 tokens, 8 instances) 1125 us, 117 TFLOP/s, where a large library product reaches 154.
-#include "cache_body.h"
+#include "cache_tiles.h"
+#include "share_body.h"
 
 namespace ap {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
 // Tiles of a split.  (g = 4, d = 128: a chunk of 101 behind 416 rows, 8 instances, by splits of 1, 2, 4 tiles 15.6, 15.6, 16.9 us; 4 tokens
 // behind 2000 rows 12.1, 11.8, 13.5; 300 of 1000 rows 25.5, 25.5, 23.0.)
 constexpr int kLeastTiles = 2;
-typedef float float16v __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef short short4v __attribute__((ext_vector_type(4)));
-
-template <typename T, int D> struct Form {
-  static constexpr int E = 16 / (int)sizeof(T);            // elements of a 16-byte piece
-  static constexpr int PIECES = D / E;                     // pieces of a row
-  static constexpr int TT = sizeof(T) == 2 ? 64 : 32;      // cache rows of a tile
-  static constexpr int TB = TT / 32;                       // blocks of 32 of them
-  static constexpr int KS = PIECES / 2;                    // pieces a lane contributes to a product over d
-  static constexpr int DB = D / 32;                        // blocks of 32 output dims
-  static constexpr int LOADS = TT * PIECES / kThreads;     // pieces a thread fetches of a tile of K, or V
-  static constexpr int TILE = TT * PIECES;                 // pieces of a tile
-  static constexpr int RPL = 64 / PIECES;                  // rows that a wave fetches with a load
-  static constexpr int RW = TT / kWaves;                   // rows of a tile that a wave fetches
-  static_assert(RPL * LOADS == RW, "a wave's rows");
-  // Piece p of row r lies at place p ^ swizzle(r) of the row, so that the lanes of one LDS cycle use different banks: K is read a row
-  // per lane, V (16 bits) in blocks of four rows by four pieces, half a wave at a time.
-  __device__ static __forceinline__ int k_place(int r, int p) { return p ^ (r & (PIECES - 1)); }
-  __device__ static __forceinline__ int v_place(int r, int p) {
-    return sizeof(T) == 2 ? p ^ (PIECES == 16 ? 4 * (r & 3) : 4 * ((r >> 1) & 1)) : p;
-  }
-};
-
 // What the queries of a tile see of an instance.
 struct Span {
   int L, n, base;        // length, queries, position of query 0 (may be negative)
@@ -57,7 +33,7 @@ struct Span {
   __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
 };
 template <int TT, int G>
-__device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, int q_cap, int window, int n_first, int inst, int row0, int rows) {
+__device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, int q_cap, int window, int n_first, int inst, int row0, int rows, int s0) {
   Span s;
   s.L = clamped(r.len[inst], 0, r.t_cap);
   s.n = n_q == nullptr ? q_cap : clamped(n_q[inst], 0, q_cap);
@@ -68,104 +44,17 @@ __device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, 
   if (last <= row0) s.p1 = -1;
   s.lo0 = window > 0 && s.p0 >= window ? s.p0 - window + 1 : 0;
   s.f = n_first < s.lo0 ? n_first : s.lo0;
+  if (s0 > 0) {                                            // rows in front of s0 are not seen
+    if (s.f <= s0) s.f = 0;
+    if (s.lo0 < s0) s.lo0 = s0;
+    if (s.p1 < s.lo0) s.p1 = s.f - 1;
+  }
   if (s.p1 < 0) { s.tiles = s.ts = s.tb = 0; return s; }
   s.ts = (s.f + TT - 1) / TT;
   s.tb = s.lo0 / TT > s.ts ? s.lo0 / TT : s.ts;
   s.tiles = s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
   return s;
 }
-
-// A wave fetches RW consecutive rows of a tile, which lie in one page, or in two of eight rows.  Rows that no query of the tile sees are not
-// read: row `alt`, which is seen, stands in for them, and may be any row of the cache.  Wave-uniform.
-struct Run {
-  const char *k, *v;                                       // row 0 of the run, as if all of it lay together
-  long long second;                                        // and what to add for its second eight rows, in bytes
-  bool all;
-  int j0, alt;
-};
-// The instance's part of the table, looked up through the scalar cache.
-struct Pages {
-  const __attribute__((address_space(4))) int32_t* table;  // of this instance, or null
-  size_t row0;                                             // contiguous: the instance's first row
-  int lb, nb_cap, n_phys;
-  __device__ __forceinline__ size_t at(int j) const {      // of row j, a multiple of 8
-    if (table == nullptr) return row0 + j;
-    const int block = j >> lb;
-    const int page = clamped(table[block < nb_cap ? block : nb_cap - 1], 0, n_phys - 1);
-    return ((size_t)page << lb) + (j & ((1 << lb) - 1));
-  }
-};
-__device__ __forceinline__ Pages pages_of(const CacheRows& r, int inst) {
-  Pages p;
-  p.table = r.table == nullptr ? nullptr : (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(r.table + (size_t)inst * r.nb_cap);
-  p.row0 = (size_t)inst * r.t_cap;
-  p.lb = r.lb; p.nb_cap = r.nb_cap; p.n_phys = r.n_phys;
-  return p;
-}
-template <typename F> __device__ __forceinline__ Run run_of(const PrefillArgs& a, const Pages& pages, const Span& s, int t0, int wave) {
-  constexpr size_t bytes = F::PIECES * 16;
-  Run x;
-  x.j0 = t0 + wave * F::RW;
-  x.all = x.j0 + F::RW - 1 <= s.p1 && (x.j0 >= s.lo0 || x.j0 + F::RW <= s.f);
-  int alt = x.j0;                                          // a row of the run that is seen, or one of another run
-  if (x.j0 >= s.f) alt = x.j0 > s.lo0 ? x.j0 : s.lo0;
-  if (alt > s.p1) alt = s.p1;
-  x.alt = alt;
-  const size_t at = pages.at(x.j0);
-  x.k = static_cast<const char*>(a.K) + at * bytes;
-  x.v = static_cast<const char*>(a.V) + at * bytes;
-  x.second = F::RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(x.j0 + 8) - at) - 8) * (long long)bytes : 0;
-  return x;
-}
-// Sends a tile of K (or V) to LDS: the lane chooses the piece, so that it lies where the swizzle says.
-template <typename F, bool IS_V>
-__device__ __forceinline__ void send_tile(const PrefillArgs& a, int inst, const Run& run, const Span& s, int wave, unsigned lds) {
-  constexpr unsigned bytes = F::PIECES * 16;
-  const int lane = threadIdx.x & 63;
-  const unsigned to = lds + wave * F::LOADS * 1024;
-  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };                   // of the run, which begins at a multiple of RW rows
-  auto piece = [&](int l) {
-    const int place = lane % F::PIECES;
-    return IS_V ? F::v_place(row(l), place) : F::k_place(wave * F::RW + row(l), place);
-  };
-  if (run.all) {
-#pragma unroll
-    for (int l = 0; l < F::LOADS; ++l)
-      to_lds<false>((IS_V ? run.v : run.k) + (l >= F::LOADS / 2 ? run.second : 0), row(l) * bytes + piece(l) * 16, to + l * 1024);
-  } else {
-#pragma unroll 1
-    for (int l = 0; l < F::LOADS; ++l) {
-      int j = run.j0 + row(l);
-      if (j > s.p1 || (j >= s.f && j < s.lo0)) j = run.alt;
-      to_lds_from(static_cast<const char*>(IS_V ? a.V : a.K) + row_at(a.r, inst, j) * bytes + piece(l) * 16, to + l * 1024);
-    }
-  }
-}
-
-// (32 rows of X in LDS) . (32 rows held as operands)^T, fp32: one block of scores.
-template <typename T, int D>
-__device__ __forceinline__ float16v product(const u32x4* X, int row0, const u32x4 (&b)[Form<T, D>::KS]) {
-  using F = Form<T, D>;
-  const int lane = threadIdx.x & 63, m = lane & 31, hb = lane >> 5;
-  float16v c;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) c[i] = 0.f;
-#pragma unroll
-  for (int k = 0; k < F::KS; ++k) {
-    const u32x4 x = X[(row0 + m) * F::PIECES + F::k_place(row0 + m, 2 * k + hb)];
-    if constexpr (sizeof(T) == 2) {
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, b[k]), c, 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(b[k][e]), c, 0, 0, 0);
-    }
-  }
-  return c;
-}
-
-// Which of 16 registers' rows: register i of a block holds row 8 (i / 4) + 4 hb + i % 4.
-__device__ __forceinline__ int reg_row(int i, int hb) { return 8 * (i >> 2) + 4 * hb + (i & 3); }
 
 // Workgroup b of tiles * n_inst: which instance and which tile.  Consecutive workgroups go to the 8 XCDs in turn, so instances are dealt
 // eight at a time, one an XCD, whose L2 then serves one instance's K and V; the fewer than eight that are left share the XCDs.
@@ -180,14 +69,19 @@ __device__ __forceinline__ Work work_of(unsigned b, int tiles, int n_inst) {
   return {(int)(whole + x % rest), (int)(x / rest)};
 }
 
-template <typename T, int D, int G, bool STAT>
-__global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
+// ARGS: SharedPrefillArgs where beginnings were read for groups of instances: their rows are not seen here, and the sums of the others are left
+// to be joined with theirs.
+template <typename T, int D, int G, bool STAT, typename ARGS>
+__global__ __launch_bounds__(kThreads) void cache_prefill_kernel(ARGS a) {
+  constexpr bool BEHIND = std::is_same<ARGS, SharedPrefillArgs>::value;
   using F = Form<T, D>;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
   const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kPrefillRows;            // the longest ones first
-  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kPrefillRows);
+  int s0 = 0;
+  if constexpr (BEHIND) s0 = a.b.start[inst];
+  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kPrefillRows, s0);
   const int rows = s.n * G;                                // of q
   if (row0 >= rows) return;
 
@@ -208,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   const float scale = kLog2E / sqrtf((float)D);
 
   const unsigned buffers = lds_address(s_tiles);
-  const Pages pages = pages_of(a.r, inst);
+  const TablePages pages = pages_of(a.r, inst);
   // Tiles of the cache in splits: this workgroup's.
   const int each = (s.tiles + a.splits - 1) / a.splits > kLeastTiles ? (s.tiles + a.splits - 1) / a.splits : kLeastTiles;
   const int u_begin = a.splits == 1 ? 0 : (int)blockIdx.y * each;
@@ -240,14 +134,16 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
     // Every row of the tile is seen by every query of it, or the scores of those that are not become -inf.
-    const bool all = t0 + F::TT - 1 <= s.p0 && (a.window <= 0 || t0 > s.p1 - a.window || t0 + F::TT <= a.n_first);
+    const bool all = t0 + F::TT - 1 <= s.p0 && (!BEHIND || t0 >= s0) && (a.window <= 0 || t0 > s.p1 - a.window || t0 + F::TT <= a.n_first);
     if (!all) {
 #pragma unroll
       for (int b = 0; b < F::TB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = t0 + 32 * b + reg_row(i, hb);
-          c[b][i] = (j > p) | ((j < lo) & (j >= a.n_first)) ? -INFINITY : c[b][i];
+          bool hidden = (j > p) | ((j < lo) & (j >= a.n_first));
+          if (BEHIND) hidden |= j < s0;
+          c[b][i] = hidden ? -INFINITY : c[b][i];
         }
     }
     float top = c[0][0];
@@ -332,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
 
   sum = sum32(sum);
   if (row >= rows) return;
-  if (a.splits > 1) {                                      // (whatever its share: the join goes by the maximum)
+  if (BEHIND || a.splits > 1) {                            // (whatever its share: the join goes by the maximum)
     const size_t at = ((size_t)blockIdx.y * a.r.n_inst + inst) * a.q_cap * G + row;
     if (hb == 0) {
       a.part_ml[at * 2] = m;
@@ -418,6 +314,52 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_join_kernel(PrefillArg
     float* st = a.stat + ((size_t)inst * a.stat_rows + row) * 2;
     st[0] = use;
     st[1] = inv;
+  }
+}
+
+// The same with the pieces of the beginnings.
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kThreads) void cache_prefill_behind_kernel(SharedPrefillArgs a) {
+  constexpr int E = D / 64;                                // outputs of a lane
+  const int inst = blockIdx.y, lane = threadIdx.x & 63, row = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
+  if (row >= nq * G) return;
+  const size_t at = (size_t)inst * a.q_cap * G + row, step = (size_t)a.r.n_inst * a.q_cap * G;
+  const Ahead ahead = ahead_of(a.b, inst, row);
+  const float m = lane < a.splits ? a.part_ml[(lane * step + at) * 2] : -INFINITY, l = lane < a.splits ? a.part_ml[(lane * step + at) * 2 + 1] : 0.f;
+  float top = m;
+  for (int p = lane; p < ahead.parts; p += 64) top = fmaxf(top, a.b.ml[(ahead.row + (size_t)kPrefillRows * p) * 2]);
+  top = wave_max(top);
+  const float use = top == -INFINITY ? 0.f : top, f = exp2_fast(m - use);
+  float sum = f * l;
+  for (int p = lane; p < ahead.parts; p += 64) {
+    const float* ml = a.b.ml + (ahead.row + (size_t)kPrefillRows * p) * 2;
+    sum += exp2_fast(ml[0] - use) * ml[1];
+  }
+  sum = wave_sum(sum);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  float o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < ahead.parts; ++p) {
+    const size_t x = ahead.row + (size_t)kPrefillRows * p;
+    const float w = exp2_fast(a.b.ml[x * 2] - use);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += w * a.b.o[x * D + lane * E + e];
+  }
+#pragma unroll 4
+  for (int x = 0; x < a.splits; ++x) {
+    const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x));
+    if (!(w > 0.f || w != w)) continue;                    // (a split without tiles has left no sums)
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += w * a.part_o[(x * step + at) * D + lane * E + e];
+  }
+  T* out = static_cast<T*>(a.out) + at * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if constexpr (sizeof(T) == 2) out[e].bits = __builtin_bit_cast(uint16_t, (__bf16)(o[e] * inv));
+    else out[e] = o[e] * inv;
   }
 }
 
@@ -608,8 +550,8 @@ template <typename T, int D, int G> hipError_t run(const Shape& s, const Prefill
   // 15.2 us and 15.3; 4 tokens behind 32 thousand rows, one instance 21.7 and 21.3, four 24.3 and 23.0.)
   const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
   const size_t lds = (size_t)2 * 2 * Form<T, D>::TILE * 16;
-  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false><<<grid, kThreads, lds, st>>>(a);
-  else cache_prefill_kernel<T, D, G, true><<<grid, kThreads, lds, st>>>(a);
+  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false, PrefillArgs><<<grid, kThreads, lds, st>>>(a);
+  else cache_prefill_kernel<T, D, G, true, PrefillArgs><<<grid, kThreads, lds, st>>>(a);
   if (a.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -625,14 +567,22 @@ template <typename T, int D, int G> hipError_t run(const Shape& s, const Prefill
   cache_weights_add_kernel<<<dim3(columns.x, columns.y), kPrefillRows, 0, st>>>(a);
   return hipGetLastError();
 }
-template <typename T, int D> hipError_t run_g(const Shape& s, const PrefillArgs& a, hipStream_t st) {
+template <typename T, int D, int G> hipError_t run(const Shape&, const SharedPrefillArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
+  cache_prefill_kernel<T, D, G, false, SharedPrefillArgs><<<grid, kThreads, (size_t)2 * 2 * Form<T, D>::TILE * 16, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  cache_prefill_behind_kernel<T, D, G><<<dim3((a.q_cap * G + kWaves - 1) / kWaves, a.r.n_inst), kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <typename T, int D, typename ARGS> hipError_t run_g(const Shape& s, const ARGS& a, hipStream_t st) {
   return s.g == 1 ? run<T, D, 1>(s, a, st) : s.g == 2 ? run<T, D, 2>(s, a, st) : s.g == 4 ? run<T, D, 4>(s, a, st) : run<T, D, 8>(s, a, st);
 }
 
 }  // namespace
 
-hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) {
-  PrefillArgs a = args;
+template <typename ARGS> static hipError_t launch(const Shape& s, const ARGS& args, hipStream_t st) {
+  ARGS a = args;
   a.stat_rows = cache_stat_rows(s, a.q_cap);
   a.tiles = (int)(((long long)a.q_cap * s.g + kPrefillRows - 1) / kPrefillRows);
   a.splits = cache_splits(s, a.q_cap, a.window, a.n_first);
@@ -640,5 +590,7 @@ hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStre
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s, a, st) : run_g<bf16_t, 64>(s, a, st);
   return s.d == 128 ? run_g<float, 128>(s, a, st) : run_g<float, 64>(s, a, st);
 }
+hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) { return launch(s, args, st); }
+hipError_t launch_cache_prefill_shared(const Shape& s, const SharedPrefillArgs& args, hipStream_t st) { return launch(s, args, st); }
 
 }  // namespace ap

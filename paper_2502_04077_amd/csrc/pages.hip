@@ -1,0 +1,456 @@
+// Pages of a pool that instances share: taken and given back, forked, compacted, copied.
+//
+// refs[p] says how often the table names page p; p is free where that is 0.  seg holds the number of free pages among each 1024, so that free
+// pages are found without reading through those in use.  Three steps, a launch each, as none can begin before the one before has ended
+// everywhere: what every instance needs, which free pages it gets (the x-th need in the order of instances and blocks gets the x-th free
+// page), and carrying it out.  The second step knows whether there are enough; if not, the third leaves all as it is.  Counts are whole numbers,
+// so that the order of atomics does not show in any result.  Where the state does not belong to the table, what comes out is unspecified, but every
+// page that is read or written lies in the pool.
+#include "cache_body.h"
+#include "share_internal.h"
+
+namespace ap {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kPickWgs = 64;
+
+struct Head { int needed, lacking, live, moved; };
+
+template <typename T> __device__ __forceinline__ T* at(char* ws, size_t offset) { return reinterpret_cast<T*>(ws + offset); }
+__device__ __forceinline__ bool in_pool(const Pages& p, int page) { return (unsigned)page < (unsigned)p.n_pages; }
+__device__ __forceinline__ int sum_int(int x) {            // over the wave's lanes
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ int lanes_before(unsigned long long mask) {
+  return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+}
+// One more, or one less, entry that names the page; info[0] and seg follow where it begins or ends to be in use.
+__device__ __forceinline__ void name_page(const Pages& p, int page, int32_t* info) {
+  if (atomicAdd(p.refs + page, 1) == 0) {
+    atomicAdd(p.seg + page / kSegment, -1);
+    atomicAdd(info, -1);
+  }
+}
+__device__ __forceinline__ void drop_page(const Pages& p, int page, int32_t* info) {
+  if (atomicAdd(p.refs + page, -1) == 1) {
+    atomicAdd(p.seg + page / kSegment, 1);
+    atomicAdd(info, 1);
+  }
+}
+// The first `rows` rows of K and V of a page, by `threads` threads.
+__device__ __forceinline__ void copy_rows(const Pages& p, int src, int dst, int rows, int tid, int threads) {
+  const int n = rows * p.row_pieces;
+  const size_t page = (size_t)p.row_pieces << p.lb;
+  for (int x = tid; x < 2 * n; x += threads) {
+    u32x4* X = static_cast<u32x4*>(x < n ? p.K : p.V);
+    const int y = x < n ? x : x - n;
+    X[dst * page + y] = X[src * page + y];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- counting
+__global__ __launch_bounds__(kThreads) void pages_clear_kernel(Pages p) {
+  const long long x = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (x < p.n_pages) p.refs[x] = 0;
+  if (x < p.segments) p.seg[x] = 0;
+}
+__global__ __launch_bounds__(kThreads) void pages_count_kernel(Pages p) {
+  const size_t all = (size_t)p.n_inst * p.nb_cap;
+  for (size_t x = (size_t)blockIdx.x * kThreads + threadIdx.x; x < all; x += (size_t)gridDim.x * kThreads)
+    if (in_pool(p, p.table[x])) atomicAdd(p.refs + p.table[x], 1);
+}
+__global__ __launch_bounds__(kThreads) void pages_free_kernel(Pages p) {
+  const int s = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (s >= p.segments) return;
+  int n = 0;
+  for (int x = lane; x < kSegment; x += 64) {
+    const long long page = (long long)s * kSegment + x;
+    n += page < p.n_pages && p.refs[page] <= 0;
+  }
+  n = sum_int(n);
+  if (lane == 0) p.seg[s] = n;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- needs
+struct Rows { int length, kept, want, own; };              // rows; rows that are not to be written; blocks; first block that is
+__device__ __forceinline__ Rows rows_of(const ResizeArgs& a, int i) {
+  Rows r;
+  r.length = clamped(a.len[i], 0, a.p.t_cap);
+  const int n = a.n_new == nullptr ? a.q_cap : clamped(a.n_new[i], 0, a.q_cap);
+  r.kept = n < r.length ? r.length - n : 0;
+  r.want = (int)(((long long)r.length + (1 << a.p.lb) - 1) >> a.p.lb);
+  r.own = n > 0 ? r.kept >> a.p.lb : r.want;
+  return r;
+}
+
+// A wave per instance: the blocks that need a page.
+__global__ __launch_bounds__(kThreads) void resize_need_kernel(ResizeArgs a) {
+  const int i = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (i >= a.p.n_inst) return;
+  const Rows r = rows_of(a, i);
+  const int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
+  int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
+  int count = 0;
+  for (int k0 = 0; k0 < r.want; k0 += 64) {
+    const int k = k0 + lane, page = k < r.want ? table[k] : 0;
+    const bool needs = k < r.want && (!in_pool(a.p, page) || (k >= r.own && a.p.refs[page] > 1));
+    const unsigned long long mask = __ballot(needs);
+    if (needs) staged[count + lanes_before(mask)] = k;
+    count += __popcll(mask);
+  }
+  if (lane == 0) at<int32_t>(a.ws, a.w.need)[i] = count;
+}
+
+// A wave per instance j, which goes on from instance p: the new table, and whether its last page is to be copied.
+__global__ __launch_bounds__(kThreads) void fork_need_kernel(ForkArgs a) {
+  const int j = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (j >= a.p.n_inst) return;
+  const int p = a.parent[j];
+  const bool some = (unsigned)p < (unsigned)a.p.n_inst;
+  int32_t* length = at<int32_t>(a.ws, a.w.length);
+  int32_t* need = at<int32_t>(a.ws, a.w.need);
+  if (!some || p == j) {
+    if (lane == 0) {
+      length[j] = some ? -1 : 0;
+      need[j] = 0;
+    }
+    return;
+  }
+  const int L = clamped(a.len[p], 0, a.p.t_cap), full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1);
+  bool heir = false;
+  if (rest > 0 && a.parent[p] != p) {                      // the lowest that goes on from p takes its last page over
+    heir = true;
+    for (int x0 = 0; x0 < j && heir; x0 += 64) heir = !__any(x0 + lane < j && a.parent[x0 + lane] == p);
+  }
+  const int32_t* table = a.p.table + (size_t)p * a.p.nb_cap;
+  int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
+  const int n = full + (rest > 0);
+  for (int k = lane; k < n; k += 64) staged[k] = table[k];
+  if (lane == 0) {
+    length[j] = L;
+    need[j] = rest > 0 && !heir && in_pool(a.p, table[full]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- free pages
+// The free pages of segments [s0, s1) are those from number `before` on; the first n of all are picked and in use from now on.  Called by a
+// workgroup; s_wave: kWaves words of LDS.
+__device__ __forceinline__ void pick_segments(const Pages& p, int s0, int s1, int before, int n, int32_t* picked, int32_t* taken, int* s_wave) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int s = s0; s < s1; ++s) {
+    int mine[kSegment / kThreads], count = 0;
+#pragma unroll
+    for (int e = 0; e < kSegment / kThreads; ++e) {
+      const long long page = (long long)s * kSegment + tid * (kSegment / kThreads) + e;
+      mine[e] = before < n && page < p.n_pages && p.refs[page] <= 0;
+      count += mine[e];
+    }
+    int upto = count;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    __syncthreads();
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    int rank = before + upto - count, all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) rank += s_wave[w];
+      all += s_wave[w];
+    }
+#pragma unroll
+    for (int e = 0; e < kSegment / kThreads; ++e)
+      if (mine[e]) {
+        if (rank >= 0 && rank < n) {
+          const int page = s * kSegment + tid * (kSegment / kThreads) + e;
+          picked[rank] = page;
+          p.refs[page] = 1;
+        }
+        ++rank;
+      }
+    if (tid == 0) taken[s] = n - before < all ? (n > before ? n - before : 0) : all;
+    before += all;
+  }
+}
+__device__ __forceinline__ int sum_of(const int32_t* x, int n, int* s_wave) {     // by a workgroup
+  int mine = 0;
+  for (int k = threadIdx.x; k < n; k += kThreads) mine += x[k];
+  mine = sum_int(mine);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  int all = 0;
+  for (int w = 0; w < kWaves; ++w) all += s_wave[w];
+  return all;
+}
+
+__global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
+  __shared__ int s_wave[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t* need = at<int32_t>(ws, w.need);
+  const int n = sum_of(need, p.n_inst, s_wave), free = clamped(sum_of(p.seg, p.segments, s_wave), 0, p.n_pages);
+  const int each = (p.segments + gridDim.x - 1) / gridDim.x;
+  const int s0 = blockIdx.x * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
+  if (s0 < s1) {
+    const int before = sum_of(p.seg, s0, s_wave);
+    pick_segments(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+  }
+  if (blockIdx.x > 0) return;
+  if (tid == 0) {
+    Head* head = at<Head>(ws, w.head);
+    head->needed = n;
+    head->lacking = n > free ? n - free : 0;
+    info[0] = n > free ? free : free - n;
+    info[1] = n > free ? n - free : 0;
+  }
+  // What the instances before need.
+  int done = 0;
+  for (int i0 = 0; i0 < p.n_inst; i0 += kThreads) {
+    const int i = i0 + tid, x = i < p.n_inst ? need[i] : 0;
+    int upto = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    __syncthreads();
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    int ahead = done + upto - x;
+    for (int v = 0; v < kWaves; ++v) {
+      if (v < wave) ahead += s_wave[v];
+      done += s_wave[v];
+    }
+    if (i < p.n_inst) at<int32_t>(ws, w.before)[i] = ahead;
+  }
+}
+__device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* taken) {
+  for (int s = blockIdx.x * kThreads + threadIdx.x; s < p.segments; s += gridDim.x * kThreads)
+    if (taken[s] > 0) atomicAdd(p.seg + s, -taken[s]);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- carrying it out
+__global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeArgs a) {
+  if (at<Head>(a.ws, a.w.head)->lacking > 0) return;
+  settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
+  const int i = blockIdx.x, tid = threadIdx.x;
+  const Rows r = rows_of(a, i);
+  int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
+  for (int k = r.want + tid; k < a.p.nb_cap; k += kThreads) {
+    const int page = table[k];
+    if (in_pool(a.p, page)) drop_page(a.p, page, a.info);
+    if (page != -1) table[k] = -1;
+  }
+  const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
+  const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + at<int32_t>(a.ws, a.w.before)[i];
+  const int n = at<int32_t>(a.ws, a.w.need)[i];
+  // The first needed block may have rows that stay, of a page that others keep.
+  if (n > 0) {
+    const int rest = r.kept & ((1 << a.p.lb) - 1);
+    for (int x = 0; rest > 0 && x < n && staged[x] <= r.own; ++x)
+      if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, kThreads);
+  }
+  __syncthreads();
+  for (int x = tid; x < n; x += kThreads) {
+    const int k = staged[x], old = table[k];
+    if (!in_pool(a.p, picked[x])) continue;
+    table[k] = picked[x];
+    if (in_pool(a.p, old)) drop_page(a.p, old, a.info);
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
+  const int j = blockIdx.x, tid = threadIdx.x;
+  if (at<Head>(a.ws, a.w.head)->lacking > 0) {
+    if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
+    return;
+  }
+  settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
+  const int L = at<int32_t>(a.ws, a.w.length)[j];
+  if (L < 0) {                                             // stays as it is
+    if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
+    return;
+  }
+  const int full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1), n = full + (rest > 0);
+  int32_t* table = a.p.table + (size_t)j * a.p.nb_cap;
+  const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
+  bool copy = at<int32_t>(a.ws, a.w.need)[j] > 0;
+  const int page = copy ? at<int32_t>(a.ws, a.w.picked)[at<int32_t>(a.ws, a.w.before)[j]] : 0;
+  copy = copy && in_pool(a.p, page);
+  if (copy) copy_rows(a.p, staged[full], page, rest, tid, kThreads);
+  for (int k = tid; k < a.p.nb_cap; k += kThreads) {
+    const int old = table[k];
+    const bool fresh = copy && k == full;
+    const int now = fresh ? page : (k < n ? staged[k] : -1);
+    if (now == old) continue;
+    table[k] = now;
+    if (!fresh && in_pool(a.p, now)) name_page(a.p, now, a.info);
+    if (in_pool(a.p, old)) drop_page(a.p, old, a.info);
+  }
+  if (tid == 0) a.len_out[j] = L;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- compaction
+// The x-th page in use that lies at `live` (their number) or behind goes to the x-th free page in front.
+__global__ __launch_bounds__(kThreads) void compact_list_kernel(CompactArgs a) {
+  __shared__ int s_wave[kWaves];
+  const Pages& p = a.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int live = p.n_pages - clamped(sum_of(p.seg, p.segments, s_wave), 0, p.n_pages);
+  // Free pages in front: those of whole segments, and of the one that `live` lies in.
+  const int sl = live / kSegment;
+  int moved = sl > 0 ? sum_of(p.seg, sl, s_wave) : 0;
+  {
+    int x = 0;
+    for (int page = sl * kSegment + tid; page < live; page += kThreads) x += p.refs[page] <= 0;
+    x = sum_int(x);
+    __syncthreads();
+    if (lane == 0) s_wave[wave] = x;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) moved += s_wave[w];
+    moved = clamped(moved, 0, live);
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    Head* head = at<Head>(a.ws, a.w.head);
+    head->live = live;
+    head->moved = moved;
+    a.info[0] = p.n_pages - live;
+    a.info[1] = moved;
+  }
+  const int each = (p.segments + gridDim.x - 1) / gridDim.x;
+  const int s0 = blockIdx.x * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
+  if (s0 >= s1) return;
+  int before = sum_of(p.seg, s0, s_wave);                  // free pages before
+  for (int s = s0; s < s1; ++s) {
+    int mine[kSegment / kThreads], count = 0;
+#pragma unroll
+    for (int e = 0; e < kSegment / kThreads; ++e) {
+      const long long page = (long long)s * kSegment + tid * (kSegment / kThreads) + e;
+      mine[e] = page < p.n_pages && p.refs[page] <= 0;
+      count += mine[e];
+    }
+    int upto = count;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    __syncthreads();
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    int rank = before + upto - count;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) rank += s_wave[w];
+      before += s_wave[w];
+    }
+#pragma unroll
+    for (int e = 0; e < kSegment / kThreads; ++e) {
+      const long long page = (long long)s * kSegment + tid * (kSegment / kThreads) + e;
+      if (page >= p.n_pages) continue;
+      if (mine[e]) {
+        if (page < live && rank >= 0 && rank < moved) at<int32_t>(a.ws, a.w.picked)[rank] = (int)page;
+        ++rank;
+      } else if (page >= live) {
+        const int x = (int)page - rank - (live - moved);   // pages in use before it, without those in front
+        if (x >= 0 && x < moved) at<int32_t>(a.ws, a.w.from)[x] = (int)page;
+        at<int32_t>(a.ws, a.w.rank)[page] = x;
+      }
+    }
+  }
+}
+__global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
+  const Pages& p = a.p;
+  const Head head = *at<Head>(a.ws, a.w.head);
+  const int32_t *hole = at<int32_t>(a.ws, a.w.picked), *from = at<int32_t>(a.ws, a.w.from), *rank = at<int32_t>(a.ws, a.w.rank);
+  const int tid = threadIdx.x;
+  for (int x = blockIdx.x; x < head.moved; x += gridDim.x) {
+    if (!in_pool(p, from[x]) || !in_pool(p, hole[x])) continue;
+    copy_rows(p, from[x], hole[x], 1 << p.lb, tid, kThreads);
+    if (tid == 0) {
+      p.refs[hole[x]] = p.refs[from[x]];
+      p.refs[from[x]] = 0;
+    }
+  }
+  const size_t all = (size_t)p.n_inst * p.nb_cap, step = (size_t)gridDim.x * kThreads;
+  for (size_t x = (size_t)blockIdx.x * kThreads + tid; x < all; x += step) {
+    const int page = p.table[x];
+    if (!in_pool(p, page) || page < head.live) continue;
+    const int y = rank[page];                              // (of a page that refs says is free, anything)
+    if ((unsigned)y < (unsigned)head.moved && from[y] == page) p.table[x] = hole[y];
+  }
+  for (int s = blockIdx.x * kThreads + tid; s < p.segments; s += gridDim.x * kThreads) {
+    const long long lo = (long long)s * kSegment, hi = lo + kSegment < p.n_pages ? lo + kSegment : p.n_pages;
+    p.seg[s] = (int)(hi <= head.live ? 0 : hi - (lo > head.live ? lo : head.live));
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void pages_copy_kernel(const u32x4* __restrict__ K_src, const u32x4* __restrict__ V_src, int n_src,
+                                                              const int32_t* __restrict__ from, u32x4* __restrict__ K_dst,
+                                                              u32x4* __restrict__ V_dst, int n_dst, const int32_t* __restrict__ to, int n,
+                                                              int page_pieces) {
+  for (int x = blockIdx.x; x < n; x += gridDim.x) {
+    const int src = from == nullptr ? x : from[x], dst = to == nullptr ? x : to[x];
+    if ((unsigned)src >= (unsigned)n_src || (unsigned)dst >= (unsigned)n_dst) continue;
+    for (int y = threadIdx.x; y < page_pieces; y += kThreads) {
+      K_dst[(size_t)dst * page_pieces + y] = K_src[(size_t)src * page_pieces + y];
+      V_dst[(size_t)dst * page_pieces + y] = V_src[(size_t)src * page_pieces + y];
+    }
+  }
+}
+
+unsigned pick_wgs(const Pages& p) { return p.segments < kPickWgs ? p.segments : kPickWgs; }
+unsigned per_wave(int n) { return ((unsigned)n + kWaves - 1) / kWaves; }
+
+}  // namespace
+
+hipError_t launch_pages_count(const Pages& p, hipStream_t st) {
+  pages_clear_kernel<<<(unsigned)(((long long)p.n_pages + kThreads - 1) / kThreads), kThreads, 0, st>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const size_t wgs = ((size_t)p.n_inst * p.nb_cap + kThreads - 1) / kThreads;
+  pages_count_kernel<<<(unsigned)(wgs < 4096 ? wgs : 4096), kThreads, 0, st>>>(p);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  pages_free_kernel<<<per_wave(p.segments), kThreads, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
+  resize_need_kernel<<<per_wave(a.p.n_inst), kThreads, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  pages_pick_kernel<<<pick_wgs(a.p), kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  resize_apply_kernel<<<a.p.n_inst, kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
+  fork_need_kernel<<<per_wave(a.p.n_inst), kThreads, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  pages_pick_kernel<<<pick_wgs(a.p), kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  fork_apply_kernel<<<a.p.n_inst, kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st) {
+  compact_list_kernel<<<pick_wgs(a.p), kThreads, 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  compact_move_kernel<<<2048, kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const void* K_src, const void* V_src, int n_src, const int32_t* from, void* K_dst, void* V_dst, int n_dst,
+                             const int32_t* to, int n, int page_pieces, hipStream_t st) {
+  pages_copy_kernel<<<n < 4096 ? n : 4096, kThreads, 0, st>>>(static_cast<const u32x4*>(K_src), static_cast<const u32x4*>(V_src), n_src, from,
+                                                              static_cast<u32x4*>(K_dst), static_cast<u32x4*>(V_dst), n_dst, to, n, page_pieces);
+  return hipGetLastError();
+}
+
+}  // namespace ap

@@ -1,0 +1,259 @@
+// C entry points of the calls on pages and on shared beginnings: argument checks, workspace, launches.
+#include "cache_checks.h"
+#include "share_internal.h"
+
+namespace ap {
+
+PagesWs pages_ws(const Shape& s, int n_pages) {
+  PagesWs w;
+  size_t o = 0;
+  auto take = [&o](size_t words) { const size_t at = o; o += (words * 4 + 15) / 16 * 16; return at; };
+  w.head = take(4);
+  w.need = take(s.n_inst);
+  w.before = take(s.n_inst);
+  w.length = take(s.n_inst);
+  w.staged = take((size_t)s.n_inst * s.nb_cap);
+  w.picked = take(n_pages);
+  w.taken = take(page_segments(n_pages));
+  w.from = take(n_pages);
+  w.rank = take(n_pages);
+  w.total = o;
+  return w;
+}
+
+size_t share_plan_bytes(const Shape& s) { return ((size_t)s.n_inst * 6 * 4 + 15) / 16 * 16; }
+SharePlan share_plan(const Shape& s, void* plan) {
+  SharePlan p;
+  p.inst = static_cast<int4*>(plan);
+  p.pos = reinterpret_cast<int32_t*>(p.inst + s.n_inst);
+  p.member = p.pos + s.n_inst;
+  return p;
+}
+
+// Chunks of so few rows of q that a tile of kPrefillRows has several instances'.
+bool few_rows(const Shape& s, int q_cap) { return q_cap * s.g <= kPrefillRows / 2; }
+
+SharedWs shared_ws(const Shape& s, int q_cap) {
+  SharedWs w;
+  size_t o = 0;
+  auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
+  const int rows = (q_cap > 0 ? q_cap : 1) * s.g;
+  w.start = take((size_t)s.n_inst * 4);
+  w.before = take((size_t)s.n_inst * 8);
+  w.units = take((size_t)s.n_inst * 4);
+  w.per = take(8);
+  const size_t pieces = (size_t)s.n_inst * rows + (size_t)kPrefillRows * kShareWgs;
+  w.ml = take(pieces * 2 * 4);
+  w.o = take(pieces * s.d * 4);
+  w.rest = o;
+  if (q_cap == 0) {
+    o += cache_decode_ws(s, false).total;
+  } else {
+    // As in cache_prefill_ws, but that sums are left to be joined with one split too.
+    size_t part = s.n_inst > kSplitWgs / 2 ? 0 : (size_t)kSplitWgs * kPrefillRows;
+    if (part < (size_t)s.n_inst * rows) part = (size_t)s.n_inst * rows;
+    o += (part * 2 * 4 + 15) / 16 * 16 + part * s.d * 4;
+  }
+  w.total = o;
+  return w;
+}
+
+}  // namespace ap
+
+using ap::Shape;
+using ap::fits;
+
+// Pages of a pool are numbered in 32 bits, with room behind them.
+static bool pool_ok(const Shape& s, int32_t n_pages) { return n_pages >= 1 && n_pages <= 1 << 30 && fits((long long)s.n_inst * 256); }
+
+static ap::Pages pages_of(const Shape& s, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state) {
+  ap::Pages p;
+  p.table = table; p.refs = state; p.seg = state + n_pages;
+  p.K = K; p.V = V;
+  p.n_inst = s.n_inst; p.t_cap = s.t_cap; p.nb_cap = s.nb_cap; p.n_pages = n_pages;
+  p.lb = 0;
+  while ((1 << p.lb) < s.b) ++p.lb;
+  p.segments = ap::page_segments(n_pages);
+  p.row_pieces = s.d * (s.kv_dtype == AP_BF16 ? 2 : 4) / 16;
+  return p;
+}
+
+// Of decode and prefill: the beginnings' part of the workspace.
+static ap::BeginArgs begin_args(const Shape& s, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
+                                const void* plan, int32_t window, int32_t n_first, char* base, const ap::SharedWs& w) {
+  ap::BeginArgs a;
+  a.r = rows_of(s, len);
+  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap;
+  a.window = seen_window(s, window); a.n_first = seen_first(s, n_first);
+  a.b.plan = ap::share_plan(s, const_cast<void*>(plan));
+  a.b.start = reinterpret_cast<int32_t*>(base + w.start);
+  a.b.before = reinterpret_cast<unsigned long long*>(base + w.before);
+  a.b.units = reinterpret_cast<int32_t*>(base + w.units);
+  a.b.per = reinterpret_cast<unsigned long long*>(base + w.per);
+  a.b.ml = reinterpret_cast<float*>(base + w.ml);
+  a.b.o = reinterpret_cast<float*>(base + w.o);
+  a.b.rows = q_cap * s.g;
+  return a;
+}
+// Rows of q of all instances are numbered in 32 bits, the pieces of the beginnings too.
+static bool rows_ok(const Shape& s, int32_t q_cap) {
+  return (long long)s.n_inst * q_cap * s.g + (long long)ap::kPrefillRows * ap::kShareWgs < (1ll << 31);
+}
+
+// As in api.hip: memory that a kernel may read and write, on the device or pinned; pageable host memory would fault the GPU.
+static bool reaches_device(const void* p) {
+  hipPointerAttribute_t a;
+  if (hipPointerGetAttributes(&a, p) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return a.type == hipMemoryTypeHost || a.type == hipMemoryTypeDevice || a.type == hipMemoryTypeManaged;
+}
+
+extern "C" {
+
+size_t ap_pages_state_bytes(const ap_ctx* ctx, int32_t n_pages) {
+  return ctx == nullptr || !pool_ok(ctx->s, n_pages) ? 0 : ((size_t)n_pages + ap::page_segments(n_pages)) * 4;
+}
+size_t ap_pages_workspace_bytes(const ap_ctx* ctx, int32_t n_pages) {
+  return ctx == nullptr || !pool_ok(ctx->s, n_pages) ? 0 : ap::pages_ws(ctx->s, n_pages).total;
+}
+
+int ap_pages_count(ap_ctx* ctx, const int32_t* table, int32_t n_pages, int32_t* state, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(table); AP_REQUIRE_PTR(state);
+  const Shape& s = ctx->s;
+  if (!pool_ok(s, n_pages)) return AP_ERR_RANGE;
+  return ap::launch_pages_count(pages_of(s, nullptr, nullptr, const_cast<int32_t*>(table), n_pages, state), static_cast<hipStream_t>(stream)) ==
+                 hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+int ap_pages_resize(ap_ctx* ctx, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state, const int32_t* len, const int32_t* n_new,
+                    int32_t q_cap, int32_t* info, void* ws, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V); AP_REQUIRE_PTR(table); AP_REQUIRE_PTR(state); AP_REQUIRE_PTR(len); AP_OPTIONAL_PTR(n_new);
+  AP_REQUIRE_PTR(info); AP_REQUIRE_PTR(ws);
+  const Shape& s = ctx->s;
+  if (!pool_ok(s, n_pages) || q_cap < 0) return AP_ERR_RANGE;
+  ap::ResizeArgs a;
+  a.p = pages_of(s, K, V, table, n_pages, state);
+  a.len = len; a.n_new = n_new; a.q_cap = q_cap; a.info = info; a.ws = static_cast<char*>(ws); a.w = ap::pages_ws(s, n_pages);
+  return ap::launch_pages_resize(a, static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+int ap_pages_fork(ap_ctx* ctx, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state, const int32_t* parent, const int32_t* len,
+                  int32_t* len_out, int32_t* info, void* ws, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V); AP_REQUIRE_PTR(table); AP_REQUIRE_PTR(state); AP_REQUIRE_PTR(parent); AP_REQUIRE_PTR(len);
+  AP_REQUIRE_PTR(len_out); AP_REQUIRE_PTR(info); AP_REQUIRE_PTR(ws);
+  const Shape& s = ctx->s;
+  if (!pool_ok(s, n_pages)) return AP_ERR_RANGE;
+  ap::ForkArgs a;
+  a.p = pages_of(s, K, V, table, n_pages, state);
+  a.parent = parent; a.len = len; a.len_out = len_out; a.info = info; a.ws = static_cast<char*>(ws); a.w = ap::pages_ws(s, n_pages);
+  return ap::launch_pages_fork(a, static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+int ap_pages_compact(ap_ctx* ctx, void* K, void* V, int32_t* table, int32_t n_pages, int32_t* state, int32_t* info, void* ws, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V); AP_REQUIRE_PTR(table); AP_REQUIRE_PTR(state); AP_REQUIRE_PTR(info); AP_REQUIRE_PTR(ws);
+  const Shape& s = ctx->s;
+  if (!pool_ok(s, n_pages)) return AP_ERR_RANGE;
+  ap::CompactArgs a;
+  a.p = pages_of(s, K, V, table, n_pages, state);
+  a.info = info; a.ws = static_cast<char*>(ws); a.w = ap::pages_ws(s, n_pages);
+  return ap::launch_pages_compact(a, static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+int ap_pages_copy(ap_ctx* ctx, const void* K_src, const void* V_src, int32_t n_src, const int32_t* src, void* K_dst, void* V_dst, int32_t n_dst,
+                  const int32_t* dst, int32_t n, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(K_src); AP_REQUIRE_PTR(V_src); AP_OPTIONAL_PTR(src); AP_REQUIRE_PTR(K_dst); AP_REQUIRE_PTR(V_dst); AP_OPTIONAL_PTR(dst);
+  const Shape& s = ctx->s;
+  if (!pool_ok(s, n_src) || !pool_ok(s, n_dst) || n < 0) return AP_ERR_RANGE;
+  if (n == 0) return AP_OK;
+  if (!reaches_device(K_src) || !reaches_device(V_src) || !reaches_device(K_dst) || !reaches_device(V_dst)) return AP_ERR_ARG;
+  return ap::launch_pages_copy(K_src, V_src, n_src, src, K_dst, V_dst, n_dst, dst, n, s.b * s.d * (s.kv_dtype == AP_BF16 ? 2 : 4) / 16,
+                               static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+size_t ap_cache_share_bytes(const ap_ctx* ctx) { return ctx == nullptr ? 0 : ap::share_plan_bytes(ctx->s); }
+
+int ap_cache_share(ap_ctx* ctx, const int32_t* group, const int32_t* shared, void* plan, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(group); AP_REQUIRE_PTR(shared); AP_REQUIRE_PTR(plan);
+  const Shape& s = ctx->s;
+  return ap::launch_cache_share(s, group, shared, ap::share_plan(s, plan), static_cast<hipStream_t>(stream)) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+size_t ap_cache_shared_workspace_bytes(const ap_ctx* ctx, int32_t q_cap) {
+  if (ctx == nullptr || q_cap < 0 || (q_cap > 0 && !chunk_ok(ctx->s, q_cap)) || !rows_ok(ctx->s, 1)) return 0;
+  const Shape& s = ctx->s;
+  size_t most = ap::shared_ws(s, 0).total;
+  // Of any chunk up to q_cap: those of few rows read beginnings for several instances at a time, the others are a prefill's.
+  int few = q_cap;
+  while (few > 0 && (!ap::few_rows(s, few) || !rows_ok(s, few))) few = few > ap::kPrefillRows ? ap::kPrefillRows : few - 1;
+  if (few > 0) {
+    const size_t x = ap::shared_ws(s, few).total;
+    if (x > most) most = x;
+  }
+  if (q_cap > 0) {
+    const size_t x = ap::cache_prefill_ws(s, q_cap, false).total;
+    if (x > most) most = x;
+  }
+  return most;
+}
+
+int ap_cache_decode_shared(ap_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* len, const void* plan, int32_t window,
+                           int32_t n_first, float* out, void* ws, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(q); AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V); AP_REQUIRE_PTR(len); AP_REQUIRE_PTR(plan); AP_REQUIRE_PTR(out); AP_REQUIRE_PTR(ws);
+  if (window < 0 || n_first < 0) return AP_ERR_ARG;
+  const Shape& s = ctx->s;
+  if (!rows_ok(s, 1)) return AP_ERR_RANGE;
+  const ap::SharedWs w = ap::shared_ws(s, 0);
+  char* base = static_cast<char*>(ws);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const ap::BeginArgs begin = begin_args(s, q, nullptr, 1, K, V, len, plan, window, n_first, base, w);
+  if (ap::launch_cache_beginnings(s, begin, true, st) != hipSuccess) return AP_ERR_HIP;
+  const ap::CacheWs d = ap::cache_decode_ws(s, false);
+  base += w.rest;
+  ap::SharedDecodeArgs a;
+  a.r = begin.r; a.q = q; a.K = K; a.V = V; a.window = begin.window; a.n_first = begin.n_first; a.out = out; a.acc = nullptr;
+  a.before = reinterpret_cast<unsigned long long*>(base + d.before);
+  a.whole = reinterpret_cast<float*>(base + d.whole);
+  a.part_ml = reinterpret_cast<float*>(base + d.part_ml);
+  a.part_acc = reinterpret_cast<float*>(base + d.part_acc);
+  a.tickets = reinterpret_cast<unsigned long long*>(base + d.tickets);
+  a.nonce = 0;            // (the launcher draws it)
+  a.logits = nullptr;
+  a.b = begin.b;
+  return ap::launch_cache_decode_shared(s, a, st) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+int ap_cache_prefill_shared(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
+                            const void* plan, int32_t window, int32_t n_first, void* out, void* ws, void* stream) {
+  if (ctx == nullptr) return AP_ERR_ARG;
+  AP_REQUIRE_PTR(q); AP_OPTIONAL_PTR(n_q); AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V); AP_REQUIRE_PTR(len); AP_REQUIRE_PTR(plan); AP_REQUIRE_PTR(out);
+  AP_REQUIRE_PTR(ws);
+  if (window < 0 || n_first < 0) return AP_ERR_ARG;
+  const Shape& s = ctx->s;
+  if (!chunk_ok(s, q_cap)) return AP_ERR_RANGE;
+  if (!ap::few_rows(s, q_cap) || !rows_ok(s, q_cap)) return ap_cache_prefill(ctx, q, n_q, q_cap, K, V, len, window, n_first, out, nullptr, ws, stream);
+  const ap::SharedWs w = ap::shared_ws(s, q_cap);
+  char* base = static_cast<char*>(ws);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const ap::BeginArgs begin = begin_args(s, q, n_q, q_cap, K, V, len, plan, window, n_first, base, w);
+  if (ap::launch_cache_beginnings(s, begin, s.kv_dtype == AP_F32, st) != hipSuccess) return AP_ERR_HIP;
+  base += w.rest;
+  ap::SharedPrefillArgs a;
+  a.r = begin.r; a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.window = begin.window; a.n_first = begin.n_first; a.out = out;
+  a.acc = nullptr; a.stat = nullptr; a.sums = nullptr;
+  const size_t part = (w.total - w.rest) / (4 * ((size_t)s.d + 2));
+  a.part_ml = reinterpret_cast<float*>(base);
+  a.part_o = reinterpret_cast<float*>(base + (part * 2 * 4 + 15) / 16 * 16);
+  a.b = begin.b;
+  return ap::launch_cache_prefill_shared(s, a, st) == hipSuccess ? AP_OK : AP_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,91 @@
+// Sequences that share pages and a beginning: what the calls on them (share_api.hip) hand to the kernels.
+#pragma once
+
+#include "cache_internal.h"
+
+namespace ap {
+
+// A pool and the table that names its pages.
+struct Pages {
+  int32_t* table;          // [n_inst][nb_cap]; entries outside the pool name no page
+  int32_t* refs;           // [n_pages] how often the table names each page; 0: free
+  int32_t* seg;            // [segments] free pages among each kSegment pages
+  void *K, *V;
+  int n_inst, t_cap, nb_cap, n_pages, lb, segments, row_pieces;      // lb = log2(b); 16-byte pieces of a row
+};
+constexpr int kSegment = 1024;
+inline int page_segments(int n_pages) { return (int)(((long long)n_pages + kSegment - 1) / kSegment); }
+
+// Workspace of the calls on pages, in bytes.  What a call needs is decided first (need, staged, kept, length), then free pages are picked
+// (before, picked, taken), then all is carried out.
+struct PagesWs {
+  size_t head;             // 4 words: pages needed, pages lacking; pages in use, pages to move
+  size_t need;             // int32 [n_inst] pages needed
+  size_t before;           // int32 [n_inst] pages needed by the instances before
+  size_t length;           // int32 [n_inst] rows from now on (fork), -1: stays as it is
+  size_t staged;           // int32 [n_inst][nb_cap] resize: the blocks that need a page; fork: the new table
+  size_t picked;           // int32 [n_pages] free pages, the lowest first; compact: those in front of the pages in use
+  size_t taken;            // int32 [segments] pages taken of each segment
+  size_t from, rank;       // int32 [n_pages] compact: pages to move, and each one's place among them
+  size_t total;
+};
+PagesWs pages_ws(const Shape& s, int n_pages);
+
+struct ResizeArgs { Pages p; const int32_t *len, *n_new; int q_cap; int32_t* info; char* ws; PagesWs w; };
+struct ForkArgs { Pages p; const int32_t *parent, *len; int32_t *len_out, *info; char* ws; PagesWs w; };
+struct CompactArgs { Pages p; int32_t* info; char* ws; PagesWs w; };
+
+hipError_t launch_pages_count(const Pages& p, hipStream_t st);
+hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st);
+hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st);
+hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st);
+// page_pieces: 16-byte pieces of a page of K, or V.  from, to: null: 0, 1, 2, ...
+hipError_t launch_pages_copy(const void* K_src, const void* V_src, int n_src, const int32_t* from, void* K_dst, void* V_dst, int n_dst,
+                             const int32_t* to, int n, int page_pieces, hipStream_t st);
+
+// Groups of instances whose first rows are the same.  plan: what ap_cache_share makes of `group` and `shared`.
+struct SharePlan {
+  int4* inst;              // [n_inst] first member (the lowest); place of its group's first row in `member`; members, 1: alone; rows in common
+  int32_t* pos;            // [n_inst] own place in `member`, -1: alone
+  int32_t* member;         // [n_inst] the groups' members, groups by their first member, members ascending
+};
+size_t share_plan_bytes(const Shape& s);
+SharePlan share_plan(const Shape& s, void* plan);
+
+// What the attention over the beginnings leaves for the attention over the rows behind them.  A group's rows of q, those of its members one after
+// the other, are in tiles of kPrefillRows, its beginning in tiles of the cache; a unit is one of each.  The units, tile by tile of each group in the
+// order of the groups, are dealt to the workgroups in equal shares; the piece that workgroup w leaves of row x (of all groups' rows) is
+// number x + kPrefillRows * w.
+struct Beginnings {
+  SharePlan plan;
+  int32_t* start;                  // [n_inst] rows that were read as a group's beginning: the others' first
+  unsigned long long* before;      // [n_inst] of a first member: units of the groups before
+  int32_t* units;                  // [n_inst] of a first member: units of a tile of its rows of q
+  unsigned long long* per;         // units of a workgroup
+  float *ml, *o;                   // [n_inst * rows + kPrefillRows * kShareWgs][2] maximum and sum, and [..][d]
+  int rows;                        // of q, of an instance
+};
+constexpr int kShareWgs = 512;     // two a CU
+
+struct BeginArgs {                 // the attention over the beginnings
+  CacheRows r;
+  const void *q, *K, *V;
+  const int32_t* n_q;              // as in PrefillArgs
+  int q_cap, window, n_first;
+  Beginnings b;
+};
+struct SharedDecodeArgs : DecodeArgs { Beginnings b; };
+struct SharedPrefillArgs : PrefillArgs { Beginnings b; };
+
+struct SharedWs { size_t start, before, units, per, ml, o, rest, total; };        // rest: of the attention over the rows behind
+SharedWs shared_ws(const Shape& s, int q_cap);
+
+hipError_t launch_cache_share(const Shape& s, const int32_t* group, const int32_t* shared, const SharePlan& plan, hipStream_t st);
+// exact: probabilities keep 32 bits.
+hipError_t launch_cache_beginnings(const Shape& s, const BeginArgs& a, bool exact, hipStream_t st);
+hipError_t launch_cache_decode_shared(const Shape& s, const SharedDecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_prefill_shared(const Shape& s, const SharedPrefillArgs& a, hipStream_t st);
+// Rows of q of an instance up to which beginnings are read for several of them at a time.
+bool few_rows(const Shape& s, int q_cap);
+
+}  // namespace ap
