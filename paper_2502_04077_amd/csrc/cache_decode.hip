@@ -170,16 +170,14 @@ __device__ __forceinline__ bool last_of(unsigned long long* word, unsigned long 
   return *s_last != 0;
 }
 
-// An output (of maximum `top` and sum `all`, which `val` has not been divided by), joined with the pieces of the beginning.
-template <int D> __device__ __forceinline__ float joined(const Beginnings& b, const Ahead& at, int h, int e, float top, float all, float val) {
-  float m = top;
+// Element e of head h of an output that the pieces of the beginning alone make.
+template <int D> __device__ __forceinline__ float joined(const Beginnings& b, const Ahead& at, int h, int e) {
+  float m = -INFINITY, all = 0.f, val = 0.f;
   const size_t first = (size_t)at.row + h;
-#pragma unroll 4
+#pragma unroll 8
   for (int p = 0; p < at.parts; ++p) m = fmaxf(m, b.ml[(first + (size_t)kPrefillRows * p) * 2]);
-  const float use = reference(m), f0 = exp2_fast(top - use);
-  all *= f0;
-  val *= f0;
-#pragma unroll 4
+  const float use = reference(m);
+#pragma unroll 8
   for (int p = 0; p < at.parts; ++p) {
     const size_t x = first + (size_t)kPrefillRows * p;
     const float f = exp2_fast(b.ml[x * 2] - use);
@@ -193,9 +191,8 @@ template <int D> __device__ __forceinline__ float joined(const Beginnings& b, co
 // inst < 0, the output.  SHARED: the pieces were written by workgroups of the same launch.  s: `bytes` of LDS, the factors of the pieces in
 // front, and behind them pieces, of which as many as there is room for are on their way at a time: one workgroup's loads are what this
 // costs (64 pieces of g = 4, d = 128, 16 in registers at a time: 12 us).
-template <int G, int D, bool SHARED, typename ARGS>
-__device__ __forceinline__ void join_pieces(const ARGS& a, int inst, int w0, int parts, float* s, int bytes, float* s_m, float* s_inv) {
-  constexpr bool BEHIND = std::is_same<ARGS, SharedDecodeArgs>::value;
+template <int G, int D, bool SHARED>
+__device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w0, int parts, float* s, int bytes, float* s_m, float* s_inv) {
   constexpr int PP = G * D / 4, R = (G * D + kThreads - 1) / kThreads;              // 16-byte pieces of a part, outputs of a thread
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   auto read = [](const float* p) { return SHARED ? ld_shared_out(p) : *p; };
@@ -243,8 +240,8 @@ __device__ __forceinline__ void join_pieces(const ARGS& a, int inst, int w0, int
     }
     all = wave_sum(all);
     if (lane == 0) {
-      s_m[h] = BEHIND ? top : use;
-      s_inv[h] = BEHIND ? all : over(1.f, all);
+      s_m[h] = use;
+      s_inv[h] = over(1.f, all);
     }
   }
   if (inst < 0) {
@@ -273,12 +270,7 @@ __device__ __forceinline__ void join_pieces(const ARGS& a, int inst, int w0, int
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int x = r * kThreads + tid;
-    if constexpr (BEHIND) {
-      const Ahead at = ahead_of(a.b, inst, 0);
-      if (x < G * D) a.out[(size_t)inst * G * D + x] = joined<D>(a.b, at, x / D, x % D, s_m[x / D], s_inv[x / D], val[r]);
-    } else {
-      if (x < G * D) a.out[(size_t)inst * G * D + x] = val[r] * s_inv[x / D];
-    }
+    if (x < G * D) a.out[(size_t)inst * G * D + x] = val[r] * s_inv[x / D];
   }
 }
 
@@ -343,7 +335,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     if constexpr (BEHIND) {                                // (what their beginning gives)
       if (see(i).n > 0) continue;
       const Ahead at = ahead_of(a.b, i, 0);
-      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = joined<D>(a.b, at, x / D, x % D, -INFINITY, 0.f, 0.f);
+      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = joined<D>(a.b, at, x / D, x % D);
     } else if (a.r.len[i] <= 0) {
       for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
     }
@@ -439,6 +431,48 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     for (int h = 0; h < G; ++h)
 #pragma unroll
       for (int e = 0; e < F::E; ++e) o[h][e] = 0.f;
+    if constexpr (BEHIND) {
+      // The pieces of the beginning are where the first piece of an instance starts from: they are joined while the first rows are on their way.
+      // The lanes that have a row of V at a time take a piece at a time, those of all waves in turn.
+      const Ahead ahead = from == 0 ? ahead_of(a.b, inst, 0) : Ahead{0, 0};
+      if (ahead.parts > 0) {
+        const int every = alone ? F::RPL : F::RPL * kWaves;
+        const int first = (alone ? 0 : wave * F::RPL) + lane / F::PIECES;
+        const float* ml = a.b.ml + (size_t)ahead.row * 2;
+        float top[G];
+#pragma unroll
+        for (int h = 0; h < G; ++h) top[h] = -INFINITY;
+        for (int p = lane; p < ahead.parts; p += kWave)
+#pragma unroll
+          for (int h = 0; h < G; ++h) top[h] = fmaxf(top[h], ml[((size_t)kPrefillRows * p + h) * 2]);
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+          top[h] = wave_max(top[h]);
+          m = head % G == h ? top[h] : m;
+        }
+#pragma unroll 2
+        for (int p = first; p < ahead.parts; p += every)
+#pragma unroll
+          for (int h = 0; h < G; ++h) {
+            const size_t x = (size_t)kPrefillRows * p + h;
+            const float f = exp2_fast(ml[x * 2] - reference(top[h]));
+            const float* from_o = a.b.o + ((size_t)ahead.row + x) * D + lane % F::PIECES * F::E;
+#pragma unroll
+            for (int e = 0; e < F::E; e += 4) {
+              const float4v y = *reinterpret_cast<const float4v*>(from_o + e);
+#pragma unroll
+              for (int w = 0; w < 4; ++w) o[h][e + w] += f * y[w];
+            }
+          }
+        // The sums: lane (head, kg) every fourth of the wave's pieces.
+        const int mine = alone ? kg : wave * 4 + kg, all_lanes = alone ? 4 : 4 * kWaves;
+        if (head < G)
+          for (int p = mine; p < ahead.parts; p += all_lanes) {
+            const float* x = ml + ((size_t)kPrefillRows * p + head) * 2;
+            sum += exp2_fast(x[0] - reference(m)) * x[1];
+          }
+      }
+    }
 
     for (int it = 0; it < mine_n; ++it) {
       const Place here = next[0];
@@ -545,20 +579,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         o[h][e] = sum32(o[h][e]);
       }
     }
-    Ahead ahead_here = {0, 0};
-    if constexpr (BEHIND) ahead_here = ahead_of(a.b, inst, 0);
     if (alone) {
 #pragma unroll
       for (int h = 0; h < G; ++h) {
         const float all = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), h));
-        const float top = BEHIND ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), h)) : 0.f;
         if (lane < F::PIECES) {
           float* to_out = a.out + ((size_t)inst * G + h) * D + lane * F::E;
 #pragma unroll
-          for (int e = 0; e < F::E; ++e) {
-            if constexpr (BEHIND) to_out[e] = joined<D>(a.b, ahead_here, h, lane * F::E + e, top, all, o[h][e]);
-            else to_out[e] = over(o[h][e], all);
-          }
+          for (int e = 0; e < F::E; ++e) to_out[e] = over(o[h][e], all);
         }
       }
       if (ACC && lane < G) {
@@ -590,9 +618,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         all += f * s_ml[w][h][1];
         val += f * s_out[w * F::WAVE * 4 + x];
       }
-      if (whole && BEHIND) {
-        if constexpr (BEHIND) a.out[((size_t)inst * G + h) * D + e] = joined<D>(a.b, ahead_here, h, e, top, all, val);
-      } else if (whole) a.out[((size_t)inst * G + h) * D + e] = over(val, all);
+      if (whole) a.out[((size_t)inst * G + h) * D + e] = over(val, all);
       else st_shared_out<!ACC>(a.part_acc + (slot * G + h) * D + e, val);
       if (e == 0 && (ACC || !whole)) {
         float* ml = whole ? a.whole + ((size_t)inst * G + h) * 2 : a.part_ml + (slot * G + h) * 2;

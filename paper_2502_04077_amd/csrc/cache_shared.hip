@@ -24,6 +24,7 @@ __global__ __launch_bounds__(kThreads) void share_group_kernel(const int32_t* __
     s_group[threadIdx.x] = k < n ? group[k] : -1;
     s_shared[threadIdx.x] = k < n ? shared[k] : 0;
     __syncthreads();
+#pragma unroll 16
     for (int x = 0; x < kThreads; ++x) {
       const bool same = s_group[x] == mine;
       lead = same && k0 + x < lead ? k0 + x : lead;
@@ -48,6 +49,7 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
     const int k = k0 + threadIdx.x;
     s_count[threadIdx.x] = k < n && inst[k].x == k && inst[k].z > 1 ? inst[k].z : 0;
     __syncthreads();
+#pragma unroll 16
     for (int x = 0; x < kThreads; ++x) ahead += k0 + x < lead ? s_count[x] : 0;
   }
   if (i >= n) return;

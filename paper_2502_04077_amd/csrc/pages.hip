@@ -13,7 +13,7 @@ namespace ap {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kPickWgs = 64;
+constexpr int kPickWgs = 64, kApplyWgs = 128;
 
 struct Head { int needed, lacking, live, moved; };
 
@@ -27,18 +27,34 @@ __device__ __forceinline__ int sum_int(int x) {            // over the wave's la
 __device__ __forceinline__ int lanes_before(unsigned long long mask) {
   return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
 }
-// One more, or one less, entry that names the page; info[0] and seg follow where it begins or ends to be in use.
-__device__ __forceinline__ void name_page(const Pages& p, int page, int32_t* info) {
-  if (atomicAdd(p.refs + page, 1) == 0) {
-    atomicAdd(p.seg + page / kSegment, -1);
-    atomicAdd(info, -1);
+// One less entry that names the page, of every lane with `some`: returns how many pages are free now.  seg follows, an addition for each segment that
+// lanes have: additions to one word wait for each other.
+__device__ __forceinline__ void add_by_segment(const Pages& p, bool some, int page, int by) {
+  unsigned long long todo = __ballot(some);
+  const int s = page / kSegment;
+  while (todo != 0) {
+    const int first = __ffsll(todo) - 1;
+    const unsigned long long same = __ballot(some && s == __builtin_amdgcn_readlane(s, first)) & todo;
+    if ((int)(threadIdx.x & 63) == first) atomicAdd(p.seg + s, by * __popcll(same));
+    todo &= ~same;
   }
 }
-__device__ __forceinline__ void drop_page(const Pages& p, int page, int32_t* info) {
-  if (atomicAdd(p.refs + page, -1) == 1) {
-    atomicAdd(p.seg + page / kSegment, 1);
-    atomicAdd(info, 1);
-  }
+__device__ __forceinline__ int drop_pages(const Pages& p, bool some, int page) {
+  const bool freed = some && atomicAdd(p.refs + page, -1) == 1;
+  add_by_segment(p, freed, page, 1);
+  return __popcll(__ballot(freed));
+}
+// One more: returns how many pages are not free any longer (that were given up by others a moment ago).
+__device__ __forceinline__ int name_pages(const Pages& p, bool some, int page) {
+  const bool was_free = some && atomicAdd(p.refs + page, 1) == 0;
+  add_by_segment(p, was_free, page, -1);
+  return __popcll(__ballot(was_free));
+}
+// A workgroup's sum of what its waves freed, to info[0]; s_free is a word of LDS that was 0.
+__device__ __forceinline__ void add_free(int freed, int* s_free, int32_t* info) {
+  if ((threadIdx.x & 63) == 0 && freed != 0) atomicAdd(s_free, freed);
+  __syncthreads();
+  if (threadIdx.x == 0 && *s_free != 0) atomicAdd(info, *s_free);
 }
 // The first `rows` rows of K and V of a page, by `threads` threads.
 __device__ __forceinline__ void copy_rows(const Pages& p, int src, int dst, int rows, int tid, int threads) {
@@ -234,47 +250,55 @@ __device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* t
 }
 
 // ---------------------------------------------------------------------------------------------------------------- carrying it out
+// A workgroup has every gridDim.x-th instance.
 __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeArgs a) {
+  __shared__ int s_free;
   if (at<Head>(a.ws, a.w.head)->lacking > 0) return;
-  settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
-  const int i = blockIdx.x, tid = threadIdx.x;
-  const Rows r = rows_of(a, i);
-  int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
-  for (int k = r.want + tid; k < a.p.nb_cap; k += kThreads) {
-    const int page = table[k];
-    if (in_pool(a.p, page)) drop_page(a.p, page, a.info);
-    if (page != -1) table[k] = -1;
-  }
-  const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
-  const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + at<int32_t>(a.ws, a.w.before)[i];
-  const int n = at<int32_t>(a.ws, a.w.need)[i];
-  // The first needed block may have rows that stay, of a page that others keep.
-  if (n > 0) {
-    const int rest = r.kept & ((1 << a.p.lb) - 1);
-    for (int x = 0; rest > 0 && x < n && staged[x] <= r.own; ++x)
-      if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, kThreads);
-  }
+  const int tid = threadIdx.x;
+  if (tid == 0) s_free = 0;
   __syncthreads();
-  for (int x = tid; x < n; x += kThreads) {
-    const int k = staged[x], old = table[k];
-    if (!in_pool(a.p, picked[x])) continue;
-    table[k] = picked[x];
-    if (in_pool(a.p, old)) drop_page(a.p, old, a.info);
+  settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
+  int freed = 0;
+  for (int i = blockIdx.x; i < a.p.n_inst; i += gridDim.x) {
+    const Rows r = rows_of(a, i);
+    int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
+    const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
+    const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + at<int32_t>(a.ws, a.w.before)[i];
+    const int n = at<int32_t>(a.ws, a.w.need)[i], rest = r.kept & ((1 << a.p.lb) - 1);
+    if (n > 0 && rest > 0 && r.own < r.want) {
+      // The first block that is written may have rows that stay, of a page that others keep.
+      for (int x = 0; x < n && staged[x] <= r.own; ++x)
+        if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, kThreads);
+      __syncthreads();
+    }
+    for (int k0 = r.want; k0 < a.p.nb_cap; k0 += kThreads) {
+      const int k = k0 + tid, page = k < a.p.nb_cap ? table[k] : -1;
+      if (__any(page != -1)) freed += drop_pages(a.p, in_pool(a.p, page), page);
+      if (page != -1) table[k] = -1;
+    }
+    for (int x0 = 0; x0 < n; x0 += kThreads) {
+      const int x = x0 + tid;
+      const bool some = x < n && in_pool(a.p, picked[x < n ? x : 0]);
+      const int k = some ? staged[x] : 0, old = some ? table[k] : -1;
+      if (some) table[k] = picked[x];
+      if (__any(in_pool(a.p, old))) freed += drop_pages(a.p, in_pool(a.p, old), old);
+    }
   }
+  add_free(freed, &s_free, a.info);
 }
 
 __global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
+  __shared__ int s_free;
   const int j = blockIdx.x, tid = threadIdx.x;
-  if (at<Head>(a.ws, a.w.head)->lacking > 0) {
-    if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
-    return;
-  }
-  settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
-  const int L = at<int32_t>(a.ws, a.w.length)[j];
+  const bool lacking = at<Head>(a.ws, a.w.head)->lacking > 0;
+  const int L = lacking ? -1 : at<int32_t>(a.ws, a.w.length)[j];
+  if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
   if (L < 0) {                                             // stays as it is
     if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
     return;
   }
+  if (tid == 0) s_free = 0;
+  __syncthreads();
   const int full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1), n = full + (rest > 0);
   int32_t* table = a.p.table + (size_t)j * a.p.nb_cap;
   const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
@@ -282,16 +306,19 @@ __global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
   const int page = copy ? at<int32_t>(a.ws, a.w.picked)[at<int32_t>(a.ws, a.w.before)[j]] : 0;
   copy = copy && in_pool(a.p, page);
   if (copy) copy_rows(a.p, staged[full], page, rest, tid, kThreads);
-  for (int k = tid; k < a.p.nb_cap; k += kThreads) {
-    const int old = table[k];
+  int freed = 0;
+  for (int k0 = 0; k0 < a.p.nb_cap; k0 += kThreads) {
+    const int k = k0 + tid, old = k < a.p.nb_cap ? table[k] : -1;
     const bool fresh = copy && k == full;
     const int now = fresh ? page : (k < n ? staged[k] : -1);
-    if (now == old) continue;
-    table[k] = now;
-    if (!fresh && in_pool(a.p, now)) name_page(a.p, now, a.info);
-    if (in_pool(a.p, old)) drop_page(a.p, old, a.info);
+    const bool changed = now != old;
+    if (changed) table[k] = now;
+    if (!__any(changed)) continue;
+    freed -= name_pages(a.p, changed && !fresh && in_pool(a.p, now), now);
+    freed += drop_pages(a.p, changed && in_pool(a.p, old), old);
   }
   if (tid == 0) a.len_out[j] = L;
+  add_free(freed, &s_free, a.info);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- compaction
@@ -424,7 +451,7 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   pages_pick_kernel<<<pick_wgs(a.p), kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  resize_apply_kernel<<<a.p.n_inst, kThreads, 0, st>>>(a);
+  resize_apply_kernel<<<a.p.n_inst < kApplyWgs ? a.p.n_inst : kApplyWgs, kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
