@@ -24,6 +24,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kGroup = 16;
 constexpr int kLeastGroups = 8;      // least share of a workgroup: two passes a wave
 constexpr int kShort = 64;           // groups of an instance that a wave goes over alone
+constexpr int kBehindGroups = 8;     // what an instance counts beside its groups, where the pieces of a beginning are joined
 constexpr unsigned long long kAlone = ~0ull;   // in the place of the number of groups: every instance was whole
 constexpr int kLongShare = 64;       // share from which on a CU has several workgroups
 
@@ -170,23 +171,6 @@ __device__ __forceinline__ bool last_of(unsigned long long* word, unsigned long 
   return *s_last != 0;
 }
 
-// Element e of head h of an output that the pieces of the beginning alone make.
-template <int D> __device__ __forceinline__ float joined(const Beginnings& b, const Ahead& at, int h, int e) {
-  float m = -INFINITY, all = 0.f, val = 0.f;
-  const size_t first = (size_t)at.row + h;
-#pragma unroll 8
-  for (int p = 0; p < at.parts; ++p) m = fmaxf(m, b.ml[(first + (size_t)kPrefillRows * p) * 2]);
-  const float use = reference(m);
-#pragma unroll 8
-  for (int p = 0; p < at.parts; ++p) {
-    const size_t x = first + (size_t)kPrefillRows * p;
-    const float f = exp2_fast(b.ml[x * 2] - use);
-    all += f * b.ml[x * 2 + 1];
-    val += f * b.o[x * D + e];
-  }
-  return over(val, all);
-}
-
 // Joins `parts` pieces, from that of workgroup w0 on, by one workgroup: maximum and 1 / sum of every head to s_m and s_inv, and, unless
 // inst < 0, the output.  SHARED: the pieces were written by workgroups of the same launch.  s: `bytes` of LDS, the factors of the pieces in
 // front, and behind them pieces, of which as many as there is room for are on their way at a time: one workgroup's loads are what this
@@ -283,6 +267,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     if constexpr (BEHIND) return seen_behind(a.r.len[i], a.b.start[i], a.r.t_cap, a.window, a.n_first);
     else return seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first);
   };
+  // What an instance counts in a share: its groups, and where a beginning may be in front of them, kBehindGroups for what an instance costs
+  // beside them.
+  constexpr int FRONT = BEHIND ? kBehindGroups : 0;
+  auto size_of = [&](int i) {
+    if constexpr (BEHIND) {
+      const int n = see(i).n;
+      return n > 0 || a.b.start[i] > 0 ? n + FRONT : 0;
+    } else {
+      return see(i).n;
+    }
+  };
   extern __shared__ __attribute__((aligned(16))) u32x4 s_rows[];          // [wave]: [buffer][K, V][TILE], queries; at the end outputs, [G][D]
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
@@ -300,9 +295,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   int longest = 0;
 #pragma unroll 4
   for (int i = i_begin; i < i_end; ++i) {
-    const int n = see(i).n;
+    const int n = size_of(i);
     mine += (unsigned)n;
-    longest = n > longest ? n : longest;
+    longest = n - FRONT > longest ? n - FRONT : longest;
   }
   unsigned long long upto = mine;
 #pragma unroll
@@ -332,19 +327,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const unsigned long long end = begin + per < groups ? begin + per : groups;
   // Empty instances have no share; their outputs are zero.
   for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS) {
-    if constexpr (BEHIND) {                                // (what their beginning gives)
-      if (see(i).n > 0) continue;
-      const Ahead at = ahead_of(a.b, i, 0);
-      for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = joined<D>(a.b, at, x / D, x % D);
-    } else if (a.r.len[i] <= 0) {
+    if (BEHIND ? size_of(i) == 0 : a.r.len[i] <= 0)
       for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
-    }
   }
   if (ACC && blockIdx.x == 0) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
       a.before[i] = at;
-      at += (unsigned)see(i).n;
+      at += (unsigned)size_of(i);
     }
     if (tid == kThreads - 1) a.before[a.r.n_inst] = alone ? kAlone : groups;
   }
@@ -353,7 +343,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   if (alone ? ahead < end && begin < ahead + mine : ahead <= begin && begin < ahead + mine) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
-      const unsigned n = (unsigned)see(i).n;
+      const unsigned n = (unsigned)size_of(i);
       if (alone) {
         if (n > 0 && at >= begin && at < end) {
           atomicMin(&s_first[(int)((at - begin) / share)], i);
@@ -383,22 +373,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   float* s_out = reinterpret_cast<float*>(s_rows);
   for (; alone ? left > 0 && inst < mine_to : left > 0; ++inst, from = 0) {
     const auto s = see(inst);
-    if (s.n <= from) continue;                             // an empty instance
-    const int to = alone ? s.n : (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
+    const int size = BEHIND ? size_of(inst) : s.n;
+    if (size <= from) continue;                            // an empty instance
+    const int to = alone ? size : (unsigned long long)(size - from) <= left ? size : from + (int)left;
     if (!alone) left -= (unsigned)(to - from);
-    const bool whole = from == 0 && to == s.n;
+    const bool whole = from == 0 && to == size;
     // The other pieces: of the workgroups from w0 on.  The last of them to be done joins them; with weights a second launch does.
     int w0 = blockIdx.x, parts = 1;
     if (!ACC && !whole) {
       if (from > 0) w0 = (int)((done - (unsigned)from) / per);
-      parts = (int)((done + (unsigned)(s.n - from) - 1) / per) - w0 + 1;
+      parts = (int)((done + (unsigned)(size - from) - 1) / per) - w0 + 1;
     }
     done += (unsigned)(to - from);
     unsigned long long* ticket = a.tickets + (size_t)w0 * kTicketStride;      // (an instance that begins in a workgroup and does not end there: one at most)
 
     // This wave's groups are from + wave, from + wave + 4, ...; two of them are on their way to LDS while one is worked off.
-    const int mine_n = alone ? s.n : (to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0);
-    const int u0 = alone ? 0 : from + wave;
+    const int g0 = !BEHIND ? from : (from > FRONT ? from - FRONT : 0), g1 = !BEHIND ? to : (to > FRONT ? to - FRONT : 0);
+    const int mine_n = alone ? s.n : (g1 - g0 > wave ? (g1 - g0 - wave + kWaves - 1) / kWaves : 0);
+    const int u0 = alone ? 0 : g0 + wave;
     Place next[2];                                         // of the groups behind the ones that were sent for
     if (mine_n > 0) {
 #pragma unroll
