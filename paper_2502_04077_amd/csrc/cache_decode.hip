@@ -25,6 +25,7 @@ constexpr int kThreads = 256, kWaves = 4, kGroup = 16;
 constexpr int kLeastGroups = 8;      // least share of a workgroup: two passes a wave
 constexpr int kShort = 64;           // groups of an instance that a wave goes over alone
 constexpr int kBehindGroups = 8;     // what an instance counts beside its groups, where the pieces of a beginning are joined
+constexpr int kLeastBehind = 16, kWholeGroups = 32;      // there: least share of a workgroup; instances up to this (or up to a share) are not cut
 constexpr unsigned long long kAlone = ~0ull;   // in the place of the number of groups: every instance was whole
 constexpr int kLongShare = 64;       // share from which on a CU has several workgroups
 
@@ -74,6 +75,11 @@ __device__ __forceinline__ SeenBehind seen_behind(int len, int s0, int t_cap, in
 __device__ __forceinline__ unsigned long long share_of(unsigned long long groups, int wgs) {
   const unsigned long long one = (groups + 255) / 256, all = (groups + wgs - 1) / wgs;
   return one <= kLeastGroups ? kLeastGroups : (one <= kLongShare ? one : (all > kLongShare ? all : kLongShare));
+}
+
+__device__ __forceinline__ unsigned long long share_behind(unsigned long long groups, int wgs) {
+  const unsigned long long all = (groups + wgs - 1) / wgs;
+  return all > kLeastBehind ? all : kLeastBehind;
 }
 
 // Scores below what 32 bits hold are -inf and weigh nothing.  Where a head has no others yet its maximum is -inf, which exponents do not refer to,
@@ -322,7 +328,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   // More instances than workgroups, all of them short: every wave takes whole instances, those that begin in its share, with no pieces and
   // nobody to wait for.
   const bool alone = __builtin_amdgcn_readfirstlane(a.r.n_inst > F::WGS && longest <= kShort);
-  const unsigned long long per = alone ? kWaves * ((groups + kWaves * F::WGS - 1) / (kWaves * F::WGS)) : share_of(groups, F::WGS);
+  const unsigned long long per = alone ? kWaves * ((groups + kWaves * F::WGS - 1) / (kWaves * F::WGS))
+                                       : (BEHIND ? share_behind(groups, F::WGS) : share_of(groups, F::WGS));
   const unsigned long long begin = (unsigned long long)blockIdx.x * per;
   const unsigned long long end = begin + per < groups ? begin + per : groups;
   // Empty instances have no share; their outputs are zero.
@@ -375,8 +382,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     const auto s = see(inst);
     const int size = BEHIND ? size_of(inst) : s.n;
     if (size <= from) continue;                            // an empty instance
-    const int to = alone ? size : (unsigned long long)(size - from) <= left ? size : from + (int)left;
-    if (!alone) left -= (unsigned)(to - from);
+    // Behind beginnings, what belongs to the workgroup that it begins in, whole.
+    const bool whole_here = BEHIND && !alone && (unsigned)size <= (per > kWholeGroups ? per : kWholeGroups);
+    if (whole_here && from > 0) {
+      left = left > (unsigned)(size - from) ? left - (unsigned)(size - from) : 0;
+      done += (unsigned)(size - from);
+      continue;
+    }
+    const int to = alone || whole_here ? size : (unsigned long long)(size - from) <= left ? size : from + (int)left;
+    if (!alone) left -= BEHIND && left < (unsigned)(to - from) ? left : (unsigned)(to - from);
     const bool whole = from == 0 && to == size;
     // The other pieces: of the workgroups from w0 on.  The last of them to be done joins them; with weights a second launch does.
     int w0 = blockIdx.x, parts = 1;
@@ -426,15 +440,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     if constexpr (BEHIND) {
       // The pieces of the beginning are where the first piece of an instance starts from: they are joined while the first rows are on their way.
       // The lanes that have a row of V at a time take a piece at a time, those of all waves in turn.
-      const Ahead ahead = from == 0 ? ahead_of(a.b, inst, 0) : Ahead{0, 0};
-      if (ahead.parts > 0) {
+      const int2 ahead = from == 0 ? ahead_of(a.b, inst, 0) : make_int2(0, 0);
+      if (ahead.y > 0) {
         const int every = alone ? F::RPL : F::RPL * kWaves;
         const int first = (alone ? 0 : wave * F::RPL) + lane / F::PIECES;
-        const float* ml = a.b.ml + (size_t)ahead.row * 2;
+        const float* ml = a.b.ml + (size_t)ahead.x * 2;
         float top[G];
 #pragma unroll
         for (int h = 0; h < G; ++h) top[h] = -INFINITY;
-        for (int p = lane; p < ahead.parts; p += kWave)
+        for (int p = lane; p < ahead.y; p += kWave)
 #pragma unroll
           for (int h = 0; h < G; ++h) top[h] = fmaxf(top[h], ml[((size_t)kPrefillRows * p + h) * 2]);
 #pragma unroll
@@ -443,12 +457,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
           m = head % G == h ? top[h] : m;
         }
 #pragma unroll 2
-        for (int p = first; p < ahead.parts; p += every)
+        for (int p = first; p < ahead.y; p += every)
 #pragma unroll
           for (int h = 0; h < G; ++h) {
             const size_t x = (size_t)kPrefillRows * p + h;
             const float f = exp2_fast(ml[x * 2] - reference(top[h]));
-            const float* from_o = a.b.o + ((size_t)ahead.row + x) * D + lane % F::PIECES * F::E;
+            const float* from_o = a.b.o + ((size_t)ahead.x + x) * D + lane % F::PIECES * F::E;
 #pragma unroll
             for (int e = 0; e < F::E; e += 4) {
               const float4v y = *reinterpret_cast<const float4v*>(from_o + e);
@@ -459,7 +473,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
         // The sums: lane (head, kg) every fourth of the wave's pieces.
         const int mine = alone ? kg : wave * 4 + kg, all_lanes = alone ? 4 : 4 * kWaves;
         if (head < G)
-          for (int p = mine; p < ahead.parts; p += all_lanes) {
+          for (int p = mine; p < ahead.y; p += all_lanes) {
             const float* x = ml + ((size_t)kPrefillRows * p + head) * 2;
             sum += exp2_fast(x[0] - reference(m)) * x[1];
           }

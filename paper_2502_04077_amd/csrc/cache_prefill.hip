@@ -325,15 +325,15 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_behind_kernel(SharedPr
   const int nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
   if (row >= nq * G) return;
   const size_t at = (size_t)inst * a.q_cap * G + row, step = (size_t)a.r.n_inst * a.q_cap * G;
-  const Ahead ahead = ahead_of(a.b, inst, row);
+  const int2 ahead = ahead_of(a.b, inst, row);
   const float m = lane < a.splits ? a.part_ml[(lane * step + at) * 2] : -INFINITY, l = lane < a.splits ? a.part_ml[(lane * step + at) * 2 + 1] : 0.f;
   float top = m;
-  for (int p = lane; p < ahead.parts; p += 64) top = fmaxf(top, a.b.ml[(ahead.row + (size_t)kPrefillRows * p) * 2]);
+  for (int p = lane; p < ahead.y; p += 64) top = fmaxf(top, a.b.ml[(ahead.x + (size_t)kPrefillRows * p) * 2]);
   top = wave_max(top);
   const float use = top == -INFINITY ? 0.f : top, f = exp2_fast(m - use);
   float sum = f * l;
-  for (int p = lane; p < ahead.parts; p += 64) {
-    const float* ml = a.b.ml + (ahead.row + (size_t)kPrefillRows * p) * 2;
+  for (int p = lane; p < ahead.y; p += 64) {
+    const float* ml = a.b.ml + (ahead.x + (size_t)kPrefillRows * p) * 2;
     sum += exp2_fast(ml[0] - use) * ml[1];
   }
   sum = wave_sum(sum);
@@ -342,8 +342,8 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_behind_kernel(SharedPr
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 4
-  for (int p = 0; p < ahead.parts; ++p) {
-    const size_t x = ahead.row + (size_t)kPrefillRows * p;
+  for (int p = 0; p < ahead.y; ++p) {
+    const size_t x = ahead.x + (size_t)kPrefillRows * p;
     const float w = exp2_fast(a.b.ml[x * 2] - use);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] += w * a.b.o[x * D + lane * E + e];

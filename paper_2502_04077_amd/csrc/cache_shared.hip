@@ -15,7 +15,7 @@ namespace {
 // First member, place among the members, number of members and rows in common: every instance looks at all others.
 __global__ __launch_bounds__(kThreads) void share_group_kernel(const int32_t* __restrict__ group, const int32_t* __restrict__ shared, int n,
                                                                int t_cap, SharePlan plan) {
-  __shared__ int s_group[kThreads], s_shared[kThreads];
+  __shared__ __attribute__((aligned(16))) int s_group[kThreads], s_shared[kThreads];
   const int i = blockIdx.x * kThreads + threadIdx.x, mine = i < n ? group[i] : -1;
   int lead = n, rank = 0, count = 0, common = t_cap;
   for (int k0 = 0; k0 < n; k0 += kThreads) {
@@ -24,13 +24,18 @@ __global__ __launch_bounds__(kThreads) void share_group_kernel(const int32_t* __
     s_group[threadIdx.x] = k < n ? group[k] : -1;
     s_shared[threadIdx.x] = k < n ? shared[k] : 0;
     __syncthreads();
-#pragma unroll 16
-    for (int x = 0; x < kThreads; ++x) {
-      const bool same = s_group[x] == mine;
-      lead = same && k0 + x < lead ? k0 + x : lead;
-      rank += same && k0 + x < i;
-      count += same;
-      common = same && s_shared[x] < common ? s_shared[x] : common;
+#pragma unroll 4
+    for (int x = 0; x < kThreads; x += 4) {
+      const int4 y = *reinterpret_cast<const int4*>(s_group + x), z = *reinterpret_cast<const int4*>(s_shared + x);
+      const int gs[4] = {y.x, y.y, y.z, y.w}, rows[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool same = gs[e] == mine;
+        lead = same && k0 + x + e < lead ? k0 + x + e : lead;
+        rank += same && k0 + x + e < i;
+        count += same;
+        common = same && rows[e] < common ? rows[e] : common;
+      }
     }
   }
   if (i >= n) return;
@@ -39,19 +44,29 @@ __global__ __launch_bounds__(kThreads) void share_group_kernel(const int32_t* __
 }
 // Groups one after the other, by their first member.
 __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan plan) {
-  __shared__ int s_count[kThreads];
+  __shared__ __attribute__((aligned(16))) int s_count[kThreads];
   const int i = blockIdx.x * kThreads + threadIdx.x;
   int4* inst = plan.inst;
   const int lead = i < n ? inst[i].x : 0, count = i < n ? inst[i].z : 1;
-  int ahead = 0;
+  int ahead = 0, groups = 0, all = 0;
   for (int k0 = 0; k0 < n; k0 += kThreads) {
     __syncthreads();
     const int k = k0 + threadIdx.x;
     s_count[threadIdx.x] = k < n && inst[k].x == k && inst[k].z > 1 ? inst[k].z : 0;
     __syncthreads();
-#pragma unroll 16
-    for (int x = 0; x < kThreads; ++x) ahead += k0 + x < lead ? s_count[x] : 0;
+#pragma unroll 4
+    for (int x = 0; x < kThreads; x += 4) {
+      const int4 y = *reinterpret_cast<const int4*>(s_count + x);
+      const int c[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        ahead += k0 + x + e < lead ? c[e] : 0;
+        groups += k0 + x + e < lead && c[e] > 0;
+        all += c[e] > 0;
+      }
+    }
   }
+  if (i == 0) *plan.count = all;
   if (i >= n) return;
   if (count < 2) {
     plan.pos[i] = -1;
@@ -61,6 +76,7 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
   inst[i].y = ahead;
   plan.pos[i] = at;
   plan.member[at] = i;
+  if (lead == i) plan.groups[groups] = make_int4(i, ahead, count, inst[i].w);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- the beginnings
@@ -75,7 +91,8 @@ struct Begin {
 template <int TT> __device__ __forceinline__ Begin begin_of(const BeginArgs& a, int4 inst) {
   Begin s;
   s.lead = inst.x; s.first = inst.y; s.count = inst.z;
-  const int L = inst.z > 1 ? clamped(a.r.len[s.lead], 0, a.r.t_cap) : 0;
+  const bool several = inst.z > 1 && (unsigned)inst.x < (unsigned)a.r.n_inst && inst.y >= 0 && inst.z <= a.r.n_inst - inst.y;
+  const int L = several ? clamped(a.r.len[s.lead], 0, a.r.t_cap) : 0;
   s.S = inst.w < L ? inst.w : L;
   s.lo0 = 0;
   s.p1 = s.S - 1;
@@ -100,16 +117,8 @@ template <int TT> __device__ __forceinline__ Begin begin_of(const BeginArgs& a, 
   s.tiles = s.p1 < 0 ? 0 : s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
   return s;
 }
-__device__ __forceinline__ int q_tiles(const BeginArgs& a, const Begin& s) {
-  return (int)(((long long)s.count * a.b.rows + kPrefillRows - 1) / kPrefillRows);
-}
-// Units of a group, counted at its first member.
-template <int TT> __device__ __forceinline__ unsigned long long units_of(const BeginArgs& a, int i, int4 inst, int* tiles) {
-  *tiles = 0;
-  if (inst.x != i || inst.z < 2) return 0;
-  const Begin s = begin_of<TT>(a, inst);
-  *tiles = s.tiles;
-  return (unsigned long long)s.tiles * q_tiles(a, s);
+__device__ __forceinline__ unsigned long long units_of(const BeginArgs& a, const Begin& s) {
+  return (unsigned long long)s.tiles * (unsigned)((s.count * a.b.rows + kPrefillRows - 1) / kPrefillRows);
 }
 constexpr int kLeastUnits = 2;      // of a workgroup
 
@@ -143,18 +152,11 @@ __global__ __launch_bounds__(kThreads) void cache_beginnings_kernel(BeginArgs a,
   __shared__ int s_first;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
 
-  // Where this workgroup's share begins: every thread sums the units of consecutive instances.
-  const int n_inst = a.r.n_inst;
-  for (int i = blockIdx.x * kThreads + tid; i < n_inst; i += gridDim.x * kThreads) {
-    const int4 inst = a.b.plan.inst[i];
-    const int L = inst.z > 1 ? clamped(a.r.len[inst.x], 0, a.r.t_cap) : 0;
-    a.b.start[i] = inst.w < L ? inst.w : L;
-  }
-  const int chunk = (n_inst + kThreads - 1) / kThreads;
-  const int i_begin = tid * chunk < n_inst ? tid * chunk : n_inst, i_end = i_begin + chunk < n_inst ? i_begin + chunk : n_inst;
+  // Where this workgroup's share begins: every thread sums the units of consecutive groups.
+  const int groups = clamped(*a.b.plan.count, 0, a.r.n_inst), chunk = (groups + kThreads - 1) / kThreads;
+  const int i_begin = tid * chunk < groups ? tid * chunk : groups, i_end = i_begin + chunk < groups ? i_begin + chunk : groups;
   unsigned long long mine = 0;
-  int tiles;
-  for (int i = i_begin; i < i_end; ++i) mine += units_of<F::TT>(a, i, a.b.plan.inst[i], &tiles);
+  for (int i = i_begin; i < i_end; ++i) mine += units_of(a, begin_of<F::TT>(a, a.b.plan.groups[i]));
   unsigned long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -170,39 +172,40 @@ __global__ __launch_bounds__(kThreads) void cache_beginnings_kernel(BeginArgs a,
   }
   unsigned long long per = (units + gridDim.x - 1) / gridDim.x;
   if (per < kLeastUnits) per = kLeastUnits;
-  const unsigned long long begin = (unsigned long long)blockIdx.x * per;
-  unsigned long long left = begin < units ? (begin + per < units ? per : units - begin) : 0;
-  if (blockIdx.x == 0 || (left > 0 && ahead <= begin && begin < ahead + mine)) {
+  unsigned long long done = (unsigned long long)blockIdx.x * per;         // units in front of the next one
+  unsigned long long left = done < units ? (done + per < units ? per : units - done) : 0;
+  if (left > 0 && ahead <= done && done < ahead + mine) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
-      const unsigned long long u = units_of<F::TT>(a, i, a.b.plan.inst[i], &tiles);
-      if (blockIdx.x == 0) {
-        a.b.before[i] = at;
-        a.b.units[i] = tiles;
-      }
-      if (left > 0 && at <= begin && begin < at + u) {
+      const unsigned long long u = units_of(a, begin_of<F::TT>(a, a.b.plan.groups[i]));
+      if (at <= done && done < at + u) {
         s_first = i;
-        s_from = begin - at;
+        s_from = done - at;
       }
       at += u;
     }
   }
-  if (blockIdx.x == 0 && tid == 0) *a.b.per = per;
+  // Where every instance's own rows begin.
+  for (int i = blockIdx.x * kThreads + tid; i < a.r.n_inst; i += gridDim.x * kThreads) {
+    const Begin s = begin_of<F::TT>(a, a.b.plan.inst[i]);
+    a.b.start[i] = s.tiles > 0 ? s.S : 0;
+  }
   if (left == 0) return;
   __syncthreads();
-  int lead = __builtin_amdgcn_readfirstlane(s_first);
   unsigned long long from = s_from;
 
   const float scale = kLog2E / sqrtf((float)D);
   const unsigned buffers = lds_address(s_tiles);
-  for (;;) {
-    const Begin s = begin_of<F::TT>(a, a.b.plan.inst[lead]);
-    const unsigned long long all_units = (unsigned long long)s.tiles * q_tiles(a, s);
-    for (; left > 0 && from < all_units;) {
+  for (int gi = __builtin_amdgcn_readfirstlane(s_first); left > 0 && gi < groups; ++gi, from = 0) {
+    const Begin s = begin_of<F::TT>(a, a.b.plan.groups[gi]);
+    const unsigned long long all_units = units_of(a, s);
+    while (left > 0 && from < all_units) {
       const int t = (int)(from / (unsigned)s.tiles), u_begin = (int)(from % (unsigned)s.tiles);
       const int u_end = (unsigned long long)(s.tiles - u_begin) < left ? s.tiles : u_begin + (int)left;
+      const int parts = (int)((done - (unsigned)u_begin + (unsigned)s.tiles - 1) / per) - (int)blockIdx.x + 1;      // of this tile, from here on
       from += (unsigned)(u_end - u_begin);
       left -= (unsigned)(u_end - u_begin);
+      done += (unsigned)(u_end - u_begin);
 
       // This lane's row of q, of all of the group's.  Rows that are none are computed as the group's first and not stored.
       const int x = t * kPrefillRows + wave * 32 + n;
@@ -363,6 +366,7 @@ __global__ __launch_bounds__(kThreads) void cache_beginnings_kernel(BeginArgs a,
       sum = sum32(sum);
       if (real) {
         const size_t slot = (size_t)s.first * a.b.rows + x + (size_t)kPrefillRows * blockIdx.x;
+        if (hb == 0 && u_begin == 0) a.b.row[(size_t)s.first * a.b.rows + x] = make_int2((int)slot, parts);
         if (hb == 0) {
           a.b.ml[slot * 2] = m;
           a.b.ml[slot * 2 + 1] = sum;
@@ -378,19 +382,6 @@ __global__ __launch_bounds__(kThreads) void cache_beginnings_kernel(BeginArgs a,
           }
       }
     }
-    if (left == 0) return;
-    // The next group: 64 instances at a time.
-    for (int i0 = lead + 1; ; i0 += 64) {
-      if (i0 >= n_inst) return;                            // (there is one as long as something is left)
-      const int i = i0 + lane;
-      const unsigned long long u = i < n_inst ? units_of<F::TT>(a, i, a.b.plan.inst[i], &tiles) : 0;
-      const unsigned long long some = __ballot(u > 0);
-      if (some == 0) continue;
-      lead = i0 + __ffsll(some) - 1;
-      break;
-    }
-    lead = __builtin_amdgcn_readfirstlane(lead);
-    from = 0;
   }
 }
 

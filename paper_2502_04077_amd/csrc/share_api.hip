@@ -21,11 +21,13 @@ PagesWs pages_ws(const Shape& s, int n_pages) {
   return w;
 }
 
-size_t share_plan_bytes(const Shape& s) { return ((size_t)s.n_inst * 6 * 4 + 15) / 16 * 16; }
+size_t share_plan_bytes(const Shape& s) { return ((size_t)s.n_inst * 10 * 4 + 16 + 15) / 16 * 16; }
 SharePlan share_plan(const Shape& s, void* plan) {
   SharePlan p;
   p.inst = static_cast<int4*>(plan);
-  p.pos = reinterpret_cast<int32_t*>(p.inst + s.n_inst);
+  p.groups = p.inst + s.n_inst;
+  p.count = reinterpret_cast<int32_t*>(p.groups + s.n_inst);
+  p.pos = p.count + 4;
   p.member = p.pos + s.n_inst;
   return p;
 }
@@ -39,9 +41,7 @@ SharedWs shared_ws(const Shape& s, int q_cap) {
   auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
   const int rows = (q_cap > 0 ? q_cap : 1) * s.g;
   w.start = take((size_t)s.n_inst * 4);
-  w.before = take((size_t)s.n_inst * 8);
-  w.units = take((size_t)s.n_inst * 4);
-  w.per = take(8);
+  w.row = take((size_t)s.n_inst * rows * 8);
   const size_t pieces = (size_t)s.n_inst * rows + (size_t)kPrefillRows * kShareWgs;
   w.ml = take(pieces * 2 * 4);
   w.o = take(pieces * s.d * 4);
@@ -87,9 +87,7 @@ static ap::BeginArgs begin_args(const Shape& s, const void* q, const int32_t* n_
   a.window = seen_window(s, window); a.n_first = seen_first(s, n_first);
   a.b.plan = ap::share_plan(s, const_cast<void*>(plan));
   a.b.start = reinterpret_cast<int32_t*>(base + w.start);
-  a.b.before = reinterpret_cast<unsigned long long*>(base + w.before);
-  a.b.units = reinterpret_cast<int32_t*>(base + w.units);
-  a.b.per = reinterpret_cast<unsigned long long*>(base + w.per);
+  a.b.row = reinterpret_cast<int2*>(base + w.row);
   a.b.ml = reinterpret_cast<float*>(base + w.ml);
   a.b.o = reinterpret_cast<float*>(base + w.o);
   a.b.rows = q_cap * s.g;

@@ -7,16 +7,9 @@
 namespace ap {
 namespace {
 
-// The pieces that the attention over an instance's beginning left of its row `rest` of q: piece p is number row + kPrefillRows * p.
-struct Ahead { int row, parts; };
-__device__ __forceinline__ Ahead ahead_of(const Beginnings& b, int inst, int rest) {
-  if (b.start[inst] == 0) return {0, 0};
-  const int4 group = b.plan.inst[inst];
-  const int k = b.units[group.x], r = (b.plan.pos[inst] - group.y) * b.rows + rest;
-  if (k == 0) return {0, 0};
-  const unsigned long long u = b.before[group.x] + (unsigned long long)(r / kPrefillRows) * k, per = *b.per;
-  const int w0 = (int)(u / per);
-  return {group.y * b.rows + r + kPrefillRows * w0, (int)((u + k - 1) / per) - w0 + 1};
+// The pieces that the attention over an instance's beginning left of its row `rest` of q: piece p is number x + kPrefillRows * p, p < y.
+__device__ __forceinline__ int2 ahead_of(const Beginnings& b, int inst, int rest) {
+  return b.start[inst] == 0 ? make_int2(0, 0) : b.row[(size_t)b.plan.pos[inst] * b.rows + rest];
 }
 
 }  // namespace

@@ -46,8 +46,10 @@ hipError_t launch_pages_copy(const void* K_src, const void* V_src, int n_src, co
 // Groups of instances whose first rows are the same.  plan: what ap_cache_share makes of `group` and `shared`.
 struct SharePlan {
   int4* inst;              // [n_inst] first member (the lowest); place of its group's first row in `member`; members, 1: alone; rows in common
+  int4* groups;            // [n_inst] the same line of every group of several members, in the order of the first ones
   int32_t* pos;            // [n_inst] own place in `member`, -1: alone
   int32_t* member;         // [n_inst] the groups' members, groups by their first member, members ascending
+  int32_t* count;          // [4] groups
 };
 size_t share_plan_bytes(const Shape& s);
 SharePlan share_plan(const Shape& s, void* plan);
@@ -59,9 +61,7 @@ SharePlan share_plan(const Shape& s, void* plan);
 struct Beginnings {
   SharePlan plan;
   int32_t* start;                  // [n_inst] rows that were read as a group's beginning: the others' first
-  unsigned long long* before;      // [n_inst] of a first member: units of the groups before
-  int32_t* units;                  // [n_inst] of a first member: units of a tile of its rows of q
-  unsigned long long* per;         // units of a workgroup
+  int2* row;                       // [n_inst * rows] of a group's row of q: the first of its pieces, and how many
   float *ml, *o;                   // [n_inst * rows + kPrefillRows * kShareWgs][2] maximum and sum, and [..][d]
   int rows;                        // of q, of an instance
 };
@@ -77,7 +77,7 @@ struct BeginArgs {                 // the attention over the beginnings
 struct SharedDecodeArgs : DecodeArgs { Beginnings b; };
 struct SharedPrefillArgs : PrefillArgs { Beginnings b; };
 
-struct SharedWs { size_t start, before, units, per, ml, o, rest, total; };        // rest: of the attention over the rows behind
+struct SharedWs { size_t start, row, ml, o, rest, total; };        // rest: of the attention over the rows behind
 SharedWs shared_ws(const Shape& s, int q_cap);
 
 hipError_t launch_cache_share(const Shape& s, const int32_t* group, const int32_t* shared, const SharePlan& plan, hipStream_t st);

@@ -98,8 +98,9 @@ def test_plan():
                 inst[i] = [m[0], len(order), len(m), max(0, min(48, min(shared[x] for x in m)))]
                 pos[i] = len(order) + k
             order += m
-        assert words[:4 * n].view(n, 4).tolist() == inst and words[4 * n:5 * n].tolist() == pos
-        assert words[5 * n:5 * n + len(order)].tolist() == order
+        groups = [inst[i] for i in range(n) if inst[i][0] == i and inst[i][2] > 1]
+        assert words[:4 * n].view(n, 4).tolist() == inst and words[4 * n:8 * n].view(n, 4)[:len(groups)].tolist() == groups and words[8 * n] == len(groups)
+        assert words[8 * n + 4:9 * n + 4].tolist() == pos and words[9 * n + 4:9 * n + 4 + len(order)].tolist() == order
 
 
 def _many(n, f):
