@@ -16,7 +16,7 @@
 // d = 64 49 us, 4.8; with rows through registers and pages looked up by vector loads, which wait for
 // the rows in flight, 246 and 639.  Where more instances than workgroups are all short, every wave takes whole ones: 2048 of 8 to 419 rows
 // (g = 1, 111 MB) 38 us, by shares of a workgroup 61; of 16 to 56 (g = 2, d = 64) 18 and 40.
-#include "share_body.h"
+#include "cache_body.h"
 
 namespace ap {
 namespace {
@@ -24,8 +24,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kGroup = 16;
 constexpr int kLeastGroups = 8;      // least share of a workgroup: two passes a wave
 constexpr int kShort = 64;           // groups of an instance that a wave goes over alone
-constexpr int kBehindGroups = 8;     // what an instance counts beside its groups, where the pieces of a beginning are joined
-constexpr int kLeastBehind = 16, kWholeGroups = 32;      // there: least share of a workgroup; instances up to this (or up to a share) are not cut
 constexpr unsigned long long kAlone = ~0ull;   // in the place of the number of groups: every instance was whole
 constexpr int kLongShare = 64;       // share from which on a CU has several workgroups
 
@@ -46,40 +44,12 @@ __device__ __forceinline__ Seen seen_of(int len, int t_cap, int window, int n_fi
   return s;
 }
 
-// The same without the rows [0, s0), which were read as the beginning of a group: [s0, f) and [lo, L), s0 <= f <= lo or f = 0.
-struct SeenBehind {
-  int L, lo, f, s0, ga, gs, gb, n;
-  __device__ __forceinline__ int group(int u) const { return u < gs ? ga + u : gb + (u - gs); }
-  __device__ __forceinline__ bool row(int j) const { return j < L && j >= s0 && (j >= lo || j < f); }
-};
-__device__ __forceinline__ SeenBehind seen_behind(int len, int s0, int t_cap, int window, int n_first) {
-  SeenBehind s;
-  s.L = clamped(len, 0, t_cap);
-  s.s0 = s0;
-  s.lo = window > 0 && s.L > window ? s.L - window : 0;
-  s.f = n_first < s.lo ? n_first : s.lo;
-  if (s.lo < s0) s.lo = s0;
-  if (s.f <= s0) s.f = 0;
-  s.ga = s0 / kGroup;
-  const int end = (s.f + kGroup - 1) / kGroup;             // behind the first rows' groups
-  s.gs = s.f > 0 ? end - s.ga : 0;
-  s.gb = s.lo / kGroup;
-  if (s.gs > 0 && s.gb < end) s.gb = end;
-  s.n = s.lo < s.L ? s.gs + (s.L - 1) / kGroup - s.gb + 1 : 0;
-  return s;
-}
-
 // Groups of a workgroup.  Up to kLongShare one workgroup a CU: what several gain in loads under way is less than what their pieces cost to
 // join (8 instances of 8000 rows, g = 4, d = 128: 512 workgroups 22 us, 250 19; of 32000 rows 36 and 33; 16 of 32000 rows, from
 // where on it does not matter, 53 and 51; 8 of 2041 rows by shares of 4, 8, 16: 13.5, 12.4, 13.4).
 __device__ __forceinline__ unsigned long long share_of(unsigned long long groups, int wgs) {
   const unsigned long long one = (groups + 255) / 256, all = (groups + wgs - 1) / wgs;
   return one <= kLeastGroups ? kLeastGroups : (one <= kLongShare ? one : (all > kLongShare ? all : kLongShare));
-}
-
-__device__ __forceinline__ unsigned long long share_behind(unsigned long long groups, int wgs) {
-  const unsigned long long all = (groups + wgs - 1) / wgs;
-  return all > kLeastBehind ? all : kLeastBehind;
 }
 
 // Scores below what 32 bits hold are -inf and weigh nothing.  Where a head has no others yet its maximum is -inf, which exponents do not refer to,
@@ -106,25 +76,16 @@ template <typename T, int D, int G> struct Form {
 
 // Where a group of 16 rows lies: its first and its second eight, in rows of K and V; and whether all 16 are seen.  Wave-uniform.
 struct Place { size_t a, b; int t0; bool all; };
-__device__ __forceinline__ bool all_seen(const Seen& s, int t0) { return t0 + kGroup <= s.L && (t0 >= s.lo || t0 + kGroup <= s.f); }
-__device__ __forceinline__ bool all_seen(const SeenBehind& s, int t0) { return t0 + kGroup <= s.L && (t0 >= s.lo || (t0 >= s.s0 && t0 + kGroup <= s.f)); }
-// A row of the group that is seen.
-__device__ __forceinline__ int one_seen(const Seen& s, int t0) { return t0 < s.f ? t0 : (t0 > s.lo ? t0 : s.lo); }
-__device__ __forceinline__ int one_seen(const SeenBehind& s, int t0) {
-  const int from = t0 < s.f ? s.s0 : s.lo;
-  return t0 > from ? t0 : from;
-}
-template <typename SEEN> __device__ __forceinline__ Place place_of(const CacheRows& r, int inst, const SEEN& s, int u) {
+__device__ __forceinline__ Place place_of(const CacheRows& r, int inst, const Seen& s, int u) {
   Place p;
   p.t0 = __builtin_amdgcn_readfirstlane(s.group(u) * kGroup);
   p.a = rows_at(r, inst, p.t0);
   p.b = r.lb == 3 && r.table != nullptr ? rows_at(r, inst, p.t0 + 8) : p.a + 8;
-  p.all = all_seen(s, p.t0);
+  p.all = p.t0 + kGroup <= s.L && (p.t0 >= s.lo || p.t0 + kGroup <= s.f);
   return p;
 }
 // Sends the rows of a group of K (or V) to LDS.
-template <typename F, bool IS_V, typename SEEN>
-__device__ __forceinline__ void send(const void* X, const Place& p, const SEEN& s, int lane, unsigned lds) {
+template <typename F, bool IS_V> __device__ __forceinline__ void send(const void* X, const Place& p, const Seen& s, int lane, unsigned lds) {
   constexpr unsigned row = F::PIECES * 16;
   if (p.all && p.b == p.a + 8) {
     const char* base = static_cast<const char*>(X) + p.a * row;
@@ -135,7 +96,7 @@ __device__ __forceinline__ void send(const void* X, const Place& p, const SEEN& 
     }
   } else {
     // Rows that are not seen are not read: another row of the group, which is, stands in for them.
-    const int other = one_seen(s, p.t0) - p.t0;
+    const int other = (p.t0 < s.f ? p.t0 : (p.t0 > s.lo ? p.t0 : s.lo)) - p.t0;
 #pragma unroll 1
     for (int l = 0; l < F::N; ++l) {
       const int x = l * kWave + lane, r = x / F::PIECES, place = x % F::PIECES;
@@ -264,26 +225,9 @@ __device__ __forceinline__ void join_pieces(const DecodeArgs& a, int inst, int w
   }
 }
 
-// ARGS: SharedDecodeArgs where beginnings were read for groups of instances: their rows are not seen here, and their pieces are joined to the outputs.
-template <typename T, int D, int G, bool ACC, typename ARGS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(ARGS a) {
-  constexpr bool BEHIND = std::is_same<ARGS, SharedDecodeArgs>::value;
+template <typename T, int D, int G, bool ACC>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T, D, G>::PER_CU))) void cache_decode_kernel(DecodeArgs a) {
   using F = Form<T, D, G>;
-  auto see = [&](int i) {
-    if constexpr (BEHIND) return seen_behind(a.r.len[i], a.b.start[i], a.r.t_cap, a.window, a.n_first);
-    else return seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first);
-  };
-  // What an instance counts in a share: its groups, and where a beginning may be in front of them, kBehindGroups for what an instance costs
-  // beside them.
-  constexpr int FRONT = BEHIND ? kBehindGroups : 0;
-  auto size_of = [&](int i) {
-    if constexpr (BEHIND) {
-      const int n = see(i).n;
-      return n > 0 || a.b.start[i] > 0 ? n + FRONT : 0;
-    } else {
-      return see(i).n;
-    }
-  };
   extern __shared__ __attribute__((aligned(16))) u32x4 s_rows[];          // [wave]: [buffer][K, V][TILE], queries; at the end outputs, [G][D]
   __shared__ __attribute__((aligned(16))) float s_p[kWaves][kGroup][G];
   __shared__ float s_ml[kWaves][G][2];
@@ -301,9 +245,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   int longest = 0;
 #pragma unroll 4
   for (int i = i_begin; i < i_end; ++i) {
-    const int n = size_of(i);
+    const int n = seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
     mine += (unsigned)n;
-    longest = n - FRONT > longest ? n - FRONT : longest;
+    longest = n > longest ? n : longest;
   }
   unsigned long long upto = mine;
 #pragma unroll
@@ -328,20 +272,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   // More instances than workgroups, all of them short: every wave takes whole instances, those that begin in its share, with no pieces and
   // nobody to wait for.
   const bool alone = __builtin_amdgcn_readfirstlane(a.r.n_inst > F::WGS && longest <= kShort);
-  const unsigned long long per = alone ? kWaves * ((groups + kWaves * F::WGS - 1) / (kWaves * F::WGS))
-                                       : (BEHIND ? share_behind(groups, F::WGS) : share_of(groups, F::WGS));
+  const unsigned long long per = alone ? kWaves * ((groups + kWaves * F::WGS - 1) / (kWaves * F::WGS)) : share_of(groups, F::WGS);
   const unsigned long long begin = (unsigned long long)blockIdx.x * per;
   const unsigned long long end = begin + per < groups ? begin + per : groups;
   // Empty instances have no share; their outputs are zero.
-  for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS) {
-    if (BEHIND ? size_of(i) == 0 : a.r.len[i] <= 0)
+  for (int i = blockIdx.x; i < a.r.n_inst; i += F::WGS)
+    if (a.r.len[i] <= 0)
       for (int x = tid; x < G * D; x += kThreads) a.out[(size_t)i * G * D + x] = 0.f;
-  }
   if (ACC && blockIdx.x == 0) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
       a.before[i] = at;
-      at += (unsigned)size_of(i);
+      at += (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
     }
     if (tid == kThreads - 1) a.before[a.r.n_inst] = alone ? kAlone : groups;
   }
@@ -350,7 +292,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   if (alone ? ahead < end && begin < ahead + mine : ahead <= begin && begin < ahead + mine) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
-      const unsigned n = (unsigned)size_of(i);
+      const unsigned n = (unsigned)seen_of(a.r.len[i], a.r.t_cap, a.window, a.n_first).n;
       if (alone) {
         if (n > 0 && at >= begin && at < end) {
           atomicMin(&s_first[(int)((at - begin) / share)], i);
@@ -379,32 +321,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
   const unsigned ring = lds_address(mine_rows);
   float* s_out = reinterpret_cast<float*>(s_rows);
   for (; alone ? left > 0 && inst < mine_to : left > 0; ++inst, from = 0) {
-    const auto s = see(inst);
-    const int size = BEHIND ? size_of(inst) : s.n;
-    if (size <= from) continue;                            // an empty instance
-    // Behind beginnings, what belongs to the workgroup that it begins in, whole.
-    const bool whole_here = BEHIND && !alone && (unsigned)size <= (per > kWholeGroups ? per : kWholeGroups);
-    if (whole_here && from > 0) {
-      left = left > (unsigned)(size - from) ? left - (unsigned)(size - from) : 0;
-      done += (unsigned)(size - from);
-      continue;
-    }
-    const int to = alone || whole_here ? size : (unsigned long long)(size - from) <= left ? size : from + (int)left;
-    if (!alone) left -= BEHIND && left < (unsigned)(to - from) ? left : (unsigned)(to - from);
-    const bool whole = from == 0 && to == size;
+    const Seen s = seen_of(a.r.len[inst], a.r.t_cap, a.window, a.n_first);
+    if (s.n <= from) continue;                             // an empty instance
+    const int to = alone ? s.n : (unsigned long long)(s.n - from) <= left ? s.n : from + (int)left;
+    if (!alone) left -= (unsigned)(to - from);
+    const bool whole = from == 0 && to == s.n;
     // The other pieces: of the workgroups from w0 on.  The last of them to be done joins them; with weights a second launch does.
     int w0 = blockIdx.x, parts = 1;
     if (!ACC && !whole) {
       if (from > 0) w0 = (int)((done - (unsigned)from) / per);
-      parts = (int)((done + (unsigned)(size - from) - 1) / per) - w0 + 1;
+      parts = (int)((done + (unsigned)(s.n - from) - 1) / per) - w0 + 1;
     }
     done += (unsigned)(to - from);
     unsigned long long* ticket = a.tickets + (size_t)w0 * kTicketStride;      // (an instance that begins in a workgroup and does not end there: one at most)
 
     // This wave's groups are from + wave, from + wave + 4, ...; two of them are on their way to LDS while one is worked off.
-    const int g0 = !BEHIND ? from : (from > FRONT ? from - FRONT : 0), g1 = !BEHIND ? to : (to > FRONT ? to - FRONT : 0);
-    const int mine_n = alone ? s.n : (g1 - g0 > wave ? (g1 - g0 - wave + kWaves - 1) / kWaves : 0);
-    const int u0 = alone ? 0 : g0 + wave;
+    const int mine_n = alone ? s.n : (to - from > wave ? (to - from - wave + kWaves - 1) / kWaves : 0);
+    const int u0 = alone ? 0 : from + wave;
     Place next[2];                                         // of the groups behind the ones that were sent for
     if (mine_n > 0) {
 #pragma unroll
@@ -437,48 +370,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(Form<T
     for (int h = 0; h < G; ++h)
 #pragma unroll
       for (int e = 0; e < F::E; ++e) o[h][e] = 0.f;
-    if constexpr (BEHIND) {
-      // The pieces of the beginning are where the first piece of an instance starts from: they are joined while the first rows are on their way.
-      // The lanes that have a row of V at a time take a piece at a time, those of all waves in turn.
-      const int2 ahead = from == 0 ? ahead_of(a.b, inst, 0) : make_int2(0, 0);
-      if (ahead.y > 0) {
-        const int every = alone ? F::RPL : F::RPL * kWaves;
-        const int first = (alone ? 0 : wave * F::RPL) + lane / F::PIECES;
-        const float* ml = a.b.ml + (size_t)ahead.x * 2;
-        float top[G];
-#pragma unroll
-        for (int h = 0; h < G; ++h) top[h] = -INFINITY;
-        for (int p = lane; p < ahead.y; p += kWave)
-#pragma unroll
-          for (int h = 0; h < G; ++h) top[h] = fmaxf(top[h], ml[((size_t)kPrefillRows * p + h) * 2]);
-#pragma unroll
-        for (int h = 0; h < G; ++h) {
-          top[h] = wave_max(top[h]);
-          m = head % G == h ? top[h] : m;
-        }
-#pragma unroll 2
-        for (int p = first; p < ahead.y; p += every)
-#pragma unroll
-          for (int h = 0; h < G; ++h) {
-            const size_t x = (size_t)kPrefillRows * p + h;
-            const float f = exp2_fast(ml[x * 2] - reference(top[h]));
-            const float* from_o = a.b.o + ((size_t)ahead.x + x) * D + lane % F::PIECES * F::E;
-#pragma unroll
-            for (int e = 0; e < F::E; e += 4) {
-              const float4v y = *reinterpret_cast<const float4v*>(from_o + e);
-#pragma unroll
-              for (int w = 0; w < 4; ++w) o[h][e + w] += f * y[w];
-            }
-          }
-        // The sums: lane (head, kg) every fourth of the wave's pieces.
-        const int mine = alone ? kg : wave * 4 + kg, all_lanes = alone ? 4 : 4 * kWaves;
-        if (head < G)
-          for (int p = mine; p < ahead.y; p += all_lanes) {
-            const float* x = ml + ((size_t)kPrefillRows * p + head) * 2;
-            sum += exp2_fast(x[0] - reference(m)) * x[1];
-          }
-      }
-    }
 
     for (int it = 0; it < mine_n; ++it) {
       const Place here = next[0];
@@ -677,32 +568,25 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(DecodeArgs a, int 
 
 template <typename T, int D, int G> hipError_t run(const DecodeArgs& a, hipStream_t st) {
   using F = Form<T, D, G>;
-  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true, DecodeArgs><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
-  else cache_decode_kernel<T, D, G, false, DecodeArgs><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
+  if (a.acc != nullptr) cache_decode_kernel<T, D, G, true><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
+  else cache_decode_kernel<T, D, G, false><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.acc == nullptr) return e;
   const unsigned columns = (unsigned)((a.r.t_cap + 4 * kThreads - 1) / (4 * kThreads));
   cache_join_kernel<G, D><<<dim3(1 + columns, a.r.n_inst), kThreads, join_bytes(G, D), st>>>(a, F::WGS);
   return hipGetLastError();
 }
-template <typename T, int D, int G> hipError_t run(const SharedDecodeArgs& a, hipStream_t st) {
-  using F = Form<T, D, G>;
-  cache_decode_kernel<T, D, G, false, SharedDecodeArgs><<<F::WGS, kThreads, F::BUFFERS, st>>>(a);
-  return hipGetLastError();
-}
-template <typename T, int D, typename ARGS> hipError_t run_g(int g, const ARGS& a, hipStream_t st) {
+template <typename T, int D> hipError_t run_g(int g, const DecodeArgs& a, hipStream_t st) {
   return g == 1 ? run<T, D, 1>(a, st) : g == 2 ? run<T, D, 2>(a, st) : g == 4 ? run<T, D, 4>(a, st) : run<T, D, 8>(a, st);
 }
 
 }  // namespace
 
-template <typename ARGS> static hipError_t launch(const Shape& s, const ARGS& args, hipStream_t st) {
-  ARGS a = args;
+hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& args, hipStream_t st) {
+  DecodeArgs a = args;
   a.nonce = new_nonce(kTicketBits);
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s.g, a, st) : run_g<bf16_t, 64>(s.g, a, st);
   return s.d == 128 ? run_g<float, 128>(s.g, a, st) : run_g<float, 64>(s.g, a, st);
 }
-hipError_t launch_cache_decode(const Shape& s, const DecodeArgs& args, hipStream_t st) { return launch(s, args, st); }
-hipError_t launch_cache_decode_shared(const Shape& s, const SharedDecodeArgs& args, hipStream_t st) { return launch(s, args, st); }
 
 }  // namespace ap

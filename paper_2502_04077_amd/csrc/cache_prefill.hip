@@ -16,7 +16,6 @@
 // this one's exponentials, three waves a SIMD with tiles of 32 rows, 256 rows a workgroup, a higher priority for the matrix phases.
 // In fp32 (4000 tokens, 8 instances) 1125 us, 117 TFLOP/s, where a large library product reaches 154.
 #include "cache_tiles.h"
-#include "share_body.h"
 
 namespace ap {
 namespace {
@@ -33,7 +32,7 @@ struct Span {
   __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
 };
 template <int TT, int G>
-__device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, int q_cap, int window, int n_first, int inst, int row0, int rows, int s0) {
+__device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, int q_cap, int window, int n_first, int inst, int row0, int rows) {
   Span s;
   s.L = clamped(r.len[inst], 0, r.t_cap);
   s.n = n_q == nullptr ? q_cap : clamped(n_q[inst], 0, q_cap);
@@ -44,11 +43,6 @@ __device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, 
   if (last <= row0) s.p1 = -1;
   s.lo0 = window > 0 && s.p0 >= window ? s.p0 - window + 1 : 0;
   s.f = n_first < s.lo0 ? n_first : s.lo0;
-  if (s0 > 0) {                                            // rows in front of s0 are not seen
-    if (s.f <= s0) s.f = 0;
-    if (s.lo0 < s0) s.lo0 = s0;
-    if (s.p1 < s.lo0) s.p1 = s.f - 1;
-  }
   if (s.p1 < 0) { s.tiles = s.ts = s.tb = 0; return s; }
   s.ts = (s.f + TT - 1) / TT;
   s.tb = s.lo0 / TT > s.ts ? s.lo0 / TT : s.ts;
@@ -69,19 +63,14 @@ __device__ __forceinline__ Work work_of(unsigned b, int tiles, int n_inst) {
   return {(int)(whole + x % rest), (int)(x / rest)};
 }
 
-// ARGS: SharedPrefillArgs where beginnings were read for groups of instances: their rows are not seen here, and the sums of the others are left
-// to be joined with theirs.
-template <typename T, int D, int G, bool STAT, typename ARGS>
-__global__ __launch_bounds__(kThreads) void cache_prefill_kernel(ARGS a) {
-  constexpr bool BEHIND = std::is_same<ARGS, SharedPrefillArgs>::value;
+template <typename T, int D, int G, bool STAT>
+__global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
   using F = Form<T, D>;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
   const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kPrefillRows;            // the longest ones first
-  int s0 = 0;
-  if constexpr (BEHIND) s0 = a.b.start[inst];
-  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kPrefillRows, s0);
+  const Span s = span_of<F::TT, G>(a.r, a.n_q, a.q_cap, a.window, a.n_first, inst, row0, kPrefillRows);
   const int rows = s.n * G;                                // of q
   if (row0 >= rows) return;
 
@@ -134,16 +123,14 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(ARGS a) {
 #pragma unroll
     for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
     // Every row of the tile is seen by every query of it, or the scores of those that are not become -inf.
-    const bool all = t0 + F::TT - 1 <= s.p0 && (!BEHIND || t0 >= s0) && (a.window <= 0 || t0 > s.p1 - a.window || t0 + F::TT <= a.n_first);
+    const bool all = t0 + F::TT - 1 <= s.p0 && (a.window <= 0 || t0 > s.p1 - a.window || t0 + F::TT <= a.n_first);
     if (!all) {
 #pragma unroll
       for (int b = 0; b < F::TB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = t0 + 32 * b + reg_row(i, hb);
-          bool hidden = (j > p) | ((j < lo) & (j >= a.n_first));
-          if (BEHIND) hidden |= j < s0;
-          c[b][i] = hidden ? -INFINITY : c[b][i];
+          c[b][i] = (j > p) | ((j < lo) & (j >= a.n_first)) ? -INFINITY : c[b][i];
         }
     }
     float top = c[0][0];
@@ -228,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(ARGS a) {
 
   sum = sum32(sum);
   if (row >= rows) return;
-  if (BEHIND || a.splits > 1) {                            // (whatever its share: the join goes by the maximum)
+  if (a.splits > 1) {                                      // (whatever its share: the join goes by the maximum)
     const size_t at = ((size_t)blockIdx.y * a.r.n_inst + inst) * a.q_cap * G + row;
     if (hb == 0) {
       a.part_ml[at * 2] = m;
@@ -314,52 +301,6 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_join_kernel(PrefillArg
     float* st = a.stat + ((size_t)inst * a.stat_rows + row) * 2;
     st[0] = use;
     st[1] = inv;
-  }
-}
-
-// The same with the pieces of the beginnings.
-template <typename T, int D, int G>
-__global__ __launch_bounds__(kThreads) void cache_prefill_behind_kernel(SharedPrefillArgs a) {
-  constexpr int E = D / 64;                                // outputs of a lane
-  const int inst = blockIdx.y, lane = threadIdx.x & 63, row = blockIdx.x * kWaves + (threadIdx.x >> 6);
-  const int nq = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
-  if (row >= nq * G) return;
-  const size_t at = (size_t)inst * a.q_cap * G + row, step = (size_t)a.r.n_inst * a.q_cap * G;
-  const int2 ahead = ahead_of(a.b, inst, row);
-  const float m = lane < a.splits ? a.part_ml[(lane * step + at) * 2] : -INFINITY, l = lane < a.splits ? a.part_ml[(lane * step + at) * 2 + 1] : 0.f;
-  float top = m;
-  for (int p = lane; p < ahead.y; p += 64) top = fmaxf(top, a.b.ml[(ahead.x + (size_t)kPrefillRows * p) * 2]);
-  top = wave_max(top);
-  const float use = top == -INFINITY ? 0.f : top, f = exp2_fast(m - use);
-  float sum = f * l;
-  for (int p = lane; p < ahead.y; p += 64) {
-    const float* ml = a.b.ml + (ahead.x + (size_t)kPrefillRows * p) * 2;
-    sum += exp2_fast(ml[0] - use) * ml[1];
-  }
-  sum = wave_sum(sum);
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  float o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < ahead.y; ++p) {
-    const size_t x = ahead.x + (size_t)kPrefillRows * p;
-    const float w = exp2_fast(a.b.ml[x * 2] - use);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += w * a.b.o[x * D + lane * E + e];
-  }
-#pragma unroll 4
-  for (int x = 0; x < a.splits; ++x) {
-    const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x));
-    if (!(w > 0.f || w != w)) continue;                    // (a split without tiles has left no sums)
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += w * a.part_o[(x * step + at) * D + lane * E + e];
-  }
-  T* out = static_cast<T*>(a.out) + at * D + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if constexpr (sizeof(T) == 2) out[e].bits = __builtin_bit_cast(uint16_t, (__bf16)(o[e] * inv));
-    else out[e] = o[e] * inv;
   }
 }
 
@@ -550,8 +491,8 @@ template <typename T, int D, int G> hipError_t run(const Shape& s, const Prefill
   // 15.2 us and 15.3; 4 tokens behind 32 thousand rows, one instance 21.7 and 21.3, four 24.3 and 23.0.)
   const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
   const size_t lds = (size_t)2 * 2 * Form<T, D>::TILE * 16;
-  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false, PrefillArgs><<<grid, kThreads, lds, st>>>(a);
-  else cache_prefill_kernel<T, D, G, true, PrefillArgs><<<grid, kThreads, lds, st>>>(a);
+  if (a.acc == nullptr) cache_prefill_kernel<T, D, G, false><<<grid, kThreads, lds, st>>>(a);
+  else cache_prefill_kernel<T, D, G, true><<<grid, kThreads, lds, st>>>(a);
   if (a.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -567,22 +508,14 @@ template <typename T, int D, int G> hipError_t run(const Shape& s, const Prefill
   cache_weights_add_kernel<<<dim3(columns.x, columns.y), kPrefillRows, 0, st>>>(a);
   return hipGetLastError();
 }
-template <typename T, int D, int G> hipError_t run(const Shape&, const SharedPrefillArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.tiles * (unsigned)a.r.n_inst, a.splits);
-  cache_prefill_kernel<T, D, G, false, SharedPrefillArgs><<<grid, kThreads, (size_t)2 * 2 * Form<T, D>::TILE * 16, st>>>(a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  cache_prefill_behind_kernel<T, D, G><<<dim3((a.q_cap * G + kWaves - 1) / kWaves, a.r.n_inst), kThreads, 0, st>>>(a);
-  return hipGetLastError();
-}
-template <typename T, int D, typename ARGS> hipError_t run_g(const Shape& s, const ARGS& a, hipStream_t st) {
+template <typename T, int D> hipError_t run_g(const Shape& s, const PrefillArgs& a, hipStream_t st) {
   return s.g == 1 ? run<T, D, 1>(s, a, st) : s.g == 2 ? run<T, D, 2>(s, a, st) : s.g == 4 ? run<T, D, 4>(s, a, st) : run<T, D, 8>(s, a, st);
 }
 
 }  // namespace
 
-template <typename ARGS> static hipError_t launch(const Shape& s, const ARGS& args, hipStream_t st) {
-  ARGS a = args;
+hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) {
+  PrefillArgs a = args;
   a.stat_rows = cache_stat_rows(s, a.q_cap);
   a.tiles = (int)(((long long)a.q_cap * s.g + kPrefillRows - 1) / kPrefillRows);
   a.splits = cache_splits(s, a.q_cap, a.window, a.n_first);
@@ -590,7 +523,5 @@ template <typename ARGS> static hipError_t launch(const Shape& s, const ARGS& ar
   if (s.kv_dtype == AP_BF16) return s.d == 128 ? run_g<bf16_t, 128>(s, a, st) : run_g<bf16_t, 64>(s, a, st);
   return s.d == 128 ? run_g<float, 128>(s, a, st) : run_g<float, 64>(s, a, st);
 }
-hipError_t launch_cache_prefill(const Shape& s, const PrefillArgs& args, hipStream_t st) { return launch(s, args, st); }
-hipError_t launch_cache_prefill_shared(const Shape& s, const SharedPrefillArgs& args, hipStream_t st) { return launch(s, args, st); }
 
 }  // namespace ap

@@ -1,10 +1,17 @@
-// Attention of groups of instances that begin with the same rows, over that beginning: it is read once for all of them.
+// Attention of one new token, or of few, per instance over a cache whose first rows the instance has in common with others.
 //
-// The members' queries are the rows of one product.  With S rows in common, for every row x of q of the group, at position p of its cache,
+// Rows in common are read once for all of a group: the members' queries are the rows of one product.  What lies behind them is every
+// instance's own.  With a source of cache rows j (a group's beginning, or an instance's rows behind it), for every row x of q that belongs to it,
+// at position p of its cache,
 //
-//   s_xj = q_x . K_j / sqrt(d),  m_x = max_j s_xj,  l_x = sum_j exp(s_xj - m_x),  o_x = sum_j exp(s_xj - m_x) V_j,   j < S that p sees;
+//   s_xj = q_x . K_j / sqrt(d),  m_x = max_j s_xj,  l_x = sum_j exp(s_xj - m_x),  o_x = sum_j exp(s_xj - m_x) V_j,   over the rows j that p sees;
 //
-// what lies behind the beginning is every instance's own (cache_decode.hip, cache_prefill.hip), and (m, l, o) of both are joined there.
+// out_x = sum over its sources of exp(m_x - m) o_x / sum of exp(m_x - m) l_x, for m the largest m_x.
+//
+// A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32).  All of these products, of all sources one after the other,
+// are cut into equal shares, a workgroup each, by what they cost; a workgroup leaves (m, l, o) of every piece that it has, and a second
+// launch joins them.  Where there are many rows of q, a wave has 32 of them and all rows of a tile of K and V; up to 16, which is memory-bound, all
+// waves have the same rows of q and a part of the tile each.
 #include "cache_tiles.h"
 #include "share_internal.h"
 
@@ -79,48 +86,208 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
   if (lead == i) plan.groups[groups] = make_int4(i, ahead, count, inst[i].w);
 }
 
-// ---------------------------------------------------------------------------------------------------------------- the beginnings
-// What a group's queries see of its beginning.
-struct Begin {
-  int lead, first, count, S;
-  int p1, lo0, f;        // rows [0, f) and [lo0, p1], f <= lo0, each of which may be empty
-  int tiles, ts, tb;     // tiles of TT rows: ts from 0 on, the others from tb
-  __device__ __forceinline__ int tile(int u) const { return u < ts ? u : tb + (u - ts); }
-};
-// inst: any member's line of the plan.  Called by a thread.
-template <int TT> __device__ __forceinline__ Begin begin_of(const BeginArgs& a, int4 inst) {
-  Begin s;
-  s.lead = inst.x; s.first = inst.y; s.count = inst.z;
-  const bool several = inst.z > 1 && (unsigned)inst.x < (unsigned)a.r.n_inst && inst.y >= 0 && inst.z <= a.r.n_inst - inst.y;
-  const int L = several ? clamped(a.r.len[s.lead], 0, a.r.t_cap) : 0;
-  s.S = inst.w < L ? inst.w : L;
-  s.lo0 = 0;
-  s.p1 = s.S - 1;
-  if (s.S > 0 && a.window > 0) {
-    int p = 0x7fffffff;                                    // the lowest position of a query
-    for (int x = 0; x < s.count; ++x) {
-      const int i = a.b.plan.member[s.first + x];
-      const int n = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[i], 0, a.q_cap);
-      const int base = clamped(a.r.len[i], 0, a.r.t_cap) - n;
-      if (n > 0 && base < p) p = base;
-    }
-    s.lo0 = p >= a.window ? p - a.window + 1 : 0;
+// ---------------------------------------------------------------------------------------------------------------- sources
+constexpr int kNarrowRows = 16;     // rows of q up to which the waves share them
+// What a tile of the cache counts with more rows of q (with fewer: 1), and what a tile of rows of q counts beside its tiles of the cache.
+constexpr int kWide = 2, kFront = 2;
+// Least share of a workgroup; a tile of rows of q that counts no more than kWhole, or than a share, is not cut.
+constexpr int kLeastShare = 4, kWhole = 8;
+
+// Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
+struct Source {
+  int inst, first, count;
+  int x0, rows;          // number of its first row of q among all sources', and how many
+  int a0, a1, p1, lo0, f;   // rows [a0, f) and [lo0, p1] are seen by one of them at least, f <= lo0; each may be empty
+  int ta, ts, tb, tiles; // tiles of TT rows: ts from ta on, the others from tb
+  __device__ __forceinline__ int tile(int u) const { return u < ts ? ta + u : tb + (u - ts); }
+  __device__ __forceinline__ bool row(int j) const { return j >= a0 && j <= p1 && (j >= lo0 || j < f); }
+  __device__ __forceinline__ int q_tiles() const { return (rows + kPrefillRows - 1) / kPrefillRows; }
+  // What a tile of rows of q counts: each but the last, and the last.
+  __device__ __forceinline__ int narrow(int t) const { return rows - t * kPrefillRows <= kNarrowRows; }
+  __device__ __forceinline__ unsigned size(int t) const { return tiles == 0 ? 0u : kFront + (unsigned)tiles * (narrow(t) ? 1 : kWide); }
+  __device__ __forceinline__ unsigned long long all() const {
+    return tiles == 0 ? 0ull : (unsigned long long)(q_tiles() - 1) * size(0) + size(q_tiles() - 1);
   }
+};
+__device__ __forceinline__ int queries(const SharedArgs& a, int i) { return a.n_q == nullptr ? a.q_cap : clamped(a.n_q[i], 0, a.q_cap); }
+// What queries from position p_min on see of rows [a0, a1).
+template <int TT> __device__ __forceinline__ void see(const SharedArgs& a, Source& s, int a0, int a1, int p_min) {
+  s.a0 = a0;
+  s.a1 = a1;
+  s.p1 = a1 - 1;
+  s.lo0 = a.window > 0 && p_min >= a.window ? p_min - a.window + 1 : 0;
   s.f = a.n_first < s.lo0 ? a.n_first : s.lo0;
-  if (s.f > s.S) s.f = s.S;
-  if (s.lo0 >= s.S) {                                      // the first rows alone
+  if (s.f > a1) s.f = a1;
+  if (s.f <= a0) s.f = 0;
+  if (s.lo0 < a0) s.lo0 = a0;
+  if (s.lo0 > s.p1) {                                      // the first rows alone
     s.lo0 = s.f;
     s.p1 = s.f - 1;
   }
-  s.ts = (s.f + TT - 1) / TT;
-  s.tb = s.lo0 / TT > s.ts ? s.lo0 / TT : s.ts;
-  s.tiles = s.p1 < 0 ? 0 : s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
+  s.ta = a0 / TT;
+  const int end = (s.f + TT - 1) / TT;
+  s.ts = s.f > 0 ? end - s.ta : 0;
+  s.tb = s.lo0 / TT;
+  if (s.ts > 0 && s.tb < end) s.tb = end;
+  s.tiles = a0 >= a1 || s.p1 < 0 || s.rows == 0 ? 0 : s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
+}
+// A group's beginning, by any member's line of the plan; without tiles where there is none, or nobody sees it.
+template <int TT> __device__ __forceinline__ Source beginning_of(const SharedArgs& a, int4 line) {
+  Source s;
+  const int n = a.r.n_inst;
+  const bool several = line.z > 1 && (unsigned)line.x < (unsigned)n && line.y >= 0 && line.z <= n - line.y;
+  s.inst = line.x; s.first = line.y; s.count = line.z;
+  s.rows = several ? line.z * a.rows : 0;
+  s.x0 = line.y * a.rows;
+  const int L = several ? clamped(a.r.len[line.x], 0, a.r.t_cap) : 0, S = line.w < L ? line.w : L;
+  int p = 0x7fffffff;                                      // the lowest position of a query
+  if (S > 0 && a.window > 0)
+    for (int x = 0; x < s.count; ++x) {
+      const int i = clamped(a.plan.member[s.first + x], 0, n - 1), m = queries(a, i), base = clamped(a.r.len[i], 0, a.r.t_cap) - m;
+      if (m > 0 && base < p) p = base;
+    }
+  see<TT>(a, s, 0, S > 0 ? S : 0, p);
   return s;
 }
-__device__ __forceinline__ unsigned long long units_of(const BeginArgs& a, const Begin& s) {
-  return (unsigned long long)s.tiles * (unsigned)((s.count * a.b.rows + kPrefillRows - 1) / kPrefillRows);
+// An instance's rows from `start` on.
+template <int TT> __device__ __forceinline__ Source behind_of(const SharedArgs& a, int i, int start) {
+  Source s;
+  const int L = clamped(a.r.len[i], 0, a.r.t_cap), m = queries(a, i);
+  s.inst = i; s.first = 0; s.count = 0;
+  s.rows = m * a.g;
+  s.x0 = (a.r.n_inst + i) * a.rows;
+  see<TT>(a, s, start, L, L - m);
+  return s;
 }
-constexpr int kLeastUnits = 2;      // of a workgroup
+// Sources in their order: the groups', then the instances'.
+template <int TT> __device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int x) {
+  if (x < groups) return beginning_of<TT>(a, a.plan.groups[x]);
+  const Source s = beginning_of<TT>(a, a.plan.inst[x - groups]);
+  return behind_of<TT>(a, x - groups, s.tiles > 0 ? s.a1 : 0);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- tiles of the cache
+// As Run in cache_tiles.h, for the rows that a source sees.
+template <typename F> __device__ __forceinline__ Run run_of(const SharedArgs& a, const TablePages& pages, const Source& s, int t0, int wave) {
+  constexpr size_t bytes = F::PIECES * 16;
+  Run x;
+  x.j0 = t0 + wave * F::RW;
+  x.all = x.j0 >= s.a0 && x.j0 + F::RW - 1 <= s.p1 && (x.j0 >= s.lo0 || x.j0 + F::RW <= s.f);
+  const int from = x.j0 < s.f ? s.a0 : s.lo0, alt = x.j0 > from ? x.j0 : from;          // a row that is seen
+  x.alt = alt < s.p1 ? alt : s.p1;
+  const size_t at = pages.at(x.j0);
+  x.k = static_cast<const char*>(a.K) + at * bytes;
+  x.v = static_cast<const char*>(a.V) + at * bytes;
+  x.second = F::RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(x.j0 + 8) - at) - 8) * (long long)bytes : 0;
+  return x;
+}
+template <typename F, bool IS_V>
+__device__ __forceinline__ void send_tile(const SharedArgs& a, const Run& run, const Source& s, int wave, unsigned lds) {
+  constexpr unsigned bytes = F::PIECES * 16;
+  const int lane = threadIdx.x & 63;
+  const unsigned to = lds + wave * F::LOADS * 1024;
+  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };                   // of the run
+  auto piece = [&](int l) {
+    const int place = lane % F::PIECES;
+    return IS_V ? F::v_place(row(l), place) : F::k_place(wave * F::RW + row(l), place);
+  };
+  if (run.all) {
+#pragma unroll
+    for (int l = 0; l < F::LOADS; ++l)
+      to_lds<false>((IS_V ? run.v : run.k) + (l >= F::LOADS / 2 ? run.second : 0), row(l) * bytes + piece(l) * 16, to + l * 1024);
+  } else {
+#pragma unroll 1
+    for (int l = 0; l < F::LOADS; ++l) {
+      const int j = s.row(run.j0 + row(l)) ? run.j0 + row(l) : run.alt;
+      to_lds_from(static_cast<const char*>(IS_V ? a.V : a.K) + row_at(a.r, s.inst, j) * bytes + piece(l) * 16, to + l * 1024);
+    }
+  }
+}
+// A piece's tiles of the cache, one after the other: tile u is worked off by `work(t0, K, V)` while the next is on its way.  All threads of the workgroup.
+template <typename F, typename WORK>
+__device__ __forceinline__ void over_tiles(const SharedArgs& a, const Source& s, int u_begin, int u_end, const u32x4* s_tiles, WORK work) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned buffers = lds_address(s_tiles);
+  const TablePages pages = pages_of(a.r, s.inst);
+  Run next = run_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
+  auto send = [&](int u) {                                 // tile u, whose rows are those of `next`
+    const unsigned to = buffers + (u % 2) * 2 * F::TILE * 16;
+    send_tile<F, false>(a, next, s, wave, to);
+    send_tile<F, true>(a, next, s, wave, to + F::TILE * 16);
+    next = run_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);         // a tile ahead: the table's latency
+  };
+  send(u_begin);
+  for (int u = u_begin; u < u_end; ++u) {
+    // This tile has landed; everybody is done with the buffer that is filled next.
+    landed<0>();
+    lds_read();
+    __builtin_amdgcn_s_barrier();
+    if (u + 1 < u_end) send(u + 1);
+    const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
+    work(s.tile(u) * F::TT, Kt, Kt + F::TILE);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- pieces
+// A lane's row of q: row x of the source.
+struct Query {
+  int inst, p, lo;       // whose; its position, and the first row that its window shows
+  bool real;             // or a row that is none: computed as another one, and not stored
+  size_t row;            // of q
+};
+__device__ __forceinline__ Query query_of(const SharedArgs& a, const Source& s, int x) {
+  Query q;
+  int rest = x;
+  q.real = x < s.rows;
+  if (s.count > 0) {
+    const int of = x / a.rows;
+    rest = x % a.rows;
+    q.inst = clamped(a.plan.member[s.first + (of < s.count ? of : 0)], 0, a.r.n_inst - 1);
+  } else {
+    q.inst = s.inst;
+  }
+  const int m = queries(a, q.inst);
+  q.real = q.real && rest < m * a.g;
+  if (!q.real) rest = 0;
+  q.p = clamped(a.r.len[q.inst], 0, a.r.t_cap) - m + rest / a.g;
+  q.lo = a.window > 0 && q.p >= a.window ? q.p - a.window + 1 : 0;
+  q.row = (size_t)q.inst * a.rows + rest;
+  return q;
+}
+__device__ __forceinline__ bool hidden(const SharedArgs& a, const Source& s, const Query& q, int j) {
+  return (j < s.a0) | (j >= s.a1) | (j > q.p) | ((j < q.lo) & (j >= a.n_first));
+}
+// Whether every row of tile t0 is seen from all positions p_min .. p_max.
+template <int TT> __device__ __forceinline__ bool all_seen(const SharedArgs& a, const Source& s, int t0, int p_min, int p_max) {
+  return t0 >= s.a0 && t0 + TT <= s.a1 && t0 + TT - 1 <= p_min && (a.window <= 0 || t0 > p_max - a.window || t0 + TT <= a.n_first);
+}
+// The lowest and the highest position of the real ones of N lanes.
+template <int N> __device__ __forceinline__ void positions(const Query& q, int* p_min, int* p_max) {
+  int lo = q.real ? q.p : 0x7fffffff, hi = q.real ? q.p : -1;
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) {
+    const int y = __shfl_xor(lo, o, 64), z = __shfl_xor(hi, o, 64);
+    lo = y < lo ? y : lo;
+    hi = z > hi ? z : hi;
+  }
+  *p_min = __builtin_amdgcn_readfirstlane(lo);
+  *p_max = __builtin_amdgcn_readfirstlane(hi);
+}
+// A pair of probabilities as PARTS pairs of bf16 that add up to them: three have all of a probability's 24 bits.
+template <int PARTS> __device__ __forceinline__ void in_parts(float x, float y, unsigned (&out)[PARTS]) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int w = 0; w < PARTS; ++w) {
+    bf16x2 z;
+    z[0] = (__bf16)x;
+    z[1] = (__bf16)y;
+    out[w] = __builtin_bit_cast(unsigned, z);
+    if (w + 1 < PARTS) {
+      x -= __uint_as_float(out[w] << 16);
+      y -= __uint_as_float(out[w] & 0xffff0000u);
+    }
+  }
+}
 
 // The product of product(), summed in four parts: fp32 sums of fewer terms round less.
 template <int D> __device__ __forceinline__ float16v product_in_parts(const u32x4* X, const u32x4 (&b)[Form<float, D>::KS]) {
@@ -143,20 +310,291 @@ template <int D> __device__ __forceinline__ float16v product_in_parts(const u32x
   return c[0];
 }
 
-// A workgroup's share of the units, piece by piece: a tile of rows of q, 32 a wave, over consecutive tiles of the beginning.
+// Tile t of a source's rows of q, 32 a wave, over its tiles [u_begin, u_end) of the cache.  slot: of the tile's first row.
 template <typename T, int D, bool EXACT>
-__global__ __launch_bounds__(kThreads) void cache_beginnings_kernel(BeginArgs a, int g) {
+__device__ __forceinline__ void wide_piece(const SharedArgs& a, const Source& s, int t, int u_begin, int u_end, size_t slot, const u32x4* s_tiles) {
+  using F = Form<T, D>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
+  const Query q = query_of(a, s, t * kPrefillRows + wave * 32 + n);
+  int p_min, p_max;
+  positions<32>(q, &p_min, &p_max);
+  const bool idle = p_max < 0;                             // a wave without rows of q (or whose rows see nothing)
+  u32x4 qf[F::KS];
+#pragma unroll
+  for (int k = 0; k < F::KS; ++k) qf[k] = static_cast<const u32x4*>(a.q)[q.row * F::PIECES + 2 * k + hb];
+  float16v o[F::DB];
+#pragma unroll
+  for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+  float m = -INFINITY, sum = 0.f;                          // the sum over this lane's half of the cache rows
+  const float scale = kLog2E / sqrtf((float)D);
+  // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
+#pragma unroll
+  for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
+  over_tiles<F>(a, s, u_begin, u_end, s_tiles, [&](int t0, const u32x4* Kt, const u32x4* Vt) {
+    if (idle) return;
+    float16v c[F::TB];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
+    } else {
+      c[0] = product_in_parts<D>(Kt, qf);
+    }
+    // Scores that a query does not see become -inf.
+    if (!all_seen<F::TT>(a, s, t0, p_min, p_max)) {
+#pragma unroll
+      for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[b][i] = hidden(a, s, q, t0 + 32 * b + reg_row(i, hb)) ? -INFINITY : c[b][i];
+    }
+    float top = c[0][0];
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, c[b][i]);
+    top = max32(top);
+    // The reference is a whole number in units of log2 (a change of it rounds nothing).  Exponents refer to 0 as long as nothing is seen, and where
+    // it is far, as the scores are brought near then.
+    const float ref = fmaxf(m, ceilf(top * scale));
+    const bool far = is_far(ref);
+    if (__any((ref != m) | far)) {
+      const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
+      sum *= shrink;
+#pragma unroll
+      for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
+      m = ref;
+      if (__any(far && m != -INFINITY)) {
+#pragma unroll
+        for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) c[b][i] = far && m != -INFINITY ? brought_near(c[b][i], scale, m) : c[b][i];
+      }
+    }
+    const float use = far ? 0.f : ref;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};                  // (sums of a tile first: long caches lose fewer digits so)
+#pragma unroll
+    for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        c[b][i] = exp2_fast(__builtin_fmaf(c[b][i], scale, -use));
+        part[i & 3] += c[b][i];
+      }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    if constexpr (sizeof(T) == 2) {
+      // Probabilities are rounded to bf16, as in a prefill, where the output is rounded to it too; else (EXACT) they keep 24 bits.
+      constexpr int PARTS = EXACT ? 3 : 1;
+#pragma unroll
+      for (int k = 0; k < F::TT / 16; ++k) {
+        typedef unsigned u32x4p __attribute__((ext_vector_type(4)));
+        u32x4p pb[PARTS];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          unsigned two[PARTS];
+          in_parts<PARTS>(c[k / 2][8 * (k % 2) + 2 * e], c[k / 2][8 * (k % 2) + 2 * e + 1], two);
+#pragma unroll
+          for (int w = 0; w < PARTS; ++w) pb[w][e] = two[w];
+        }
+        // V^T of 16 cache rows: the transposing read gives lane (m, hb) column m of four rows; a lane of 16 points to the 8 bytes at
+        // row lane / 4, columns 4 (lane % 4).
+        const int i = lane & 15, r = 16 * k + 4 * hb + (i >> 2);
+#pragma unroll
+        for (int b = 0; b < F::DB; ++b) {
+          const int col = 32 * b + 16 * ((lane >> 4) & 1) + 4 * (i & 3), piece = col / 8;
+          bf16x8 va;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int rr = r + 8 * half;
+            const char* at = reinterpret_cast<const char*>(Vt + rr * F::PIECES + F::v_place(rr, piece)) + (col % 8) * 2;
+            const short4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+            const bf16x4 y = __builtin_bit_cast(bf16x4, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) va[4 * half + e] = y[e];
+          }
+#pragma unroll
+          for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, __builtin_bit_cast(bf16x8, pb[w]), o[b], 0, 0, 0);
+        }
+      }
+    } else {
+      const float* Vf = reinterpret_cast<const float*>(Vt);
+#pragma unroll
+      for (int b = 0; b < F::DB; ++b) {
+        float16v y;                                        // of this tile alone, as the sums
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          y = __builtin_amdgcn_mfma_f32_32x32x2f32(Vf[reg_row(i, hb) * D + 32 * b + n], c[0][i], y, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] += y[i];
+      }
+    }
+  });
+  sum = sum32(sum);
+  if (!q.real) return;
+  slot += wave * 32 + n;
+  if (hb == 0) {
+    a.ml[slot * 2] = m;
+    a.ml[slot * 2 + 1] = sum;
+  }
+#pragma unroll
+  for (int b = 0; b < F::DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      float4v y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = o[b][i + e];
+      *reinterpret_cast<float4v*>(a.o + slot * D + 32 * b + reg_row(i, hb)) = y;
+    }
+}
+
+// The same of up to 16 rows of q, which all waves have; a wave goes over 16 rows of each tile of the cache (fp32: two waves do), and their sums
+// are joined at the end.
+template <typename T, int D, bool EXACT>
+__device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& s, int t, int u_begin, int u_end, size_t slot, u32x4* s_tiles) {
+  using F = Form<T, D>;
+  constexpr int KS = F::PIECES / 4, DB = D / 16, ACTIVE = F::TT / 16;      // pieces of a row that a lane has; blocks of 16 dims; waves
+  static_assert(4 * F::TILE * 16 >= ACTIVE * (16 * D + 32) * 4, "the waves' sums");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
+  const Query q = query_of(a, s, t * kPrefillRows + n);
+  int p_min, p_max;
+  positions<16>(q, &p_min, &p_max);
+  u32x4 qf[KS];
+#pragma unroll
+  for (int l = 0; l < KS; ++l) qf[l] = static_cast<const u32x4*>(a.q)[q.row * F::PIECES + 4 * l + kg];
+  float4v o[DB];
+#pragma unroll
+  for (int b = 0; b < DB; ++b) o[b] = float4v{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, sum = 0.f;                          // the sum over this lane's rows
+  const float scale = kLog2E / sqrtf((float)D);
+#pragma unroll
+  for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[l]));
+  over_tiles<F>(a, s, u_begin, u_end, s_tiles, [&](int t0, const u32x4* Kt, const u32x4* Vt) {
+    if (wave >= ACTIVE) return;
+    // Rows j0 + 4 kg + r of the tile, of query n.  fp32 products go into four sums.
+    const int j0 = 16 * wave;
+    constexpr int SUMS = sizeof(T) == 2 ? 1 : 4;
+    float4v sums[SUMS];
+#pragma unroll
+    for (int x = 0; x < SUMS; ++x) sums[x] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int l = 0; l < KS; ++l) {
+      const u32x4 k = Kt[(j0 + n) * F::PIECES + F::k_place(j0 + n, 4 * l + kg)];
+      if constexpr (sizeof(T) == 2) {
+        sums[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), sums[0], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sums[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), sums[e], 0, 0, 0);
+      }
+    }
+    float4v c = sums[0];
+    if constexpr (SUMS == 4) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) c[r] = (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]);
+    }
+    if (!all_seen<F::TT>(a, s, t0, p_min, p_max)) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) c[r] = hidden(a, s, q, t0 + j0 + 4 * kg + r) ? -INFINITY : c[r];
+    }
+    float top = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
+    top = max32(max16(top));
+    const float ref = fmaxf(m, ceilf(top * scale));        // a whole number in units of log2, as above
+    if (__any(ref != m)) {
+      const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
+      sum *= shrink;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[b][r] *= shrink;
+      m = ref;
+    }
+    const float use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c[r] = exp2_of(c[r], scale, use);
+    sum += (c[0] + c[1]) + (c[2] + c[3]);
+    if constexpr (sizeof(T) == 2) {
+      constexpr int PARTS = EXACT ? 3 : 1;
+      typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+      short4v pb[PARTS];
+      unsigned two[2][PARTS];
+      in_parts<PARTS>(c[0], c[1], two[0]);
+      in_parts<PARTS>(c[2], c[3], two[1]);
+#pragma unroll
+      for (int w = 0; w < PARTS; ++w) pb[w] = __builtin_bit_cast(short4v, u32x2{two[0][w], two[1][w]});
+      const int r = j0 + 4 * kg + (n >> 2);
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const int col = 16 * b + 4 * (n & 3);
+        const char* at = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
+        const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+#pragma unroll
+        for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pb[w], o[b], 0, 0, 0);
+      }
+    } else {
+      const float* Vf = reinterpret_cast<const float*>(Vt);
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vf[(j0 + 4 * kg + r) * D + 16 * b + n], c[r], o[b], 0, 0, 0);
+    }
+  });
+  // The waves' sums: [wave][16][D], and their maxima and sums behind.
+  float* s_o = reinterpret_cast<float*>(s_tiles);
+  float* s_ml = s_o + ACTIVE * 16 * D;
+  sum = sum32(sum16(sum));
+  __syncthreads();                                         // everybody is done with the tiles
+  if (wave < ACTIVE) {
+#pragma unroll
+    for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(s_o + (wave * 16 + n) * D + 16 * b + 4 * kg) = o[b];
+    if (kg == 0) {
+      s_ml[(wave * 16 + n) * 2] = m;
+      s_ml[(wave * 16 + n) * 2 + 1] = sum;
+    }
+  }
+  __syncthreads();
+  const int rows = s.rows - t * kPrefillRows;
+  for (int x = tid; x < rows * (D / 4); x += kThreads) {
+    const int row = x / (D / 4), e = x % (D / 4) * 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < ACTIVE; ++w) top = fmaxf(top, s_ml[(w * 16 + row) * 2]);
+    const float use = top == -INFINITY ? 0.f : top;
+    float4v y = {0.f, 0.f, 0.f, 0.f};
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < ACTIVE; ++w) {
+      const float f = exp2_fast(s_ml[(w * 16 + row) * 2] - use);
+      all += f * s_ml[(w * 16 + row) * 2 + 1];
+      const float4v z = *reinterpret_cast<const float4v*>(s_o + (w * 16 + row) * D + e);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] += f * z[r];
+    }
+    *reinterpret_cast<float4v*>(a.o + (slot + row) * D + e) = y;
+    if (e == 0) {
+      a.ml[(slot + row) * 2] = top;
+      a.ml[(slot + row) * 2 + 1] = all;
+    }
+  }
+}
+
+// A workgroup's share of all products, piece by piece.
+template <typename T, int D, bool EXACT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
   __shared__ unsigned long long s_wave[kWaves], s_from;
   __shared__ int s_first;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-  // Where this workgroup's share begins: every thread sums the units of consecutive groups.
-  const int groups = clamped(*a.b.plan.count, 0, a.r.n_inst), chunk = (groups + kThreads - 1) / kThreads;
-  const int i_begin = tid * chunk < groups ? tid * chunk : groups, i_end = i_begin + chunk < groups ? i_begin + chunk : groups;
+  // Where this workgroup's share begins: every thread sums up consecutive sources.
+  const int groups = clamped(*a.plan.count, 0, a.r.n_inst), sources = groups + a.r.n_inst, chunk = (sources + kThreads - 1) / kThreads;
+  const int i_begin = tid * chunk < sources ? tid * chunk : sources, i_end = i_begin + chunk < sources ? i_begin + chunk : sources;
   unsigned long long mine = 0;
-  for (int i = i_begin; i < i_end; ++i) mine += units_of(a, begin_of<F::TT>(a, a.b.plan.groups[i]));
+  for (int i = i_begin; i < i_end; ++i) mine += source_of<F::TT>(a, groups, i).all();
   unsigned long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -165,231 +603,133 @@ __global__ __launch_bounds__(kThreads) void cache_beginnings_kernel(BeginArgs a,
   }
   if (lane == 63) s_wave[wave] = upto;
   __syncthreads();
-  unsigned long long units = 0, ahead = upto - mine;
+  unsigned long long all = 0, ahead = upto - mine;
   for (int w = 0; w < kWaves; ++w) {
     if (w < wave) ahead += s_wave[w];
-    units += s_wave[w];
+    all += s_wave[w];
   }
-  unsigned long long per = (units + gridDim.x - 1) / gridDim.x;
-  if (per < kLeastUnits) per = kLeastUnits;
-  unsigned long long done = (unsigned long long)blockIdx.x * per;         // units in front of the next one
-  unsigned long long left = done < units ? (done + per < units ? per : units - done) : 0;
-  if (left > 0 && ahead <= done && done < ahead + mine) {
+  const unsigned long long share = (all + gridDim.x - 1) / gridDim.x;
+  const unsigned per = share < kLeastShare ? kLeastShare : (unsigned)share;
+  const unsigned long long begin = (unsigned long long)blockIdx.x * per;
+  unsigned left = begin < all ? (begin + per < all ? per : (unsigned)(all - begin)) : 0;
+  if (left > 0 && ahead <= begin && begin < ahead + mine) {
     unsigned long long at = ahead;
     for (int i = i_begin; i < i_end; ++i) {
-      const unsigned long long u = units_of(a, begin_of<F::TT>(a, a.b.plan.groups[i]));
-      if (at <= done && done < at + u) {
+      const unsigned long long n = source_of<F::TT>(a, groups, i).all();
+      if (at <= begin && begin < at + n) {
         s_first = i;
-        s_from = done - at;
+        s_from = begin - at;
       }
-      at += u;
+      at += n;
     }
   }
-  // Where every instance's own rows begin.
+  // What the join looks for, of every instance: rows in common that were read, and tiles of its own.
   for (int i = blockIdx.x * kThreads + tid; i < a.r.n_inst; i += gridDim.x * kThreads) {
-    const Begin s = begin_of<F::TT>(a, a.b.plan.inst[i]);
-    a.b.start[i] = s.tiles > 0 ? s.S : 0;
+    const Source s = beginning_of<F::TT>(a, a.plan.inst[i]);
+    a.has[i] = make_int2(s.tiles, behind_of<F::TT>(a, i, s.tiles > 0 ? s.a1 : 0).tiles);
   }
   if (left == 0) return;
   __syncthreads();
   unsigned long long from = s_from;
-
-  const float scale = kLog2E / sqrtf((float)D);
-  const unsigned buffers = lds_address(s_tiles);
-  for (int gi = __builtin_amdgcn_readfirstlane(s_first); left > 0 && gi < groups; ++gi, from = 0) {
-    const Begin s = begin_of<F::TT>(a, a.b.plan.groups[gi]);
-    const unsigned long long all_units = units_of(a, s);
-    while (left > 0 && from < all_units) {
-      const int t = (int)(from / (unsigned)s.tiles), u_begin = (int)(from % (unsigned)s.tiles);
-      const int u_end = (unsigned long long)(s.tiles - u_begin) < left ? s.tiles : u_begin + (int)left;
-      const int parts = (int)((done - (unsigned)u_begin + (unsigned)s.tiles - 1) / per) - (int)blockIdx.x + 1;      // of this tile, from here on
-      from += (unsigned)(u_end - u_begin);
-      left -= (unsigned)(u_end - u_begin);
-      done += (unsigned)(u_end - u_begin);
-
-      // This lane's row of q, of all of the group's.  Rows that are none are computed as the group's first and not stored.
-      const int x = t * kPrefillRows + wave * 32 + n;
-      const int of = x / a.b.rows, rest = x % a.b.rows;
-      const int inst = a.b.plan.member[s.first + (of < s.count ? of : 0)];
-      const int n_q = a.n_q == nullptr ? a.q_cap : clamped(a.n_q[inst], 0, a.q_cap);
-      const bool real = of < s.count && rest / g < n_q;
-      const int p = clamped(a.r.len[inst], 0, a.r.t_cap) - n_q + rest / g;
-      const int lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
-      int p_min = real ? p : 0x7fffffff, p_max = real ? p : -1;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const int y = __shfl_xor(p_min, o, 64), z = __shfl_xor(p_max, o, 64);
-        p_min = y < p_min ? y : p_min;
-        p_max = z > p_max ? z : p_max;
-      }
-      p_min = __builtin_amdgcn_readfirstlane(p_min);
-      p_max = __builtin_amdgcn_readfirstlane(p_max);
-      const bool idle = p_max < 0;                         // a wave without rows (or whose rows see nothing)
-      const size_t q_row = (size_t)inst * a.b.rows + (real ? rest : 0);
-      u32x4 qf[F::KS];
-#pragma unroll
-      for (int k = 0; k < F::KS; ++k) qf[k] = static_cast<const u32x4*>(a.q)[q_row * F::PIECES + 2 * k + hb];
-
-      float16v o[F::DB];
-#pragma unroll
-      for (int b = 0; b < F::DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
-      float m = -INFINITY, sum = 0.f;                      // the sum over this lane's half of the cache rows
-
-      const TablePages pages = pages_of(a.r, s.lead);
+  for (int x = __builtin_amdgcn_readfirstlane(s_first); left > 0 && x < sources; ++x, from = 0) {
+    const Source s = source_of<F::TT>(a, groups, x);
+    const unsigned long long end = s.all();
+    while (left > 0 && from < end) {
+      // Tile t of its rows of q, from `r` on.
+      const unsigned first_size = s.size(0);
+      const int last = s.q_tiles() - 1;
+      const int t = __builtin_amdgcn_readfirstlane(from / first_size < (unsigned)last ? (int)(from / first_size) : last);
+      const unsigned r = (unsigned)(from - (unsigned long long)t * first_size), size = s.size(t);
+      const bool whole = size <= (per > kWhole ? per : kWhole);           // belongs to the workgroup that it begins in
+      const unsigned n = whole || size - r < left ? size - r : left;       // (whole: with what lies in others' shares)
+      from += n;
+      left -= n < left ? n : left;
+      if (whole && r > 0) continue;
+      const bool narrow = s.narrow(t);
+      const unsigned each = narrow ? 1 : kWide;
+      const int u_begin = r <= kFront ? 0 : (int)((r - kFront + each - 1) / each);
+      const int u_end = r + n <= kFront ? 0 : (int)((r + n - kFront + each - 1) / each);
+      const size_t x0 = (size_t)s.x0 + (size_t)t * kPrefillRows, slot = x0 + (size_t)kPrefillRows * blockIdx.x;
+      const int rows = s.rows - t * kPrefillRows < kPrefillRows ? s.rows - t * kPrefillRows : kPrefillRows;
+      if (r == 0 && tid < rows) a.row[x0 + tid] = make_int2((int)slot + tid, 1 + (int)((size - n + per - 1) / per));
       __syncthreads();                                     // everybody is done with the piece before
-      Run next = run_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
-      auto send = [&](int u) {                             // tile u, whose rows are those of `next`
-        const unsigned to = buffers + (u % 2) * 2 * F::TILE * 16;
-        send_tile<F, false>(a, s.lead, next, s, wave, to);
-        send_tile<F, true>(a, s.lead, next, s, wave, to + F::TILE * 16);
-        next = run_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);
-      };
-      send(u_begin);
-      // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
-#pragma unroll
-      for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
-      for (int u = u_begin; u < u_end; ++u) {
-        // This tile has landed; everybody is done with the buffer that is filled next.
-        landed<0>();
-        lds_read();
-        __builtin_amdgcn_s_barrier();
-        const int t0 = s.tile(u) * F::TT;
-        const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
-        const u32x4* Vt = Kt + F::TILE;
-        if (u + 1 < u_end) send(u + 1);
-        if (idle) continue;
-        float16v c[F::TB];
-        if constexpr (sizeof(T) == 2 || !EXACT) {
-#pragma unroll
-          for (int b = 0; b < F::TB; ++b) c[b] = product<T, D>(Kt, 32 * b, qf);
-        } else {
-          c[0] = product_in_parts<D>(Kt, qf);
+      if (u_begin >= u_end) {                              // (what is in front alone)
+        if (tid < rows) {
+          a.ml[(slot + tid) * 2] = -INFINITY;
+          a.ml[(slot + tid) * 2 + 1] = 0.f;
         }
-        // Every row of the tile is seen by every query of the wave, or the scores of those that are not become -inf.
-        const bool all = t0 + F::TT <= s.S && t0 + F::TT - 1 <= p_min && (a.window <= 0 || t0 > p_max - a.window || t0 + F::TT <= a.n_first);
-        if (!all) {
-#pragma unroll
-          for (int b = 0; b < F::TB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int j = t0 + 32 * b + reg_row(i, hb);
-              c[b][i] = (j >= s.S) | (j > p) | ((j < lo) & (j >= a.n_first)) ? -INFINITY : c[b][i];
-            }
-        }
-        float top = c[0][0];
-#pragma unroll
-        for (int b = 0; b < F::TB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, c[b][i]);
-        top = max32(top);
-        // The reference is a whole number in units of log2 (a change of it rounds nothing).  Exponents refer to 0 as long as nothing is seen, and
-        // where it is far, as the scores are brought near then.
-        const float ref = fmaxf(m, ceilf(top * scale));
-        const bool far = is_far(ref);
-        if (__any((ref != m) | far)) {
-          const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
-          sum *= shrink;
-#pragma unroll
-          for (int b = 0; b < F::DB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[b][i] *= shrink;
-          m = ref;
-          if (__any(far && m != -INFINITY)) {
-#pragma unroll
-            for (int b = 0; b < F::TB; ++b)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) c[b][i] = far && m != -INFINITY ? brought_near(c[b][i], scale, m) : c[b][i];
-          }
-        }
-        const float use = far ? 0.f : ref;
-        float part[4] = {0.f, 0.f, 0.f, 0.f};              // (sums of a tile first: long caches lose fewer digits so)
-#pragma unroll
-        for (int b = 0; b < F::TB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            c[b][i] = exp2_fast(__builtin_fmaf(c[b][i], scale, -use));
-            part[i & 3] += c[b][i];
-          }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-          for (int k = 0; k < F::TT / 16; ++k) {
-            // A probability is the sum of three numbers of bf16, 24 bits, where the output has 32 (EXACT); else it is rounded to one, as in a prefill.
-            constexpr int PARTS = EXACT ? 3 : 1;
-            bf16x8 pb[PARTS];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float y = c[k / 2][8 * (k % 2) + e];
-#pragma unroll
-              for (int w = 0; w < PARTS; ++w) {
-                pb[w][e] = (__bf16)y;
-                y -= (float)pb[w][e];
-              }
-            }
-            // V^T of 16 cache rows: the transposing read gives lane (m, hb) column m of four rows; a lane of 16 points to the 8 bytes at
-            // row lane / 4, columns 4 (lane % 4).
-            const int i = lane & 15, r = 16 * k + 4 * hb + (i >> 2);
-#pragma unroll
-            for (int b = 0; b < F::DB; ++b) {
-              const int col = 32 * b + 16 * ((lane >> 4) & 1) + 4 * (i & 3), piece = col / 8;
-              bf16x8 va;
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const int rr = r + 8 * half;
-                const char* at = reinterpret_cast<const char*>(Vt + rr * F::PIECES + F::v_place(rr, piece)) + (col % 8) * 2;
-                const short4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
-                const bf16x4 y = __builtin_bit_cast(bf16x4, w);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) va[4 * half + e] = y[e];
-              }
-#pragma unroll
-              for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[w], o[b], 0, 0, 0);
-            }
-          }
-        } else {
-          const float* Vf = reinterpret_cast<const float*>(Vt);
-#pragma unroll
-          for (int b = 0; b < F::DB; ++b) {
-            float16v y;                                    // of this tile alone, as the sums
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              y = __builtin_amdgcn_mfma_f32_32x32x2f32(Vf[reg_row(i, hb) * D + 32 * b + n], c[0][i], y, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[b][i] += y[i];
-          }
-        }
-      }
-      sum = sum32(sum);
-      if (real) {
-        const size_t slot = (size_t)s.first * a.b.rows + x + (size_t)kPrefillRows * blockIdx.x;
-        if (hb == 0 && u_begin == 0) a.b.row[(size_t)s.first * a.b.rows + x] = make_int2((int)slot, parts);
-        if (hb == 0) {
-          a.b.ml[slot * 2] = m;
-          a.b.ml[slot * 2 + 1] = sum;
-        }
-#pragma unroll
-        for (int b = 0; b < F::DB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            float4v y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = o[b][i + e];
-            *reinterpret_cast<float4v*>(a.b.o + slot * D + 32 * b + reg_row(i, hb)) = y;
-          }
+      } else if (narrow) {
+        narrow_piece<T, D, EXACT>(a, s, t, u_begin, u_end, slot, s_tiles);
+      } else {
+        wide_piece<T, D, EXACT>(a, s, t, u_begin, u_end, slot, s_tiles);
       }
     }
   }
 }
 
-template <typename T, int D> hipError_t run(const Shape& s, const BeginArgs& a, bool exact, hipStream_t st) {
-  const size_t lds = (size_t)2 * 2 * Form<T, D>::TILE * 16;
-  if (exact) cache_beginnings_kernel<T, D, true><<<kShareWgs, kThreads, lds, st>>>(a, s.g);
-  else cache_beginnings_kernel<T, D, false><<<kShareWgs, kThreads, lds, st>>>(a, s.g);
+// Joins the pieces: a wave per row of q.  OUT: float, or the type of q.
+template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(SharedArgs a) {
+  constexpr int E = D / 64;                                // outputs of a lane
+  const long long at = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int inst = (int)(at / a.rows), row = (int)(at % a.rows), lane = threadIdx.x & 63;
+  if (inst >= a.r.n_inst || row >= queries(a, inst) * a.g) return;
+  const int2 has = a.has[inst];
+  const int pos = a.plan.pos[inst];
+  const bool some = has.x > 0 && (unsigned)pos < (unsigned)a.r.n_inst;
+  const int2 first = some ? a.row[(size_t)pos * a.rows + row] : make_int2(0, 0);
+  const int2 own = has.y > 0 ? a.row[((size_t)a.r.n_inst + inst) * a.rows + row] : make_int2(0, 0);
+  const int parts = first.y + own.y;
+  auto slot = [&](int p) { return p < first.y ? (size_t)first.x + (size_t)kPrefillRows * p : (size_t)own.x + (size_t)kPrefillRows * (p - first.y); };
+  float top = -INFINITY;
+  for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.ml[slot(p) * 2]);
+  top = wave_max(top);
+  const float use = top == -INFINITY ? 0.f : top;
+  float o[E], all = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const int p = p0 + lane;
+    const float f = p < parts ? exp2_fast(a.ml[slot(p) * 2] - use) : 0.f;
+    all += p < parts ? f * a.ml[slot(p) * 2 + 1] : 0.f;
+    const int n = parts - p0 < 64 ? parts - p0 : 64;
+    constexpr int kAhead = 8;                              // loads under way
+    for (int x0 = 0; x0 < n; x0 += kAhead) {
+      float v[kAhead][E];
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        const float* src = a.o + slot(p0 + (x0 + x < n ? x0 + x : n - 1)) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[x][e] = src[e];
+      }
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        const float w = x0 + x < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x0 + x)) : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += w == 0.f ? 0.f : w * v[x][e];            // (a piece without tiles has left no sums)
+      }
+    }
+  }
+  all = wave_sum(all);
+  OUT* out = static_cast<OUT*>(a.out) + ((size_t)inst * a.rows + row) * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float y = all == 0.f ? 0.f : o[e] / all;         // a query that sees nothing has a zero output
+    if constexpr (sizeof(OUT) == 2) out[e].bits = __builtin_bit_cast(uint16_t, (__bf16)y);
+    else out[e] = y;
+  }
+}
+
+template <typename T, int D, bool EXACT, typename OUT> hipError_t run(const SharedArgs& a, hipStream_t st) {
+  cache_shared_kernel<T, D, EXACT><<<kShareWgs, kThreads, (size_t)2 * 2 * Form<T, D>::TILE * 16, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const unsigned wgs = (unsigned)(((long long)a.r.n_inst * a.rows + kWaves - 1) / kWaves);
+  cache_shared_join_kernel<T, D, OUT><<<wgs, kThreads, 0, st>>>(a);
   return hipGetLastError();
+}
+template <typename T, int D> hipError_t run(const SharedArgs& a, bool decode, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) return decode ? run<T, D, true, float>(a, st) : run<T, D, false, T>(a, st);
+  else return run<T, D, true, float>(a, st);
 }
 
 }  // namespace
@@ -403,9 +743,9 @@ hipError_t launch_cache_share(const Shape& s, const int32_t* group, const int32_
   return hipGetLastError();
 }
 
-hipError_t launch_cache_beginnings(const Shape& s, const BeginArgs& a, bool exact, hipStream_t st) {
-  if (s.kv_dtype == AP_BF16) return s.d == 128 ? run<bf16_t, 128>(s, a, exact, st) : run<bf16_t, 64>(s, a, exact, st);
-  return s.d == 128 ? run<float, 128>(s, a, exact, st) : run<float, 64>(s, a, exact, st);
+hipError_t launch_cache_shared(const Shape& s, const SharedArgs& a, bool decode, hipStream_t st) {
+  if (s.kv_dtype == AP_BF16) return s.d == 128 ? run<bf16_t, 128>(a, decode, st) : run<bf16_t, 64>(a, decode, st);
+  return s.d == 128 ? run<float, 128>(a, decode, st) : run<float, 64>(a, decode, st);
 }
 
 }  // namespace ap

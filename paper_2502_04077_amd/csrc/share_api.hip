@@ -32,28 +32,15 @@ SharePlan share_plan(const Shape& s, void* plan) {
   return p;
 }
 
-// Chunks of so few rows of q that a tile of kPrefillRows has several instances'.
-bool few_rows(const Shape& s, int q_cap) { return q_cap * s.g <= kPrefillRows / 2; }
-
 SharedWs shared_ws(const Shape& s, int q_cap) {
   SharedWs w;
   size_t o = 0;
   auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
-  const int rows = (q_cap > 0 ? q_cap : 1) * s.g;
-  w.start = take((size_t)s.n_inst * 4);
-  w.row = take((size_t)s.n_inst * rows * 8);
-  const size_t pieces = (size_t)s.n_inst * rows + (size_t)kPrefillRows * kShareWgs;
+  const size_t rows = (size_t)2 * s.n_inst * q_cap * s.g, pieces = rows + (size_t)kPrefillRows * kShareWgs;
+  w.has = take((size_t)s.n_inst * 8);
+  w.row = take(rows * 8);
   w.ml = take(pieces * 2 * 4);
   w.o = take(pieces * s.d * 4);
-  w.rest = o;
-  if (q_cap == 0) {
-    o += cache_decode_ws(s, false).total;
-  } else {
-    // As in cache_prefill_ws, but that sums are left to be joined with one split too.
-    size_t part = s.n_inst > kSplitWgs / 2 ? 0 : (size_t)kSplitWgs * kPrefillRows;
-    if (part < (size_t)s.n_inst * rows) part = (size_t)s.n_inst * rows;
-    o += (part * 2 * 4 + 15) / 16 * 16 + part * s.d * 4;
-  }
   w.total = o;
   return w;
 }
@@ -78,24 +65,25 @@ static ap::Pages pages_of(const Shape& s, void* K, void* V, int32_t* table, int3
   return p;
 }
 
-// Of decode and prefill: the beginnings' part of the workspace.
-static ap::BeginArgs begin_args(const Shape& s, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
-                                const void* plan, int32_t window, int32_t n_first, char* base, const ap::SharedWs& w) {
-  ap::BeginArgs a;
-  a.r = rows_of(s, len);
-  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap;
-  a.window = seen_window(s, window); a.n_first = seen_first(s, n_first);
-  a.b.plan = ap::share_plan(s, const_cast<void*>(plan));
-  a.b.start = reinterpret_cast<int32_t*>(base + w.start);
-  a.b.row = reinterpret_cast<int2*>(base + w.row);
-  a.b.ml = reinterpret_cast<float*>(base + w.ml);
-  a.b.o = reinterpret_cast<float*>(base + w.o);
-  a.b.rows = q_cap * s.g;
-  return a;
+// Chunks of so few rows of q that a tile of kPrefillRows has several instances'; and all rows are numbered in 32 bits, and their pieces.
+static bool few_rows(const Shape& s, int32_t q_cap) {
+  return q_cap * s.g <= ap::kPrefillRows / 2 &&
+         2ll * s.n_inst * q_cap * s.g + (long long)ap::kPrefillRows * ap::kShareWgs < (1ll << 31);
 }
-// Rows of q of all instances are numbered in 32 bits, the pieces of the beginnings too.
-static bool rows_ok(const Shape& s, int32_t q_cap) {
-  return (long long)s.n_inst * q_cap * s.g + (long long)ap::kPrefillRows * ap::kShareWgs < (1ll << 31);
+static hipError_t launch_shared(const Shape& s, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
+                                const void* plan, int32_t window, int32_t n_first, void* out, bool decode, void* ws, void* stream) {
+  const ap::SharedWs w = ap::shared_ws(s, q_cap);
+  char* base = static_cast<char*>(ws);
+  ap::SharedArgs a;
+  a.r = rows_of(s, len);
+  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.g = s.g; a.rows = q_cap * s.g;
+  a.window = seen_window(s, window); a.n_first = seen_first(s, n_first); a.out = out;
+  a.plan = ap::share_plan(s, const_cast<void*>(plan));
+  a.has = reinterpret_cast<int2*>(base + w.has);
+  a.row = reinterpret_cast<int2*>(base + w.row);
+  a.ml = reinterpret_cast<float*>(base + w.ml);
+  a.o = reinterpret_cast<float*>(base + w.o);
+  return ap::launch_cache_shared(s, a, decode, static_cast<hipStream_t>(stream));
 }
 
 // As in api.hip: memory that a kernel may read and write, on the device or pinned; pageable host memory would fault the GPU.
@@ -185,21 +173,13 @@ int ap_cache_share(ap_ctx* ctx, const int32_t* group, const int32_t* shared, voi
 }
 
 size_t ap_cache_shared_workspace_bytes(const ap_ctx* ctx, int32_t q_cap) {
-  if (ctx == nullptr || q_cap < 0 || (q_cap > 0 && !chunk_ok(ctx->s, q_cap)) || !rows_ok(ctx->s, 1)) return 0;
+  if (ctx == nullptr || q_cap < 0 || (q_cap > 0 && !chunk_ok(ctx->s, q_cap)) || !few_rows(ctx->s, 1)) return 0;
   const Shape& s = ctx->s;
-  size_t most = ap::shared_ws(s, 0).total;
-  // Of any chunk up to q_cap: those of few rows read beginnings for several instances at a time, the others are a prefill's.
-  int few = q_cap;
-  while (few > 0 && (!ap::few_rows(s, few) || !rows_ok(s, few))) few = few > ap::kPrefillRows ? ap::kPrefillRows : few - 1;
-  if (few > 0) {
-    const size_t x = ap::shared_ws(s, few).total;
-    if (x > most) most = x;
-  }
-  if (q_cap > 0) {
-    const size_t x = ap::cache_prefill_ws(s, q_cap, false).total;
-    if (x > most) most = x;
-  }
-  return most;
+  // Of any chunk up to q_cap: those of few rows read rows in common once, the others are a prefill's.
+  int few = q_cap < ap::kPrefillRows ? q_cap : ap::kPrefillRows;
+  while (few > 1 && !few_rows(s, few)) --few;
+  const size_t shared = ap::shared_ws(s, few > 1 ? few : 1).total, prefill = q_cap > 0 ? ap::cache_prefill_ws(s, q_cap, false).total : 0;
+  return shared > prefill ? shared : prefill;
 }
 
 int ap_cache_decode_shared(ap_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* len, const void* plan, int32_t window,
@@ -208,25 +188,8 @@ int ap_cache_decode_shared(ap_ctx* ctx, const void* q, const void* K, const void
   AP_REQUIRE_PTR(q); AP_REQUIRE_PTR(K); AP_REQUIRE_PTR(V); AP_REQUIRE_PTR(len); AP_REQUIRE_PTR(plan); AP_REQUIRE_PTR(out); AP_REQUIRE_PTR(ws);
   if (window < 0 || n_first < 0) return AP_ERR_ARG;
   const Shape& s = ctx->s;
-  if (!rows_ok(s, 1)) return AP_ERR_RANGE;
-  const ap::SharedWs w = ap::shared_ws(s, 0);
-  char* base = static_cast<char*>(ws);
-  const hipStream_t st = static_cast<hipStream_t>(stream);
-  const ap::BeginArgs begin = begin_args(s, q, nullptr, 1, K, V, len, plan, window, n_first, base, w);
-  if (ap::launch_cache_beginnings(s, begin, true, st) != hipSuccess) return AP_ERR_HIP;
-  const ap::CacheWs d = ap::cache_decode_ws(s, false);
-  base += w.rest;
-  ap::SharedDecodeArgs a;
-  a.r = begin.r; a.q = q; a.K = K; a.V = V; a.window = begin.window; a.n_first = begin.n_first; a.out = out; a.acc = nullptr;
-  a.before = reinterpret_cast<unsigned long long*>(base + d.before);
-  a.whole = reinterpret_cast<float*>(base + d.whole);
-  a.part_ml = reinterpret_cast<float*>(base + d.part_ml);
-  a.part_acc = reinterpret_cast<float*>(base + d.part_acc);
-  a.tickets = reinterpret_cast<unsigned long long*>(base + d.tickets);
-  a.nonce = 0;            // (the launcher draws it)
-  a.logits = nullptr;
-  a.b = begin.b;
-  return ap::launch_cache_decode_shared(s, a, st) == hipSuccess ? AP_OK : AP_ERR_HIP;
+  if (!few_rows(s, 1)) return AP_ERR_RANGE;
+  return launch_shared(s, q, nullptr, 1, K, V, len, plan, window, n_first, out, true, ws, stream) == hipSuccess ? AP_OK : AP_ERR_HIP;
 }
 
 int ap_cache_prefill_shared(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
@@ -237,21 +200,8 @@ int ap_cache_prefill_shared(ap_ctx* ctx, const void* q, const int32_t* n_q, int3
   if (window < 0 || n_first < 0) return AP_ERR_ARG;
   const Shape& s = ctx->s;
   if (!chunk_ok(s, q_cap)) return AP_ERR_RANGE;
-  if (!ap::few_rows(s, q_cap) || !rows_ok(s, q_cap)) return ap_cache_prefill(ctx, q, n_q, q_cap, K, V, len, window, n_first, out, nullptr, ws, stream);
-  const ap::SharedWs w = ap::shared_ws(s, q_cap);
-  char* base = static_cast<char*>(ws);
-  const hipStream_t st = static_cast<hipStream_t>(stream);
-  const ap::BeginArgs begin = begin_args(s, q, n_q, q_cap, K, V, len, plan, window, n_first, base, w);
-  if (ap::launch_cache_beginnings(s, begin, s.kv_dtype == AP_F32, st) != hipSuccess) return AP_ERR_HIP;
-  base += w.rest;
-  ap::SharedPrefillArgs a;
-  a.r = begin.r; a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.window = begin.window; a.n_first = begin.n_first; a.out = out;
-  a.acc = nullptr; a.stat = nullptr; a.sums = nullptr;
-  const size_t part = (w.total - w.rest) / (4 * ((size_t)s.d + 2));
-  a.part_ml = reinterpret_cast<float*>(base);
-  a.part_o = reinterpret_cast<float*>(base + (part * 2 * 4 + 15) / 16 * 16);
-  a.b = begin.b;
-  return ap::launch_cache_prefill_shared(s, a, st) == hipSuccess ? AP_OK : AP_ERR_HIP;
+  if (!few_rows(s, q_cap)) return ap_cache_prefill(ctx, q, n_q, q_cap, K, V, len, window, n_first, out, nullptr, ws, stream);
+  return launch_shared(s, q, n_q, q_cap, K, V, len, plan, window, n_first, out, false, ws, stream) == hipSuccess ? AP_OK : AP_ERR_HIP;
 }
 
 }  // extern "C"

@@ -54,38 +54,27 @@ struct SharePlan {
 size_t share_plan_bytes(const Shape& s);
 SharePlan share_plan(const Shape& s, void* plan);
 
-// What the attention over the beginnings leaves for the attention over the rows behind them.  A group's rows of q, those of its members one after
-// the other, are in tiles of kPrefillRows, its beginning in tiles of the cache; a unit is one of each.  The units, tile by tile of each group in the
-// order of the groups, are dealt to the workgroups in equal shares; the piece that workgroup w leaves of row x (of all groups' rows) is
-// number x + kPrefillRows * w.
-struct Beginnings {
-  SharePlan plan;
-  int32_t* start;                  // [n_inst] rows that were read as a group's beginning: the others' first
-  int2* row;                       // [n_inst * rows] of a group's row of q: the first of its pieces, and how many
-  float *ml, *o;                   // [n_inst * rows + kPrefillRows * kShareWgs][2] maximum and sum, and [..][d]
-  int rows;                        // of q, of an instance
-};
-constexpr int kShareWgs = 512;     // two a CU
+// Workgroups of the attention, two a CU.
+constexpr int kShareWgs = 512;
 
-struct BeginArgs {                 // the attention over the beginnings
+// Rows of q, `rows` an instance, are numbered twice: those of the groups' members one after the other, x < n_inst * rows, for the groups' beginnings; and
+// n_inst * rows + those of the instances for what lies behind.  The piece that workgroup w leaves of row x is number x + kPrefillRows * w.
+struct SharedArgs {
   CacheRows r;
   const void *q, *K, *V;
-  const int32_t* n_q;              // as in PrefillArgs
-  int q_cap, window, n_first;
-  Beginnings b;
+  const int32_t* n_q;              // [n_inst], or null: q_cap each
+  int q_cap, g, rows, window, n_first;
+  void* out;
+  SharePlan plan;
+  int2* has;                       // workspace: [n_inst] tiles of the beginning, and of the rows behind it
+  int2* row;                       // workspace: [2 * n_inst * rows] of a row of q: the first of its pieces, and how many
+  float *ml, *o;                   // workspace: [2 * n_inst * rows + kPrefillRows * kShareWgs][2] maximum and sum, and [..][d]
 };
-struct SharedDecodeArgs : DecodeArgs { Beginnings b; };
-struct SharedPrefillArgs : PrefillArgs { Beginnings b; };
-
-struct SharedWs { size_t start, row, ml, o, rest, total; };        // rest: of the attention over the rows behind
+struct SharedWs { size_t has, row, ml, o, total; };
 SharedWs shared_ws(const Shape& s, int q_cap);
 
 hipError_t launch_cache_share(const Shape& s, const int32_t* group, const int32_t* shared, const SharePlan& plan, hipStream_t st);
-// exact: probabilities keep 32 bits.
-hipError_t launch_cache_beginnings(const Shape& s, const BeginArgs& a, bool exact, hipStream_t st);
-hipError_t launch_cache_decode_shared(const Shape& s, const SharedDecodeArgs& a, hipStream_t st);
-hipError_t launch_cache_prefill_shared(const Shape& s, const SharedPrefillArgs& a, hipStream_t st);
-// Rows of q of an instance up to which beginnings are read for several of them at a time.
-bool few_rows(const Shape& s, int q_cap);
+// decode: the output is fp32, and probabilities keep 24 bits; else it is of the kv dtype.
+hipError_t launch_cache_shared(const Shape& s, const SharedArgs& a, bool decode, hipStream_t st);
 
 }  // namespace ap
