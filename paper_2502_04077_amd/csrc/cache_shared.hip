@@ -88,25 +88,29 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
 
 // ---------------------------------------------------------------------------------------------------------------- sources
 constexpr int kNarrowRows = 16;     // rows of q up to which the waves share them
-// What a tile of the cache counts with more rows of q (with fewer: 1), and what a tile of rows of q counts beside its tiles of the cache.
-constexpr int kWide = 2, kFront = 2;
-// Least share of a workgroup; a tile of rows of q that counts no more than kWhole, or than a share, is not cut.
-constexpr int kLeastShare = 4, kWhole = 8;
+// What a tile of the cache counts with up to 16 rows of q, and with more; what a tile of rows of q counts beside its tiles of the cache; the
+// least share of a workgroup.
+template <typename T, bool EXACT> struct Counts {
+  static constexpr int NARROW = 4, WIDE = sizeof(T) == 4 ? 12 : (EXACT ? 7 : 5), FRONT = 8, LEAST = 16;
+};
 
 // Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
 struct Source {
   int inst, first, count;
   int x0, rows;          // number of its first row of q among all sources', and how many
+  int p0;                // count 0: the position of the first query
   int a0, a1, p1, lo0, f;   // rows [a0, f) and [lo0, p1] are seen by one of them at least, f <= lo0; each may be empty
   int ta, ts, tb, tiles; // tiles of TT rows: ts from ta on, the others from tb
   __device__ __forceinline__ int tile(int u) const { return u < ts ? ta + u : tb + (u - ts); }
   __device__ __forceinline__ bool row(int j) const { return j >= a0 && j <= p1 && (j >= lo0 || j < f); }
   __device__ __forceinline__ int q_tiles() const { return (rows + kPrefillRows - 1) / kPrefillRows; }
-  // What a tile of rows of q counts: each but the last, and the last.
-  __device__ __forceinline__ int narrow(int t) const { return rows - t * kPrefillRows <= kNarrowRows; }
-  __device__ __forceinline__ unsigned size(int t) const { return tiles == 0 ? 0u : kFront + (unsigned)tiles * (narrow(t) ? 1 : kWide); }
-  __device__ __forceinline__ unsigned long long all() const {
-    return tiles == 0 ? 0ull : (unsigned long long)(q_tiles() - 1) * size(0) + size(q_tiles() - 1);
+  // What a tile of rows of q counts, and all of them.
+  __device__ __forceinline__ bool narrow(int t) const { return rows - t * kPrefillRows <= kNarrowRows; }
+  template <typename C> __device__ __forceinline__ unsigned size(int t) const {
+    return tiles == 0 ? 0u : C::FRONT + (unsigned)tiles * (narrow(t) ? C::NARROW : C::WIDE);
+  }
+  template <typename C> __device__ __forceinline__ unsigned long long all() const {
+    return tiles == 0 ? 0ull : (unsigned long long)(q_tiles() - 1) * size<C>(0) + size<C>(q_tiles() - 1);
   }
 };
 __device__ __forceinline__ int queries(const SharedArgs& a, int i) { return a.n_q == nullptr ? a.q_cap : clamped(a.n_q[i], 0, a.q_cap); }
@@ -131,102 +135,129 @@ template <int TT> __device__ __forceinline__ void see(const SharedArgs& a, Sourc
   if (s.ts > 0 && s.tb < end) s.tb = end;
   s.tiles = a0 >= a1 || s.p1 < 0 || s.rows == 0 ? 0 : s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
 }
-// A group's beginning, by any member's line of the plan; without tiles where there is none, or nobody sees it.
-template <int TT> __device__ __forceinline__ Source beginning_of(const SharedArgs& a, int4 line) {
-  Source s;
-  const int n = a.r.n_inst;
-  const bool several = line.z > 1 && (unsigned)line.x < (unsigned)n && line.y >= 0 && line.z <= n - line.y;
-  s.inst = line.x; s.first = line.y; s.count = line.z;
-  s.rows = several ? line.z * a.rows : 0;
-  s.x0 = line.y * a.rows;
-  const int L = several ? clamped(a.r.len[line.x], 0, a.r.t_cap) : 0, S = line.w < L ? line.w : L;
-  int p = 0x7fffffff;                                      // the lowest position of a query
-  if (S > 0 && a.window > 0)
-    for (int x = 0; x < s.count; ++x) {
-      const int i = clamped(a.plan.member[s.first + x], 0, n - 1), m = queries(a, i), base = clamped(a.r.len[i], 0, a.r.t_cap) - m;
-      if (m > 0 && base < p) p = base;
-    }
-  see<TT>(a, s, 0, S > 0 ? S : 0, p);
+// A source that is the same for all lanes.
+__device__ __forceinline__ Source uniform(Source s) {
+  int* w = reinterpret_cast<int*>(&s);
+#pragma unroll
+  for (int k = 0; k < (int)(sizeof(Source) / 4); ++k) w[k] = __builtin_amdgcn_readfirstlane(w[k]);
   return s;
 }
-// An instance's rows from `start` on.
-template <int TT> __device__ __forceinline__ Source behind_of(const SharedArgs& a, int i, int start) {
-  Source s;
-  const int L = clamped(a.r.len[i], 0, a.r.t_cap), m = queries(a, i);
-  s.inst = i; s.first = 0; s.count = 0;
-  s.rows = m * a.g;
-  s.x0 = (a.r.n_inst + i) * a.rows;
-  see<TT>(a, s, start, L, L - m);
-  return s;
-}
-// Sources in their order: the groups', then the instances'.
+// Sources in their order: the groups', then the instances'.  What has to be loaded for source x is asked for together.
 template <int TT> __device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int x) {
-  if (x < groups) return beginning_of<TT>(a, a.plan.groups[x]);
-  const Source s = beginning_of<TT>(a, a.plan.inst[x - groups]);
-  return behind_of<TT>(a, x - groups, s.tiles > 0 ? s.a1 : 0);
+  const int n = a.r.n_inst, i = x < groups ? 0 : x - groups;
+  const int4 line = *(x < groups ? a.plan.groups + x : a.plan.inst + i);
+  const int m = queries(a, i), own = clamped(a.r.len[i], 0, a.r.t_cap);
+  const bool several = line.z > 1 && (unsigned)line.x < (unsigned)n && line.y >= 0 && line.z <= n - line.y;
+  const int lead = clamped(a.r.len[several ? line.x : i], 0, a.r.t_cap);
+  const int S = several ? clamped(line.w, 0, lead) : 0;
+  Source s;
+  if (x < groups) {
+    s.inst = line.x; s.first = line.y; s.count = line.z;
+    s.rows = several ? line.z * a.rows : 0;
+    s.x0 = line.y * a.rows;
+    s.p0 = 0;
+    int p = 0x7fffffff;                                    // the lowest position of a query
+    if (S > 0 && a.window > 0)
+      for (int k = 0; k < s.count; ++k) {
+        const int member = clamped(a.plan.member[s.first + k], 0, n - 1), q = queries(a, member), base = clamped(a.r.len[member], 0, a.r.t_cap) - q;
+        if (q > 0 && base < p) p = base;
+      }
+    see<TT>(a, s, 0, S, p);
+  } else {
+    s.inst = i; s.first = 0; s.count = 0;
+    s.rows = m * a.g;
+    s.x0 = (n + i) * a.rows;
+    s.p0 = own - m;
+    see<TT>(a, s, S, own, s.p0);
+  }
+  return s;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- tiles of the cache
-// As Run in cache_tiles.h, for the rows that a source sees.
-template <typename F> __device__ __forceinline__ Run run_of(const SharedArgs& a, const TablePages& pages, const Source& s, int t0, int wave) {
-  constexpr size_t bytes = F::PIECES * 16;
-  Run x;
+// The consecutive rows of a tile that a wave fetches: they lie in one page, or in two of eight rows.  In the place of rows that the source does not see,
+// which are not read, stands one that it does.  Wave-uniform, and looked up through the scalar cache: a vector load of the table's would wait
+// for the tiles under way (a tile that is seen in part then took some 8 us).
+struct Fetch {
+  const char *k, *v;                                       // row 0, as if all of them lay together
+  long long second;                                        // and what to add for the second eight, in bytes
+  long long other;                                         // the one that stands in, relative to row 0
+  bool all;
+  int j0;
+};
+template <typename F> __device__ __forceinline__ Fetch fetch_of(const SharedArgs& a, const TablePages& pages, const Source& s, int t0, int wave) {
+  constexpr long long bytes = F::PIECES * 16;
+  Fetch x;
   x.j0 = t0 + wave * F::RW;
   x.all = x.j0 >= s.a0 && x.j0 + F::RW - 1 <= s.p1 && (x.j0 >= s.lo0 || x.j0 + F::RW <= s.f);
-  const int from = x.j0 < s.f ? s.a0 : s.lo0, alt = x.j0 > from ? x.j0 : from;          // a row that is seen
-  x.alt = alt < s.p1 ? alt : s.p1;
   const size_t at = pages.at(x.j0);
   x.k = static_cast<const char*>(a.K) + at * bytes;
   x.v = static_cast<const char*>(a.V) + at * bytes;
-  x.second = F::RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(x.j0 + 8) - at) - 8) * (long long)bytes : 0;
+  x.second = F::RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(x.j0 + 8) - at) - 8) * bytes : 0;
+  x.other = 0;
+  if (!x.all) {
+    const int from = x.j0 < s.f ? s.a0 : s.lo0;
+    int j = x.j0 > from ? x.j0 : from;
+    if (j > s.p1) j = s.p1;
+    x.other = ((long long)(pages.at(j & ~7) - at) + (j & 7)) * bytes;
+  }
   return x;
 }
-template <typename F, bool IS_V>
-__device__ __forceinline__ void send_tile(const SharedArgs& a, const Run& run, const Source& s, int wave, unsigned lds) {
+template <typename F, bool IS_V> __device__ __forceinline__ void send_tile(const Fetch& x, const Source& s, int wave, unsigned lds) {
   constexpr unsigned bytes = F::PIECES * 16;
   const int lane = threadIdx.x & 63;
   const unsigned to = lds + wave * F::LOADS * 1024;
-  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };                   // of the run
+  const char* base = IS_V ? x.v : x.k;
+  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };                   // of the wave's
   auto piece = [&](int l) {
     const int place = lane % F::PIECES;
     return IS_V ? F::v_place(row(l), place) : F::k_place(wave * F::RW + row(l), place);
   };
-  if (run.all) {
+  if (x.all) {
 #pragma unroll
-    for (int l = 0; l < F::LOADS; ++l)
-      to_lds<false>((IS_V ? run.v : run.k) + (l >= F::LOADS / 2 ? run.second : 0), row(l) * bytes + piece(l) * 16, to + l * 1024);
+    for (int l = 0; l < F::LOADS; ++l) to_lds<false>(base + (l >= F::LOADS / 2 ? x.second : 0), row(l) * bytes + piece(l) * 16, to + l * 1024);
   } else {
-#pragma unroll 1
+#pragma unroll
     for (int l = 0; l < F::LOADS; ++l) {
-      const int j = s.row(run.j0 + row(l)) ? run.j0 + row(l) : run.alt;
-      to_lds_from(static_cast<const char*>(IS_V ? a.V : a.K) + row_at(a.r, s.inst, j) * bytes + piece(l) * 16, to + l * 1024);
+      const long long at = s.row(x.j0 + row(l)) ? (l >= F::LOADS / 2 ? x.second : 0) + row(l) * (long long)bytes : x.other;
+      to_lds_from(base + at + piece(l) * 16, to + l * 1024);
     }
   }
 }
-// A piece's tiles of the cache, one after the other: tile u is worked off by `work(t0, K, V)` while the next is on its way.  All threads of the workgroup.
-template <typename F, typename WORK>
-__device__ __forceinline__ void over_tiles(const SharedArgs& a, const Source& s, int u_begin, int u_end, const u32x4* s_tiles, WORK work) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const unsigned buffers = lds_address(s_tiles);
-  const TablePages pages = pages_of(a.r, s.inst);
-  Run next = run_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
-  auto send = [&](int u) {                                 // tile u, whose rows are those of `next`
-    const unsigned to = buffers + (u % 2) * 2 * F::TILE * 16;
-    send_tile<F, false>(a, next, s, wave, to);
-    send_tile<F, true>(a, next, s, wave, to + F::TILE * 16);
-    next = run_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);         // a tile ahead: the table's latency
-  };
-  send(u_begin);
-  for (int u = u_begin; u < u_end; ++u) {
-    // This tile has landed; everybody is done with the buffer that is filled next.
-    landed<0>();
-    lds_read();
-    __builtin_amdgcn_s_barrier();
-    if (u + 1 < u_end) send(u + 1);
-    const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
-    work(s.tile(u) * F::TT, Kt, Kt + F::TILE);
+// A piece's tiles of the cache, one after the other.  The first is sent for where this is made, the others while the one before is worked off.
+// All threads of the workgroup.
+template <typename F> struct Tiles {
+  const SharedArgs& a;
+  const Source& s;
+  const u32x4* s_tiles;
+  int u_begin, u_end, wave;
+  unsigned buffers;
+  TablePages pages;
+  Fetch next;
+  __device__ __forceinline__ Tiles(const SharedArgs& a_, const Source& s_, int u0, int u1, const u32x4* lds) : a(a_), s(s_), s_tiles(lds), u_begin(u0), u_end(u1) {
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    buffers = lds_address(s_tiles);
+    pages = pages_of(a.r, s.inst);
+    next = fetch_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
+    send(u_begin);
   }
-}
+  __device__ __forceinline__ void send(int u) {            // tile u, whose rows are those of `next`
+    const unsigned to = buffers + (u % 2) * 2 * F::TILE * 16;
+    send_tile<F, false>(next, s, wave, to);
+    send_tile<F, true>(next, s, wave, to + F::TILE * 16);
+    next = fetch_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);         // a tile ahead: the table's latency
+  }
+  template <typename WORK> __device__ __forceinline__ void each(WORK work) {                // work(t0, K, V)
+    for (int u = u_begin; u < u_end; ++u) {
+      // This tile has landed; everybody is done with the buffer that is filled next.
+      landed<0>();
+      lds_read();
+      __builtin_amdgcn_s_barrier();
+      if (u + 1 < u_end) send(u + 1);
+      const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
+      work(s.tile(u) * F::TT, Kt, Kt + F::TILE);
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------------------------------------------- pieces
 // A lane's row of q: row x of the source.
@@ -243,13 +274,15 @@ __device__ __forceinline__ Query query_of(const SharedArgs& a, const Source& s, 
     const int of = x / a.rows;
     rest = x % a.rows;
     q.inst = clamped(a.plan.member[s.first + (of < s.count ? of : 0)], 0, a.r.n_inst - 1);
+    const int m = queries(a, q.inst), L = clamped(a.r.len[q.inst], 0, a.r.t_cap);
+    q.real = q.real && rest < m * a.g;
+    if (!q.real) rest = 0;
+    q.p = L - m + rest / a.g;
   } else {
+    if (!q.real) rest = 0;
     q.inst = s.inst;
+    q.p = s.p0 + rest / a.g;
   }
-  const int m = queries(a, q.inst);
-  q.real = q.real && rest < m * a.g;
-  if (!q.real) rest = 0;
-  q.p = clamped(a.r.len[q.inst], 0, a.r.t_cap) - m + rest / a.g;
   q.lo = a.window > 0 && q.p >= a.window ? q.p - a.window + 1 : 0;
   q.row = (size_t)q.inst * a.rows + rest;
   return q;
@@ -315,6 +348,7 @@ template <typename T, int D, bool EXACT>
 __device__ __forceinline__ void wide_piece(const SharedArgs& a, const Source& s, int t, int u_begin, int u_end, size_t slot, const u32x4* s_tiles) {
   using F = Form<T, D>;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, hb = lane >> 5;
+  Tiles<F> tiles(a, s, u_begin, u_end, s_tiles);
   const Query q = query_of(a, s, t * kPrefillRows + wave * 32 + n);
   int p_min, p_max;
   positions<32>(q, &p_min, &p_max);
@@ -332,7 +366,7 @@ __device__ __forceinline__ void wide_piece(const SharedArgs& a, const Source& s,
   // (From here on the compiler counts no load of its own as under way, and waits for none in the loop.)
 #pragma unroll
   for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
-  over_tiles<F>(a, s, u_begin, u_end, s_tiles, [&](int t0, const u32x4* Kt, const u32x4* Vt) {
+  tiles.each([&](int t0, const u32x4* Kt, const u32x4* Vt) {
     if (idle) return;
     float16v c[F::TB];
     if constexpr (sizeof(T) == 2) {
@@ -458,6 +492,7 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
   constexpr int KS = F::PIECES / 4, DB = D / 16, ACTIVE = F::TT / 16;      // pieces of a row that a lane has; blocks of 16 dims; waves
   static_assert(4 * F::TILE * 16 >= ACTIVE * (16 * D + 32) * 4, "the waves' sums");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
+  Tiles<F> tiles(a, s, u_begin, u_end, s_tiles);
   const Query q = query_of(a, s, t * kPrefillRows + n);
   int p_min, p_max;
   positions<16>(q, &p_min, &p_max);
@@ -471,7 +506,7 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
   const float scale = kLog2E / sqrtf((float)D);
 #pragma unroll
   for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[l]));
-  over_tiles<F>(a, s, u_begin, u_end, s_tiles, [&](int t0, const u32x4* Kt, const u32x4* Vt) {
+  tiles.each([&](int t0, const u32x4* Kt, const u32x4* Vt) {
     if (wave >= ACTIVE) return;
     // Rows j0 + 4 kg + r of the tile, of query n.  fp32 products go into four sums.
     const int j0 = 16 * wave;
@@ -585,16 +620,37 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
 template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
+  using C = Counts<T, EXACT>;
+  constexpr int kHeld = 8, kListed = 32;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
   __shared__ unsigned long long s_wave[kWaves], s_from;
   __shared__ int s_first;
+  __shared__ Source s_source[kListed];                                    // from s_first on
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
   // Where this workgroup's share begins: every thread sums up consecutive sources.
   const int groups = clamped(*a.plan.count, 0, a.r.n_inst), sources = groups + a.r.n_inst, chunk = (sources + kThreads - 1) / kThreads;
   const int i_begin = tid * chunk < sources ? tid * chunk : sources, i_end = i_begin + chunk < sources ? i_begin + chunk : sources;
-  unsigned long long mine = 0;
-  for (int i = i_begin; i < i_end; ++i) mine += source_of<F::TT>(a, groups, i).all();
+  unsigned long long size[kHeld], mine = 0;
+  int tiles[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    size[k] = 0;
+    tiles[k] = 0;
+  }
+  if (chunk <= kHeld) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (k < chunk) {
+        const int i = i_begin + k < i_end ? i_begin + k : sources - 1;    // (the loads of all of them are under way together)
+        const Source s = source_of<F::TT>(a, groups, i);
+        tiles[k] = s.tiles;
+        size[k] = i_begin + k < i_end ? s.template all<C>() : 0;
+        mine += size[k];
+      }
+  } else {
+    for (int i = i_begin; i < i_end; ++i) mine += source_of<F::TT>(a, groups, i).template all<C>();
+  }
   unsigned long long upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -609,49 +665,70 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     all += s_wave[w];
   }
   const unsigned long long share = (all + gridDim.x - 1) / gridDim.x;
-  const unsigned per = share < kLeastShare ? kLeastShare : (unsigned)share;
+  const unsigned per = share < C::LEAST ? C::LEAST : (unsigned)share;
   const unsigned long long begin = (unsigned long long)blockIdx.x * per;
   unsigned left = begin < all ? (begin + per < all ? per : (unsigned)(all - begin)) : 0;
   if (left > 0 && ahead <= begin && begin < ahead + mine) {
     unsigned long long at = ahead;
-    for (int i = i_begin; i < i_end; ++i) {
-      const unsigned long long n = source_of<F::TT>(a, groups, i).all();
-      if (at <= begin && begin < at + n) {
-        s_first = i;
-        s_from = begin - at;
+    if (chunk <= kHeld) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        if (at <= begin && begin < at + size[k]) {
+          s_first = i_begin + k;
+          s_from = begin - at;
+        }
+        at += size[k];
       }
-      at += n;
+    } else {
+      for (int i = i_begin; i < i_end; ++i) {
+        const unsigned long long n = source_of<F::TT>(a, groups, i).template all<C>();
+        if (at <= begin && begin < at + n) {
+          s_first = i;
+          s_from = begin - at;
+        }
+        at += n;
+      }
     }
   }
-  // What the join looks for, of every instance: rows in common that were read, and tiles of its own.
-  for (int i = blockIdx.x * kThreads + tid; i < a.r.n_inst; i += gridDim.x * kThreads) {
-    const Source s = beginning_of<F::TT>(a, a.plan.inst[i]);
-    a.has[i] = make_int2(s.tiles, behind_of<F::TT>(a, i, s.tiles > 0 ? s.a1 : 0).tiles);
+  // Which sources have tiles, for the join: the groups by their first member, the instances.
+  auto note = [&](int x, int n) {
+    if (x < groups) a.begun[clamped(a.plan.groups[x].x, 0, a.r.n_inst - 1)] = n;
+    else a.behind[x - groups] = n;
+  };
+  if (chunk <= kHeld) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (i_begin + k < i_end && (unsigned)(i_begin + k) % gridDim.x == blockIdx.x) note(i_begin + k, tiles[k]);
+  } else {
+    for (int x = blockIdx.x * kThreads + tid; x < sources; x += gridDim.x * kThreads) note(x, source_of<F::TT>(a, groups, x).tiles);
   }
   if (left == 0) return;
   __syncthreads();
+  const int x_first = __builtin_amdgcn_readfirstlane(s_first);
+  if (tid < kListed) s_source[tid] = source_of<F::TT>(a, groups, x_first + tid < sources ? x_first + tid : sources - 1);
+  __syncthreads();
   unsigned long long from = s_from;
-  for (int x = __builtin_amdgcn_readfirstlane(s_first); left > 0 && x < sources; ++x, from = 0) {
-    const Source s = source_of<F::TT>(a, groups, x);
-    const unsigned long long end = s.all();
+  for (int x = x_first; left > 0 && x < sources; ++x, from = 0) {
+    const Source s = uniform(x - x_first < kListed ? s_source[x - x_first] : source_of<F::TT>(a, groups, x));
+    const unsigned long long end = s.template all<C>();
     while (left > 0 && from < end) {
       // Tile t of its rows of q, from `r` on.
-      const unsigned first_size = s.size(0);
+      const unsigned first_size = s.template size<C>(0);
       const int last = s.q_tiles() - 1;
-      const int t = __builtin_amdgcn_readfirstlane(from / first_size < (unsigned)last ? (int)(from / first_size) : last);
-      const unsigned r = (unsigned)(from - (unsigned long long)t * first_size), size = s.size(t);
-      const bool whole = size <= (per > kWhole ? per : kWhole);           // belongs to the workgroup that it begins in
-      const unsigned n = whole || size - r < left ? size - r : left;       // (whole: with what lies in others' shares)
+      const int t = __builtin_amdgcn_readfirstlane(last == 0 || from / first_size >= (unsigned)last ? last : (int)(from / first_size));
+      const unsigned r = (unsigned)(from - (unsigned long long)t * first_size), of_tile = s.template size<C>(t);
+      // A small one belongs to the workgroup that it begins in.
+      const bool whole = of_tile <= (per / 4 > C::LEAST ? per / 4 : C::LEAST);
+      const unsigned n = whole || of_tile - r < left ? of_tile - r : left;
       from += n;
       left -= n < left ? n : left;
       if (whole && r > 0) continue;
       const bool narrow = s.narrow(t);
-      const unsigned each = narrow ? 1 : kWide;
-      const int u_begin = r <= kFront ? 0 : (int)((r - kFront + each - 1) / each);
-      const int u_end = r + n <= kFront ? 0 : (int)((r + n - kFront + each - 1) / each);
+      const unsigned each = narrow ? C::NARROW : C::WIDE;
+      const int u_begin = r <= C::FRONT ? 0 : (int)((r - C::FRONT + each - 1) / each);
+      const int u_end = r + n <= C::FRONT ? 0 : (int)((r + n - C::FRONT + each - 1) / each);
       const size_t x0 = (size_t)s.x0 + (size_t)t * kPrefillRows, slot = x0 + (size_t)kPrefillRows * blockIdx.x;
       const int rows = s.rows - t * kPrefillRows < kPrefillRows ? s.rows - t * kPrefillRows : kPrefillRows;
-      if (r == 0 && tid < rows) a.row[x0 + tid] = make_int2((int)slot + tid, 1 + (int)((size - n + per - 1) / per));
       __syncthreads();                                     // everybody is done with the piece before
       if (u_begin >= u_end) {                              // (what is in front alone)
         if (tid < rows) {
@@ -663,6 +740,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       } else {
         wide_piece<T, D, EXACT>(a, s, t, u_begin, u_end, slot, s_tiles);
       }
+      if (r == 0 && tid < rows) a.row[x0 + tid] = make_int2((int)slot + tid, 1 + (int)((of_tile - n + per - 1) / per));
     }
   }
 }
@@ -673,11 +751,11 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
   const long long at = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int inst = (int)(at / a.rows), row = (int)(at % a.rows), lane = threadIdx.x & 63;
   if (inst >= a.r.n_inst || row >= queries(a, inst) * a.g) return;
-  const int2 has = a.has[inst];
-  const int pos = a.plan.pos[inst];
-  const bool some = has.x > 0 && (unsigned)pos < (unsigned)a.r.n_inst;
+  const int4 line = a.plan.inst[inst];
+  const int pos = a.plan.pos[inst], behind = a.behind[inst];
+  const bool some = line.z > 1 && (unsigned)pos < (unsigned)a.r.n_inst && a.begun[clamped(line.x, 0, a.r.n_inst - 1)] > 0;
   const int2 first = some ? a.row[(size_t)pos * a.rows + row] : make_int2(0, 0);
-  const int2 own = has.y > 0 ? a.row[((size_t)a.r.n_inst + inst) * a.rows + row] : make_int2(0, 0);
+  const int2 own = behind > 0 ? a.row[((size_t)a.r.n_inst + inst) * a.rows + row] : make_int2(0, 0);
   const int parts = first.y + own.y;
   auto slot = [&](int p) { return p < first.y ? (size_t)first.x + (size_t)kPrefillRows * p : (size_t)own.x + (size_t)kPrefillRows * (p - first.y); };
   float top = -INFINITY;

@@ -37,7 +37,8 @@ SharedWs shared_ws(const Shape& s, int q_cap) {
   size_t o = 0;
   auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
   const size_t rows = (size_t)2 * s.n_inst * q_cap * s.g, pieces = rows + (size_t)kPrefillRows * kShareWgs;
-  w.has = take((size_t)s.n_inst * 8);
+  w.begun = take((size_t)s.n_inst * 4);
+  w.behind = take((size_t)s.n_inst * 4);
   w.row = take(rows * 8);
   w.ml = take(pieces * 2 * 4);
   w.o = take(pieces * s.d * 4);
@@ -79,7 +80,8 @@ static hipError_t launch_shared(const Shape& s, const void* q, const int32_t* n_
   a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.g = s.g; a.rows = q_cap * s.g;
   a.window = seen_window(s, window); a.n_first = seen_first(s, n_first); a.out = out;
   a.plan = ap::share_plan(s, const_cast<void*>(plan));
-  a.has = reinterpret_cast<int2*>(base + w.has);
+  a.begun = reinterpret_cast<int32_t*>(base + w.begun);
+  a.behind = reinterpret_cast<int32_t*>(base + w.behind);
   a.row = reinterpret_cast<int2*>(base + w.row);
   a.ml = reinterpret_cast<float*>(base + w.ml);
   a.o = reinterpret_cast<float*>(base + w.o);

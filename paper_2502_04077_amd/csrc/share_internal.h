@@ -66,11 +66,11 @@ struct SharedArgs {
   int q_cap, g, rows, window, n_first;
   void* out;
   SharePlan plan;
-  int2* has;                       // workspace: [n_inst] tiles of the beginning, and of the rows behind it
+  int32_t *begun, *behind;         // workspace: [n_inst] tiles of the beginning that an instance is the first member of; of the rows behind
   int2* row;                       // workspace: [2 * n_inst * rows] of a row of q: the first of its pieces, and how many
   float *ml, *o;                   // workspace: [2 * n_inst * rows + kPrefillRows * kShareWgs][2] maximum and sum, and [..][d]
 };
-struct SharedWs { size_t has, row, ml, o, total; };
+struct SharedWs { size_t begun, behind, row, ml, o, total; };
 SharedWs shared_ws(const Shape& s, int q_cap);
 
 hipError_t launch_cache_share(const Shape& s, const int32_t* group, const int32_t* shared, const SharePlan& plan, hipStream_t st);
