@@ -8,10 +8,10 @@
 //
 // out_x = sum over its sources of exp(m_x - m) o_x / sum of exp(m_x - m) l_x, for m the largest m_x.
 //
-// A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32).  All of these products, of all sources one after the other,
-// are cut into equal shares, a workgroup each, by what they cost; a workgroup leaves (m, l, o) of every piece that it has, and a second
-// launch joins them.  Where there are many rows of q, a wave has 32 of them and all rows of a tile of K and V; up to 16, which is memory-bound, all
-// waves have the same rows of q and a part of the tile each.
+// A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32); where a tile has no more than 16 rows of q, which is
+// memory-bound, in groups of 16.  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each,
+// and those of few rows into shares of a wave each: the one needs the matrix unit, the other the memory, and a CU has a workgroup of both.
+// Whoever has a share leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
 #include "cache_tiles.h"
 #include "share_internal.h"
 
@@ -87,11 +87,13 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- sources
-constexpr int kNarrowRows = 16;     // rows of q up to which the waves share them
-// What a tile of the cache counts with up to 16 rows of q, and with more; what a tile of rows of q counts beside its tiles of the cache; the
-// least share of a workgroup.
+constexpr int kNarrowRows = 16;     // rows of q up to which a wave has them alone
+constexpr int kGroup = 16;          // rows of the cache that it goes over at a time
+// What a share counts, in tenths of a microsecond: of a workgroup's time a tile of the cache, and what a tile of rows of q costs beside them; of a
+// wave's time a group, and the same.  The least shares.
 template <typename T, bool EXACT> struct Counts {
-  static constexpr int NARROW = 4, WIDE = sizeof(T) == 4 ? 12 : (EXACT ? 7 : 5), FRONT = 8, LEAST = 16;
+  static constexpr int WIDE = sizeof(T) == 4 ? 40 : (EXACT ? 20 : 14), WIDE_FRONT = 40, WIDE_LEAST = 80;
+  static constexpr int NARROW = 12, NARROW_FRONT = 40, NARROW_LEAST = 64;
 };
 
 // Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
@@ -100,22 +102,38 @@ struct Source {
   int x0, rows;          // number of its first row of q among all sources', and how many
   int p0;                // count 0: the position of the first query
   int a0, a1, p1, lo0, f;   // rows [a0, f) and [lo0, p1] are seen by one of them at least, f <= lo0; each may be empty
-  int ta, ts, tb, tiles; // tiles of TT rows: ts from ta on, the others from tb
-  __device__ __forceinline__ int tile(int u) const { return u < ts ? ta + u : tb + (u - ts); }
   __device__ __forceinline__ bool row(int j) const { return j >= a0 && j <= p1 && (j >= lo0 || j < f); }
-  __device__ __forceinline__ int q_tiles() const { return (rows + kPrefillRows - 1) / kPrefillRows; }
-  // What a tile of rows of q counts, and all of them.
-  __device__ __forceinline__ bool narrow(int t) const { return rows - t * kPrefillRows <= kNarrowRows; }
-  template <typename C> __device__ __forceinline__ unsigned size(int t) const {
-    return tiles == 0 ? 0u : C::FRONT + (unsigned)tiles * (narrow(t) ? C::NARROW : C::WIDE);
-  }
-  template <typename C> __device__ __forceinline__ unsigned long long all() const {
-    return tiles == 0 ? 0ull : (unsigned long long)(q_tiles() - 1) * size<C>(0) + size<C>(q_tiles() - 1);
-  }
+  // Tiles of rows of q: those with many rows, and one with few at the end.
+  __device__ __forceinline__ int wide() const { return rows / kPrefillRows + (rows % kPrefillRows > kNarrowRows); }
+  __device__ __forceinline__ bool narrow() const { return rows % kPrefillRows > 0 && rows % kPrefillRows <= kNarrowRows; }
 };
+// The tiles of TT cache rows that it sees: ts from ta on, the others from tb.
+struct Tiling {
+  int ta, ts, tb, n;
+  __device__ __forceinline__ int tile(int u) const { return u < ts ? ta + u : tb + (u - ts); }
+};
+template <int TT> __device__ __forceinline__ Tiling tiling_of(const Source& s) {
+  Tiling t;
+  t.ta = s.a0 / TT;
+  const int end = (s.f + TT - 1) / TT;
+  t.ts = s.f > 0 ? end - t.ta : 0;
+  t.tb = s.lo0 / TT;
+  if (t.ts > 0 && t.tb < end) t.tb = end;
+  t.n = s.a0 >= s.a1 || s.p1 < 0 || s.rows == 0 ? 0 : t.ts + (s.p1 / TT >= t.tb ? s.p1 / TT - t.tb + 1 : 0);
+  return t;
+}
+// What a tile of many rows of q counts, and the one with few.
+template <typename C, int TT> __device__ __forceinline__ unsigned wide_size(const Source& s) {
+  const int n = tiling_of<TT>(s).n;
+  return n == 0 ? 0u : C::WIDE_FRONT + (unsigned)n * C::WIDE;
+}
+template <typename C> __device__ __forceinline__ unsigned narrow_size(const Source& s) {
+  const int n = s.narrow() ? tiling_of<kGroup>(s).n : 0;
+  return n == 0 ? 0u : C::NARROW_FRONT + (unsigned)n * C::NARROW;
+}
 __device__ __forceinline__ int queries(const SharedArgs& a, int i) { return a.n_q == nullptr ? a.q_cap : clamped(a.n_q[i], 0, a.q_cap); }
 // What queries from position p_min on see of rows [a0, a1).
-template <int TT> __device__ __forceinline__ void see(const SharedArgs& a, Source& s, int a0, int a1, int p_min) {
+__device__ __forceinline__ void see(const SharedArgs& a, Source& s, int a0, int a1, int p_min) {
   s.a0 = a0;
   s.a1 = a1;
   s.p1 = a1 - 1;
@@ -128,12 +146,6 @@ template <int TT> __device__ __forceinline__ void see(const SharedArgs& a, Sourc
     s.lo0 = s.f;
     s.p1 = s.f - 1;
   }
-  s.ta = a0 / TT;
-  const int end = (s.f + TT - 1) / TT;
-  s.ts = s.f > 0 ? end - s.ta : 0;
-  s.tb = s.lo0 / TT;
-  if (s.ts > 0 && s.tb < end) s.tb = end;
-  s.tiles = a0 >= a1 || s.p1 < 0 || s.rows == 0 ? 0 : s.ts + (s.p1 / TT >= s.tb ? s.p1 / TT - s.tb + 1 : 0);
 }
 // A source that is the same for all lanes.
 __device__ __forceinline__ Source uniform(Source s) {
@@ -143,7 +155,7 @@ __device__ __forceinline__ Source uniform(Source s) {
   return s;
 }
 // Sources in their order: the groups', then the instances'.  What has to be loaded for source x is asked for together.
-template <int TT> __device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int x) {
+__device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int x) {
   const int n = a.r.n_inst, i = x < groups ? 0 : x - groups;
   const int4 line = *(x < groups ? a.plan.groups + x : a.plan.inst + i);
   const int m = queries(a, i), own = clamped(a.r.len[i], 0, a.r.t_cap);
@@ -162,21 +174,21 @@ template <int TT> __device__ __forceinline__ Source source_of(const SharedArgs& 
         const int member = clamped(a.plan.member[s.first + k], 0, n - 1), q = queries(a, member), base = clamped(a.r.len[member], 0, a.r.t_cap) - q;
         if (q > 0 && base < p) p = base;
       }
-    see<TT>(a, s, 0, S, p);
+    see(a, s, 0, S, p);
   } else {
     s.inst = i; s.first = 0; s.count = 0;
     s.rows = m * a.g;
     s.x0 = (n + i) * a.rows;
     s.p0 = own - m;
-    see<TT>(a, s, S, own, s.p0);
+    see(a, s, S, own, s.p0);
   }
   return s;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- tiles of the cache
-// The consecutive rows of a tile that a wave fetches: they lie in one page, or in two of eight rows.  In the place of rows that the source does not see,
-// which are not read, stands one that it does.  Wave-uniform, and looked up through the scalar cache: a vector load of the table's would wait
-// for the tiles under way (a tile that is seen in part then took some 8 us).
+// RW consecutive rows that a wave fetches: they lie in one page, or in two of eight rows.  In the place of rows that the source does not see, which
+// are not read, stands one that it does.  Wave-uniform, and looked up through the scalar cache: a vector load of the table's would wait for the
+// rows under way (a tile that is seen in part then took some 8 us).
 struct Fetch {
   const char *k, *v;                                       // row 0, as if all of them lay together
   long long second;                                        // and what to add for the second eight, in bytes
@@ -184,42 +196,43 @@ struct Fetch {
   bool all;
   int j0;
 };
-template <typename F> __device__ __forceinline__ Fetch fetch_of(const SharedArgs& a, const TablePages& pages, const Source& s, int t0, int wave) {
-  constexpr long long bytes = F::PIECES * 16;
+template <int RW, int PIECES> __device__ __forceinline__ Fetch fetch_of(const SharedArgs& a, const TablePages& pages, const Source& s, int j0) {
+  constexpr long long bytes = PIECES * 16;
   Fetch x;
-  x.j0 = t0 + wave * F::RW;
-  x.all = x.j0 >= s.a0 && x.j0 + F::RW - 1 <= s.p1 && (x.j0 >= s.lo0 || x.j0 + F::RW <= s.f);
-  const size_t at = pages.at(x.j0);
+  x.j0 = j0;
+  x.all = j0 >= s.a0 && j0 + RW - 1 <= s.p1 && (j0 >= s.lo0 || j0 + RW <= s.f);
+  const size_t at = pages.at(j0);
   x.k = static_cast<const char*>(a.K) + at * bytes;
   x.v = static_cast<const char*>(a.V) + at * bytes;
-  x.second = F::RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(x.j0 + 8) - at) - 8) * bytes : 0;
+  x.second = RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(j0 + 8) - at) - 8) * bytes : 0;
   x.other = 0;
   if (!x.all) {
-    const int from = x.j0 < s.f ? s.a0 : s.lo0;
-    int j = x.j0 > from ? x.j0 : from;
+    const int from = j0 < s.f ? s.a0 : s.lo0;
+    int j = j0 > from ? j0 : from;
     if (j > s.p1) j = s.p1;
     x.other = ((long long)(pages.at(j & ~7) - at) + (j & 7)) * bytes;
   }
   return x;
 }
-template <typename F, bool IS_V> __device__ __forceinline__ void send_tile(const Fetch& x, const Source& s, int wave, unsigned lds) {
+// Sends them to LDS: the lane chooses the piece, so that it lies where the swizzle says.  r0: the first one's row of the tile.
+template <int RW, typename F, bool IS_V, bool ONCE> __device__ __forceinline__ void send_rows(const Fetch& x, const Source& s, int r0, unsigned lds) {
   constexpr unsigned bytes = F::PIECES * 16;
+  constexpr int LOADS = RW * F::PIECES / 64;
   const int lane = threadIdx.x & 63;
-  const unsigned to = lds + wave * F::LOADS * 1024;
   const char* base = IS_V ? x.v : x.k;
-  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };                   // of the wave's
+  auto row = [&](int l) { return l * F::RPL + lane / F::PIECES; };
   auto piece = [&](int l) {
     const int place = lane % F::PIECES;
-    return IS_V ? F::v_place(row(l), place) : F::k_place(wave * F::RW + row(l), place);
+    return IS_V ? F::v_place(row(l), place) : F::k_place(r0 + row(l), place);
   };
   if (x.all) {
 #pragma unroll
-    for (int l = 0; l < F::LOADS; ++l) to_lds<false>(base + (l >= F::LOADS / 2 ? x.second : 0), row(l) * bytes + piece(l) * 16, to + l * 1024);
+    for (int l = 0; l < LOADS; ++l) to_lds<ONCE>(base + (l >= LOADS / 2 ? x.second : 0), row(l) * bytes + piece(l) * 16, lds + l * 1024);
   } else {
 #pragma unroll
-    for (int l = 0; l < F::LOADS; ++l) {
-      const long long at = s.row(x.j0 + row(l)) ? (l >= F::LOADS / 2 ? x.second : 0) + row(l) * (long long)bytes : x.other;
-      to_lds_from(base + at + piece(l) * 16, to + l * 1024);
+    for (int l = 0; l < LOADS; ++l) {
+      const long long at = s.row(x.j0 + row(l)) ? (l >= LOADS / 2 ? x.second : 0) + row(l) * (long long)bytes : x.other;
+      to_lds_from(base + at + piece(l) * 16, lds + l * 1024);
     }
   }
 }
@@ -231,20 +244,25 @@ template <typename F> struct Tiles {
   const u32x4* s_tiles;
   int u_begin, u_end, wave;
   unsigned buffers;
+  Tiling tiling;
   TablePages pages;
   Fetch next;
   __device__ __forceinline__ Tiles(const SharedArgs& a_, const Source& s_, int u0, int u1, const u32x4* lds) : a(a_), s(s_), s_tiles(lds), u_begin(u0), u_end(u1) {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     buffers = lds_address(s_tiles);
+    tiling = tiling_of<F::TT>(s);
     pages = pages_of(a.r, s.inst);
-    next = fetch_of<F>(a, pages, s, s.tile(u_begin) * F::TT, wave);
+    next = fetch(u_begin);
     send(u_begin);
   }
+  __device__ __forceinline__ Fetch fetch(int u) const {
+    return fetch_of<F::RW, F::PIECES>(a, pages, s, tiling.tile(u) * F::TT + wave * F::RW);
+  }
   __device__ __forceinline__ void send(int u) {            // tile u, whose rows are those of `next`
-    const unsigned to = buffers + (u % 2) * 2 * F::TILE * 16;
-    send_tile<F, false>(next, s, wave, to);
-    send_tile<F, true>(next, s, wave, to + F::TILE * 16);
-    next = fetch_of<F>(a, pages, s, s.tile(u + 1 < u_end ? u + 1 : u) * F::TT, wave);         // a tile ahead: the table's latency
+    const unsigned to = buffers + ((u % 2) * 2 * F::TILE + wave * F::LOADS * 64) * 16;
+    send_rows<F::RW, F, false, false>(next, s, wave * F::RW, to);
+    send_rows<F::RW, F, true, false>(next, s, wave * F::RW, to + F::TILE * 16);
+    next = fetch(u + 1 < u_end ? u + 1 : u);               // a tile ahead: the table's latency
   }
   template <typename WORK> __device__ __forceinline__ void each(WORK work) {                // work(t0, K, V)
     for (int u = u_begin; u < u_end; ++u) {
@@ -254,7 +272,7 @@ template <typename F> struct Tiles {
       __builtin_amdgcn_s_barrier();
       if (u + 1 < u_end) send(u + 1);
       const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
-      work(s.tile(u) * F::TT, Kt, Kt + F::TILE);
+      work(tiling.tile(u) * F::TT, Kt, Kt + F::TILE);
     }
   }
 };
@@ -484,16 +502,38 @@ __device__ __forceinline__ void wide_piece(const SharedArgs& a, const Source& s,
     }
 }
 
-// The same of up to 16 rows of q, which all waves have; a wave goes over 16 rows of each tile of the cache (fp32: two waves do), and their sums
-// are joined at the end.
-template <typename T, int D, bool EXACT>
-__device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& s, int t, int u_begin, int u_end, size_t slot, u32x4* s_tiles) {
+// Waits until no more than FIRST loads and N for each of r later groups are under way, r < R or as if it were R - 1.
+template <int N, int R, int FIRST = 0> __device__ __forceinline__ void landed_behind(int r) {
+  if constexpr (R == 1) {
+    landed<FIRST>();
+  } else {
+    if (r >= R - 1) landed<FIRST + N * (R - 1)>();
+    else landed_behind<N, R - 1, FIRST>(r);
+  }
+}
+
+// The last rows of q of a source, up to 16, over its groups [u_begin, u_end) of 16 cache rows, by a wave: RING groups of K and V are on their way to
+// LDS, past the registers.  A lane has scores of row n of q and of four cache rows, which are the second product's operand as they are, and sums of
+// 4 of each 16 dims.  slot: of the first of the rows.  lds: RING * 2 * 16 * PIECES pieces.
+template <typename T, int D, bool EXACT, int RING>
+__device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& s, int u_begin, int u_end, size_t slot, const u32x4* lds) {
   using F = Form<T, D>;
-  constexpr int KS = F::PIECES / 4, DB = D / 16, ACTIVE = F::TT / 16;      // pieces of a row that a lane has; blocks of 16 dims; waves
-  static_assert(4 * F::TILE * 16 >= ACTIVE * (16 * D + 32) * 4, "the waves' sums");
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
-  Tiles<F> tiles(a, s, u_begin, u_end, s_tiles);
-  const Query q = query_of(a, s, t * kPrefillRows + n);
+  constexpr int KS = F::PIECES / 4, DB = D / 16, N = F::PIECES / 4, GROUP = kGroup * F::PIECES;     // N: loads of a group's K, or V; GROUP: its pieces
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4, count = u_end - u_begin;
+  const Tiling tiling = tiling_of<kGroup>(s);
+  const TablePages pages = pages_of(a.r, s.inst);
+  const unsigned ring = lds_address(lds);
+  auto fetch = [&](int it) { return fetch_of<kGroup, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * kGroup); };
+  auto at = [&](int it) { return (it % RING) * 2 * GROUP; };
+  Fetch next = fetch(0);
+#pragma unroll
+  for (int it = 0; it < RING; ++it)
+    if (it < count) {
+      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      next = fetch(it + 1);
+    }
+  const Query q = query_of(a, s, s.rows / kPrefillRows * kPrefillRows + n);
   int p_min, p_max;
   positions<16>(q, &p_min, &p_max);
   u32x4 qf[KS];
@@ -506,17 +546,19 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
   const float scale = kLog2E / sqrtf((float)D);
 #pragma unroll
   for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[l]));
-  tiles.each([&](int t0, const u32x4* Kt, const u32x4* Vt) {
-    if (wave >= ACTIVE) return;
-    // Rows j0 + 4 kg + r of the tile, of query n.  fp32 products go into four sums.
-    const int j0 = 16 * wave;
+  for (int it = 0; it < count; ++it) {
+    const int t0 = tiling.tile(u_begin + it) * kGroup, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
+    const u32x4 *Kt = lds + at(it), *Vt = Kt + GROUP;
+    const bool more = it + RING < count;
+    landed_behind<2 * N, RING, N>(behind);
+    // Rows t0 + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
     constexpr int SUMS = sizeof(T) == 2 ? 1 : 4;
     float4v sums[SUMS];
 #pragma unroll
     for (int x = 0; x < SUMS; ++x) sums[x] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int l = 0; l < KS; ++l) {
-      const u32x4 k = Kt[(j0 + n) * F::PIECES + F::k_place(j0 + n, 4 * l + kg)];
+      const u32x4 k = Kt[n * F::PIECES + F::k_place(n, 4 * l + kg)];
       if constexpr (sizeof(T) == 2) {
         sums[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), sums[0], 0, 0, 0);
       } else {
@@ -530,9 +572,13 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
 #pragma unroll
       for (int r = 0; r < 4; ++r) c[r] = (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]);
     }
-    if (!all_seen<F::TT>(a, s, t0, p_min, p_max)) {
+    if (more) {
+      lds_read();
+      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
+    }
+    if (!all_seen<kGroup>(a, s, t0, p_min, p_max)) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) c[r] = hidden(a, s, q, t0 + j0 + 4 * kg + r) ? -INFINITY : c[r];
+      for (int r = 0; r < 4; ++r) c[r] = hidden(a, s, q, t0 + 4 * kg + r) ? -INFINITY : c[r];
     }
     float top = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
     top = max32(max16(top));
@@ -550,6 +596,9 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
 #pragma unroll
     for (int r = 0; r < 4; ++r) c[r] = exp2_of(c[r], scale, use);
     sum += (c[0] + c[1]) + (c[2] + c[3]);
+    // This group's V: behind it came the later groups, and the K that was just sent for.
+    if (more) landed<2 * N * (RING - 1) + N>();
+    else landed_behind<2 * N, RING>(behind);
     if constexpr (sizeof(T) == 2) {
       constexpr int PARTS = EXACT ? 3 : 1;
       typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
@@ -559,12 +608,12 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
       in_parts<PARTS>(c[2], c[3], two[1]);
 #pragma unroll
       for (int w = 0; w < PARTS; ++w) pb[w] = __builtin_bit_cast(short4v, u32x2{two[0][w], two[1][w]});
-      const int r = j0 + 4 * kg + (n >> 2);
+      const int r = 4 * kg + (n >> 2);
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const int col = 16 * b + 4 * (n & 3);
-        const char* at = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
-        const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+        const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
+        const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
 #pragma unroll
         for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pb[w], o[b], 0, 0, 0);
       }
@@ -574,173 +623,202 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vf[(j0 + 4 * kg + r) * D + 16 * b + n], c[r], o[b], 0, 0, 0);
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vf[(4 * kg + r) * D + 16 * b + n], c[r], o[b], 0, 0, 0);
     }
-  });
-  // The waves' sums: [wave][16][D], and their maxima and sums behind.
-  float* s_o = reinterpret_cast<float*>(s_tiles);
-  float* s_ml = s_o + ACTIVE * 16 * D;
+    if (more) {
+      lds_read();
+      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      next = fetch(it + RING + 1);
+    }
+  }
   sum = sum32(sum16(sum));
-  __syncthreads();                                         // everybody is done with the tiles
-  if (wave < ACTIVE) {
-#pragma unroll
-    for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(s_o + (wave * 16 + n) * D + 16 * b + 4 * kg) = o[b];
-    if (kg == 0) {
-      s_ml[(wave * 16 + n) * 2] = m;
-      s_ml[(wave * 16 + n) * 2 + 1] = sum;
-    }
+  if (!q.real) return;
+  slot += n;
+  if (kg == 0) {
+    a.ml[slot * 2] = m;
+    a.ml[slot * 2 + 1] = sum;
   }
-  __syncthreads();
-  const int rows = s.rows - t * kPrefillRows;
-  for (int x = tid; x < rows * (D / 4); x += kThreads) {
-    const int row = x / (D / 4), e = x % (D / 4) * 4;
-    float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < ACTIVE; ++w) top = fmaxf(top, s_ml[(w * 16 + row) * 2]);
-    const float use = top == -INFINITY ? 0.f : top;
-    float4v y = {0.f, 0.f, 0.f, 0.f};
-    float all = 0.f;
-#pragma unroll
-    for (int w = 0; w < ACTIVE; ++w) {
-      const float f = exp2_fast(s_ml[(w * 16 + row) * 2] - use);
-      all += f * s_ml[(w * 16 + row) * 2 + 1];
-      const float4v z = *reinterpret_cast<const float4v*>(s_o + (w * 16 + row) * D + e);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] += f * z[r];
-    }
-    *reinterpret_cast<float4v*>(a.o + (slot + row) * D + e) = y;
-    if (e == 0) {
-      a.ml[(slot + row) * 2] = top;
-      a.ml[(slot + row) * 2 + 1] = all;
-    }
-  }
+  for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(a.o + slot * D + 16 * b + 4 * kg) = o[b];
 }
 
-// A workgroup's share of all products, piece by piece.
+// Shares of the products of many rows of q, a workgroup each, and of those of few, a wave each.
 template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 8, kListed = 32;
-  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
-  __shared__ unsigned long long s_wave[kWaves], s_from;
-  __shared__ int s_first;
-  __shared__ Source s_source[kListed];                                    // from s_first on
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kHeld = 8, kListed = 16, RING = 4 * F::TILE / (kWaves * 2 * kGroup * F::PIECES);
+  static_assert(RING >= 1 && RING * kWaves * 2 * kGroup * F::PIECES <= 4 * F::TILE, "LDS");
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][16 rows]
+  __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[kWaves];
+  __shared__ int s_first[kWaves];
+  __shared__ Source s_source[kWaves][kListed];                            // from s_first on
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // Where this workgroup's share begins: every thread sums up consecutive sources.
+  // All that there is to do: every thread sums up consecutive sources.
   const int groups = clamped(*a.plan.count, 0, a.r.n_inst), sources = groups + a.r.n_inst, chunk = (sources + kThreads - 1) / kThreads;
   const int i_begin = tid * chunk < sources ? tid * chunk : sources, i_end = i_begin + chunk < sources ? i_begin + chunk : sources;
-  unsigned long long size[kHeld], mine = 0;
-  int tiles[kHeld];
+  unsigned long long wide[kHeld], my_wide = 0, my_narrow = 0;
+  unsigned narrow[kHeld];
+  bool seen[kHeld];
+  auto sizes = [&](const Source& s, unsigned long long* w, unsigned* n) {
+    *w = (unsigned long long)wide_size<C, F::TT>(s) * (unsigned)s.wide();
+    *n = narrow_size<C>(s);
+  };
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) {
-    size[k] = 0;
-    tiles[k] = 0;
+    wide[k] = 0;
+    narrow[k] = 0;
+    seen[k] = false;
   }
   if (chunk <= kHeld) {
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
       if (k < chunk) {
-        const int i = i_begin + k < i_end ? i_begin + k : sources - 1;    // (the loads of all of them are under way together)
-        const Source s = source_of<F::TT>(a, groups, i);
-        tiles[k] = s.tiles;
-        size[k] = i_begin + k < i_end ? s.template all<C>() : 0;
-        mine += size[k];
+        const bool mine = i_begin + k < i_end;
+        const Source s = source_of(a, groups, mine ? i_begin + k : sources - 1);          // (the loads of all of them are under way together)
+        sizes(s, &wide[k], &narrow[k]);
+        seen[k] = mine && tiling_of<kGroup>(s).n > 0;
+        wide[k] = mine ? wide[k] : 0;
+        narrow[k] = mine ? narrow[k] : 0;
+        my_wide += wide[k];
+        my_narrow += narrow[k];
       }
   } else {
-    for (int i = i_begin; i < i_end; ++i) mine += source_of<F::TT>(a, groups, i).template all<C>();
+    for (int i = i_begin; i < i_end; ++i) {
+      unsigned long long w;
+      unsigned n;
+      sizes(source_of(a, groups, i), &w, &n);
+      my_wide += w;
+      my_narrow += n;
+    }
   }
-  unsigned long long upto = mine;
+  unsigned long long upto_wide = my_wide, upto_narrow = my_narrow;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long y = __shfl_up(upto, o, 64);
-    if (lane >= o) upto += y;
+    const unsigned long long x = __shfl_up(upto_wide, o, 64), y = __shfl_up(upto_narrow, o, 64);
+    if (lane >= o) {
+      upto_wide += x;
+      upto_narrow += y;
+    }
   }
-  if (lane == 63) s_wave[wave] = upto;
+  if (lane == 63) {
+    s_wide[wave] = upto_wide;
+    s_narrow[wave] = upto_narrow;
+  }
   __syncthreads();
-  unsigned long long all = 0, ahead = upto - mine;
+  unsigned long long all_wide = 0, all_narrow = 0, at_wide = upto_wide - my_wide, at_narrow = upto_narrow - my_narrow;
   for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) ahead += s_wave[w];
-    all += s_wave[w];
+    if (w < wave) {
+      at_wide += s_wide[w];
+      at_narrow += s_narrow[w];
+    }
+    all_wide += s_wide[w];
+    all_narrow += s_narrow[w];
   }
-  const unsigned long long share = (all + gridDim.x - 1) / gridDim.x;
-  const unsigned per = share < C::LEAST ? C::LEAST : (unsigned)share;
-  const unsigned long long begin = (unsigned long long)blockIdx.x * per;
-  unsigned left = begin < all ? (begin + per < all ? per : (unsigned)(all - begin)) : 0;
-  if (left > 0 && ahead <= begin && begin < ahead + mine) {
-    unsigned long long at = ahead;
+  // Workgroups for the one and for the other, by the time that both take.
+  const float part = (float)all_wide / ((float)all_wide + 0.25f * (float)all_narrow);     // (NaN where there is nothing to do)
+  int wide_wgs = (int)(part * (float)gridDim.x + 0.5f);
+  if (all_wide > 0 && wide_wgs < 1) wide_wgs = 1;
+  if (all_narrow > 0 && wide_wgs > (int)gridDim.x - 1) wide_wgs = (int)gridDim.x - 1;
+  if (all_wide == 0) wide_wgs = 0;
+  wide_wgs = __builtin_amdgcn_readfirstlane(wide_wgs);
+  const bool is_wide = (int)blockIdx.x < wide_wgs;
+  const unsigned long long all = is_wide ? all_wide : all_narrow;
+  const int sharers = is_wide ? wide_wgs : kWaves * ((int)gridDim.x - wide_wgs);
+  const int least = is_wide ? C::WIDE_LEAST : C::NARROW_LEAST;
+  const unsigned long long share = (all + sharers - 1) / sharers;
+  const unsigned per = share < (unsigned)least ? least : (unsigned)share;
+  const int first_sharer = is_wide ? (int)blockIdx.x : kWaves * ((int)blockIdx.x - wide_wgs);      // of this workgroup's
+  // Where the shares begin: s_first[0], or every wave's.
+  if (tid < kWaves) s_first[tid] = sources;
+  __syncthreads();
+  const unsigned long long from_here = is_wide ? at_wide : at_narrow, to_here = from_here + (is_wide ? my_wide : my_narrow);
+  for (int w = 0; w < (is_wide ? 1 : kWaves); ++w) {
+    const unsigned long long begin = (unsigned long long)(first_sharer + w) * per;
+    if (from_here > begin || begin >= to_here) continue;
+    unsigned long long at = from_here;
     if (chunk <= kHeld) {
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
-        if (at <= begin && begin < at + size[k]) {
-          s_first = i_begin + k;
-          s_from = begin - at;
+        const unsigned long long n = is_wide ? wide[k] : narrow[k];
+        if (at <= begin && begin < at + n) {
+          s_first[w] = i_begin + k;
+          s_from[w] = begin - at;
         }
-        at += size[k];
+        at += n;
       }
     } else {
       for (int i = i_begin; i < i_end; ++i) {
-        const unsigned long long n = source_of<F::TT>(a, groups, i).template all<C>();
+        unsigned long long x;
+        unsigned y;
+        sizes(source_of(a, groups, i), &x, &y);
+        const unsigned long long n = is_wide ? x : y;
         if (at <= begin && begin < at + n) {
-          s_first = i;
-          s_from = begin - at;
+          s_first[w] = i;
+          s_from[w] = begin - at;
         }
         at += n;
       }
     }
   }
   // Which sources have tiles, for the join: the groups by their first member, the instances.
-  auto note = [&](int x, int n) {
-    if (x < groups) a.begun[clamped(a.plan.groups[x].x, 0, a.r.n_inst - 1)] = n;
-    else a.behind[x - groups] = n;
+  auto note = [&](int x, bool some) {
+    if (x < groups) a.begun[clamped(a.plan.groups[x].x, 0, a.r.n_inst - 1)] = some;
+    else a.behind[x - groups] = some;
   };
   if (chunk <= kHeld) {
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-      if (i_begin + k < i_end && (unsigned)(i_begin + k) % gridDim.x == blockIdx.x) note(i_begin + k, tiles[k]);
+      if (i_begin + k < i_end && (unsigned)(i_begin + k) % gridDim.x == blockIdx.x) note(i_begin + k, seen[k]);
   } else {
-    for (int x = blockIdx.x * kThreads + tid; x < sources; x += gridDim.x * kThreads) note(x, source_of<F::TT>(a, groups, x).tiles);
+    for (int x = blockIdx.x * kThreads + tid; x < sources; x += gridDim.x * kThreads) note(x, tiling_of<kGroup>(source_of(a, groups, x)).n > 0);
   }
-  if (left == 0) return;
   __syncthreads();
-  const int x_first = __builtin_amdgcn_readfirstlane(s_first);
-  if (tid < kListed) s_source[tid] = source_of<F::TT>(a, groups, x_first + tid < sources ? x_first + tid : sources - 1);
+  const int w = is_wide ? 0 : wave, x_first = __builtin_amdgcn_readfirstlane(s_first[w]);
+  if (!is_wide && lane < kListed) s_source[wave][lane] = source_of(a, groups, x_first + lane < sources ? x_first + lane : sources - 1);
+  if (is_wide && tid < kListed) s_source[0][tid] = source_of(a, groups, x_first + tid < sources ? x_first + tid : sources - 1);
   __syncthreads();
-  unsigned long long from = s_from;
+  if (x_first >= sources) return;
+  const unsigned long long begin = (unsigned long long)(first_sharer + w) * per;
+  unsigned left = begin + per < all ? per : (unsigned)(all - begin);
+  unsigned long long from = s_from[w];
+  // A small tile of rows of q belongs to the share that it begins in.
+  const unsigned small = per / 4 > (unsigned)least ? per / 4 : (unsigned)least;
   for (int x = x_first; left > 0 && x < sources; ++x, from = 0) {
-    const Source s = uniform(x - x_first < kListed ? s_source[x - x_first] : source_of<F::TT>(a, groups, x));
-    const unsigned long long end = s.template all<C>();
+    const Source s = uniform(x - x_first < kListed ? s_source[w][x - x_first] : source_of(a, groups, x));
+    const unsigned size = is_wide ? wide_size<C, F::TT>(s) : narrow_size<C>(s);
+    const int tiles = size == 0 ? 0 : (is_wide ? s.wide() : 1);            // of rows of q
+    const unsigned long long end = (unsigned long long)size * (unsigned)tiles;
     while (left > 0 && from < end) {
       // Tile t of its rows of q, from `r` on.
-      const unsigned first_size = s.template size<C>(0);
-      const int last = s.q_tiles() - 1;
-      const int t = __builtin_amdgcn_readfirstlane(last == 0 || from / first_size >= (unsigned)last ? last : (int)(from / first_size));
-      const unsigned r = (unsigned)(from - (unsigned long long)t * first_size), of_tile = s.template size<C>(t);
-      // A small one belongs to the workgroup that it begins in.
-      const bool whole = of_tile <= (per / 4 > C::LEAST ? per / 4 : C::LEAST);
-      const unsigned n = whole || of_tile - r < left ? of_tile - r : left;
+      const int t = __builtin_amdgcn_readfirstlane(tiles == 1 ? 0 : (int)(from / size));
+      const unsigned r = (unsigned)(from - (unsigned long long)t * size);
+      const bool whole = size <= small;
+      const unsigned n = __builtin_amdgcn_readfirstlane(whole || size - r < left ? size - r : left);
       from += n;
       left -= n < left ? n : left;
       if (whole && r > 0) continue;
-      const bool narrow = s.narrow(t);
-      const unsigned each = narrow ? C::NARROW : C::WIDE;
-      const int u_begin = r <= C::FRONT ? 0 : (int)((r - C::FRONT + each - 1) / each);
-      const int u_end = r + n <= C::FRONT ? 0 : (int)((r + n - C::FRONT + each - 1) / each);
-      const size_t x0 = (size_t)s.x0 + (size_t)t * kPrefillRows, slot = x0 + (size_t)kPrefillRows * blockIdx.x;
-      const int rows = s.rows - t * kPrefillRows < kPrefillRows ? s.rows - t * kPrefillRows : kPrefillRows;
-      __syncthreads();                                     // everybody is done with the piece before
+      const unsigned front = is_wide ? C::WIDE_FRONT : C::NARROW_FRONT, each = is_wide ? C::WIDE : C::NARROW;
+      const int u_begin = r <= front ? 0 : (int)((r - front + each - 1) / each);
+      const int u_end = r + n <= front ? 0 : (int)((r + n - front + each - 1) / each);
+      const int row0 = is_wide ? t * kPrefillRows : s.rows / kPrefillRows * kPrefillRows;
+      const int rows = s.rows - row0 < kPrefillRows ? s.rows - row0 : kPrefillRows, my_row = is_wide ? tid : lane;
+      const size_t x0 = (size_t)s.x0 + row0;
+      const size_t slot = is_wide ? x0 + (size_t)kPrefillRows * first_sharer : (size_t)a.narrow0 + x0 + (size_t)kNarrowRows * (first_sharer + wave);
+      const int parts = 1 + (int)((size - n + per - 1) / per);
+      if (is_wide) __syncthreads();                        // everybody is done with the piece before
       if (u_begin >= u_end) {                              // (what is in front alone)
-        if (tid < rows) {
-          a.ml[(slot + tid) * 2] = -INFINITY;
-          a.ml[(slot + tid) * 2 + 1] = 0.f;
+        if (my_row < rows) {
+          a.ml[(slot + my_row) * 2] = -INFINITY;
+          a.ml[(slot + my_row) * 2 + 1] = 0.f;
         }
-      } else if (narrow) {
-        narrow_piece<T, D, EXACT>(a, s, t, u_begin, u_end, slot, s_tiles);
-      } else {
+      } else if (is_wide) {
         wide_piece<T, D, EXACT>(a, s, t, u_begin, u_end, slot, s_tiles);
+      } else {
+        narrow_piece<T, D, EXACT, RING>(a, s, u_begin, u_end, slot, s_tiles + wave * RING * 2 * kGroup * F::PIECES);
       }
-      if (r == 0 && tid < rows) a.row[x0 + tid] = make_int2((int)slot + tid, 1 + (int)((of_tile - n + per - 1) / per));
+      if (r == 0 && my_row < rows) a.row[x0 + my_row] = make_int2((int)slot + my_row, is_wide ? parts : -parts);
     }
   }
 }
@@ -756,8 +834,9 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
   const bool some = line.z > 1 && (unsigned)pos < (unsigned)a.r.n_inst && a.begun[clamped(line.x, 0, a.r.n_inst - 1)] > 0;
   const int2 first = some ? a.row[(size_t)pos * a.rows + row] : make_int2(0, 0);
   const int2 own = behind > 0 ? a.row[((size_t)a.r.n_inst + inst) * a.rows + row] : make_int2(0, 0);
-  const int parts = first.y + own.y;
-  auto slot = [&](int p) { return p < first.y ? (size_t)first.x + (size_t)kPrefillRows * p : (size_t)own.x + (size_t)kPrefillRows * (p - first.y); };
+  const int ahead = first.y < 0 ? -first.y : first.y, parts = ahead + (own.y < 0 ? -own.y : own.y);
+  const int step = first.y < 0 ? kNarrowRows : kPrefillRows, own_step = own.y < 0 ? kNarrowRows : kPrefillRows;
+  auto slot = [&](int p) { return p < ahead ? (size_t)first.x + (size_t)step * p : (size_t)own.x + (size_t)own_step * (p - ahead); };
   float top = -INFINITY;
   for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.ml[slot(p) * 2]);
   top = wave_max(top);

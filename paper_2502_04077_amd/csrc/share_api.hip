@@ -36,7 +36,7 @@ SharedWs shared_ws(const Shape& s, int q_cap) {
   SharedWs w;
   size_t o = 0;
   auto take = [&o](size_t bytes) { const size_t at = o; o += (bytes + 15) / 16 * 16; return at; };
-  const size_t rows = (size_t)2 * s.n_inst * q_cap * s.g, pieces = rows + (size_t)kPrefillRows * kShareWgs;
+  const size_t rows = (size_t)2 * s.n_inst * q_cap * s.g, pieces = shared_pieces(s, q_cap);
   w.begun = take((size_t)s.n_inst * 4);
   w.behind = take((size_t)s.n_inst * 4);
   w.row = take(rows * 8);
@@ -69,7 +69,7 @@ static ap::Pages pages_of(const Shape& s, void* K, void* V, int32_t* table, int3
 // Chunks of so few rows of q that a tile of kPrefillRows has several instances'; and all rows are numbered in 32 bits, and their pieces.
 static bool few_rows(const Shape& s, int32_t q_cap) {
   return q_cap * s.g <= ap::kPrefillRows / 2 &&
-         2ll * s.n_inst * q_cap * s.g + (long long)ap::kPrefillRows * ap::kShareWgs < (1ll << 31);
+         ap::shared_pieces(s, q_cap) < (size_t)1 << 31;
 }
 static hipError_t launch_shared(const Shape& s, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
                                 const void* plan, int32_t window, int32_t n_first, void* out, bool decode, void* ws, void* stream) {
@@ -77,7 +77,7 @@ static hipError_t launch_shared(const Shape& s, const void* q, const int32_t* n_
   char* base = static_cast<char*>(ws);
   ap::SharedArgs a;
   a.r = rows_of(s, len);
-  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.g = s.g; a.rows = q_cap * s.g;
+  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.g = s.g; a.rows = q_cap * s.g; a.narrow0 = (int)ap::shared_narrow0(s, q_cap);
   a.window = seen_window(s, window); a.n_first = seen_first(s, n_first); a.out = out;
   a.plan = ap::share_plan(s, const_cast<void*>(plan));
   a.begun = reinterpret_cast<int32_t*>(base + w.begun);

@@ -58,18 +58,24 @@ SharePlan share_plan(const Shape& s, void* plan);
 constexpr int kShareWgs = 512;
 
 // Rows of q, `rows` an instance, are numbered twice: those of the groups' members one after the other, x < n_inst * rows, for the groups' beginnings; and
-// n_inst * rows + those of the instances for what lies behind.  The piece that workgroup w leaves of row x is number x + kPrefillRows * w.
+// n_inst * rows + those of the instances for what lies behind.  The piece that workgroup w leaves of row x is number x + kPrefillRows * w; that
+// wave w leaves of a tile of few rows, narrow0 + x + 16 * w.
 struct SharedArgs {
   CacheRows r;
   const void *q, *K, *V;
   const int32_t* n_q;              // [n_inst], or null: q_cap each
-  int q_cap, g, rows, window, n_first;
+  int q_cap, g, rows, window, n_first, narrow0;
   void* out;
   SharePlan plan;
-  int32_t *begun, *behind;         // workspace: [n_inst] tiles of the beginning that an instance is the first member of; of the rows behind
-  int2* row;                       // workspace: [2 * n_inst * rows] of a row of q: the first of its pieces, and how many
-  float *ml, *o;                   // workspace: [2 * n_inst * rows + kPrefillRows * kShareWgs][2] maximum and sum, and [..][d]
+  int32_t *begun, *behind;         // workspace: [n_inst] whether there are pieces of the beginning that an instance is the first member of; of the rows behind
+  int2* row;                       // workspace: [2 * n_inst * rows] of a row of q: the first of its pieces, and how many (a wave's: negative)
+  float *ml, *o;                   // workspace: [shared_pieces][2] maximum and sum, and [..][d]
 };
+// Pieces: those of workgroups, in front of narrow0, and of waves.
+inline size_t shared_narrow0(const Shape& s, int q_cap) { return (size_t)2 * s.n_inst * q_cap * s.g + (size_t)kPrefillRows * kShareWgs; }
+inline size_t shared_pieces(const Shape& s, int q_cap) {
+  return shared_narrow0(s, q_cap) + (size_t)2 * s.n_inst * q_cap * s.g + (size_t)16 * 4 * kShareWgs;
+}
 struct SharedWs { size_t begun, behind, row, ml, o, total; };
 SharedWs shared_ws(const Shape& s, int q_cap);
 
