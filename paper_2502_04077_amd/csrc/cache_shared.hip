@@ -9,9 +9,9 @@
 // out_x = sum over its sources of exp(m_x - m) o_x / sum of exp(m_x - m) l_x, for m the largest m_x.
 //
 // A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32); where a tile has no more than 16 rows of q, which is
-// memory-bound, in groups of 16.  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each,
-// and those of few rows into shares of a wave each: the one needs the matrix unit, the other the memory, and a CU has a workgroup of both.
-// Whoever has a share leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
+// memory-bound, in groups of 32 (16).  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each,
+// and those of few rows into shares of a wave each; a workgroup has one of the former and then its waves one of the latter each.  Whoever has a share
+// leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
 #include "cache_tiles.h"
 #include "share_internal.h"
 
@@ -88,12 +88,13 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
 
 // ---------------------------------------------------------------------------------------------------------------- sources
 constexpr int kNarrowRows = 16;     // rows of q up to which a wave has them alone
-constexpr int kGroup = 16;          // rows of the cache that it goes over at a time
+template <typename T> constexpr int kGroup = sizeof(T) == 2 ? 32 : 16;      // rows of the cache that it goes over at a time
+constexpr int kSharedLds = 64 * 1024;       // two workgroups a CU
 // What a share counts, in tenths of a microsecond: of a workgroup's time a tile of the cache, and what a tile of rows of q costs beside them; of a
 // wave's time a group, and the same.  The least shares.
 template <typename T, bool EXACT> struct Counts {
   static constexpr int WIDE = sizeof(T) == 4 ? 40 : (EXACT ? 20 : 14), WIDE_FRONT = 40, WIDE_LEAST = 80;
-  static constexpr int NARROW = 12, NARROW_FRONT = 40, NARROW_LEAST = 64;
+  static constexpr int NARROW = sizeof(T) == 4 ? 16 : 20, NARROW_FRONT = 40, NARROW_LEAST = 64;
 };
 
 // Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
@@ -127,8 +128,8 @@ template <typename C, int TT> __device__ __forceinline__ unsigned wide_size(cons
   const int n = tiling_of<TT>(s).n;
   return n == 0 ? 0u : C::WIDE_FRONT + (unsigned)n * C::WIDE;
 }
-template <typename C> __device__ __forceinline__ unsigned narrow_size(const Source& s) {
-  const int n = s.narrow() ? tiling_of<kGroup>(s).n : 0;
+template <typename C, int TT> __device__ __forceinline__ unsigned narrow_size(const Source& s) {
+  const int n = s.narrow() ? tiling_of<TT>(s).n : 0;
   return n == 0 ? 0u : C::NARROW_FRONT + (unsigned)n * C::NARROW;
 }
 __device__ __forceinline__ int queries(const SharedArgs& a, int i) { return a.n_q == nullptr ? a.q_cap : clamped(a.n_q[i], 0, a.q_cap); }
@@ -154,19 +155,19 @@ __device__ __forceinline__ Source uniform(Source s) {
   for (int k = 0; k < (int)(sizeof(Source) / 4); ++k) w[k] = __builtin_amdgcn_readfirstlane(w[k]);
   return s;
 }
-// Sources in their order: the groups', then the instances'.  What has to be loaded for source x is asked for together.
-__device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int x) {
-  const int n = a.r.n_inst, i = x < groups ? 0 : x - groups;
-  const int4 line = *(x < groups ? a.plan.groups + x : a.plan.inst + i);
+// Sources in their order: the instances', then the groups'.  What has to be loaded for source x is asked for together.
+__device__ __forceinline__ Source source_of(const SharedArgs& a, int x) {
+  const int n = a.r.n_inst, i = x < n ? x : 0;
+  const int4 line = *(x < n ? a.plan.inst + i : a.plan.groups + (x - n));
   const int m = queries(a, i), own = clamped(a.r.len[i], 0, a.r.t_cap);
   const bool several = line.z > 1 && (unsigned)line.x < (unsigned)n && line.y >= 0 && line.z <= n - line.y;
   const int lead = clamped(a.r.len[several ? line.x : i], 0, a.r.t_cap);
   const int S = several ? clamped(line.w, 0, lead) : 0;
   Source s;
-  if (x < groups) {
+  if (x >= n) {
     s.inst = line.x; s.first = line.y; s.count = line.z;
     s.rows = several ? line.z * a.rows : 0;
-    s.x0 = line.y * a.rows;
+    s.x0 = (n + line.y) * a.rows;
     s.p0 = 0;
     int p = 0x7fffffff;                                    // the lowest position of a query
     if (S > 0 && a.window > 0)
@@ -178,7 +179,7 @@ __device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int
   } else {
     s.inst = i; s.first = 0; s.count = 0;
     s.rows = m * a.g;
-    s.x0 = (n + i) * a.rows;
+    s.x0 = i * a.rows;
     s.p0 = own - m;
     see(a, s, S, own, s.p0);
   }
@@ -186,25 +187,28 @@ __device__ __forceinline__ Source source_of(const SharedArgs& a, int groups, int
 }
 
 // ---------------------------------------------------------------------------------------------------------------- tiles of the cache
-// RW consecutive rows that a wave fetches: they lie in one page, or in two of eight rows.  In the place of rows that the source does not see, which
-// are not read, stands one that it does.  Wave-uniform, and looked up through the scalar cache: a vector load of the table's would wait for the
+// RW consecutive rows that a wave fetches, which may lie in several pages of eight rows and more.  In the place of rows that the source does not see,
+// which are not read, stands one that it does.  Wave-uniform, and looked up through the scalar cache: a vector load of the table's would wait for the
 // rows under way (a tile that is seen in part then took some 8 us).
-struct Fetch {
+template <int RW> struct Fetch {
+  static constexpr int RUNS = (RW + 7) / 8;
   const char *k, *v;                                       // row 0, as if all of them lay together
-  long long second;                                        // and what to add for the second eight, in bytes
+  long long run[RUNS];                                     // and what to add for every eight, in bytes
   long long other;                                         // the one that stands in, relative to row 0
   bool all;
   int j0;
 };
-template <int RW, int PIECES> __device__ __forceinline__ Fetch fetch_of(const SharedArgs& a, const TablePages& pages, const Source& s, int j0) {
+template <int RW, int PIECES> __device__ __forceinline__ Fetch<RW> fetch_of(const SharedArgs& a, const TablePages& pages, const Source& s, int j0) {
   constexpr long long bytes = PIECES * 16;
-  Fetch x;
+  Fetch<RW> x;
   x.j0 = j0;
   x.all = j0 >= s.a0 && j0 + RW - 1 <= s.p1 && (j0 >= s.lo0 || j0 + RW <= s.f);
   const size_t at = pages.at(j0);
   x.k = static_cast<const char*>(a.K) + at * bytes;
   x.v = static_cast<const char*>(a.V) + at * bytes;
-  x.second = RW == 16 && pages.lb == 3 && pages.table != nullptr ? ((long long)(pages.at(j0 + 8) - at) - 8) * bytes : 0;
+#pragma unroll
+  for (int e = 0; e < Fetch<RW>::RUNS; ++e)
+    x.run[e] = pages.table == nullptr || (8 * e) >> pages.lb == 0 ? 0 : ((long long)(pages.at(j0 + 8 * e) - at) - 8 * e) * bytes;
   x.other = 0;
   if (!x.all) {
     const int from = j0 < s.f ? s.a0 : s.lo0;
@@ -215,7 +219,7 @@ template <int RW, int PIECES> __device__ __forceinline__ Fetch fetch_of(const Sh
   return x;
 }
 // Sends them to LDS: the lane chooses the piece, so that it lies where the swizzle says.  r0: the first one's row of the tile.
-template <int RW, typename F, bool IS_V, bool ONCE> __device__ __forceinline__ void send_rows(const Fetch& x, const Source& s, int r0, unsigned lds) {
+template <int RW, typename F, bool IS_V, bool ONCE> __device__ __forceinline__ void send_rows(const Fetch<RW>& x, const Source& s, int r0, unsigned lds) {
   constexpr unsigned bytes = F::PIECES * 16;
   constexpr int LOADS = RW * F::PIECES / 64;
   const int lane = threadIdx.x & 63;
@@ -227,11 +231,11 @@ template <int RW, typename F, bool IS_V, bool ONCE> __device__ __forceinline__ v
   };
   if (x.all) {
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l) to_lds<ONCE>(base + (l >= LOADS / 2 ? x.second : 0), row(l) * bytes + piece(l) * 16, lds + l * 1024);
+    for (int l = 0; l < LOADS; ++l) to_lds<ONCE>(base + x.run[l * F::RPL / 8], row(l) * bytes + piece(l) * 16, lds + l * 1024);
   } else {
 #pragma unroll
     for (int l = 0; l < LOADS; ++l) {
-      const long long at = s.row(x.j0 + row(l)) ? (l >= LOADS / 2 ? x.second : 0) + row(l) * (long long)bytes : x.other;
+      const long long at = s.row(x.j0 + row(l)) ? x.run[l * F::RPL / 8] + row(l) * (long long)bytes : x.other;
       to_lds_from(base + at + piece(l) * 16, lds + l * 1024);
     }
   }
@@ -246,7 +250,7 @@ template <typename F> struct Tiles {
   unsigned buffers;
   Tiling tiling;
   TablePages pages;
-  Fetch next;
+  Fetch<F::RW> next;
   __device__ __forceinline__ Tiles(const SharedArgs& a_, const Source& s_, int u0, int u1, const u32x4* lds) : a(a_), s(s_), s_tiles(lds), u_begin(u0), u_end(u1) {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     buffers = lds_address(s_tiles);
@@ -255,7 +259,7 @@ template <typename F> struct Tiles {
     next = fetch(u_begin);
     send(u_begin);
   }
-  __device__ __forceinline__ Fetch fetch(int u) const {
+  __device__ __forceinline__ Fetch<F::RW> fetch(int u) const {
     return fetch_of<F::RW, F::PIECES>(a, pages, s, tiling.tile(u) * F::TT + wave * F::RW);
   }
   __device__ __forceinline__ void send(int u) {            // tile u, whose rows are those of `next`
@@ -512,25 +516,26 @@ template <int N, int R, int FIRST = 0> __device__ __forceinline__ void landed_be
   }
 }
 
-// The last rows of q of a source, up to 16, over its groups [u_begin, u_end) of 16 cache rows, by a wave: RING groups of K and V are on their way to
-// LDS, past the registers.  A lane has scores of row n of q and of four cache rows, which are the second product's operand as they are, and sums of
-// 4 of each 16 dims.  slot: of the first of the rows.  lds: RING * 2 * 16 * PIECES pieces.
+// The last rows of q of a source, up to 16, over its groups [u_begin, u_end) of cache rows, by a wave: RING groups of K and V are on their way to
+// LDS, past the registers.  A lane has scores of row n of q and of four of each 16 cache rows, which are the second product's operand as they are, and
+// sums of four of each 16 dims.  slot: of the first of the rows.  lds: RING groups.
 template <typename T, int D, bool EXACT, int RING>
 __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& s, int u_begin, int u_end, size_t slot, const u32x4* lds) {
   using F = Form<T, D>;
-  constexpr int KS = F::PIECES / 4, DB = D / 16, N = F::PIECES / 4, GROUP = kGroup * F::PIECES;     // N: loads of a group's K, or V; GROUP: its pieces
+  constexpr int ROWS = kGroup<T>, KB = ROWS / 16, KS = F::PIECES / 4, DB = D / 16;                  // of a group; blocks of 16 rows, of 16 dims
+  constexpr int GROUP = ROWS * F::PIECES, N = GROUP / 64;  // pieces of a group's K, or V, and loads
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4, count = u_end - u_begin;
-  const Tiling tiling = tiling_of<kGroup>(s);
+  const Tiling tiling = tiling_of<ROWS>(s);
   const TablePages pages = pages_of(a.r, s.inst);
   const unsigned ring = lds_address(lds);
-  auto fetch = [&](int it) { return fetch_of<kGroup, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * kGroup); };
+  auto fetch = [&](int it) { return fetch_of<ROWS, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * ROWS); };
   auto at = [&](int it) { return (it % RING) * 2 * GROUP; };
-  Fetch next = fetch(0);
+  Fetch<ROWS> next = fetch(0);
 #pragma unroll
   for (int it = 0; it < RING; ++it)
     if (it < count) {
-      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
-      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      send_rows<ROWS, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<ROWS, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
       next = fetch(it + 1);
     }
   const Query q = query_of(a, s, s.rows / kPrefillRows * kPrefillRows + n);
@@ -547,40 +552,48 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
 #pragma unroll
   for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[l]));
   for (int it = 0; it < count; ++it) {
-    const int t0 = tiling.tile(u_begin + it) * kGroup, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
+    const int t0 = tiling.tile(u_begin + it) * ROWS, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
     const u32x4 *Kt = lds + at(it), *Vt = Kt + GROUP;
     const bool more = it + RING < count;
     landed_behind<2 * N, RING, N>(behind);
-    // Rows t0 + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
+    // Rows t0 + 16 b + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
     constexpr int SUMS = sizeof(T) == 2 ? 1 : 4;
-    float4v sums[SUMS];
+    float4v c[KB];
 #pragma unroll
-    for (int x = 0; x < SUMS; ++x) sums[x] = float4v{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < KB; ++b) {
+      float4v sums[SUMS];
 #pragma unroll
-    for (int l = 0; l < KS; ++l) {
-      const u32x4 k = Kt[n * F::PIECES + F::k_place(n, 4 * l + kg)];
-      if constexpr (sizeof(T) == 2) {
-        sums[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), sums[0], 0, 0, 0);
-      } else {
+      for (int x = 0; x < SUMS; ++x) sums[x] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sums[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), sums[e], 0, 0, 0);
+      for (int l = 0; l < KS; ++l) {
+        const u32x4 k = Kt[(16 * b + n) * F::PIECES + F::k_place(16 * b + n, 4 * l + kg)];
+        if constexpr (sizeof(T) == 2) {
+          sums[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), sums[0], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sums[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), sums[e], 0, 0, 0);
+        }
       }
-    }
-    float4v c = sums[0];
-    if constexpr (SUMS == 4) {
+      c[b] = sums[0];
+      if constexpr (SUMS == 4) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) c[r] = (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]);
+        for (int r = 0; r < 4; ++r) c[b][r] = (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]);
+      }
     }
     if (more) {
       lds_read();
-      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<ROWS, F, false, true>(next, s, 0, ring + at(it) * 16);
     }
-    if (!all_seen<kGroup>(a, s, t0, p_min, p_max)) {
+    if (!all_seen<ROWS>(a, s, t0, p_min, p_max)) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) c[r] = hidden(a, s, q, t0 + 4 * kg + r) ? -INFINITY : c[r];
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[b][r] = hidden(a, s, q, t0 + 16 * b + 4 * kg + r) ? -INFINITY : c[b][r];
     }
-    float top = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) top = fmaxf(top, fmaxf(fmaxf(c[b][0], c[b][1]), fmaxf(c[b][2], c[b][3])));
     top = max32(max16(top));
     const float ref = fmaxf(m, ceilf(top * scale));        // a whole number in units of log2, as above
     if (__any(ref != m)) {
@@ -594,28 +607,41 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
     }
     const float use = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = exp2_of(c[r], scale, use);
-    sum += (c[0] + c[1]) + (c[2] + c[3]);
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) c[b][r] = exp2_of(c[b][r], scale, use);
+      sum += (c[b][0] + c[b][1]) + (c[b][2] + c[b][3]);
+    }
     // This group's V: behind it came the later groups, and the K that was just sent for.
     if (more) landed<2 * N * (RING - 1) + N>();
     else landed_behind<2 * N, RING>(behind);
     if constexpr (sizeof(T) == 2) {
+      // Both blocks of rows in one product: its contraction index 8 kg + e is row 4 kg + e of the first, or of the second.
       constexpr int PARTS = EXACT ? 3 : 1;
-      typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-      short4v pb[PARTS];
-      unsigned two[2][PARTS];
-      in_parts<PARTS>(c[0], c[1], two[0]);
-      in_parts<PARTS>(c[2], c[3], two[1]);
+      typedef unsigned u32x4p __attribute__((ext_vector_type(4)));
+      u32x4p pb[PARTS];
 #pragma unroll
-      for (int w = 0; w < PARTS; ++w) pb[w] = __builtin_bit_cast(short4v, u32x2{two[0][w], two[1][w]});
-      const int r = 4 * kg + (n >> 2);
+      for (int e = 0; e < 4; ++e) {
+        unsigned two[PARTS];
+        in_parts<PARTS>(c[e / 2][2 * (e % 2)], c[e / 2][2 * (e % 2) + 1], two);
+#pragma unroll
+        for (int w = 0; w < PARTS; ++w) pb[w][e] = two[w];
+      }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const int col = 16 * b + 4 * (n & 3);
-        const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
-        const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
+        bf16x8 v;
 #pragma unroll
-        for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pb[w], o[b], 0, 0, 0);
+        for (int half = 0; half < 2; ++half) {
+          const int r = 16 * half + 4 * kg + (n >> 2);
+          const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
+          const short4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
+          const bf16x4 y = __builtin_bit_cast(bf16x4, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * half + e] = y[e];
+        }
+#pragma unroll
+        for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pb[w]), o[b], 0, 0, 0);
       }
     } else {
       const float* Vf = reinterpret_cast<const float*>(Vt);
@@ -623,11 +649,11 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vf[(4 * kg + r) * D + 16 * b + n], c[r], o[b], 0, 0, 0);
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vf[(4 * kg + r) * D + 16 * b + n], c[0][r], o[b], 0, 0, 0);
     }
     if (more) {
       lds_read();
-      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      send_rows<ROWS, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
       next = fetch(it + RING + 1);
     }
   }
@@ -642,55 +668,80 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
   for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(a.o + slot * D + 16 * b + 4 * kg) = o[b];
 }
 
-// Shares of the products of many rows of q, a workgroup each, and of those of few, a wave each.
+// A share: `all` of a kind dealt to so many.
+struct Share {
+  unsigned per;
+  unsigned long long begin;
+  unsigned left;
+};
+__device__ __forceinline__ Share share_of(unsigned long long all, int sharers, int least, int which) {
+  Share s;
+  const unsigned long long each = (all + sharers - 1) / sharers;
+  s.per = each < (unsigned)least ? least : (unsigned)each;
+  s.begin = (unsigned long long)which * s.per;
+  s.left = s.begin >= all ? 0 : (s.begin + s.per < all ? s.per : (unsigned)(all - s.begin));
+  return s;
+}
+// What a sharer does of a tile of rows of q that counts `size`, from `r` on: `n` of it, which are its tiles [u_begin, u_end) of the cache.  A small one
+// belongs to the share that it begins in.
+struct Cut { unsigned n; bool skipped; int u_begin, u_end, parts; };
+template <unsigned FRONT, unsigned EACH> __device__ __forceinline__ Cut cut_of(unsigned size, unsigned r, unsigned per, unsigned left, unsigned least) {
+  Cut c;
+  const unsigned small = per / 4 > least ? per / 4 : least;
+  const bool whole = size <= small;
+  c.n = __builtin_amdgcn_readfirstlane(whole || size - r < left ? size - r : left);
+  c.skipped = whole && r > 0;
+  c.u_begin = r <= FRONT ? 0 : (int)((r - FRONT + EACH - 1) / EACH);
+  c.u_end = r + c.n <= FRONT ? 0 : (int)((r + c.n - FRONT + EACH - 1) / EACH);
+  c.parts = c.n == size ? 1 : 1 + (int)((size - c.n + per - 1) / per);       // (asked for where r = 0)
+  return c;
+}
+
 template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 8, kListed = 16, RING = 4 * F::TILE / (kWaves * 2 * kGroup * F::PIECES);
-  static_assert(RING >= 1 && RING * kWaves * 2 * kGroup * F::PIECES <= 4 * F::TILE, "LDS");
-  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][16 rows]
-  __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[kWaves];
-  __shared__ int s_first[kWaves];
-  __shared__ Source s_source[kWaves][kListed];                            // from s_first on
+  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup<T> * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
+  static_assert(RING >= 1 && 4 * F::TILE * 16 <= kSharedLds, "LDS");
+  extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][group]
+  __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[1 + kWaves];
+  __shared__ int s_first[1 + kWaves];                                     // of the workgroup's share, and of its waves'
+  __shared__ Source s_source[1 + kWaves][kListed];                        // from there on
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // All that there is to do: every thread sums up consecutive sources.
-  const int groups = clamped(*a.plan.count, 0, a.r.n_inst), sources = groups + a.r.n_inst, chunk = (sources + kThreads - 1) / kThreads;
-  const int i_begin = tid * chunk < sources ? tid * chunk : sources, i_end = i_begin + chunk < sources ? i_begin + chunk : sources;
+  // All that there is to do: every thread sums up consecutive sources.  (Of groups there are half as many as instances at most; how many is asked for
+  // at the same time.)
+  const int places = a.r.n_inst + a.r.n_inst / 2, chunk = (places + kThreads - 1) / kThreads;
+  const int groups = clamped(*a.plan.count, 0, a.r.n_inst / 2), sources = a.r.n_inst + groups;
+  const int i_begin = tid * chunk;
   unsigned long long wide[kHeld], my_wide = 0, my_narrow = 0;
   unsigned narrow[kHeld];
-  bool seen[kHeld];
-  auto sizes = [&](const Source& s, unsigned long long* w, unsigned* n) {
-    *w = (unsigned long long)wide_size<C, F::TT>(s) * (unsigned)s.wide();
-    *n = narrow_size<C>(s);
-  };
-#pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
-    wide[k] = 0;
-    narrow[k] = 0;
-    seen[k] = false;
-  }
-  if (chunk <= kHeld) {
+  // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's.
+  auto sizes = [&](int i0) {
+    Source s[kHeld];
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-      if (k < chunk) {
-        const bool mine = i_begin + k < i_end;
-        const Source s = source_of(a, groups, mine ? i_begin + k : sources - 1);          // (the loads of all of them are under way together)
-        sizes(s, &wide[k], &narrow[k]);
-        seen[k] = mine && tiling_of<kGroup>(s).n > 0;
-        wide[k] = mine ? wide[k] : 0;
-        narrow[k] = mine ? narrow[k] : 0;
-        my_wide += wide[k];
-        my_narrow += narrow[k];
+      if (i0 + k < chunk) s[k] = source_of(a, i_begin + i0 + k < places ? i_begin + i0 + k : 0);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      const int x = i_begin + i0 + k;
+      const bool mine = i0 + k < chunk && x < sources;
+      wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
+      narrow[k] = mine ? narrow_size<C, kGroup<T>>(s[k]) : 0;
+      // Which sources have pieces, for the join: the instances, and the groups by their first member.
+      if (mine && (unsigned)x % gridDim.x == blockIdx.x) {
+        const bool some = wide[k] > 0 || narrow[k] > 0;
+        if (x < a.r.n_inst) a.behind[x] = some;
+        else a.begun[clamped(s[k].inst, 0, a.r.n_inst - 1)] = some;
       }
-  } else {
-    for (int i = i_begin; i < i_end; ++i) {
-      unsigned long long w;
-      unsigned n;
-      sizes(source_of(a, groups, i), &w, &n);
-      my_wide += w;
-      my_narrow += n;
+    }
+  };
+  for (int i0 = 0; i0 < chunk; i0 += kHeld) {
+    sizes(i0);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      my_wide += wide[k];
+      my_narrow += narrow[k];
     }
   }
   unsigned long long upto_wide = my_wide, upto_narrow = my_narrow;
@@ -706,6 +757,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     s_wide[wave] = upto_wide;
     s_narrow[wave] = upto_narrow;
   }
+  if (tid <= kWaves) s_first[tid] = sources;
   __syncthreads();
   unsigned long long all_wide = 0, all_narrow = 0, at_wide = upto_wide - my_wide, at_narrow = upto_narrow - my_narrow;
   for (int w = 0; w < kWaves; ++w) {
@@ -716,110 +768,88 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     all_wide += s_wide[w];
     all_narrow += s_narrow[w];
   }
-  // Workgroups for the one and for the other, by the time that both take.
-  const float part = (float)all_wide / ((float)all_wide + 0.25f * (float)all_narrow);     // (NaN where there is nothing to do)
-  int wide_wgs = (int)(part * (float)gridDim.x + 0.5f);
-  if (all_wide > 0 && wide_wgs < 1) wide_wgs = 1;
-  if (all_narrow > 0 && wide_wgs > (int)gridDim.x - 1) wide_wgs = (int)gridDim.x - 1;
-  if (all_wide == 0) wide_wgs = 0;
-  wide_wgs = __builtin_amdgcn_readfirstlane(wide_wgs);
-  const bool is_wide = (int)blockIdx.x < wide_wgs;
-  const unsigned long long all = is_wide ? all_wide : all_narrow;
-  const int sharers = is_wide ? wide_wgs : kWaves * ((int)gridDim.x - wide_wgs);
-  const int least = is_wide ? C::WIDE_LEAST : C::NARROW_LEAST;
-  const unsigned long long share = (all + sharers - 1) / sharers;
-  const unsigned per = share < (unsigned)least ? least : (unsigned)share;
-  const int first_sharer = is_wide ? (int)blockIdx.x : kWaves * ((int)blockIdx.x - wide_wgs);      // of this workgroup's
-  // Where the shares begin: s_first[0], or every wave's.
-  if (tid < kWaves) s_first[tid] = sources;
-  __syncthreads();
-  const unsigned long long from_here = is_wide ? at_wide : at_narrow, to_here = from_here + (is_wide ? my_wide : my_narrow);
-  for (int w = 0; w < (is_wide ? 1 : kWaves); ++w) {
-    const unsigned long long begin = (unsigned long long)(first_sharer + w) * per;
-    if (from_here > begin || begin >= to_here) continue;
-    unsigned long long at = from_here;
-    if (chunk <= kHeld) {
+  // Where the shares begin: number 0 is the workgroup's, 1 + w that of wave w.  The waves' go round the workgroups, so that few of them are spread.
+  auto share = [&](int y) {
+    return y == 0 ? share_of(all_wide, gridDim.x, C::WIDE_LEAST, blockIdx.x)
+                  : share_of(all_narrow, kWaves * gridDim.x, C::NARROW_LEAST, (y - 1) * (int)gridDim.x + (int)blockIdx.x);
+  };
+  const int held = chunk <= kHeld ? 1 : 0;
+  for (int y = 0; y <= kWaves; ++y) {
+    const Share s = share(y);
+    unsigned long long at = y == 0 ? at_wide : at_narrow;
+    if (s.left == 0 || s.begin < at || s.begin >= at + (y == 0 ? my_wide : my_narrow)) continue;
+    for (int i0 = 0; i0 < chunk; i0 += kHeld) {
+      if (!held) sizes(i0);
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
-        const unsigned long long n = is_wide ? wide[k] : narrow[k];
-        if (at <= begin && begin < at + n) {
-          s_first[w] = i_begin + k;
-          s_from[w] = begin - at;
-        }
-        at += n;
-      }
-    } else {
-      for (int i = i_begin; i < i_end; ++i) {
-        unsigned long long x;
-        unsigned y;
-        sizes(source_of(a, groups, i), &x, &y);
-        const unsigned long long n = is_wide ? x : y;
-        if (at <= begin && begin < at + n) {
-          s_first[w] = i;
-          s_from[w] = begin - at;
+        const unsigned long long n = y == 0 ? wide[k] : narrow[k];
+        if (at <= s.begin && s.begin < at + n) {
+          s_first[y] = i_begin + i0 + k;
+          s_from[y] = s.begin - at;
         }
         at += n;
       }
     }
   }
-  // Which sources have tiles, for the join: the groups by their first member, the instances.
-  auto note = [&](int x, bool some) {
-    if (x < groups) a.begun[clamped(a.plan.groups[x].x, 0, a.r.n_inst - 1)] = some;
-    else a.behind[x - groups] = some;
-  };
-  if (chunk <= kHeld) {
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (i_begin + k < i_end && (unsigned)(i_begin + k) % gridDim.x == blockIdx.x) note(i_begin + k, seen[k]);
-  } else {
-    for (int x = blockIdx.x * kThreads + tid; x < sources; x += gridDim.x * kThreads) note(x, tiling_of<kGroup>(source_of(a, groups, x)).n > 0);
+  __syncthreads();
+  if (tid < (1 + kWaves) * kListed) {
+    const int x = s_first[tid / kListed] + tid % kListed;
+    s_source[tid / kListed][tid % kListed] = source_of(a, x < sources ? x : 0);
   }
   __syncthreads();
-  const int w = is_wide ? 0 : wave, x_first = __builtin_amdgcn_readfirstlane(s_first[w]);
-  if (!is_wide && lane < kListed) s_source[wave][lane] = source_of(a, groups, x_first + lane < sources ? x_first + lane : sources - 1);
-  if (is_wide && tid < kListed) s_source[0][tid] = source_of(a, groups, x_first + tid < sources ? x_first + tid : sources - 1);
-  __syncthreads();
-  if (x_first >= sources) return;
-  const unsigned long long begin = (unsigned long long)(first_sharer + w) * per;
-  unsigned left = begin + per < all ? per : (unsigned)(all - begin);
-  unsigned long long from = s_from[w];
-  // A small tile of rows of q belongs to the share that it begins in.
-  const unsigned small = per / 4 > (unsigned)least ? per / 4 : (unsigned)least;
-  for (int x = x_first; left > 0 && x < sources; ++x, from = 0) {
-    const Source s = uniform(x - x_first < kListed ? s_source[w][x - x_first] : source_of(a, groups, x));
-    const unsigned size = is_wide ? wide_size<C, F::TT>(s) : narrow_size<C>(s);
-    const int tiles = size == 0 ? 0 : (is_wide ? s.wide() : 1);            // of rows of q
-    const unsigned long long end = (unsigned long long)size * (unsigned)tiles;
-    while (left > 0 && from < end) {
-      // Tile t of its rows of q, from `r` on.
-      const int t = __builtin_amdgcn_readfirstlane(tiles == 1 ? 0 : (int)(from / size));
-      const unsigned r = (unsigned)(from - (unsigned long long)t * size);
-      const bool whole = size <= small;
-      const unsigned n = __builtin_amdgcn_readfirstlane(whole || size - r < left ? size - r : left);
-      from += n;
-      left -= n < left ? n : left;
-      if (whole && r > 0) continue;
-      const unsigned front = is_wide ? C::WIDE_FRONT : C::NARROW_FRONT, each = is_wide ? C::WIDE : C::NARROW;
-      const int u_begin = r <= front ? 0 : (int)((r - front + each - 1) / each);
-      const int u_end = r + n <= front ? 0 : (int)((r + n - front + each - 1) / each);
-      const int row0 = is_wide ? t * kPrefillRows : s.rows / kPrefillRows * kPrefillRows;
-      const int rows = s.rows - row0 < kPrefillRows ? s.rows - row0 : kPrefillRows, my_row = is_wide ? tid : lane;
-      const size_t x0 = (size_t)s.x0 + row0;
-      const size_t slot = is_wide ? x0 + (size_t)kPrefillRows * first_sharer : (size_t)a.narrow0 + x0 + (size_t)kNarrowRows * (first_sharer + wave);
-      const int parts = 1 + (int)((size - n + per - 1) / per);
-      if (is_wide) __syncthreads();                        // everybody is done with the piece before
-      if (u_begin >= u_end) {                              // (what is in front alone)
-        if (my_row < rows) {
-          a.ml[(slot + my_row) * 2] = -INFINITY;
-          a.ml[(slot + my_row) * 2 + 1] = 0.f;
+
+  {                                                        // the workgroup's share
+    const int x_first = __builtin_amdgcn_readfirstlane(s_first[0]);
+    const Share share0 = share(0);
+    unsigned left = share0.left;
+    unsigned long long from = x_first < sources ? s_from[0] : 0;
+    for (int x = x_first; left > 0 && x < sources; ++x, from = 0) {
+      const Source s = uniform(x - x_first < kListed ? s_source[0][x - x_first] : source_of(a, x));
+      const unsigned size = wide_size<C, F::TT>(s);
+      const unsigned long long end = (unsigned long long)size * (unsigned)s.wide();
+      while (left > 0 && from < end) {
+        const int t = __builtin_amdgcn_readfirstlane(end == size ? 0 : (int)(from / size));            // tile t of its rows of q
+        const Cut c = cut_of<C::WIDE_FRONT, C::WIDE>(size, (unsigned)(from - (unsigned long long)t * size), share0.per, left, C::WIDE_LEAST);
+        const bool first = from == (unsigned long long)t * size;
+        from += c.n;
+        left -= c.n < left ? c.n : left;
+        if (c.skipped) continue;
+        const size_t x0 = (size_t)s.x0 + (size_t)t * kPrefillRows, slot = x0 + (size_t)kPrefillRows * blockIdx.x;
+        const int rows = s.rows - t * kPrefillRows;
+        __syncthreads();                                   // everybody is done with the piece before
+        if (c.u_begin < c.u_end) {
+          wide_piece<T, D, EXACT>(a, s, t, c.u_begin, c.u_end, slot, s_tiles);
+        } else if (tid < rows && tid < kPrefillRows) {     // (what is in front alone)
+          a.ml[(slot + tid) * 2] = -INFINITY;
+          a.ml[(slot + tid) * 2 + 1] = 0.f;
         }
-      } else if (is_wide) {
-        wide_piece<T, D, EXACT>(a, s, t, u_begin, u_end, slot, s_tiles);
-      } else {
-        narrow_piece<T, D, EXACT, RING>(a, s, u_begin, u_end, slot, s_tiles + wave * RING * 2 * kGroup * F::PIECES);
+        if (first && tid < rows && tid < kPrefillRows) a.row[x0 + tid] = make_int2((int)slot + tid, c.parts);
       }
-      if (r == 0 && my_row < rows) a.row[x0 + my_row] = make_int2((int)slot + my_row, is_wide ? parts : -parts);
     }
+    __syncthreads();
+  }
+
+  // This wave's share.
+  const int x_first = __builtin_amdgcn_readfirstlane(s_first[1 + wave]);
+  const Share mine = share(1 + wave);
+  const int number = wave * (int)gridDim.x + (int)blockIdx.x;
+  unsigned left = __builtin_amdgcn_readfirstlane(mine.left), r = x_first < sources ? __builtin_amdgcn_readfirstlane((unsigned)s_from[1 + wave]) : 0;
+  for (int x = x_first; left > 0 && x < sources; ++x, r = 0) {
+    const Source s = uniform(x - x_first < kListed ? s_source[1 + wave][x - x_first] : source_of(a, x));
+    const unsigned size = narrow_size<C, kGroup<T>>(s);
+    if (size <= r) continue;
+    const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, mine.per, left, C::NARROW_LEAST);
+    left -= c.n < left ? c.n : left;
+    if (c.skipped) continue;
+    const int row0 = s.rows / kPrefillRows * kPrefillRows, rows = s.rows - row0;
+    const size_t x0 = (size_t)s.x0 + row0, slot = (size_t)a.narrow0 + x0 + (size_t)kNarrowRows * number;
+    if (c.u_begin < c.u_end) {
+      narrow_piece<T, D, EXACT, RING>(a, s, c.u_begin, c.u_end, slot, s_tiles + wave * RING * GROUP);
+    } else if (lane < rows) {
+      a.ml[(slot + lane) * 2] = -INFINITY;
+      a.ml[(slot + lane) * 2 + 1] = 0.f;
+    }
+    if (r == 0 && lane < rows) a.row[x0 + lane] = make_int2((int)slot + lane, -c.parts);
   }
 }
 
@@ -829,38 +859,49 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
   const long long at = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int inst = (int)(at / a.rows), row = (int)(at % a.rows), lane = threadIdx.x & 63;
   if (inst >= a.r.n_inst || row >= queries(a, inst) * a.g) return;
+  // (What may be there is asked for together with whether it is: every dependent load is a trip to memory.)
   const int4 line = a.plan.inst[inst];
-  const int pos = a.plan.pos[inst], behind = a.behind[inst];
-  const bool some = line.z > 1 && (unsigned)pos < (unsigned)a.r.n_inst && a.begun[clamped(line.x, 0, a.r.n_inst - 1)] > 0;
-  const int2 first = some ? a.row[(size_t)pos * a.rows + row] : make_int2(0, 0);
-  const int2 own = behind > 0 ? a.row[((size_t)a.r.n_inst + inst) * a.rows + row] : make_int2(0, 0);
+  const int pos = clamped(a.plan.pos[inst], 0, a.r.n_inst - 1), behind = a.behind[inst];
+  const int2 own_row = a.row[(size_t)inst * a.rows + row];
+  const int begun = a.begun[clamped(line.x, 0, a.r.n_inst - 1)];
+  const int2 first_row = a.row[((size_t)a.r.n_inst + pos) * a.rows + row];
+  const int2 first = line.z > 1 && begun > 0 ? first_row : make_int2(0, 0), own = behind > 0 ? own_row : make_int2(0, 0);
   const int ahead = first.y < 0 ? -first.y : first.y, parts = ahead + (own.y < 0 ? -own.y : own.y);
   const int step = first.y < 0 ? kNarrowRows : kPrefillRows, own_step = own.y < 0 ? kNarrowRows : kPrefillRows;
   auto slot = [&](int p) { return p < ahead ? (size_t)first.x + (size_t)step * p : (size_t)own.x + (size_t)own_step * (p - ahead); };
-  float top = -INFINITY;
-  for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.ml[slot(p) * 2]);
+  constexpr int kAhead = 16;                               // loads under way
+  float v[kAhead][E];
+  auto load = [&](int p0) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x)
+      if (p0 + x < parts) {
+        const float* src = a.o + slot(p0 + x) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[x][e] = src[e];
+      }
+  };
+  load(0);
+  float m = lane < parts ? a.ml[slot(lane) * 2] : -INFINITY, l = lane < parts ? a.ml[slot(lane) * 2 + 1] : 0.f, top = m;
+  for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, a.ml[slot(p) * 2]);
   top = wave_max(top);
   const float use = top == -INFINITY ? 0.f : top;
   float o[E], all = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
   for (int p0 = 0; p0 < parts; p0 += 64) {
-    const int p = p0 + lane;
-    const float f = p < parts ? exp2_fast(a.ml[slot(p) * 2] - use) : 0.f;
-    all += p < parts ? f * a.ml[slot(p) * 2 + 1] : 0.f;
+    if (p0 > 0) {
+      m = p0 + lane < parts ? a.ml[slot(p0 + lane) * 2] : -INFINITY;
+      l = p0 + lane < parts ? a.ml[slot(p0 + lane) * 2 + 1] : 0.f;
+    }
+    const float f = exp2_fast(m - use);
+    all += f * l;
     const int n = parts - p0 < 64 ? parts - p0 : 64;
-    constexpr int kAhead = 8;                              // loads under way
     for (int x0 = 0; x0 < n; x0 += kAhead) {
-      float v[kAhead][E];
+      if (p0 + x0 > 0) load(p0 + x0);
 #pragma unroll
       for (int x = 0; x < kAhead; ++x) {
-        const float* src = a.o + slot(p0 + (x0 + x < n ? x0 + x : n - 1)) * D + lane * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[x][e] = src[e];
-      }
-#pragma unroll
-      for (int x = 0; x < kAhead; ++x) {
-        const float w = x0 + x < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x0 + x)) : 0.f;
+        if (x0 + x >= n) break;
+        const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x0 + x));
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] += w == 0.f ? 0.f : w * v[x][e];            // (a piece without tiles has left no sums)
       }
@@ -877,7 +918,7 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
 }
 
 template <typename T, int D, bool EXACT, typename OUT> hipError_t run(const SharedArgs& a, hipStream_t st) {
-  cache_shared_kernel<T, D, EXACT><<<kShareWgs, kThreads, (size_t)2 * 2 * Form<T, D>::TILE * 16, st>>>(a);
+  cache_shared_kernel<T, D, EXACT><<<kShareWgs, kThreads, kSharedLds, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned wgs = (unsigned)(((long long)a.r.n_inst * a.rows + kWaves - 1) / kWaves);

@@ -57,8 +57,8 @@ SharePlan share_plan(const Shape& s, void* plan);
 // Workgroups of the attention, two a CU.
 constexpr int kShareWgs = 512;
 
-// Rows of q, `rows` an instance, are numbered twice: those of the groups' members one after the other, x < n_inst * rows, for the groups' beginnings; and
-// n_inst * rows + those of the instances for what lies behind.  The piece that workgroup w leaves of row x is number x + kPrefillRows * w; that
+// Rows of q, `rows` an instance, are numbered twice: those of the instances, x < n_inst * rows, for what lies behind the beginnings; and n_inst * rows +
+// those of the groups' members one after the other for the groups' beginnings.  The piece that workgroup w leaves of row x is number x + kPrefillRows * w; that
 // wave w leaves of a tile of few rows, narrow0 + x + 16 * w.
 struct SharedArgs {
   CacheRows r;
