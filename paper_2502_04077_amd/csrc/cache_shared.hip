@@ -8,10 +8,10 @@
 //
 // out_x = sum over its sources of exp(m_x - m) o_x / sum of exp(m_x - m) l_x, for m the largest m_x.
 //
-// A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32); where a tile has no more than 16 rows of q, which is
-// memory-bound, in groups of 32 (16).  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each,
-// and those of few rows into shares of a wave each; a workgroup has one of the former and then its waves one of the latter each.  Whoever has a share
-// leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
+// A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32); where a tile has no more than 32 rows of q, which is
+// memory-bound, in groups of 16.  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each, and those of
+// few rows into shares of a wave each: the one needs the matrix unit, the other the memory, and a CU has room for a workgroup of both.  Whoever has a
+// share leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
 #include "cache_tiles.h"
 #include "share_internal.h"
 
@@ -87,14 +87,13 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- sources
-constexpr int kNarrowRows = 16;     // rows of q up to which a wave has them alone
-template <typename T> constexpr int kGroup = sizeof(T) == 2 ? 32 : 16;      // rows of the cache that it goes over at a time
+constexpr int kGroup = 16;          // rows of the cache that a wave with few rows of q goes over at a time
 constexpr int kSharedLds = 64 * 1024;       // two workgroups a CU
 // What a share counts, in tenths of a microsecond: of a workgroup's time a tile of the cache, and what a tile of rows of q costs beside them; of a
 // wave's time a group, and the same.  The least shares.
 template <typename T, bool EXACT> struct Counts {
-  static constexpr int WIDE = sizeof(T) == 4 ? 40 : (EXACT ? 20 : 14), WIDE_FRONT = 40, WIDE_LEAST = 80;
-  static constexpr int NARROW = sizeof(T) == 4 ? 16 : 20, NARROW_FRONT = 40, NARROW_LEAST = 64;
+  static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 24), WIDE_FRONT = 60, WIDE_LEAST = 120;
+  static constexpr int NARROW = sizeof(T) == 4 ? 24 : 16, NARROW_FRONT = 50, NARROW_LEAST = 64;
 };
 
 // Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
@@ -516,156 +515,169 @@ template <int N, int R, int FIRST = 0> __device__ __forceinline__ void landed_be
   }
 }
 
-// The last rows of q of a source, up to 16, over its groups [u_begin, u_end) of cache rows, by a wave: RING groups of K and V are on their way to
-// LDS, past the registers.  A lane has scores of row n of q and of four of each 16 cache rows, which are the second product's operand as they are, and
-// sums of four of each 16 dims.  slot: of the first of the rows.  lds: RING groups.
-template <typename T, int D, bool EXACT, int RING>
+// The last rows of q of a source, up to 16 RB, over its groups [u_begin, u_end) of 16 cache rows, by a wave: RING groups of K and V are on their way to
+// LDS, past the registers.  A lane has, of each 16 rows of q, scores of row n and of four cache rows, which are the second product's operand as they are,
+// and sums of four of each 16 dims.  slot: of the first of the rows.  lds: RING groups.
+template <typename T, int D, bool EXACT, int RING, int RB>
 __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& s, int u_begin, int u_end, size_t slot, const u32x4* lds) {
   using F = Form<T, D>;
-  constexpr int ROWS = kGroup<T>, KB = ROWS / 16, KS = F::PIECES / 4, DB = D / 16;                  // of a group; blocks of 16 rows, of 16 dims
-  constexpr int GROUP = ROWS * F::PIECES, N = GROUP / 64;  // pieces of a group's K, or V, and loads
+  constexpr int KS = F::PIECES / 4, DB = D / 16, GROUP = kGroup * F::PIECES, N = GROUP / 64;       // pieces of a group's K, or V, and loads
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4, count = u_end - u_begin;
-  const Tiling tiling = tiling_of<ROWS>(s);
+  const Tiling tiling = tiling_of<kGroup>(s);
   const TablePages pages = pages_of(a.r, s.inst);
   const unsigned ring = lds_address(lds);
-  auto fetch = [&](int it) { return fetch_of<ROWS, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * ROWS); };
+  auto fetch = [&](int it) { return fetch_of<kGroup, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * kGroup); };
   auto at = [&](int it) { return (it % RING) * 2 * GROUP; };
-  Fetch<ROWS> next = fetch(0);
+  Fetch<kGroup> next = fetch(0);
 #pragma unroll
   for (int it = 0; it < RING; ++it)
     if (it < count) {
-      send_rows<ROWS, F, false, true>(next, s, 0, ring + at(it) * 16);
-      send_rows<ROWS, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
       next = fetch(it + 1);
     }
-  const Query q = query_of(a, s, s.rows / kPrefillRows * kPrefillRows + n);
-  int p_min, p_max;
-  positions<16>(q, &p_min, &p_max);
-  u32x4 qf[KS];
+  Query q[RB];
+  int p_min = 0x7fffffff, p_max = -1;
+  u32x4 qf[RB][KS];
+  float4v o[RB][DB];
+  float m[RB], sum[RB];                                    // the sums over this lane's rows
 #pragma unroll
-  for (int l = 0; l < KS; ++l) qf[l] = static_cast<const u32x4*>(a.q)[q.row * F::PIECES + 4 * l + kg];
-  float4v o[DB];
+  for (int y = 0; y < RB; ++y) {
+    q[y] = query_of(a, s, s.rows / kPrefillRows * kPrefillRows + 16 * y + n);
+    int lo, hi;
+    positions<16>(q[y], &lo, &hi);
+    p_min = lo < p_min ? lo : p_min;
+    p_max = hi > p_max ? hi : p_max;
 #pragma unroll
-  for (int b = 0; b < DB; ++b) o[b] = float4v{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, sum = 0.f;                          // the sum over this lane's rows
+    for (int l = 0; l < KS; ++l) qf[y][l] = static_cast<const u32x4*>(a.q)[q[y].row * F::PIECES + 4 * l + kg];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) o[y][b] = float4v{0.f, 0.f, 0.f, 0.f};
+    m[y] = -INFINITY;
+    sum[y] = 0.f;
+  }
   const float scale = kLog2E / sqrtf((float)D);
 #pragma unroll
-  for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[l]));
+  for (int y = 0; y < RB; ++y)
+#pragma unroll
+    for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[y][l]));
   for (int it = 0; it < count; ++it) {
-    const int t0 = tiling.tile(u_begin + it) * ROWS, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
+    const int t0 = tiling.tile(u_begin + it) * kGroup, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
     const u32x4 *Kt = lds + at(it), *Vt = Kt + GROUP;
     const bool more = it + RING < count;
     landed_behind<2 * N, RING, N>(behind);
-    // Rows t0 + 16 b + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
+    // Rows t0 + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
     constexpr int SUMS = sizeof(T) == 2 ? 1 : 4;
-    float4v c[KB];
+    float4v sums[RB][SUMS], c[RB];
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      float4v sums[SUMS];
+    for (int y = 0; y < RB; ++y)
 #pragma unroll
-      for (int x = 0; x < SUMS; ++x) sums[x] = float4v{0.f, 0.f, 0.f, 0.f};
+      for (int x = 0; x < SUMS; ++x) sums[y][x] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int l = 0; l < KS; ++l) {
-        const u32x4 k = Kt[(16 * b + n) * F::PIECES + F::k_place(16 * b + n, 4 * l + kg)];
+    for (int l = 0; l < KS; ++l) {
+      const u32x4 k = Kt[n * F::PIECES + F::k_place(n, 4 * l + kg)];
+#pragma unroll
+      for (int y = 0; y < RB; ++y) {
         if constexpr (sizeof(T) == 2) {
-          sums[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[l]), sums[0], 0, 0, 0);
+          sums[y][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[y][l]), sums[y][0], 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            sums[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[l][e]), sums[e], 0, 0, 0);
+            sums[y][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[y][l][e]), sums[y][e], 0, 0, 0);
         }
       }
-      c[b] = sums[0];
+    }
+#pragma unroll
+    for (int y = 0; y < RB; ++y) {
+      c[y] = sums[y][0];
       if constexpr (SUMS == 4) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) c[b][r] = (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]);
+        for (int r = 0; r < 4; ++r) c[y][r] = (sums[y][0][r] + sums[y][1][r]) + (sums[y][2][r] + sums[y][3][r]);
       }
     }
     if (more) {
       lds_read();
-      send_rows<ROWS, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
     }
-    if (!all_seen<ROWS>(a, s, t0, p_min, p_max)) {
+    if (!all_seen<kGroup>(a, s, t0, p_min, p_max)) {
 #pragma unroll
-      for (int b = 0; b < KB; ++b)
+      for (int y = 0; y < RB; ++y)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) c[b][r] = hidden(a, s, q, t0 + 16 * b + 4 * kg + r) ? -INFINITY : c[b][r];
+        for (int r = 0; r < 4; ++r) c[y][r] = hidden(a, s, q[y], t0 + 4 * kg + r) ? -INFINITY : c[y][r];
     }
-    float top = -INFINITY;
 #pragma unroll
-    for (int b = 0; b < KB; ++b) top = fmaxf(top, fmaxf(fmaxf(c[b][0], c[b][1]), fmaxf(c[b][2], c[b][3])));
-    top = max32(max16(top));
-    const float ref = fmaxf(m, ceilf(top * scale));        // a whole number in units of log2, as above
-    if (__any(ref != m)) {
-      const float shrink = ref == m ? 1.f : exp2_fast(m - ref);
-      sum *= shrink;
+    for (int y = 0; y < RB; ++y) {
+      float top = fmaxf(fmaxf(c[y][0], c[y][1]), fmaxf(c[y][2], c[y][3]));
+      top = max32(max16(top));
+      const float ref = fmaxf(m[y], ceilf(top * scale));   // a whole number in units of log2, as above
+      if (__any(ref != m[y])) {
+        const float shrink = ref == m[y] ? 1.f : exp2_fast(m[y] - ref);
+        sum[y] *= shrink;
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
+        for (int b = 0; b < DB; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[b][r] *= shrink;
-      m = ref;
-    }
-    const float use = m == -INFINITY ? 0.f : m;
+          for (int r = 0; r < 4; ++r) o[y][b][r] *= shrink;
+        m[y] = ref;
+      }
+      const float use = m[y] == -INFINITY ? 0.f : m[y];
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) c[b][r] = exp2_of(c[b][r], scale, use);
-      sum += (c[b][0] + c[b][1]) + (c[b][2] + c[b][3]);
+      for (int r = 0; r < 4; ++r) c[y][r] = exp2_of(c[y][r], scale, use);
+      sum[y] += (c[y][0] + c[y][1]) + (c[y][2] + c[y][3]);
     }
     // This group's V: behind it came the later groups, and the K that was just sent for.
     if (more) landed<2 * N * (RING - 1) + N>();
     else landed_behind<2 * N, RING>(behind);
     if constexpr (sizeof(T) == 2) {
-      // Both blocks of rows in one product: its contraction index 8 kg + e is row 4 kg + e of the first, or of the second.
       constexpr int PARTS = EXACT ? 3 : 1;
-      typedef unsigned u32x4p __attribute__((ext_vector_type(4)));
-      u32x4p pb[PARTS];
+      typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+      short4v pb[RB][PARTS];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        unsigned two[PARTS];
-        in_parts<PARTS>(c[e / 2][2 * (e % 2)], c[e / 2][2 * (e % 2) + 1], two);
+      for (int y = 0; y < RB; ++y) {
+        unsigned two[2][PARTS];
+        in_parts<PARTS>(c[y][0], c[y][1], two[0]);
+        in_parts<PARTS>(c[y][2], c[y][3], two[1]);
 #pragma unroll
-        for (int w = 0; w < PARTS; ++w) pb[w][e] = two[w];
+        for (int w = 0; w < PARTS; ++w) pb[y][w] = __builtin_bit_cast(short4v, u32x2{two[0][w], two[1][w]});
       }
+      const int r = 4 * kg + (n >> 2);
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const int col = 16 * b + 4 * (n & 3);
-        bf16x8 v;
+        const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
+        const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int r = 16 * half + 4 * kg + (n >> 2);
-          const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
-          const short4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
-          const bf16x4 y = __builtin_bit_cast(bf16x4, w);
+        for (int y = 0; y < RB; ++y)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[4 * half + e] = y[e];
-        }
-#pragma unroll
-        for (int w = PARTS - 1; w >= 0; --w) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pb[w]), o[b], 0, 0, 0);
+          for (int w = PARTS - 1; w >= 0; --w) o[y][b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pb[y][w], o[y][b], 0, 0, 0);
       }
     } else {
       const float* Vf = reinterpret_cast<const float*>(Vt);
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(Vf[(4 * kg + r) * D + 16 * b + n], c[0][r], o[b], 0, 0, 0);
+        for (int r = 0; r < 4; ++r) {
+          const float v = Vf[(4 * kg + r) * D + 16 * b + n];
+#pragma unroll
+          for (int y = 0; y < RB; ++y) o[y][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, c[y][r], o[y][b], 0, 0, 0);
+        }
     }
     if (more) {
       lds_read();
-      send_rows<ROWS, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
       next = fetch(it + RING + 1);
     }
   }
-  sum = sum32(sum16(sum));
-  if (!q.real) return;
-  slot += n;
-  if (kg == 0) {
-    a.ml[slot * 2] = m;
-    a.ml[slot * 2 + 1] = sum;
-  }
 #pragma unroll
-  for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(a.o + slot * D + 16 * b + 4 * kg) = o[b];
+  for (int y = 0; y < RB; ++y) {
+    sum[y] = sum32(sum16(sum[y]));
+    if (!q[y].real) continue;
+    const size_t to = slot + 16 * y + n;
+    if (kg == 0) {
+      a.ml[to * 2] = m[y];
+      a.ml[to * 2 + 1] = sum[y];
+    }
+#pragma unroll
+    for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(a.o + to * D + 16 * b + 4 * kg) = o[y][b];
+  }
 }
 
 // A share: `all` of a kind dealt to so many.
@@ -701,7 +713,7 @@ template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup<T> * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
+  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
   static_assert(RING >= 1 && 4 * F::TILE * 16 <= kSharedLds, "LDS");
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][group]
   __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[1 + kWaves];
@@ -727,7 +739,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const int x = i_begin + i0 + k;
       const bool mine = i0 + k < chunk && x < sources;
       wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
-      narrow[k] = mine ? narrow_size<C, kGroup<T>>(s[k]) : 0;
+      narrow[k] = mine ? narrow_size<C, kGroup>(s[k]) : 0;
       // Which sources have pieces, for the join: the instances, and the groups by their first member.
       if (mine && (unsigned)x % gridDim.x == blockIdx.x) {
         const bool some = wide[k] > 0 || narrow[k] > 0;
@@ -768,13 +780,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     all_wide += s_wide[w];
     all_narrow += s_narrow[w];
   }
+  // Workgroups for the one and for the other, by the time that both take.
+  const float part = (float)all_wide / ((float)all_wide + (float)all_narrow / kWaves);    // (not a number where there is nothing to do)
+  int wide_wgs = all_wide == 0 ? 0 : (int)(part * (float)gridDim.x + 0.5f);
+  if (all_wide > 0 && wide_wgs < 1) wide_wgs = 1;
+  if (all_narrow > 0 && wide_wgs > (int)gridDim.x - 1) wide_wgs = (int)gridDim.x - 1;
+  wide_wgs = __builtin_amdgcn_readfirstlane(wide_wgs);
+  const int narrow_wgs = (int)gridDim.x - wide_wgs;
+  const bool is_wide = (int)blockIdx.x < wide_wgs;
   // Where the shares begin: number 0 is the workgroup's, 1 + w that of wave w.  The waves' go round the workgroups, so that few of them are spread.
+  auto number = [&](int w) { return w * narrow_wgs + (int)blockIdx.x - wide_wgs; };
   auto share = [&](int y) {
-    return y == 0 ? share_of(all_wide, gridDim.x, C::WIDE_LEAST, blockIdx.x)
-                  : share_of(all_narrow, kWaves * gridDim.x, C::NARROW_LEAST, (y - 1) * (int)gridDim.x + (int)blockIdx.x);
+    if (y == 0) return share_of(all_wide, wide_wgs > 0 ? wide_wgs : 1, C::WIDE_LEAST, blockIdx.x);
+    return share_of(all_narrow, kWaves * (narrow_wgs > 0 ? narrow_wgs : 1), C::NARROW_LEAST, number(y - 1));
   };
   const int held = chunk <= kHeld ? 1 : 0;
-  for (int y = 0; y <= kWaves; ++y) {
+  for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
     const Share s = share(y);
     unsigned long long at = y == 0 ? at_wide : at_narrow;
     if (s.left == 0 || s.begin < at || s.begin >= at + (y == 0 ? my_wide : my_narrow)) continue;
@@ -798,7 +819,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
   __syncthreads();
 
-  {                                                        // the workgroup's share
+  if (is_wide) {                                           // the workgroup's share
     const int x_first = __builtin_amdgcn_readfirstlane(s_first[0]);
     const Share share0 = share(0);
     unsigned left = share0.left;
@@ -826,25 +847,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         if (first && tid < rows && tid < kPrefillRows) a.row[x0 + tid] = make_int2((int)slot + tid, c.parts);
       }
     }
-    __syncthreads();
+    return;
   }
 
   // This wave's share.
   const int x_first = __builtin_amdgcn_readfirstlane(s_first[1 + wave]);
   const Share mine = share(1 + wave);
-  const int number = wave * (int)gridDim.x + (int)blockIdx.x;
   unsigned left = __builtin_amdgcn_readfirstlane(mine.left), r = x_first < sources ? __builtin_amdgcn_readfirstlane((unsigned)s_from[1 + wave]) : 0;
   for (int x = x_first; left > 0 && x < sources; ++x, r = 0) {
     const Source s = uniform(x - x_first < kListed ? s_source[1 + wave][x - x_first] : source_of(a, x));
-    const unsigned size = narrow_size<C, kGroup<T>>(s);
+    const unsigned size = narrow_size<C, kGroup>(s);
     if (size <= r) continue;
     const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, mine.per, left, C::NARROW_LEAST);
     left -= c.n < left ? c.n : left;
     if (c.skipped) continue;
     const int row0 = s.rows / kPrefillRows * kPrefillRows, rows = s.rows - row0;
-    const size_t x0 = (size_t)s.x0 + row0, slot = (size_t)a.narrow0 + x0 + (size_t)kNarrowRows * number;
+    const size_t x0 = (size_t)s.x0 + row0, slot = (size_t)a.narrow0 + x0 + (size_t)kNarrowRows * number(wave);
     if (c.u_begin < c.u_end) {
-      narrow_piece<T, D, EXACT, RING>(a, s, c.u_begin, c.u_end, slot, s_tiles + wave * RING * GROUP);
+      if (rows <= 16) narrow_piece<T, D, EXACT, RING, 1>(a, s, c.u_begin, c.u_end, slot, s_tiles + wave * RING * GROUP);
+      else narrow_piece<T, D, EXACT, RING, 2>(a, s, c.u_begin, c.u_end, slot, s_tiles + wave * RING * GROUP);
     } else if (lane < rows) {
       a.ml[(slot + lane) * 2] = -INFINITY;
       a.ml[(slot + lane) * 2 + 1] = 0.f;

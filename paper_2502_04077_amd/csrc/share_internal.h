@@ -56,10 +56,11 @@ SharePlan share_plan(const Shape& s, void* plan);
 
 // Workgroups of the attention, two a CU.
 constexpr int kShareWgs = 512;
+constexpr int kNarrowRows = 32;     // rows of q of a tile up to which a wave has them alone
 
 // Rows of q, `rows` an instance, are numbered twice: those of the instances, x < n_inst * rows, for what lies behind the beginnings; and n_inst * rows +
 // those of the groups' members one after the other for the groups' beginnings.  The piece that workgroup w leaves of row x is number x + kPrefillRows * w; that
-// wave w leaves of a tile of few rows, narrow0 + x + 16 * w.
+// wave w leaves of a tile of few rows, narrow0 + x + kNarrowRows * w.
 struct SharedArgs {
   CacheRows r;
   const void *q, *K, *V;
@@ -74,7 +75,7 @@ struct SharedArgs {
 // Pieces: those of workgroups, in front of narrow0, and of waves.
 inline size_t shared_narrow0(const Shape& s, int q_cap) { return (size_t)2 * s.n_inst * q_cap * s.g + (size_t)kPrefillRows * kShareWgs; }
 inline size_t shared_pieces(const Shape& s, int q_cap) {
-  return shared_narrow0(s, q_cap) + (size_t)2 * s.n_inst * q_cap * s.g + (size_t)16 * 4 * kShareWgs;
+  return shared_narrow0(s, q_cap) + (size_t)2 * s.n_inst * q_cap * s.g + (size_t)kNarrowRows * 4 * kShareWgs;
 }
 struct SharedWs { size_t begun, behind, row, ml, o, total; };
 SharedWs shared_ws(const Shape& s, int q_cap);
