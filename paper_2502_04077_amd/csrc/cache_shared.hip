@@ -713,7 +713,7 @@ template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
+  constexpr int kHeld = 16, kBatch = 4, kListed = 16, GROUP = 2 * kGroup * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
   static_assert(RING >= 1 && 4 * F::TILE * 16 <= kSharedLds, "LDS");
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][group]
   __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[1 + kWaves];
@@ -728,28 +728,39 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int i_begin = tid * chunk;
   unsigned long long wide[kHeld], my_wide = 0, my_narrow = 0;
   unsigned narrow[kHeld];
-  // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's.
-  auto sizes = [&](int i0) {
-    Source s[kHeld];
+  // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's; the loads of several are under way together.
+  auto sizes = [&](int i0, bool note) {
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (i0 + k < chunk) s[k] = source_of(a, i_begin + i0 + k < places ? i_begin + i0 + k : 0);
+    for (int k0 = 0; k0 < kHeld; k0 += kBatch) {
+      if (i0 + k0 >= chunk) {
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-      const int x = i_begin + i0 + k;
-      const bool mine = i0 + k < chunk && x < sources;
-      wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
-      narrow[k] = mine ? narrow_size<C, kGroup>(s[k]) : 0;
-      // Which sources have pieces, for the join: the instances, and the groups by their first member.
-      if (mine && (unsigned)x % gridDim.x == blockIdx.x) {
-        const bool some = wide[k] > 0 || narrow[k] > 0;
-        if (x < a.r.n_inst) a.behind[x] = some;
-        else a.begun[clamped(s[k].inst, 0, a.r.n_inst - 1)] = some;
+        for (int k = k0; k < k0 + kBatch; ++k) {
+          wide[k] = 0;
+          narrow[k] = 0;
+        }
+        continue;
+      }
+      Source s[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) s[k] = source_of(a, i0 + k0 + k < chunk && i_begin + i0 + k0 + k < places ? i_begin + i0 + k0 + k : 0);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int x = i_begin + i0 + k0 + k;
+        const bool mine = i0 + k0 + k < chunk && x < sources;
+        const unsigned long long w = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
+        const unsigned n = mine ? narrow_size<C, kGroup>(s[k]) : 0;
+        wide[k0 + k] = w;
+        narrow[k0 + k] = n;
+        // Which sources have pieces, for the join: the instances, and the groups by their first member.
+        if (note && mine && (unsigned)x % gridDim.x == blockIdx.x) {
+          if (x < a.r.n_inst) a.behind[x] = w + n > 0;
+          else a.begun[clamped(s[k].inst, 0, a.r.n_inst - 1)] = w + n > 0;
+        }
       }
     }
   };
   for (int i0 = 0; i0 < chunk; i0 += kHeld) {
-    sizes(i0);
+    sizes(i0, true);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       my_wide += wide[k];
@@ -794,23 +805,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (y == 0) return share_of(all_wide, wide_wgs > 0 ? wide_wgs : 1, C::WIDE_LEAST, blockIdx.x);
     return share_of(all_narrow, kWaves * (narrow_wgs > 0 ? narrow_wgs : 1), C::NARROW_LEAST, number(y - 1));
   };
-  const int held = chunk <= kHeld ? 1 : 0;
-  for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
-    const Share s = share(y);
-    unsigned long long at = y == 0 ? at_wide : at_narrow;
-    if (s.left == 0 || s.begin < at || s.begin >= at + (y == 0 ? my_wide : my_narrow)) continue;
-    for (int i0 = 0; i0 < chunk; i0 += kHeld) {
-      if (!held) sizes(i0);
+  unsigned long long at = is_wide ? at_wide : at_narrow;
+  for (int i0 = 0; i0 < chunk; i0 += kHeld) {
+    if (chunk > kHeld) sizes(i0, false);
+    unsigned long long here = 0;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) here += is_wide ? wide[k] : narrow[k];
+    for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
+      const Share s = share(y);
+      if (s.left == 0 || s.begin < at || s.begin >= at + here) continue;
+      unsigned long long to = at;
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
-        const unsigned long long n = y == 0 ? wide[k] : narrow[k];
-        if (at <= s.begin && s.begin < at + n) {
+        const unsigned long long n = is_wide ? wide[k] : narrow[k];
+        if (to <= s.begin && s.begin < to + n) {
           s_first[y] = i_begin + i0 + k;
-          s_from[y] = s.begin - at;
+          s_from[y] = s.begin - to;
         }
-        at += n;
+        to += n;
       }
     }
+    at += here;
   }
   __syncthreads();
   if (tid < (1 + kWaves) * kListed) {
