@@ -154,6 +154,15 @@ __device__ __forceinline__ Source uniform(Source s) {
   for (int k = 0; k < (int)(sizeof(Source) / 4); ++k) w[k] = __builtin_amdgcn_readfirstlane(w[k]);
   return s;
 }
+// The lowest position of a query of a group's members.  (A call: few need it, and the launch's code is to stay in the instruction cache.)
+__device__ __attribute__((noinline)) int lowest_position(const int32_t* member, const int32_t* len, const int32_t* n_q, int q_cap, int t_cap, int n_inst, int count) {
+  int p = 0x7fffffff;
+  for (int k = 0; k < count; ++k) {
+    const int i = clamped(member[k], 0, n_inst - 1), q = n_q == nullptr ? q_cap : clamped(n_q[i], 0, q_cap), base = clamped(len[i], 0, t_cap) - q;
+    if (q > 0 && base < p) p = base;
+  }
+  return p;
+}
 // Sources in their order: the instances', then the groups'.  What has to be loaded for source x is asked for together.
 __device__ __forceinline__ Source source_of(const SharedArgs& a, int x) {
   const int n = a.r.n_inst, i = x < n ? x : 0;
@@ -168,16 +177,12 @@ __device__ __forceinline__ Source source_of(const SharedArgs& a, int x) {
     s.rows = several ? line.z * a.rows : 0;
     s.x0 = (n + line.y) * a.rows;
     s.p0 = 0;
-    int p = 0x7fffffff;                                    // the lowest position of a query
-    if (S > 0 && a.window > 0)
-      for (int k = 0; k < s.count; ++k) {
-        const int member = clamped(a.plan.member[s.first + k], 0, n - 1), q = queries(a, member), base = clamped(a.r.len[member], 0, a.r.t_cap) - q;
-        if (q > 0 && base < p) p = base;
-      }
+    int p = 0x7fffffff;
+    if (S > 0 && a.window > 0) p = lowest_position(a.plan.member + s.first, a.r.len, a.n_q, a.q_cap, a.r.t_cap, n, s.count);
     see(a, s, 0, S, p);
   } else {
     s.inst = i; s.first = 0; s.count = 0;
-    s.rows = m * a.g;
+    s.rows = m << a.lg;
     s.x0 = i * a.rows;
     s.p0 = own - m;
     see(a, s, S, own, s.p0);
@@ -293,16 +298,16 @@ __device__ __forceinline__ Query query_of(const SharedArgs& a, const Source& s, 
   q.real = x < s.rows;
   if (s.count > 0) {
     const int of = x / a.rows;
-    rest = x % a.rows;
+    rest = x - of * a.rows;
     q.inst = clamped(a.plan.member[s.first + (of < s.count ? of : 0)], 0, a.r.n_inst - 1);
     const int m = queries(a, q.inst), L = clamped(a.r.len[q.inst], 0, a.r.t_cap);
-    q.real = q.real && rest < m * a.g;
+    q.real = q.real && rest < m << a.lg;
     if (!q.real) rest = 0;
-    q.p = L - m + rest / a.g;
+    q.p = L - m + (rest >> a.lg);
   } else {
     if (!q.real) rest = 0;
     q.inst = s.inst;
-    q.p = s.p0 + rest / a.g;
+    q.p = s.p0 + (rest >> a.lg);
   }
   q.lo = a.window > 0 && q.p >= a.window ? q.p - a.window + 1 : 0;
   q.row = (size_t)q.inst * a.rows + rest;
@@ -680,18 +685,15 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
   }
 }
 
-// A share: `all` of a kind dealt to so many.
+// A share of `all`, of which everybody has `per`.
 struct Share {
-  unsigned per;
   unsigned long long begin;
   unsigned left;
 };
-__device__ __forceinline__ Share share_of(unsigned long long all, int sharers, int least, int which) {
+__device__ __forceinline__ Share share_of(unsigned long long all, unsigned per, int which) {
   Share s;
-  const unsigned long long each = (all + sharers - 1) / sharers;
-  s.per = each < (unsigned)least ? least : (unsigned)each;
-  s.begin = (unsigned long long)which * s.per;
-  s.left = s.begin >= all ? 0 : (s.begin + s.per < all ? s.per : (unsigned)(all - s.begin));
+  s.begin = (unsigned long long)which * per;
+  s.left = s.begin >= all ? 0 : (s.begin + per < all ? per : (unsigned)(all - s.begin));
   return s;
 }
 // What a sharer does of a tile of rows of q that counts `size`, from `r` on: `n` of it, which are its tiles [u_begin, u_end) of the cache.  A small one
@@ -713,7 +715,7 @@ template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 16, kBatch = 4, kListed = 16, GROUP = 2 * kGroup * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
+  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
   static_assert(RING >= 1 && 4 * F::TILE * 16 <= kSharedLds, "LDS");
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][group]
   __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[1 + kWaves];
@@ -726,106 +728,101 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int places = a.r.n_inst + a.r.n_inst / 2, chunk = (places + kThreads - 1) / kThreads;
   const int groups = clamped(*a.plan.count, 0, a.r.n_inst / 2), sources = a.r.n_inst + groups;
   const int i_begin = tid * chunk;
-  unsigned long long wide[kHeld], my_wide = 0, my_narrow = 0;
-  unsigned narrow[kHeld];
-  // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's; the loads of several are under way together.
-  auto sizes = [&](int i0, bool note) {
+  unsigned long long wide[kHeld], my_wide = 0, my_narrow = 0, all_wide = 0, all_narrow = 0, at = 0;
+  unsigned narrow[kHeld], per = 0;
+  int wide_wgs = 0, narrow_wgs = kShareWgs;
+  bool is_wide = false;
+  // The waves' shares go round the workgroups, so that few of them are spread.
+  auto number = [&](int w) { return w * narrow_wgs + (int)blockIdx.x - wide_wgs; };
+  auto share = [&](int y) { return y == 0 ? share_of(all_wide, per, blockIdx.x) : share_of(all_narrow, per, number(y - 1)); };
+  // Twice: what there is; and, by the threads in whose sources they lie, where shares begin.
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+    for (int i0 = 0; i0 < chunk; i0 += kHeld) {
+      // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's, whose loads are under way together; they are held where these are all.
+      if (pass == 0 || chunk > kHeld) {
+        Source s[kHeld];
 #pragma unroll
-    for (int k0 = 0; k0 < kHeld; k0 += kBatch) {
-      if (i0 + k0 >= chunk) {
+        for (int k = 0; k < kHeld; ++k) s[k] = source_of(a, i0 + k < chunk && i_begin + i0 + k < places ? i_begin + i0 + k : 0);
 #pragma unroll
-        for (int k = k0; k < k0 + kBatch; ++k) {
-          wide[k] = 0;
-          narrow[k] = 0;
+        for (int k = 0; k < kHeld; ++k) {
+          const int x = i_begin + i0 + k;
+          const bool mine = i0 + k < chunk && x < sources;
+          wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
+          narrow[k] = mine ? narrow_size<C, kGroup>(s[k]) : 0;
+          // Which sources have pieces, for the join: the instances, and the groups by their first member.
+          if (pass == 0 && mine && x % kShareWgs == (int)blockIdx.x) {
+            int32_t* some = x < a.r.n_inst ? a.behind + x : a.begun + clamped(s[k].inst, 0, a.r.n_inst - 1);
+            *some = wide[k] + narrow[k] > 0;
+          }
+        }
+      }
+      if (pass == 0) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) {
+          my_wide += wide[k];
+          my_narrow += narrow[k];
         }
         continue;
       }
-      Source s[kBatch];
+      unsigned long long here = 0;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) s[k] = source_of(a, i0 + k0 + k < chunk && i_begin + i0 + k0 + k < places ? i_begin + i0 + k0 + k : 0);
+      for (int k = 0; k < kHeld; ++k) here += is_wide ? wide[k] : narrow[k];
+#pragma unroll 1
+      for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
+        const Share s = share(y);
+        if (s.left == 0 || s.begin < at || s.begin >= at + here) continue;
+        unsigned long long to = at;
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int x = i_begin + i0 + k0 + k;
-        const bool mine = i0 + k0 + k < chunk && x < sources;
-        const unsigned long long w = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
-        const unsigned n = mine ? narrow_size<C, kGroup>(s[k]) : 0;
-        wide[k0 + k] = w;
-        narrow[k0 + k] = n;
-        // Which sources have pieces, for the join: the instances, and the groups by their first member.
-        if (note && mine && (unsigned)x % gridDim.x == blockIdx.x) {
-          if (x < a.r.n_inst) a.behind[x] = w + n > 0;
-          else a.begun[clamped(s[k].inst, 0, a.r.n_inst - 1)] = w + n > 0;
+        for (int k = 0; k < kHeld; ++k) {
+          const unsigned long long n = is_wide ? wide[k] : narrow[k];
+          if (to <= s.begin && s.begin < to + n) {
+            s_first[y] = i_begin + i0 + k;
+            s_from[y] = s.begin - to;
+          }
+          to += n;
         }
       }
+      at += here;
     }
-  };
-  for (int i0 = 0; i0 < chunk; i0 += kHeld) {
-    sizes(i0, true);
+    if (pass == 1) break;
+    unsigned long long upto_wide = my_wide, upto_narrow = my_narrow;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-      my_wide += wide[k];
-      my_narrow += narrow[k];
-    }
-  }
-  unsigned long long upto_wide = my_wide, upto_narrow = my_narrow;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long x = __shfl_up(upto_wide, o, 64), y = __shfl_up(upto_narrow, o, 64);
-    if (lane >= o) {
-      upto_wide += x;
-      upto_narrow += y;
-    }
-  }
-  if (lane == 63) {
-    s_wide[wave] = upto_wide;
-    s_narrow[wave] = upto_narrow;
-  }
-  if (tid <= kWaves) s_first[tid] = sources;
-  __syncthreads();
-  unsigned long long all_wide = 0, all_narrow = 0, at_wide = upto_wide - my_wide, at_narrow = upto_narrow - my_narrow;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) {
-      at_wide += s_wide[w];
-      at_narrow += s_narrow[w];
-    }
-    all_wide += s_wide[w];
-    all_narrow += s_narrow[w];
-  }
-  // Workgroups for the one and for the other, by the time that both take.
-  const float part = (float)all_wide / ((float)all_wide + (float)all_narrow / kWaves);    // (not a number where there is nothing to do)
-  int wide_wgs = all_wide == 0 ? 0 : (int)(part * (float)gridDim.x + 0.5f);
-  if (all_wide > 0 && wide_wgs < 1) wide_wgs = 1;
-  if (all_narrow > 0 && wide_wgs > (int)gridDim.x - 1) wide_wgs = (int)gridDim.x - 1;
-  wide_wgs = __builtin_amdgcn_readfirstlane(wide_wgs);
-  const int narrow_wgs = (int)gridDim.x - wide_wgs;
-  const bool is_wide = (int)blockIdx.x < wide_wgs;
-  // Where the shares begin: number 0 is the workgroup's, 1 + w that of wave w.  The waves' go round the workgroups, so that few of them are spread.
-  auto number = [&](int w) { return w * narrow_wgs + (int)blockIdx.x - wide_wgs; };
-  auto share = [&](int y) {
-    if (y == 0) return share_of(all_wide, wide_wgs > 0 ? wide_wgs : 1, C::WIDE_LEAST, blockIdx.x);
-    return share_of(all_narrow, kWaves * (narrow_wgs > 0 ? narrow_wgs : 1), C::NARROW_LEAST, number(y - 1));
-  };
-  unsigned long long at = is_wide ? at_wide : at_narrow;
-  for (int i0 = 0; i0 < chunk; i0 += kHeld) {
-    if (chunk > kHeld) sizes(i0, false);
-    unsigned long long here = 0;
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) here += is_wide ? wide[k] : narrow[k];
-    for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
-      const Share s = share(y);
-      if (s.left == 0 || s.begin < at || s.begin >= at + here) continue;
-      unsigned long long to = at;
-#pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        const unsigned long long n = is_wide ? wide[k] : narrow[k];
-        if (to <= s.begin && s.begin < to + n) {
-          s_first[y] = i_begin + i0 + k;
-          s_from[y] = s.begin - to;
-        }
-        to += n;
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned long long x = __shfl_up(upto_wide, o, 64), y = __shfl_up(upto_narrow, o, 64);
+      if (lane >= o) {
+        upto_wide += x;
+        upto_narrow += y;
       }
     }
-    at += here;
+    if (lane == 63) {
+      s_wide[wave] = upto_wide;
+      s_narrow[wave] = upto_narrow;
+    }
+    if (tid <= kWaves) s_first[tid] = sources;
+    __syncthreads();
+    unsigned long long at_wide = upto_wide - my_wide, at_narrow = upto_narrow - my_narrow;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) {
+        at_wide += s_wide[w];
+        at_narrow += s_narrow[w];
+      }
+      all_wide += s_wide[w];
+      all_narrow += s_narrow[w];
+    }
+    // Workgroups for the one and for the other, by the time that both take.
+    const float part = (float)all_wide / ((float)all_wide + (float)all_narrow / kWaves);    // (not a number where there is nothing to do)
+    wide_wgs = all_wide == 0 ? 0 : (int)(part * (float)kShareWgs + 0.5f);
+    if (all_wide > 0 && wide_wgs < 1) wide_wgs = 1;
+    if (all_narrow > 0 && wide_wgs > kShareWgs - 1) wide_wgs = kShareWgs - 1;
+    wide_wgs = __builtin_amdgcn_readfirstlane(wide_wgs);
+    narrow_wgs = wide_wgs < kShareWgs ? kShareWgs - wide_wgs : 1;
+    is_wide = (int)blockIdx.x < wide_wgs;
+    at = is_wide ? at_wide : at_narrow;
+    const unsigned sharers = is_wide ? wide_wgs : kWaves * narrow_wgs, least = is_wide ? C::WIDE_LEAST : C::NARROW_LEAST;
+    const unsigned long long each = ((is_wide ? all_wide : all_narrow) + sharers - 1) / sharers;
+    per = __builtin_amdgcn_readfirstlane(each < least ? least : (unsigned)each);
   }
   __syncthreads();
   if (tid < (1 + kWaves) * kListed) {
@@ -845,7 +842,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const unsigned long long end = (unsigned long long)size * (unsigned)s.wide();
       while (left > 0 && from < end) {
         const int t = __builtin_amdgcn_readfirstlane(end == size ? 0 : (int)(from / size));            // tile t of its rows of q
-        const Cut c = cut_of<C::WIDE_FRONT, C::WIDE>(size, (unsigned)(from - (unsigned long long)t * size), share0.per, left, C::WIDE_LEAST);
+        const Cut c = cut_of<C::WIDE_FRONT, C::WIDE>(size, (unsigned)(from - (unsigned long long)t * size), per, left, C::WIDE_LEAST);
         const bool first = from == (unsigned long long)t * size;
         from += c.n;
         left -= c.n < left ? c.n : left;
@@ -873,7 +870,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const Source s = uniform(x - x_first < kListed ? s_source[1 + wave][x - x_first] : source_of(a, x));
     const unsigned size = narrow_size<C, kGroup>(s);
     if (size <= r) continue;
-    const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, mine.per, left, C::NARROW_LEAST);
+    const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, per, left, C::NARROW_LEAST);
     left -= c.n < left ? c.n : left;
     if (c.skipped) continue;
     const int row0 = s.rows / kPrefillRows * kPrefillRows, rows = s.rows - row0;
@@ -894,7 +891,7 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
   constexpr int E = D / 64;                                // outputs of a lane
   const long long at = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int inst = (int)(at / a.rows), row = (int)(at % a.rows), lane = threadIdx.x & 63;
-  if (inst >= a.r.n_inst || row >= queries(a, inst) * a.g) return;
+  if (inst >= a.r.n_inst || row >= queries(a, inst) << a.lg) return;
   // (What may be there is asked for together with whether it is: every dependent load is a trip to memory.)
   const int4 line = a.plan.inst[inst];
   const int pos = clamped(a.plan.pos[inst], 0, a.r.n_inst - 1), behind = a.behind[inst];

@@ -77,7 +77,9 @@ static hipError_t launch_shared(const Shape& s, const void* q, const int32_t* n_
   char* base = static_cast<char*>(ws);
   ap::SharedArgs a;
   a.r = rows_of(s, len);
-  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.g = s.g; a.rows = q_cap * s.g; a.narrow0 = (int)ap::shared_narrow0(s, q_cap);
+  a.q = q; a.K = K; a.V = V; a.n_q = n_q; a.q_cap = q_cap; a.rows = q_cap * s.g; a.narrow0 = (int)ap::shared_narrow0(s, q_cap);
+  a.lg = 0;
+  while ((1 << a.lg) < s.g) ++a.lg;
   a.window = seen_window(s, window); a.n_first = seen_first(s, n_first); a.out = out;
   a.plan = ap::share_plan(s, const_cast<void*>(plan));
   a.begun = reinterpret_cast<int32_t*>(base + w.begun);

@@ -65,7 +65,7 @@ struct SharedArgs {
   CacheRows r;
   const void *q, *K, *V;
   const int32_t* n_q;              // [n_inst], or null: q_cap each
-  int q_cap, g, rows, window, n_first, narrow0;
+  int q_cap, lg, rows, window, n_first, narrow0;      // lg = log2(g)
   void* out;
   SharePlan plan;
   int32_t *begun, *behind;         // workspace: [n_inst] whether there are pieces of the beginning that an instance is the first member of; of the rows behind
