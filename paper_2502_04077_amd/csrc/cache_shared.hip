@@ -886,9 +886,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
-// Joins the pieces: a wave per row of q.  OUT: float, or the type of q.
+// Joins the pieces: a wave per row of q; D / 4 lanes have a piece at a time.  OUT: float, or the type of q.
 template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(SharedArgs a) {
-  constexpr int E = D / 64;                                // outputs of a lane
+  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
   const long long at = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int inst = (int)(at / a.rows), row = (int)(at % a.rows), lane = threadIdx.x & 63;
   if (inst >= a.r.n_inst || row >= queries(a, inst) << a.lg) return;
@@ -902,51 +902,61 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
   const int ahead = first.y < 0 ? -first.y : first.y, parts = ahead + (own.y < 0 ? -own.y : own.y);
   const int step = first.y < 0 ? kNarrowRows : kPrefillRows, own_step = own.y < 0 ? kNarrowRows : kPrefillRows;
   auto slot = [&](int p) { return p < ahead ? (size_t)first.x + (size_t)step * p : (size_t)own.x + (size_t)own_step * (p - ahead); };
-  constexpr int kAhead = 16;                               // loads under way
-  float v[kAhead][E];
+  constexpr int kAhead = 8;                                // loads under way, of AT_ONCE pieces
+  const int which = lane / LANES, col = lane % LANES * 4;
+  float4v v[kAhead];
   auto load = [&](int p0) {
 #pragma unroll
-    for (int x = 0; x < kAhead; ++x)
-      if (p0 + x < parts) {
-        const float* src = a.o + slot(p0 + x) * D + lane * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[x][e] = src[e];
-      }
+    for (int x = 0; x < kAhead; ++x) {
+      const int p = p0 + x * AT_ONCE + which;
+      if (p < parts) v[x] = *reinterpret_cast<const float4v*>(a.o + slot(p) * D + col);
+    }
   };
   load(0);
   float m = lane < parts ? a.ml[slot(lane) * 2] : -INFINITY, l = lane < parts ? a.ml[slot(lane) * 2 + 1] : 0.f, top = m;
   for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, a.ml[slot(p) * 2]);
   top = wave_max(top);
   const float use = top == -INFINITY ? 0.f : top;
-  float o[E], all = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  float4v o = {0.f, 0.f, 0.f, 0.f};
+  float all = 0.f;
   for (int p0 = 0; p0 < parts; p0 += 64) {
     if (p0 > 0) {
       m = p0 + lane < parts ? a.ml[slot(p0 + lane) * 2] : -INFINITY;
       l = p0 + lane < parts ? a.ml[slot(p0 + lane) * 2 + 1] : 0.f;
     }
-    const float f = exp2_fast(m - use);
+    const float f = exp2_fast(m - use);                    // (0 behind the last piece)
     all += f * l;
     const int n = parts - p0 < 64 ? parts - p0 : 64;
-    for (int x0 = 0; x0 < n; x0 += kAhead) {
+    for (int x0 = 0; x0 < n; x0 += kAhead * AT_ONCE) {
       if (p0 + x0 > 0) load(p0 + x0);
 #pragma unroll
       for (int x = 0; x < kAhead; ++x) {
-        if (x0 + x >= n) break;
-        const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), x0 + x));
+        const float w = __shfl(f, x0 + x * AT_ONCE + which, 64);
+        if (x0 + x * AT_ONCE + which < n && w != 0.f) {    // (a piece without tiles has left no sums)
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += w == 0.f ? 0.f : w * v[x][e];            // (a piece without tiles has left no sums)
+          for (int e = 0; e < 4; ++e) o[e] += w * v[x][e];
+        }
       }
     }
   }
   all = wave_sum(all);
-  OUT* out = static_cast<OUT*>(a.out) + ((size_t)inst * a.rows + row) * D + lane * E;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float y = all == 0.f ? 0.f : o[e] / all;         // a query that sees nothing has a zero output
-    if constexpr (sizeof(OUT) == 2) out[e].bits = __builtin_bit_cast(uint16_t, (__bf16)y);
-    else out[e] = y;
+  for (int e = 0; e < 4; ++e) {
+    if (LANES <= 16) o[e] = sum16(o[e]);
+    o[e] = sum32(o[e]);
+  }
+  if (which > 0) return;
+  OUT* out = static_cast<OUT*>(a.out) + ((size_t)inst * a.rows + row) * D + col;
+  float4v y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = all == 0.f ? 0.f : o[e] / all;          // a query that sees nothing has a zero output
+  if constexpr (sizeof(OUT) == 2) {
+    bf16x4 z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = (__bf16)y[e];
+    *reinterpret_cast<bf16x4*>(out) = z;
+  } else {
+    *reinterpret_cast<float4v*>(out) = y;
   }
 }
 
