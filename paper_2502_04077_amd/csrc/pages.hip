@@ -4,7 +4,7 @@
 // pages are found without reading through those in use.  Three steps, a launch each, as none can begin before the one before has ended
 // everywhere: what every instance needs, which free pages it gets (the x-th need in the order of instances and blocks gets the x-th free
 // page), and carrying it out.  The second step knows whether there are enough; if not, the third leaves all as it is.  Counts are whole numbers,
-// so that the order of atomics does not show in any result.  Where the state does not belong to the table, what comes out is unspecified, but every
+// so that the order of atomics does not show in any result.  Where there is little to do one workgroup takes all three steps (small).  Where the state does not belong to the table, what comes out is unspecified, but every
 // page that is read or written lies in the pool.
 #include "cache_body.h"
 #include "share_internal.h"
@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kPickWgs = 64, kApplyWgs = 128;
+constexpr int kSmallThreads = 1024, kSmallSegments = 256;
 
 struct Head { int needed, lacking, live, moved; };
 
@@ -56,6 +57,8 @@ __device__ __forceinline__ void add_free(int freed, int* s_free, int32_t* info) 
   __syncthreads();
   if (threadIdx.x == 0 && *s_free != 0) atomicAdd(info, *s_free);
 }
+// Number of this wave in the workgroup.
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 // The first `rows` rows of K and V of a page, by `threads` threads.
 __device__ __forceinline__ void copy_rows(const Pages& p, int src, int dst, int rows, int tid, int threads) {
   const int n = rows * p.row_pieces;
@@ -64,6 +67,24 @@ __device__ __forceinline__ void copy_rows(const Pages& p, int src, int dst, int 
     u32x4* X = static_cast<u32x4*>(x < n ? p.K : p.V);
     const int y = x < n ? x : x - n;
     X[dst * page + y] = X[src * page + y];
+  }
+}
+
+// Whole pages of K and V, one a workgroup at a time: page(x) says where from and where to, and whether at all.  The memory's rate bounds it, and what a
+// call moves is not read again soon, so it goes past the caches: 2 x 130 MB of a pool of 4 GB 114 us (4.6 TB/s), with ordinary loads and stores 122;
+// 2 x 170 MB of sequences set aside 137 (5.0) and 142.  Two or four pages of a thread under way change nothing.
+struct Move { int src, dst; bool real; };
+template <typename PAGE>
+__device__ __forceinline__ void move_pages(const u32x4* K_src, const u32x4* V_src, u32x4* K_dst, u32x4* V_dst, int n, int page_pieces, PAGE page) {
+  for (int x = blockIdx.x; x < n; x += gridDim.x) {
+    const Move m = page(x);
+    if (!m.real) continue;
+    const size_t src = (size_t)m.src * page_pieces, dst = (size_t)m.dst * page_pieces;
+    for (int y = threadIdx.x; y < page_pieces; y += kThreads) {
+      const u32x4 k = __builtin_nontemporal_load(K_src + src + y), v = __builtin_nontemporal_load(V_src + src + y);
+      __builtin_nontemporal_store(k, K_dst + dst + y);
+      __builtin_nontemporal_store(v, V_dst + dst + y);
+    }
   }
 }
 
@@ -102,10 +123,9 @@ __device__ __forceinline__ Rows rows_of(const ResizeArgs& a, int i) {
   return r;
 }
 
-// A wave per instance: the blocks that need a page.
-__global__ __launch_bounds__(kThreads) void resize_need_kernel(ResizeArgs a) {
-  const int i = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (i >= a.p.n_inst) return;
+// A wave: the blocks of instance i that need a page.
+__device__ __forceinline__ void resize_need(const ResizeArgs& a, int i) {
+  const int lane = threadIdx.x & 63;
   const Rows r = rows_of(a, i);
   const int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
   int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
@@ -119,12 +139,14 @@ __global__ __launch_bounds__(kThreads) void resize_need_kernel(ResizeArgs a) {
   }
   if (lane == 0) at<int32_t>(a.ws, a.w.need)[i] = count;
 }
+__global__ __launch_bounds__(kThreads) void resize_need_kernel(ResizeArgs a) {
+  const int i = blockIdx.x * kWaves + wave_of();
+  if (i < a.p.n_inst) resize_need(a, i);
+}
 
-// A wave per instance j, which goes on from instance p: the new table, and whether its last page is to be copied.
-__global__ __launch_bounds__(kThreads) void fork_need_kernel(ForkArgs a) {
-  const int j = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (j >= a.p.n_inst) return;
-  const int p = a.parent[j];
+// A wave: the new table of instance j, which goes on from instance p, and whether its last page is to be copied.
+__device__ __forceinline__ void fork_need(const ForkArgs& a, int j) {
+  const int lane = threadIdx.x & 63, p = a.parent[j];
   const bool some = (unsigned)p < (unsigned)a.p.n_inst;
   int32_t* length = at<int32_t>(a.ws, a.w.length);
   int32_t* need = at<int32_t>(a.ws, a.w.need);
@@ -150,17 +172,26 @@ __global__ __launch_bounds__(kThreads) void fork_need_kernel(ForkArgs a) {
     need[j] = rest > 0 && !heir && in_pool(a.p, table[full]);
   }
 }
+__global__ __launch_bounds__(kThreads) void fork_need_kernel(ForkArgs a) {
+  const int j = blockIdx.x * kWaves + wave_of();
+  if (j < a.p.n_inst) fork_need(a, j);
+}
 
 // ---------------------------------------------------------------------------------------------------------------- free pages
 // The free pages of segments [s0, s1) are those from number `before` on; the first n of all are picked and in use from now on.  Called by a
-// workgroup; s_wave: kWaves words of LDS.
-__device__ __forceinline__ void pick_segments(const Pages& p, int s0, int s1, int before, int n, int32_t* picked, int32_t* taken, int* s_wave) {
+// workgroup of NT threads; s_wave: a word of LDS for each of its waves.
+template <int NT> __device__ __forceinline__ void pick_segments(const Pages& p, int s0, int s1, int before, int n, int32_t* picked, int32_t* taken, int* s_wave) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int s = s0; s < s1; ++s) {
-    int mine[kSegment / kThreads], count = 0;
+    if (before >= n) {                                     // (no more are wanted)
+      for (; s < s1; s += NT)
+        if (s + tid < s1) taken[s + tid] = 0;
+      return;
+    }
+    int mine[kSegment / NT], count = 0;
 #pragma unroll
-    for (int e = 0; e < kSegment / kThreads; ++e) {
-      const long long page = (long long)s * kSegment + tid * (kSegment / kThreads) + e;
+    for (int e = 0; e < kSegment / NT; ++e) {
+      const long long page = (long long)s * kSegment + tid * (kSegment / NT) + e;
       mine[e] = before < n && page < p.n_pages && p.refs[page] <= 0;
       count += mine[e];
     }
@@ -174,15 +205,15 @@ __device__ __forceinline__ void pick_segments(const Pages& p, int s0, int s1, in
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
     int rank = before + upto - count, all = 0;
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
       if (w < wave) rank += s_wave[w];
       all += s_wave[w];
     }
 #pragma unroll
-    for (int e = 0; e < kSegment / kThreads; ++e)
+    for (int e = 0; e < kSegment / NT; ++e)
       if (mine[e]) {
         if (rank >= 0 && rank < n) {
-          const int page = s * kSegment + tid * (kSegment / kThreads) + e;
+          const int page = s * kSegment + tid * (kSegment / NT) + e;
           picked[rank] = page;
           p.refs[page] = 1;
         }
@@ -192,30 +223,30 @@ __device__ __forceinline__ void pick_segments(const Pages& p, int s0, int s1, in
     before += all;
   }
 }
-__device__ __forceinline__ int sum_of(const int32_t* x, int n, int* s_wave) {     // by a workgroup
+template <int NT> __device__ __forceinline__ int sum_of(const int32_t* x, int n, int* s_wave) {     // by a workgroup
   int mine = 0;
-  for (int k = threadIdx.x; k < n; k += kThreads) mine += x[k];
+  for (int k = threadIdx.x; k < n; k += NT) mine += x[k];
   mine = sum_int(mine);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = mine;
   __syncthreads();
   int all = 0;
-  for (int w = 0; w < kWaves; ++w) all += s_wave[w];
+  for (int w = 0; w < NT / 64; ++w) all += s_wave[w];
   return all;
 }
 
-__global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
-  __shared__ int s_wave[kWaves];
+// Picks the pages of the instances' needs: workgroup `which` of `wgs`.  info as if nothing were given up.
+template <int NT> __device__ __forceinline__ void pick_pages(const Pages& p, char* ws, const PagesWs& w, int32_t* info, int which, int wgs, int* s_wave) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* need = at<int32_t>(ws, w.need);
-  const int n = sum_of(need, p.n_inst, s_wave), free = clamped(sum_of(p.seg, p.segments, s_wave), 0, p.n_pages);
-  const int each = (p.segments + gridDim.x - 1) / gridDim.x;
-  const int s0 = blockIdx.x * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
+  const int n = sum_of<NT>(need, p.n_inst, s_wave), free = clamped(sum_of<NT>(p.seg, p.segments, s_wave), 0, p.n_pages);
+  const int each = (p.segments + wgs - 1) / wgs;
+  const int s0 = which * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
   if (s0 < s1) {
-    const int before = sum_of(p.seg, s0, s_wave);
-    pick_segments(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+    const int before = s0 == 0 ? 0 : sum_of<NT>(p.seg, s0, s_wave);
+    pick_segments<NT>(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
   }
-  if (blockIdx.x > 0) return;
+  if (which > 0) return;
   if (tid == 0) {
     Head* head = at<Head>(ws, w.head);
     head->needed = n;
@@ -225,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws,
   }
   // What the instances before need.
   int done = 0;
-  for (int i0 = 0; i0 < p.n_inst; i0 += kThreads) {
+  for (int i0 = 0; i0 < p.n_inst; i0 += NT) {
     const int i = i0 + tid, x = i < p.n_inst ? need[i] : 0;
     int upto = x;
 #pragma unroll
@@ -244,70 +275,70 @@ __global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws,
     if (i < p.n_inst) at<int32_t>(ws, w.before)[i] = ahead;
   }
 }
+__global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
+  __shared__ int s_wave[kWaves];
+  pick_pages<kThreads>(p, ws, w, info, blockIdx.x, gridDim.x, s_wave);
+}
 __device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* taken) {
-  for (int s = blockIdx.x * kThreads + threadIdx.x; s < p.segments; s += gridDim.x * kThreads)
+  for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < p.segments; s += gridDim.x * blockDim.x)
     if (taken[s] > 0) atomicAdd(p.seg + s, -taken[s]);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- carrying it out
-// A workgroup has every gridDim.x-th instance.
+// Instance i's, by NT threads: a workgroup, or (64) a wave.  Returns how many pages are free now, a wave's own count.
+template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& a, int i, int tid) {
+  const Rows r = rows_of(a, i);
+  int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
+  const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
+  const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + at<int32_t>(a.ws, a.w.before)[i];
+  const int n = at<int32_t>(a.ws, a.w.need)[i], rest = r.kept & ((1 << a.p.lb) - 1);
+  int freed = 0;
+  if (n > 0 && rest > 0 && r.own < r.want) {
+    // The first block that is written may have rows that stay, of a page that others keep.
+    for (int x = 0; x < n && staged[x] <= r.own; ++x)
+      if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, NT);
+    if (NT > 64) __syncthreads();
+  }
+  for (int k0 = r.want; k0 < a.p.nb_cap; k0 += NT) {
+    const int k = k0 + tid, page = k < a.p.nb_cap ? table[k] : -1;
+    if (__any(page != -1)) freed += drop_pages(a.p, in_pool(a.p, page), page);
+    if (page != -1) table[k] = -1;
+  }
+  for (int x0 = 0; x0 < n; x0 += NT) {
+    const int x = x0 + tid;
+    const bool some = x < n && in_pool(a.p, picked[x < n ? x : 0]);
+    const int k = some ? staged[x] : 0, old = some ? table[k] : -1;
+    if (some) table[k] = picked[x];
+    if (__any(in_pool(a.p, old))) freed += drop_pages(a.p, in_pool(a.p, old), old);
+  }
+  return freed;
+}
 __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeArgs a) {
   __shared__ int s_free;
   if (at<Head>(a.ws, a.w.head)->lacking > 0) return;
-  const int tid = threadIdx.x;
-  if (tid == 0) s_free = 0;
+  if (threadIdx.x == 0) s_free = 0;
   __syncthreads();
   settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
   int freed = 0;
-  for (int i = blockIdx.x; i < a.p.n_inst; i += gridDim.x) {
-    const Rows r = rows_of(a, i);
-    int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
-    const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
-    const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + at<int32_t>(a.ws, a.w.before)[i];
-    const int n = at<int32_t>(a.ws, a.w.need)[i], rest = r.kept & ((1 << a.p.lb) - 1);
-    if (n > 0 && rest > 0 && r.own < r.want) {
-      // The first block that is written may have rows that stay, of a page that others keep.
-      for (int x = 0; x < n && staged[x] <= r.own; ++x)
-        if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, kThreads);
-      __syncthreads();
-    }
-    for (int k0 = r.want; k0 < a.p.nb_cap; k0 += kThreads) {
-      const int k = k0 + tid, page = k < a.p.nb_cap ? table[k] : -1;
-      if (__any(page != -1)) freed += drop_pages(a.p, in_pool(a.p, page), page);
-      if (page != -1) table[k] = -1;
-    }
-    for (int x0 = 0; x0 < n; x0 += kThreads) {
-      const int x = x0 + tid;
-      const bool some = x < n && in_pool(a.p, picked[x < n ? x : 0]);
-      const int k = some ? staged[x] : 0, old = some ? table[k] : -1;
-      if (some) table[k] = picked[x];
-      if (__any(in_pool(a.p, old))) freed += drop_pages(a.p, in_pool(a.p, old), old);
-    }
-  }
+  for (int i = blockIdx.x; i < a.p.n_inst; i += gridDim.x) freed += resize_apply<kThreads>(a, i, threadIdx.x);
   add_free(freed, &s_free, a.info);
 }
 
-__global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
-  __shared__ int s_free;
-  const int j = blockIdx.x, tid = threadIdx.x;
-  const bool lacking = at<Head>(a.ws, a.w.head)->lacking > 0;
+template <int NT> __device__ __forceinline__ int fork_apply(const ForkArgs& a, int j, int tid, bool lacking) {
   const int L = lacking ? -1 : at<int32_t>(a.ws, a.w.length)[j];
-  if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
   if (L < 0) {                                             // stays as it is
     if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
-    return;
+    return 0;
   }
-  if (tid == 0) s_free = 0;
-  __syncthreads();
   const int full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1), n = full + (rest > 0);
   int32_t* table = a.p.table + (size_t)j * a.p.nb_cap;
   const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
   bool copy = at<int32_t>(a.ws, a.w.need)[j] > 0;
   const int page = copy ? at<int32_t>(a.ws, a.w.picked)[at<int32_t>(a.ws, a.w.before)[j]] : 0;
   copy = copy && in_pool(a.p, page);
-  if (copy) copy_rows(a.p, staged[full], page, rest, tid, kThreads);
+  if (copy) copy_rows(a.p, staged[full], page, rest, tid, NT);
   int freed = 0;
-  for (int k0 = 0; k0 < a.p.nb_cap; k0 += kThreads) {
+  for (int k0 = 0; k0 < a.p.nb_cap; k0 += NT) {
     const int k = k0 + tid, old = k < a.p.nb_cap ? table[k] : -1;
     const bool fresh = copy && k == full;
     const int now = fresh ? page : (k < n ? staged[k] : -1);
@@ -318,7 +349,50 @@ __global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
     freed += drop_pages(a.p, changed && in_pool(a.p, old), old);
   }
   if (tid == 0) a.len_out[j] = L;
-  add_free(freed, &s_free, a.info);
+  return freed;
+}
+__global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
+  __shared__ int s_free;
+  const bool lacking = at<Head>(a.ws, a.w.head)->lacking > 0;
+  if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
+  if (threadIdx.x == 0) s_free = 0;
+  __syncthreads();
+  add_free(fork_apply<kThreads>(a, blockIdx.x, threadIdx.x, lacking), &s_free, a.info);
+}
+
+// All of it by one workgroup, an instance a wave at a time.
+template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline__ void by_one(const ARGS& a, NEED need, APPLY apply) {
+  __shared__ int s_wave[kSmallThreads / 64], s_free, s_info[2];
+  const int wave = wave_of();
+  if (threadIdx.x == 0) s_free = 0;
+  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) need(i);
+  __syncthreads();
+  pick_pages<kSmallThreads>(a.p, a.ws, a.w, s_info, 0, 1, s_wave);
+  __syncthreads();
+  const bool lacking = s_info[1] > 0;
+  if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
+  int freed = 0;
+  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) freed += apply(i, lacking);
+  if ((threadIdx.x & 63) == 0 && freed != 0) atomicAdd(&s_free, freed);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.info[0] = s_info[0] + s_free;
+    a.info[1] = s_info[1];
+  }
+}
+__global__ __launch_bounds__(kSmallThreads) void resize_small_kernel(ResizeArgs a) {
+  const int lane = threadIdx.x & 63;
+  by_one(a, [&](int i) { resize_need(a, i); }, [&](int i, bool lacking) { return lacking ? 0 : resize_apply<64>(a, i, lane); });
+}
+__global__ __launch_bounds__(kSmallThreads) void fork_small_kernel(ForkArgs a) {
+  const int lane = threadIdx.x & 63;
+  by_one(a, [&](int j) { fork_need(a, j); }, [&](int j, bool lacking) { return fork_apply<64>(a, j, lane, lacking); });
+}
+// What one workgroup does sooner than three launches, by the entries of the tables that it looks through, and the bytes that it may have to copy.
+// Resize, a table's 132 entries, 8, 32, 64, 128 instances: 8.5, 8.8, 12.2, 17.9 us, by three launches 15; fork of 32 instances with 132 entries each and
+// pages of 8 KB (K and V) 13.0 and 16.5 us, of 64 22.1 and 16.5, of 32 with 504 entries 18.9 and 16.6, with pages of 32 KB 22.3 and 16.6.
+bool small(const Pages& p, int entries, long long copied) {
+  return (long long)p.n_inst * p.nb_cap <= entries && p.segments <= kSmallSegments && copied <= 256 * 1024;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- compaction
@@ -327,10 +401,10 @@ __global__ __launch_bounds__(kThreads) void compact_list_kernel(CompactArgs a) {
   __shared__ int s_wave[kWaves];
   const Pages& p = a.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int live = p.n_pages - clamped(sum_of(p.seg, p.segments, s_wave), 0, p.n_pages);
+  const int live = p.n_pages - clamped(sum_of<kThreads>(p.seg, p.segments, s_wave), 0, p.n_pages);
   // Free pages in front: those of whole segments, and of the one that `live` lies in.
   const int sl = live / kSegment;
-  int moved = sl > 0 ? sum_of(p.seg, sl, s_wave) : 0;
+  int moved = sl > 0 ? sum_of<kThreads>(p.seg, sl, s_wave) : 0;
   {
     int x = 0;
     for (int page = sl * kSegment + tid; page < live; page += kThreads) x += p.refs[page] <= 0;
@@ -351,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void compact_list_kernel(CompactArgs a) {
   const int each = (p.segments + gridDim.x - 1) / gridDim.x;
   const int s0 = blockIdx.x * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
   if (s0 >= s1) return;
-  int before = sum_of(p.seg, s0, s_wave);                  // free pages before
+  int before = sum_of<kThreads>(p.seg, s0, s_wave);                  // free pages before
   for (int s = s0; s < s1; ++s) {
     int mine[kSegment / kThreads], count = 0;
 #pragma unroll
@@ -394,14 +468,13 @@ __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
   const Head head = *at<Head>(a.ws, a.w.head);
   const int32_t *hole = at<int32_t>(a.ws, a.w.picked), *from = at<int32_t>(a.ws, a.w.from), *rank = at<int32_t>(a.ws, a.w.rank);
   const int tid = threadIdx.x;
-  for (int x = blockIdx.x; x < head.moved; x += gridDim.x) {
-    if (!in_pool(p, from[x]) || !in_pool(p, hole[x])) continue;
-    copy_rows(p, from[x], hole[x], 1 << p.lb, tid, kThreads);
-    if (tid == 0) {
+  move_pages(static_cast<const u32x4*>(p.K), static_cast<const u32x4*>(p.V), static_cast<u32x4*>(p.K), static_cast<u32x4*>(p.V), head.moved,
+             p.row_pieces << p.lb, [&](int x) { return Move{from[x], hole[x], in_pool(p, from[x]) && in_pool(p, hole[x])}; });
+  for (int x = blockIdx.x * kThreads + tid; x < head.moved; x += gridDim.x * kThreads)
+    if (in_pool(p, from[x]) && in_pool(p, hole[x])) {
       p.refs[hole[x]] = p.refs[from[x]];
       p.refs[from[x]] = 0;
     }
-  }
   const size_t all = (size_t)p.n_inst * p.nb_cap, step = (size_t)gridDim.x * kThreads;
   for (size_t x = (size_t)blockIdx.x * kThreads + tid; x < all; x += step) {
     const int page = p.table[x];
@@ -415,18 +488,12 @@ __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
   }
 }
 
-__global__ __launch_bounds__(kThreads) void pages_copy_kernel(const u32x4* __restrict__ K_src, const u32x4* __restrict__ V_src, int n_src,
-                                                              const int32_t* __restrict__ from, u32x4* __restrict__ K_dst,
-                                                              u32x4* __restrict__ V_dst, int n_dst, const int32_t* __restrict__ to, int n,
-                                                              int page_pieces) {
-  for (int x = blockIdx.x; x < n; x += gridDim.x) {
+__global__ __launch_bounds__(kThreads) void pages_copy_kernel(const u32x4* K_src, const u32x4* V_src, int n_src, const int32_t* from, u32x4* K_dst,
+                                                              u32x4* V_dst, int n_dst, const int32_t* to, int n, int page_pieces) {
+  move_pages(K_src, V_src, K_dst, V_dst, n, page_pieces, [&](int x) {
     const int src = from == nullptr ? x : from[x], dst = to == nullptr ? x : to[x];
-    if ((unsigned)src >= (unsigned)n_src || (unsigned)dst >= (unsigned)n_dst) continue;
-    for (int y = threadIdx.x; y < page_pieces; y += kThreads) {
-      K_dst[(size_t)dst * page_pieces + y] = K_src[(size_t)src * page_pieces + y];
-      V_dst[(size_t)dst * page_pieces + y] = V_src[(size_t)src * page_pieces + y];
-    }
-  }
+    return Move{src, dst, (unsigned)src < (unsigned)n_src && (unsigned)dst < (unsigned)n_dst};
+  });
 }
 
 unsigned pick_wgs(const Pages& p) { return p.segments < kPickWgs ? p.segments : kPickWgs; }
@@ -446,6 +513,10 @@ hipError_t launch_pages_count(const Pages& p, hipStream_t st) {
 }
 
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
+  if (small(a.p, 10 * 1024, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
+    resize_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
+    return hipGetLastError();
+  }
   resize_need_kernel<<<per_wave(a.p.n_inst), kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -456,6 +527,10 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
+  if (small(a.p, 5 * 1024, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
+    fork_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
+    return hipGetLastError();
+  }
   fork_need_kernel<<<per_wave(a.p.n_inst), kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
