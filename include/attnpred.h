@@ -387,7 +387,7 @@ int ap_cache_share(ap_ctx* ctx, const int32_t* group, const int32_t* shared, voi
 size_t ap_cache_shared_workspace_bytes(const ap_ctx* ctx, int32_t q_cap);
 int ap_cache_decode_shared(ap_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* len, const void* plan, int32_t window,
                            int32_t n_first, float* out, void* ws, void* stream);
-/* Chunks of few tokens (g q_cap <= 64) go through the groups; larger ones read every instance's own rows, which costs no more. */
+/* Chunks of few tokens (g q_cap <= 32, fp32 64) go through the groups; larger ones read every instance's own rows, which costs no more. */
 int ap_cache_prefill_shared(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
                             const void* plan, int32_t window, int32_t n_first, void* out, void* ws, void* stream);
 
