@@ -161,7 +161,33 @@ class DenseRun:
         self.ctx.sparse_decode(q, K, V, t, self.idx, self.cnt, self.out, self.row, self.ws)
 
 
-class CacheRun:
+class _Lengths:
+    """Caches whose lengths `len` live on the device; the host only knows `longest`, which none exceeds."""
+
+    def _grow(self, n, by):
+        if self.longest + by > self.w.t_cap:
+            raise ValueError(f"caches of up to {self.longest} rows have no room for {by} more (t_cap = {self.w.t_cap})")
+        self.len += n
+        self.longest += by
+
+    def _grown(self, n, by, calls):
+        """The calls on caches that are n rows longer.  If one of them is refused, the lengths are what they were: rows behind them
+        hold nothing."""
+        if self.longest + by > self.w.t_cap:
+            # The bound counts every token of a chunk, the caches may be shorter: only now are the device's lengths asked, and waited for.
+            self.longest, after = torch.stack([self.len.max(), (self.len + n).max()]).tolist()
+            by = after - self.longest
+        longest = self.longest
+        self._grow(n, by)
+        try:
+            calls()
+        except Exception:
+            self.len -= n
+            self.longest = longest
+            raise
+
+
+class CacheRun(_Lengths):
     """Layers whose caches have lengths of their own: prompts of different lengths go in by chunks, every token attends to its whole
     cache (or to a window and the first rows), and every `evict_every` steps caches beyond the budget lose the rows that gathered the
     least attention weight - the eviction that the predicted selection of DecodeRun is an alternative to.  The first n_sink and the last
@@ -193,28 +219,6 @@ class CacheRun:
         self.ws = torch.zeros((size,), dtype=torch.uint8, device=self.dev)
         self.steps_done = 0
         self.longest = 0          # no cache is longer than this
-
-    def _grow(self, n, by):
-        if self.longest + by > self.w.t_cap:
-            raise ValueError(f"caches of up to {self.longest} rows have no room for {by} more (t_cap = {self.w.t_cap})")
-        self.len += n
-        self.longest += by
-
-    def _grown(self, n, by, calls):
-        """The calls on caches that are n rows longer.  If one of them is refused, the lengths are what they were: rows behind them
-        hold nothing."""
-        if self.longest + by > self.w.t_cap:
-            # The bound counts every token of a chunk, the caches may be shorter: only now are the device's lengths asked, and waited for.
-            self.longest, after = torch.stack([self.len.max(), (self.len + n).max()]).tolist()
-            by = after - self.longest
-        longest = self.longest
-        self._grow(n, by)
-        try:
-            calls()
-        except Exception:
-            self.len -= n
-            self.longest = longest
-            raise
 
     def prefill(self, q, k, v, n_new=None):
         """The next chunk of every prompt, q [n_inst][m][g][d] and k, v [n_inst][m][d] with m <= q_cap; n_new: int32 [n_inst], how many
@@ -249,3 +253,190 @@ class CacheRun:
         self.ctx.cache_evict(self.K, self.V, self.acc, self.len, self.w.budget_tokens, self.n_first, self.n_last, self.acc, self.len,
                              self.kept)
         self.longest = min(self.longest, self.w.budget_tokens)
+
+
+class PagedRun(_Lengths):
+    """Sequences whose pages come from one pool as they grow, and whose beginnings in common are held once and read once: samples and beams
+    that go on from one another (`fork`), drafted tokens that are taken back (`take_back`), sequences that end (`end`) or wait in host memory
+    (`set_aside`, `bring_back`).  Every token attends to its whole cache, or to a window and the first n_sink blocks of the workload's budget.
+
+    Every instance starts empty and alone.  Lengths, tables and counts live on the device; the host knows how many pages are free at least,
+    and asks only where that might not do.  What is refused, for want of pages too, leaves every cache as it was."""
+
+    def __init__(self, w, n_pages, device="cuda:0", q_cap=1, window=0):
+        """n_pages: of the pool, for all instances.  q_cap: most tokens of a chunk."""
+        self.w, self.q_cap, self.window, self.n_pages = w, q_cap, window, n_pages
+        self.dev = torch.device(device)
+        self.ctx = Context(n_inst=w.n_inst, g=w.g, head_dim=w.head_dim, block=w.block, hist_len=w.hist_len, t_cap=w.t_cap,
+                           k_blocks=w.k_blocks, n_sink=w.n_sink, n_local=w.n_local, c1=w.c1, c2=w.c2, kv_dtype=w.kv_dtype)
+        self.n_first = w.n_sink * w.block
+        new = lambda shape, dtype, value=0: torch.full(shape, value, dtype=dtype, device=self.dev)  # noqa: E731
+        i32, u8, n = torch.int32, torch.uint8, w.n_inst
+        self.table = new((n, w.t_cap // w.block), i32, -1)
+        self.ctx.set_block_table(self.table, n_pages)
+        self.K = new((n_pages, w.block, w.head_dim), w.torch_dtype())
+        self.V = torch.zeros_like(self.K)
+        self.state = new((self.ctx.pages_state_bytes(n_pages) // 4,), i32)
+        self.info = new((2,), i32)
+        self.pages_ws = new((max(16, self.ctx.pages_workspace_bytes(n_pages)),), u8)
+        self.len = new((n,), i32)
+        self.none_new = new((n,), i32)
+        self.group, self.shared = new((n,), i32, -1), new((n,), i32)
+        self.plan = new((max(16, self.ctx.cache_share_bytes()),), u8)
+        self.ws = new((max(16, self.ctx.cache_shared_workspace_bytes(q_cap)),), u8)
+        self.out = new((n, w.g, w.head_dim), torch.float32)
+        self.chunk_out = new((n, q_cap, w.g, w.head_dim), w.torch_dtype())
+        self.free = n_pages        # at least so many pages are free
+        self.longest = 0           # no cache is longer than this
+        self.ctx.pages_count(self.table, n_pages, self.state)
+        self.share(self.group, self.shared)
+
+    # -- pages ------------------------------------------------------------------------------------
+    def _given(self, most, call):
+        """A call that takes at most so many pages: where fewer may be free, what it says is waited for."""
+        call()
+        if most <= self.free:
+            self.free -= most
+        else:
+            self.free, lacking = self.info.tolist()
+            if lacking > 0:
+                raise MemoryError(f"{self.free} of {self.n_pages} pages are free, {lacking} too few")
+
+    def _resize(self, n_new, m):
+        """The tables of caches of `len` rows, of which n_new (None: m) are about to be written; at most m each."""
+        most = self.w.n_inst * ((m + self.w.block - 2) // self.w.block + 1) if m > 0 else 0
+        self._given(most, lambda: self.ctx.pages_resize(self.K, self.V, self.table, self.state, self.len, n_new, m, self.info, self.pages_ws))
+
+    def free_pages(self):
+        """How many pages are free (waits for the device)."""
+        self.free = int((self.state[:self.n_pages] == 0).sum())
+        return self.free
+
+    def compact(self):
+        """Moves the pages in use to the pool's front."""
+        self.ctx.pages_compact(self.K, self.V, self.table, self.state, self.info, self.pages_ws)
+
+    # -- tokens -----------------------------------------------------------------------------------
+    def prefill(self, q, k, v, n_new=None):
+        """As CacheRun.prefill: the next chunk of every sequence, q [n_inst][m][g][d], k and v [n_inst][m][d]; n_new: int32 [n_inst]."""
+        m = q.shape[1]
+        if m > self.q_cap:
+            raise ValueError(f"a chunk has at most q_cap = {self.q_cap} tokens")
+        if k.shape[:2] != q.shape[:2] or v.shape[:2] != q.shape[:2]:
+            raise ValueError(f"{list(q.shape[:2])} queries and rows k, v of {list(k.shape[:2])}, {list(v.shape[:2])}")
+        out = self.chunk_out.view(-1)[:q.numel()].view(q.shape)
+
+        def calls():
+            self._resize(n_new, m)
+            self.ctx.cache_append(k, v, n_new, self.len, self.K, self.V)
+            self.ctx.cache_prefill_shared(q, n_new, self.K, self.V, self.len, self.plan, self.window, self.n_first, out, self.ws)
+        self._grown(m if n_new is None else n_new.clamp(0, m), m, calls)
+        return out
+
+    def step(self, q, k, v):
+        """One decode step: q [n_inst][g][d], k and v [n_inst][d].  Returns the outputs, float [n_inst][g][d], a buffer that the next step uses
+        again.  (Where some sequences rest: prefill, with chunks of one token and counts.)"""
+        def calls():
+            self._resize(None, 1)
+            self.ctx.cache_append(k.unsqueeze(1), v.unsqueeze(1), None, self.len, self.K, self.V)
+            self.ctx.cache_decode_shared(q, self.K, self.V, self.len, self.plan, self.window, self.n_first, self.out, self.ws)
+        self._grown(1, 1, calls)
+        return self.out
+
+    # -- sequences --------------------------------------------------------------------------------
+    def share(self, group, shared):
+        """Says which instances have how many first rows in common, int32 [n_inst] each (group < 0: none)."""
+        self.ctx.cache_share(group, shared, self.plan)
+        self.group.copy_(group)
+        self.shared.copy_(shared)
+
+    def _regroup(self, number, members, shared):
+        """Groups by numbers in [0, 2 n_inst): they are numbered anew, by their lowest members, and who is left alone is alone."""
+        n = self.w.n_inst
+        each = torch.arange(n, device=self.dev)
+        number = torch.where(members, number, 2 * n)
+        low = torch.full((2 * n + 1,), n, device=self.dev).scatter_reduce_(0, number, each, "amin")[number]
+        high = torch.full((2 * n + 1,), -1, device=self.dev).scatter_reduce_(0, number, each, "amax")[number]
+        grouped = members & (low < high)
+        self.share(torch.where(grouped, low, -1).int(), torch.where(grouped, shared, 0).int())
+
+    def fork(self, parent):
+        """Instance j goes on from parent[j], int32 [n_inst]; one outside [0, n_inst) ends.  Those that go on from members of a group are a group,
+        and have in common what it had; those that go on from one instance alone have all its rows in common."""
+        n = self.w.n_inst
+        before = self.len.clone()
+        self._given(n, lambda: self.ctx.pages_fork(self.K, self.V, self.table, self.state, parent, before, self.len, self.info, self.pages_ws))
+        members = (parent >= 0) & (parent < n)
+        p = parent.clamp(0, n - 1).long()
+        number = torch.where(self.group[p] < 0, n + p, self.group[p].long())
+        at = torch.where(members, number, 2 * n)
+        first = torch.full((2 * n + 1,), n, device=self.dev).scatter_reduce_(0, at, p, "amin")[number]
+        last = torch.full((2 * n + 1,), -1, device=self.dev).scatter_reduce_(0, at, p, "amax")[number]
+        self._regroup(number, members, torch.where(first == last, before[p], self.shared[p]))
+
+    def _shorter(self, length):
+        before = self.len.clone()
+        self.len.copy_(length)
+        try:
+            self._resize(self.none_new, 0)
+        except Exception:
+            self.len.copy_(before)
+            raise
+
+    def take_back(self, n):
+        """The last n tokens of every cache, int32 [n_inst], are taken back (drafts that were not accepted)."""
+        self._check_each(n, torch.int32)
+        self._shorter((self.len - n.clamp(min=0)).clamp(min=0))
+        self.share(self.group, torch.minimum(self.shared, self.len))
+
+    def end(self, which):
+        """Sequences that end, bool [n_inst]: their pages are free, unless others have them too."""
+        self._check_each(which, torch.bool)
+        self._shorter(torch.where(which, 0, self.len))
+        self._regroup(self.group.clamp(min=0).long(), (self.group >= 0) & ~which, self.shared)
+
+    def _check_each(self, x, dtype):
+        if x.dtype is not dtype or x.shape != self.len.shape or x.device != self.len.device:
+            raise ValueError(f"expected {dtype} {list(self.len.shape)} on {self.len.device}")
+
+    def _check_instances(self, instances):
+        if not instances or len(set(instances)) != len(instances) or not all(0 <= i < self.w.n_inst for i in instances):
+            raise ValueError(f"expected different instances out of {self.w.n_inst}, not {instances}")
+
+    def _pages_of(self, instances, pages):
+        return torch.cat([self.table[i, :m] for i, m in zip(instances, pages)])
+
+    def set_aside(self, instances):
+        """Moves the caches of a list of instances to pinned host memory, and ends them: returns what bring_back takes.  Waits for the device."""
+        self._check_instances(instances)
+        lens = self.len[instances].tolist()
+        pages = [-(-x // self.w.block) for x in lens]
+        away = {"len": lens}
+        if sum(pages):
+            shape = (sum(pages), self.w.block, self.w.head_dim)
+            away["K"], away["V"] = (torch.empty(shape, dtype=self.K.dtype, pin_memory=True) for _ in "KV")
+            self.ctx.pages_copy(self.K, self.V, self._pages_of(instances, pages), away["K"], away["V"], None)
+            torch.cuda.current_stream(self.dev).synchronize()
+        which = torch.zeros(self.w.n_inst, dtype=torch.bool)
+        which[instances] = True
+        self.end(which.to(self.dev))
+        return away
+
+    def bring_back(self, away, instances):
+        """The caches of set_aside go on as these instances, which are empty, each alone.  Waits for the device."""
+        self._check_instances(instances)
+        if len(instances) != len(away["len"]) or max(self.len[instances].tolist()) > 0:
+            raise ValueError(f"{len(away['len'])} caches need as many empty instances, not {instances}")
+        before, longest = self.len.clone(), self.longest
+        pages = [-(-x // self.w.block) for x in away["len"]]
+        self.len[instances] = torch.tensor(away["len"], dtype=torch.int32, device=self.dev)
+        self.longest = max(self.longest, max(away["len"]))
+        try:
+            self._given(sum(pages), lambda: self.ctx.pages_resize(self.K, self.V, self.table, self.state, self.len, self.none_new, 0, self.info, self.pages_ws))
+            if sum(pages):
+                self.ctx.pages_copy(away["K"], away["V"], None, self.K, self.V, self._pages_of(instances, pages))
+                torch.cuda.current_stream(self.dev).synchronize()
+        except Exception:
+            self.len.copy_(before)
+            self.longest = longest
+            raise
