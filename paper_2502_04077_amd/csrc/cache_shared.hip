@@ -886,6 +886,48 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
+// A row of q over what it sees alone, as plain sums: D / 4 lanes have a row of the cache at a time, four dims each.  l: this lane's part of the sum of
+// probabilities, o: of the output.
+template <typename T, int D> __device__ __forceinline__ void one_row(const SharedArgs& a, int inst, int row, float& l, float4v& o) {
+  constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
+  const int lane = threadIdx.x & 63, which = lane / LANES, col = lane % LANES * 4;
+  const int p = clamped(a.r.len[inst], 0, a.r.t_cap) - queries(a, inst) + (row >> a.lg);
+  const int lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0, f = a.n_first < lo ? a.n_first : lo;
+  const TablePages pages = pages_of(a.r, inst);
+  auto four = [&](const void* from, size_t r) {
+    float4v x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (sizeof(T) == 2) x[e] = (float)static_cast<const __bf16*>(from)[r * D + col + e];
+      else x[e] = static_cast<const float*>(from)[r * D + col + e];
+    }
+    return x;
+  };
+  const float4v q = four(a.q, (size_t)inst * a.rows + row);
+  const float scale = kLog2E / sqrtf((float)D);
+  float m = -INFINITY;
+  l = 0.f;
+  o = float4v{0.f, 0.f, 0.f, 0.f};
+  for (int x = which; x < f + (p - lo + 1); x += AT_ONCE) {
+    const int j = x < f ? x : lo + (x - f);
+    const size_t r = pages.at(j & ~7) + (j & 7);
+    const float4v k = four(a.K, r), v = four(a.V, r);
+    float s = (q[0] * k[0] + q[1] * k[1]) + (q[2] * k[2] + q[3] * k[3]);
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
+    if (s == -INFINITY) continue;
+    const float top = fmaxf(m, s), shrink = m == -INFINITY ? 0.f : exp2_fast((m - top) * scale), w = exp2_fast((s - top) * scale);
+    l = l * shrink + w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * shrink + w * v[e];
+    m = top;
+  }
+  const float top = wave_max(m), shrink = m == -INFINITY ? 0.f : exp2_fast((m - top) * scale);
+  l = col == 0 ? l * shrink : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] *= shrink;
+}
+
 // Joins the pieces: a wave per row of q; D / 4 lanes have a piece at a time.  OUT: float, or the type of q.
 template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads) void cache_shared_join_kernel(SharedArgs a) {
   constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
@@ -939,11 +981,20 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
       }
     }
   }
-  all = wave_sum(all);
+  auto add_up = [&]() {
+    all = wave_sum(all);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (LANES <= 16) o[e] = sum16(o[e]);
-    o[e] = sum32(o[e]);
+    for (int e = 0; e < 4; ++e) {
+      if (LANES <= 16) o[e] = sum16(o[e]);
+      o[e] = sum32(o[e]);
+    }
+  };
+  add_up();
+  // A row of the cache that no finite number is in makes NaN of every row of q that its tile is read for, also of those that do not see it: 0 x NaN.
+  // Where a row is NaN it is computed again by itself.
+  if (__any((all != all) | (o[0] != o[0]) | (o[1] != o[1]) | (o[2] != o[2]) | (o[3] != o[3]))) {
+    one_row<T, D>(a, inst, row, all, o);
+    add_up();
   }
   if (which > 0) return;
   OUT* out = static_cast<OUT*>(a.out) + ((size_t)inst * a.rows + row) * D + col;
