@@ -168,7 +168,7 @@ class Context:
         self._h = h
         self._lib = lib
         # what the cache_* calls check their tensors against on every call
-        self._n, self._g, self._d, self._t_cap = n_inst, g, head_dim, t_cap
+        self._n, self._g, self._d, self._t_cap, self._b = n_inst, g, head_dim, t_cap, block
         self._dtype = torch.bfloat16 if self.cfg.kv_dtype == AP_BF16 else torch.float32
         self._kv_numel, self._kv_unit = n_inst * t_cap * head_dim, t_cap * head_dim      # of K; of a cache, or a page
         self._decode_ws = [self.cache_workspace_bytes(0, weights) for weights in (False, True)]
@@ -364,17 +364,17 @@ class Context:
 
     def _pool(self, K, V):
         """Checks the pools K and V [n_pages][b][d]; the device they lie on, and their pages."""
-        dev = K.get_device()
-        if K.dim() != 3 or K.shape[1:] != (self.cfg.block, self._d) or K.shape != V.shape or K.dtype is not self._dtype or V.dtype is not self._dtype:
-            raise ValueError(f"K and V: two pools [n_pages][{self.cfg.block}][{self._d}] of one shape, in the context's dtype")
+        dev, shape = K.get_device(), K.shape
+        if len(shape) != 3 or shape[1] != self._b or shape[2] != self._d or V.shape != shape or K.dtype is not self._dtype or V.dtype is not self._dtype:
+            raise ValueError(f"K and V: two pools [n_pages][{self._b}][{self._d}] of one shape, in the context's dtype")
         if dev < 0 or V.get_device() != dev or not (K.is_contiguous() and V.is_contiguous()):
             raise ValueError("K and V: expected contiguous tensors on one device")
-        return dev, K.shape[0]
+        return dev, shape[0]
 
     def _pages_state(self, table, state, n_pages, dev):
-        nb, key = self._t_cap // self.cfg.block, n_pages
-        if self._pages[0] != key:                             # (the sizes of a pool, asked once)
-            self._pages = (key, self.pages_state_bytes(n_pages) // 4, self.pages_workspace_bytes(n_pages))
+        nb = self._t_cap // self._b
+        if self._pages[0] != n_pages:                             # (the sizes of a pool, asked once)
+            self._pages = (n_pages, self.pages_state_bytes(n_pages) // 4, self.pages_workspace_bytes(n_pages))
         return self._cache_arg("table", table, torch.int32, (self._n, nb), dev), self._cache_arg("state", state, torch.int32, (self._pages[1],), dev)
 
     def pages_count(self, table, n_pages, state) -> None:
@@ -411,24 +411,36 @@ class Context:
 
     def pages_copy(self, K_src, V_src, src, K_dst, V_dst, dst, n=None) -> None:
         """Pools [..][b][d], on the device or in pinned host memory; src, dst: int32 [n] or None (0, 1, 2, ...; with both None, n says how many)."""
-        dev = max(t.get_device() for t in (K_src, K_dst, *(x for x in (src, dst) if x is not None)))
-        for a, b in ((K_src, V_src), (K_dst, V_dst)):
-            if a.dim() != 3 or a.shape[1:] != (self.cfg.block, self._d) or a.shape != b.shape or a.dtype is not self._dtype or b.dtype is not self._dtype:
-                raise ValueError(f"K and V: pools [..][{self.cfg.block}][{self._d}] in the context's dtype")
-            for t in (a, b):
-                if not t.is_contiguous() or not (t.get_device() == dev if t.is_cuda else t.is_pinned()):
-                    raise ValueError("pools: expected contiguous tensors on one device, or in pinned host memory")
+        dev = K_src.get_device()
+        for t in (K_dst, src, dst):                           # (the first of them that lies on a device)
+            if dev < 0 and t is not None:
+                dev = t.get_device()
         if dev < 0:
             raise ValueError("pools: one of them at least lies on a device")
-        counts = {x.numel() for x in (src, dst) if x is not None} | ({n} if n is not None else set())
-        if len(counts) != 1:
-            raise ValueError("src and dst: as many entries each; n where both are None")
-        n, = counts
-        if n < 0 or any(x is None and n > t.shape[0] for x, t in ((src, K_src), (dst, K_dst))):
+        n_src, n_dst = self._moved(K_src, V_src, dev), self._moved(K_dst, V_dst, dev)
+        for x in (src, dst):
+            if x is not None:
+                if n is not None and x.numel() != n:
+                    raise ValueError("src and dst: as many entries each, n")
+                n = x.numel()
+        if n is None:
+            raise ValueError("n: where src and dst are None")
+        if n < 0 or (src is None and n > n_src) or (dst is None and n > n_dst):
             raise ValueError(f"{n} pages are more than a pool has")
-        list_of = lambda name, x: None if x is None else self._cache_arg(name, x, torch.int32, (n,), dev)  # noqa: E731
-        self._cache_call(dev, self._lib.ap_pages_copy, self._h, K_src.data_ptr(), V_src.data_ptr(), K_src.shape[0], list_of("src", src),
-                         K_dst.data_ptr(), V_dst.data_ptr(), K_dst.shape[0], list_of("dst", dst), n)
+        arg = self._cache_arg
+        self._cache_call(dev, self._lib.ap_pages_copy, self._h, K_src.data_ptr(), V_src.data_ptr(), n_src,
+                         None if src is None else arg("src", src, torch.int32, (n,), dev), K_dst.data_ptr(), V_dst.data_ptr(), n_dst,
+                         None if dst is None else arg("dst", dst, torch.int32, (n,), dev), n)
+
+    def _moved(self, K, V, dev) -> int:
+        """Checks the pools K and V of pages that are moved; their pages."""
+        shape = K.shape
+        if len(shape) != 3 or shape[1] != self._b or shape[2] != self._d or V.shape != shape or K.dtype is not self._dtype or V.dtype is not self._dtype:
+            raise ValueError(f"K and V: pools [..][{self._b}][{self._d}] in the context's dtype")
+        for t in (K, V):
+            if not t.is_contiguous() or (t.get_device() != dev and (t.is_cuda or not t.is_pinned())):
+                raise ValueError("pools: expected contiguous tensors on one device, or in pinned host memory")
+        return shape[0]
 
     # -- attention of instances whose first rows are the same ------------------------------------
     def cache_share_bytes(self) -> int:
