@@ -9,9 +9,15 @@
 // out_x = sum over its sources of exp(m_x - m) o_x / sum of exp(m_x - m) l_x, for m the largest m_x.
 //
 // A source's rows of q are in tiles of 128, its rows of K and V in tiles of 64 (fp32: 32); where a tile has no more than 32 rows of q, which is
-// memory-bound, in groups of 16.  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each, and those of
+// memory-bound, in groups of 32 (fp32, d = 128: 16).  The products of many rows of q, of all sources one after the other, are cut into equal shares, a workgroup each, and those of
 // few rows into shares of a wave each: the one needs the matrix unit, the other the memory, and a CU has room for a workgroup of both.  Whoever has a
 // share leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
+//
+// 64 sequences of 40 to 2050 rows behind 8190 in common (8 KV heads, g = 4, d = 128, decode) take 56 us; their 172 MB are read in 24 at the rate of a large
+// read.  Of the first launch's 50 us 7 go by until the shares are known (two trips to memory, sums over the sources, the sources of a share), 5 to 8 until a
+// piece's first product (table, rows; members, lengths, queries), and the shares' ends lie 5 apart.  A tile of 64 rows takes a workgroup 2.4 us (128 rows of
+// q: 0.88 PFLOP/s, the matrix unit) and 3.3 where probabilities keep 24 bits (the same), a group of 32 a wave 3 to 4 us (two groups under way a wave: bytes in flight).
+// Four samples of one prompt of 2041 rows take 21 us, which is this chain and the second launch's.
 #include "cache_tiles.h"
 #include "share_internal.h"
 
@@ -87,13 +93,15 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- sources
-constexpr int kGroup = 16;          // rows of the cache that a wave with few rows of q goes over at a time
+// Rows of the cache that a wave with few rows of q goes over at a time, as many as its part of LDS holds: 16 or 32.
+template <typename T, int D> constexpr int kGroup = sizeof(T) == 4 && D == 128 ? 16 : 32;
 constexpr int kSharedLds = 64 * 1024;       // two workgroups a CU
 // What a share counts, in tenths of a microsecond: of a workgroup's time a tile of the cache, and what a tile of rows of q costs beside them; of a
-// wave's time a group, and the same.  The least shares.
+// wave's time a group, and the same.  The least shares.  (As measured, and then varied by a third either way: no time of ten calls, 20 to 130 us, moves
+// by more than 4 %.)
 template <typename T, bool EXACT> struct Counts {
-  static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 24), WIDE_FRONT = 60, WIDE_LEAST = 120;
-  static constexpr int NARROW = sizeof(T) == 4 ? 24 : 16, NARROW_FRONT = 50, NARROW_LEAST = 64;
+  static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 24), WIDE_FRONT = sizeof(T) == 4 ? 60 : 80, WIDE_LEAST = 120;
+  static constexpr int NARROW = sizeof(T) == 4 ? 24 : 32, NARROW_FRONT = 50, NARROW_LEAST = sizeof(T) == 4 ? 64 : 90;
 };
 
 // Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
@@ -520,25 +528,26 @@ template <int N, int R, int FIRST = 0> __device__ __forceinline__ void landed_be
   }
 }
 
-// The last rows of q of a source, up to 16 RB, over its groups [u_begin, u_end) of 16 cache rows, by a wave: RING groups of K and V are on their way to
-// LDS, past the registers.  A lane has, of each 16 rows of q, scores of row n and of four cache rows, which are the second product's operand as they are,
-// and sums of four of each 16 dims.  slot: of the first of the rows.  lds: RING groups.
+// The last rows of q of a source, up to 16 RB, over its groups [u_begin, u_end) of 16 or 32 cache rows, by a wave: RING groups of K and V are on their way
+// to LDS, past the registers.  A lane has, of each 16 rows of q, scores of row n and of four of each 16 cache rows, which are the second product's operand as
+// they are, and sums of four of each 16 dims.  slot: of the first of the rows.  lds: RING groups.  Groups of 32 against two of 16 under way: drafts of 16
+// sequences 45.8 -> 44.5 us, 42 sequences behind 6 prompts 61 -> 59, the 64 above 57.5 -> 56.
 template <typename T, int D, bool EXACT, int RING, int RB>
 __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& s, int u_begin, int u_end, size_t slot, const u32x4* lds) {
   using F = Form<T, D>;
-  constexpr int KS = F::PIECES / 4, DB = D / 16, GROUP = kGroup * F::PIECES, N = GROUP / 64;       // pieces of a group's K, or V, and loads
+  constexpr int G = kGroup<T, D>, XS = G / 16, KS = F::PIECES / 4, DB = D / 16, GROUP = G * F::PIECES, N = GROUP / 64;     // pieces of a group's K, or V, and loads
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4, count = u_end - u_begin;
-  const Tiling tiling = tiling_of<kGroup>(s);
+  const Tiling tiling = tiling_of<G>(s);
   const TablePages pages = pages_of(a.r, s.inst);
   const unsigned ring = lds_address(lds);
-  auto fetch = [&](int it) { return fetch_of<kGroup, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * kGroup); };
+  auto fetch = [&](int it) { return fetch_of<G, F::PIECES>(a, pages, s, tiling.tile(u_begin + (it < count ? it : count - 1)) * G); };
   auto at = [&](int it) { return (it % RING) * 2 * GROUP; };
-  Fetch<kGroup> next = fetch(0);
+  Fetch<G> next = fetch(0);
 #pragma unroll
   for (int it = 0; it < RING; ++it)
     if (it < count) {
-      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
-      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      send_rows<G, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<G, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
       next = fetch(it + 1);
     }
   Query q[RB];
@@ -566,52 +575,62 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
 #pragma unroll
     for (int l = 0; l < KS; ++l) asm volatile("" : "+v"(qf[y][l]));
   for (int it = 0; it < count; ++it) {
-    const int t0 = tiling.tile(u_begin + it) * kGroup, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
+    const int t0 = tiling.tile(u_begin + it) * G, behind = count - 1 - it;           // groups that were sent for after this one, RING - 1 at most
     const u32x4 *Kt = lds + at(it), *Vt = Kt + GROUP;
     const bool more = it + RING < count;
     landed_behind<2 * N, RING, N>(behind);
-    // Rows t0 + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
+    // Rows t0 + 16 x + 4 kg + r, of query n.  fp32 products go into four sums, whose roundings are smaller than those of one over all of d.
     constexpr int SUMS = sizeof(T) == 2 ? 1 : 4;
-    float4v sums[RB][SUMS], c[RB];
+    float4v c[RB][XS];
 #pragma unroll
-    for (int y = 0; y < RB; ++y)
+    for (int x = 0; x < XS; ++x) {
+      float4v sums[RB][SUMS];
 #pragma unroll
-      for (int x = 0; x < SUMS; ++x) sums[y][x] = float4v{0.f, 0.f, 0.f, 0.f};
+      for (int y = 0; y < RB; ++y)
 #pragma unroll
-    for (int l = 0; l < KS; ++l) {
-      const u32x4 k = Kt[n * F::PIECES + F::k_place(n, 4 * l + kg)];
+        for (int e = 0; e < SUMS; ++e) sums[y][e] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int y = 0; y < RB; ++y) {
-        if constexpr (sizeof(T) == 2) {
-          sums[y][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[y][l]), sums[y][0], 0, 0, 0);
-        } else {
+      for (int l = 0; l < KS; ++l) {
+        const u32x4 k = Kt[(16 * x + n) * F::PIECES + F::k_place(16 * x + n, 4 * l + kg)];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sums[y][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[y][l][e]), sums[y][e], 0, 0, 0);
+        for (int y = 0; y < RB; ++y) {
+          if constexpr (sizeof(T) == 2) {
+            sums[y][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qf[y][l]), sums[y][0], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sums[y][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[y][l][e]), sums[y][e], 0, 0, 0);
+          }
         }
       }
-    }
 #pragma unroll
-    for (int y = 0; y < RB; ++y) {
-      c[y] = sums[y][0];
-      if constexpr (SUMS == 4) {
+      for (int y = 0; y < RB; ++y) {
+        c[y][x] = sums[y][0];
+        if constexpr (SUMS == 4) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) c[y][r] = (sums[y][0][r] + sums[y][1][r]) + (sums[y][2][r] + sums[y][3][r]);
+          for (int r = 0; r < 4; ++r) c[y][x][r] = (sums[y][0][r] + sums[y][1][r]) + (sums[y][2][r] + sums[y][3][r]);
+        }
       }
     }
     if (more) {
       lds_read();
-      send_rows<kGroup, F, false, true>(next, s, 0, ring + at(it) * 16);
+      send_rows<G, F, false, true>(next, s, 0, ring + at(it) * 16);
     }
-    if (!all_seen<kGroup>(a, s, t0, p_min, p_max)) {
+    if (!all_seen<G>(a, s, t0, p_min, p_max)) {
 #pragma unroll
       for (int y = 0; y < RB; ++y)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) c[y][r] = hidden(a, s, q[y], t0 + 4 * kg + r) ? -INFINITY : c[y][r];
+        for (int x = 0; x < XS; ++x)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) c[y][x][r] = hidden(a, s, q[y], t0 + 16 * x + 4 * kg + r) ? -INFINITY : c[y][x][r];
     }
 #pragma unroll
     for (int y = 0; y < RB; ++y) {
-      float top = fmaxf(fmaxf(c[y][0], c[y][1]), fmaxf(c[y][2], c[y][3]));
+      float top = c[y][0][0];
+#pragma unroll
+      for (int x = 0; x < XS; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, c[y][x][r]);
       top = max32(max16(top));
       const float ref = fmaxf(m[y], ceilf(top * scale));   // a whole number in units of log2, as above
       if (__any(ref != m[y])) {
@@ -624,9 +643,15 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
         m[y] = ref;
       }
       const float use = m[y] == -INFINITY ? 0.f : m[y];
+      float part[XS];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) c[y][r] = exp2_of(c[y][r], scale, use);
-      sum[y] += (c[y][0] + c[y][1]) + (c[y][2] + c[y][3]);
+      for (int x = 0; x < XS; ++x) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[y][x][r] = exp2_of(c[y][x][r], scale, use);
+        part[x] = (c[y][x][0] + c[y][x][1]) + (c[y][x][2] + c[y][x][3]);
+      }
+      if constexpr (XS == 2) part[0] += part[1];
+      sum[y] += part[0];
     }
     // This group's V: behind it came the later groups, and the K that was just sent for.
     if (more) landed<2 * N * (RING - 1) + N>();
@@ -634,40 +659,44 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
     if constexpr (sizeof(T) == 2) {
       constexpr int PARTS = EXACT ? 3 : 1;
       typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-      short4v pb[RB][PARTS];
 #pragma unroll
-      for (int y = 0; y < RB; ++y) {
-        unsigned two[2][PARTS];
-        in_parts<PARTS>(c[y][0], c[y][1], two[0]);
-        in_parts<PARTS>(c[y][2], c[y][3], two[1]);
+      for (int x = 0; x < XS; ++x) {
+        short4v v[DB];
+        const int r = 16 * x + 4 * kg + (n >> 2);
 #pragma unroll
-        for (int w = 0; w < PARTS; ++w) pb[y][w] = __builtin_bit_cast(short4v, u32x2{two[0][w], two[1][w]});
-      }
-      const int r = 4 * kg + (n >> 2);
+        for (int b = 0; b < DB; ++b) {
+          const int col = 16 * b + 4 * (n & 3);
+          const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
+          v[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
+        }
 #pragma unroll
-      for (int b = 0; b < DB; ++b) {
-        const int col = 16 * b + 4 * (n & 3);
-        const char* from = reinterpret_cast<const char*>(Vt + r * F::PIECES + F::v_place(r, col / 8)) + (col % 8) * 2;
-        const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)from);
+        for (int y = 0; y < RB; ++y) {
+          unsigned two[2][PARTS];
+          in_parts<PARTS>(c[y][x][0], c[y][x][1], two[0]);
+          in_parts<PARTS>(c[y][x][2], c[y][x][3], two[1]);
 #pragma unroll
-        for (int y = 0; y < RB; ++y)
+          for (int w = PARTS - 1; w >= 0; --w)
 #pragma unroll
-          for (int w = PARTS - 1; w >= 0; --w) o[y][b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, pb[y][w], o[y][b], 0, 0, 0);
+            for (int b = 0; b < DB; ++b)
+              o[y][b] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[b], __builtin_bit_cast(short4v, u32x2{two[0][w], two[1][w]}), o[y][b], 0, 0, 0);
+        }
       }
     } else {
       const float* Vf = reinterpret_cast<const float*>(Vt);
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
+      for (int x = 0; x < XS; ++x)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float v = Vf[(4 * kg + r) * D + 16 * b + n];
+        for (int b = 0; b < DB; ++b)
 #pragma unroll
-          for (int y = 0; y < RB; ++y) o[y][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, c[y][r], o[y][b], 0, 0, 0);
-        }
+          for (int r = 0; r < 4; ++r) {
+            const float v = Vf[(16 * x + 4 * kg + r) * D + 16 * b + n];
+#pragma unroll
+            for (int y = 0; y < RB; ++y) o[y][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, c[y][x][r], o[y][b], 0, 0, 0);
+          }
     }
     if (more) {
       lds_read();
-      send_rows<kGroup, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
+      send_rows<G, F, true, true>(next, s, 0, ring + (at(it) + GROUP) * 16);
       next = fetch(it + RING + 1);
     }
   }
@@ -715,7 +744,7 @@ template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
+  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup<T, D> * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
   static_assert(RING >= 1 && 4 * F::TILE * 16 <= kSharedLds, "LDS");
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][group]
   __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[1 + kWaves];
@@ -750,7 +779,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
           const int x = i_begin + i0 + k;
           const bool mine = i0 + k < chunk && x < sources;
           wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
-          narrow[k] = mine ? narrow_size<C, kGroup>(s[k]) : 0;
+          narrow[k] = mine ? narrow_size<C, kGroup<T, D>>(s[k]) : 0;
           // Which sources have pieces, for the join: the instances, and the groups by their first member.
           if (pass == 0 && mine && x % kShareWgs == (int)blockIdx.x) {
             int32_t* some = x < a.r.n_inst ? a.behind + x : a.begun + clamped(s[k].inst, 0, a.r.n_inst - 1);
@@ -868,7 +897,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   unsigned left = __builtin_amdgcn_readfirstlane(mine.left), r = x_first < sources ? __builtin_amdgcn_readfirstlane((unsigned)s_from[1 + wave]) : 0;
   for (int x = x_first; left > 0 && x < sources; ++x, r = 0) {
     const Source s = uniform(x - x_first < kListed ? s_source[1 + wave][x - x_first] : source_of(a, x));
-    const unsigned size = narrow_size<C, kGroup>(s);
+    const unsigned size = narrow_size<C, kGroup<T, D>>(s);
     if (size <= r) continue;
     const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, per, left, C::NARROW_LEAST);
     left -= c.n < left ? c.n : left;

