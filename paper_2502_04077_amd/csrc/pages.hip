@@ -271,7 +271,7 @@ template <int NT> __device__ __forceinline__ void pick_pages(const Pages& p, cha
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
     int ahead = done + upto - x;
-    for (int v = 0; v < kWaves; ++v) {
+    for (int v = 0; v < NT / 64; ++v) {
       if (v < wave) ahead += s_wave[v];
       done += s_wave[v];
     }
@@ -391,11 +391,12 @@ __global__ __launch_bounds__(kSmallThreads) void fork_small_kernel(ForkArgs a) {
   const int lane = threadIdx.x & 63;
   by_one(a, [&](int j) { fork_need(a, j); }, [&](int j, bool lacking) { return fork_apply<64>(a, j, lane, lacking); });
 }
-// What one workgroup does sooner than three launches, by the entries of the tables that it looks through, and the bytes that it may have to copy.
-// Resize, a table's 132 entries, 8, 32, 64, 128 instances: 8.5, 8.8, 12.2, 17.9 us, by three launches 15; fork of 32 instances with 132 entries each and
-// pages of 8 KB (K and V) 13.0 and 16.5 us, of 64 22.1 and 16.5, of 32 with 504 entries 18.9 and 16.6, with pages of 32 KB 22.3 and 16.6.
-bool small(const Pages& p, int entries, long long copied) {
-  return (long long)p.n_inst * p.nb_cap <= entries && p.segments <= kSmallSegments && copied <= 256 * 1024;
+// What one workgroup does sooner than three launches: few instances, tables that are looked through quickly, and few bytes that it may have to copy.
+// Resize, a table's 132 entries, 8, 32, 64, 128 instances: 8.5, 8.8, 12.2, 17.9 us, by three launches 15; of 64 with 252 entries, 63 of them to be given
+// out each, 19 and 15.  Fork of 32 instances with 132 entries each and pages of 8 KB (K and V) 13.0 and 16.5 us, of 64 22.1 and 16.5, of 32 with 504
+// entries 18.9 and 16.6, with pages of 32 KB 22.3 and 16.6.
+bool small(const Pages& p, int instances, long long copied) {
+  return p.n_inst <= instances && (long long)p.n_inst * p.nb_cap <= 160 * instances && p.segments <= kSmallSegments && copied <= 256 * 1024;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- compaction
@@ -516,7 +517,7 @@ hipError_t launch_pages_count(const Pages& p, hipStream_t st) {
 }
 
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
-  if (small(a.p, 10 * 1024, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
+  if (small(a.p, 64, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
     resize_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
     return hipGetLastError();
   }
@@ -530,7 +531,7 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
-  if (small(a.p, 5 * 1024, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
+  if (small(a.p, 32, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
     fork_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
     return hipGetLastError();
   }

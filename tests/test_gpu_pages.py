@@ -25,6 +25,9 @@ SHAPES = [  # n, nb, n_pages, b, d, dtype
     (4, 130, 600, 8, 64, "bf16"),          # rows of a table longer than a wave
     (300, 8, 1500, 8, 64, "bf16"),         # more instances than threads of a workgroup, pages in two segments
     (6, 400, 2049, 8, 64, "bf16"),         # one page in the third segment
+    (700, 7, 3500, 8, 64, "bf16"),         # more instances than a fourth of the threads of a large workgroup
+    (1270, 4, 4000, 8, 64, "bf16"),        # more than all of them
+    (1200, 8, 7000, 8, 64, "bf16"),        # a fork in three launches, a resize in one
 ]
 
 
