@@ -740,6 +740,8 @@ template <unsigned FRONT, unsigned EACH> __device__ __forceinline__ Cut cut_of(u
   return c;
 }
 
+template <int N> struct Number { static constexpr int value = N; };
+
 template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
@@ -770,22 +772,32 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll 1
     for (int i0 = 0; i0 < chunk; i0 += kHeld) {
       // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's, whose loads are under way together; they are held where these are all.
-      if (pass == 0 || chunk > kHeld) {
-        Source s[kHeld];
+      auto look = [&](auto some) {
+        constexpr int M = decltype(some)::value;
+        Source s[M];
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) s[k] = source_of(a, i0 + k < chunk && i_begin + i0 + k < places ? i_begin + i0 + k : 0);
+        for (int k = 0; k < M; ++k) s[k] = source_of(a, i0 + k < chunk && i_begin + i0 + k < places ? i_begin + i0 + k : 0);
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) {
+          wide[k] = 0;
+          narrow[k] = 0;
+          if (k >= M) continue;
+          const Source& y = s[k < M ? k : 0];
           const int x = i_begin + i0 + k;
           const bool mine = i0 + k < chunk && x < sources;
-          wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(s[k]) * (unsigned)s[k].wide() : 0;
-          narrow[k] = mine ? narrow_size<C, kGroup<T, D>>(s[k]) : 0;
+          wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(y) * (unsigned)y.wide() : 0;
+          narrow[k] = mine ? narrow_size<C, kGroup<T, D>>(y) : 0;
           // Which sources have pieces, for the join: the instances, and the groups by their first member.
           if (pass == 0 && mine && x % kShareWgs == (int)blockIdx.x) {
-            int32_t* some = x < a.r.n_inst ? a.behind + x : a.begun + clamped(s[k].inst, 0, a.r.n_inst - 1);
-            *some = wide[k] + narrow[k] > 0;
+            int32_t* has = x < a.r.n_inst ? a.behind + x : a.begun + clamped(y.inst, 0, a.r.n_inst - 1);
+            *has = wide[k] + narrow[k] > 0;
           }
         }
+      };
+      if (pass == 0 || chunk > kHeld) {
+        if (chunk == 1) look(Number<1>());
+        else if (chunk <= 3) look(Number<3>());
+        else look(Number<kHeld>());
       }
       if (pass == 0) {
 #pragma unroll
