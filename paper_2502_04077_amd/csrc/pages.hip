@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kPickWgs = 64, kApplyWgs = 128;
-constexpr int kSmallThreads = 1024, kSmallSegments = 256;
+constexpr int kSmallThreads = 1024, kSmallSegments = 256, kSmallInstances = 64;
 
 struct Head { int needed, lacking, live, moved; };
 
@@ -239,15 +239,17 @@ template <int NT> __device__ __forceinline__ int sum_of(const int32_t* x, int n,
 }
 
 // Picks the pages of the instances' needs: workgroup `which` of `wgs`.  info as if nothing were given up.
-template <int NT> __device__ __forceinline__ void pick_pages(const Pages& p, char* ws, const PagesWs& w, int32_t* info, int which, int wgs, int* s_wave) {
+__global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
+  __shared__ int s_wave[kWaves];
+  const int which = blockIdx.x, wgs = gridDim.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* need = at<int32_t>(ws, w.need);
-  const int n = sum_of<NT>(need, p.n_inst, s_wave), free = clamped(sum_of<NT>(p.seg, p.segments, s_wave), 0, p.n_pages);
+  const int n = sum_of<kThreads>(need, p.n_inst, s_wave), free = clamped(sum_of<kThreads>(p.seg, p.segments, s_wave), 0, p.n_pages);
   const int each = (p.segments + wgs - 1) / wgs;
   const int s0 = which * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
   if (s0 < s1) {
-    const int before = s0 == 0 ? 0 : sum_of<NT>(p.seg, s0, s_wave);
-    pick_segments<NT>(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+    const int before = s0 == 0 ? 0 : sum_of<kThreads>(p.seg, s0, s_wave);
+    pick_segments<kThreads>(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
   }
   if (which > 0) return;
   if (tid == 0) {
@@ -259,7 +261,7 @@ template <int NT> __device__ __forceinline__ void pick_pages(const Pages& p, cha
   }
   // What the instances before need.
   int done = 0;
-  for (int i0 = 0; i0 < p.n_inst; i0 += NT) {
+  for (int i0 = 0; i0 < p.n_inst; i0 += kThreads) {
     const int i = i0 + tid, x = i < p.n_inst ? need[i] : 0;
     int upto = x;
 #pragma unroll
@@ -271,16 +273,12 @@ template <int NT> __device__ __forceinline__ void pick_pages(const Pages& p, cha
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
     int ahead = done + upto - x;
-    for (int v = 0; v < NT / 64; ++v) {
+    for (int v = 0; v < kWaves; ++v) {
       if (v < wave) ahead += s_wave[v];
       done += s_wave[v];
     }
     if (i < p.n_inst) at<int32_t>(ws, w.before)[i] = ahead;
   }
-}
-__global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
-  __shared__ int s_wave[kWaves];
-  pick_pages<kThreads>(p, ws, w, info, blockIdx.x, gridDim.x, s_wave);
 }
 __device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* taken) {
   for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < p.segments; s += gridDim.x * blockDim.x)
@@ -363,6 +361,36 @@ __global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
   add_free(fork_apply<kThreads>(a, blockIdx.x, threadIdx.x, lacking), &s_free, a.info);
 }
 
+// As pick_pages, by one workgroup for kSmallInstances instances and kSmallSegments segments at most: what is loaded is asked for together.
+__device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const PagesWs& w, int* info, int* s_wave) {
+  __shared__ int s_needed, s_sums[kSmallSegments / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (tid < kSmallSegments) {
+    const int x = tid < p.n_inst ? at<int32_t>(ws, w.need)[tid] : 0, segment = sum_int(tid < p.segments ? p.seg[tid] : 0);
+    if (lane == 0) s_sums[tid >> 6] = segment;
+    if (tid < kSmallInstances) {
+      int upto = x;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += y;
+      }
+      if (tid < p.n_inst) at<int32_t>(ws, w.before)[tid] = upto - x;
+      if (lane == 63) s_needed = upto;
+    }
+  }
+  __syncthreads();
+  int free = 0;
+#pragma unroll
+  for (int v = 0; v < kSmallSegments / 64; ++v) free += s_sums[v];
+  const int n = s_needed;
+  free = clamped(free, 0, p.n_pages);
+  pick_segments<kSmallThreads>(p, 0, p.segments, 0, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+  if (tid == 0) {
+    info[0] = n > free ? free : free - n;
+    info[1] = n > free ? n - free : 0;
+  }
+}
 // All of it by one workgroup, an instance a wave at a time.
 template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline__ void by_one(const ARGS& a, NEED need, APPLY apply) {
   __shared__ int s_wave[kSmallThreads / 64], s_free, s_info[2];
@@ -370,7 +398,7 @@ template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline
   if (threadIdx.x == 0) s_free = 0;
   for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) need(i);
   __syncthreads();
-  pick_pages<kSmallThreads>(a.p, a.ws, a.w, s_info, 0, 1, s_wave);
+  pick_by_one(a.p, a.ws, a.w, s_info, s_wave);
   __syncthreads();
   const bool lacking = s_info[1] > 0;
   if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
@@ -517,7 +545,7 @@ hipError_t launch_pages_count(const Pages& p, hipStream_t st) {
 }
 
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
-  if (small(a.p, 64, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
+  if (small(a.p, kSmallInstances, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
     resize_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
     return hipGetLastError();
   }
@@ -531,7 +559,7 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
-  if (small(a.p, 32, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
+  if (small(a.p, kSmallInstances / 2, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
     fork_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
     return hipGetLastError();
   }
