@@ -16,7 +16,10 @@ namespace ap {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kPickWgs = 64, kApplyWgs = 128;
+// Workgroups that carry a resize out, each instance after instance: 512 instances that give up and take 128 pages each, and 2048 with 4 pages, by 128, 256,
+// 512 and 4096 workgroups 16.9, 14.6, 14.8, 14.8 and 38, 29, 26.5, 32 us.
+constexpr int kPickWgs = 64, kApplyWgs = 512;
+constexpr int kEntries = 4;                                // of a table that a lane asks for together: one after the other, each is a trip to memory
 constexpr int kSmallThreads = 1024, kSmallSegments = 256, kSmallInstances = 64;
 
 struct Head { int needed, lacking, live, moved; };
@@ -43,16 +46,32 @@ __device__ __forceinline__ void add_by_segment(const Pages& p, bool some, int pa
     todo &= ~same;
   }
 }
-__device__ __forceinline__ int drop_pages(const Pages& p, bool some, int page) {
-  const bool freed = some && atomicAdd(p.refs + page, -1) == 1;
-  add_by_segment(p, freed, page, 1);
-  return __popcll(__ballot(freed));
+// U of them, whose counts are asked for together.
+template <int U> __device__ __forceinline__ int change_pages(const Pages& p, const bool (&some)[U], const int (&page)[U], int by, int border) {
+  int was[U], n = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) was[u] = some[u] ? atomicAdd(p.refs + page[u], by) : border - 1;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const bool crossed = some[u] && was[u] == border;
+    add_by_segment(p, crossed, page[u], -by);
+    n += __popcll(__ballot(crossed));
+  }
+  return n;
+}
+template <int U> __device__ __forceinline__ int drop_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
+  return change_pages<U>(p, some, page, -1, 1);
 }
 // One more: returns how many pages are not free any longer (that were given up by others a moment ago).
-__device__ __forceinline__ int name_pages(const Pages& p, bool some, int page) {
-  const bool was_free = some && atomicAdd(p.refs + page, 1) == 0;
-  add_by_segment(p, was_free, page, -1);
-  return __popcll(__ballot(was_free));
+template <int U> __device__ __forceinline__ int name_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
+  return change_pages<U>(p, some, page, 1, 0);
+}
+// Whether any lane has any of U.
+template <int U> __device__ __forceinline__ bool any_of(const bool (&x)[U]) {
+  bool y = false;
+#pragma unroll
+  for (int u = 0; u < U; ++u) y |= x[u];
+  return __any(y);
 }
 // A workgroup's sum of what its waves freed, to info[0]; s_free is a word of LDS that was 0.
 __device__ __forceinline__ void add_free(int freed, int* s_free, int32_t* info) {
@@ -126,40 +145,61 @@ __device__ __forceinline__ Rows rows_of(const ResizeArgs& a, int i) {
   return r;
 }
 
+// What an instance needs: pages, and (fork) the rows it has from now on.
+struct Need { int pages, rows; };
 // A wave: the blocks of instance i that need a page.
-__device__ __forceinline__ void resize_need(const ResizeArgs& a, int i) {
+__device__ __forceinline__ Need resize_need(const ResizeArgs& a, int i) {
   const int lane = threadIdx.x & 63;
   const Rows r = rows_of(a, i);
   const int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
   int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
   int count = 0;
-  for (int k0 = 0; k0 < r.want; k0 += 64) {
-    const int k = k0 + lane, page = k < r.want ? table[k] : 0;
-    const bool needs = k < r.want && (!in_pool(a.p, page) || (k >= r.own && a.p.refs[page] > 1));
-    const unsigned long long mask = __ballot(needs);
-    if (needs) staged[count + lanes_before(mask)] = k;
-    count += __popcll(mask);
+  for (int k0 = 0; k0 < r.want; k0 += 64 * kEntries) {
+    int page[kEntries];
+    bool needs[kEntries], asks[kEntries];
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) {
+      const int k = k0 + 64 * u + lane;
+      page[u] = table[k < a.p.nb_cap ? k : a.p.nb_cap - 1];
+    }
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) {
+      const int k = k0 + 64 * u + lane;
+      needs[u] = k < r.want && !in_pool(a.p, page[u]);
+      asks[u] = k < r.want && k >= r.own && !needs[u];
+    }
+    if (any_of(asks)) {                                    // of pages of its own, or shared?
+      int refs[kEntries];
+#pragma unroll
+      for (int u = 0; u < kEntries; ++u) refs[u] = a.p.refs[asks[u] ? page[u] : 0];
+#pragma unroll
+      for (int u = 0; u < kEntries; ++u) needs[u] |= asks[u] && refs[u] > 1;
+    }
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) {
+      const unsigned long long mask = __ballot(needs[u]);
+      if (needs[u]) staged[count + lanes_before(mask)] = k0 + 64 * u + lane;
+      count += __popcll(mask);
+    }
   }
-  if (lane == 0) at<int32_t>(a.ws, a.w.need)[i] = count;
+  return Need{count, 0};
+}
+// To the launches that follow.
+__device__ __forceinline__ void hand_on(char* ws, const PagesWs& w, int i, Need need) {
+  if ((threadIdx.x & 63) != 0) return;
+  at<int32_t>(ws, w.need)[i] = need.pages;
+  at<int32_t>(ws, w.length)[i] = need.rows;
 }
 __global__ __launch_bounds__(kThreads) void resize_need_kernel(ResizeArgs a) {
   const int i = blockIdx.x * kWaves + wave_of();
-  if (i < a.p.n_inst) resize_need(a, i);
+  if (i < a.p.n_inst) hand_on(a.ws, a.w, i, resize_need(a, i));
 }
 
-// A wave: the new table of instance j, which goes on from instance p, and whether its last page is to be copied.
-__device__ __forceinline__ void fork_need(const ForkArgs& a, int j) {
+// A wave: the new table of instance j, which goes on from instance p, and whether its last page is to be copied.  Rows: -1 if it stays as it is.
+__device__ __forceinline__ Need fork_need(const ForkArgs& a, int j) {
   const int lane = threadIdx.x & 63, p = a.parent[j];
   const bool some = (unsigned)p < (unsigned)a.p.n_inst;
-  int32_t* length = at<int32_t>(a.ws, a.w.length);
-  int32_t* need = at<int32_t>(a.ws, a.w.need);
-  if (!some || p == j) {
-    if (lane == 0) {
-      length[j] = some ? -1 : 0;
-      need[j] = 0;
-    }
-    return;
-  }
+  if (!some || p == j) return Need{0, some ? -1 : 0};
   const int L = clamped(a.len[p], 0, a.p.t_cap), full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1);
   bool heir = false;
   if (rest > 0 && a.parent[p] != p) {                      // the lowest that goes on from p takes its last page over
@@ -169,15 +209,24 @@ __device__ __forceinline__ void fork_need(const ForkArgs& a, int j) {
   const int32_t* table = a.p.table + (size_t)p * a.p.nb_cap;
   int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
   const int n = full + (rest > 0);
-  for (int k = lane; k < n; k += 64) staged[k] = table[k];
-  if (lane == 0) {
-    length[j] = L;
-    need[j] = rest > 0 && !heir && in_pool(a.p, table[full]);
+  for (int k0 = 0; k0 < n; k0 += 64 * kEntries) {
+    int page[kEntries];
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) {
+      const int k = k0 + 64 * u + lane;
+      page[u] = table[k < a.p.nb_cap ? k : a.p.nb_cap - 1];
+    }
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) {
+      const int k = k0 + 64 * u + lane;
+      if (k < n) staged[k] = page[u];
+    }
   }
+  return Need{rest > 0 && !heir && in_pool(a.p, table[full]), L};
 }
 __global__ __launch_bounds__(kThreads) void fork_need_kernel(ForkArgs a) {
   const int j = blockIdx.x * kWaves + wave_of();
-  if (j < a.p.n_inst) fork_need(a, j);
+  if (j < a.p.n_inst) hand_on(a.ws, a.w, j, fork_need(a, j));
 }
 
 // ---------------------------------------------------------------------------------------------------------------- free pages
@@ -286,13 +335,15 @@ __device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* t
 }
 
 // ---------------------------------------------------------------------------------------------------------------- carrying it out
-// Instance i's, by NT threads: a workgroup, or (64) a wave.  Returns how many pages are free now, a wave's own count.
-template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& a, int i, int tid) {
+// Instance i's, by NT threads: a workgroup, or (64) a wave.  n pages are needed, `before` by the instances in front.  Returns how many pages are free now, a
+// wave's own count.
+template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& a, int i, int n, int before, int tid) {
+  constexpr int U = NT == 64 ? kEntries : 1;
   const Rows r = rows_of(a, i);
   int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
   const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
-  const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + at<int32_t>(a.ws, a.w.before)[i];
-  const int n = at<int32_t>(a.ws, a.w.need)[i], rest = r.kept & ((1 << a.p.lb) - 1);
+  const int32_t* picked = at<int32_t>(a.ws, a.w.picked) + before;
+  const int rest = r.kept & ((1 << a.p.lb) - 1);
   int freed = 0;
   if (n > 0 && rest > 0 && r.own < r.want) {
     // The first block that is written may have rows that stay, of a page that others keep.
@@ -300,17 +351,30 @@ template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& 
       if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, NT);
     if (NT > 64) __syncthreads();
   }
-  for (int k0 = r.want; k0 < a.p.nb_cap; k0 += NT) {
-    const int k = k0 + tid, page = k < a.p.nb_cap ? table[k] : -1;
-    if (__any(page != -1)) freed += drop_pages(a.p, in_pool(a.p, page), page);
-    if (page != -1) table[k] = -1;
+  for (int k0 = r.want; k0 < a.p.nb_cap; k0 += NT * U) {
+    int page[U];
+    bool named[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + NT * u + tid;
+      page[u] = table[k < a.p.nb_cap ? k : a.p.nb_cap - 1];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + NT * u + tid;
+      if (k >= a.p.nb_cap) page[u] = -1;
+      named[u] = in_pool(a.p, page[u]);
+      if (page[u] != -1) table[k] = -1;
+    }
+    if (any_of(named)) freed += drop_pages<U>(a.p, named, page);
   }
   for (int x0 = 0; x0 < n; x0 += NT) {
-    const int x = x0 + tid;
-    const bool some = x < n && in_pool(a.p, picked[x < n ? x : 0]);
-    const int k = some ? staged[x] : 0, old = some ? table[k] : -1;
-    if (some) table[k] = picked[x];
-    if (__any(in_pool(a.p, old))) freed += drop_pages(a.p, in_pool(a.p, old), old);
+    const int x = x0 + tid, page = picked[x < n ? x : 0];
+    const bool some = x < n && in_pool(a.p, page);
+    const int k = staged[x < n ? x : 0], old[1] = {some ? table[k] : -1};
+    const bool named[1] = {in_pool(a.p, old[0])};
+    if (some) table[k] = page;
+    if (any_of(named)) freed += drop_pages<1>(a.p, named, old);
   }
   return freed;
 }
@@ -320,34 +384,47 @@ __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeArgs a) {
   if (threadIdx.x == 0) s_free = 0;
   __syncthreads();
   settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
+  const int32_t *need = at<int32_t>(a.ws, a.w.need), *before = at<int32_t>(a.ws, a.w.before);
   int freed = 0;
-  for (int i = blockIdx.x; i < a.p.n_inst; i += gridDim.x) freed += resize_apply<kThreads>(a, i, threadIdx.x);
+  for (int i = blockIdx.x; i < a.p.n_inst; i += gridDim.x) freed += resize_apply<kThreads>(a, i, need[i], before[i], threadIdx.x);
   add_free(freed, &s_free, a.info);
 }
 
-template <int NT> __device__ __forceinline__ int fork_apply(const ForkArgs& a, int j, int tid, bool lacking) {
-  const int L = lacking ? -1 : at<int32_t>(a.ws, a.w.length)[j];
-  if (L < 0) {                                             // stays as it is
+// L: its rows from now on, -1: it stays as it is.
+template <int NT> __device__ __forceinline__ int fork_apply(const ForkArgs& a, int j, int L, int need, int before, int tid) {
+  constexpr int U = NT == 64 ? kEntries : 2;
+  if (L < 0) {
     if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
     return 0;
   }
   const int full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1), n = full + (rest > 0);
   int32_t* table = a.p.table + (size_t)j * a.p.nb_cap;
   const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
-  bool copy = at<int32_t>(a.ws, a.w.need)[j] > 0;
-  const int page = copy ? at<int32_t>(a.ws, a.w.picked)[at<int32_t>(a.ws, a.w.before)[j]] : 0;
-  copy = copy && in_pool(a.p, page);
+  const int page = need > 0 ? at<int32_t>(a.ws, a.w.picked)[before] : 0;
+  const bool copy = need > 0 && in_pool(a.p, page);
   if (copy) copy_rows(a.p, staged[full], page, rest, tid, NT);
   int freed = 0;
-  for (int k0 = 0; k0 < a.p.nb_cap; k0 += NT) {
-    const int k = k0 + tid, old = k < a.p.nb_cap ? table[k] : -1;
-    const bool fresh = copy && k == full;
-    const int now = fresh ? page : (k < n ? staged[k] : -1);
-    const bool changed = now != old;
-    if (changed) table[k] = now;
-    if (!__any(changed)) continue;
-    freed -= name_pages(a.p, changed && !fresh && in_pool(a.p, now), now);
-    freed += drop_pages(a.p, changed && in_pool(a.p, old), old);
+  for (int k0 = 0; k0 < a.p.nb_cap; k0 += NT * U) {
+    int old[U], now[U];
+    bool changed[U], named[U], gone[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + NT * u + tid, x = k < a.p.nb_cap ? k : a.p.nb_cap - 1;
+      old[u] = table[x];
+      now[u] = staged[x];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + NT * u + tid;
+      const bool fresh = copy && k == full;
+      now[u] = fresh ? page : (k < n ? now[u] : -1);
+      changed[u] = k < a.p.nb_cap && now[u] != old[u];
+      if (changed[u]) table[k] = now[u];
+      named[u] = changed[u] && !fresh && in_pool(a.p, now[u]);
+      gone[u] = changed[u] && in_pool(a.p, old[u]);
+    }
+    if (any_of(named)) freed -= name_pages<U>(a.p, named, now);
+    if (any_of(gone)) freed += drop_pages<U>(a.p, gone, old);
   }
   if (tid == 0) a.len_out[j] = L;
   return freed;
@@ -358,15 +435,17 @@ __global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
   if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
   if (threadIdx.x == 0) s_free = 0;
   __syncthreads();
-  add_free(fork_apply<kThreads>(a, blockIdx.x, threadIdx.x, lacking), &s_free, a.info);
+  const int j = blockIdx.x, L = lacking ? -1 : at<int32_t>(a.ws, a.w.length)[j];
+  add_free(fork_apply<kThreads>(a, j, L, at<int32_t>(a.ws, a.w.need)[j], at<int32_t>(a.ws, a.w.before)[j], threadIdx.x), &s_free, a.info);
 }
 
 // As pick_pages, by one workgroup for kSmallInstances instances and kSmallSegments segments at most: what is loaded is asked for together.
-__device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const PagesWs& w, int* info, int* s_wave) {
+// need, before: in LDS.
+__device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const PagesWs& w, const Need* need, int* before, int* info, int* s_wave) {
   __shared__ int s_needed, s_sums[kSmallSegments / 64];
   const int tid = threadIdx.x, lane = tid & 63;
   if (tid < kSmallSegments) {
-    const int x = tid < p.n_inst ? at<int32_t>(ws, w.need)[tid] : 0, segment = sum_int(tid < p.segments ? p.seg[tid] : 0);
+    const int x = tid < p.n_inst ? need[tid].pages : 0, segment = sum_int(tid < p.segments ? p.seg[tid] : 0);
     if (lane == 0) s_sums[tid >> 6] = segment;
     if (tid < kSmallInstances) {
       int upto = x;
@@ -375,7 +454,7 @@ __device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const Page
         const int y = __shfl_up(upto, o, 64);
         if (lane >= o) upto += y;
       }
-      if (tid < p.n_inst) at<int32_t>(ws, w.before)[tid] = upto - x;
+      if (tid < p.n_inst) before[tid] = upto - x;
       if (lane == 63) s_needed = upto;
     }
   }
@@ -393,17 +472,21 @@ __device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const Page
 }
 // All of it by one workgroup, an instance a wave at a time.
 template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline__ void by_one(const ARGS& a, NEED need, APPLY apply) {
-  __shared__ int s_wave[kSmallThreads / 64], s_free, s_info[2];
+  __shared__ int s_wave[kSmallThreads / 64], s_free, s_info[2], s_before[kSmallInstances];
+  __shared__ Need s_need[kSmallInstances];
   const int wave = wave_of();
   if (threadIdx.x == 0) s_free = 0;
-  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) need(i);
+  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) {
+    const Need x = need(i);
+    if ((threadIdx.x & 63) == 0) s_need[i] = x;
+  }
   __syncthreads();
-  pick_by_one(a.p, a.ws, a.w, s_info, s_wave);
+  pick_by_one(a.p, a.ws, a.w, s_need, s_before, s_info, s_wave);
   __syncthreads();
   const bool lacking = s_info[1] > 0;
   if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
   int freed = 0;
-  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) freed += apply(i, lacking);
+  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) freed += apply(i, s_need[i], s_before[i], lacking);
   if ((threadIdx.x & 63) == 0 && freed != 0) atomicAdd(&s_free, freed);
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -413,11 +496,15 @@ template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline
 }
 __global__ __launch_bounds__(kSmallThreads) void resize_small_kernel(ResizeArgs a) {
   const int lane = threadIdx.x & 63;
-  by_one(a, [&](int i) { resize_need(a, i); }, [&](int i, bool lacking) { return lacking ? 0 : resize_apply<64>(a, i, lane); });
+  by_one(a, [&](int i) { return resize_need(a, i); }, [&](int i, Need need, int before, bool lacking) {
+    return lacking ? 0 : resize_apply<64>(a, i, need.pages, before, lane);
+  });
 }
 __global__ __launch_bounds__(kSmallThreads) void fork_small_kernel(ForkArgs a) {
   const int lane = threadIdx.x & 63;
-  by_one(a, [&](int j) { fork_need(a, j); }, [&](int j, bool lacking) { return fork_apply<64>(a, j, lane, lacking); });
+  by_one(a, [&](int j) { return fork_need(a, j); }, [&](int j, Need need, int before, bool lacking) {
+    return fork_apply<64>(a, j, lacking ? -1 : need.rows, need.pages, before, lane);
+  });
 }
 // What one workgroup does sooner than three launches: few instances, tables that are looked through quickly, and few bytes that it may have to copy.
 // Resize, a table's 132 entries, 8, 32, 64, 128 instances: 8.5, 8.8, 12.2, 17.9 us, by three launches 15; of 64 with 252 entries, 63 of them to be given
