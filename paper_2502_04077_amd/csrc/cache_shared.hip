@@ -112,8 +112,10 @@ struct Source {
   int a0, a1, p1, lo0, f;   // rows [a0, f) and [lo0, p1] are seen by one of them at least, f <= lo0; each may be empty
   __device__ __forceinline__ bool row(int j) const { return j >= a0 && j <= p1 && (j >= lo0 || j < f); }
   // Tiles of rows of q: those with many rows, and one with few at the end.
-  __device__ __forceinline__ int wide() const { return rows / kPrefillRows + (rows % kPrefillRows > kNarrowRows); }
-  __device__ __forceinline__ bool narrow() const { return rows % kPrefillRows > 0 && rows % kPrefillRows <= kNarrowRows; }
+  // (rows >= 0, and so are the bounds but for p1: as unsigned numbers, division is a shift.)
+  __device__ __forceinline__ unsigned last() const { return (unsigned)rows % kPrefillRows; }
+  __device__ __forceinline__ unsigned wide() const { return (unsigned)rows / kPrefillRows + (last() > kNarrowRows); }
+  __device__ __forceinline__ bool narrow() const { return last() - 1u < (unsigned)kNarrowRows; }
 };
 // The tiles of TT cache rows that it sees: ts from ta on, the others from tb.
 struct Tiling {
@@ -122,12 +124,12 @@ struct Tiling {
 };
 template <int TT> __device__ __forceinline__ Tiling tiling_of(const Source& s) {
   Tiling t;
-  t.ta = s.a0 / TT;
-  const int end = (s.f + TT - 1) / TT;
+  t.ta = (unsigned)s.a0 / TT;
+  const int end = (unsigned)(s.f + TT - 1) / TT, behind = (unsigned)(s.p1 + TT) / TT;
   t.ts = s.f > 0 ? end - t.ta : 0;
-  t.tb = s.lo0 / TT;
+  t.tb = (unsigned)s.lo0 / TT;
   if (t.ts > 0 && t.tb < end) t.tb = end;
-  t.n = s.a0 >= s.a1 || s.p1 < 0 || s.rows == 0 ? 0 : t.ts + (s.p1 / TT >= t.tb ? s.p1 / TT - t.tb + 1 : 0);
+  t.n = s.a0 >= s.a1 || s.p1 < 0 || s.rows == 0 ? 0 : t.ts + (behind > t.tb ? behind - t.tb : 0);
   return t;
 }
 // What a tile of many rows of q counts, and the one with few.
@@ -557,7 +559,7 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
   float m[RB], sum[RB];                                    // the sums over this lane's rows
 #pragma unroll
   for (int y = 0; y < RB; ++y) {
-    q[y] = query_of(a, s, s.rows / kPrefillRows * kPrefillRows + 16 * y + n);
+    q[y] = query_of(a, s, (int)(s.rows - s.last()) + 16 * y + n);
     int lo, hi;
     positions<16>(q[y], &lo, &hi);
     p_min = lo < p_min ? lo : p_min;
@@ -764,6 +766,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   int wide_wgs = 0, narrow_wgs = kShareWgs;
   bool is_wide = false;
   // The waves' shares go round the workgroups, so that few of them are spread.
+  // All sources stay in LDS, where they fit, until a share's are picked out: to look them up again is two trips to memory.
+  Source* s_all = reinterpret_cast<Source*>(s_tiles);
+  const bool kept = a.window > 0 && places * (int)sizeof(Source) <= kSharedLds;
   auto number = [&](int w) { return w * narrow_wgs + (int)blockIdx.x - wide_wgs; };
   auto share = [&](int y) { return y == 0 ? share_of(all_wide, per, blockIdx.x) : share_of(all_narrow, per, number(y - 1)); };
   // Twice: what there is; and, by the threads in whose sources they lie, where shares begin.
@@ -785,10 +790,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
           const Source& y = s[k < M ? k : 0];
           const int x = i_begin + i0 + k;
           const bool mine = i0 + k < chunk && x < sources;
-          wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(y) * (unsigned)y.wide() : 0;
+          wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(y) * y.wide() : 0;
           narrow[k] = mine ? narrow_size<C, kGroup<T, D>>(y) : 0;
           // Which sources have pieces, for the join: the instances, and the groups by their first member.
-          if (pass == 0 && mine && x % kShareWgs == (int)blockIdx.x) {
+          if (pass == 0 && mine && kept) s_all[x] = y;
+          if (pass == 0 && mine && (unsigned)x % kShareWgs == blockIdx.x) {
             int32_t* has = x < a.r.n_inst ? a.behind + x : a.begun + clamped(y.inst, 0, a.r.n_inst - 1);
             *has = wide[k] + narrow[k] > 0;
           }
@@ -868,7 +874,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   __syncthreads();
   if (tid < (1 + kWaves) * kListed) {
     const int x = s_first[tid / kListed] + tid % kListed;
-    s_source[tid / kListed][tid % kListed] = source_of(a, x < sources ? x : 0);
+    s_source[tid / kListed][tid % kListed] = kept ? s_all[x < sources ? x : 0] : source_of(a, x < sources ? x : 0);
   }
   __syncthreads();
 
@@ -880,7 +886,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int x = x_first; left > 0 && x < sources; ++x, from = 0) {
       const Source s = uniform(x - x_first < kListed ? s_source[0][x - x_first] : source_of(a, x));
       const unsigned size = wide_size<C, F::TT>(s);
-      const unsigned long long end = (unsigned long long)size * (unsigned)s.wide();
+      const unsigned long long end = (unsigned long long)size * s.wide();
       while (left > 0 && from < end) {
         const int t = __builtin_amdgcn_readfirstlane(end == size ? 0 : (int)(from / size));            // tile t of its rows of q
         const Cut c = cut_of<C::WIDE_FRONT, C::WIDE>(size, (unsigned)(from - (unsigned long long)t * size), per, left, C::WIDE_LEAST);
@@ -914,7 +920,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, per, left, C::NARROW_LEAST);
     left -= c.n < left ? c.n : left;
     if (c.skipped) continue;
-    const int row0 = s.rows / kPrefillRows * kPrefillRows, rows = s.rows - row0;
+    const int rows = s.last(), row0 = s.rows - rows;
     const size_t x0 = (size_t)s.x0 + row0, slot = (size_t)a.narrow0 + x0 + (size_t)kNarrowRows * number(wave);
     if (c.u_begin < c.u_end) {
       if (rows <= 16) narrow_piece<T, D, EXACT, RING, 1>(a, s, c.u_begin, c.u_end, slot, s_tiles + wave * RING * GROUP);
