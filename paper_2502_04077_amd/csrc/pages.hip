@@ -19,7 +19,7 @@ constexpr int kThreads = 256, kWaves = 4;
 // Workgroups that carry a resize out, each instance after instance: 512 instances that give up and take 128 pages each, and 2048 with 4 pages, by 128, 256,
 // 512 and 4096 workgroups 16.9, 14.6, 14.8, 14.8 and 38, 29, 26.5, 32 us.
 constexpr int kPickWgs = 64, kApplyWgs = 512;
-constexpr int kEntries = 4;                                // of a table that a lane asks for together: one after the other, each is a trip to memory
+constexpr int kEntries = 256;                              // of a table that a wave, or half of one, asks for together: one after the other is a trip to memory each
 constexpr int kSmallThreads = 1024, kSmallSegments = 256, kSmallInstances = 64;
 
 struct Head { int needed, lacking, live, moved; };
@@ -34,6 +34,10 @@ __device__ __forceinline__ int sum_int(int x) {            // over the wave's la
 __device__ __forceinline__ int lanes_before(unsigned long long mask) {
   return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
 }
+// An instance is a workgroup's, a wave's or, where one workgroup has them all, half a wave's: LANES of a wave, whose halves may go different ways.
+template <int LANES> __device__ __forceinline__ unsigned long long ballot_of(bool x) {      // over the instance's lanes
+  return __ballot(x) & (LANES == 64 ? ~0ull : 0xffffffffull << (threadIdx.x & 32));
+}
 // One less entry that names the page, of every lane with `some`: returns how many pages are free now.  seg follows, an addition for each segment that
 // lanes have: additions to one word wait for each other.
 __device__ __forceinline__ void add_by_segment(const Pages& p, bool some, int page, int by) {
@@ -47,7 +51,7 @@ __device__ __forceinline__ void add_by_segment(const Pages& p, bool some, int pa
   }
 }
 // U of them, whose counts are asked for together.
-template <int U> __device__ __forceinline__ int change_pages(const Pages& p, const bool (&some)[U], const int (&page)[U], int by, int border) {
+template <int LANES, int U> __device__ __forceinline__ int change_pages(const Pages& p, const bool (&some)[U], const int (&page)[U], int by, int border) {
   int was[U], n = 0;
 #pragma unroll
   for (int u = 0; u < U; ++u) was[u] = some[u] ? atomicAdd(p.refs + page[u], by) : border - 1;
@@ -55,16 +59,16 @@ template <int U> __device__ __forceinline__ int change_pages(const Pages& p, con
   for (int u = 0; u < U; ++u) {
     const bool crossed = some[u] && was[u] == border;
     add_by_segment(p, crossed, page[u], -by);
-    n += __popcll(__ballot(crossed));
+    n += __popcll(ballot_of<LANES>(crossed));
   }
   return n;
 }
-template <int U> __device__ __forceinline__ int drop_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
-  return change_pages<U>(p, some, page, -1, 1);
+template <int LANES, int U> __device__ __forceinline__ int drop_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
+  return change_pages<LANES, U>(p, some, page, -1, 1);
 }
 // One more: returns how many pages are not free any longer (that were given up by others a moment ago).
-template <int U> __device__ __forceinline__ int name_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
-  return change_pages<U>(p, some, page, 1, 0);
+template <int LANES, int U> __device__ __forceinline__ int name_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
+  return change_pages<LANES, U>(p, some, page, 1, 0);
 }
 // Whether any lane has any of U.
 template <int U> __device__ __forceinline__ bool any_of(const bool (&x)[U]) {
@@ -81,16 +85,43 @@ __device__ __forceinline__ void add_free(int freed, int* s_free, int32_t* info) 
 }
 // Number of this wave in the workgroup.
 __device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-// The first `rows` rows of K and V of a page, by `threads` threads.
-__device__ __forceinline__ void copy_rows(const Pages& p, int src, int dst, int rows, int tid, int threads) {
-  const int n = rows * p.row_pieces;
-  const size_t page = (size_t)p.row_pieces << p.lb;
-  for (int x = tid; x < 2 * n; x += threads) {
-    u32x4* X = static_cast<u32x4*>(x < n ? p.K : p.V);
-    const int y = x < n ? x : x - n;
-    X[dst * page + y] = X[src * page + y];
+// The first `rows` rows of K and V of a page, by `threads` threads: load() asks for kPieces pieces of each, store() puts them and all others.
+struct RowCopy {
+  static constexpr int kPieces = 4;
+  u32x4 *K, *V;
+  size_t src, dst;
+  int n, tid, threads;
+  u32x4 k[kPieces], v[kPieces];
+  __device__ __forceinline__ RowCopy(const Pages& p, int from, int to, int rows, int tid_, int threads_) : tid(tid_), threads(threads_) {
+    const size_t page = (size_t)p.row_pieces << p.lb;
+    K = static_cast<u32x4*>(p.K); V = static_cast<u32x4*>(p.V);
+    src = from * page; dst = to * page;
+    n = rows * p.row_pieces;
   }
-}
+  __device__ __forceinline__ void load(int x0 = 0) {
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) {
+      const int x = x0 + tid + u * threads;
+      if (x < n) {
+        k[u] = K[src + x];
+        v[u] = V[src + x];
+      }
+    }
+  }
+  __device__ __forceinline__ void store() {
+    for (int x0 = 0; x0 < n; x0 += kPieces * threads) {
+      if (x0 > 0) load(x0);
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) {
+        const int x = x0 + tid + u * threads;
+        if (x < n) {
+          K[dst + x] = k[u];
+          V[dst + x] = v[u];
+        }
+      }
+    }
+  }
+};
 
 // Whole pages of K and V, one a workgroup at a time: page(x) says where from and where to, and whether at all.  The memory's rate bounds it, and what a
 // call moves is not read again soon, so it goes past the caches: 2 x 130 MB of a pool of 4 GB 114 us (4.6 TB/s), with ordinary loads and stores 122;
@@ -147,38 +178,39 @@ __device__ __forceinline__ Rows rows_of(const ResizeArgs& a, int i) {
 
 // What an instance needs: pages, and (fork) the rows it has from now on.
 struct Need { int pages, rows; };
-// A wave: the blocks of instance i that need a page.
-__device__ __forceinline__ Need resize_need(const ResizeArgs& a, int i) {
-  const int lane = threadIdx.x & 63;
+// The blocks of instance i that need a page.
+template <int LANES> __device__ __forceinline__ Need resize_need(const ResizeArgs& a, int i) {
+  constexpr int U = kEntries / LANES;
+  const int lane = threadIdx.x & (LANES - 1);
   const Rows r = rows_of(a, i);
   const int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
   int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
   int count = 0;
-  for (int k0 = 0; k0 < r.want; k0 += 64 * kEntries) {
-    int page[kEntries];
-    bool needs[kEntries], asks[kEntries];
+  for (int k0 = 0; k0 < r.want; k0 += kEntries) {
+    int page[U];
+    bool needs[U], asks[U];
 #pragma unroll
-    for (int u = 0; u < kEntries; ++u) {
-      const int k = k0 + 64 * u + lane;
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + LANES * u + lane;
       page[u] = table[k < a.p.nb_cap ? k : a.p.nb_cap - 1];
     }
 #pragma unroll
-    for (int u = 0; u < kEntries; ++u) {
-      const int k = k0 + 64 * u + lane;
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + LANES * u + lane;
       needs[u] = k < r.want && !in_pool(a.p, page[u]);
       asks[u] = k < r.want && k >= r.own && !needs[u];
     }
     if (any_of(asks)) {                                    // of pages of its own, or shared?
-      int refs[kEntries];
+      int refs[U];
 #pragma unroll
-      for (int u = 0; u < kEntries; ++u) refs[u] = a.p.refs[asks[u] ? page[u] : 0];
+      for (int u = 0; u < U; ++u) refs[u] = a.p.refs[asks[u] ? page[u] : 0];
 #pragma unroll
-      for (int u = 0; u < kEntries; ++u) needs[u] |= asks[u] && refs[u] > 1;
+      for (int u = 0; u < U; ++u) needs[u] |= asks[u] && refs[u] > 1;
     }
 #pragma unroll
-    for (int u = 0; u < kEntries; ++u) {
-      const unsigned long long mask = __ballot(needs[u]);
-      if (needs[u]) staged[count + lanes_before(mask)] = k0 + 64 * u + lane;
+    for (int u = 0; u < U; ++u) {
+      const unsigned long long mask = ballot_of<LANES>(needs[u]);
+      if (needs[u]) staged[count + lanes_before(mask)] = k0 + LANES * u + lane;
       count += __popcll(mask);
     }
   }
@@ -192,33 +224,34 @@ __device__ __forceinline__ void hand_on(char* ws, const PagesWs& w, int i, Need 
 }
 __global__ __launch_bounds__(kThreads) void resize_need_kernel(ResizeArgs a) {
   const int i = blockIdx.x * kWaves + wave_of();
-  if (i < a.p.n_inst) hand_on(a.ws, a.w, i, resize_need(a, i));
+  if (i < a.p.n_inst) hand_on(a.ws, a.w, i, resize_need<64>(a, i));
 }
 
-// A wave: the new table of instance j, which goes on from instance p, and whether its last page is to be copied.  Rows: -1 if it stays as it is.
-__device__ __forceinline__ Need fork_need(const ForkArgs& a, int j) {
-  const int lane = threadIdx.x & 63, p = a.parent[j];
+// The new table of instance j, which goes on from instance p, and whether its last page is to be copied.  Rows: -1 if it stays as it is.
+template <int LANES> __device__ __forceinline__ Need fork_need(const ForkArgs& a, int j) {
+  constexpr int U = kEntries / LANES;
+  const int lane = threadIdx.x & (LANES - 1), p = a.parent[j];
   const bool some = (unsigned)p < (unsigned)a.p.n_inst;
   if (!some || p == j) return Need{0, some ? -1 : 0};
   const int L = clamped(a.len[p], 0, a.p.t_cap), full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1);
   bool heir = false;
   if (rest > 0 && a.parent[p] != p) {                      // the lowest that goes on from p takes its last page over
     heir = true;
-    for (int x0 = 0; x0 < j && heir; x0 += 64) heir = !__any(x0 + lane < j && a.parent[x0 + lane] == p);
+    for (int x0 = 0; x0 < j && heir; x0 += LANES) heir = ballot_of<LANES>(x0 + lane < j && a.parent[x0 + lane] == p) == 0;
   }
   const int32_t* table = a.p.table + (size_t)p * a.p.nb_cap;
   int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
   const int n = full + (rest > 0);
-  for (int k0 = 0; k0 < n; k0 += 64 * kEntries) {
-    int page[kEntries];
+  for (int k0 = 0; k0 < n; k0 += kEntries) {
+    int page[U];
 #pragma unroll
-    for (int u = 0; u < kEntries; ++u) {
-      const int k = k0 + 64 * u + lane;
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + LANES * u + lane;
       page[u] = table[k < a.p.nb_cap ? k : a.p.nb_cap - 1];
     }
 #pragma unroll
-    for (int u = 0; u < kEntries; ++u) {
-      const int k = k0 + 64 * u + lane;
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + LANES * u + lane;
       if (k < n) staged[k] = page[u];
     }
   }
@@ -226,7 +259,7 @@ __device__ __forceinline__ Need fork_need(const ForkArgs& a, int j) {
 }
 __global__ __launch_bounds__(kThreads) void fork_need_kernel(ForkArgs a) {
   const int j = blockIdx.x * kWaves + wave_of();
-  if (j < a.p.n_inst) hand_on(a.ws, a.w, j, fork_need(a, j));
+  if (j < a.p.n_inst) hand_on(a.ws, a.w, j, fork_need<64>(a, j));
 }
 
 // ---------------------------------------------------------------------------------------------------------------- free pages
@@ -335,10 +368,10 @@ __device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* t
 }
 
 // ---------------------------------------------------------------------------------------------------------------- carrying it out
-// Instance i's, by NT threads: a workgroup, or (64) a wave.  n pages are needed, `before` by the instances in front.  Returns how many pages are free now, a
-// wave's own count.
+// Instance i's, by NT threads: a workgroup, or half a wave.  n pages are needed, `before` by the instances in front.  Returns how many pages are free now, a
+// wave's (half's) own count.
 template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& a, int i, int n, int before, int tid) {
-  constexpr int U = NT == 64 ? kEntries : 1;
+  constexpr int LANES = NT < 64 ? NT : 64, U = NT < 64 ? kEntries / NT : 1;
   const Rows r = rows_of(a, i);
   int32_t* table = a.p.table + (size_t)i * a.p.nb_cap;
   const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)i * a.p.nb_cap;
@@ -348,7 +381,11 @@ template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& 
   if (n > 0 && rest > 0 && r.own < r.want) {
     // The first block that is written may have rows that stay, of a page that others keep.
     for (int x = 0; x < n && staged[x] <= r.own; ++x)
-      if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) copy_rows(a.p, table[r.own], picked[x], rest, tid, NT);
+      if (staged[x] == r.own && in_pool(a.p, table[r.own]) && in_pool(a.p, picked[x])) {
+        RowCopy copy(a.p, table[r.own], picked[x], rest, tid, NT);
+        copy.load();
+        copy.store();
+      }
     if (NT > 64) __syncthreads();
   }
   for (int k0 = r.want; k0 < a.p.nb_cap; k0 += NT * U) {
@@ -366,7 +403,7 @@ template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& 
       named[u] = in_pool(a.p, page[u]);
       if (page[u] != -1) table[k] = -1;
     }
-    if (any_of(named)) freed += drop_pages<U>(a.p, named, page);
+    if (any_of(named)) freed += drop_pages<LANES, U>(a.p, named, page);
   }
   for (int x0 = 0; x0 < n; x0 += NT) {
     const int x = x0 + tid, page = picked[x < n ? x : 0];
@@ -374,7 +411,7 @@ template <int NT> __device__ __forceinline__ int resize_apply(const ResizeArgs& 
     const int k = staged[x < n ? x : 0], old[1] = {some ? table[k] : -1};
     const bool named[1] = {in_pool(a.p, old[0])};
     if (some) table[k] = page;
-    if (any_of(named)) freed += drop_pages<1>(a.p, named, old);
+    if (any_of(named)) freed += drop_pages<LANES, 1>(a.p, named, old);
   }
   return freed;
 }
@@ -392,7 +429,7 @@ __global__ __launch_bounds__(kThreads) void resize_apply_kernel(ResizeArgs a) {
 
 // L: its rows from now on, -1: it stays as it is.
 template <int NT> __device__ __forceinline__ int fork_apply(const ForkArgs& a, int j, int L, int need, int before, int tid) {
-  constexpr int U = NT == 64 ? kEntries : 2;
+  constexpr int LANES = NT < 64 ? NT : 64, U = NT < 64 ? kEntries / NT : 2;
   if (L < 0) {
     if (tid == 0 && a.len_out != a.len) a.len_out[j] = a.len[j];
     return 0;
@@ -400,32 +437,39 @@ template <int NT> __device__ __forceinline__ int fork_apply(const ForkArgs& a, i
   const int full = L >> a.p.lb, rest = L & ((1 << a.p.lb) - 1), n = full + (rest > 0);
   int32_t* table = a.p.table + (size_t)j * a.p.nb_cap;
   const int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
-  const int page = need > 0 ? at<int32_t>(a.ws, a.w.picked)[before] : 0;
-  const bool copy = need > 0 && in_pool(a.p, page);
-  if (copy) copy_rows(a.p, staged[full], page, rest, tid, NT);
-  int freed = 0;
-  for (int k0 = 0; k0 < a.p.nb_cap; k0 += NT * U) {
-    int old[U], now[U];
-    bool changed[U], named[U], gone[U];
+  int old[U], now[U];
+  auto ask = [&](int k0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + NT * u + tid, x = k < a.p.nb_cap ? k : a.p.nb_cap - 1;
       old[u] = table[x];
       now[u] = staged[x];
     }
+  };
+  // The tables, then the rows that are copied and the counts: what a step needs is asked for together.
+  const int page = need > 0 ? at<int32_t>(a.ws, a.w.picked)[before] : 0, last = need > 0 ? staged[full] : 0;
+  ask(0);
+  const bool copied = need > 0 && in_pool(a.p, page);
+  RowCopy copy(a.p, last, page, copied ? rest : 0, tid, NT);
+  copy.load();
+  int freed = 0;
+  for (int k0 = 0; k0 < a.p.nb_cap; k0 += NT * U) {
+    bool changed[U], named[U], gone[U];
+    if (k0 > 0) ask(k0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + NT * u + tid;
-      const bool fresh = copy && k == full;
+      const bool fresh = copied && k == full;
       now[u] = fresh ? page : (k < n ? now[u] : -1);
       changed[u] = k < a.p.nb_cap && now[u] != old[u];
       if (changed[u]) table[k] = now[u];
       named[u] = changed[u] && !fresh && in_pool(a.p, now[u]);
       gone[u] = changed[u] && in_pool(a.p, old[u]);
     }
-    if (any_of(named)) freed -= name_pages<U>(a.p, named, now);
-    if (any_of(gone)) freed += drop_pages<U>(a.p, gone, old);
+    if (any_of(named)) freed -= name_pages<LANES, U>(a.p, named, now);
+    if (any_of(gone)) freed += drop_pages<LANES, U>(a.p, gone, old);
   }
+  copy.store();
   if (tid == 0) a.len_out[j] = L;
   return freed;
 }
@@ -470,15 +514,16 @@ __device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const Page
     info[1] = n > free ? n - free : 0;
   }
 }
-// All of it by one workgroup, an instance a wave at a time.
+// All of it by one workgroup, an instance half a wave at a time: a fork of 32 instances and a resize of them are one round of trips to memory each.
+constexpr int kHalf = 32, kHalves = kSmallThreads / kHalf;
 template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline__ void by_one(const ARGS& a, NEED need, APPLY apply) {
   __shared__ int s_wave[kSmallThreads / 64], s_free, s_info[2], s_before[kSmallInstances];
   __shared__ Need s_need[kSmallInstances];
-  const int wave = wave_of();
+  const int half = threadIdx.x / kHalf;
   if (threadIdx.x == 0) s_free = 0;
-  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) {
+  for (int i = half; i < a.p.n_inst; i += kHalves) {
     const Need x = need(i);
-    if ((threadIdx.x & 63) == 0) s_need[i] = x;
+    if (threadIdx.x % kHalf == 0) s_need[i] = x;
   }
   __syncthreads();
   pick_by_one(a.p, a.ws, a.w, s_need, s_before, s_info, s_wave);
@@ -486,8 +531,8 @@ template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline
   const bool lacking = s_info[1] > 0;
   if (!lacking) settle_segments(a.p, at<int32_t>(a.ws, a.w.taken));
   int freed = 0;
-  for (int i = wave; i < a.p.n_inst; i += kSmallThreads / 64) freed += apply(i, s_need[i], s_before[i], lacking);
-  if ((threadIdx.x & 63) == 0 && freed != 0) atomicAdd(&s_free, freed);
+  for (int i = half; i < a.p.n_inst; i += kHalves) freed += apply(i, s_need[i], s_before[i], lacking);
+  if (threadIdx.x % kHalf == 0 && freed != 0) atomicAdd(&s_free, freed);
   __syncthreads();
   if (threadIdx.x == 0) {
     a.info[0] = s_info[0] + s_free;
@@ -495,15 +540,15 @@ template <typename ARGS, typename NEED, typename APPLY> __device__ __forceinline
   }
 }
 __global__ __launch_bounds__(kSmallThreads) void resize_small_kernel(ResizeArgs a) {
-  const int lane = threadIdx.x & 63;
-  by_one(a, [&](int i) { return resize_need(a, i); }, [&](int i, Need need, int before, bool lacking) {
-    return lacking ? 0 : resize_apply<64>(a, i, need.pages, before, lane);
+  const int lane = threadIdx.x % kHalf;
+  by_one(a, [&](int i) { return resize_need<kHalf>(a, i); }, [&](int i, Need need, int before, bool lacking) {
+    return lacking ? 0 : resize_apply<kHalf>(a, i, need.pages, before, lane);
   });
 }
 __global__ __launch_bounds__(kSmallThreads) void fork_small_kernel(ForkArgs a) {
-  const int lane = threadIdx.x & 63;
-  by_one(a, [&](int j) { return fork_need(a, j); }, [&](int j, Need need, int before, bool lacking) {
-    return fork_apply<64>(a, j, lacking ? -1 : need.rows, need.pages, before, lane);
+  const int lane = threadIdx.x % kHalf;
+  by_one(a, [&](int j) { return fork_need<kHalf>(a, j); }, [&](int j, Need need, int before, bool lacking) {
+    return fork_apply<kHalf>(a, j, lacking ? -1 : need.rows, need.pages, before, lane);
   });
 }
 // What one workgroup does sooner than three launches: few instances, tables that are looked through quickly, and few bytes that it may have to copy.
