@@ -97,11 +97,12 @@ __global__ __launch_bounds__(kThreads) void share_place_kernel(int n, SharePlan 
 template <typename T, int D> constexpr int kGroup = sizeof(T) == 4 && D == 128 ? 16 : 32;
 constexpr int kSharedLds = 64 * 1024;       // two workgroups a CU
 // What a share counts, in tenths of a microsecond: of a workgroup's time a tile of the cache, and what a tile of rows of q costs beside them; of a
-// wave's time a group, and the same.  The least shares.  (As measured, and then varied by a third either way: no time of ten calls, 20 to 130 us, moves
-// by more than 4 %.)
+// wave's time a group, and the same.  The least shares.  (As measured, and then varied by a third either way.  Of a wave's, in front and least, 40 and 60: a
+// sequence of 150 rows 14.7 us, 4 samples of 2041 and more 18.3, 32 sequences of 110 to 400 19.3, drafts 42.1; 50 and 90: 16.0, 18.5, 20.7, 42.8; 40 and 45:
+// 14.6, 19.3, 19.6, 42.1; 50 and 130: 19.1, 20.8, 23.4, 42.7.)
 template <typename T, bool EXACT> struct Counts {
   static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 24), WIDE_FRONT = sizeof(T) == 4 ? 60 : 80, WIDE_LEAST = 120;
-  static constexpr int NARROW = sizeof(T) == 4 ? 24 : 32, NARROW_FRONT = 50, NARROW_LEAST = sizeof(T) == 4 ? 64 : 90;
+  static constexpr int NARROW = sizeof(T) == 4 ? 24 : 32, NARROW_FRONT = 40, NARROW_LEAST = sizeof(T) == 4 ? 50 : 60;
 };
 
 // Rows [a0, a1) of a cache, and the rows of q that they are for: of a group's members, one after the other, or of the instance alone (count 0).
