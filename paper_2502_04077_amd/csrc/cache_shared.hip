@@ -165,17 +165,15 @@ __device__ __forceinline__ Source uniform(Source s) {
   for (int k = 0; k < (int)(sizeof(Source) / 4); ++k) w[k] = __builtin_amdgcn_readfirstlane(w[k]);
   return s;
 }
-// The lowest position of a query of a group's members.  (A call: few need it, and the launch's code is to stay in the instruction cache.)
-__device__ __attribute__((noinline)) int lowest_position(const int32_t* member, const int32_t* len, const int32_t* n_q, int q_cap, int t_cap, int n_inst, int count) {
-  int p = 0x7fffffff;
-  for (int k = 0; k < count; ++k) {
-    const int i = clamped(member[k], 0, n_inst - 1), q = n_q == nullptr ? q_cap : clamped(n_q[i], 0, q_cap), base = clamped(len[i], 0, t_cap) - q;
-    if (q > 0 && base < p) p = base;
-  }
-  return p;
+// The position of an instance's first query; past all others if it has none.
+__device__ __forceinline__ int first_position(const SharedArgs& a, int i) {
+  const int q = queries(a, i), own = clamped(a.r.len[i], 0, a.r.t_cap);
+  return q > 0 ? own - q : 0x7fffffff;
 }
-// Sources in their order: the instances', then the groups'.  What has to be loaded for source x is asked for together.
-__device__ __forceinline__ Source source_of(const SharedArgs& a, int x) {
+// Sources in their order: the instances', then the groups'.  What has to be loaded for source x is asked for together.  s_low: by the first member, the
+// lowest position of a query of the group (only with a window: members one after the other are two trips to memory each); a.low where sizes are in the workspace.
+typedef const __attribute__((address_space(3))) int* LowestInLds;
+__device__ __forceinline__ Source source_of(const SharedArgs& a, int x, LowestInLds s_low) {
   const int n = a.r.n_inst, i = x < n ? x : 0;
   const int4 line = *(x < n ? a.plan.inst + i : a.plan.groups + (x - n));
   const int m = queries(a, i), own = clamped(a.r.len[i], 0, a.r.t_cap);
@@ -188,8 +186,11 @@ __device__ __forceinline__ Source source_of(const SharedArgs& a, int x) {
     s.rows = several ? line.z * a.rows : 0;
     s.x0 = (n + line.y) * a.rows;
     s.p0 = 0;
-    int p = 0x7fffffff;
-    if (S > 0 && a.window > 0) p = lowest_position(a.plan.member + s.first, a.r.len, a.n_q, a.q_cap, a.r.t_cap, n, s.count);
+    int p = 0;
+    if (S > 0 && a.window > 0) {
+      if (a.sized) p = a.low[line.x];
+      else p = s_low[line.x];
+    }
     see(a, s, 0, S, p);
   } else {
     s.inst = i; s.first = 0; s.count = 0;
@@ -745,96 +746,159 @@ template <unsigned FRONT, unsigned EACH> __device__ __forceinline__ Cut cut_of(u
 
 template <int N> struct Number { static constexpr int value = N; };
 
+// Sources that a thread holds the sizes of.  Where there are more of them, launches of their own leave the sizes in the workspace, not every workgroup for
+// itself: decode of 4096 caches, two behind each beginning of 17 rows, with a window 127 -> 59 us, of 3280 behind 656 of 65 rows 66 -> 29.
+constexpr int kHeld = 6;
+__host__ __device__ constexpr int places_of(int n_inst) { return n_inst + n_inst / 2; }           // (of groups there are half as many as instances at most)
+__host__ __device__ constexpr int blocks_of(int n_inst) { return (places_of(n_inst) + kThreads - 1) / kThreads; }
+
+// The groups' lowest positions, a wave each.
+__global__ __launch_bounds__(kThreads) void share_low_kernel(SharedArgs a) {
+  constexpr int U = 4;                                     // loads under way
+  const int n = a.r.n_inst, lane = threadIdx.x & 63, groups = clamped(*a.plan.count, 0, n / 2);
+  for (int g = blockIdx.x * kWaves + (threadIdx.x >> 6); g < groups; g += gridDim.x * kWaves) {
+    const int4 line = a.plan.groups[g];
+    const int count = line.y >= 0 && line.z <= n - line.y ? line.z : 0;
+    int p = 0x7fffffff;
+    for (int k0 = 0; k0 < count; k0 += 64 * U) {
+      int i[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) i[u] = clamped(a.plan.member[line.y + (k0 + 64 * u + lane < count ? k0 + 64 * u + lane : 0)], 0, n - 1);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int y = first_position(a, i[u]);
+        p = y < p ? y : p;
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const int y = __shfl_xor(p, o, 64);
+      p = y < p ? y : p;
+    }
+    if (lane == 0) a.low[clamped(line.x, 0, n - 1)] = p;
+  }
+}
+// The sources' sizes, as sums over those in front in a block of kThreads, and the blocks' sums.
+template <typename T, int D, bool EXACT> __global__ __launch_bounds__(kThreads) void share_sizes_kernel(SharedArgs a) {
+  using C = Counts<T, EXACT>;
+  __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves];
+  const int n = a.r.n_inst, places = places_of(n), sources = n + clamped(*a.plan.count, 0, n / 2);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = blockIdx.x * kThreads + threadIdx.x;
+  const Source y = source_of(a, x < places ? x : 0, nullptr);
+  const unsigned long long wide = x < sources ? (unsigned long long)wide_size<C, Form<T, D>::TT>(y) * y.wide() : 0;
+  const unsigned long long narrow = x < sources ? narrow_size<C, kGroup<T, D>>(y) : 0;
+  if (x < sources) (x < n ? a.behind + x : a.begun + clamped(y.inst, 0, n - 1))[0] = wide + narrow > 0;
+  unsigned long long at_wide = wide, at_narrow = narrow;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long u = __shfl_up(at_wide, o, 64), v = __shfl_up(at_narrow, o, 64);
+    if (lane >= o) {
+      at_wide += u;
+      at_narrow += v;
+    }
+  }
+  if (lane == 63) {
+    s_wide[wave] = at_wide;
+    s_narrow[wave] = at_narrow;
+  }
+  __syncthreads();
+  at_wide -= wide;
+  at_narrow -= narrow;
+  unsigned long long all_wide = 0, all_narrow = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) {
+      at_wide += s_wide[w];
+      at_narrow += s_narrow[w];
+    }
+    all_wide += s_wide[w];
+    all_narrow += s_narrow[w];
+  }
+  a.sizes[2 * x] = at_wide;
+  a.sizes[2 * x + 1] = at_narrow;
+  if (threadIdx.x == 0) {
+    a.totals[2 * blockIdx.x] = all_wide;
+    a.totals[2 * blockIdx.x + 1] = all_narrow;
+  }
+}
+
 template <typename T, int D, bool EXACT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void cache_shared_kernel(SharedArgs a) {
   using F = Form<T, D>;
   using C = Counts<T, EXACT>;
-  constexpr int kHeld = 6, kListed = 16, GROUP = 2 * kGroup<T, D> * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
+  constexpr int kListed = 16, GROUP = 2 * kGroup<T, D> * F::PIECES, RING = kSharedLds / 16 / (kWaves * GROUP);
   static_assert(RING >= 1 && 4 * F::TILE * 16 <= kSharedLds, "LDS");
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE], or [wave][RING][K, V][group]
   __shared__ unsigned long long s_wide[kWaves], s_narrow[kWaves], s_from[1 + kWaves];
   __shared__ int s_first[1 + kWaves];                                     // of the workgroup's share, and of its waves'
   __shared__ Source s_source[1 + kWaves][kListed];                        // from there on
+  __shared__ int s_low[kThreads * kHeld * 2 / 3];                         // (as many instances as there are where this is used)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // All that there is to do: every thread sums up consecutive sources.  (Of groups there are half as many as instances at most; how many is asked for
-  // at the same time.)
-  const int places = a.r.n_inst + a.r.n_inst / 2, chunk = (places + kThreads - 1) / kThreads;
-  const int groups = clamped(*a.plan.count, 0, a.r.n_inst / 2), sources = a.r.n_inst + groups;
-  const int i_begin = tid * chunk;
-  unsigned long long wide[kHeld], my_wide = 0, my_narrow = 0, all_wide = 0, all_narrow = 0, at = 0;
-  unsigned narrow[kHeld], per = 0;
+  const int places = places_of(a.r.n_inst), groups = clamped(*a.plan.count, 0, a.r.n_inst / 2), sources = a.r.n_inst + groups;
+  const LowestInLds lowest = (LowestInLds)s_low;
+  if (a.window > 0 && !a.sized) {
+    for (int i = tid; i < a.r.n_inst; i += kThreads) s_low[i] = 0x7fffffff;
+    __syncthreads();
+    for (int i0 = tid; i0 < a.r.n_inst; i0 += 2 * kThreads) {
+      const int i1 = i0 + kThreads < a.r.n_inst ? i0 + kThreads : i0;
+      const int4 y0 = a.plan.inst[i0], y1 = a.plan.inst[i1];
+      const int p0 = first_position(a, i0), p1 = first_position(a, i1);
+      if (y0.z > 1) atomicMin(s_low + clamped(y0.x, 0, a.r.n_inst - 1), p0);
+      if (y1.z > 1) atomicMin(s_low + clamped(y1.x, 0, a.r.n_inst - 1), p1);
+    }
+    __syncthreads();
+  }
+
+  // All that there is to do: every thread sums up consecutive sources, or blocks of them.  (How many groups there are is asked for at the same time.)
+  const int chunk = ((a.sized ? blocks_of(a.r.n_inst) : places) + kThreads - 1) / kThreads, i_begin = tid * chunk;
+  unsigned long long wide[kHeld], narrow[kHeld], my_wide = 0, my_narrow = 0, all_wide = 0, all_narrow = 0, at = 0;
+  unsigned per = 0;
   int wide_wgs = 0, narrow_wgs = kShareWgs;
   bool is_wide = false;
   // The waves' shares go round the workgroups, so that few of them are spread.
-  // All sources stay in LDS, where they fit, until a share's are picked out: to look them up again is two trips to memory.
-  Source* s_all = reinterpret_cast<Source*>(s_tiles);
-  const bool kept = a.window > 0 && places * (int)sizeof(Source) <= kSharedLds;
   auto number = [&](int w) { return w * narrow_wgs + (int)blockIdx.x - wide_wgs; };
   auto share = [&](int y) { return y == 0 ? share_of(all_wide, per, blockIdx.x) : share_of(all_narrow, per, number(y - 1)); };
-  // Twice: what there is; and, by the threads in whose sources they lie, where shares begin.
-#pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-    for (int i0 = 0; i0 < chunk; i0 += kHeld) {
-      // The sizes of sources i0 .. i0 + kHeld - 1 of this thread's, whose loads are under way together; they are held where these are all.
-      auto look = [&](auto some) {
-        constexpr int M = decltype(some)::value;
-        Source s[M];
+  // The sizes of sources i_begin .. i_begin + M - 1, whose loads are under way together.
+  auto look = [&](auto some) {
+    constexpr int M = decltype(some)::value;
+    Source s[M];
 #pragma unroll
-        for (int k = 0; k < M; ++k) s[k] = source_of(a, i0 + k < chunk && i_begin + i0 + k < places ? i_begin + i0 + k : 0);
+    for (int k = 0; k < M; ++k) s[k] = source_of(a, k < chunk && i_begin + k < places ? i_begin + k : 0, lowest);
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          wide[k] = 0;
-          narrow[k] = 0;
-          if (k >= M) continue;
-          const Source& y = s[k < M ? k : 0];
-          const int x = i_begin + i0 + k;
-          const bool mine = i0 + k < chunk && x < sources;
-          wide[k] = mine ? (unsigned long long)wide_size<C, F::TT>(y) * y.wide() : 0;
-          narrow[k] = mine ? narrow_size<C, kGroup<T, D>>(y) : 0;
-          // Which sources have pieces, for the join: the instances, and the groups by their first member.
-          if (pass == 0 && mine && kept) s_all[x] = y;
-          if (pass == 0 && mine && (unsigned)x % kShareWgs == blockIdx.x) {
-            int32_t* has = x < a.r.n_inst ? a.behind + x : a.begun + clamped(y.inst, 0, a.r.n_inst - 1);
-            *has = wide[k] + narrow[k] > 0;
-          }
-        }
-      };
-      if (pass == 0 || chunk > kHeld) {
-        if (chunk == 1) look(Number<1>());
-        else if (chunk <= 3) look(Number<3>());
-        else look(Number<kHeld>());
+    for (int k = 0; k < M; ++k) {
+      const int x = i_begin + k;
+      if (k >= chunk || x >= sources) continue;
+      wide[k] = (unsigned long long)wide_size<C, F::TT>(s[k]) * s[k].wide();
+      narrow[k] = narrow_size<C, kGroup<T, D>>(s[k]);
+      // Which sources have pieces, for the join: the instances, and the groups by their first member.
+      if ((unsigned)x % kShareWgs == blockIdx.x) {
+        int32_t* has = x < a.r.n_inst ? a.behind + x : a.begun + clamped(s[k].inst, 0, a.r.n_inst - 1);
+        *has = wide[k] + narrow[k] > 0;
       }
-      if (pass == 0) {
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          my_wide += wide[k];
-          my_narrow += narrow[k];
-        }
-        continue;
-      }
-      unsigned long long here = 0;
-#pragma unroll
-      for (int k = 0; k < kHeld; ++k) here += is_wide ? wide[k] : narrow[k];
-#pragma unroll 1
-      for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
-        const Share s = share(y);
-        if (s.left == 0 || s.begin < at || s.begin >= at + here) continue;
-        unsigned long long to = at;
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          const unsigned long long n = is_wide ? wide[k] : narrow[k];
-          if (to <= s.begin && s.begin < to + n) {
-            s_first[y] = i_begin + i0 + k;
-            s_from[y] = s.begin - to;
-          }
-          to += n;
-        }
-      }
-      at += here;
     }
-    if (pass == 1) break;
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) wide[k] = narrow[k] = 0;
+  if (a.sized) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (k < chunk && i_begin + k < blocks_of(a.r.n_inst)) {
+        wide[k] = a.totals[2 * (i_begin + k)];
+        narrow[k] = a.totals[2 * (i_begin + k) + 1];
+      }
+  } else if (chunk == 1) {
+    look(Number<1>());
+  } else if (chunk <= 3) {
+    look(Number<3>());
+  } else {
+    look(Number<kHeld>());
+  }
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    my_wide += wide[k];
+    my_narrow += narrow[k];
+  }
+  {
     unsigned long long upto_wide = my_wide, upto_narrow = my_narrow;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -848,7 +912,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       s_wide[wave] = upto_wide;
       s_narrow[wave] = upto_narrow;
     }
-    if (tid <= kWaves) s_first[tid] = sources;
+    if (tid <= kWaves) s_first[tid] = 0x7fffffff - kListed;          // (none)
     __syncthreads();
     unsigned long long at_wide = upto_wide - my_wide, at_narrow = upto_narrow - my_narrow;
     for (int w = 0; w < kWaves; ++w) {
@@ -872,10 +936,55 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const unsigned long long each = ((is_wide ? all_wide : all_narrow) + sharers - 1) / sharers;
     per = __builtin_amdgcn_readfirstlane(each < least ? least : (unsigned)each);
   }
+  // Where shares begin, by the threads in whose sources they lie.
+  {
+    unsigned long long here = 0;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) here += is_wide ? wide[k] : narrow[k];
+#pragma unroll 1
+    for (int y = is_wide ? 0 : 1; y <= (is_wide ? 0 : kWaves); ++y) {
+      const Share s = share(y);
+      if (s.left == 0 || s.begin < at || s.begin >= at + here) continue;
+      unsigned long long to = at;
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const unsigned long long n = is_wide ? wide[k] : narrow[k];
+        if (to <= s.begin && s.begin < to + n) {
+          s_first[y] = i_begin + k;
+          s_from[y] = s.begin - to;
+        }
+        to += n;
+      }
+    }
+  }
   __syncthreads();
+  if (a.sized) {                                           // that was a block: now its sources
+    int block[1 + kWaves];
+    unsigned long long from[1 + kWaves], before[1 + kWaves], behind[1 + kWaves];
+#pragma unroll
+    for (int y = 0; y <= kWaves; ++y) {
+      block[y] = s_first[y];
+      from[y] = s_from[y];
+      const bool some = block[y] < blocks_of(a.r.n_inst);
+      const int x = (some ? block[y] : 0) * kThreads + tid, next = tid == kThreads - 1 ? x : x + 1;
+      before[y] = a.sizes[2 * x + (y > 0)];
+      behind[y] = tid == kThreads - 1 ? a.totals[2 * (some ? block[y] : 0) + (y > 0)] : a.sizes[2 * next + (y > 0)];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int y = 0; y <= kWaves; ++y) {
+      if (block[y] >= blocks_of(a.r.n_inst)) {
+        if (tid == 0) s_first[y] = sources;
+      } else if (before[y] <= from[y] && from[y] < behind[y]) {
+        s_first[y] = block[y] * kThreads + tid;
+        s_from[y] = from[y] - before[y];
+      }
+    }
+    __syncthreads();
+  }
   if (tid < (1 + kWaves) * kListed) {
     const int x = s_first[tid / kListed] + tid % kListed;
-    s_source[tid / kListed][tid % kListed] = kept ? s_all[x < sources ? x : 0] : source_of(a, x < sources ? x : 0);
+    s_source[tid / kListed][tid % kListed] = source_of(a, x < sources ? x : 0, lowest);
   }
   __syncthreads();
 
@@ -885,7 +994,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     unsigned left = share0.left;
     unsigned long long from = x_first < sources ? s_from[0] : 0;
     for (int x = x_first; left > 0 && x < sources; ++x, from = 0) {
-      const Source s = uniform(x - x_first < kListed ? s_source[0][x - x_first] : source_of(a, x));
+      const Source s = uniform(x - x_first < kListed ? s_source[0][x - x_first] : source_of(a, x, lowest));
       const unsigned size = wide_size<C, F::TT>(s);
       const unsigned long long end = (unsigned long long)size * s.wide();
       while (left > 0 && from < end) {
@@ -915,7 +1024,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const Share mine = share(1 + wave);
   unsigned left = __builtin_amdgcn_readfirstlane(mine.left), r = x_first < sources ? __builtin_amdgcn_readfirstlane((unsigned)s_from[1 + wave]) : 0;
   for (int x = x_first; left > 0 && x < sources; ++x, r = 0) {
-    const Source s = uniform(x - x_first < kListed ? s_source[1 + wave][x - x_first] : source_of(a, x));
+    const Source s = uniform(x - x_first < kListed ? s_source[1 + wave][x - x_first] : source_of(a, x, lowest));
     const unsigned size = narrow_size<C, kGroup<T, D>>(s);
     if (size <= r) continue;
     const Cut c = cut_of<C::NARROW_FRONT, C::NARROW>(size, r, per, left, C::NARROW_LEAST);
@@ -1059,10 +1168,20 @@ template <typename T, int D, typename OUT> __global__ __launch_bounds__(kThreads
   }
 }
 
-template <typename T, int D, bool EXACT, typename OUT> hipError_t run(const SharedArgs& a, hipStream_t st) {
+template <typename T, int D, bool EXACT, typename OUT> hipError_t run(const SharedArgs& given, hipStream_t st) {
+  hipError_t e;
+  SharedArgs a = given;
+  a.sized = places_of(a.r.n_inst) > kThreads * kHeld;
+  if (a.sized && a.window > 0) {
+    share_low_kernel<<<kShareWgs, kThreads, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.sized) {
+    share_sizes_kernel<T, D, EXACT><<<blocks_of(a.r.n_inst), kThreads, 0, st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   cache_shared_kernel<T, D, EXACT><<<kShareWgs, kThreads, kSharedLds, st>>>(a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   const unsigned wgs = (unsigned)(((long long)a.r.n_inst * a.rows + kWaves - 1) / kWaves);
   cache_shared_join_kernel<T, D, OUT><<<wgs, kThreads, 0, st>>>(a);
   return hipGetLastError();

@@ -40,6 +40,9 @@ SharedWs shared_ws(const Shape& s, int q_cap) {
   w.begun = take((size_t)s.n_inst * 4);
   w.behind = take((size_t)s.n_inst * 4);
   w.row = take(rows * 8);
+  w.low = take((size_t)s.n_inst * 4);
+  w.sizes = take(shared_sources(s) * 16);
+  w.totals = take(shared_sources(s) / 256 * 16);
   w.ml = take(pieces * 2 * 4);
   w.o = take(pieces * s.d * 4);
   w.total = o;
@@ -88,6 +91,10 @@ static hipError_t launch_shared(const Shape& s, const void* q, const int32_t* n_
   a.begun = reinterpret_cast<int32_t*>(base + w.begun);
   a.behind = reinterpret_cast<int32_t*>(base + w.behind);
   a.row = reinterpret_cast<int2*>(base + w.row);
+  a.sized = 0;
+  a.low = reinterpret_cast<int32_t*>(base + w.low);
+  a.sizes = reinterpret_cast<unsigned long long*>(base + w.sizes);
+  a.totals = reinterpret_cast<unsigned long long*>(base + w.totals);
   a.ml = reinterpret_cast<float*>(base + w.ml);
   a.o = reinterpret_cast<float*>(base + w.o);
   return ap::launch_cache_shared(s, a, decode, static_cast<hipStream_t>(stream));

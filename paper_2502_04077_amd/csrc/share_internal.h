@@ -70,6 +70,10 @@ struct SharedArgs {
   SharePlan plan;
   int32_t *begun, *behind;         // workspace: [n_inst] whether there are pieces of the beginning that an instance is the first member of; of the rows behind
   int2* row;                       // workspace: [2 * n_inst * rows] of a row of q: the first of its pieces, and how many (a wave's: negative)
+  int sized;                       // whether the sizes of the sources are in the workspace:
+  int32_t* low;                    // [n_inst] with a window: by a group's first member, the lowest position of its queries
+  unsigned long long* sizes;       // [whole blocks of sources][2] sizes of those in front in the block: of tiles with many rows of q, and with few
+  unsigned long long* totals;      // [blocks][2]
   float *ml, *o;                   // workspace: [shared_pieces][2] maximum and sum, and [..][d]
 };
 // Pieces: those of workgroups, in front of narrow0, and of waves.
@@ -77,7 +81,9 @@ inline size_t shared_narrow0(const Shape& s, int q_cap) { return (size_t)2 * s.n
 inline size_t shared_pieces(const Shape& s, int q_cap) {
   return shared_narrow0(s, q_cap) + (size_t)2 * s.n_inst * q_cap * s.g + (size_t)kNarrowRows * 4 * kShareWgs;
 }
-struct SharedWs { size_t begun, behind, row, ml, o, total; };
+// Of so many sources at most, in whole blocks of 256.
+inline size_t shared_sources(const Shape& s) { return ((size_t)s.n_inst + s.n_inst / 2 + 255) / 256 * 256; }
+struct SharedWs { size_t begun, behind, row, low, sizes, totals, ml, o, total; };
 SharedWs shared_ws(const Shape& s, int q_cap);
 
 hipError_t launch_cache_share(const Shape& s, const int32_t* group, const int32_t* shared, const SharePlan& plan, hipStream_t st);

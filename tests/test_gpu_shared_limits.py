@@ -185,7 +185,7 @@ def test_numbers_of_instances_and_groups(n, groups):
         assert (two[i, new[i]:] == 7).all()
 
 
-@pytest.mark.parametrize("n", [1500, 5000])
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 1500, 5000])
 def test_many_groups_and_windows(n):
     """More sources than the threads of a workgroup hold at once, most of them of no or few tiles, with windows that leave some beginnings."""
     import paper_2502_04077_amd as ap
