@@ -13,11 +13,11 @@
 // few rows into shares of a wave each: the one needs the matrix unit, the other the memory, and a CU has room for a workgroup of both.  Whoever has a
 // share leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
 //
-// 64 sequences of 40 to 2050 rows behind 8190 in common (8 KV heads, g = 4, d = 128, decode) take 56 us; their 172 MB are read in 24 at the rate of a large
-// read.  Of the first launch's 50 us 7 go by until the shares are known (two trips to memory, sums over the sources, the sources of a share), 5 to 8 until a
+// 64 sequences of 40 to 2050 rows behind 8190 in common (8 KV heads, g = 4, d = 128, decode) take 53 us; their 172 MB are read in 24 at the rate of a large
+// read.  Of the first launch's 48 us 6 go by until the shares are known (two trips to memory, sums over the sources, the sources of a share), 3 to 6 until a
 // piece's first product (table, rows; members, lengths, queries), and the shares' ends lie 5 apart.  A tile of 64 rows takes a workgroup 2.4 us (128 rows of
 // q: 0.88 PFLOP/s, the matrix unit) and 3.3 where probabilities keep 24 bits (the same), a group of 32 a wave 3 to 4 us (two groups under way a wave: bytes in flight).
-// Four samples of one prompt of 2041 rows take 21 us, which is this chain and the second launch's.
+// Four samples of one prompt of 2041 rows take 18 us, which is this chain (4 us until the shares are known, 2.5 until the first product) and the second launch's.
 #include "cache_tiles.h"
 #include "share_internal.h"
 

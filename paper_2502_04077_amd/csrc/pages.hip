@@ -7,8 +7,8 @@
 // so that the order of atomics does not show in any result.  Where there is little to do one workgroup takes all three steps (small).  Where the state does not belong to the
 // table, what comes out is unspecified, but every page that is read or written lies in the pool.
 //
-// Latency bounds all but the copies: a resize of 32 instances takes 8 us (7 of them its one launch, four trips to memory one after the other), of 512
-// instances with 128 pages to give out each 20 (4.4, 6.5 and 9 to 17 of three launches, where segments' free pages are counted), a fork of 512 17.
+// Latency bounds all but the copies: a resize of 32 instances takes 7.6 us (6 of them its one launch, trips to memory one after the other), of 512 instances
+// with 128 pages to give out each 16 (3.8, 6.6 and 10 of three launches), a fork of 32 instances 9.8, of 512 17.
 #include "cache_body.h"
 #include "share_internal.h"
 
@@ -20,7 +20,7 @@ constexpr int kThreads = 256, kWaves = 4;
 // 512 and 4096 workgroups 16.9, 14.6, 14.8, 14.8 and 38, 29, 26.5, 32 us.
 constexpr int kPickWgs = 64, kApplyWgs = 512;
 constexpr int kEntries = 256;                              // of a table that a wave, or half of one, asks for together: one after the other is a trip to memory each
-constexpr int kSmallThreads = 1024, kSmallSegments = 256, kSmallInstances = 64;
+constexpr int kSmallThreads = 1024, kSmallSegments = 256, kSmallInstances = 32;
 
 struct Head { int needed, lacking, live, moved; };
 
@@ -491,7 +491,7 @@ __device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const Page
   if (tid < kSmallSegments) {
     const int x = tid < p.n_inst ? need[tid].pages : 0, segment = sum_int(tid < p.segments ? p.seg[tid] : 0);
     if (lane == 0) s_sums[tid >> 6] = segment;
-    if (tid < kSmallInstances) {
+    if (tid < 64) {
       int upto = x;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -552,11 +552,11 @@ __global__ __launch_bounds__(kSmallThreads) void fork_small_kernel(ForkArgs a) {
   });
 }
 // What one workgroup does sooner than three launches: few instances, tables that are looked through quickly, and few bytes that it may have to copy.
-// Resize, a table's 132 entries, 8, 32, 64, 128 instances: 8.5, 8.8, 12.2, 17.9 us, by three launches 15; of 64 with 252 entries, 63 of them to be given
-// out each, 19 and 15.  Fork of 32 instances with 132 entries each and pages of 8 KB (K and V) 13.0 and 16.5 us, of 64 22.1 and 16.5, of 32 with 504
-// entries 18.9 and 16.6, with pages of 32 KB 22.3 and 16.6.
-bool small(const Pages& p, int instances, long long copied) {
-  return p.n_inst <= instances && (long long)p.n_inst * p.nb_cap <= 160 * instances && p.segments <= kSmallSegments && copied <= 256 * 1024;
+// Tables of 132 entries, captured and called one by one (where three launches are bound by the host): resize of 8, 32, 48, 64 instances 6.7 and 7.3, 9.2 and
+// 9.5, 11.9 and 12.0, 14.5 and 14.7 us, by three launches 9.5 and 12.8; fork of 8, 32, 64 instances, pages of 8 KB (K and V), 9.1 and 9.2, 10.6 and 10.6, 16,
+// by three launches 11.4 and 13.3.
+bool small(const Pages& p, long long copied) {
+  return p.n_inst <= kSmallInstances && (long long)p.n_inst * p.nb_cap <= 160 * kSmallInstances && p.segments <= kSmallSegments && copied <= 256 * 1024;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- compaction
@@ -677,7 +677,7 @@ hipError_t launch_pages_count(const Pages& p, hipStream_t st) {
 }
 
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
-  if (small(a.p, kSmallInstances, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
+  if (small(a.p, 0)) {                                     // (copies are rare here: where rows go back into shared pages)
     resize_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
     return hipGetLastError();
   }
@@ -691,7 +691,7 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
-  if (small(a.p, kSmallInstances / 2, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
+  if (small(a.p, (long long)a.p.n_inst * 32 * a.p.row_pieces << a.p.lb)) {
     fork_small_kernel<<<1, kSmallThreads, 0, st>>>(a);
     return hipGetLastError();
   }

@@ -28,11 +28,11 @@ SHAPES = [  # n, nb, n_pages, b, d, dtype
     (700, 7, 3500, 8, 64, "bf16"),         # more instances than a fourth of the threads of a large workgroup
     (1270, 4, 4000, 8, 64, "bf16"),        # more than all of them
     (1200, 8, 7000, 8, 64, "bf16"),
-    (32, 300, 5000, 8, 64, "bf16"),        # tables of more than four entries a lane, by a wave and by a workgroup
-    (17, 256, 2500, 16, 64, "f32"),        # one instance more than a workgroup has waves
-    (50, 30, 900, 8, 64, "bf16"),          # more than a fork has in one workgroup, not more than a resize
-    (64, 11, 500, 8, 64, "bf16"),
-    (65, 11, 500, 8, 64, "bf16"),
+    (13, 300, 3000, 8, 64, "bf16"),        # tables longer than half a wave looks at together
+    (17, 256, 2500, 16, 64, "f32"),
+    (50, 30, 900, 8, 64, "bf16"),
+    (32, 11, 250, 8, 64, "bf16"),          # as many instances as one workgroup takes, and one more
+    (33, 11, 250, 8, 64, "bf16"),
     (3, 2100, 4100, 8, 64, "bf16"),        # rows of a table longer than a workgroup looks at together
 ]
 
