@@ -126,7 +126,7 @@ struct Tiling {
 template <int TT> __device__ __forceinline__ Tiling tiling_of(const Source& s) {
   Tiling t;
   t.ta = (unsigned)s.a0 / TT;
-  const int end = (unsigned)(s.f + TT - 1) / TT, behind = (unsigned)(s.p1 + TT) / TT;
+  const int end = ((unsigned)s.f + (TT - 1)) / TT, behind = ((unsigned)s.p1 + TT) / TT;
   t.ts = s.f > 0 ? end - t.ta : 0;
   t.tb = (unsigned)s.lo0 / TT;
   if (t.ts > 0 && t.tb < end) t.tb = end;

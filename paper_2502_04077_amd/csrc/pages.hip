@@ -237,7 +237,15 @@ template <int LANES> __device__ __forceinline__ Need fork_need(const ForkArgs& a
   bool heir = false;
   if (rest > 0 && a.parent[p] != p) {                      // the lowest that goes on from p takes its last page over
     heir = true;
-    for (int x0 = 0; x0 < j && heir; x0 += LANES) heir = ballot_of<LANES>(x0 + lane < j && a.parent[x0 + lane] == p) == 0;
+    for (int x0 = 0; x0 < j && heir; x0 += kEntries) {
+      int of[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) of[u] = a.parent[x0 + LANES * u + lane < j ? x0 + LANES * u + lane : 0];
+      bool other = false;
+#pragma unroll
+      for (int u = 0; u < U; ++u) other |= x0 + LANES * u + lane < j && of[u] == p;
+      heir = ballot_of<LANES>(other) == 0;
+    }
   }
   const int32_t* table = a.p.table + (size_t)p * a.p.nb_cap;
   int32_t* staged = at<int32_t>(a.ws, a.w.staged) + (size_t)j * a.p.nb_cap;
@@ -320,32 +328,41 @@ template <int NT> __device__ __forceinline__ int sum_of(const int32_t* x, int n,
   return all;
 }
 
-// Picks the pages of the instances' needs: workgroup `which` of `wgs`.  info as if nothing were given up.
+// Picks the pages of the instances' needs: workgroup `which` of `wgs`; the one behind them sums up what the instances before each one need.  info as if
+// nothing were given up.
 __global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
   __shared__ int s_wave[kWaves];
-  const int which = blockIdx.x, wgs = gridDim.x;
+  const int which = blockIdx.x, wgs = gridDim.x - 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* need = at<int32_t>(ws, w.need);
-  const int n = sum_of<kThreads>(need, p.n_inst, s_wave), free = clamped(sum_of<kThreads>(p.seg, p.segments, s_wave), 0, p.n_pages);
-  const int each = (p.segments + wgs - 1) / wgs;
-  const int s0 = which * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
-  if (s0 < s1) {
-    const int before = s0 == 0 ? 0 : sum_of<kThreads>(p.seg, s0, s_wave);
-    pick_segments<kThreads>(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+  if (which < wgs) {
+    const int n = sum_of<kThreads>(need, p.n_inst, s_wave), free = clamped(sum_of<kThreads>(p.seg, p.segments, s_wave), 0, p.n_pages);
+    const int each = (p.segments + wgs - 1) / wgs;
+    const int s0 = which * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
+    if (s0 < s1) {
+      const int before = s0 == 0 ? 0 : sum_of<kThreads>(p.seg, s0, s_wave);
+      pick_segments<kThreads>(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+    }
+    if (which == 0 && tid == 0) {
+      Head* head = at<Head>(ws, w.head);
+      head->needed = n;
+      head->lacking = n > free ? n - free : 0;
+      info[0] = n > free ? free : free - n;
+      info[1] = n > free ? n - free : 0;
+    }
+    return;
   }
-  if (which > 0) return;
-  if (tid == 0) {
-    Head* head = at<Head>(ws, w.head);
-    head->needed = n;
-    head->lacking = n > free ? n - free : 0;
-    info[0] = n > free ? free : free - n;
-    info[1] = n > free ? n - free : 0;
-  }
-  // What the instances before need.
+  constexpr int U = 4;                                     // instances of a thread at a time
   int done = 0;
-  for (int i0 = 0; i0 < p.n_inst; i0 += kThreads) {
-    const int i = i0 + tid, x = i < p.n_inst ? need[i] : 0;
-    int upto = x;
+  for (int i0 = 0; i0 < p.n_inst; i0 += U * kThreads) {
+    int x[U], mine = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + U * tid + u;
+      x[u] = i < p.n_inst ? need[i] : 0;
+      mine += x[u];
+    }
+    int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int y = __shfl_up(upto, o, 64);
@@ -354,12 +371,17 @@ __global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws,
     __syncthreads();
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
-    int ahead = done + upto - x;
+    int ahead = done + upto - mine;
     for (int v = 0; v < kWaves; ++v) {
       if (v < wave) ahead += s_wave[v];
       done += s_wave[v];
     }
-    if (i < p.n_inst) at<int32_t>(ws, w.before)[i] = ahead;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + U * tid + u;
+      if (i < p.n_inst) at<int32_t>(ws, w.before)[i] = ahead;
+      ahead += x[u];
+    }
   }
 }
 __device__ __forceinline__ void settle_segments(const Pages& p, const int32_t* taken) {
@@ -684,7 +706,7 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
   resize_need_kernel<<<per_wave(a.p.n_inst), kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  pages_pick_kernel<<<pick_wgs(a.p), kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
+  pages_pick_kernel<<<pick_wgs(a.p) + 1, kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   resize_apply_kernel<<<a.p.n_inst < kApplyWgs ? a.p.n_inst : kApplyWgs, kThreads, 0, st>>>(a);
   return hipGetLastError();
@@ -698,7 +720,7 @@ hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
   fork_need_kernel<<<per_wave(a.p.n_inst), kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  pages_pick_kernel<<<pick_wgs(a.p), kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
+  pages_pick_kernel<<<pick_wgs(a.p) + 1, kThreads, 0, st>>>(a.p, a.ws, a.w, a.info);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   fork_apply_kernel<<<a.p.n_inst, kThreads, 0, st>>>(a);
   return hipGetLastError();
