@@ -289,7 +289,7 @@ class PagedRun(_Lengths):
         self.free = n_pages        # at least so many pages are free
         self.longest = 0           # no cache is longer than this
         self.ctx.pages_count(self.table, n_pages, self.state)
-        self.share(self.group, self.shared)
+        self._share(self.group, self.shared)
 
     # -- pages ------------------------------------------------------------------------------------
     def _given(self, most, call):
@@ -345,7 +345,18 @@ class PagedRun(_Lengths):
 
     # -- sequences --------------------------------------------------------------------------------
     def share(self, group, shared):
-        """Says which instances have how many first rows in common, int32 [n_inst] each (group < 0: none)."""
+        """Says which instances have how many first rows in common, int32 [n_inst] each (group < 0: none).  A group has any number; it is kept
+        under its lowest member's."""
+        self._check_each(group, torch.int32)
+        self._check_each(shared, torch.int32)
+        ordered, at = torch.sort(group, stable=True)
+        begins = torch.ones_like(ordered)
+        begins[1:] = ordered[1:] != ordered[:-1]
+        number = torch.empty_like(at).scatter_(0, at, begins.cumsum(0) - 1)
+        self._regroup(number, group >= 0, shared)
+
+    def _share(self, group, shared):
+        """The same of groups that have their lowest members' numbers; the others, that follow from them, count on it."""
         self.ctx.cache_share(group, shared, self.plan)
         self.group.copy_(group)
         self.shared.copy_(shared)
@@ -358,7 +369,7 @@ class PagedRun(_Lengths):
         low = torch.full((2 * n + 1,), n, device=self.dev).scatter_reduce_(0, number, each, "amin")[number]
         high = torch.full((2 * n + 1,), -1, device=self.dev).scatter_reduce_(0, number, each, "amax")[number]
         grouped = members & (low < high)
-        self.share(torch.where(grouped, low, -1).int(), torch.where(grouped, shared, 0).int())
+        self._share(torch.where(grouped, low, -1).int(), torch.where(grouped, shared, 0).int())
 
     def fork(self, parent):
         """Instance j goes on from parent[j], int32 [n_inst]; one outside [0, n_inst) ends.  Those that go on from members of a group are a group,
@@ -387,7 +398,7 @@ class PagedRun(_Lengths):
         """The last n tokens of every cache, int32 [n_inst], are taken back (drafts that were not accepted)."""
         self._check_each(n, torch.int32)
         self._shorter((self.len - n.clamp(min=0)).clamp(min=0))
-        self.share(self.group, torch.minimum(self.shared, self.len))
+        self._share(self.group, torch.minimum(self.shared, self.len))
 
     def end(self, which):
         """Sequences that end, bool [n_inst]: their pages are free, unless others have them too."""

@@ -156,3 +156,22 @@ def test_a_pool_that_is_full():
     assert x.whole() == 28
     x.step()
     assert x.whole() == 29
+
+
+@pytest.mark.parametrize("number", [8, 15, 16, 1000, 2 ** 31 - 1])
+def test_groups_of_any_number(number):
+    """Groups that the caller names anew, by numbers that are no instance's, beside instances that stand alone."""
+    x = Model(100)
+    x.prefill(120, [100, 0, 0, 60, 50, 70, 0, 0])
+    x.fork([0, 0, 0, 3, 4, 5, 0, -1])
+    x.run.share(x.i32([number, number, -1, number - 8, -5, 2 ** 31 - 2, number, -1]), x.i32([100, 90, 100, 60, 50, 70, 95, 0]))
+    assert x.run.group.tolist() == [0, 0, -1, -1, -1, -1, 0, -1] and x.run.shared.tolist() == [100, 90, 0, 0, 0, 0, 95, 0]
+    x.step()
+    x.fork([0, 1, 2, 3, 3, 5, 6, 3])
+    assert x.run.group.tolist() == [0, 0, -1, 3, 3, -1, 0, 3] and x.run.shared.tolist() == [100, 90, 0, 61, 61, 0, 95, 61]
+    x.step()
+    x.end([0])
+    assert x.run.group.tolist() == [-1, 1, -1, 3, 3, -1, 1, 3]
+    x.prefill(7, [7, 7, 0, 7, 5, 7, 3, 1])
+    x.take_back([0, 60, 0, 7, 5, 0, 0, 9])
+    x.step()

@@ -126,6 +126,41 @@ def test_groups_follow_forks(run):
     assert run.free_pages() == 24
 
 
+# Numbers that groups are given: below the number of instances, up to twice as many, above, and the largest.
+NUMBERS = [0, 3, N, N + 3, 2 * N - 1, 2 * N, 1000, 2 ** 31 - 1]
+
+
+@pytest.mark.parametrize("number", NUMBERS)
+def test_groups_of_any_number(run, number):
+    """What a group is called does not matter: everything that follows is as for groups that are called by their lowest member."""
+    other = (number + 1) % 2 ** 31
+    run.prefill(*_rows(80), _i([40] * 6))
+    run.share(_i([-1, number, number, other, -2 ** 31, other]), _i([40] * 6))
+    assert run.group.tolist() == [-1, 1, 1, 3, -1, 3] and run.shared.tolist()[1:4] == [40] * 3
+    run.fork(torch.arange(N, dtype=I32))                   # each from itself: nothing changes
+    assert run.group.tolist() == [-1, 1, 1, 3, -1, 3] and run.shared.tolist() == [0, 40, 40, 40, 0, 40]
+    run.take_back(_i([0, 0, 3, 0, 0, 0]))
+    assert run.group.tolist() == [-1, 1, 1, 3, -1, 3] and run.shared.tolist() == [0, 40, 37, 40, 0, 40]
+    run.end(torch.tensor([False, False, False, True, False, False]))
+    assert run.group.tolist() == [-1, 1, 1, -1, -1, -1] and run.shared.tolist() == [0, 40, 37, 0, 0, 0]
+
+
+@pytest.mark.parametrize("number", NUMBERS)
+def test_children_of_one_that_stood_alone_are_nobody_elses(run, number):
+    """Two instances of a group, and children of one that stands alone."""
+    run.prefill(*_rows(80), _i([40] * 6))
+    run.share(_i([number, number, -1, -1, -1, -1]), _i([16] * 6))
+    run.fork(_i([0, 1, 3, 3, -1, -1]))
+    assert run.group.tolist() == [0, 0, 2, 2, -1, -1] and run.shared.tolist() == [16, 16, 40, 40, 0, 0]
+
+
+def test_a_group_of_one_number_stands_alone(run):
+    run.prefill(*_rows(80), _i([40] * 6))
+    run.share(_i([7, 8, 9, 10, 11, 12]), _i([16] * 6))
+    run.fork(_i([0, 0, 2, 3, 4, 5]))
+    assert run.group.tolist() == [0, 0, -1, -1, -1, -1] and run.shared.tolist() == [40, 40, 0, 0, 0, 0]
+
+
 def test_tokens_are_taken_back(run):
     run.prefill(*_rows(80), _i([33, 0, 0, 0, 0, 20]))
     run.fork(_i([0, 0, 0, -1, -1, 5]))
