@@ -331,8 +331,8 @@ int ap_cache_evict(ap_ctx* ctx, void* K, void* V, const float* acc, const int32_
  *   state  device int32, ap_pages_state_bytes: word p < n_pages is how often the table names page p, and p is free where that is 0; the
  *          words behind are the library's.  Written by ap_pages_count first.  Where it does not belong to the table what these calls do is
  *          unspecified, but they stay inside the pool
- *   info   device int32 [2]: free pages after the call; and of resize and fork how many pages were lacking.  With one lacking nothing at all
- *          is changed
+ *   info   device int32 [2]: free pages after the call; and of resize and fork how many pages were lacking (2^31 - 1: so many or more).  With
+ *          one lacking nothing at all is changed
  *   ws     device scratch of ap_pages_workspace_bytes; its contents carry nothing between calls, and calls that share one are issued in
  *          stream order on one stream
  * Pages are given out the lowest free one first, to the needs in the order of instances and of their blocks; a page that a call itself gives

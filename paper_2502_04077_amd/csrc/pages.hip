@@ -22,11 +22,18 @@ constexpr int kPickWgs = 64, kApplyWgs = 512;
 constexpr int kEntries = 256;                              // of a table that a wave, or half of one, asks for together: one after the other is a trip to memory each
 constexpr int kSmallThreads = 1024, kSmallSegments = 256, kSmallInstances = 32;
 
+constexpr int kMostLacking = 0x7fffffff;                   // that info has room for
+
 struct Head { int needed, lacking, live, moved; };
 
 template <typename T> __device__ __forceinline__ T* at(char* ws, size_t offset) { return reinterpret_cast<T*>(ws + offset); }
 __device__ __forceinline__ bool in_pool(const Pages& p, int page) { return (unsigned)page < (unsigned)p.n_pages; }
 __device__ __forceinline__ int sum_int(int x) {            // over the wave's lanes
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ long long sum_long(long long x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
   return x;
@@ -328,50 +335,65 @@ template <int NT> __device__ __forceinline__ int sum_of(const int32_t* x, int n,
   return all;
 }
 
-// Picks the pages of the instances' needs: workgroup `which` of `wgs`; the one behind them sums up what the instances before each one need.  info as if
-// nothing were given up.
+// What all instances need, by a workgroup: up to all entries of the table, which may be more than 32 bits hold.
+__device__ __forceinline__ long long needed(const int32_t* need, int n, long long* s_wave) {
+  long long mine = 0;
+  for (int k = threadIdx.x; k < n; k += kThreads) mine += need[k];
+  mine = sum_long(mine);
+  if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  long long all = 0;
+  for (int w = 0; w < kWaves; ++w) all += s_wave[w];
+  return all;
+}
+
+// Picks the pages of the instances' needs: workgroup `which` of `wgs`; the one behind them sums up what the instances before each one need (sums that
+// are asked for only where all of them are no more than the pool has pages).  info as if nothing were given up.
 __global__ __launch_bounds__(kThreads) void pages_pick_kernel(Pages p, char* ws, PagesWs w, int32_t* info) {
   __shared__ int s_wave[kWaves];
+  __shared__ long long s_needed[kWaves];
   const int which = blockIdx.x, wgs = gridDim.x - 1;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* need = at<int32_t>(ws, w.need);
   if (which < wgs) {
-    const int n = sum_of<kThreads>(need, p.n_inst, s_wave), free = clamped(sum_of<kThreads>(p.seg, p.segments, s_wave), 0, p.n_pages);
+    const long long all = needed(need, p.n_inst, s_needed);
+    const int free = clamped(sum_of<kThreads>(p.seg, p.segments, s_wave), 0, p.n_pages), n = all <= free ? (int)all : 0;
     const int each = (p.segments + wgs - 1) / wgs;
     const int s0 = which * each, s1 = s0 + each < p.segments ? s0 + each : p.segments;
     if (s0 < s1) {
       const int before = s0 == 0 ? 0 : sum_of<kThreads>(p.seg, s0, s_wave);
-      pick_segments<kThreads>(p, s0, s1, before, n <= free ? n : 0, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
+      pick_segments<kThreads>(p, s0, s1, before, n, at<int32_t>(ws, w.picked), at<int32_t>(ws, w.taken), s_wave);
     }
     if (which == 0 && tid == 0) {
+      const long long lacking = all - free;
       Head* head = at<Head>(ws, w.head);
       head->needed = n;
-      head->lacking = n > free ? n - free : 0;
-      info[0] = n > free ? free : free - n;
-      info[1] = n > free ? n - free : 0;
+      head->lacking = lacking <= 0 ? 0 : (lacking < kMostLacking ? (int)lacking : kMostLacking);
+      info[0] = free - n;
+      info[1] = head->lacking;
     }
     return;
   }
   constexpr int U = 4;                                     // instances of a thread at a time
-  int done = 0;
+  unsigned done = 0;
   for (int i0 = 0; i0 < p.n_inst; i0 += U * kThreads) {
-    int x[U], mine = 0;
+    unsigned x[U], mine = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + U * tid + u;
       x[u] = i < p.n_inst ? need[i] : 0;
       mine += x[u];
     }
-    int upto = mine;
+    unsigned upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(upto, o, 64);
+      const unsigned y = __shfl_up(upto, o, 64);
       if (lane >= o) upto += y;
     }
     __syncthreads();
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
-    int ahead = done + upto - mine;
+    unsigned ahead = done + upto - mine;
     for (int v = 0; v < kWaves; ++v) {
       if (v < wave) ahead += s_wave[v];
       done += s_wave[v];

@@ -230,3 +230,25 @@ def test_many_pages():
     assert torch.equal(K.view(torch.int32)[:, 0, 0][table[there].long()], before[there]) and torch.equal(V[table[there].long()], V[before[there].long()])
     stay = there & (before < live)
     assert torch.equal(table[stay], before[stay])
+
+
+def test_needs_beyond_32_bits():
+    """Tables with more entries than 32 bits count: what lacks is said as far as there is room for it, and nothing is changed."""
+    import paper_2502_04077_amd as ap
+    n, nb, b, d, n_pages = 65535, 65538, 8, 64, 4
+    ctx = ap.Context(n_inst=n, g=1, head_dim=d, block=b, hist_len=1, t_cap=nb * b, k_blocks=1, n_sink=0, n_local=0, c1=4, c2=4, kv_dtype="bf16")
+    K, V = (torch.full((n_pages, b, d), x, dtype=torch.bfloat16, device="cuda:0") for x in (1.0, 2.0))
+    table = torch.full((n, nb), -1, dtype=torch.int32, device="cuda:0")
+    state = torch.zeros(ctx.pages_state_bytes(n_pages) // 4, dtype=torch.int32, device="cuda:0")
+    ws, info = torch.empty(ctx.pages_workspace_bytes(n_pages), dtype=torch.uint8, device="cuda:0"), torch.zeros(2, dtype=torch.int32, device="cuda:0")
+    ctx.pages_count(table, n_pages, state)
+    for needs in (2 ** 32 + 2, 2 ** 32 - 1, 2 ** 31, 2 ** 31 + 3, 2 ** 31 + 4, n * nb, 5, 3):
+        lens = torch.zeros(n, dtype=torch.int32)
+        lens[:needs // nb] = nb * b
+        if needs % nb:
+            lens[needs // nb] = needs % nb * b
+        ctx.pages_resize(K, V, table, state, lens.cuda(), None, 0, info, ws)
+        if needs > n_pages:
+            assert info.tolist() == [n_pages, min(needs - n_pages, 2 ** 31 - 1)] and state.tolist() == [0] * 4 + [4], needs
+            assert int(table.max()) == -1 and (K == 1).all() and (V == 2).all(), needs
+    assert info.tolist() == [1, 0] and table[0, :4].tolist() == [0, 1, 2, -1] and state.tolist() == [1, 1, 1, 0, 1]
