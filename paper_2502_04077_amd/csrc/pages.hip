@@ -136,8 +136,8 @@ struct RowCopy {
 struct Move { int src, dst; bool real; };
 template <typename PAGE>
 __device__ __forceinline__ void move_pages(const u32x4* K_src, const u32x4* V_src, u32x4* K_dst, u32x4* V_dst, int n, int page_pieces, PAGE page) {
-  for (int x = blockIdx.x; x < n; x += gridDim.x) {
-    const Move m = page(x);
+  for (unsigned x = blockIdx.x; x < (unsigned)n; x += gridDim.x) {          // (up to 2^31 - 1, and a step behind)
+    const Move m = page((int)x);
     if (!m.real) continue;
     const size_t src = (size_t)m.src * page_pieces, dst = (size_t)m.dst * page_pieces;
     for (int y = threadIdx.x; y < page_pieces; y += kThreads) {

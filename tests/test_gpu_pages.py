@@ -252,3 +252,20 @@ def test_needs_beyond_32_bits():
             assert info.tolist() == [n_pages, min(needs - n_pages, 2 ** 31 - 1)] and state.tolist() == [0] * 4 + [4], needs
             assert int(table.max()) == -1 and (K == 1).all() and (V == 2).all(), needs
     assert info.tolist() == [1, 0] and table[0, :4].tolist() == [0, 1, 2, -1] and state.tolist() == [1, 1, 1, 0, 1]
+
+
+def test_the_longest_list_of_pages():
+    """As many entries as a call takes, which all but for the first lie outside the pools."""
+    import ctypes as C
+
+    import paper_2502_04077_amd as ap
+    ctx = Device(ap, _pool(2, 2, 3, 8, 64, "bf16", 1), 16, 64).ctx
+    src, dst = ([torch.randn((p, 8, 64), device="cuda:0").to(torch.bfloat16) for _ in range(2)] for p in (5, 7))
+    want = [torch.cat([s, x[5:]]) for s, x in zip(src, dst)]
+    for n in (2 ** 31 - 1, 2 ** 31 - 4096, 2 ** 31 - 4097):
+        on = [x.clone() for x in dst]
+        p = [C.c_void_p(x.data_ptr()) for x in src + on]
+        rc = ap.load_library().ap_pages_copy(ctx._h, p[0], p[1], 5, None, p[2], p[3], 7, None, n, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        torch.cuda.synchronize()
+        assert torch.equal(on[0], want[0]) and torch.equal(on[1], want[1])
