@@ -438,8 +438,13 @@ class PagedRun(_Lengths):
         self._check_instances(instances)
         if len(instances) != len(away["len"]) or max(self.len[instances].tolist()) > 0:
             raise ValueError(f"{len(away['len'])} caches need as many empty instances, not {instances}")
-        before, longest = self.len.clone(), self.longest
+        if max(away["len"]) > self.w.t_cap:
+            raise ValueError(f"a cache of {max(away['len'])} rows has no room here (t_cap = {self.w.t_cap})")
         pages = [-(-x // self.w.block) for x in away["len"]]
+        for name in "KV" if sum(pages) else "":
+            if away[name].dtype is not self.K.dtype or away[name].shape != (sum(pages),) + self.K.shape[1:]:
+                raise ValueError(f"{name}: {sum(pages)} pages as this pool's, not {away[name].dtype} {list(away[name].shape)}")
+        before, longest = self.len.clone(), self.longest
         self.len[instances] = torch.tensor(away["len"], dtype=torch.int32, device=self.dev)
         self.longest = max(self.longest, max(away["len"]))
         try:

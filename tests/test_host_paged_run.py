@@ -261,3 +261,25 @@ def test_an_empty_cache_waits_and_comes_back(run):
     run.bring_back(away, [5])
     assert away["len"] == [0] and run.len.tolist() == [20, 3, 1, 20, 20, 0]
     _whole(run)
+
+
+def _away(lens, block=B, d=128, dtype=torch.bfloat16):
+    """What set_aside of a run with such pages returns."""
+    pages = sum(-(-x // block) for x in lens)
+    return {"len": lens, "K": torch.ones((pages, block, d), dtype=dtype), "V": torch.ones((pages, block, d), dtype=dtype)}
+
+
+@pytest.mark.parametrize("away,instances", [
+    (_away([CAP + 1, 5]), [5, 4]),                         # longer than a cache here
+    (_away([5, CAP + 1]), [4, 5]),
+    (_away([40], block=8), [5]),
+    (_away([40], d=64), [5]),
+    (_away([40], dtype=torch.float32), [5]),
+    ({**_away([40]), "len": [20]}, [5]),                   # fewer rows than pages
+], ids=str)
+def test_caches_of_another_kind_do_not_come_back(run, away, instances):
+    run.prefill(*_rows(20), _i([20, 3, 1, 20, 0, 0]))
+    before = _state(run)
+    with pytest.raises(ValueError):
+        run.bring_back(away, instances)
+    assert _state(run) == before
