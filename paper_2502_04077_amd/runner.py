@@ -404,7 +404,7 @@ class PagedRun(_Lengths):
         """Sequences that end, bool [n_inst]: their pages are free, unless others have them too."""
         self._check_each(which, torch.bool)
         self._shorter(torch.where(which, 0, self.len))
-        self._regroup(self.group.clamp(min=0).long(), (self.group >= 0) & ~which, self.shared)
+        self._without(which)
 
     def _check_each(self, x, dtype):
         if x.dtype is not dtype or x.shape != self.len.shape or x.device != self.len.device:
@@ -413,6 +413,15 @@ class PagedRun(_Lengths):
     def _check_instances(self, instances):
         if not instances or len(set(instances)) != len(instances) or not all(0 <= i < self.w.n_inst for i in instances):
             raise ValueError(f"expected different instances out of {self.w.n_inst}, not {instances}")
+
+    def _which(self, instances):
+        which = torch.zeros(self.w.n_inst, dtype=torch.bool)
+        which[instances] = True
+        return which.to(self.dev)
+
+    def _without(self, which):
+        """These leave their groups."""
+        self._regroup(self.group.clamp(min=0).long(), (self.group >= 0) & ~which, self.shared)
 
     def _pages_of(self, instances, pages):
         return torch.cat([self.table[i, :m] for i, m in zip(instances, pages)])
@@ -428,9 +437,7 @@ class PagedRun(_Lengths):
             away["K"], away["V"] = (torch.empty(shape, dtype=self.K.dtype, pin_memory=True) for _ in "KV")
             self.ctx.pages_copy(self.K, self.V, self._pages_of(instances, pages), away["K"], away["V"], None)
             torch.cuda.current_stream(self.dev).synchronize()
-        which = torch.zeros(self.w.n_inst, dtype=torch.bool)
-        which[instances] = True
-        self.end(which.to(self.dev))
+        self.end(self._which(instances))
         return away
 
     def bring_back(self, away, instances):
@@ -456,3 +463,4 @@ class PagedRun(_Lengths):
             self.len.copy_(before)
             self.longest = longest
             raise
+        self._without(self._which(instances))

@@ -1,4 +1,6 @@
 """The bookkeeping of PagedRun on the CPU: calls on pages by their definition (page_reference.py), attention that does nothing."""
+from types import SimpleNamespace
+
 import pytest
 import torch
 
@@ -283,3 +285,15 @@ def test_caches_of_another_kind_do_not_come_back(run, away, instances):
     with pytest.raises(ValueError):
         run.bring_back(away, instances)
     assert _state(run) == before
+
+
+def test_caches_come_back_alone(run, monkeypatch):
+    """Also as an instance that was said to share a beginning while it was empty."""
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: SimpleNamespace(synchronize=lambda: None))
+    run.prefill(*_rows(20), _i([20, 3, 0, 0, 0, 0]))
+    away = _away([18, 5])
+    run.share(_i([-1, -1, 9, 9, 9, 7]), _i([0, 0, 16, 16, 16, 16]))
+    run.bring_back(away, [3, 5])
+    assert run.len.tolist() == [20, 3, 0, 18, 0, 5]
+    assert run.group.tolist() == [-1, -1, 2, -1, 2, -1] and run.shared.tolist() == [0, 0, 16, 0, 16, 0]
+    assert run.ctx.plans[-1] == (run.group.tolist(), run.shared.tolist())
