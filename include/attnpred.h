@@ -281,7 +281,8 @@ int ap_offload_step(ap_ctx* ctx, float* hist, int64_t n_pushed, const void* q, c
  *   A score q . K[j] is a sum in 32 bits.  One that is below what they hold, -inf, has no weight; a head that sees no other has a zero output,
  *   as one that sees nothing.  One that is above makes the head's output NaN
  *   window, n_first  a token at position p sees the rows j <= p, with window > 0 only those with j > p - window or j < n_first; window
- *         = 0 shows all.  Positions are places in the cache: rows that an eviction moved have their new ones
+ *         = 0 shows all.  Positions are places in the cache: rows that an eviction moved have their new ones.  What a row that
+ *         a token does not see holds, NaN and infinities included, does not matter to its outputs
  *   ws    device scratch of ap_cache_workspace_bytes; its contents carry nothing between calls, and calls that share one are issued in
  *         stream order on one stream
  * The lengths are read on the device only: a captured call follows lengths that change between replays. */

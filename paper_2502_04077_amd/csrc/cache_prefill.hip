@@ -50,6 +50,38 @@ __device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, 
   return s;
 }
 
+// A row of V in which a number is not finite makes NaN of every output that its product is taken for, also of queries that do not see the row and give it
+// the weight 0.  In tiles that some query sees in part a wave therefore looks through the rows that it fetched, sets such rows to 0 and says which they
+// are, bit by bit; they are added for those queries alone that see them.  What looking costs (g = 4, d = 128, without it and with it): a prompt of
+// 8190 tokens, 8 instances, 532 and 534 us, 1000 behind 7000 151.3 and 151.4, a window of 512 over 4096 61.4 and 62.6, 101 behind 416 15.1 and 15.5, prompts
+// of 100 in 512 instances 42.8 and 44.4.  Looked before the tile's first barrier, which saves one, 550, 154, 64.7, 15.5 and 45.3: the loop's schedule suffers.
+template <typename F, typename T> __device__ __forceinline__ unsigned take_out(u32x4* V, int wave) {
+  // An exponent of ones and one more carries into the sign.
+  constexpr unsigned exponents = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, one = sizeof(T) == 2 ? 0x00800080u : 0x00800000u, signs = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));                           // (made anew each time: no registers for what is seldom done)
+  u32x4* mine = V + wave * F::LOADS * 64 + lane;
+  unsigned found[F::LOADS], any = 0, rows = 0;
+#pragma unroll
+  for (int l = 0; l < F::LOADS; ++l) {
+    const u32x4 x = mine[l * 64];
+    found[l] = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) found[l] |= (x[e] & exponents) + one;
+    found[l] &= signs;
+    any |= found[l];
+  }
+  if (!__any(any != 0)) return 0;
+#pragma unroll
+  for (int l = 0; l < F::LOADS; ++l) {
+    const unsigned long long bad = __ballot(found[l] != 0), row = F::PIECES == 64 ? ~0ull : (1ull << F::PIECES) - 1;
+    if (bad >> (lane / F::PIECES * F::PIECES) & row) mine[l * 64] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < F::RPL; ++r) rows |= (bad >> (r * F::PIECES) & row) != 0 ? 1u << (l * F::RPL + r) : 0u;
+  }
+  return rows;
+}
+
 // Workgroup b of tiles * n_inst: which instance and which tile.  Consecutive workgroups go to the 8 XCDs in turn, so instances are dealt
 // eight at a time, one an XCD, whose L2 then serves one instance's K and V; the fewer than eight that are left share the XCDs.
 struct Work { int inst, tile; };
@@ -64,9 +96,10 @@ __device__ __forceinline__ Work work_of(unsigned b, int tiles, int n_inst) {
 }
 
 template <typename T, int D, int G, bool STAT>
-__global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && D == 128 ? 2 : 1))) void cache_prefill_kernel(PrefillArgs a) {
   using F = Form<T, D>;
   extern __shared__ __attribute__((aligned(16))) u32x4 s_tiles[];         // [2][K, V][TILE]
+  __shared__ unsigned s_out[2][kWaves];                                   // rows of V that were taken out
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hb = lane >> 5;
   const Work job = work_of(blockIdx.x, a.tiles, a.r.n_inst);
   const int inst = job.inst, row0 = (a.tiles - 1 - job.tile) * kPrefillRows;            // the longest ones first
@@ -112,12 +145,12 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
   for (int k = 0; k < F::KS; ++k) asm volatile("" : "+v"(qf[k]));
   for (int u = u_begin; u < u_end; ++u) {
     // This tile has landed; everybody is done with the buffer that is filled next.
+    const int t0 = s.tile(u) * F::TT;
+    u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
+    u32x4* Vt = Kt + F::TILE;
     landed<0>();
     lds_read();
     __builtin_amdgcn_s_barrier();
-    const int t0 = s.tile(u) * F::TT;
-    const u32x4* Kt = s_tiles + (u % 2) * 2 * F::TILE;
-    const u32x4* Vt = Kt + F::TILE;
     if (u + 1 < u_end) send(u + 1);
     float16v c[F::TB];
 #pragma unroll
@@ -168,6 +201,41 @@ __global__ __launch_bounds__(kThreads) void cache_prefill_kernel(PrefillArgs a) 
         part[i & 3] += c[b][i];
       }
     sum += (part[0] + part[1]) + (part[2] + part[3]);
+    if (!all) {                                            // (the same for all of the workgroup)
+      const unsigned out = take_out<F, T>(Vt, wave);
+      if (lane == 0) s_out[u % 2][wave] = out;
+      lds_read();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      unsigned long long rest = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) rest |= (unsigned long long)__builtin_amdgcn_readfirstlane(s_out[u % 2][w]) << (w * F::RW);
+      for (; rest != 0; rest &= rest - 1) {
+        const int r = __builtin_ctzll(rest), j = t0 + r;
+        if (j > s.p1 || (j >= s.f && j < s.lo0)) continue; // (that nobody sees, and was not read)
+        int half = threadIdx.x & 32;
+        asm volatile("" : "+v"(half));
+        const int mine = r - half / 8;                       // (register i holds row 8 (i / 4) + i % 4 of it)
+        float w = 0.f;
+#pragma unroll
+        for (int b = 0; b < F::TB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w = mine == 32 * b + reg_row(i, 0) ? c[b][i] : w;
+        w = sum32(w);
+        const bool hidden = (j > p) | ((j < lo) & (j >= a.n_first));
+        const size_t at = row_at(a.r, inst, j) * D + half / 8;
+#pragma unroll
+        for (int b = 0; b < F::DB; ++b) {
+          __builtin_amdgcn_sched_barrier(0);               // (few registers at a time)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const size_t x = at + 32 * b + reg_row(i, 0);
+            const float v = sizeof(T) == 2 ? (float)static_cast<const __bf16*>(a.V)[x] : static_cast<const float*>(a.V)[x];
+            o[b][i] += hidden ? 0.f : w * v;
+          }
+        }
+      }
+    }
     if constexpr (sizeof(T) == 2) {
       // Probabilities are rounded to bf16 for the matrix unit; their sum is taken before.  That adds an error of the size of the output's own
       // rounding: relative to the definition, outputs of scores spread by 2 are off by 0.0024 (root mean square), 0.0017 if the rounding of the output
