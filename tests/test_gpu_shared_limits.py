@@ -364,3 +364,36 @@ def test_what_a_query_does_not_see_does_not_matter(dt, d, g, bad):
             if r == m - 1:
                 assert ((one[i] - ref).abs() <= off).all(), i
     assert clean > n
+
+
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("where", ["q", "K", "V", "K first", "V first"])
+def test_what_holds_no_numbers_costs_little(where, dt, d):
+    """A sequence whose q, or a row of whose cache, holds no numbers: NaN for those that see it, the same bytes for the others, and in about the time."""
+    import paper_2502_04077_amd as ap
+    n, g, L, S = 16, 4, 16000, 15000
+    gen = torch.Generator(device="cuda:0").manual_seed(d)
+    K, V, q = (torch.randn(s, generator=gen, device="cuda:0").to(DT[dt]) for s in ((n, L, d), (n, L, d), (n, g, d)))
+    ctx = ap.Context(n_inst=n, g=g, head_dim=d, block=16, hist_len=1, t_cap=L, k_blocks=1, n_sink=0, n_local=0, c1=4, c2=4, kv_dtype=dt)
+    length, plan, ws = _i32([L] * n), _plan(ctx, [0] * n, [S] * n), _ws(ctx)
+
+    def timed():
+        out, best = torch.full((n, g, d), 7.0, device="cuda:0"), math.inf
+        for _ in range(5):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            for _ in range(4):
+                ctx.cache_decode_shared(q, K, V, length, plan, 0, 0, out, ws)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        return out, best
+    good, usual = timed()
+    for at in {"q": [q[3, 1]], "K": [K[3, L - 2]], "V": [V[3, L - 2]], "K first": K[:, 5], "V first": V[:, 5]}[where]:
+        at.fill_(math.nan)
+    bad, slow = timed()
+    hit = torch.full((n, g), "first" in where, device="cuda:0")
+    hit[3, 1 if where == "q" else slice(None)] = True
+    assert bad[hit].isnan().all() and torch.equal(bad[~hit], good[~hit])
+    # (Rows of q that go over all rows of the cache one after the other take some 5 ms, the call some 40 us.)
+    assert slow < 5 * usual, (usual, slow)
