@@ -54,7 +54,10 @@ __device__ __forceinline__ Span span_of(const CacheRows& r, const int32_t* n_q, 
 // the weight 0.  In tiles that some query sees in part a wave therefore looks through the rows that it fetched, sets such rows to 0 and says which they
 // are, bit by bit; they are added for those queries alone that see them.  What looking costs (g = 4, d = 128, without it and with it): a prompt of
 // 8190 tokens, 8 instances, 532 and 534 us, 1000 behind 7000 151.3 and 151.4, a window of 512 over 4096 61.4 and 62.6, 101 behind 416 15.1 and 15.5, prompts
-// of 100 in 512 instances 42.8 and 44.4.  Looked before the tile's first barrier, which saves one, 550, 154, 64.7, 15.5 and 45.3: the loop's schedule suffers.
+// of 100 in 512 instances 42.8 and 44.4; most where a tile in three is seen in part: 34 behind 2000 with a window of 395 and 37 first rows, 624 instances,
+// 91.8 and 97.2.  Tried and slower: looking before the tile's first barrier, which saves one (550, 154, 64.7, 15.5, 45.3, 100.5: the loop's schedule suffers);
+// a second pass over the tiles where an output is NaN (1.4 % of the prompt, 8 % of short ones: registers of the outer loop); adding the rows behind the second product
+// (their registers); looking at fewer rows of a tile (no gain: the barrier and the division of the loop's body count).
 template <typename F, typename T> __device__ __forceinline__ unsigned take_out(u32x4* V, int wave) {
   // An exponent of ones and one more carries into the sign.
   constexpr unsigned exponents = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, one = sizeof(T) == 2 ? 0x00800080u : 0x00800000u, signs = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
