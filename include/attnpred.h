@@ -388,7 +388,8 @@ int ap_cache_share(ap_ctx* ctx, const int32_t* group, const int32_t* shared, voi
 size_t ap_cache_shared_workspace_bytes(const ap_ctx* ctx, int32_t q_cap);
 int ap_cache_decode_shared(ap_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* len, const void* plan, int32_t window,
                            int32_t n_first, float* out, void* ws, void* stream);
-/* Chunks of few tokens (g q_cap <= 32, fp32 64) go through the groups; larger ones read every instance's own rows, which costs no more. */
+/* Chunks of few tokens (g q_cap <= 32, fp32 64) go through the groups; larger ones read every instance's own rows, which costs no more.  With bf16,
+ * probabilities of the former keep 16 bits, which the output's rounding covers; of the latter 8, as in ap_cache_prefill. */
 int ap_cache_prefill_shared(ap_ctx* ctx, const void* q, const int32_t* n_q, int32_t q_cap, const void* K, const void* V, const int32_t* len,
                             const void* plan, int32_t window, int32_t n_first, void* out, void* ws, void* stream);
 

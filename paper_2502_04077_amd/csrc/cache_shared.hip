@@ -14,9 +14,12 @@
 // share leaves (m, l, o) of every piece of it, and a second launch joins the pieces.
 //
 // 64 sequences of 40 to 2050 rows behind 8190 in common (8 KV heads, g = 4, d = 128, decode) take 53 us; their 172 MB are read in 24 at the rate of a large
-// read.  Of the first launch's 48 us 6 go by until the shares are known (two trips to memory, sums over the sources, the sources of a share), 3 to 6 until a
-// piece's first product (table, rows; members, lengths, queries), and the shares' ends lie 5 apart.  A tile of 64 rows takes a workgroup 2.4 us (128 rows of
-// q: 0.88 PFLOP/s, the matrix unit) and 3.3 where probabilities keep 24 bits (the same), a group of 32 a wave 3 to 4 us (two groups under way a wave: bytes in flight).
+// read.  Of the first launch's 46 us 6 go by until the shares are known (two trips to memory, sums over the sources, the sources of a share), 3 to 6 until a
+// piece's first product (table, rows; members, lengths, queries), and the shares' ends lie 5 apart.  A tile of 64 rows takes a workgroup 3.3 us (128 rows of
+// q, probabilities of 24 bits; the matrix unit), a group of 32 a wave 3 to 4 us: at d = 128 its part of LDS holds one group, whose K is sent for again when
+// its scores are done and whose V when its second product is, so that every group waits for memory.  Over the launch the matrix unit is busy 25 % of the time, 36 % of the
+// waves' time is spent waiting, and 210 MB come from memory, 4.6 TB/s.  In fp32 (16 sequences of 50 to 500 rows behind two beginnings of 4000, 36 us) 25 % and
+// 42 %, 100 MB, 2.8 TB/s: bytes under way, one group of 16 rows a wave.
 // Four samples of one prompt of 2041 rows take 18 us, which is this chain (4 us until the shares are known, 2.5 until the first product) and the second launch's.
 #include "cache_tiles.h"
 #include "share_internal.h"
@@ -101,7 +104,7 @@ constexpr int kSharedLds = 64 * 1024;       // two workgroups a CU
 // sequence of 150 rows 14.7 us, 4 samples of 2041 and more 18.3, 32 sequences of 110 to 400 19.3, drafts 42.1; 50 and 90: 16.0, 18.5, 20.7, 42.8; 40 and 45:
 // 14.6, 19.3, 19.6, 42.1; 50 and 130: 19.1, 20.8, 23.4, 42.7.)
 template <typename T, bool EXACT> struct Counts {
-  static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 24), WIDE_FRONT = sizeof(T) == 4 ? 60 : 80, WIDE_LEAST = 120;
+  static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 28), WIDE_FRONT = sizeof(T) == 4 ? 60 : 80, WIDE_LEAST = 120;
   static constexpr int NARROW = sizeof(T) == 4 ? 24 : 32, NARROW_FRONT = 40, NARROW_LEAST = sizeof(T) == 4 ? 50 : 60;
 };
 
@@ -456,8 +459,9 @@ __device__ __forceinline__ void wide_piece(const SharedArgs& a, const Source& s,
       }
     sum += (part[0] + part[1]) + (part[2] + part[3]);
     if constexpr (sizeof(T) == 2) {
-      // Probabilities are rounded to bf16, as in a prefill, where the output is rounded to it too; else (EXACT) they keep 24 bits.
-      constexpr int PARTS = EXACT ? 3 : 1;
+      // Where the output is rounded to bf16, probabilities keep 16 bits, else (EXACT) 24: two bf16 parts, or three.  Outputs of scores spread by 2 are off by
+      // 0.0017 relative to the definition (root mean square), which is the rounding of the output; with one part 0.0023, drafts 47.7 -> 46.5 us.
+      constexpr int PARTS = EXACT ? 3 : 2;
 #pragma unroll
       for (int k = 0; k < F::TT / 16; ++k) {
         typedef unsigned u32x4p __attribute__((ext_vector_type(4)));
@@ -661,7 +665,7 @@ __device__ __forceinline__ void narrow_piece(const SharedArgs& a, const Source& 
     if (more) landed<2 * N * (RING - 1) + N>();
     else landed_behind<2 * N, RING>(behind);
     if constexpr (sizeof(T) == 2) {
-      constexpr int PARTS = EXACT ? 3 : 1;
+      constexpr int PARTS = EXACT ? 3 : 2;
       typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
       for (int x = 0; x < XS; ++x) {
