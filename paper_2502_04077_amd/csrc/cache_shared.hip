@@ -102,7 +102,7 @@ constexpr int kSharedLds = 64 * 1024;       // two workgroups a CU
 // What a share counts, in tenths of a microsecond: of a workgroup's time a tile of the cache, and what a tile of rows of q costs beside them; of a
 // wave's time a group, and the same.  The least shares.  (As measured, and then varied by a third either way.  Of a wave's, in front and least, 40 and 60: a
 // sequence of 150 rows 14.7 us, 4 samples of 2041 and more 18.3, 32 sequences of 110 to 400 19.3, drafts 42.1; 50 and 90: 16.0, 18.5, 20.7, 42.8; 40 and 45:
-// 14.6, 19.3, 19.6, 42.1; 50 and 130: 19.1, 20.8, 23.4, 42.7.)
+// 14.6, 19.3, 19.6, 42.1; 50 and 130: 19.1, 20.8, 23.4, 42.7.  A tile of the cache with probabilities of two parts, 24, 26, 28, 30: drafts 50.9, 48.6, 47.7, 48.6.)
 template <typename T, bool EXACT> struct Counts {
   static constexpr int WIDE = sizeof(T) == 4 ? 84 : (EXACT ? 32 : 28), WIDE_FRONT = sizeof(T) == 4 ? 60 : 80, WIDE_LEAST = 120;
   static constexpr int NARROW = sizeof(T) == 4 ? 24 : 32, NARROW_FRONT = 40, NARROW_LEAST = sizeof(T) == 4 ? 50 : 60;

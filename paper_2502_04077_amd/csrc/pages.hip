@@ -1,14 +1,17 @@
 // Pages of a pool that instances share: taken and given back, forked, compacted, copied.
 //
-// refs[p] says how often the table names page p; p is free where that is 0.  seg holds the number of free pages among each 1024, so that free
-// pages are found without reading through those in use.  Three steps, a launch each, as none can begin before the one before has ended
+// refs[p] says how often the table names page p; p is free where that is 0.  seg holds the number of free pages among each 1024, so that workgroups know how
+// many lie in front of their own segments, and whether there are enough, without reading through the counts; of its own segments a workgroup reads all counts, also of
+// those without free pages, until enough are found.  Three steps, a launch each, as none can begin before the one before has ended
 // everywhere: what every instance needs, which free pages it gets (the x-th need in the order of instances and blocks gets the x-th free
 // page), and carrying it out.  The second step knows whether there are enough; if not, the third leaves all as it is.  Counts are whole numbers,
 // so that the order of atomics does not show in any result.  Where there is little to do one workgroup takes all three steps (small).  Where the state does not belong to the
 // table, what comes out is unspecified, but every page that is read or written lies in the pool.
 //
-// Latency bounds all but the copies: a resize of 32 instances takes 7.6 us (6 of them its one launch, trips to memory one after the other), of 512 instances
-// with 128 pages to give out each 16 (3.8, 6.6 and 10 of three launches), a fork of 32 instances 9.8, of 512 17.
+// Latency bounds all but the copies: a resize of 32 instances takes 7.6 us (6 of them its one launch, trips to memory one after the other), one of 512 instances
+// that give up 128 pages each 15 (3, 4 and 9 of three launches) and take them again 15 (3.5, 8 and 4), a fork of 32 instances 9.8, of 512 15.  Many instances and large pools
+// are behind steps that go one after the other: 8064 instances 50 (resize) and 87 (fork), and a pool of 24 million pages in use but for its last hundred
+// 223 us, as 64 workgroups read its counts; with the first hundred free 30.
 #include "cache_body.h"
 #include "share_internal.h"
 
@@ -45,8 +48,7 @@ __device__ __forceinline__ int lanes_before(unsigned long long mask) {
 template <int LANES> __device__ __forceinline__ unsigned long long ballot_of(bool x) {      // over the instance's lanes
   return __ballot(x) & (LANES == 64 ? ~0ull : 0xffffffffull << (threadIdx.x & 32));
 }
-// One less entry that names the page, of every lane with `some`: returns how many pages are free now.  seg follows, an addition for each segment that
-// lanes have: additions to one word wait for each other.
+// Adds to seg, of the page of every lane with `some`: an addition for each segment that lanes have, as additions to one word wait for each other.
 __device__ __forceinline__ void add_by_segment(const Pages& p, bool some, int page, int by) {
   unsigned long long todo = __ballot(some);
   const int s = page / kSegment;
@@ -57,7 +59,7 @@ __device__ __forceinline__ void add_by_segment(const Pages& p, bool some, int pa
     todo &= ~same;
   }
 }
-// U of them, whose counts are asked for together.
+// Adds to the counts of U pages of every lane with `some`, which are asked for together: returns how many were `border` before.  seg follows.
 template <int LANES, int U> __device__ __forceinline__ int change_pages(const Pages& p, const bool (&some)[U], const int (&page)[U], int by, int border) {
   int was[U], n = 0;
 #pragma unroll
@@ -70,6 +72,7 @@ template <int LANES, int U> __device__ __forceinline__ int change_pages(const Pa
   }
   return n;
 }
+// One less entry that names the page: returns how many pages are free now.
 template <int LANES, int U> __device__ __forceinline__ int drop_pages(const Pages& p, const bool (&some)[U], const int (&page)[U]) {
   return change_pages<LANES, U>(p, some, page, -1, 1);
 }
@@ -527,7 +530,7 @@ __global__ __launch_bounds__(kThreads) void fork_apply_kernel(ForkArgs a) {
   add_free(fork_apply<kThreads>(a, j, L, at<int32_t>(a.ws, a.w.need)[j], at<int32_t>(a.ws, a.w.before)[j], threadIdx.x), &s_free, a.info);
 }
 
-// As pick_pages, by one workgroup for kSmallInstances instances and kSmallSegments segments at most: what is loaded is asked for together.
+// As pages_pick_kernel, by one workgroup for kSmallInstances instances and kSmallSegments segments at most: what is loaded is asked for together.
 // need, before: in LDS.
 __device__ __forceinline__ void pick_by_one(const Pages& p, char* ws, const PagesWs& w, const Need* need, int* before, int* info, int* s_wave) {
   __shared__ int s_needed, s_sums[kSmallSegments / 64];

@@ -70,10 +70,11 @@ static ap::Pages pages_of(const Shape& s, void* K, void* V, int32_t* table, int3
 }
 
 // Chunks of so few rows of q that reading rows in common once is sooner than the prefill's tiles over every instance's own: an instance's rows are a
-// wave's (kNarrowRows), and for fp32, where the prefill's product is slow, twice that.  Measured against the prefill, 8 KV heads, d = 128, behind a
-// beginning of 6000 tokens, 16 and 128 sequences, 8, 32, 64, 128 rows: bf16 30, 47, 62, 98 us (60, 59, 63, 72) and 71, 183, 310, 607 (358, 370, 389,
-// 423), 48 rows 82 (61) and 370 (379); fp32 60, 203, 248, 468 (411, 418, 425, 434) and 287, 1314, 1749, 3359 (3102, 3119, 3133, 3148).  And all rows
-// are numbered in 32 bits, and their pieces.
+// wave's (kNarrowRows), and for fp32, where the prefill's product is slow, twice that.  Measured against the prefill, 8 KV heads, g = 4, d = 128, behind a
+// beginning of 6000 tokens in pages that all share, by 8, 32, 48, 64, 128 rows of q: bf16, 16 sequences 29, 49, 55, 66, 100 us (the prefill 60, 62, 65, 66, 76), 128
+// sequences 65, 172, 242, 319, 624 (356, 364, 375, 374, 412); fp32, 16 sequences 63, 174, 186, 237, 450 (378, 391, 396, 397, 414), 128 sequences 257, 1355, 1261, 1676, 3550
+// (2974, 2993, 2998, 2998, 3038).  (bf16 chunks of 33 to 64 rows would be sooner by groups where many sequences share.)  And all rows are numbered in 32
+// bits, and their pieces.
 static bool few_rows(const Shape& s, int32_t q_cap) {
   return q_cap * s.g <= (s.kv_dtype == AP_BF16 ? 1 : 2) * ap::kNarrowRows && ap::shared_pieces(s, q_cap) < (size_t)1 << 31;
 }

@@ -19,7 +19,7 @@ inline int page_segments(int n_pages) { return (int)(((long long)n_pages + kSegm
 // Workspace of the calls on pages, in bytes.  What a call needs is decided first (need, staged, kept, length), then free pages are picked
 // (before, picked, taken), then all is carried out.
 struct PagesWs {
-  size_t head;             // 4 words: pages needed, pages lacking; pages in use, pages to move
+  size_t head;             // 4 words: pages given out (0 where some lack), pages lacking; pages in use, pages to move
   size_t need;             // int32 [n_inst] pages needed
   size_t before;           // int32 [n_inst] pages needed by the instances before
   size_t length;           // int32 [n_inst] rows from now on (fork), -1: stays as it is
