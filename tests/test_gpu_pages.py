@@ -269,3 +269,34 @@ def test_the_longest_list_of_pages():
         assert rc == 0
         torch.cuda.synchronize()
         assert torch.equal(on[0], want[0]) and torch.equal(on[1], want[1])
+
+
+def test_copies_follow_lists_in_a_graph():
+    """Captured copies to other pages, to pinned memory and back, replayed with lists and pages that change."""
+    import paper_2502_04077_amd as ap
+    ctx = Device(ap, _pool(2, 2, 3, 16, 128, "bf16", 1), 32, 128).ctx
+    K, V, K2, V2 = (torch.zeros((40, 16, 128), dtype=torch.bfloat16, device="cuda:0") for _ in range(4))
+    host = [torch.zeros((10, 16, 128), dtype=torch.bfloat16, pin_memory=True) for _ in range(2)]
+    src, dst = (torch.zeros(10, dtype=torch.int32, device="cuda:0") for _ in range(2))
+
+    def calls():
+        ctx.pages_copy(K, V, src, *host, None)
+        ctx.pages_copy(*host, None, K2, V2, dst)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    gen = torch.Generator().manual_seed(4)
+    for _ in range(4):
+        for x in (K, V, K2, V2):
+            x.copy_(torch.randn(x.shape, generator=gen).to(torch.bfloat16))
+        src.copy_(torch.randperm(40, generator=gen)[:10])
+        dst.copy_(torch.randperm(40, generator=gen)[:10])
+        want = K2.clone(), V2.clone()
+        for x, y in zip(want, (K, V)):
+            x[dst.long()] = y[src.long()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(K2, want[0]) and torch.equal(V2, want[1])
+        assert torch.equal(host[0], K[src.long()].cpu()) and torch.equal(host[1], V[src.long()].cpu())
