@@ -9,8 +9,8 @@
 // K q^T and V^T P^T: a lane then has scores, statistics and outputs of one query row, and the scores' registers are the second product's
 // operand as they are, since the order of its contraction index is free.  V^T comes out of LDS by the transposing read.
 //
-// A prompt of 8190 tokens (8 instances, g = 4, d = 128) takes 556 us, 990 TFLOP/s of useful products, where a large library product
-// reaches 1210.  What bounds it is the vector unit beside the matrix unit: a wave's tile has 32 exponentials and some 170 other instructions a
+// A prompt of 8190 tokens (8 instances, g = 4, d = 128) takes 535 to 565 us (cards differ), 970 to 1030 TFLOP/s of useful products, where a large library
+// product reaches 1210.  What bounds it is the vector unit beside the matrix unit: a wave's tile has 32 exponentials and some 170 other instructions a
 // lane for its 32 matrix instructions, some 1180 cycles and 1024, and a SIMD's two waves hardly cover each other - the cycles of both units
 // add up to nearly all of the time -, and the clock, which falls to 1.8 GHz under it.  Tried and no faster: the next tile's scores beside
 // this one's exponentials, three waves a SIMD with tiles of 32 rows, 256 rows a workgroup, a higher priority for the matrix phases.
